@@ -217,7 +217,8 @@ def run(st):
 def _linear_own(st):
     from paper_2502_06786_b200 import binding as mq
     mq.quantize_tokens(st["x"], xq=st["xq"], scale=st["scale"], rowsum=st["rowsum"])
-    mq.gemm_a8(st["xq"], st["scale"], st["rowsum"], st["codes"], st["alpha"], st["zero"], y=st["y"])
+    mq.gemm_a8(st["xq"], st["scale"], st["rowsum"], st["codes"], st["alpha"], st["zero"], y=st["y"],
+               flags=mq.GEMV_PDL)                                       # the call before writes no weights
     return st["xq"], st["scale"], st["y"]
 
 

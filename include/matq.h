@@ -50,7 +50,9 @@ enum matq_status {
     /* written to dev_status by kernels */
     MATQ_ERR_NONFINITE = 8,    /* a weight is NaN or +-Inf */
     MATQ_ERR_CAPACITY = 9,     /* extra-precision overflow list does not fit ovf_capacity */
-    MATQ_ERR_TIMEOUT = 10      /* a bounded device-side wait gave up */
+    MATQ_ERR_TIMEOUT = 10,     /* a bounded device-side wait gave up */
+    MATQ_ERR_PAGE = 11         /* paged cache: a page number outside [0, n_pages), a sequence longer than its page-table row,
+                                  a position outside the rotation table, or cu_q / kv_len that contradict one another */
 };
 
 /* Where matq_gemm_multi takes the weights from. */
@@ -358,6 +360,120 @@ int matq_gemm_multi_test_stall(int on);
  * does not take (K % 16 != 0, K > 16384, 2^31 codes or more) have no device-side wait and ignore it.
  */
 int matq_slice_pack_test_stall(int on);
+
+/*
+ * ---- Serving a chunk of new tokens next to the nested planes: entry points (6) to (9). ----
+ * A prompt (or any batch with too many tokens for the decode GEMV) goes through a linear layer in 8-bit integers, (6) and (7);
+ * its keys and values go into a paged cache, (8); its queries attend to that cache, (9).
+ */
+
+/*
+ * (6) Activations to 8 bits, one symmetric scale per token (row):
+ *       scale_m   = max( max_k |X[m,k]| / 127, 2^-126 )
+ *       xq[m,k]   = clamp( round_half_even( X[m,k] / scale_m ), -127, 127 )
+ *       rowsum_m  = sum_k xq[m,k]
+ *     Both divisions are IEEE binary32, correctly rounded: the codes are defined bit for bit.
+ *   X        in   bf16 [M, K], row stride ldx elements        xq  out  int8 [M, K], row stride ldq bytes
+ *   scale    out  fp32 [M]                                    rowsum  out  int32 [M]
+ *   A row that holds NaN or Inf sets dev_status = MATQ_ERR_NONFINITE and gets scale NaN, codes 0, sum 0, so that its outputs in
+ *   (7) are NaN and no other row is touched.
+ *   Requires K % 16 == 0, 16 <= K <= 65536, ldx % 8 == 0, ldq % 16 == 0, X and xq 16-byte aligned.
+ */
+int matq_quantize_tokens(const void *X, int64_t M, int64_t K, int64_t ldx,
+                         int8_t *xq, int64_t ldq, float *scale, int32_t *rowsum,
+                         int32_t *dev_status, void *stream);
+
+/* Type of the outputs of (7). */
+enum matq_out_type { MATQ_OUT_F32 = 0, MATQ_OUT_BF16 = 1 };
+
+/*
+ * (7) Dense linear layer on 8-bit codes with 8-bit activations (prompt processing, batches of any size):
+ *       Y[m,n] = xscale_m * alpha_n * ( sum_k xq[m,k] * q[n,k]  -  z_n * sum_k xq[m,k] )
+ *     i.e. xscale_m xq . dequant(q)^T with dequantisation alpha * (q - z).  The products are summed exactly, as 32-bit integers
+ *     on the tensor cores; 128 * rowsum is taken off in integers too (z lies near 128 for weights around zero), and what
+ *     follows is fp32, rounded once more to bf16 when out_type asks for it.  The result does not depend on the launch shape.
+ *   xq, xscale, xsum   in   as written by (6); xq row stride ldxq bytes
+ *   q            in   uint8 [N, K], row stride ldw bytes: the codes of (1), or a slice S(q, r) of them for a nested
+ *                     precision (matq_slice_pack's sliced_unpacked; dequantisation is alpha * (S - z) either way)
+ *   alpha, zero  in   fp32 [N]
+ *   Y            out  fp32 or bf16 [M, N], row stride ldy elements
+ *   flags        0 or MATQ_GEMV_PDL (the previous kernel of the stream writes neither q nor alpha nor zero: the kernel then
+ *                     starts fetching weights before that kernel has ended, as in matq_gemv)
+ *   c must be 8.  Requires K % 16 == 0, 16 <= K <= 65536, ldxq % 16 == 0, ldw % 16 == 0, xq and q 16-byte aligned, M and N below 2^31;
+ *   any M, N >= 0.  A device-side wait that runs out sets dev_status = MATQ_ERR_TIMEOUT; Y is then unspecified.
+ */
+int matq_gemm_a8(const int8_t *xq, int64_t M, int64_t K, int64_t ldxq, const float *xscale, const int32_t *xsum,
+                 const uint8_t *q, int64_t N, int64_t ldw, int c, const float *alpha, const float *zero,
+                 int out_type, void *Y, int64_t ldy, unsigned flags,
+                 int32_t *dev_status, void *stream);
+
+/*
+ * A paged cache of keys and values and the batch of sequences that uses it.  (8) writes it and (9) reads it through the same
+ * descriptor.  Sequence b has n_b = cu_q[b+1] - cu_q[b] new tokens in this call, rows cu_q[b] .. of the token arrays, and
+ * kv_len[b] keys in all, the new ones last: new token i of it stands at position p = kv_len[b] - n_b + i.  The key of position p is in
+ * page page_table[b * table_stride + p / page_size], slot p % page_size.
+ * The struct itself is HOST memory, read during the call only; the pointers in it are DEVICE pointers.
+ */
+typedef struct matq_paged_kv {
+    void *k, *v;                 /* bf16 [n_pages, kv_heads, page_size, head_dim], contiguous, 16-byte aligned */
+    int64_t n_pages;
+    int page_size, kv_heads, head_dim;
+    int batch;                   /* sequences */
+    const int32_t *page_table;   /* int32 [batch, table_width], rows table_stride entries apart; entries past a sequence's last page are not read */
+    int64_t table_stride, table_width;
+    const int32_t *cu_q;         /* int32 [batch + 1], cu_q[0] = 0, ascending; a sequence may have no new token */
+    const int32_t *kv_len;       /* int32 [batch]: keys per sequence, the new tokens included */
+} matq_paged_kv;
+
+/*
+ * (8) Appends the new tokens' keys and values to the cache and rotates keys and queries by their positions on the way.
+ *     With rot = rot_dim, the pair (a, b) of elements (i, i + rot/2) (or (2i, 2i+1) when `interleaved`), i < rot/2, at position p becomes
+ *       ( a cos_p[i] - b sin_p[i],  b cos_p[i] + a sin_p[i] )
+ *     in fp32, rounded once; elements rot .. head_dim - 1 and all values are copied.
+ *   cos_sin  in   fp32 [max_pos, rot_dim]: row p holds cos_p[0 .. rot/2), sin_p[0 .. rot/2); may be NULL when rot_dim == 0
+ *   q        in   bf16 [T, q_heads, head_dim], token stride ldq elements (heads of a token adjacent); may be NULL with q_out NULL
+ *   k, v     in   bf16 [T, kv_heads, head_dim], token strides ldk, ldv
+ *   q_out    out  bf16 [T, q_heads, head_dim], token stride ldqo; may be q itself (with ldqo == ldq)
+ *   T        rows of the token arrays.  Rows from cu_q[batch] on belong to no sequence: they are neither read nor written.
+ *   Requires head_dim % 8 == 0, rot_dim % 16 == 0, rot_dim <= head_dim, every pointer 16-byte aligned, every stride a multiple of 8; any page_size >= 1.
+ *   A token whose position, page or table index is out of range sets dev_status = MATQ_ERR_PAGE; neither its key and value
+ *   nor its q_out are written.
+ */
+int matq_kv_append(const matq_paged_kv *cache, int64_t T, const void *q, int q_heads, int64_t ldq,
+                   const void *k, int64_t ldk, const void *v, int64_t ldv,
+                   const float *cos_sin, int64_t max_pos, int rot_dim, int interleaved,
+                   void *q_out, int64_t ldqo, int32_t *dev_status, void *stream);
+
+/*
+ * (9) Attention of the new tokens over the paged cache: for the query at position p of its sequence, head h, and the keys
+ *     J = { j : max(0, p - window + 1) <= j <= p } of key head h / (q_heads / kv_heads),
+ *       s_j = scale * q . k_j,   s_j <- softcap * tanh(s_j / softcap) if softcap > 0,   out = sum_J softmax(s)_j v_j.
+ *     One call serves single tokens, a few drafted tokens and whole chunks, in any mix.  Scores, maxima, sums and accumulators
+ *     are fp32; the weights are rounded to bf16 for the product with v.  Keys outside J contribute nothing whatever the cache holds there (NaN and Inf
+ *     included).  A query with empty J (kv_len smaller than the number of new tokens, as for padding) gives zeros.
+ *   q       in   bf16 [T, q_heads, head_dim], token stride ldq;  out  bf16 likewise, ldo.  Rows from cu_q[batch] on are left alone.
+ *   window  0 = every earlier key
+ *   max_q, max_kv   upper bounds of n_b and kv_len[b] that the caller knows on the host.  They choose the kernel and the split over
+ *           keys; values that are too small cost time, not correctness.
+ *   workspace   at least matq_attn_paged_workspace_bytes(...) bytes, 16-byte aligned; contents need not be initialised
+ *   Requires head_dim in {64, 128, 256}, page_size in {16, 32, 64, 128, 256}, q_heads a multiple of kv_heads with at most 64 query heads per
+ *   key head, 16-byte aligned pointers, strides multiples of 8, n_pages * kv_heads * page_size < 2^31.
+ *   Data errors set dev_status: MATQ_ERR_PAGE (the affected sequence's outputs are unspecified, no memory outside the cache is read) or
+ *   MATQ_ERR_TIMEOUT (a device-side wait gave up; outputs unspecified).
+ */
+size_t matq_attn_paged_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim,
+                                       int64_t max_q, int64_t max_kv, int64_t window);
+int matq_attn_paged(const matq_paged_kv *cache, int64_t T, const void *q, int q_heads, int64_t ldq,
+                    float scale, float softcap, int64_t window, int64_t max_q, int64_t max_kv,
+                    void *out, int64_t ldo, void *workspace, size_t workspace_bytes,
+                    int32_t *dev_status, void *stream);
+
+/*
+ * Testing hook for the error paths of (7) and (9), as matq_gemm_multi_test_stall: while `on` is non-zero their kernels issue no
+ * copies and their waits give up after about a millisecond; a call reports MATQ_ERR_TIMEOUT through dev_status, returns, and leaves the
+ * GPU ready for the next.  Process-wide; returns the previous setting.
+ */
+int matq_serving_test_stall(int on);
 
 #ifdef __cplusplus
 }

@@ -17,8 +17,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libmatq.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_SHAPE, ERR_ALIGNMENT = 0, 1, 2, 3, 4
-ERR_WORKSPACE, ERR_CUDA, ERR_NONFINITE, ERR_CAPACITY, ERR_TIMEOUT = 5, 6, 8, 9, 10
+ERR_WORKSPACE, ERR_CUDA, ERR_NONFINITE, ERR_CAPACITY, ERR_TIMEOUT, ERR_PAGE = 5, 6, 8, 9, 10, 11
 SRC_BF16, SRC_CODES8, SRC_PACKED = 0, 1, 2
+OUT_F32, OUT_BF16 = 0, 1
 GEMV_AUTO, GEMV_CUDA_CORE, GEMV_TENSOR, GEMV_TCGEN05, GEMV_TENSOR_INT8, GEMV_STREAM, GEMV_PDL = 0, 1, 2, 3, 4, 5, 0x100
 GEMV_TEST_STALL = 0x8000
 TEACHER_AND_TARGET = 256    # matq_gemm_multi_loss: teacher[i] = TEACHER_AND_TARGET + j
@@ -28,7 +29,9 @@ EXPORTS = ["matq_status_string", "matq_version", "matq_packed_row_bytes", "matq_
            "matq_gemm_multi_workspace_bytes", "matq_gemm_multi",
            "matq_gemm_multi_loss_workspace_bytes", "matq_gemm_multi_loss",
            "matq_gemm_multi_test_stall", "matq_slice_pack_test_stall",
-           "matq_gemm_multi_static_max_bytes", "matq_gemm_multi_static"]
+           "matq_gemm_multi_static_max_bytes", "matq_gemm_multi_static",
+           "matq_quantize_tokens", "matq_gemm_a8", "matq_kv_append", "matq_attn_paged_workspace_bytes", "matq_attn_paged",
+           "matq_serving_test_stall"]
 
 
 class GemvProblem(C.Structure):
@@ -36,6 +39,13 @@ class GemvProblem(C.Structure):
     _fields_ = [("packed", C.c_void_p), ("N", C.c_int64), ("K", C.c_int64), ("r", C.c_int),
                 ("alpha", C.c_void_p), ("zero", C.c_void_p), ("ovf_row_ptr", C.c_void_p), ("ovf_col", C.c_void_p),
                 ("x", C.c_void_p), ("y", C.c_void_p), ("B", C.c_int64)]
+
+
+class PagedKv(C.Structure):
+    """matq_paged_kv."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int64), ("page_size", C.c_int), ("kv_heads", C.c_int),
+                ("head_dim", C.c_int), ("batch", C.c_int), ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int64),
+                ("cu_q", C.c_void_p), ("kv_len", C.c_void_p)]
 
 
 class MatqError(RuntimeError):
@@ -91,6 +101,19 @@ def _load():
     lib.matq_gemm_multi_static.restype = i32
     lib.matq_gemm_multi_static.argtypes = [i32, vp, i64, i64, i32, vp, vp, i32, vp, vp, vp, i64, i64,
                                            C.POINTER(C.c_int), i32, C.POINTER(C.c_void_p), i64, vp, vp]
+    f32 = C.c_float
+    lib.matq_quantize_tokens.restype = i32
+    lib.matq_quantize_tokens.argtypes = [vp, i64, i64, i64, vp, i64, vp, vp, vp, vp]
+    lib.matq_gemm_a8.restype = i32
+    lib.matq_gemm_a8.argtypes = [vp, i64, i64, i64, vp, vp, vp, i64, i64, i32, vp, vp, i32, vp, i64, u32, vp, vp]
+    lib.matq_kv_append.restype = i32
+    lib.matq_kv_append.argtypes = [C.POINTER(PagedKv), i64, vp, i32, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp, i64, vp, vp]
+    lib.matq_attn_paged_workspace_bytes.restype = sz
+    lib.matq_attn_paged_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i64, i64]
+    lib.matq_attn_paged.restype = i32
+    lib.matq_attn_paged.argtypes = [C.POINTER(PagedKv), i64, vp, i32, i64, f32, f32, i64, i64, i64, vp, i64, vp, sz, vp, vp]
+    lib.matq_serving_test_stall.restype = i32
+    lib.matq_serving_test_stall.argtypes = [i32]
     return lib
 
 
@@ -396,3 +419,144 @@ def gemm_multi_static(src_kind, Wsrc, K, X, Ys, alpha, zero, rs=(8, 4, 2), extra
                                      _ptr(ovf_row_ptr), _ptr(ovf_col), _ptr(X), M, _ld(X, K), rs_arr, len(rs),
                                      y_arr, _ld(Ys[0], N), _ptr(dev_status), _stream())
     return _check(st, "matq_gemm_multi_static", raise_on_error)
+
+
+def quantize_tokens(X, xq=None, scale=None, rowsum=None, dev_status=None):
+    """matq_quantize_tokens.  X: bf16 [M, K].  Returns (xq int8 [M, K], scale fp32 [M], rowsum int32 [M])."""
+    _dev(X, torch.bfloat16, "X", 2)
+    if X.stride(1) != 1:
+        raise ValueError("X: unit stride along K required")
+    M, K = X.shape
+    if xq is None:
+        xq = torch.empty((M, K), dtype=torch.int8, device=X.device)
+    if scale is None:
+        scale = torch.empty(M, dtype=torch.float32, device=X.device)
+    if rowsum is None:
+        rowsum = torch.empty(M, dtype=torch.int32, device=X.device)
+    _dev(xq, torch.int8, "xq", 2); _vector(scale, torch.float32, "scale", M); _vector(rowsum, torch.int32, "rowsum", M)
+    if tuple(xq.shape) != (M, K) or xq.stride(1) != 1:
+        raise ValueError("xq: int8 [M, K] with unit stride along K required")
+    st = _lib.matq_quantize_tokens(_ptr(X), M, K, _ld(X, K), _ptr(xq), _ld(xq, K), _ptr(scale), _ptr(rowsum),
+                                   _ptr(dev_status), _stream())
+    _check(st, "matq_quantize_tokens")
+    return xq, scale, rowsum
+
+
+def _vector(t, dtype, name, n):
+    _dev(t, dtype, name, 1)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous, {n} elements required")
+    return t
+
+
+def gemm_a8(xq, scale, rowsum, q, alpha, zero, y=None, out_dtype=torch.float32, flags=0, dev_status=None, c=8):
+    """matq_gemm_a8.  xq, scale, rowsum: as returned by quantize_tokens; q: uint8 [N, K] codes or a slice of them (unpacked).
+    Returns y [M, N], fp32 or bf16 (the type of ``y`` when it is given, ``out_dtype`` otherwise)."""
+    _dev(xq, torch.int8, "xq", 2); _dev(q, torch.uint8, "q", 2)
+    M, K = xq.shape
+    N = q.shape[0]
+    if q.shape[1] != K or xq.stride(1) != 1 or q.stride(1) != 1:
+        raise ValueError("xq [M, K] and q [N, K] with unit stride along K required")
+    _vector(scale, torch.float32, "scale", M); _vector(rowsum, torch.int32, "rowsum", M)
+    _vector(alpha, torch.float32, "alpha", N); _vector(zero, torch.float32, "zero", N)
+    if y is None:
+        y = torch.empty((M, N), dtype=out_dtype, device=xq.device)
+    if y.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("y: fp32 or bf16 required")
+    _dev(y, y.dtype, "y", 2)
+    if tuple(y.shape) != (M, N) or y.stride(1) != 1:
+        raise ValueError("y: [M, N] with unit stride along N required")
+    st = _lib.matq_gemm_a8(_ptr(xq), M, K, _ld(xq, K), _ptr(scale), _ptr(rowsum), _ptr(q), N, _ld(q, K), c, _ptr(alpha), _ptr(zero),
+                           OUT_F32 if y.dtype == torch.float32 else OUT_BF16, _ptr(y), _ld(y, N), int(flags),
+                           _ptr(dev_status), _stream())
+    _check(st, "matq_gemm_a8")
+    return y
+
+
+def _paged(k_cache, v_cache, page_table, cu_q, kv_len):
+    _dev(k_cache, torch.bfloat16, "k_cache", 4); _dev(v_cache, torch.bfloat16, "v_cache", 4)
+    if k_cache.shape != v_cache.shape or not k_cache.is_contiguous() or not v_cache.is_contiguous():
+        raise ValueError("k_cache, v_cache: contiguous [n_pages, kv_heads, page_size, head_dim] of one shape required")
+    _dev(page_table, torch.int32, "page_table", 2)
+    B = page_table.shape[0]
+    if page_table.stride(1) != 1:
+        raise ValueError("page_table: unit stride along the pages required")
+    _vector(cu_q, torch.int32, "cu_q", B + 1); _vector(kv_len, torch.int32, "kv_len", B)
+    c = PagedKv()
+    c.k, c.v = k_cache.data_ptr(), v_cache.data_ptr()
+    c.n_pages, c.kv_heads, c.page_size, c.head_dim = k_cache.shape
+    c.batch, c.page_table, c.table_stride, c.table_width = B, page_table.data_ptr(), _ld(page_table, page_table.shape[1]), page_table.shape[1]
+    c.cu_q, c.kv_len = cu_q.data_ptr(), kv_len.data_ptr()
+    return c
+
+
+def _heads(t, name, heads, D):
+    _dev(t, torch.bfloat16, name, 3)
+    if (heads is not None and t.shape[1] != heads) or t.shape[2] != D or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != D):
+        raise ValueError(f"{name}: bf16 [T, heads, head_dim] with a token's heads adjacent required")
+    return t
+
+
+def kv_append(k_cache, v_cache, page_table, cu_q, kv_len, k, v, cos_sin=None, q=None, q_out=None, interleaved=False, dev_status=None):
+    """matq_kv_append.  k_cache, v_cache: bf16 [n_pages, kv_heads, page_size, head_dim]; page_table: int32 [B, pages]; cu_q: int32
+    [B + 1]; kv_len: int32 [B], the new tokens included; k, v: bf16 [T, kv_heads, head_dim]; cos_sin: fp32 [max_pos, rot_dim] or None (no
+    rotation); q: bf16 [T, q_heads, head_dim] or None.  Writes the caches; returns q_out (pass q itself to rotate in place)."""
+    cache = _paged(k_cache, v_cache, page_table, cu_q, kv_len)
+    Hkv, D = cache.kv_heads, cache.head_dim
+    T = k.shape[0]
+    _heads(k, "k", Hkv, D); _heads(v, "v", Hkv, D)
+    if v.shape[0] != T:
+        raise ValueError("k and v: one row per token each")
+    max_pos = rot = 0
+    if cos_sin is not None:
+        _dev(cos_sin, torch.float32, "cos_sin", 2)
+        if not cos_sin.is_contiguous():
+            raise ValueError("cos_sin: contiguous [max_pos, rot_dim] required")
+        max_pos, rot = cos_sin.shape
+    if q is not None:
+        _heads(q, "q", None, D)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        _heads(q_out, "q_out", q.shape[1], D)
+        if q.shape[0] != T or q_out.shape[0] != T:
+            raise ValueError("q and q_out: one row per token each")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    st = _lib.matq_kv_append(C.byref(cache), T, _ptr(q), 0 if q is None else q.shape[1], 0 if q is None else _ld(q, q.shape[1] * D),
+                             _ptr(k), _ld(k, Hkv * D), _ptr(v), _ld(v, Hkv * D), _ptr(cos_sin), max_pos, rot, int(bool(interleaved)),
+                             _ptr(q_out), 0 if q is None else _ld(q_out, q.shape[1] * D), _ptr(dev_status), _stream())
+    _check(st, "matq_kv_append")
+    return q_out
+
+
+def attn_paged_workspace_bytes(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window=0) -> int:
+    return int(_lib.matq_attn_paged_workspace_bytes(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window))
+
+
+def attn_paged(q, k_cache, v_cache, page_table, cu_q, kv_len, max_q, max_kv, scale=None, softcap=0.0, window=0, out=None,
+               workspace=None, dev_status=None):
+    """matq_attn_paged.  q: bf16 [T, q_heads, head_dim]; the cache as in kv_append; max_q, max_kv: host-side upper bounds of the new
+    tokens and the keys of a sequence.  scale defaults to head_dim ** -0.5.  Returns out, bf16 [T, q_heads, head_dim]."""
+    cache = _paged(k_cache, v_cache, page_table, cu_q, kv_len)
+    Hkv, D = cache.kv_heads, cache.head_dim
+    _heads(q, "q", None, D)
+    T, Hq = q.shape[0], q.shape[1]
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=q.device)
+    _heads(out, "out", Hq, D)
+    if out.shape[0] != T:
+        raise ValueError("out: one row per token")
+    need = attn_paged_workspace_bytes(T, cache.batch, Hq, Hkv, D, max_q, max_kv, window)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    st = _lib.matq_attn_paged(C.byref(cache), T, _ptr(q), Hq, _ld(q, Hq * D), float(D ** -0.5 if scale is None else scale), float(softcap),
+                              int(window), int(max_q), int(max_kv), _ptr(out), _ld(out, Hq * D),
+                              _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                              _ptr(dev_status), _stream())
+    _check(st, "matq_attn_paged")
+    return out
+
+
+def serving_test_stall(on) -> int:
+    """matq_serving_test_stall: switch the "issue no copies" test mode of gemm_a8 and attn_paged; returns the previous setting."""
+    return int(_lib.matq_serving_test_stall(1 if on else 0))

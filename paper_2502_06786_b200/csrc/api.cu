@@ -15,6 +15,18 @@ extern "C" const char* matq_status_string(int status) {
         case MATQ_ERR_NONFINITE: return "non-finite weight";
         case MATQ_ERR_CAPACITY: return "overflow list capacity exceeded";
         case MATQ_ERR_TIMEOUT: return "device-side wait timed out";
+        case MATQ_ERR_PAGE: return "page, position or sequence bounds out of range";
         default: return "unknown status";
     }
 }
+
+// Tests of the error paths (matq_serving_test_stall): process-wide, read when a call builds its launch.
+static std::atomic<int> g_serving_stall{0};
+
+extern "C" int matq_serving_test_stall(int on) { return g_serving_stall.exchange(on ? 1 : 0); }
+
+namespace matq {
+namespace tc {
+bool test_stall() { return g_serving_stall.load(std::memory_order_relaxed) != 0; }
+}  // namespace tc
+}  // namespace matq

@@ -1,0 +1,112 @@
+// What the kernels of matq_attn_paged share: parameters, page lookup, the score function, the join of key splits.
+#pragma once
+
+#include "tc.cuh"
+
+namespace matq {
+namespace attn {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct Params {
+    const __nv_bfloat16* q;
+    __nv_bfloat16* out;
+    const int32_t *table, *cu_q, *kv_len;
+    int64_t ldq, ldo, table_stride, table_width, n_pages, T;
+    int64_t window;              // 0 = none
+    int batch, q_heads, kv_heads, group, page_size, page_shift;
+    int tiles_per_seq;           // row tiles that the grid holds per sequence (a sequence with more is walked in steps)
+    int splits;                  // parts of the key range
+    int64_t split_keys;          // keys per part, a multiple of the key tile; the last part takes what is left
+    float scale, softcap;
+    float* part_o;               // [splits][T * q_heads][D], not normalised; only with splits > 1
+    float2* part_ml;             // [splits][T * q_heads]: running maximum (of base-2 exponents) and sum
+    int32_t* dev_status;
+    long long wait_cycles;
+    int hold;
+};
+
+// Scores as exponents of two: p = 2^(value - maximum).  Without a cap that is one product; the cap's tanh is written with an
+// exponential, 1 - 2 / (1 + e^2x), whose absolute error stays at fp32's where x is small and saturates without overflow where it is large.
+struct Score {
+    float mul, cap2;             // cap2 = softcap * log2(e); 0 without a cap
+    __device__ __forceinline__ Score(float scale, float softcap) {
+        mul = softcap > 0.f ? scale / softcap * (2.f * kLog2e) : scale * kLog2e;
+        cap2 = softcap > 0.f ? softcap * kLog2e : 0.f;
+    }
+};
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float capped(float s, float mul, float cap2) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(s * mul)));
+    return fmaf(-2.f * r, cap2, cap2);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&h);
+}
+__device__ __forceinline__ bool nonfinite_bf16(uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u; }
+
+// First row, in the cache seen as rows of D elements, of the slots that hold keys key .. of sequence b, head h.  A page number that is out of
+// range gives a row past the end, which reads as zeros, and is reported.
+__device__ __forceinline__ int cache_row(const Params& P, int b, int h, int64_t key, int64_t kv_len) {
+    const int64_t last = P.n_pages * P.kv_heads * P.page_size;
+    if (key >= kv_len) return (int)last;
+    const int64_t pg = key >> P.page_shift;
+    int64_t page = -1;
+    if (pg < P.table_width) page = P.table[(int64_t)b * P.table_stride + pg];
+    if (page < 0 || page >= P.n_pages) {
+        report(P.dev_status, MATQ_ERR_PAGE);
+        return (int)last;
+    }
+    return (int)((page * P.kv_heads + h) * P.page_size + (key & (P.page_size - 1)));
+}
+
+// Joins the parts of the key range: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s, the parts in their order.  One warp per (token, head).
+template <int D>
+__global__ void __launch_bounds__(128) attn_join_kernel(const Params P) {
+    after_previous_kernel();
+    let_next_kernel_start();
+    const int lane = threadIdx.x & 31;
+    const int64_t rows = P.T * P.q_heads, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const int64_t t = row / P.q_heads;
+    if (t >= P.cu_q[P.batch]) return;
+    constexpr int kV = D / 64;                                         // float2 pieces per lane
+    float mx = -INFINITY;
+    for (int s = lane; s < P.splits; s += 32) mx = fmaxf(mx, P.part_ml[(int64_t)s * rows + row].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    float2 acc[kV];
+#pragma unroll
+    for (int j = 0; j < kV; ++j) acc[j] = make_float2(0.f, 0.f);
+    float sum = 0.f;
+    bool any = false;
+    for (int s = 0; s < P.splits; ++s) {
+        const float2 ml = P.part_ml[(int64_t)s * rows + row];
+        if (ml.y == 0.f && ml.x == -INFINITY) continue;                 // a part without keys for this row
+        any = true;
+        const float w = mx == -INFINITY ? 0.f : ex2(ml.x - mx);
+        sum = fmaf(ml.y, w, sum);
+        const float2* o = reinterpret_cast<const float2*>(P.part_o + ((int64_t)s * rows + row) * D);
+#pragma unroll
+        for (int j = 0; j < kV; ++j) {
+            const float2 v = o[lane + 32 * j];
+            acc[j].x = fmaf(v.x, w, acc[j].x);
+            acc[j].y = fmaf(v.y, w, acc[j].y);
+        }
+    }
+    const float inv = any ? 1.f / sum : 0.f;
+    const int h = (int)(row - t * P.q_heads);
+    uint32_t* dst = reinterpret_cast<uint32_t*>(P.out + t * P.ldo + (int64_t)h * D);
+#pragma unroll
+    for (int j = 0; j < kV; ++j) dst[lane + 32 * j] = any ? pack_bf16(acc[j].x * inv, acc[j].y * inv) : 0u;
+}
+
+}  // namespace attn
+}  // namespace matq

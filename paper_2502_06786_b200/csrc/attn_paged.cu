@@ -1,0 +1,111 @@
+// matq_attn_paged: attention of new tokens over a paged cache (argument checks, choice of kernel and split).
+#include "attn_decode.cuh"
+
+namespace matq {
+namespace attn {
+
+struct Plan {
+    int64_t tiles_per_seq, splits, split_keys;
+};
+
+// Parts of the key range: enough CTAs to fill the GPU, but at least 256 keys (four stages) per part.
+inline Plan plan(int batch, int kv_heads, int group, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
+    Plan p;
+    const int64_t rows = max_q * group;
+    p.tiles_per_seq = (rows + kDecRows - 1) / kDecRows;
+    if (p.tiles_per_seq < 1) p.tiles_per_seq = 1;
+    int64_t range = max_kv;
+    if (window > 0 && window + kDecRows < range) range = window + kDecRows;
+    range = (range + kDecKeys - 1) / kDecKeys + 1;                      // stages; one more when the window starts inside one
+    const int64_t ctas = p.tiles_per_seq * batch * kv_heads;
+    int64_t splits = ctas > 0 ? (4 * sms + ctas - 1) / ctas : 1;
+    if (splits > range / 4) splits = range / 4;
+    if (splits < 1) splits = 1;
+    int64_t per = (range + splits - 1) / splits;
+    p.splits = (range + per - 1) / per;
+    p.split_keys = per * kDecKeys;
+    return p;
+}
+
+inline size_t part_bytes(int64_t T, int q_heads, int D, int64_t splits) {
+    return splits > 1 ? (size_t)splits * T * q_heads * (D + 2) * sizeof(float) : 0;
+}
+
+inline bool cache_map(CUtensorMap* tm, const void* base, int64_t rows, int D, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)D * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    return tc::make_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box);
+}
+
+template <int D>
+int launch_decode(const CUtensorMap& tk, const CUtensorMap& tv, const Params& P, cudaStream_t s) {
+    static std::atomic<unsigned long long> smem_ok{0};
+    if (!opt_in_max_smem(attn_decode_kernel<D>, smem_ok)) return MATQ_ERR_CUDA;
+    const int64_t grid = (int64_t)P.splits * P.kv_heads * P.batch * P.tiles_per_seq;
+    if (grid >= (1ll << 31)) return MATQ_ERR_SHAPE;
+    if (launch_overlapped(attn_decode_kernel<D>, dim3((unsigned)grid), dim3(kDecThreads), DecCfg<D>::kSmem, s, tk, tv, P) != cudaSuccess) {
+        cudaGetLastError();
+        return MATQ_ERR_CUDA;
+    }
+    if (P.splits > 1) {
+        const int64_t blocks = (P.T * P.q_heads + 3) / 4;
+        if (blocks >= (1ll << 31)) return MATQ_ERR_SHAPE;
+        if (launch_overlapped(attn_join_kernel<D>, dim3((unsigned)blocks), dim3(128), 0, s, P) != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
+    }
+    return launch_status();
+}
+
+}  // namespace attn
+}  // namespace matq
+
+extern "C" size_t matq_attn_paged_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim,
+                                                  int64_t max_q, int64_t max_kv, int64_t window) {
+    using namespace matq::attn;
+    if (T <= 0 || batch <= 0 || q_heads <= 0 || kv_heads <= 0 || q_heads % kv_heads != 0 || head_dim <= 0) return 0;
+    const Plan p = plan(batch, kv_heads, q_heads / kv_heads, max_q, max_kv, window, matq::sm_count());
+    return part_bytes(T, q_heads, head_dim, p.splits);
+}
+
+extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap,
+                               int64_t window, int64_t max_q, int64_t max_kv, void* out, int64_t ldo, void* workspace,
+                               size_t workspace_bytes, int32_t* dev_status, void* stream) {
+    using namespace matq;
+    using namespace matq::attn;
+    if (!cache || T < 0 || q_heads < 1 || cache->batch < 0 || cache->n_pages < 0 || cache->kv_heads < 1 || cache->table_width < 0 || (cache->batch > 1 && cache->table_stride < cache->table_width) ||
+        window < 0 || max_q < 0 || max_kv < 0 || !(softcap >= 0.f) || !(scale == scale))
+        return MATQ_ERR_INVALID_ARG;
+    const int D = cache->head_dim, ps = cache->page_size;
+    if (D != 64 && D != 128 && D != 256) return MATQ_ERR_UNSUPPORTED;
+    if (ps != 16 && ps != 32 && ps != 64 && ps != 128 && ps != 256) return MATQ_ERR_UNSUPPORTED;
+    if (q_heads % cache->kv_heads != 0 || q_heads / cache->kv_heads > 64) return MATQ_ERR_UNSUPPORTED;
+    const int64_t w = (int64_t)q_heads * D, rows = cache->n_pages * cache->kv_heads * ps;
+    if (ldq < w || ldq % 8 != 0 || ldo < w || ldo % 8 != 0 || T >= (1ll << 31) || cache->n_pages >= (1ll << 31) || rows >= (1ll << 31)) return MATQ_ERR_SHAPE;
+    if (T == 0 || cache->batch == 0) return MATQ_OK;
+    if (!q || !out || !cache->k || !cache->v || !cache->page_table || !cache->cu_q || !cache->kv_len || cache->n_pages == 0) return MATQ_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(cache->k) || !aligned16(cache->v) || !aligned16(workspace)) return MATQ_ERR_ALIGNMENT;
+    const int group = q_heads / cache->kv_heads;
+    const Plan p = plan(cache->batch, cache->kv_heads, group, max_q, max_kv, window, sm_count());
+    if (part_bytes(T, q_heads, D, p.splits) > workspace_bytes || (p.splits > 1 && !workspace)) return MATQ_ERR_WORKSPACE;
+
+    Params P;
+    P.q = static_cast<const __nv_bfloat16*>(q); P.out = static_cast<__nv_bfloat16*>(out);
+    P.table = cache->page_table; P.cu_q = cache->cu_q; P.kv_len = cache->kv_len;
+    P.ldq = ldq; P.ldo = ldo; P.table_stride = cache->table_stride; P.table_width = cache->table_width; P.n_pages = cache->n_pages; P.T = T; P.window = window;
+    P.batch = cache->batch; P.q_heads = q_heads; P.kv_heads = cache->kv_heads; P.group = group;
+    P.page_size = ps; P.page_shift = ps == 16 ? 4 : ps == 32 ? 5 : ps == 64 ? 6 : ps == 128 ? 7 : 8;
+    P.tiles_per_seq = (int)p.tiles_per_seq; P.splits = (int)p.splits; P.split_keys = p.split_keys;
+    P.scale = scale; P.softcap = softcap;
+    P.part_o = static_cast<float*>(workspace);
+    P.part_ml = reinterpret_cast<float2*>(P.part_o + (size_t)p.splits * T * q_heads * D);
+    P.dev_status = dev_status;
+    P.hold = tc::test_stall() ? 1 : 0;
+    P.wait_cycles = P.hold ? tc::kStallWaitCycles : tc::kWaitCycles;
+    CUtensorMap tk, tv;
+    const int box = ps < kDecKeys ? ps : kDecKeys;
+    if (!cache_map(&tk, cache->k, rows, D, box) || !cache_map(&tv, cache->v, rows, D, box)) return MATQ_ERR_CUDA;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (D == 64) return launch_decode<64>(tk, tv, P, s);
+    if (D == 128) return launch_decode<128>(tk, tv, P, s);
+    return launch_decode<256>(tk, tv, P, s);
+}

@@ -1,0 +1,253 @@
+// matq_gemm_a8: Y[m,n] = xscale_m alpha_n ( sum_k xq[m,k] q[n,k] - z_n sum_k xq[m,k] ), the sums in 8-bit integers on the tensor cores.
+#include "tc.cuh"
+
+namespace matq {
+namespace a8 {
+
+constexpr int kThreads = 192;
+constexpr int kBM = 128;             // channels of a tile: the rows of the accumulator (tensor-memory lanes)
+constexpr int kBK = 128;             // bytes of K per stage: one 128-byte swizzle row
+constexpr int kMaxStages = 8;
+constexpr int kMaxNT = 256;
+
+struct Params {
+    const float *alpha, *zero, *xscale;
+    const int32_t* xsum;
+    void* Y;
+    int64_t M, N, ldy;
+    int nkb, nt, splits, stages, tmem_cols, bf16_out, early;
+    int32_t* dev_status;
+    long long wait_cycles;
+    int hold;
+};
+
+// kind::i8, D = s32, A = u8 (codes), B = s8 (activations), both K-major
+__device__ __forceinline__ uint32_t idesc_i8(int m, int n) {
+    return (2u << 4) | (0u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+__device__ __forceinline__ float finish(int acc, int xsum, float xs, float al, float zc) {
+    return (xs * al) * ((float)(acc - 128 * xsum) - zc * (float)xsum);
+}
+__device__ __forceinline__ void store_y(const Params& P, int64_t m, int64_t n, float y) {
+    if (P.bf16_out) static_cast<__nv_bfloat16*>(P.Y)[m * P.ldy + n] = __float2bfloat16_rn(y);
+    else static_cast<float*>(P.Y)[m * P.ldy + n] = y;
+}
+
+__global__ void __launch_bounds__(kThreads)
+gemm_a8_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const Params P) {
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_acc;
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_timeout;
+    __shared__ float s_xs[kMaxNT];
+    __shared__ int s_xsum[kMaxNT];
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int split = (int)(blockIdx.x % (unsigned)P.splits);            // rank in the cluster
+    const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)P.splits) * kBM, m0 = (int64_t)blockIdx.y * P.nt;
+    const int kb0 = (int)((int64_t)P.nkb * split / P.splits), kb1 = (int)((int64_t)P.nkb * (split + 1) / P.splits);
+    const int stage_bytes = kBM * kBK + P.nt * kBK;
+    unsigned char* ring = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
+
+    if (!P.early) after_previous_kernel();
+    if (tid == 0) {
+        for (int s = 0; s < P.stages; ++s) { tc::mbar_init(tc::smem_u32(&s_full[s]), 1); tc::mbar_init(tc::smem_u32(&s_empty[s]), 1); }
+        tc::mbar_init(tc::smem_u32(&s_acc), 1);
+        tc::mbar_init_fence();
+        s_timeout = 0;
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(&s_tmem)), "r"(P.tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = s_tmem;
+    let_next_kernel_start();
+
+    const int64_t n = n0 + (warp & 3) * 32 + lane;                      // epilogue warps: this thread's channel
+    float al = 0.f, zc = 0.f;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            // the weights of the first stages are fetched before the activations are known to be there
+            const int ahead = min(P.stages, kb1 - kb0);
+            if (!P.hold) {
+                for (int i = 0; i < ahead; ++i) {
+                    const uint32_t bar = tc::smem_u32(&s_full[i]);
+                    tc::mbar_expect_tx(bar, stage_bytes);
+                    tc::tma_load_2d(tc::smem_u32(ring + (size_t)i * stage_bytes), &tm_w, (kb0 + i) * kBK, (int)n0, bar);
+                }
+            }
+            if (P.early) after_previous_kernel();
+            int issued = 0;
+            for (int kb = kb0; kb < kb1 && !P.hold; ++kb) {
+                const int i = kb - kb0, s = i % P.stages;
+                const uint32_t bar = tc::smem_u32(&s_full[s]);
+                unsigned char* st = ring + (size_t)s * stage_bytes;
+                if (i >= ahead) {
+                    if (!tc::mbar_wait(tc::smem_u32(&s_empty[s]), ((uint32_t)(i / P.stages) & 1u) ^ 1u, P.wait_cycles)) { s_timeout = 1; break; }
+                    tc::mbar_expect_tx(bar, stage_bytes);
+                    tc::tma_load_2d(tc::smem_u32(st), &tm_w, kb * kBK, (int)n0, bar);
+                }
+                tc::tma_load_2d(tc::smem_u32(st + kBM * kBK), &tm_x, kb * kBK, (int)m0, bar);
+                issued = i + 1;
+            }
+            // no copy may be in flight when the CTA ends, whatever became of its consumer
+            for (int i = max(0, issued - P.stages); i < issued; ++i)
+                tc::mbar_wait(tc::smem_u32(&s_full[i % P.stages]), (uint32_t)(i / P.stages) & 1u, P.wait_cycles);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = idesc_i8(kBM, P.nt);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                const int i = kb - kb0, s = i % P.stages;
+                if (!tc::mbar_wait(tc::smem_u32(&s_full[s]), (uint32_t)(i / P.stages) & 1u, P.wait_cycles)) {
+                    *(volatile int*)&s_timeout = 1;
+                    __threadfence_block();
+                    break;
+                }
+                tc::fence_after();
+                const uint32_t a = tc::smem_u32(ring + (size_t)s * stage_bytes), b = a + kBM * kBK;
+#pragma unroll
+                for (int kk = 0; kk < kBK / 32; ++kk)
+                    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p; }"
+                                 ::"r"(tmem), "l"(tc::sw128_desc(a + kk * 32)), "l"(tc::sw128_desc(b + kk * 32)), "r"(idesc),
+                                   "r"((i > 0 || kk > 0) ? 1u : 0u) : "memory");
+                tc::tc_commit(tc::smem_u32(&s_empty[s]));
+            }
+            tc::tc_commit(tc::smem_u32(&s_acc));
+        }
+    } else {
+        if (n < P.N) { al = P.alpha[n]; zc = P.zero[n] - 128.f; }
+        if (P.early) after_previous_kernel();
+        for (int c = tid - 64; c < P.nt; c += 128) {
+            const bool in = m0 + c < P.M;
+            s_xs[c] = in ? P.xscale[m0 + c] : 0.f;
+            s_xsum[c] = in ? P.xsum[m0 + c] : 0;
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const bool done = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_acc), 0, P.wait_cycles)) && *(volatile int*)&s_timeout == 0;
+        if (!done) *(volatile int*)&s_timeout = 1;
+        tc::fence_after();
+        const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const int cols = (int)min((int64_t)P.nt, P.M - m0);
+        if (done) {
+            for (int c0 = 0; c0 < cols; c0 += 16) {
+                uint32_t d[16];
+                tc::tmem_ld16(lane_addr + c0, d);
+                tc::tmem_wait_ld();
+                if (P.splits == 1) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c0 + j < cols && n < P.N) store_y(P, m0 + c0 + j, n, finish((int)d[j], s_xsum[c0 + j], s_xs[c0 + j], al, zc));
+                } else {                                                // partial sums go where the stages were: [token][channel]
+                    int* part = reinterpret_cast<int*>(ring);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) part[(c0 + j) * kBM + (warp & 3) * 32 + lane] = (int)d[j];
+                }
+            }
+        }
+    }
+    if (P.splits > 1) {
+        // The CTAs of a cluster hold the same tile for different parts of K: each finishes every splits-th token.  Integer sums: the order is free.
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned; barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (warp >= 2) {
+            const int cols = (int)min((int64_t)P.nt, P.M - m0);
+            const uint32_t mine = tc::smem_u32(ring) + ((warp & 3) * 32 + lane) * 4;
+            bool ok = true;
+            for (int r = 0; r < P.splits; ++r) {
+                uint32_t a, t;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tc::smem_u32(&s_timeout)), "r"(r));
+                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(t) : "r"(a) : "memory");
+                ok &= t == 0;
+            }
+            for (int c = split; c < cols && ok; c += P.splits) {
+                int sum = 0;
+                for (int r = 0; r < P.splits; ++r) {
+                    uint32_t a, v;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(mine + c * kBM * 4), "r"(r));
+                    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+                    sum += (int)v;
+                }
+                if (n < P.N) store_y(P, m0 + c, n, finish(sum, s_xsum[c], s_xs[c], al, zc));
+            }
+        }
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned; barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    tc::fence_before();
+    __syncthreads();
+    if (tid == 0 && s_timeout) report(P.dev_status, MATQ_ERR_TIMEOUT);
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(P.tmem_cols) : "memory");
+}
+
+inline bool byte_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t K, int64_t ld, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {(cuuint32_t)kBK, (cuuint32_t)box_rows};
+    return tc::make_map(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box);
+}
+
+}  // namespace a8
+}  // namespace matq
+
+extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq, const float* xscale, const int32_t* xsum,
+                            const uint8_t* q, int64_t N, int64_t ldw, int c, const float* alpha, const float* zero,
+                            int out_type, void* Y, int64_t ldy, unsigned flags, int32_t* dev_status, void* stream) {
+    using namespace matq;
+    using namespace matq::a8;
+    if (M < 0 || N < 0 || K <= 0 || (out_type != MATQ_OUT_F32 && out_type != MATQ_OUT_BF16) || (flags & ~(unsigned)MATQ_GEMV_PDL)) return MATQ_ERR_INVALID_ARG;
+    if (c != kCodeBits) return MATQ_ERR_UNSUPPORTED;
+    if (K % 16 != 0 || K > 65536 || ldxq < K || ldxq % 16 != 0 || ldw < K || ldw % 16 != 0 || ldy < N || M >= (1ll << 31) || N >= (1ll << 31)) return MATQ_ERR_SHAPE;
+    if (M == 0 || N == 0) return MATQ_OK;
+    if (!xq || !xscale || !xsum || !q || !alpha || !zero || !Y) return MATQ_ERR_INVALID_ARG;
+    if (!aligned16(xq) || !aligned16(q)) return MATQ_ERR_ALIGNMENT;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+
+    Params P;
+    P.alpha = alpha; P.zero = zero; P.xscale = xscale; P.xsum = xsum; P.Y = Y; P.M = M; P.N = N; P.ldy = ldy;
+    P.bf16_out = out_type == MATQ_OUT_BF16;
+    P.early = (flags & MATQ_GEMV_PDL) ? 1 : 0;
+    P.dev_status = dev_status;
+    P.hold = tc::test_stall() ? 1 : 0;
+    P.wait_cycles = P.hold ? tc::kStallWaitCycles : tc::kWaitCycles;
+    P.nkb = (int)((K + kBK - 1) / kBK);
+    P.nt = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
+    P.tmem_cols = P.nt < 32 ? 32 : P.nt;
+    const int64_t n_tiles = (N + kBM - 1) / kBM, m_tiles = (M + P.nt - 1) / P.nt;
+    if (m_tiles > 65535) return MATQ_ERR_SHAPE;
+    const int sms = sm_count();
+    P.splits = 1;
+    while (P.nt <= 128 && P.splits < 8 && n_tiles * m_tiles * P.splits * 2 <= 2 * sms && P.nkb >= 4 * P.splits) P.splits *= 2;
+    const int stage_bytes = (kBM + P.nt) * kBK;
+    P.stages = (P.nt <= 64 ? 104 * 1024 : 200 * 1024) / stage_bytes;
+    if (P.stages > kMaxStages) P.stages = kMaxStages;
+    size_t smem = (size_t)P.stages * stage_bytes;
+    if (P.splits > 1 && smem < (size_t)P.nt * kBM * 4) smem = (size_t)P.nt * kBM * 4;
+    smem += 1024;
+    CUtensorMap tm_w, tm_x;
+    if (!byte_map(&tm_w, q, N, K, ldw, kBM) || !byte_map(&tm_x, xq, M, K, ldxq, P.nt)) return MATQ_ERR_CUDA;
+    static std::atomic<unsigned long long> smem_ok{0};
+    if (!opt_in_max_smem(gemm_a8_kernel, smem_ok)) return MATQ_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(n_tiles * P.splits), (unsigned)m_tiles);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)P.splits;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, gemm_a8_kernel, tm_w, tm_x, P) != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
+    return launch_status();
+}

@@ -452,7 +452,7 @@ int matq_kv_append(const matq_paged_kv *cache, int64_t T, const void *q, int q_h
  *     are fp32; the weights are rounded to bf16 for the product with v.  Keys outside J contribute nothing whatever the cache holds there (NaN and Inf
  *     included).  A query with empty J (kv_len smaller than the number of new tokens, as for padding) gives zeros.
  *   q       in   bf16 [T, q_heads, head_dim], token stride ldq;  out  bf16 likewise, ldo.  Rows from cu_q[batch] on are left alone.
- *   window  0 = every earlier key
+ *   scale > 0, softcap >= 0 (0 = none), window >= 0 (0 = every earlier key)
  *   max_q, max_kv   upper bounds of n_b and kv_len[b] that the caller knows on the host.  They choose the kernel and the split over
  *           keys; values that are too small cost time, not correctness.
  *   workspace   at least matq_attn_paged_workspace_bytes(...) bytes, 16-byte aligned; contents need not be initialised

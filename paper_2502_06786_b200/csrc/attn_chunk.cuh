@@ -1,0 +1,418 @@
+// Attention of a chunk of new tokens over the paged cache on the fifth-generation tensor cores.
+//
+// A query tile is 128 accumulator rows: floor(128 / group) tokens times the heads of one key head's group, so that a key is read once for the
+// whole group.  A CTA takes kTiles such tiles and walks the keys that they see, kKeys at a time:
+//   warp 4 kTiles      producer: queries once, then keys and values into a ring (one box per page and 64 columns, 128-byte swizzle);
+//   warp 4 kTiles + 1  issues S = Q K^T and O += P V (tcgen05.mma, both accumulators and P in tensor memory);
+//   warps 0 .. 4 kTiles - 1  softmax, one thread per row: S from tensor memory, exponentials, P back over S as bf16.
+// P takes the place of S: the product with V that reads it is issued before the scores that overwrite it.  The row maximum is a reference only: it
+// moves, and O is rescaled, when a score exceeds it by more than 2^8, which leaves p <= 256 and the quotient O / l unchanged.
+// D <= 128: two tiles, whose softmax and tensor work alternate.  D = 256: tensor memory holds one tile's O and two S buffers of 64 keys,
+// so that the scores of the next keys are computed while the present ones are exponentiated.
+#pragma once
+
+#include "attn_common.cuh"
+
+namespace matq {
+namespace attn {
+
+constexpr int kMaxMasked = 16;          // tiles at a range's ends that some row does not see in full
+
+template <int D, int TILES>
+struct ChunkCfg {
+    static constexpr int kTiles = TILES;
+    static_assert(TILES == 1 || (TILES == 2 && D <= 128), "two accumulators and their scores must fit 512 columns");
+    static constexpr int kKeys = D <= 128 ? 128 : 64;
+    static constexpr int kPanels = D / 64;
+    static constexpr int kQBytes = 128 * D * 2;                         // one query tile
+    static constexpr int kKvBytes = kKeys * D * 2;                      // the keys, or the values, of a step
+    static constexpr int kStages = D == 64 ? 8 : 5;
+    static constexpr int kSoft = kTiles * 128;                          // softmax threads
+    static constexpr int kThreads = kSoft + 64;
+    static constexpr int kTmemO = 256;                                  // first column of the output accumulators; S starts at column 0
+    static constexpr size_t kSmem = (size_t)kTiles * kQBytes + (size_t)kStages * kKvBytes + 1024;
+};
+
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* d) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+                 ::"r"(d[0]), "r"(d[1]), "r"(d[2]), "r"(d[3]), "r"(d[4]), "r"(d[5]), "r"(d[6]), "r"(d[7]),
+                   "r"(d[8]), "r"(d[9]), "r"(d[10]), "r"(d[11]), "r"(d[12]), "r"(d[13]), "r"(d[14]), "r"(d[15]),
+                   "r"(d[16]), "r"(d[17]), "r"(d[18]), "r"(d[19]), "r"(d[20]), "r"(d[21]), "r"(d[22]), "r"(d[23]),
+                   "r"(d[24]), "r"(d[25]), "r"(d[26]), "r"(d[27]), "r"(d[28]), "r"(d[29]), "r"(d[30]), "r"(d[31]), "r"(addr) : "memory");
+}
+// D = fp32, A = B = bf16, 128 rows
+__device__ __forceinline__ constexpr uint32_t idesc_bf16(int n, bool b_mn_major) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+
+template <int D, int TILES>
+__global__ void __launch_bounds__(ChunkCfg<D, TILES>::kThreads, 1)
+attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Params P) {
+    using C = ChunkCfg<D, TILES>;
+    constexpr int kKeys = C::kKeys;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[C::kStages], s_empty[C::kStages], s_q, s_score[2], s_prob[2], s_pv, s_out, s_read;
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_timeout, s_any_bad, s_bad_key[kMaxMasked];
+    __shared__ uint32_t s_bad[kMaxMasked][kKeys / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    unsigned char* smem = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
+    unsigned char* ring = smem + C::kTiles * C::kQBytes;
+
+    if (tid == 0) {
+        for (int s = 0; s < C::kStages; ++s) { tc::mbar_init(tc::smem_u32(&s_full[s]), 1); tc::mbar_init(tc::smem_u32(&s_empty[s]), 1); }
+        tc::mbar_init(tc::smem_u32(&s_q), 1);
+        for (int t = 0; t < 2; ++t) { tc::mbar_init(tc::smem_u32(&s_score[t]), 1); tc::mbar_init(tc::smem_u32(&s_prob[t]), 128); }
+        tc::mbar_init(tc::smem_u32(&s_pv), 1);
+        tc::mbar_init(tc::smem_u32(&s_out), 1);
+        tc::mbar_init(tc::smem_u32(&s_read), C::kSoft);
+        tc::mbar_init_fence();
+        s_timeout = 0;
+    }
+    if (warp == C::kSoft / 32 + 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(&s_tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = s_tmem;
+    after_previous_kernel();
+    let_next_kernel_start();
+
+    const int part = (int)(blockIdx.x % (unsigned)P.splits);
+    const unsigned rest = blockIdx.x / (unsigned)P.splits;
+    const int h = (int)(rest % (unsigned)P.kv_heads);
+    const int bt = (int)(rest / (unsigned)P.kv_heads);
+    const int b = bt / P.tiles_per_seq;
+    const int64_t q0 = P.cu_q[b], n_new = P.cu_q[b + 1] - q0;
+    const int kv_len = P.kv_len[b];
+    const bool sane = q0 >= 0 && q0 + n_new <= P.T && kv_len <= P.table_width * P.page_size;
+    if (!sane && n_new > 0 && tid == 0) report(P.dev_status, MATQ_ERR_PAGE);
+    const int tok_tile = 128 / P.group, rows_tile = tok_tile * P.group;  // tokens and used rows of a query tile
+    const int tok_cta = tok_tile * C::kTiles;
+    const int64_t tiles = n_new > 0 && sane ? (n_new + tok_cta - 1) / tok_cta : 0;
+    const int64_t ctx = kv_len - n_new;
+    const auto lo = [&](int64_t p) { return P.window && p - P.window + 1 > 0 ? (int)(p - P.window + 1) : 0; };
+
+    int it = 0, issued = 0, q_issued = 0;                               // steps over keys so far; copies issued (producer)
+    int round = 0;                                                      // tiles with keys so far
+    // the last tiles see the most keys: they are started first
+    for (int64_t tile = P.tiles_per_seq - 1 - (bt - (int64_t)b * P.tiles_per_seq); tile < tiles; tile += P.tiles_per_seq) {
+        const int64_t t0 = tile * tok_cta, t1 = min(t0 + tok_cta, n_new) - 1;      // first and last token
+        const int p_lo = (int)(ctx + t0), p_hi = (int)(ctx + t1);
+        const int first = lo(p_lo), all_from = lo(p_hi);                // some row sees [first, p_hi], every row [all_from, p_lo]
+        const int64_t k_lo64 = (int64_t)(first & ~(kKeys - 1)) + part * P.split_keys;
+        int64_t k_hi64 = (int64_t)p_hi + 1;
+        if (part + 1 < P.splits) k_hi64 = min(k_hi64, k_lo64 + P.split_keys);
+        const int n_it = k_hi64 > k_lo64 ? (int)((k_hi64 - k_lo64 + kKeys - 1) / kKeys) : 0;
+        const int k_lo = n_it ? (int)k_lo64 : 0;
+        const auto is_masked = [&](int j0) { return j0 + kKeys - 1 > p_lo || j0 < all_from; };
+
+        if (warp == C::kSoft / 32) {
+            // ---------------- producer
+            bool ok = true;
+            if (n_it > 0) {
+                if (round > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_out), (uint32_t)(round - 1) & 1u, P.wait_cycles));
+                if (ok && !P.hold && lane == 0) {
+                    q_issued = round + 1;
+                    tc::mbar_expect_tx(tc::smem_u32(&s_q), C::kTiles * C::kPanels * rows_tile * 128);
+                    for (int t = 0; t < C::kTiles; ++t)
+                        for (int p = 0; p < C::kPanels; ++p)
+                            tc::tma_load_3d(tc::smem_u32(smem) + t * C::kQBytes + p * (128 * 128), &tm_q, p * 64, h * P.group,
+                                            (int)(q0 + t0 + t * tok_tile), tc::smem_u32(&s_q));
+                }
+            }
+            const int rows_box = min(P.page_size, kKeys), runs = kKeys / rows_box, boxes = runs * C::kPanels;
+            int next_row = lane < runs && n_it > 0 ? cache_row(P, b, h, (int64_t)k_lo + lane * rows_box, rows_box, first, kv_len) : 0;
+            for (int i = 0; i < n_it && ok; ++i) {
+                const int row = next_row;
+                if (lane < runs && i + 1 < n_it) next_row = cache_row(P, b, h, (int64_t)k_lo + (i + 1) * kKeys + lane * rows_box, rows_box, first, kv_len);
+                for (int v = 0; v < 2; ++v) {
+                    const int u = 2 * (it + i) + v, s = u % C::kStages;
+                    ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_empty[s]), ((uint32_t)(u / C::kStages) & 1u) ^ 1u, P.wait_cycles)) && !P.hold;
+                    if (!ok) break;
+                    const uint32_t bar = tc::smem_u32(&s_full[s]);
+                    if (lane == 0) tc::mbar_expect_tx(bar, C::kKvBytes);
+                    __syncwarp();
+                    // runs and panels are powers of two: a box per lane, at most 32 of them
+                    const int run = lane & (runs - 1), panel = lane / runs;
+                    const int y = __shfl_sync(0xffffffffu, row, run);
+                    if (lane < boxes)
+                        tc::tma_load_2d(tc::smem_u32(ring) + (uint32_t)s * C::kKvBytes + (uint32_t)panel * (kKeys * 128) + (uint32_t)run * rows_box * 128,
+                                        v ? &tm_v : &tm_k, panel * 64, y, bar);
+                    issued = u + 1;
+                }
+            }
+            if (!ok) {
+                if (lane == 0) *(volatile int*)&s_timeout = 1;
+                break;
+            }
+        } else if (warp == C::kSoft / 32 + 1) {
+            // ---------------- tensor cores: one thread issues
+            if (lane == 0 && n_it > 0) {
+                bool ok = tc::mbar_wait(tc::smem_u32(&s_q), (uint32_t)round & 1u, P.wait_cycles);
+                const auto wait_kv = [&](int u) { return tc::mbar_wait(tc::smem_u32(&s_full[u % C::kStages]), (uint32_t)(u / C::kStages) & 1u, P.wait_cycles); };
+                const auto kv_at = [&](int u) { return tc::smem_u32(ring) + (uint32_t)(u % C::kStages) * C::kKvBytes; };
+                const auto scores = [&](int t, int i) {                 // S_t = Q_t K_i^T
+                    const uint32_t a = tc::smem_u32(smem) + (C::kTiles == 2 ? t * C::kQBytes : 0), kb = kv_at(2 * (it + i));
+                    const uint32_t d = tmem + t * kKeys;
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks)
+                        asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
+                                     ::"r"(d), "l"(tc::sw128_desc(a + (ks / 4) * (128 * 128) + (ks & 3) * 32)),
+                                       "l"(tc::sw128_desc(kb + (ks / 4) * (kKeys * 128) + (ks & 3) * 32)), "r"(idesc_bf16(kKeys, false)), "r"(ks > 0 ? 1u : 0u) : "memory");
+                    tc::tc_commit(tc::smem_u32(&s_score[t]));
+                };
+                const auto product = [&](int t, int i) {                // O_t += P_t V_i
+                    const uint32_t vb = kv_at(2 * (it + i) + 1), d = tmem + C::kTmemO + (C::kTiles == 2 ? t * D : 0);
+#pragma unroll
+                    for (int ks = 0; ks < kKeys / 16; ++ks)
+                        asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
+                                     ::"r"(d), "r"(tmem + t * kKeys + ks * 8), "l"(tc::sw128_desc(vb + ks * 2048, kKeys * 128, 1024)),
+                                       "r"(idesc_bf16(D, true)), "r"((i > 0 || ks > 0) ? 1u : 0u) : "memory");
+                };
+                const auto free_kv = [&](int u) { tc::tc_commit(tc::smem_u32(&s_empty[u % C::kStages])); };
+                if (ok) ok = wait_kv(2 * it);
+                tc::fence_after();
+                if (C::kTiles == 2) {
+                    if (ok) { scores(0, 0); scores(1, 0); free_kv(2 * it); }
+                    for (int i = 0; i < n_it && ok; ++i) {
+                        for (int t = 0; t < 2 && ok; ++t) {
+                            ok = tc::mbar_wait(tc::smem_u32(&s_prob[t]), (uint32_t)(it + i) & 1u, P.wait_cycles) && wait_kv(2 * (it + i) + 1);
+                            if (ok && i == 0 && t == 0 && round > 0) ok = tc::mbar_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles);
+                            if (!ok) break;
+                            tc::fence_after();
+                            product(t, i);
+                            if (t == 1) free_kv(2 * (it + i) + 1);
+                            if (i + 1 < n_it) {
+                                ok = wait_kv(2 * (it + i + 1));
+                                if (!ok) break;
+                                tc::fence_after();
+                                scores(t, i + 1);
+                                if (t == 1) free_kv(2 * (it + i + 1));
+                            }
+                        }
+                    }
+                } else {
+                    if (ok) { scores(it & 1, 0); free_kv(2 * it); }
+                    for (int i = 0; i < n_it && ok; ++i) {
+                        if (i + 1 < n_it) {
+                            ok = wait_kv(2 * (it + i + 1));
+                            if (!ok) break;
+                            tc::fence_after();
+                            scores((it + i + 1) & 1, i + 1);
+                            free_kv(2 * (it + i + 1));
+                        }
+                        ok = tc::mbar_wait(tc::smem_u32(&s_prob[(it + i) & 1]), (uint32_t)((it + i) >> 1) & 1u, P.wait_cycles) && wait_kv(2 * (it + i) + 1);
+                        if (ok && i == 0 && round > 0) ok = tc::mbar_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles);
+                        if (!ok) break;
+                        tc::fence_after();
+                        product((it + i) & 1, i);
+                        free_kv(2 * (it + i) + 1);
+                        tc::tc_commit(tc::smem_u32(&s_pv));
+                    }
+                }
+                if (!ok) { *(volatile int*)&s_timeout = 1; __threadfence_block(); }
+                tc::tc_commit(tc::smem_u32(&s_out));                    // also when giving up: nobody waits for longer than its limit
+            }
+            __syncwarp();
+        } else {
+            // ---------------- softmax: thread = row of tile t
+            const int t = C::kTiles == 2 ? warp >> 2 : 0, r = tid & 127;
+            const int64_t tok = t0 + t * tok_tile + r / P.group;
+            const bool live = r < rows_tile && tok < n_new;
+            const int see_hi = live ? (int)(ctx + tok) : -1, see_lo = live ? lo(see_hi) : 0;
+            const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+            const uint32_t o_addr = lane_addr + C::kTmemO + t * D;
+            const Score sc(P.scale, P.softcap);
+            float m = -INFINITY, l = 0.f;
+            bool ok = true;
+            int masked_no = 0;
+            if (tid == 0) s_any_bad = 0;
+            for (int x = tid; x < kMaxMasked * (kKeys / 32); x += C::kSoft) (&s_bad[0][0])[x] = 0;
+            asm volatile("bar.sync 1, %0;" ::"n"(C::kSoft) : "memory");
+
+            for (int i = 0; i < n_it; ++i) {
+                const int gi = it + i, j0 = k_lo + i * kKeys;
+                const int which = C::kTiles == 2 ? t : gi & 1;
+                const uint32_t par = C::kTiles == 2 ? (uint32_t)gi & 1u : (uint32_t)(gi >> 1) & 1u;
+                if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_score[which]), par, P.wait_cycles)) && *(volatile int*)&s_timeout == 0;
+                ok = __all_sync(0xffffffffu, ok);
+                const bool masked = is_masked(j0);
+                if (ok) {
+                    tc::fence_after();
+                    const uint32_t s_addr = lane_addr + which * kKeys;
+                    uint32_t sr[kKeys];
+#pragma unroll
+                    for (int c = 0; c < kKeys; c += 32) tc::tmem_ld32(s_addr + c, sr + c);
+                    tc::tmem_wait_ld();
+                    float mul = sc.mul;
+                    if (sc.cap2 > 0.f) {
+#pragma unroll
+                        for (int c = 0; c < kKeys; ++c) sr[c] = __float_as_uint(capped(__uint_as_float(sr[c]), sc.mul, sc.cap2));
+                        mul = 1.f;
+                    }
+                    if (masked) {
+#pragma unroll
+                        for (int c = 0; c < kKeys; ++c)
+                            if (j0 + c > see_hi || j0 + c < see_lo) sr[c] = 0xff800000u;
+                    }
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < kKeys; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(sr[c]));
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
+                    const bool raise = top > m + 8.f;                    // also from -inf to anything finite
+                    if (__any_sync(0xffffffffu, raise)) {
+                        const float f = raise ? ex2(m - top) : 1.f;
+                        if (raise) m = top;
+                        l *= f;
+                        if (i > 0) {
+                            // O holds the steps before this one.  With two tiles the scores' arrival says that their product is done.
+                            if (C::kTiles == 1) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_pv), (uint32_t)(gi - 1) & 1u, P.wait_cycles));
+                            tc::fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 32) {
+                                uint32_t o[32];
+                                tc::tmem_ld32(o_addr + c, o);
+                                tc::tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st32(o_addr + c, o);
+                            }
+                        }
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < kKeys; c += 64) {
+                        uint32_t pk[32];
+#pragma unroll
+                        for (int e = 0; e < 64; e += 2) {
+                            const float a = ex2(fmaf(__uint_as_float(sr[c + e]), mul, -ref)), d = ex2(fmaf(__uint_as_float(sr[c + e + 1]), mul, -ref));
+                            sum[e & 2] += a;
+                            sum[(e & 2) + 1] += d;
+                            pk[e / 2] = pack_bf16(a, d);
+                        }
+                        tmem_st32(s_addr + c / 2, pk);
+                    }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    tc::tmem_wait_st();
+                }
+                if (masked) {
+                    // A weight of zero does not silence a NaN or Inf.  Values that no row sees become zero; non-finite ones that only some rows
+                    // see leave the tile, and those rows get them at the end.  Every thread looks at one key, all or half of it.
+                    const int u = 2 * gi + 1;
+                    if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_full[u % C::kStages]), (uint32_t)(u / C::kStages) & 1u, P.wait_cycles));
+                    if (ok) {
+                        constexpr int kShare = C::kSoft / kKeys;         // threads per key: 2
+                        const int key = tid % kKeys, j = j0 + key;
+                        const bool unseen = j > p_hi || j < first, all = j <= p_lo && j >= all_from;
+                        const uint32_t vb = tc::smem_u32(ring) + (uint32_t)(u % C::kStages) * C::kKvBytes + key * 128;
+                        bool bad = false;
+                        if (!all) {
+                            for (int ch = tid / kKeys; ch < D / 8; ch += kShare) {
+                                const uint32_t at = vb + (uint32_t)(ch >> 3) * (kKeys * 128) + (((ch & 7) ^ (key & 7)) << 4);
+                                if (unseen) {
+                                    asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at), "r"(0) : "memory");
+                                } else {
+                                    uint32_t w[4];
+                                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+                                    bool here = false;
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        if (nonfinite_bf16(w[e])) { here = true; w[e] &= 0xffff0000u; }
+                                        if (nonfinite_bf16(w[e] >> 16)) { here = true; w[e] &= 0x0000ffffu; }
+                                    }
+                                    if (here) asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                                    bad |= here;
+                                }
+                            }
+                        }
+                        if (bad && masked_no < kMaxMasked) {
+                            atomicOr(&s_bad[masked_no][key >> 5], 1u << (key & 31));
+                            s_any_bad = 1;
+                        }
+                        if (tid == 0 && masked_no < kMaxMasked) s_bad_key[masked_no] = j0;
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                    ++masked_no;
+                    asm volatile("bar.sync 1, %0;" ::"n"(C::kSoft) : "memory");     // both tiles' products read the mended values
+                }
+                tc::fence_before();
+                tc::mbar_arrive(tc::smem_u32(&s_prob[which]));
+            }
+
+            // ---------------- outputs
+            if (n_it > 0 && ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_out), (uint32_t)round & 1u, P.wait_cycles)) && *(volatile int*)&s_timeout == 0;
+            ok = __all_sync(0xffffffffu, ok);
+            tc::fence_after();
+            const int64_t row = (q0 + tok) * P.q_heads + h * P.group + r % P.group;
+            const bool any = see_hi >= 0;
+            const float inv = any ? 1.f / l : 0.f;
+            if (!ok) *(volatile int*)&s_timeout = 1;
+            if (ok && live && P.splits > 1) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(m, l);
+            if (ok && !(P.splits > 1 && n_it == 0)) {
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    if (n_it > 0) {
+                        tc::tmem_ld32(o_addr + c, o);
+                        tc::tmem_wait_ld();
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = 0u;
+                    }
+                    if (s_any_bad && live) {
+                        for (int x = 0; x < min(masked_no, kMaxMasked); ++x)
+                            for (int key = 0; key < kKeys; ++key) {
+                                const int j = s_bad_key[x] + key;
+                                if (!((s_bad[x][key >> 5] >> (key & 31)) & 1u) || j > see_hi || j < see_lo) continue;
+                                const int64_t at = cache_row(P, b, h, j, 1, 0, kv_len);
+                                if (at >= P.n_pages * P.kv_heads * P.page_size) continue;
+                                const uint16_t* v = reinterpret_cast<const uint16_t*>(P.v) + at * D + c;
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    if (nonfinite_bf16(v[e])) o[e] = __float_as_uint(__uint_as_float(o[e]) + bf16_bits_to_float(v[e]));
+                            }
+                    }
+                    if (!live) continue;
+                    if (P.splits > 1) {
+                        uint4* dst = reinterpret_cast<uint4*>(P.part_o + ((int64_t)part * (P.T * P.q_heads) + row) * D + c);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) dst[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    } else {
+                        uint4* dst = reinterpret_cast<uint4*>(P.out + (q0 + tok) * P.ldo + (int64_t)(h * P.group + r % P.group) * D + c);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                w[x] = any ? pack_bf16(__uint_as_float(o[8 * e + 2 * x]) * inv, __uint_as_float(o[8 * e + 2 * x + 1]) * inv) : 0u;
+                            dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                }
+            }
+            tc::fence_before();
+            if (n_it > 0) tc::mbar_arrive(tc::smem_u32(&s_read));
+            asm volatile("bar.sync 1, %0;" ::"n"(C::kSoft) : "memory");             // s_bad is read before the next tile clears it
+        }
+        it += n_it;
+        if (n_it > 0) ++round;
+    }
+    if (warp == C::kSoft / 32) {                                        // no copy may be in flight when the CTA ends, whatever became of its consumer
+        for (int u = max(0, issued - C::kStages); u < issued; ++u)
+            tc::mbar_wait(tc::smem_u32(&s_full[u % C::kStages]), (uint32_t)(u / C::kStages) & 1u, P.wait_cycles);
+        if (q_issued) tc::mbar_wait(tc::smem_u32(&s_q), (uint32_t)(q_issued - 1) & 1u, P.wait_cycles);
+    }
+    tc::fence_before();
+    __syncthreads();
+    if (tid == 0 && s_timeout) report(P.dev_status, MATQ_ERR_TIMEOUT);
+    if (warp == C::kSoft / 32 + 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+}  // namespace attn
+}  // namespace matq

@@ -9,7 +9,7 @@ namespace attn {
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Params {
-    const __nv_bfloat16* q;
+    const __nv_bfloat16 *q, *v;
     __nv_bfloat16* out;
     const int32_t *table, *cu_q, *kv_len;
     int64_t ldq, ldo, table_stride, table_width, n_pages, T;
@@ -52,11 +52,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 __device__ __forceinline__ bool nonfinite_bf16(uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u; }
 
-// First row, in the cache seen as rows of D elements, of the slots that hold keys key .. of sequence b, head h.  A page number that is out of
-// range gives a row past the end, which reads as zeros, and is reported.
-__device__ __forceinline__ int cache_row(const Params& P, int b, int h, int64_t key, int64_t kv_len) {
+// First row, in the cache seen as rows of D elements, of the slots that hold keys key .. key + count - 1 of sequence b, head h (all in one page).
+// Slots of which no query sees a key (below `first`, where a sliding window may have given its pages back, or past the sequence) are not looked up: the
+// row past the end reads as zeros.  So does a page number that is out of range, which is reported.
+__device__ __forceinline__ int cache_row(const Params& P, int b, int h, int64_t key, int count, int first, int kv_len) {
     const int64_t last = P.n_pages * P.kv_heads * P.page_size;
-    if (key >= kv_len) return (int)last;
+    if (key >= kv_len || key + count <= first) return (int)last;
     const int64_t pg = key >> P.page_shift;
     int64_t page = -1;
     if (pg < P.table_width) page = P.table[(int64_t)b * P.table_stride + pg];
@@ -67,45 +68,65 @@ __device__ __forceinline__ int cache_row(const Params& P, int b, int h, int64_t 
     return (int)((page * P.kv_heads + h) * P.page_size + (key & (P.page_size - 1)));
 }
 
-// Joins the parts of the key range: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s, the parts in their order.  One warp per (token, head).
+// Joins the parts of the key range: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  A CTA per (token, head): the weights of the
+// parts are made side by side, then eight warps take every eighth part each, and their sums are added in a fixed order.
+constexpr int kMaxSplits = 256, kJoinThreads = 256;
 template <int D>
-__global__ void __launch_bounds__(128) attn_join_kernel(const Params P) {
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const Params P) {
+    __shared__ float s_w[kMaxSplits], s_red[2][8];
+    __shared__ float s_o[8][D];
     after_previous_kernel();
     let_next_kernel_start();
-    const int lane = threadIdx.x & 31;
-    const int64_t rows = P.T * P.q_heads, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (row >= rows) return;
-    const int64_t t = row / P.q_heads;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t rows = P.T * P.q_heads, row = blockIdx.x, t = row / P.q_heads;
     if (t >= P.cu_q[P.batch]) return;
-    constexpr int kV = D / 64;                                         // float2 pieces per lane
-    float mx = -INFINITY;
-    for (int s = lane; s < P.splits; s += 32) mx = fmaxf(mx, P.part_ml[(int64_t)s * rows + row].x);
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (tid < P.splits) ml = P.part_ml[(int64_t)tid * rows + row];
+    float mx = ml.x;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    if (lane == 0) s_red[0][warp] = mx;
+    __syncthreads();
+    mx = s_red[0][0];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) mx = fmaxf(mx, s_red[0][w]);
+    const bool any = !(ml.x == -INFINITY && ml.y == 0.f);               // the part holds keys of this row
+    const float w = any && mx != -INFINITY ? ex2(ml.x - mx) : 0.f;
+    s_w[tid] = any ? w : -1.f;                                          // negative: the part's sums were not written
+    float sum = any ? ml.y * w : 0.f;
+    if (any && mx == -INFINITY) sum = ml.y;                              // NaN
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_red[1][warp] = sum;
+    const bool seen = __syncthreads_or(any);
+    sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) sum += s_red[1][v];
+    constexpr int kV = D / 64;                                          // float2 pieces per lane
     float2 acc[kV];
 #pragma unroll
     for (int j = 0; j < kV; ++j) acc[j] = make_float2(0.f, 0.f);
-    float sum = 0.f;
-    bool any = false;
-    for (int s = 0; s < P.splits; ++s) {
-        const float2 ml = P.part_ml[(int64_t)s * rows + row];
-        if (ml.y == 0.f && ml.x == -INFINITY) continue;                 // a part without keys for this row
-        any = true;
-        const float w = mx == -INFINITY ? 0.f : ex2(ml.x - mx);
-        sum = fmaf(ml.y, w, sum);
+#pragma unroll 4
+    for (int s = warp; s < P.splits; s += 8) {
+        const float ws = s_w[s];
         const float2* o = reinterpret_cast<const float2*>(P.part_o + ((int64_t)s * rows + row) * D);
 #pragma unroll
         for (int j = 0; j < kV; ++j) {
-            const float2 v = o[lane + 32 * j];
-            acc[j].x = fmaf(v.x, w, acc[j].x);
-            acc[j].y = fmaf(v.y, w, acc[j].y);
+            const float2 v = ws >= 0.f ? o[lane + 32 * j] : make_float2(0.f, 0.f);
+            acc[j].x = fmaf(v.x, ws, acc[j].x);
+            acc[j].y = fmaf(v.y, ws, acc[j].y);
         }
     }
-    const float inv = any ? 1.f / sum : 0.f;
-    const int h = (int)(row - t * P.q_heads);
-    uint32_t* dst = reinterpret_cast<uint32_t*>(P.out + t * P.ldo + (int64_t)h * D);
 #pragma unroll
-    for (int j = 0; j < kV; ++j) dst[lane + 32 * j] = any ? pack_bf16(acc[j].x * inv, acc[j].y * inv) : 0u;
+    for (int j = 0; j < kV; ++j) *reinterpret_cast<float2*>(&s_o[warp][2 * (lane + 32 * j)]) = acc[j];
+    __syncthreads();
+    if (tid < D / 2) {
+        float a = 0.f, b = 0.f;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) { a += s_o[v][2 * tid]; b += s_o[v][2 * tid + 1]; }
+        const float inv = 1.f / sum;
+        reinterpret_cast<uint32_t*>(P.out + t * P.ldo + (row - t * P.q_heads) * D)[tid] = seen ? pack_bf16(a * inv, b * inv) : 0u;
+    }
 }
 
 }  // namespace attn

@@ -91,10 +91,10 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             const int rows_box = min(P.page_size, kDecKeys);            // rows of a box
             const int runs = kDecKeys / rows_box, boxes = runs * C::kPanels * 2;
             bool ok = true;
+            int next_row = lane < runs && n_it > 0 ? cache_row(P, b, h, (int64_t)k_lo + lane * rows_box, rows_box, first, kv_len) : 0;
             for (int i = 0; i < n_it && ok; ++i) {
-                const int s = (it + i) % C::kStages;
-                int row = 0;
-                if (lane < runs) row = cache_row(P, b, h, (int64_t)k_lo + i * kDecKeys + lane * rows_box, kv_len);
+                const int s = (it + i) % C::kStages, row = next_row;    // the page of the next stage is looked up while this one waits
+                if (lane < runs && i + 1 < n_it) next_row = cache_row(P, b, h, (int64_t)k_lo + (i + 1) * kDecKeys + lane * rows_box, rows_box, first, kv_len);
                 ok = tc::mbar_wait(tc::smem_u32(&s_empty[s]), ((uint32_t)((it + i) / C::kStages) & 1u) ^ 1u, P.wait_cycles);
                 if (!__all_sync(0xffffffffu, ok) || P.hold) { ok = false; break; }
                 const uint32_t bar = tc::smem_u32(&s_full[s]);

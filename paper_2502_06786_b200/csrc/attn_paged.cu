@@ -1,29 +1,35 @@
 // matq_attn_paged: attention of new tokens over a paged cache (argument checks, choice of kernel and split).
+#include "attn_chunk.cuh"
 #include "attn_decode.cuh"
 
 namespace matq {
 namespace attn {
 
 struct Plan {
+    int kind;                    // 0: 16-row tiles; 1, 2: query tiles of 128 rows per CTA
     int64_t tiles_per_seq, splits, split_keys;
 };
 
-// Parts of the key range: enough CTAs to fill the GPU, but at least 256 keys (four stages) per part.
-inline Plan plan(int batch, int kv_heads, int group, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
+// Kernel and split from sizes that the host knows.
+inline Plan plan(int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
     Plan p;
     const int64_t rows = max_q * group;
-    p.tiles_per_seq = (rows + kDecRows - 1) / kDecRows;
+    p.kind = rows <= kDecRows ? 0 : (rows <= 128 || D == 256 ? 1 : 2);
+    const int keys = p.kind == 0 || D == 256 ? 64 : 128;
+    const int64_t tok = p.kind == 0 ? 0 : (int64_t)(128 / group) * p.kind;       // tokens per CTA
+    p.tiles_per_seq = p.kind == 0 ? (rows + kDecRows - 1) / kDecRows : (max_q + tok - 1) / tok;
     if (p.tiles_per_seq < 1) p.tiles_per_seq = 1;
-    int64_t range = max_kv;
-    if (window > 0 && window + kDecRows < range) range = window + kDecRows;
-    range = (range + kDecKeys - 1) / kDecKeys + 1;                      // stages; one more when the window starts inside one
+    int64_t range = max_kv;                                             // keys that a tile can see
+    if (window > 0 && window + tok + 16 < range) range = window + tok + 16;
+    range = (range + keys - 1) / keys + 1;                              // steps; one more when the window starts inside one
     const int64_t ctas = p.tiles_per_seq * batch * kv_heads;
-    int64_t splits = ctas > 0 ? (4 * sms + ctas - 1) / ctas : 1;
-    if (splits > range / 4) splits = range / 4;
+    int64_t splits = ctas > 0 ? (p.kind == 0 ? (2 * sms + ctas - 1) / ctas : sms / ctas) : 1;
+    if (splits > range / 4) splits = range / 4;                         // four steps per part at least
+    if (splits > kMaxSplits) splits = kMaxSplits;
     if (splits < 1) splits = 1;
-    int64_t per = (range + splits - 1) / splits;
+    const int64_t per = (range + splits - 1) / splits;
     p.splits = (range + per - 1) / per;
-    p.split_keys = per * kDecKeys;
+    p.split_keys = per * keys;
     return p;
 }
 
@@ -38,20 +44,52 @@ inline bool cache_map(CUtensorMap* tm, const void* base, int64_t rows, int D, in
     return tc::make_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box);
 }
 
+// queries as [token][head][D]: a box is 64 columns of the heads of a group for the tokens of a tile
+inline bool query_map(CUtensorMap* tm, const void* q, int64_t T, int q_heads, int D, int64_t ldq, int group) {
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)q_heads, (cuuint64_t)T};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)ldq * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)group, (cuuint32_t)(128 / group)};
+    return tc::make_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, q, dims, strides, box);
+}
+
 template <int D>
-int launch_decode(const CUtensorMap& tk, const CUtensorMap& tv, const Params& P, cudaStream_t s) {
+int launch_decode(const CUtensorMap& tk, const CUtensorMap& tv, const Params& P, unsigned grid, cudaStream_t s) {
     static std::atomic<unsigned long long> smem_ok{0};
     if (!opt_in_max_smem(attn_decode_kernel<D>, smem_ok)) return MATQ_ERR_CUDA;
-    const int64_t grid = (int64_t)P.splits * P.kv_heads * P.batch * P.tiles_per_seq;
-    if (grid >= (1ll << 31)) return MATQ_ERR_SHAPE;
-    if (launch_overlapped(attn_decode_kernel<D>, dim3((unsigned)grid), dim3(kDecThreads), DecCfg<D>::kSmem, s, tk, tv, P) != cudaSuccess) {
+    if (launch_overlapped(attn_decode_kernel<D>, dim3(grid), dim3(kDecThreads), DecCfg<D>::kSmem, s, tk, tv, P) != cudaSuccess) {
         cudaGetLastError();
         return MATQ_ERR_CUDA;
     }
-    if (P.splits > 1) {
-        const int64_t blocks = (P.T * P.q_heads + 3) / 4;
-        if (blocks >= (1ll << 31)) return MATQ_ERR_SHAPE;
-        if (launch_overlapped(attn_join_kernel<D>, dim3((unsigned)blocks), dim3(128), 0, s, P) != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
+    return MATQ_OK;
+}
+
+template <int D, int TILES>
+int launch_chunk(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const Params& P, unsigned grid, cudaStream_t s) {
+    using C = ChunkCfg<D, TILES>;
+    static std::atomic<unsigned long long> smem_ok{0};
+    if (!opt_in_max_smem(attn_chunk_kernel<D, TILES>, smem_ok)) return MATQ_ERR_CUDA;
+    if (launch_overlapped(attn_chunk_kernel<D, TILES>, dim3(grid), dim3(C::kThreads), C::kSmem, s, tq, tk, tv, P) != cudaSuccess) {
+        cudaGetLastError();
+        return MATQ_ERR_CUDA;
+    }
+    return MATQ_OK;
+}
+
+template <int D>
+int launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const Params& P, int kind, unsigned grid, cudaStream_t s) {
+    int st;
+    if (kind == 0) {
+        st = launch_decode<D>(tk, tv, P, grid, s);
+    } else if (kind == 1) {
+        st = launch_chunk<D, 1>(tq, tk, tv, P, grid, s);
+    } else {
+        if constexpr (D <= 128) st = launch_chunk<D, 2>(tq, tk, tv, P, grid, s);
+        else st = MATQ_ERR_UNSUPPORTED;
+    }
+    if (st != MATQ_OK) return st;
+    if (P.splits > 1 && launch_overlapped(attn_join_kernel<D>, dim3((unsigned)(P.T * P.q_heads)), dim3(kJoinThreads), 0, s, P) != cudaSuccess) {
+        cudaGetLastError();
+        return MATQ_ERR_CUDA;
     }
     return launch_status();
 }
@@ -62,8 +100,8 @@ int launch_decode(const CUtensorMap& tk, const CUtensorMap& tv, const Params& P,
 extern "C" size_t matq_attn_paged_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim,
                                                   int64_t max_q, int64_t max_kv, int64_t window) {
     using namespace matq::attn;
-    if (T <= 0 || batch <= 0 || q_heads <= 0 || kv_heads <= 0 || q_heads % kv_heads != 0 || head_dim <= 0) return 0;
-    const Plan p = plan(batch, kv_heads, q_heads / kv_heads, max_q, max_kv, window, matq::sm_count());
+    if (T <= 0 || batch <= 0 || q_heads <= 0 || kv_heads <= 0 || q_heads % kv_heads != 0 || q_heads / kv_heads > 64 || head_dim <= 0 || max_q < 0 || max_kv < 0) return 0;
+    const Plan p = plan(batch, kv_heads, q_heads / kv_heads, head_dim, max_q, max_kv, window, matq::sm_count());
     return part_bytes(T, q_heads, head_dim, p.splits);
 }
 
@@ -73,7 +111,7 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     using namespace matq;
     using namespace matq::attn;
     if (!cache || T < 0 || q_heads < 1 || cache->batch < 0 || cache->n_pages < 0 || cache->kv_heads < 1 || cache->table_width < 0 || (cache->batch > 1 && cache->table_stride < cache->table_width) ||
-        window < 0 || max_q < 0 || max_kv < 0 || !(softcap >= 0.f) || !(scale == scale))
+        window < 0 || max_q < 0 || max_kv < 0 || !(softcap >= 0.f) || !(scale > 0.f))
         return MATQ_ERR_INVALID_ARG;
     const int D = cache->head_dim, ps = cache->page_size;
     if (D != 64 && D != 128 && D != 256) return MATQ_ERR_UNSUPPORTED;
@@ -85,11 +123,11 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     if (!q || !out || !cache->k || !cache->v || !cache->page_table || !cache->cu_q || !cache->kv_len || cache->n_pages == 0) return MATQ_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out) || !aligned16(cache->k) || !aligned16(cache->v) || !aligned16(workspace)) return MATQ_ERR_ALIGNMENT;
     const int group = q_heads / cache->kv_heads;
-    const Plan p = plan(cache->batch, cache->kv_heads, group, max_q, max_kv, window, sm_count());
+    const Plan p = plan(cache->batch, cache->kv_heads, group, D, max_q, max_kv, window, sm_count());
     if (part_bytes(T, q_heads, D, p.splits) > workspace_bytes || (p.splits > 1 && !workspace)) return MATQ_ERR_WORKSPACE;
 
     Params P;
-    P.q = static_cast<const __nv_bfloat16*>(q); P.out = static_cast<__nv_bfloat16*>(out);
+    P.q = static_cast<const __nv_bfloat16*>(q); P.v = static_cast<const __nv_bfloat16*>(cache->v); P.out = static_cast<__nv_bfloat16*>(out);
     P.table = cache->page_table; P.cu_q = cache->cu_q; P.kv_len = cache->kv_len;
     P.ldq = ldq; P.ldo = ldo; P.table_stride = cache->table_stride; P.table_width = cache->table_width; P.n_pages = cache->n_pages; P.T = T; P.window = window;
     P.batch = cache->batch; P.q_heads = q_heads; P.kv_heads = cache->kv_heads; P.group = group;
@@ -101,11 +139,13 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     P.dev_status = dev_status;
     P.hold = tc::test_stall() ? 1 : 0;
     P.wait_cycles = P.hold ? tc::kStallWaitCycles : tc::kWaitCycles;
-    CUtensorMap tk, tv;
-    const int box = ps < kDecKeys ? ps : kDecKeys;
-    if (!cache_map(&tk, cache->k, rows, D, box) || !cache_map(&tv, cache->v, rows, D, box)) return MATQ_ERR_CUDA;
+    const int64_t grid = p.splits * cache->kv_heads * cache->batch * p.tiles_per_seq;
+    if (grid >= (1ll << 31) || (p.splits > 1 && T * q_heads >= (1ll << 31))) return MATQ_ERR_SHAPE;
+    CUtensorMap tq, tk, tv;
+    const int keys = p.kind == 0 || D == 256 ? 64 : 128, box = ps < keys ? ps : keys;
+    if (!cache_map(&tk, cache->k, rows, D, box) || !cache_map(&tv, cache->v, rows, D, box) || !query_map(&tq, q, T, q_heads, D, ldq, group)) return MATQ_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (D == 64) return launch_decode<64>(tk, tv, P, s);
-    if (D == 128) return launch_decode<128>(tk, tv, P, s);
-    return launch_decode<256>(tk, tv, P, s);
+    if (D == 64) return launch<64>(tq, tk, tv, P, p.kind, (unsigned)grid, s);
+    if (D == 128) return launch<128>(tq, tk, tv, P, p.kind, (unsigned)grid, s);
+    return launch<256>(tq, tk, tv, P, p.kind, (unsigned)grid, s);
 }

@@ -141,7 +141,8 @@ def _ptr(t):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # the raw handle: building a torch.cuda.Stream object costs 3 us, more than everything else on a call's way to the library
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _dev(t, dtype, name, ndim=None):
@@ -421,111 +422,132 @@ def gemm_multi_static(src_kind, Wsrc, K, X, Ys, alpha, zero, rs=(8, 4, 2), extra
     return _check(st, "matq_gemm_multi_static", raise_on_error)
 
 
-def quantize_tokens(X, xq=None, scale=None, rowsum=None, dev_status=None):
-    """matq_quantize_tokens.  X: bf16 [M, K].  Returns (xq int8 [M, K], scale fp32 [M], rowsum int32 [M])."""
-    _dev(X, torch.bfloat16, "X", 2)
-    if X.stride(1) != 1:
-        raise ValueError("X: unit stride along K required")
-    M, K = X.shape
-    if xq is None:
-        xq = torch.empty((M, K), dtype=torch.int8, device=X.device)
-    if scale is None:
-        scale = torch.empty(M, dtype=torch.float32, device=X.device)
-    if rowsum is None:
-        rowsum = torch.empty(M, dtype=torch.int32, device=X.device)
-    _dev(xq, torch.int8, "xq", 2); _vector(scale, torch.float32, "scale", M); _vector(rowsum, torch.int32, "rowsum", M)
-    if tuple(xq.shape) != (M, K) or xq.stride(1) != 1:
-        raise ValueError("xq: int8 [M, K] with unit stride along K required")
-    st = _lib.matq_quantize_tokens(_ptr(X), M, K, _ld(X, K), _ptr(xq), _ld(xq, K), _ptr(scale), _ptr(rowsum),
-                                   _ptr(dev_status), _stream())
-    _check(st, "matq_quantize_tokens")
-    return xq, scale, rowsum
+# The serving calls below are short (a decode step's take a few microseconds on the GPU), so their argument checks read each attribute once
+# and pass plain integers.
+
+_BF16, _F32, _I32, _I8, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.int8, torch.uint8
 
 
 def _vector(t, dtype, name, n):
-    _dev(t, dtype, name, 1)
-    if t.numel() != n or not t.is_contiguous():
+    """Address of a contiguous one-dimensional CUDA tensor of n elements."""
+    if t.dtype is not dtype or not t.is_cuda:
+        _dev(t, dtype, name)
+    if t.dim() != 1 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name}: contiguous, {n} elements required")
-    return t
+    return t.data_ptr()
+
+
+def _matrix(t, dtype, name):
+    """(address, rows, columns, row stride) of a two-dimensional CUDA tensor with unit stride along its columns."""
+    if t.dtype is not dtype or not t.is_cuda:
+        _dev(t, dtype, name)
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected 2 dimensions")
+    rows, cols = t.shape
+    ld, unit = t.stride()
+    if unit != 1 and cols > 1:
+        raise ValueError(f"{name}: unit stride along its second dimension required")
+    return t.data_ptr(), rows, cols, ld if rows > 1 else max(cols, ld)
+
+
+def _heads(t, name, D):
+    """(address, tokens, heads, token stride) of a bf16 [T, heads, D] CUDA tensor whose heads of a token are adjacent."""
+    if t.dtype is not _BF16 or not t.is_cuda:
+        _dev(t, _BF16, name)
+    if t.dim() != 3:
+        raise ValueError(f"{name}: expected 3 dimensions")
+    T, H, d = t.shape
+    ld, hs, unit = t.stride()
+    if d != D or unit != 1 or (hs != D and H > 1):
+        raise ValueError(f"{name}: bf16 [T, heads, {D}] with a token's heads adjacent required")
+    return t.data_ptr(), T, H, ld if T > 1 else max(H * D, ld)
+
+
+def _opt(t):
+    return None if t is None else t.data_ptr()
+
+
+def quantize_tokens(X, xq=None, scale=None, rowsum=None, dev_status=None):
+    """matq_quantize_tokens.  X: bf16 [M, K].  Returns (xq int8 [M, K], scale fp32 [M], rowsum int32 [M])."""
+    x, M, K, ldx = _matrix(X, _BF16, "X")
+    if xq is None:
+        xq = torch.empty((M, K), dtype=_I8, device=X.device)
+    if scale is None:
+        scale = torch.empty(M, dtype=_F32, device=X.device)
+    if rowsum is None:
+        rowsum = torch.empty(M, dtype=_I32, device=X.device)
+    o, Mo, Ko, ldq = _matrix(xq, _I8, "xq")
+    if Mo != M or Ko != K:
+        raise ValueError("xq: int8 [M, K] required")
+    st = _lib.matq_quantize_tokens(x, M, K, ldx, o, ldq, _vector(scale, _F32, "scale", M), _vector(rowsum, _I32, "rowsum", M),
+                                   _opt(dev_status), _stream())
+    if st:
+        raise MatqError(st, "matq_quantize_tokens")
+    return xq, scale, rowsum
 
 
 def gemm_a8(xq, scale, rowsum, q, alpha, zero, y=None, out_dtype=torch.float32, flags=0, dev_status=None, c=8):
     """matq_gemm_a8.  xq, scale, rowsum: as returned by quantize_tokens; q: uint8 [N, K] codes or a slice of them (unpacked).
     Returns y [M, N], fp32 or bf16 (the type of ``y`` when it is given, ``out_dtype`` otherwise)."""
-    _dev(xq, torch.int8, "xq", 2); _dev(q, torch.uint8, "q", 2)
-    M, K = xq.shape
-    N = q.shape[0]
-    if q.shape[1] != K or xq.stride(1) != 1 or q.stride(1) != 1:
-        raise ValueError("xq [M, K] and q [N, K] with unit stride along K required")
-    _vector(scale, torch.float32, "scale", M); _vector(rowsum, torch.int32, "rowsum", M)
-    _vector(alpha, torch.float32, "alpha", N); _vector(zero, torch.float32, "zero", N)
+    x, M, K, ldx = _matrix(xq, _I8, "xq")
+    w, N, Kw, ldw = _matrix(q, _U8, "q")
+    if Kw != K:
+        raise ValueError("xq [M, K] and q [N, K] required")
     if y is None:
         y = torch.empty((M, N), dtype=out_dtype, device=xq.device)
-    if y.dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError("y: fp32 or bf16 required")
-    _dev(y, y.dtype, "y", 2)
-    if tuple(y.shape) != (M, N) or y.stride(1) != 1:
-        raise ValueError("y: [M, N] with unit stride along N required")
-    st = _lib.matq_gemm_a8(_ptr(xq), M, K, _ld(xq, K), _ptr(scale), _ptr(rowsum), _ptr(q), N, _ld(q, K), c, _ptr(alpha), _ptr(zero),
-                           OUT_F32 if y.dtype == torch.float32 else OUT_BF16, _ptr(y), _ld(y, N), int(flags),
-                           _ptr(dev_status), _stream())
-    _check(st, "matq_gemm_a8")
+    out_type = OUT_BF16 if y.dtype is _BF16 else OUT_F32
+    o, My, Ny, ldy = _matrix(y, _BF16 if out_type == OUT_BF16 else _F32, "y")
+    if My != M or Ny != N:
+        raise ValueError("y: [M, N] required")
+    st = _lib.matq_gemm_a8(x, M, K, ldx, _vector(scale, _F32, "scale", M), _vector(rowsum, _I32, "rowsum", M), w, N, ldw, c,
+                           _vector(alpha, _F32, "alpha", N), _vector(zero, _F32, "zero", N), out_type, o, ldy, flags,
+                           _opt(dev_status), _stream())
+    if st:
+        raise MatqError(st, "matq_gemm_a8")
     return y
 
 
 def _paged(k_cache, v_cache, page_table, cu_q, kv_len):
-    _dev(k_cache, torch.bfloat16, "k_cache", 4); _dev(v_cache, torch.bfloat16, "v_cache", 4)
-    if k_cache.shape != v_cache.shape or not k_cache.is_contiguous() or not v_cache.is_contiguous():
+    if k_cache.dtype is not _BF16 or not k_cache.is_cuda or v_cache.dtype is not _BF16 or not v_cache.is_cuda:
+        _dev(k_cache, _BF16, "k_cache"); _dev(v_cache, _BF16, "v_cache")
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or not k_cache.is_contiguous() or not v_cache.is_contiguous():
         raise ValueError("k_cache, v_cache: contiguous [n_pages, kv_heads, page_size, head_dim] of one shape required")
-    _dev(page_table, torch.int32, "page_table", 2)
-    B = page_table.shape[0]
-    if page_table.stride(1) != 1:
-        raise ValueError("page_table: unit stride along the pages required")
-    _vector(cu_q, torch.int32, "cu_q", B + 1); _vector(kv_len, torch.int32, "kv_len", B)
-    c = PagedKv()
-    c.k, c.v = k_cache.data_ptr(), v_cache.data_ptr()
-    c.n_pages, c.kv_heads, c.page_size, c.head_dim = k_cache.shape
-    c.batch, c.page_table, c.table_stride, c.table_width = B, page_table.data_ptr(), _ld(page_table, page_table.shape[1]), page_table.shape[1]
-    c.cu_q, c.kv_len = cu_q.data_ptr(), kv_len.data_ptr()
-    return c
-
-
-def _heads(t, name, heads, D):
-    _dev(t, torch.bfloat16, name, 3)
-    if (heads is not None and t.shape[1] != heads) or t.shape[2] != D or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != D):
-        raise ValueError(f"{name}: bf16 [T, heads, head_dim] with a token's heads adjacent required")
-    return t
+    n_pages, Hkv, ps, D = k_cache.shape
+    table, B, width, stride = _matrix(page_table, _I32, "page_table")
+    return PagedKv(k_cache.data_ptr(), v_cache.data_ptr(), n_pages, ps, Hkv, D, B, table, stride, width,
+                   _vector(cu_q, _I32, "cu_q", B + 1), _vector(kv_len, _I32, "kv_len", B)), B, Hkv, D
 
 
 def kv_append(k_cache, v_cache, page_table, cu_q, kv_len, k, v, cos_sin=None, q=None, q_out=None, interleaved=False, dev_status=None):
     """matq_kv_append.  k_cache, v_cache: bf16 [n_pages, kv_heads, page_size, head_dim]; page_table: int32 [B, pages]; cu_q: int32
     [B + 1]; kv_len: int32 [B], the new tokens included; k, v: bf16 [T, kv_heads, head_dim]; cos_sin: fp32 [max_pos, rot_dim] or None (no
     rotation); q: bf16 [T, q_heads, head_dim] or None.  Writes the caches; returns q_out (pass q itself to rotate in place)."""
-    cache = _paged(k_cache, v_cache, page_table, cu_q, kv_len)
-    Hkv, D = cache.kv_heads, cache.head_dim
-    T = k.shape[0]
-    _heads(k, "k", Hkv, D); _heads(v, "v", Hkv, D)
-    if v.shape[0] != T:
-        raise ValueError("k and v: one row per token each")
+    cache, B, Hkv, D = _paged(k_cache, v_cache, page_table, cu_q, kv_len)
+    kp, T, kh, ldk = _heads(k, "k", D)
+    vp, Tv, vh, ldv = _heads(v, "v", D)
+    if kh != Hkv or vh != Hkv or Tv != T:
+        raise ValueError("k and v: [T, kv_heads, head_dim] each required")
+    cs = None
     max_pos = rot = 0
     if cos_sin is not None:
-        _dev(cos_sin, torch.float32, "cos_sin", 2)
-        if not cos_sin.is_contiguous():
+        cs, max_pos, rot, ld = _matrix(cos_sin, _F32, "cos_sin")
+        if ld != rot:
             raise ValueError("cos_sin: contiguous [max_pos, rot_dim] required")
-        max_pos, rot = cos_sin.shape
+    qp = op = None
+    Hq = ldq = ldo = 0
     if q is not None:
-        _heads(q, "q", None, D)
+        qp, Tq, Hq, ldq = _heads(q, "q", D)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _heads(q_out, "q_out", q.shape[1], D)
-        if q.shape[0] != T or q_out.shape[0] != T:
-            raise ValueError("q and q_out: one row per token each")
+            q_out = torch.empty((T, Hq, D), dtype=_BF16, device=q.device)
+        op, To, Ho, ldo = _heads(q_out, "q_out", D)
+        if Tq != T or To != T or Ho != Hq:
+            raise ValueError("q and q_out: one row per token each, of the same heads")
     elif q_out is not None:
         raise ValueError("q_out without q")
-    st = _lib.matq_kv_append(C.byref(cache), T, _ptr(q), 0 if q is None else q.shape[1], 0 if q is None else _ld(q, q.shape[1] * D),
-                             _ptr(k), _ld(k, Hkv * D), _ptr(v), _ld(v, Hkv * D), _ptr(cos_sin), max_pos, rot, int(bool(interleaved)),
-                             _ptr(q_out), 0 if q is None else _ld(q_out, q.shape[1] * D), _ptr(dev_status), _stream())
-    _check(st, "matq_kv_append")
+    st = _lib.matq_kv_append(C.byref(cache), T, qp, Hq, ldq, kp, ldk, vp, ldv, cs, max_pos, rot, 1 if interleaved else 0, op, ldo,
+                             _opt(dev_status), _stream())
+    if st:
+        raise MatqError(st, "matq_kv_append")
     return q_out
 
 
@@ -537,23 +559,22 @@ def attn_paged(q, k_cache, v_cache, page_table, cu_q, kv_len, max_q, max_kv, sca
                workspace=None, dev_status=None):
     """matq_attn_paged.  q: bf16 [T, q_heads, head_dim]; the cache as in kv_append; max_q, max_kv: host-side upper bounds of the new
     tokens and the keys of a sequence.  scale defaults to head_dim ** -0.5.  Returns out, bf16 [T, q_heads, head_dim]."""
-    cache = _paged(k_cache, v_cache, page_table, cu_q, kv_len)
-    Hkv, D = cache.kv_heads, cache.head_dim
-    _heads(q, "q", None, D)
-    T, Hq = q.shape[0], q.shape[1]
+    cache, B, Hkv, D = _paged(k_cache, v_cache, page_table, cu_q, kv_len)
+    qp, T, Hq, ldq = _heads(q, "q", D)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=q.device)
-    _heads(out, "out", Hq, D)
-    if out.shape[0] != T:
-        raise ValueError("out: one row per token")
-    need = attn_paged_workspace_bytes(T, cache.batch, Hq, Hkv, D, max_q, max_kv, window)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    st = _lib.matq_attn_paged(C.byref(cache), T, _ptr(q), Hq, _ld(q, Hq * D), float(D ** -0.5 if scale is None else scale), float(softcap),
-                              int(window), int(max_q), int(max_kv), _ptr(out), _ld(out, Hq * D),
-                              _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
-                              _ptr(dev_status), _stream())
-    _check(st, "matq_attn_paged")
+        out = torch.empty((T, Hq, D), dtype=_BF16, device=q.device)
+    op, To, Ho, ldo = _heads(out, "out", D)
+    if To != T or Ho != Hq:
+        raise ValueError("out: one row per token, of q's heads")
+    if workspace is None:
+        need = attn_paged_workspace_bytes(T, B, Hq, Hkv, D, max_q, max_kv, window)
+        if need:
+            workspace = torch.empty(need, dtype=_U8, device=q.device)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    st = _lib.matq_attn_paged(C.byref(cache), T, qp, Hq, ldq, D ** -0.5 if scale is None else scale, softcap, window, max_q, max_kv,
+                              op, ldo, ws, ws_bytes, _opt(dev_status), _stream())
+    if st:
+        raise MatqError(st, "matq_attn_paged")
     return out
 
 

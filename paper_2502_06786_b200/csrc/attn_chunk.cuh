@@ -54,6 +54,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t s_full[C::kStages], s_empty[C::kStages], s_q, s_score[2], s_prob[2], s_pv, s_out, s_read;
     __shared__ uint32_t s_tmem;
+    __shared__ Sequence s_seq;
     __shared__ int s_timeout, s_any_bad, s_bad_key[kMaxMasked];
     __shared__ uint32_t s_bad[kMaxMasked][kKeys / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -74,25 +75,23 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(&s_tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    tc::fence_before();
-    __syncthreads();
-    tc::fence_after();
-    const uint32_t tmem = s_tmem;
-    after_previous_kernel();
-    let_next_kernel_start();
-
     const int part = (int)(blockIdx.x % (unsigned)P.splits);
     const unsigned rest = blockIdx.x / (unsigned)P.splits;
     const int h = (int)(rest % (unsigned)P.kv_heads);
     const int bt = (int)(rest / (unsigned)P.kv_heads);
     const int b = bt / P.tiles_per_seq;
-    const int64_t q0 = P.cu_q[b], n_new = P.cu_q[b + 1] - q0;
-    const int kv_len = P.kv_len[b];
-    const bool sane = q0 >= 0 && q0 + n_new <= P.T && kv_len <= P.table_width * P.page_size;
-    if (!sane && n_new > 0 && tid == 0) report(P.dev_status, MATQ_ERR_PAGE);
+    after_previous_kernel();
+    if (tid == 0) s_seq = sequence(P, b);                               // read once: all warps act on the same numbers
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    let_next_kernel_start();
+    const uint32_t tmem = s_tmem;
+    const int64_t q0 = s_seq.q0, n_new = s_seq.n_new;
+    const int kv_len = s_seq.kv_len;
     const int tok_tile = 128 / P.group, rows_tile = tok_tile * P.group;  // tokens and used rows of a query tile
     const int tok_cta = tok_tile * C::kTiles;
-    const int64_t tiles = n_new > 0 && sane ? (n_new + tok_cta - 1) / tok_cta : 0;
+    const int64_t tiles = n_new > 0 ? (n_new + tok_cta - 1) / tok_cta : 0;
     const int64_t ctx = kv_len - n_new;
     const auto lo = [&](int64_t p) { return P.window && p - P.window + 1 > 0 ? (int)(p - P.window + 1) : 0; };
 

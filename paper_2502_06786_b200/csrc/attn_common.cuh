@@ -52,6 +52,23 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 __device__ __forceinline__ bool nonfinite_bf16(uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u; }
 
+// A sequence's bounds; n_new = 0 when it has no new token or when they contradict the token arrays or the page table (reported).
+struct Sequence {
+    int64_t q0, n_new;
+    int kv_len;
+};
+__device__ __forceinline__ Sequence sequence(const Params& P, int b) {
+    Sequence s;
+    s.q0 = P.cu_q[b];
+    s.n_new = P.cu_q[b + 1] - s.q0;
+    s.kv_len = P.kv_len[b];
+    if (s.n_new > 0 && (s.q0 < 0 || s.q0 + s.n_new > P.T || s.kv_len > P.table_width * P.page_size)) {
+        report(P.dev_status, MATQ_ERR_PAGE);
+        s.n_new = 0;
+    }
+    return s;
+}
+
 // First row, in the cache seen as rows of D elements, of the slots that hold keys key .. key + count - 1 of sequence b, head h (all in one page).
 // Slots of which no query sees a key (below `first`, where a sliding window may have given its pages back, or past the sequence) are not looked up: the
 // row past the end reads as zeros.  So does a page number that is out of range, which is reported.

@@ -2,9 +2,11 @@
 // key range.  Every key and value is read once for the whole group, so the cache's bytes are what bounds it.
 //
 // A producer warp brings 64 keys and values per stage into a ring (one box per page and 64 columns, 128-byte swizzle, one lane per box,
-// so that the page numbers of a stage are fetched side by side).  Four consumer warps take 16 keys each of every stage: scores
-// by mma.sync m16n8k16 with the queries held in registers, a running maximum and sum per row, and the product with the values into 16 x D
-// fp32 accumulators in registers.  The warps meet only at the end, where their four partial results are joined in shared memory.
+// so that the page numbers of a stage are fetched side by side).  Eight consumer warps in two groups that take the stages in turn, 16 keys per
+// warp: scores by mma.sync m16n8k16, a running maximum and sum per row, and the product with the values into 16 x D fp32 accumulators in
+// registers.  The warps meet only at the end, where their partial results are joined in shared memory.
+// One CTA per SM: a unit of 16 keys is a chain of some thousand cycles in its warp, so the warps have to be eight, and the ring takes the rest of the
+// SM's shared memory (about 190 KB in flight).
 #pragma once
 
 #include "attn_common.cuh"
@@ -12,7 +14,7 @@
 namespace matq {
 namespace attn {
 
-constexpr int kDecRows = 16, kDecKeys = 64, kDecWarps = 4, kDecThreads = 32 * (kDecWarps + 1);
+constexpr int kDecRows = 16, kDecKeys = 64, kDecWarps = 8, kDecThreads = 32 * (kDecWarps + 1);
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -29,45 +31,48 @@ template <int D>
 struct DecCfg {
     static constexpr int kPanels = D / 64;                              // 64-column panels of 128-byte rows
     static constexpr int kTile = kDecKeys * D * 2;                      // bytes of 64 keys (or values)
-    static constexpr int kStages = D == 256 ? 3 : (D == 128 ? 3 : 4);
+    // Even, so that a slot of the ring always belongs to the same group of consumer warps.  With an odd count a group would meet a slot only every
+    // other phase, and its parity wait could pass on the phase before the other group's.
+    static constexpr int kStages = D == 256 ? 2 : 192 * 1024 / (2 * kTile);
+    static_assert(kStages % 2 == 0, "see above");
+    static constexpr bool kQShared = D == 256;                          // 64 registers of queries beside 128 of accumulators would not fit
+    static constexpr int kQStride = D * 2 + 16;                         // bytes; rows 16 bytes apart modulo the banks
     static constexpr int kMergeStride = D + 8;                          // floats; rows 32 bytes apart modulo the banks
-    static constexpr size_t kSmem = (size_t)kStages * 2 * kTile + 1024;
-    static_assert((size_t)kStages * 2 * kTile >= (size_t)kDecWarps * kDecRows * kMergeStride * 4, "the join reuses the ring");
+    static constexpr size_t kRing = (size_t)kStages * 2 * kTile, kMerge = (size_t)kDecWarps * kDecRows * kMergeStride * 4;
+    static constexpr size_t kSmem = (kRing > kMerge ? kRing : kMerge) + 1024;         // the join at the end reuses the ring
 };
 
 template <int D>
-__global__ void __launch_bounds__(kDecThreads)
+__global__ void __launch_bounds__(kDecThreads, 1)
 attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Params P) {
     using C = DecCfg<D>;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t s_full[C::kStages], s_empty[C::kStages], s_tile;
     __shared__ float s_m[kDecWarps][kDecRows], s_l[kDecWarps][kDecRows];
     __shared__ int s_timeout, s_gave_up[kDecWarps];
+    __shared__ Sequence s_seq;
+    __shared__ __align__(16) unsigned char s_q[C::kQShared ? kDecRows * C::kQStride : 16];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned char* ring = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
 
     if (tid == 0) {
-        for (int s = 0; s < C::kStages; ++s) { tc::mbar_init(tc::smem_u32(&s_full[s]), 1); tc::mbar_init(tc::smem_u32(&s_empty[s]), kDecWarps); }
+        for (int s = 0; s < C::kStages; ++s) { tc::mbar_init(tc::smem_u32(&s_full[s]), 1); tc::mbar_init(tc::smem_u32(&s_empty[s]), kDecWarps / 2); }
         tc::mbar_init(tc::smem_u32(&s_tile), kDecWarps);
         tc::mbar_init_fence();
         s_timeout = 0;
     }
-    __syncthreads();
-    after_previous_kernel();
-    let_next_kernel_start();
-
     const int part = (int)(blockIdx.x % (unsigned)P.splits);
     const unsigned rest = blockIdx.x / (unsigned)P.splits;
     const int h = (int)(rest % (unsigned)P.kv_heads);
     const int bt = (int)(rest / (unsigned)P.kv_heads);
     const int b = bt / P.tiles_per_seq;
-    const int64_t q0 = P.cu_q[b], n_new = P.cu_q[b + 1] - q0;
-    const int kv_len = P.kv_len[b];
+    after_previous_kernel();
+    if (tid == 0) s_seq = sequence(P, b);                               // read once: all warps act on the same numbers
+    __syncthreads();
+    let_next_kernel_start();
+    const int64_t q0 = s_seq.q0, n_new = s_seq.n_new;
+    const int kv_len = s_seq.kv_len;
     if (n_new <= 0) return;
-    if (q0 < 0 || q0 + n_new > P.T || kv_len > P.table_width * P.page_size) {     // contradicts the token arrays or the page table
-        if (tid == 0) report(P.dev_status, MATQ_ERR_PAGE);
-        return;
-    }
     const int64_t n_rows = n_new * P.group, tiles = (n_rows + kDecRows - 1) / kDecRows;
     const int64_t ctx = kv_len - n_new;                                 // position of the first new token (negative: it sees nothing)
 
@@ -122,7 +127,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 
         // ---------------- consumers
         const int g = lane >> 2, c2 = (lane & 3) * 2;
-        uint32_t qf[D / 16][4];
+        uint32_t qf[C::kQShared ? 1 : D / 16][4];
         int see_hi[2], see_lo[2];                                       // rows g and g + 8 see the keys [see_lo, see_hi]
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -132,11 +137,23 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             see_hi[i] = live ? (int)(ctx + tok) : p_hi;
             see_lo[i] = lo(see_hi[i]);
             const __nv_bfloat16* src = P.q + (q0 + tok) * P.ldq + (int64_t)(h * P.group + (live ? (int)(r - tok * P.group) : 0)) * D;
+            if constexpr (!C::kQShared) {
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                qf[ks][i] = live ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + c2) : 0u;
-                qf[ks][2 + i] = live ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + c2) : 0u;
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    qf[ks][i] = live ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + c2) : 0u;
+                    qf[ks][2 + i] = live ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8 + c2) : 0u;
+                }
             }
+        }
+        if constexpr (C::kQShared) {
+            for (int x = tid; x < kDecRows * (D / 8); x += kDecWarps * 32) {
+                const int rr = x / (D / 8), ch = x % (D / 8);
+                const int64_t r = r0 + rr, tok = r <= r1 ? r / P.group : 0;
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if (r <= r1) v = *reinterpret_cast<const uint4*>(P.q + (q0 + tok) * P.ldq + (int64_t)(h * P.group + (int)(r - tok * P.group)) * D + ch * 8);
+                *reinterpret_cast<uint4*>(s_q + rr * C::kQStride + ch * 16) = v;
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
         }
         float o[D / 8][4];
 #pragma unroll
@@ -146,13 +163,13 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
         const Score sc(P.scale, P.softcap);
         bool ok = true;
-        for (int i = 0; i < n_it; ++i) {
+        for (int i = (it ^ (warp >> 2)) & 1; i < n_it; i += 2) {        // this group's stages
             const int s = (it + i) % C::kStages;
             ok = tc::mbar_wait(tc::smem_u32(&s_full[s]), (uint32_t)((it + i) / C::kStages) & 1u, P.wait_cycles);
             if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-            const int j0 = k_lo + i * kDecKeys + warp * 16;             // this warp's first key
+            const int j0 = k_lo + i * kDecKeys + (warp & 3) * 16;       // this warp's first key
             if (j0 < k_hi && j0 + 15 >= first) {
-                const uint32_t kb = tc::smem_u32(ring) + (uint32_t)(s * 2) * C::kTile + (uint32_t)(warp * 16) * 128;
+                const uint32_t kb = tc::smem_u32(ring) + (uint32_t)(s * 2) * C::kTile + (uint32_t)((warp & 3) * 16) * 128;
                 const uint32_t vb = kb + C::kTile;
                 float sv[2][4] = {};
                 const int mi = lane >> 3, mr = lane & 7;
@@ -161,8 +178,15 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
                     uint32_t r[4];
                     const int key = (mi >> 1) * 8 + mr, ch = (2 * ks + (mi & 1)) & 7;
                     ldsm4(r, kb + (uint32_t)(ks / 4) * (kDecKeys * 128) + key * 128 + ((ch ^ (key & 7)) << 4));
-                    mma16816(sv[0], qf[ks], r[0], r[1]);
-                    mma16816(sv[1], qf[ks], r[2], r[3]);
+                    if constexpr (C::kQShared) {
+                        uint32_t a[4];
+                        ldsm4(a, tc::smem_u32(s_q) + ((mi & 1) * 8 + mr) * C::kQStride + ks * 32 + (mi >> 1) * 16);
+                        mma16816(sv[0], a, r[0], r[1]);
+                        mma16816(sv[1], a, r[2], r[3]);
+                    } else {
+                        mma16816(sv[0], qf[ks], r[0], r[1]);
+                        mma16816(sv[1], qf[ks], r[2], r[3]);
+                    }
                 }
                 const bool masked = j0 + 15 > p_lo || j0 < all_from;
                 // fold scale and cap in; hide what a row does not see
@@ -260,7 +284,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             if (lane == 0) tc::mbar_arrive(tc::smem_u32(&s_empty[s]));
         }
         it += n_it;
-        // ---------------- join of the four warps (their key sets are disjoint)
+        // ---------------- join of the warps (their key sets are disjoint)
         if (lane == 0) s_gave_up[warp] = !ok;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -268,27 +292,36 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
             if ((lane & 3) == 0) { s_m[warp][g + 8 * i] = m[i]; s_l[warp][g + 8 * i] = l[i]; }
         }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (s_gave_up[0] | s_gave_up[1] | s_gave_up[2] | s_gave_up[3]) {   // written before the barrier only: the warps leave together and nothing is stored
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        int gave_up = 0;
+#pragma unroll
+        for (int w = 0; w < kDecWarps; ++w) gave_up |= s_gave_up[w];
+        if (gave_up) {                                                   // written before the barrier only: the warps leave together and nothing is stored
             *(volatile int*)&s_timeout = 1;
             break;
         }
+        const auto row_max = [&](int r) {
+            float mx = s_m[0][r];
+#pragma unroll
+            for (int w = 1; w < kDecWarps; ++w) mx = fmaxf(mx, s_m[w][r]);
+            return mx;
+        };
         float* merge = reinterpret_cast<float*>(ring);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int r = g + 8 * i;
-            const float mx = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+            const float mx = row_max(r);
             const float f = mx == -INFINITY ? 0.f : ex2(m[i] - mx);
 #pragma unroll
             for (int j = 0; j < D / 8; ++j)
                 *reinterpret_cast<float2*>(merge + (size_t)(warp * kDecRows + r) * C::kMergeStride + j * 8 + c2) = make_float2(o[j][2 * i] * f, o[j][2 * i + 1] * f);
         }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        asm volatile("bar.sync 1, 256;" ::: "memory");
         {
-            const int r = tid >> 3, c0 = tid & 7;                       // eight threads per row, four columns at a time
+            const int r = tid >> 4, c0 = tid & 15;                      // sixteen threads per row, four columns at a time
             const int64_t rr = r0 + r;
             if (rr <= r1) {
-                const float mx = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+                const float mx = row_max(r);
                 float sum = 0.f;
 #pragma unroll
                 for (int w = 0; w < kDecWarps; ++w) sum += mx == -INFINITY ? s_l[w][r] : s_l[w][r] * ex2(s_m[w][r] - mx);
@@ -297,8 +330,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
                 const float inv = any ? 1.f / sum : 0.f;
                 if (P.splits > 1 && c0 == 0) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(mx, sum);
 #pragma unroll
-                for (int j = 0; j < D / 32; ++j) {
-                    const int c = j * 32 + c0 * 4;
+                for (int j = 0; j < D / 64; ++j) {
+                    const int c = j * 64 + c0 * 4;
                     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                     for (int w = 0; w < kDecWarps; ++w) {
@@ -315,7 +348,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        asm volatile("bar.sync 1, 256;" ::: "memory");
         if (lane == 0) tc::mbar_arrive(tc::smem_u32(&s_tile));
     }
     if (warp == kDecWarps)                                              // no copy may be in flight when the CTA ends, whatever became of its consumers

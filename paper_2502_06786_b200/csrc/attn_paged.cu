@@ -23,7 +23,7 @@ inline Plan plan(int batch, int kv_heads, int group, int D, int64_t max_q, int64
     if (window > 0 && window + tok + 16 < range) range = window + tok + 16;
     range = (range + keys - 1) / keys + 1;                              // steps; one more when the window starts inside one
     const int64_t ctas = p.tiles_per_seq * batch * kv_heads;
-    int64_t splits = ctas > 0 ? (p.kind == 0 ? (2 * sms + ctas - 1) / ctas : sms / ctas) : 1;
+    int64_t splits = ctas > 0 ? (p.kind == 0 && ctas >= sms ? (2 * sms + ctas - 1) / ctas : sms / ctas) : 1;
     if (splits > range / 4) splits = range / 4;                         // four steps per part at least
     if (splits > kMaxSplits) splits = kMaxSplits;
     if (splits < 1) splits = 1;

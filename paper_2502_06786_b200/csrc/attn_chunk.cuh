@@ -2,8 +2,8 @@
 //
 // A query tile is 128 accumulator rows: floor(128 / group) tokens times the heads of one key head's group, so that a key is read once for the
 // whole group.  A CTA takes kTiles such tiles and walks the keys that they see, kKeys at a time:
-//   warp 4 kTiles      producer: queries once, then keys and values into a ring (one box per page and 64 columns, 128-byte swizzle);
-//   warp 4 kTiles + 1  issues S = Q K^T and O += P V (tcgen05.mma, both accumulators and P in tensor memory);
+//   warps 4 kTiles, 4 kTiles + 1  producers: queries once and keys; values; a ring each (one box per page and 64 columns, 128-byte swizzle);
+//   warp 4 kTiles + 2  issues S = Q K^T and O += P V (tcgen05.mma, both accumulators and P in tensor memory);
 //   warps 0 .. 4 kTiles - 1  softmax, one thread per row: S from tensor memory, exponentials, P back over S as bf16.
 // P takes the place of S: the product with V that reads it is issued before the scores that overwrite it.  The row maximum is a reference only: it
 // moves, and O is rescaled, when a score exceeds it by more than 2^8, which leaves p <= 256 and the quotient O / l unchanged.
@@ -26,11 +26,11 @@ struct ChunkCfg {
     static constexpr int kPanels = D / 64;
     static constexpr int kQBytes = 128 * D * 2;                         // one query tile
     static constexpr int kKvBytes = kKeys * D * 2;                      // the keys, or the values, of a step
-    static constexpr int kStages = D == 64 ? 8 : 5;
+    static constexpr int kStagesK = D == 64 ? 4 : 3, kStagesV = D == 64 ? 4 : TILES * D == 128 ? 3 : 2;
     static constexpr int kSoft = kTiles * 128;                          // softmax threads
-    static constexpr int kThreads = kSoft + 64;
+    static constexpr int kThreads = kSoft + 96;
     static constexpr int kTmemO = 256;                                  // first column of the output accumulators; S starts at column 0
-    static constexpr size_t kSmem = (size_t)kTiles * kQBytes + (size_t)kStages * kKvBytes + 1024;
+    static constexpr size_t kSmem = (size_t)kTiles * kQBytes + (size_t)(kStagesK + kStagesV) * kKvBytes + 1024;
 };
 
 __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* d) {
@@ -52,17 +52,20 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     using C = ChunkCfg<D, TILES>;
     constexpr int kKeys = C::kKeys;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t s_full[C::kStages], s_empty[C::kStages], s_q, s_score[2], s_prob[2], s_pv, s_out, s_read;
+    __shared__ __align__(8) uint64_t s_kfull[C::kStagesK], s_kempty[C::kStagesK], s_vfull[C::kStagesV], s_vempty[C::kStagesV], s_q, s_score[2], s_prob[2], s_pv, s_out, s_read;
     __shared__ uint32_t s_tmem;
     __shared__ Sequence s_seq;
     __shared__ int s_timeout, s_any_bad, s_bad_key[kMaxMasked];
     __shared__ uint32_t s_bad[kMaxMasked][kKeys / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned char* smem = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
-    unsigned char* ring = smem + C::kTiles * C::kQBytes;
+    unsigned char* ring_k = smem + C::kTiles * C::kQBytes;
+    unsigned char* ring_v = ring_k + C::kStagesK * C::kKvBytes;
+    constexpr int kWarpK = C::kSoft / 32, kWarpV = kWarpK + 1, kWarpMma = kWarpK + 2;
 
     if (tid == 0) {
-        for (int s = 0; s < C::kStages; ++s) { tc::mbar_init(tc::smem_u32(&s_full[s]), 1); tc::mbar_init(tc::smem_u32(&s_empty[s]), 1); }
+        for (int s = 0; s < C::kStagesK; ++s) { tc::mbar_init(tc::smem_u32(&s_kfull[s]), 1); tc::mbar_init(tc::smem_u32(&s_kempty[s]), 1); }
+        for (int s = 0; s < C::kStagesV; ++s) { tc::mbar_init(tc::smem_u32(&s_vfull[s]), 1); tc::mbar_init(tc::smem_u32(&s_vempty[s]), 1); }
         tc::mbar_init(tc::smem_u32(&s_q), 1);
         for (int t = 0; t < 2; ++t) { tc::mbar_init(tc::smem_u32(&s_score[t]), 1); tc::mbar_init(tc::smem_u32(&s_prob[t]), 128); }
         tc::mbar_init(tc::smem_u32(&s_pv), 1);
@@ -71,7 +74,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         tc::mbar_init_fence();
         s_timeout = 0;
     }
-    if (warp == C::kSoft / 32 + 1) {
+    if (warp == kWarpMma) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(&s_tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -109,10 +112,18 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         const int k_lo = n_it ? (int)k_lo64 : 0;
         const auto is_masked = [&](int j0) { return j0 + kKeys - 1 > p_lo || j0 < all_from; };
 
-        if (warp == C::kSoft / 32) {
-            // ---------------- producer
+        if (warp == kWarpK || warp == kWarpV) {
+            // ---------------- producers
+            const bool v = warp == kWarpV;
+            const CUtensorMap* tm = v ? &tm_v : &tm_k;
+            const int stages = v ? C::kStagesV : C::kStagesK;
+            const int rows_box = min(P.page_size, kKeys), runs = kKeys / rows_box, boxes = runs * C::kPanels;       // powers of two, 32 boxes at most
+            const int run = lane & (runs - 1), x = (lane / runs) * 64;  // this lane's box of a step
+            const uint32_t dst = tc::smem_u32(v ? ring_v : ring_k) + (uint32_t)(x >> 6) * (kKeys * 128) + (uint32_t)run * rows_box * 128;
+            const uint32_t full = tc::smem_u32(v ? s_vfull : s_kfull), empty = tc::smem_u32(v ? s_vempty : s_kempty);
+            const auto row_of = [&](int i) { return cache_row(P, b, h, (int64_t)k_lo + (int64_t)i * kKeys + run * rows_box, rows_box, first, kv_len); };
             bool ok = true;
-            if (n_it > 0) {
+            if (n_it > 0 && !v) {
                 if (round > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_out), (uint32_t)(round - 1) & 1u, P.wait_cycles));
                 if (ok && !P.hold && lane == 0) {
                     q_issued = round + 1;
@@ -123,39 +134,31 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                                             (int)(q0 + t0 + t * tok_tile), tc::smem_u32(&s_q));
                 }
             }
-            const int rows_box = min(P.page_size, kKeys), runs = kKeys / rows_box, boxes = runs * C::kPanels;
-            int next_row = lane < runs && n_it > 0 ? cache_row(P, b, h, (int64_t)k_lo + lane * rows_box, rows_box, first, kv_len) : 0;
+            int next_row = n_it > 0 ? row_of(0) : 0;                    // a step's pages are looked up while the one before waits
+            int s = it % stages;
+            uint32_t phase = (uint32_t)(it / stages) & 1u;
             for (int i = 0; i < n_it && ok; ++i) {
                 const int row = next_row;
-                if (lane < runs && i + 1 < n_it) next_row = cache_row(P, b, h, (int64_t)k_lo + (i + 1) * kKeys + lane * rows_box, rows_box, first, kv_len);
-                for (int v = 0; v < 2; ++v) {
-                    const int u = 2 * (it + i) + v, s = u % C::kStages;
-                    ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_empty[s]), ((uint32_t)(u / C::kStages) & 1u) ^ 1u, P.wait_cycles)) && !P.hold;
-                    if (!ok) break;
-                    const uint32_t bar = tc::smem_u32(&s_full[s]);
-                    if (lane == 0) tc::mbar_expect_tx(bar, C::kKvBytes);
-                    __syncwarp();
-                    // runs and panels are powers of two: a box per lane, at most 32 of them
-                    const int run = lane & (runs - 1), panel = lane / runs;
-                    const int y = __shfl_sync(0xffffffffu, row, run);
-                    if (lane < boxes)
-                        tc::tma_load_2d(tc::smem_u32(ring) + (uint32_t)s * C::kKvBytes + (uint32_t)panel * (kKeys * 128) + (uint32_t)run * rows_box * 128,
-                                        v ? &tm_v : &tm_k, panel * 64, y, bar);
-                    issued = u + 1;
-                }
+                if (i + 1 < n_it) next_row = row_of(i + 1);
+                ok = __all_sync(0xffffffffu, tc::mbar_wait(empty + 8 * s, phase ^ 1u, P.wait_cycles)) && !P.hold;
+                if (!ok) break;
+                if (lane == 0) tc::mbar_expect_tx(full + 8 * s, C::kKvBytes);   // the phase cannot end before this arrival, whichever copy comes first
+                if (lane < boxes) tc::tma_load_2d(dst + (uint32_t)s * C::kKvBytes, tm, x, row, full + 8 * s);
+                ++issued;
+                if (++s == stages) { s = 0; phase ^= 1u; }
             }
             if (!ok) {
                 if (lane == 0) *(volatile int*)&s_timeout = 1;
                 break;
             }
-        } else if (warp == C::kSoft / 32 + 1) {
+        } else if (warp == kWarpMma) {
             // ---------------- tensor cores: one thread issues
             if (lane == 0 && n_it > 0) {
                 bool ok = tc::mbar_wait(tc::smem_u32(&s_q), (uint32_t)round & 1u, P.wait_cycles);
-                const auto wait_kv = [&](int u) { return tc::mbar_wait(tc::smem_u32(&s_full[u % C::kStages]), (uint32_t)(u / C::kStages) & 1u, P.wait_cycles); };
-                const auto kv_at = [&](int u) { return tc::smem_u32(ring) + (uint32_t)(u % C::kStages) * C::kKvBytes; };
+                const auto wait_k = [&](int i) { return tc::mbar_wait(tc::smem_u32(&s_kfull[(it + i) % C::kStagesK]), (uint32_t)((it + i) / C::kStagesK) & 1u, P.wait_cycles); };
+                const auto wait_v = [&](int i) { return tc::mbar_wait(tc::smem_u32(&s_vfull[(it + i) % C::kStagesV]), (uint32_t)((it + i) / C::kStagesV) & 1u, P.wait_cycles); };
                 const auto scores = [&](int t, int i) {                 // S_t = Q_t K_i^T
-                    const uint32_t a = tc::smem_u32(smem) + (C::kTiles == 2 ? t * C::kQBytes : 0), kb = kv_at(2 * (it + i));
+                    const uint32_t a = tc::smem_u32(smem) + (C::kTiles == 2 ? t * C::kQBytes : 0), kb = tc::smem_u32(ring_k) + (uint32_t)((it + i) % C::kStagesK) * C::kKvBytes;
                     const uint32_t d = tmem + t * kKeys;
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks)
@@ -165,51 +168,52 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     tc::tc_commit(tc::smem_u32(&s_score[t]));
                 };
                 const auto product = [&](int t, int i) {                // O_t += P_t V_i
-                    const uint32_t vb = kv_at(2 * (it + i) + 1), d = tmem + C::kTmemO + (C::kTiles == 2 ? t * D : 0);
+                    const uint32_t vb = tc::smem_u32(ring_v) + (uint32_t)((it + i) % C::kStagesV) * C::kKvBytes, d = tmem + C::kTmemO + (C::kTiles == 2 ? t * D : 0);
 #pragma unroll
                     for (int ks = 0; ks < kKeys / 16; ++ks)
                         asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
                                      ::"r"(d), "r"(tmem + t * kKeys + ks * 8), "l"(tc::sw128_desc(vb + ks * 2048, kKeys * 128, 1024)),
                                        "r"(idesc_bf16(D, true)), "r"((i > 0 || ks > 0) ? 1u : 0u) : "memory");
                 };
-                const auto free_kv = [&](int u) { tc::tc_commit(tc::smem_u32(&s_empty[u % C::kStages])); };
-                if (ok) ok = wait_kv(2 * it);
+                const auto free_k = [&](int i) { tc::tc_commit(tc::smem_u32(&s_kempty[(it + i) % C::kStagesK])); };
+                const auto free_v = [&](int i) { tc::tc_commit(tc::smem_u32(&s_vempty[(it + i) % C::kStagesV])); };
+                if (ok) ok = wait_k(0);
                 tc::fence_after();
                 if (C::kTiles == 2) {
-                    if (ok) { scores(0, 0); scores(1, 0); free_kv(2 * it); }
+                    if (ok) { scores(0, 0); scores(1, 0); free_k(0); }
                     for (int i = 0; i < n_it && ok; ++i) {
                         for (int t = 0; t < 2 && ok; ++t) {
-                            ok = tc::mbar_wait(tc::smem_u32(&s_prob[t]), (uint32_t)(it + i) & 1u, P.wait_cycles) && wait_kv(2 * (it + i) + 1);
+                            ok = tc::mbar_wait(tc::smem_u32(&s_prob[t]), (uint32_t)(it + i) & 1u, P.wait_cycles) && wait_v(i);
                             if (ok && i == 0 && t == 0 && round > 0) ok = tc::mbar_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles);
                             if (!ok) break;
                             tc::fence_after();
                             product(t, i);
-                            if (t == 1) free_kv(2 * (it + i) + 1);
+                            if (t == 1) free_v(i);
                             if (i + 1 < n_it) {
-                                ok = wait_kv(2 * (it + i + 1));
+                                ok = wait_k(i + 1);
                                 if (!ok) break;
                                 tc::fence_after();
                                 scores(t, i + 1);
-                                if (t == 1) free_kv(2 * (it + i + 1));
+                                if (t == 1) free_k(i + 1);
                             }
                         }
                     }
                 } else {
-                    if (ok) { scores(it & 1, 0); free_kv(2 * it); }
+                    if (ok) { scores(it & 1, 0); free_k(0); }
                     for (int i = 0; i < n_it && ok; ++i) {
                         if (i + 1 < n_it) {
-                            ok = wait_kv(2 * (it + i + 1));
+                            ok = wait_k(i + 1);
                             if (!ok) break;
                             tc::fence_after();
                             scores((it + i + 1) & 1, i + 1);
-                            free_kv(2 * (it + i + 1));
+                            free_k(i + 1);
                         }
-                        ok = tc::mbar_wait(tc::smem_u32(&s_prob[(it + i) & 1]), (uint32_t)((it + i) >> 1) & 1u, P.wait_cycles) && wait_kv(2 * (it + i) + 1);
+                        ok = tc::mbar_wait(tc::smem_u32(&s_prob[(it + i) & 1]), (uint32_t)((it + i) >> 1) & 1u, P.wait_cycles) && wait_v(i);
                         if (ok && i == 0 && round > 0) ok = tc::mbar_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles);
                         if (!ok) break;
                         tc::fence_after();
                         product((it + i) & 1, i);
-                        free_kv(2 * (it + i) + 1);
+                        free_v(i);
                         tc::tc_commit(tc::smem_u32(&s_pv));
                     }
                 }
@@ -302,13 +306,13 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (masked) {
                     // A weight of zero does not silence a NaN or Inf.  Values that no row sees become zero; non-finite ones that only some rows
                     // see leave the tile, and those rows get them at the end.  Every thread looks at one key, all or half of it.
-                    const int u = 2 * gi + 1;
-                    if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_full[u % C::kStages]), (uint32_t)(u / C::kStages) & 1u, P.wait_cycles));
+                    // (The slot's last use was freed before these scores were issued, so the parity wait cannot pass a phase early.)
+                    if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_vfull[gi % C::kStagesV]), (uint32_t)(gi / C::kStagesV) & 1u, P.wait_cycles));
                     if (ok) {
                         constexpr int kShare = C::kSoft / kKeys;         // threads per key: 2
                         const int key = tid % kKeys, j = j0 + key;
                         const bool unseen = j > p_hi || j < first, all = j <= p_lo && j >= all_from;
-                        const uint32_t vb = tc::smem_u32(ring) + (uint32_t)(u % C::kStages) * C::kKvBytes + key * 128;
+                        const uint32_t vb = tc::smem_u32(ring_v) + (uint32_t)(gi % C::kStagesV) * C::kKvBytes + key * 128;
                         bool bad = false;
                         if (!all) {
                             for (int ch = tid / kKeys; ch < D / 8; ch += kShare) {
@@ -401,15 +405,16 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         it += n_it;
         if (n_it > 0) ++round;
     }
-    if (warp == C::kSoft / 32) {                                        // no copy may be in flight when the CTA ends, whatever became of its consumer
-        for (int u = max(0, issued - C::kStages); u < issued; ++u)
-            tc::mbar_wait(tc::smem_u32(&s_full[u % C::kStages]), (uint32_t)(u / C::kStages) & 1u, P.wait_cycles);
+    if (warp == kWarpK || warp == kWarpV) {                             // no copy may be in flight when the CTA ends, whatever became of its consumer
+        const int stages = warp == kWarpV ? C::kStagesV : C::kStagesK;
+        for (int u = max(0, issued - stages); u < issued; ++u)
+            tc::mbar_wait(tc::smem_u32(warp == kWarpV ? s_vfull : s_kfull) + 8 * (u % stages), (uint32_t)(u / stages) & 1u, P.wait_cycles);
         if (q_issued) tc::mbar_wait(tc::smem_u32(&s_q), (uint32_t)(q_issued - 1) & 1u, P.wait_cycles);
     }
     tc::fence_before();
     __syncthreads();
     if (tid == 0 && s_timeout) report(P.dev_status, MATQ_ERR_TIMEOUT);
-    if (warp == C::kSoft / 32 + 1)
+    if (warp == kWarpMma)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 

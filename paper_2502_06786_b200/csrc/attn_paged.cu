@@ -6,7 +6,8 @@ namespace matq {
 namespace attn {
 
 struct Plan {
-    int kind;                    // 0: 16-row tiles; 1, 2: query tiles of 128 rows per CTA
+    int kind;                    // 1, 2: attn_chunk with so many query tiles of 128 rows per CTA; 8, 16: attn_decode with so many rows
+    int keys;                    // keys of a step: the parts of the key range are multiples of it
     int64_t tiles_per_seq, splits, split_keys;
 };
 
@@ -14,17 +15,18 @@ struct Plan {
 inline Plan plan(int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
     Plan p;
     const int64_t rows = max_q * group;
-    p.kind = rows <= kDecRows ? 0 : (rows <= 128 || D == 256 ? 1 : 2);
-    const int keys = p.kind == 0 || D == 256 ? 64 : 128;
-    const int64_t tok = p.kind == 0 ? 0 : (int64_t)(128 / group) * p.kind;       // tokens per CTA
-    p.tiles_per_seq = p.kind == 0 ? (rows + kDecRows - 1) / kDecRows : (max_q + tok - 1) / tok;
+    p.kind = rows <= 8 ? 8 : rows <= 16 ? 16 : (rows <= 128 || D == 256 ? 1 : 2);
+    const bool decode = p.kind >= 8;
+    const int keys = p.keys = decode ? (D == 256 ? 32 : 64) : (D == 256 ? 64 : 128);
+    const int64_t tok = decode ? 0 : (int64_t)(128 / group) * p.kind;   // tokens per CTA
+    p.tiles_per_seq = decode ? (rows + p.kind - 1) / p.kind : (max_q + tok - 1) / tok;
     if (p.tiles_per_seq < 1) p.tiles_per_seq = 1;
     int64_t range = max_kv;                                             // keys that a tile can see
     if (window > 0 && window + tok + 16 < range) range = window + tok + 16;
     range = (range + keys - 1) / keys + 1;                              // steps; one more when the window starts inside one
     const int64_t ctas = p.tiles_per_seq * batch * kv_heads;
-    int64_t splits = ctas > 0 ? (p.kind == 0 && ctas >= sms ? (2 * sms + ctas - 1) / ctas : sms / ctas) : 1;
-    if (splits > range / 4) splits = range / 4;                         // four steps per part at least
+    int64_t splits = ctas > 0 ? (decode && ctas >= sms ? (2 * sms + ctas - 1) / ctas : sms / ctas) : 1;
+    if (splits > range * keys / 256) splits = range * keys / 256;       // 256 keys per part at least
     if (splits > kMaxSplits) splits = kMaxSplits;
     if (splits < 1) splits = 1;
     const int64_t per = (range + splits - 1) / splits;
@@ -52,11 +54,12 @@ inline bool query_map(CUtensorMap* tm, const void* q, int64_t T, int q_heads, in
     return tc::make_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, q, dims, strides, box);
 }
 
-template <int D>
+template <int D, int NT>
 int launch_decode(const CUtensorMap& tk, const CUtensorMap& tv, const Params& P, unsigned grid, cudaStream_t s) {
+    using C = DecCfg<D, NT>;
     static std::atomic<unsigned long long> smem_ok{0};
-    if (!opt_in_max_smem(attn_decode_kernel<D>, smem_ok)) return MATQ_ERR_CUDA;
-    if (launch_overlapped(attn_decode_kernel<D>, dim3(grid), dim3(kDecThreads), DecCfg<D>::kSmem, s, tk, tv, P) != cudaSuccess) {
+    if (!opt_in_max_smem(attn_decode_kernel<D, NT>, smem_ok)) return MATQ_ERR_CUDA;
+    if (launch_overlapped(attn_decode_kernel<D, NT>, dim3(grid), dim3(C::kThreads), C::kSmem, s, tk, tv, P) != cudaSuccess) {
         cudaGetLastError();
         return MATQ_ERR_CUDA;
     }
@@ -78,8 +81,10 @@ int launch_chunk(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap
 template <int D>
 int launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const Params& P, int kind, unsigned grid, cudaStream_t s) {
     int st;
-    if (kind == 0) {
-        st = launch_decode<D>(tk, tv, P, grid, s);
+    if (kind == 8) {
+        st = launch_decode<D, 1>(tk, tv, P, grid, s);
+    } else if (kind == 16) {
+        st = launch_decode<D, 2>(tk, tv, P, grid, s);
     } else if (kind == 1) {
         st = launch_chunk<D, 1>(tq, tk, tv, P, grid, s);
     } else {
@@ -142,7 +147,7 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     const int64_t grid = p.splits * cache->kv_heads * cache->batch * p.tiles_per_seq;
     if (grid >= (1ll << 31) || (p.splits > 1 && T * q_heads >= (1ll << 31))) return MATQ_ERR_SHAPE;
     CUtensorMap tq, tk, tv;
-    const int keys = p.kind == 0 || D == 256 ? 64 : 128, box = ps < keys ? ps : keys;
+    const int box = ps < p.keys ? ps : p.keys;
     if (!cache_map(&tk, cache->k, rows, D, box) || !cache_map(&tv, cache->v, rows, D, box) || !query_map(&tq, q, T, q_heads, D, ldq, group)) return MATQ_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (D == 64) return launch<64>(tq, tk, tv, P, p.kind, (unsigned)grid, s);

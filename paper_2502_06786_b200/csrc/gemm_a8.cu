@@ -186,6 +186,160 @@ gemm_a8_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(P.tmem_cols) : "memory");
 }
 
+// ---------------------------------------------------------------- many tokens: pairs of SMs
+//
+// Two CTAs of a cluster share a tile of 256 channels x nt tokens (tcgen05.mma with cta_group::2): each holds its 128 channels and half of the
+// tokens in shared memory and its 128 channels x nt sums in tensor memory, so that a byte brought into an SM meets twice the products of
+// a CTA by itself.  The even CTA issues the products for both; a stage's barrier lives in it and collects both CTAs' copies, and one commit frees
+// the stage in both.  The kernel is persistent: a pair takes every (number of pairs)-th tile, two accumulators take turns, and eight
+// warps store one tile while the next is summed.  Channels are the accumulator's rows, so a thread keeps its channel's alpha and z in registers and a
+// warp's stores run along a token's outputs.
+constexpr int kPairWarps = 8, kPairThreads = 32 * (2 + kPairWarps), kPairStages = 6;
+constexpr int kPairStageBytes = 2 * kBM * kBK;       // 128 channels and up to 128 tokens
+
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+// a copy into this CTA whose bytes are counted by a barrier of either CTA of the pair
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* tm, int x, int y, uint32_t cluster_bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(tm), "r"(x), "r"(y), "r"(cluster_bar) : "memory");
+}
+// arrives on the same barrier of both CTAs when every product issued so far has ended
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+gemm_a8_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const Params P) {
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t s_full[kPairStages], s_empty[kPairStages], s_acc[2], s_read[2];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_timeout;
+    __shared__ float s_xs[2][kMaxNT];
+    __shared__ int s_xsum[2][kMaxNT];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t rank = blockIdx.x & 1u;
+    unsigned char* ring = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);      // the same offset in both CTAs
+
+    if (tid == 0) {
+        for (int s = 0; s < kPairStages; ++s) { tc::mbar_init(tc::smem_u32(&s_full[s]), 1); tc::mbar_init(tc::smem_u32(&s_empty[s]), 1); }
+        for (int a = 0; a < 2; ++a) { tc::mbar_init(tc::smem_u32(&s_acc[a]), 1); tc::mbar_init(tc::smem_u32(&s_read[a]), 2 * kPairWarps); }
+        tc::mbar_init_fence();
+        s_timeout = 0;
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(&s_tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc::fence_before();
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned; barrier.cluster.wait.acquire.aligned;" ::: "memory");     // the other CTA's barriers are there
+    tc::fence_after();
+    const uint32_t tmem = s_tmem;
+    after_previous_kernel();
+    let_next_kernel_start();
+
+    const int m_tiles = (int)((P.M + P.nt - 1) / P.nt), n_tiles = (int)((P.N + 2 * kBM - 1) / (2 * kBM)), tiles = m_tiles * n_tiles;
+    const int pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1), half = P.nt / 2;
+    int u = 0, round = 0;                                               // stages and tiles so far
+
+    if (warp == 0) {
+        if (lane == 0 && !P.hold) {
+            bool ok = true;
+            for (int tile = pair; tile < tiles && ok; tile += pairs) {
+                const int m0 = tile % m_tiles * P.nt + (int)rank * half, n0 = tile / m_tiles * (2 * kBM) + (int)rank * kBM;
+                for (int kb = 0; kb < P.nkb; ++kb, ++u) {
+                    const int s = u % kPairStages;
+                    if (!(ok = tc::mbar_wait(tc::smem_u32(&s_empty[s]), ((uint32_t)(u / kPairStages) & 1u) ^ 1u, P.wait_cycles))) { *(volatile int*)&s_timeout = 1; break; }
+                    const uint32_t bar = tc::smem_u32(&s_full[s]), dst = tc::smem_u32(ring) + s * kPairStageBytes;
+                    if (rank == 0) tc::mbar_expect_tx(bar, 2 * (kBM + half) * kBK);
+                    const uint32_t lead = in_cta(bar, 0);
+                    tma_load_pair(dst, &tm_w, kb * kBK, n0, lead);
+                    tma_load_pair(dst + kBM * kBK, &tm_x, kb * kBK, m0, lead);
+                }
+            }
+            // the commits that free the last stages arrive here from the even CTA: they are waited for, so that none meets a CTA that has ended
+            for (int v = max(0, u - kPairStages); v < u && ok; ++v)
+                ok = tc::mbar_wait(tc::smem_u32(&s_empty[v % kPairStages]), (uint32_t)(v / kPairStages) & 1u, P.wait_cycles);
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = idesc_i8(2 * kBM, P.nt);
+            bool ok = true;
+            for (int tile = pair; tile < tiles; tile += pairs, ++round) {
+                const int a = round & 1;
+                if (ok) ok = tc::mbar_wait(tc::smem_u32(&s_read[a]), ((uint32_t)(round >> 1) & 1u) ^ 1u, P.wait_cycles);
+                tc::fence_after();
+                for (int kb = 0; kb < P.nkb && ok; ++kb, ++u) {
+                    const int s = u % kPairStages;
+                    if (!(ok = tc::mbar_wait(tc::smem_u32(&s_full[s]), (uint32_t)(u / kPairStages) & 1u, P.wait_cycles))) break;
+                    tc::fence_after();
+                    const uint32_t wa = tc::smem_u32(ring) + s * kPairStageBytes, xa = wa + kBM * kBK;
+#pragma unroll
+                    for (int kk = 0; kk < kBK / 32; ++kk)
+                        asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p; }"
+                                     ::"r"(tmem + a * 256), "l"(tc::sw128_desc(wa + kk * 32)), "l"(tc::sw128_desc(xa + kk * 32)), "r"(idesc),
+                                       "r"((kb > 0 || kk > 0) ? 1u : 0u) : "memory");
+                    commit_pair(tc::smem_u32(&s_empty[s]));
+                }
+                if (!ok) { *(volatile int*)&s_timeout = 1; __threadfence_block(); break; }
+                commit_pair(tc::smem_u32(&s_acc[a]));
+            }
+        }
+    } else {
+        // ---------------- outputs: thread = channel; the two warps of a lane quarter take half of the tokens each
+        const int quad = warp & 3, part = (warp - 2) >> 2;
+        const int c_lo = part * half, c_hi = part ? P.nt : half;
+        bool ok = true;
+        for (int tile = pair; tile < tiles; tile += pairs, ++round) {
+            const int64_t m0 = (int64_t)(tile % m_tiles) * P.nt, n = (int64_t)(tile / m_tiles) * (2 * kBM) + rank * kBM + quad * 32 + lane;
+            const int a = round & 1;
+            for (int c = tid - 64; c < P.nt; c += 32 * kPairWarps) {
+                const bool in = m0 + c < P.M;
+                s_xs[a][c] = in ? P.xscale[m0 + c] : 0.f;
+                s_xsum[a][c] = in ? P.xsum[m0 + c] : 0;
+            }
+            float al = 0.f, zc = 0.f;
+            if (n < P.N) { al = P.alpha[n]; zc = P.zero[n] - 128.f; }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_acc[a]), (uint32_t)(round >> 1) & 1u, P.wait_cycles));
+            if (ok) {
+                tc::fence_after();
+                const uint32_t addr = tmem + ((uint32_t)(quad * 32) << 16) + a * 256;
+                const int cols = (int)min((int64_t)c_hi, P.M - m0);
+                for (int c0 = c_lo; c0 < cols; c0 += 16) {
+                    uint32_t d[16];
+                    tc::tmem_ld16(addr + c0, d);
+                    tc::tmem_wait_ld();
+                    if (n < P.N) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (c0 + j < cols) store_y(P, m0 + c0 + j, n, finish((int)d[j], s_xsum[a][c0 + j], s_xs[a][c0 + j], al, zc));
+                    }
+                }
+                tc::fence_before();
+            } else {
+                *(volatile int*)&s_timeout = 1;
+            }
+            __syncwarp();
+            if (lane == 0)
+                asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_cta(tc::smem_u32(&s_read[a]), 0)) : "memory");
+        }
+    }
+    // Nobody leaves while the other may still write into its barriers or read its stages.  The pair's copies are over by then: the even CTA consumed
+    // them all, or its waits for them ran out first.
+    __syncwarp();
+    tc::fence_before();
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned; barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (tid == 0 && s_timeout) report(P.dev_status, MATQ_ERR_TIMEOUT);
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
 inline bool byte_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t K, int64_t ld, int box_rows) {
     const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)ld};
@@ -217,11 +371,35 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
     P.hold = tc::test_stall() ? 1 : 0;
     P.wait_cycles = P.hold ? tc::kStallWaitCycles : tc::kWaitCycles;
     P.nkb = (int)((K + kBK - 1) / kBK);
-    P.nt = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
-    P.tmem_cols = P.nt < 32 ? 32 : P.nt;
-    const int64_t n_tiles = (N + kBM - 1) / kBM, m_tiles = (M + P.nt - 1) / P.nt;
-    if (m_tiles > 65535) return MATQ_ERR_SHAPE;
     const int sms = sm_count();
+    CUtensorMap tm_w, tm_x;
+    if (!byte_map(&tm_w, q, N, K, ldw, kBM)) return MATQ_ERR_CUDA;
+
+    if (M > 128) {
+        // Tokens per tile: the value whose rounds over the pairs of SMs cost least.
+        const int pairs = sms / 2;
+        const int64_t n_pair = (N + 2 * kBM - 1) / (2 * kBM);
+        int64_t best = -1;
+        for (int nt = 256; nt >= 128; nt -= 32) {
+            const int64_t tiles = n_pair * ((M + nt - 1) / nt), cost = (tiles + pairs - 1) / pairs * nt;
+            if (best < 0 || cost < best) { best = cost; P.nt = nt; }
+        }
+        const int64_t tiles = n_pair * ((M + P.nt - 1) / P.nt);
+        if (tiles >= (1ll << 30)) return MATQ_ERR_SHAPE;
+        if (!byte_map(&tm_x, xq, M, K, ldxq, P.nt / 2)) return MATQ_ERR_CUDA;
+        static std::atomic<unsigned long long> pair_ok{0};
+        if (!opt_in_max_smem(gemm_a8_pair_kernel, pair_ok)) return MATQ_ERR_CUDA;
+        const unsigned grid = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
+        if (launch_overlapped(gemm_a8_pair_kernel, dim3(grid), dim3(kPairThreads), (size_t)kPairStages * kPairStageBytes + 1024, s, tm_w, tm_x, P) != cudaSuccess) {
+            cudaGetLastError();
+            return MATQ_ERR_CUDA;
+        }
+        return launch_status();
+    }
+
+    P.nt = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    P.tmem_cols = P.nt < 32 ? 32 : P.nt;
+    const int64_t n_tiles = (N + kBM - 1) / kBM, m_tiles = 1;
     P.splits = 1;
     while (P.nt <= 128 && P.splits < 8 && n_tiles * m_tiles * P.splits * 2 <= 2 * sms && P.nkb >= 4 * P.splits) P.splits *= 2;
     const int stage_bytes = (kBM + P.nt) * kBK;
@@ -230,8 +408,7 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
     size_t smem = (size_t)P.stages * stage_bytes;
     if (P.splits > 1 && smem < (size_t)P.nt * kBM * 4) smem = (size_t)P.nt * kBM * 4;
     smem += 1024;
-    CUtensorMap tm_w, tm_x;
-    if (!byte_map(&tm_w, q, N, K, ldw, kBM) || !byte_map(&tm_x, xq, M, K, ldxq, P.nt)) return MATQ_ERR_CUDA;
+    if (!byte_map(&tm_x, xq, M, K, ldxq, P.nt)) return MATQ_ERR_CUDA;
     static std::atomic<unsigned long long> smem_ok{0};
     if (!opt_in_max_smem(gemm_a8_kernel, smem_ok)) return MATQ_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};

@@ -9,6 +9,7 @@ constexpr int kBM = 128;             // channels of a tile: the rows of the accu
 constexpr int kBK = 128;             // bytes of K per stage: one 128-byte swizzle row
 constexpr int kMaxStages = 8;
 constexpr int kMaxNT = 256;
+constexpr int kMaxSplitsK = 8;
 
 struct Params {
     const float *alpha, *zero, *xscale;
@@ -82,41 +83,47 @@ gemm_a8_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
                 }
             }
             if (P.early) after_previous_kernel();
-            int issued = 0;
+            // (each of the two loops over K is one thread's chain of instructions: slots and descriptors are stepped, not computed)
+            const uint32_t full = tc::smem_u32(s_full), empty = tc::smem_u32(s_empty), base = tc::smem_u32(ring);
+            int s = 0, issued = 0;
+            uint32_t phase = 1;
             for (int kb = kb0; kb < kb1 && !P.hold; ++kb) {
-                const int i = kb - kb0, s = i % P.stages;
-                const uint32_t bar = tc::smem_u32(&s_full[s]);
-                unsigned char* st = ring + (size_t)s * stage_bytes;
-                if (i >= ahead) {
-                    if (!tc::mbar_wait(tc::smem_u32(&s_empty[s]), ((uint32_t)(i / P.stages) & 1u) ^ 1u, P.wait_cycles)) { s_timeout = 1; break; }
-                    tc::mbar_expect_tx(bar, stage_bytes);
-                    tc::tma_load_2d(tc::smem_u32(st), &tm_w, kb * kBK, (int)n0, bar);
+                const uint32_t dst = base + (uint32_t)(s * stage_bytes);
+                if (issued >= ahead) {
+                    if (!tc::mbar_wait(empty + 8 * s, phase, P.wait_cycles)) { s_timeout = 1; break; }
+                    tc::mbar_expect_tx(full + 8 * s, stage_bytes);
+                    tc::tma_load_2d(dst, &tm_w, kb * kBK, (int)n0, full + 8 * s);
                 }
-                tc::tma_load_2d(tc::smem_u32(st + kBM * kBK), &tm_x, kb * kBK, (int)m0, bar);
-                issued = i + 1;
+                tc::tma_load_2d(dst + kBM * kBK, &tm_x, kb * kBK, (int)m0, full + 8 * s);
+                ++issued;
+                if (++s == P.stages) { s = 0; phase ^= 1u; }
             }
             // no copy may be in flight when the CTA ends, whatever became of its consumer
             for (int i = max(0, issued - P.stages); i < issued; ++i)
-                tc::mbar_wait(tc::smem_u32(&s_full[i % P.stages]), (uint32_t)(i / P.stages) & 1u, P.wait_cycles);
+                tc::mbar_wait(full + 8 * (i % P.stages), (uint32_t)(i / P.stages) & 1u, P.wait_cycles);
         }
     } else if (warp == 1) {
         if (lane == 0) {
-            const uint32_t idesc = idesc_i8(kBM, P.nt);
+            const uint32_t idesc = idesc_i8(kBM, P.nt), full = tc::smem_u32(s_full), empty = tc::smem_u32(s_empty);
+            const uint64_t desc0 = tc::sw128_desc(tc::smem_u32(ring));
+            int s = 0;
+            uint32_t phase = 0, more = 0;
             for (int kb = kb0; kb < kb1; ++kb) {
-                const int i = kb - kb0, s = i % P.stages;
-                if (!tc::mbar_wait(tc::smem_u32(&s_full[s]), (uint32_t)(i / P.stages) & 1u, P.wait_cycles)) {
+                if (!tc::mbar_wait(full + 8 * s, phase, P.wait_cycles)) {
                     *(volatile int*)&s_timeout = 1;
                     __threadfence_block();
                     break;
                 }
                 tc::fence_after();
-                const uint32_t a = tc::smem_u32(ring + (size_t)s * stage_bytes), b = a + kBM * kBK;
+                const uint64_t w = desc0 + (uint64_t)(s * (stage_bytes >> 4));
 #pragma unroll
-                for (int kk = 0; kk < kBK / 32; ++kk)
+                for (int kk = 0; kk < kBK / 32; ++kk) {
                     asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p; }"
-                                 ::"r"(tmem), "l"(tc::sw128_desc(a + kk * 32)), "l"(tc::sw128_desc(b + kk * 32)), "r"(idesc),
-                                   "r"((i > 0 || kk > 0) ? 1u : 0u) : "memory");
-                tc::tc_commit(tc::smem_u32(&s_empty[s]));
+                                 ::"r"(tmem), "l"(w + (uint64_t)(kk * 2)), "l"(w + (uint64_t)((kBM * kBK >> 4) + kk * 2)), "r"(idesc), "r"(more) : "memory");
+                    more = 1;
+                }
+                tc::tc_commit(empty + 8 * s);
+                if (++s == P.stages) { s = 0; phase ^= 1u; }
             }
             tc::tc_commit(tc::smem_u32(&s_acc));
         }
@@ -165,15 +172,28 @@ gemm_a8_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
                 asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(t) : "r"(a) : "memory");
                 ok &= t == 0;
             }
-            for (int c = split; c < cols && ok; c += P.splits) {
-                int sum = 0;
-                for (int r = 0; r < P.splits; ++r) {
-                    uint32_t a, v;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(mine + c * kBM * 4), "r"(r));
-                    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-                    sum += (int)v;
+            // all parts of four tokens are requested before the first is added: a load from another SM takes some hundred cycles
+            uint32_t from[kMaxSplitsK];
+#pragma unroll
+            for (int r = 0; r < kMaxSplitsK; ++r) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from[r]) : "r"(mine), "r"(min(r, P.splits - 1)));
+            for (int c0 = split; c0 < cols && ok; c0 += 4 * P.splits) {
+                int v[4][kMaxSplitsK];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < kMaxSplitsK; ++r) {
+                        const int c = c0 + i * P.splits;
+                        v[i][r] = 0;
+                        if (r < P.splits && c < cols) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v[i][r]) : "r"(from[r] + c * kBM * 4));
+                    }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = c0 + i * P.splits;
+                    int sum = 0;
+#pragma unroll
+                    for (int r = 0; r < kMaxSplitsK; ++r) sum += v[i][r];
+                    if (c < cols && n < P.N) store_y(P, m0 + c, n, finish(sum, s_xsum[c], s_xs[c], al, zc));
                 }
-                if (n < P.N) store_y(P, m0 + c, n, finish(sum, s_xsum[c], s_xs[c], al, zc));
             }
         }
         __syncwarp();
@@ -194,8 +214,11 @@ gemm_a8_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
 // the stage in both.  The kernel is persistent: a pair takes every (number of pairs)-th tile, two accumulators take turns, and eight
 // warps store one tile while the next is summed.  Channels are the accumulator's rows, so a thread keeps its channel's alpha and z in registers and a
 // warp's stores run along a token's outputs.
-constexpr int kPairWarps = 8, kPairThreads = 32 * (2 + kPairWarps), kPairStages = 6;
-constexpr int kPairStageBytes = 2 * kBM * kBK;       // 128 channels and up to 128 tokens
+// A stage is 256 bytes of K, two blocks of 128: waiting for a stage, issuing and committing cost the issuing thread about 500 cycles whatever the
+// stage holds, and the products of one block take no more than that (4096 x 14336 x 4096: 770 cycles a block with one block per stage).
+constexpr int kPairWarps = 8, kPairThreads = 32 * (2 + kPairWarps), kPairStages = 3, kPairBlocks = 2;
+constexpr int kPairBlockBytes = 2 * kBM * kBK;       // 128 channels and up to 128 tokens
+constexpr int kPairStageBytes = kPairBlocks * kPairBlockBytes;
 
 __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
     uint32_t a;
@@ -244,46 +267,64 @@ gemm_a8_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
 
     const int m_tiles = (int)((P.M + P.nt - 1) / P.nt), n_tiles = (int)((P.N + 2 * kBM - 1) / (2 * kBM)), tiles = m_tiles * n_tiles;
     const int pairs = (int)(gridDim.x >> 1), pair = (int)(blockIdx.x >> 1), half = P.nt / 2;
-    int u = 0, round = 0;                                               // stages and tiles so far
+    int round = 0;                                                      // tiles so far
 
+    // The two loops over K are each one thread's chain of instructions, and a stage's products take 512 cycles: everything that does not change
+    // with the stage stays out of them (with slot numbers by division and descriptors put together in place they took a thousand).
     if (warp == 0) {
         if (lane == 0 && !P.hold) {
             bool ok = true;
+            int s = 0;
+            uint32_t phase = 1;
+            const uint32_t full = tc::smem_u32(s_full), empty = tc::smem_u32(s_empty), lead = in_cta(full, 0), base = tc::smem_u32(ring);
+            const uint32_t bytes = 2 * kPairBlocks * (kBM + half) * kBK;
             for (int tile = pair; tile < tiles && ok; tile += pairs) {
                 const int m0 = tile % m_tiles * P.nt + (int)rank * half, n0 = tile / m_tiles * (2 * kBM) + (int)rank * kBM;
-                for (int kb = 0; kb < P.nkb; ++kb, ++u) {
-                    const int s = u % kPairStages;
-                    if (!(ok = tc::mbar_wait(tc::smem_u32(&s_empty[s]), ((uint32_t)(u / kPairStages) & 1u) ^ 1u, P.wait_cycles))) { *(volatile int*)&s_timeout = 1; break; }
-                    const uint32_t bar = tc::smem_u32(&s_full[s]), dst = tc::smem_u32(ring) + s * kPairStageBytes;
-                    if (rank == 0) tc::mbar_expect_tx(bar, 2 * (kBM + half) * kBK);
-                    const uint32_t lead = in_cta(bar, 0);
-                    tma_load_pair(dst, &tm_w, kb * kBK, n0, lead);
-                    tma_load_pair(dst + kBM * kBK, &tm_x, kb * kBK, m0, lead);
+                for (int x = 0; x < P.nkb * kBK; x += kPairBlocks * kBK) {             // past K the copies bring zeros
+                    if (!tc::mbar_wait(empty + 8 * s, phase, P.wait_cycles)) { *(volatile int*)&s_timeout = 1; ok = false; break; }
+                    if (rank == 0) tc::mbar_expect_tx(full + 8 * s, bytes);
+                    const uint32_t dst = base + s * kPairStageBytes;
+#pragma unroll
+                    for (int i = 0; i < kPairBlocks; ++i) {
+                        tma_load_pair(dst + i * kPairBlockBytes, &tm_w, x + i * kBK, n0, lead + 8 * s);
+                        tma_load_pair(dst + i * kPairBlockBytes + kBM * kBK, &tm_x, x + i * kBK, m0, lead + 8 * s);
+                    }
+                    if (++s == kPairStages) { s = 0; phase ^= 1u; }
                 }
             }
             // the commits that free the last stages arrive here from the even CTA: they are waited for, so that none meets a CTA that has ended
-            for (int v = max(0, u - kPairStages); v < u && ok; ++v)
-                ok = tc::mbar_wait(tc::smem_u32(&s_empty[v % kPairStages]), (uint32_t)(v / kPairStages) & 1u, P.wait_cycles);
+            for (int i = 0; i < kPairStages && ok; ++i) {
+                ok = tc::mbar_wait(empty + 8 * s, phase, P.wait_cycles);
+                if (++s == kPairStages) { s = 0; phase ^= 1u; }
+            }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
             const uint32_t idesc = idesc_i8(2 * kBM, P.nt);
             bool ok = true;
+            int s = 0;
+            uint32_t phase = 0;
+            const uint32_t full = tc::smem_u32(s_full), empty = tc::smem_u32(s_empty);
+            const uint64_t desc0 = tc::sw128_desc(tc::smem_u32(ring));
             for (int tile = pair; tile < tiles; tile += pairs, ++round) {
                 const int a = round & 1;
                 if (ok) ok = tc::mbar_wait(tc::smem_u32(&s_read[a]), ((uint32_t)(round >> 1) & 1u) ^ 1u, P.wait_cycles);
                 tc::fence_after();
-                for (int kb = 0; kb < P.nkb && ok; ++kb, ++u) {
-                    const int s = u % kPairStages;
-                    if (!(ok = tc::mbar_wait(tc::smem_u32(&s_full[s]), (uint32_t)(u / kPairStages) & 1u, P.wait_cycles))) break;
+                const uint32_t d = tmem + a * 256;
+                uint32_t more = 0;
+                for (int kb = 0; kb < P.nkb && ok; kb += kPairBlocks) {
+                    if (!(ok = tc::mbar_wait(full + 8 * s, phase, P.wait_cycles))) break;
                     tc::fence_after();
-                    const uint32_t wa = tc::smem_u32(ring) + s * kPairStageBytes, xa = wa + kBM * kBK;
+                    const uint64_t w = desc0 + (uint64_t)(s * (kPairStageBytes >> 4));
 #pragma unroll
-                    for (int kk = 0; kk < kBK / 32; ++kk)
+                    for (int kk = 0; kk < kPairBlocks * kBK / 32; ++kk) {
+                        const uint64_t at = w + (uint64_t)((kk / 4) * (kPairBlockBytes >> 4) + (kk & 3) * 2);
                         asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p; }"
-                                     ::"r"(tmem + a * 256), "l"(tc::sw128_desc(wa + kk * 32)), "l"(tc::sw128_desc(xa + kk * 32)), "r"(idesc),
-                                       "r"((kb > 0 || kk > 0) ? 1u : 0u) : "memory");
-                    commit_pair(tc::smem_u32(&s_empty[s]));
+                                     ::"r"(d), "l"(at), "l"(at + (uint64_t)(kBM * kBK >> 4)), "r"(idesc), "r"(more) : "memory");
+                        more = 1;
+                    }
+                    commit_pair(empty + 8 * s);
+                    if (++s == kPairStages) { s = 0; phase ^= 1u; }
                 }
                 if (!ok) { *(volatile int*)&s_timeout = 1; __threadfence_block(); break; }
                 commit_pair(tc::smem_u32(&s_acc[a]));
@@ -381,7 +422,7 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
         const int64_t n_pair = (N + 2 * kBM - 1) / (2 * kBM);
         int64_t best = -1;
         for (int nt = 256; nt >= 128; nt -= 32) {
-            const int64_t tiles = n_pair * ((M + nt - 1) / nt), cost = (tiles + pairs - 1) / pairs * nt;
+            const int64_t tiles = n_pair * ((M + nt - 1) / nt), cost = (tiles + pairs - 1) / pairs * (nt > 192 ? nt : 192);     // below 192 tokens a stage's fixed part shows
             if (best < 0 || cost < best) { best = cost; P.nt = nt; }
         }
         const int64_t tiles = n_pair * ((M + P.nt - 1) / P.nt);
@@ -401,7 +442,7 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
     P.tmem_cols = P.nt < 32 ? 32 : P.nt;
     const int64_t n_tiles = (N + kBM - 1) / kBM, m_tiles = 1;
     P.splits = 1;
-    while (P.nt <= 128 && P.splits < 8 && n_tiles * m_tiles * P.splits * 2 <= 2 * sms && P.nkb >= 4 * P.splits) P.splits *= 2;
+    while (P.nt <= 128 && P.splits < kMaxSplitsK && n_tiles * m_tiles * P.splits * 2 <= 2 * sms && P.nkb >= 4 * P.splits) P.splits *= 2;
     const int stage_bytes = (kBM + P.nt) * kBK;
     P.stages = (P.nt <= 64 ? 104 * 1024 : 200 * 1024) / stage_bytes;
     if (P.stages > kMaxStages) P.stages = kMaxStages;

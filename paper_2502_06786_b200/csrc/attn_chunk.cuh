@@ -2,14 +2,17 @@
 //
 // A query tile is 128 accumulator rows: floor(128 / group) tokens times the heads of one key head's group, so that a key is read once for the
 // whole group.  A CTA takes kTiles such tiles and walks the keys that they see, kKeys at a time:
-//   warps 4 kTiles, 4 kTiles + 1  producers: queries once and keys; values; a ring each (one box per page and 64 columns, 128-byte swizzle);
-//   warp 4 kTiles + 2  issues S = Q K^T and O += P V (tcgen05.mma, both accumulators and P in tensor memory);
-//   warps 0 .. 4 kTiles - 1  softmax, one thread per row: S from tensor memory, exponentials, P back over S as bf16.
+//   warps 8, 9         producers: queries once and keys; values; a ring each (one box per page and 64 columns, 128-byte swizzle);
+//   warp 10            issues S = Q K^T and O += P V (tcgen05.mma, both accumulators and P in tensor memory);
+//   warps 0 .. 7       softmax, one thread per row (two, with half of the keys each, when there is one tile): S from tensor memory, exponentials,
+//                      P back over S as bf16.
 // P takes the place of S: the product with V that reads it is issued before the scores that overwrite it.  The row maximum is a reference only: it
 // moves, and O is rescaled, when a score exceeds it by more than 2^8, which leaves p <= 256 and the quotient O / l unchanged.
 // D <= 128: two tiles, whose softmax and tensor work alternate.  D = 256: tensor memory holds one tile's O and two S buffers of 64 keys,
 // so that the scores of the next keys are computed while the present ones are exponentiated.
 #pragma once
+
+#include <type_traits>
 
 #include "attn_common.cuh"
 
@@ -27,7 +30,8 @@ struct ChunkCfg {
     static constexpr int kQBytes = 128 * D * 2;                         // one query tile
     static constexpr int kKvBytes = kKeys * D * 2;                      // the keys, or the values, of a step
     static constexpr int kStagesK = D == 64 ? 4 : 3, kStagesV = D == 64 ? 4 : TILES * D == 128 ? 3 : 2;
-    static constexpr int kSoft = kTiles * 128;                          // softmax threads
+    static constexpr int kSoft = 256;                                   // softmax threads: one per row of two tiles, two per row of one
+    static constexpr int kCols = kKeys * TILES / 2;                     // keys of a step per softmax thread
     static constexpr int kThreads = kSoft + 96;
     static constexpr int kTmemO = 256;                                  // first column of the output accumulators; S starts at column 0
     static constexpr size_t kSmem = (size_t)kTiles * kQBytes + (size_t)(kStagesK + kStagesV) * kKvBytes + 1024;
@@ -41,12 +45,18 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* d) {
                    "r"(d[16]), "r"(d[17]), "r"(d[18]), "r"(d[19]), "r"(d[20]), "r"(d[21]), "r"(d[22]), "r"(d[23]),
                    "r"(d[24]), "r"(d[25]), "r"(d[26]), "r"(d[27]), "r"(d[28]), "r"(d[29]), "r"(d[30]), "r"(d[31]), "r"(addr) : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* d) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 ::"r"(d[0]), "r"(d[1]), "r"(d[2]), "r"(d[3]), "r"(d[4]), "r"(d[5]), "r"(d[6]), "r"(d[7]),
+                   "r"(d[8]), "r"(d[9]), "r"(d[10]), "r"(d[11]), "r"(d[12]), "r"(d[13]), "r"(d[14]), "r"(d[15]), "r"(addr) : "memory");
+}
 // D = fp32, A = B = bf16, 128 rows
 __device__ __forceinline__ constexpr uint32_t idesc_bf16(int n, bool b_mn_major) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
 
-template <int D, int TILES>
+// CAP: with the cap on the scores
+template <int D, int TILES, bool CAP>
 __global__ void __launch_bounds__(ChunkCfg<D, TILES>::kThreads, 1)
 attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Params P) {
     using C = ChunkCfg<D, TILES>;
@@ -57,6 +67,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     __shared__ Sequence s_seq;
     __shared__ int s_timeout, s_any_bad, s_bad_key[kMaxMasked];
     __shared__ uint32_t s_bad[kMaxMasked][kKeys / 32];
+    __shared__ float s_half[2][128];                                    // one tile: what the two threads of a row tell one another
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned char* smem = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
     unsigned char* ring_k = smem + C::kTiles * C::kQBytes;
@@ -67,7 +78,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         for (int s = 0; s < C::kStagesK; ++s) { tc::mbar_init(tc::smem_u32(&s_kfull[s]), 1); tc::mbar_init(tc::smem_u32(&s_kempty[s]), 1); }
         for (int s = 0; s < C::kStagesV; ++s) { tc::mbar_init(tc::smem_u32(&s_vfull[s]), 1); tc::mbar_init(tc::smem_u32(&s_vempty[s]), 1); }
         tc::mbar_init(tc::smem_u32(&s_q), 1);
-        for (int t = 0; t < 2; ++t) { tc::mbar_init(tc::smem_u32(&s_score[t]), 1); tc::mbar_init(tc::smem_u32(&s_prob[t]), 128); }
+        for (int t = 0; t < 2; ++t) { tc::mbar_init(tc::smem_u32(&s_score[t]), 1); tc::mbar_init(tc::smem_u32(&s_prob[t]), C::kSoft / C::kTiles); }
         tc::mbar_init(tc::smem_u32(&s_pv), 1);
         tc::mbar_init(tc::smem_u32(&s_out), 1);
         tc::mbar_init(tc::smem_u32(&s_read), C::kSoft);
@@ -155,66 +166,74 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             // ---------------- tensor cores: one thread issues
             if (lane == 0 && n_it > 0) {
                 bool ok = tc::mbar_wait(tc::smem_u32(&s_q), (uint32_t)round & 1u, P.wait_cycles);
-                const auto wait_k = [&](int i) { return tc::mbar_wait(tc::smem_u32(&s_kfull[(it + i) % C::kStagesK]), (uint32_t)((it + i) / C::kStagesK) & 1u, P.wait_cycles); };
-                const auto wait_v = [&](int i) { return tc::mbar_wait(tc::smem_u32(&s_vfull[(it + i) % C::kStagesV]), (uint32_t)((it + i) / C::kStagesV) & 1u, P.wait_cycles); };
-                const auto scores = [&](int t, int i) {                 // S_t = Q_t K_i^T
-                    const uint32_t a = tc::smem_u32(smem) + (C::kTiles == 2 ? t * C::kQBytes : 0), kb = tc::smem_u32(ring_k) + (uint32_t)((it + i) % C::kStagesK) * C::kKvBytes;
+                // Descriptors and slots are stepped, not computed: a product of 16 keys or columns takes 64 cycles, about what a handful of dependent
+                // instructions takes.
+                const uint64_t q_desc = tc::sw128_desc(tc::smem_u32(smem)), k_desc = tc::sw128_desc(tc::smem_u32(ring_k)),
+                               v_desc = tc::sw128_desc(tc::smem_u32(ring_v), kKeys * 128, 1024);
+                const uint32_t kfull = tc::smem_u32(s_kfull), kempty = tc::smem_u32(s_kempty), vfull = tc::smem_u32(s_vfull), vempty = tc::smem_u32(s_vempty);
+                int ks = it % C::kStagesK, vs = it % C::kStagesV;       // slots of the next keys and values
+                uint32_t kp = (uint32_t)(it / C::kStagesK) & 1u, vp = (uint32_t)(it / C::kStagesV) & 1u;
+                const auto next_k = [&] { if (++ks == C::kStagesK) { ks = 0; kp ^= 1u; } };
+                const auto next_v = [&] { if (++vs == C::kStagesV) { vs = 0; vp ^= 1u; } };
+                const auto scores = [&](int t) {                        // S_t = Q_t K^T
+                    const uint64_t qd = q_desc + (uint64_t)(C::kTiles == 2 ? t * (C::kQBytes >> 4) : 0), kd = k_desc + (uint64_t)(ks * (C::kKvBytes >> 4));
                     const uint32_t d = tmem + t * kKeys;
 #pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks)
+                    for (int x = 0; x < D / 16; ++x)
                         asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
-                                     ::"r"(d), "l"(tc::sw128_desc(a + (ks / 4) * (128 * 128) + (ks & 3) * 32)),
-                                       "l"(tc::sw128_desc(kb + (ks / 4) * (kKeys * 128) + (ks & 3) * 32)), "r"(idesc_bf16(kKeys, false)), "r"(ks > 0 ? 1u : 0u) : "memory");
+                                     ::"r"(d), "l"(qd + (uint64_t)((x / 4) * (128 * 128 >> 4) + (x & 3) * 2)),
+                                       "l"(kd + (uint64_t)((x / 4) * (kKeys * 128 >> 4) + (x & 3) * 2)), "r"(idesc_bf16(kKeys, false)), "r"(x > 0 ? 1u : 0u) : "memory");
                     tc::tc_commit(tc::smem_u32(&s_score[t]));
                 };
-                const auto product = [&](int t, int i) {                // O_t += P_t V_i
-                    const uint32_t vb = tc::smem_u32(ring_v) + (uint32_t)((it + i) % C::kStagesV) * C::kKvBytes, d = tmem + C::kTmemO + (C::kTiles == 2 ? t * D : 0);
+                const auto product = [&](int t, int i) {                // O_t += P_t V
+                    const uint64_t vd = v_desc + (uint64_t)(vs * (C::kKvBytes >> 4));
+                    const uint32_t d = tmem + C::kTmemO + (C::kTiles == 2 ? t * D : 0);
 #pragma unroll
-                    for (int ks = 0; ks < kKeys / 16; ++ks)
+                    for (int x = 0; x < kKeys / 16; ++x)
                         asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
-                                     ::"r"(d), "r"(tmem + t * kKeys + ks * 8), "l"(tc::sw128_desc(vb + ks * 2048, kKeys * 128, 1024)),
-                                       "r"(idesc_bf16(D, true)), "r"((i > 0 || ks > 0) ? 1u : 0u) : "memory");
+                                     ::"r"(d), "r"(tmem + t * kKeys + x * 8), "l"(vd + (uint64_t)(x * (2048 >> 4))),
+                                       "r"(idesc_bf16(D, true)), "r"((i > 0 || x > 0) ? 1u : 0u) : "memory");
                 };
-                const auto free_k = [&](int i) { tc::tc_commit(tc::smem_u32(&s_kempty[(it + i) % C::kStagesK])); };
-                const auto free_v = [&](int i) { tc::tc_commit(tc::smem_u32(&s_vempty[(it + i) % C::kStagesV])); };
-                if (ok) ok = wait_k(0);
+                const auto first_read = [&](int i) { return i > 0 || round == 0 || tc::mbar_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles); };
+                if (ok) ok = tc::mbar_wait(kfull + 8 * ks, kp, P.wait_cycles);
                 tc::fence_after();
                 if (C::kTiles == 2) {
-                    if (ok) { scores(0, 0); scores(1, 0); free_k(0); }
+                    if (ok) { scores(0); scores(1); tc::tc_commit(kempty + 8 * ks); next_k(); }
                     for (int i = 0; i < n_it && ok; ++i) {
-                        for (int t = 0; t < 2 && ok; ++t) {
-                            ok = tc::mbar_wait(tc::smem_u32(&s_prob[t]), (uint32_t)(it + i) & 1u, P.wait_cycles) && wait_v(i);
-                            if (ok && i == 0 && t == 0 && round > 0) ok = tc::mbar_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles);
+                        const bool more = i + 1 < n_it;
+                        for (int t = 0; t < 2; ++t) {
+                            ok = tc::mbar_wait(tc::smem_u32(&s_prob[t]), (uint32_t)(it + i) & 1u, P.wait_cycles);
+                            if (ok && t == 0) ok = tc::mbar_wait(vfull + 8 * vs, vp, P.wait_cycles) && first_read(i);
                             if (!ok) break;
                             tc::fence_after();
                             product(t, i);
-                            if (t == 1) free_v(i);
-                            if (i + 1 < n_it) {
-                                ok = wait_k(i + 1);
-                                if (!ok) break;
+                            if (t == 1) { tc::tc_commit(vempty + 8 * vs); next_v(); }
+                            if (more) {
+                                if (t == 0 && !(ok = tc::mbar_wait(kfull + 8 * ks, kp, P.wait_cycles))) break;
                                 tc::fence_after();
-                                scores(t, i + 1);
-                                if (t == 1) free_k(i + 1);
+                                scores(t);
+                                if (t == 1) { tc::tc_commit(kempty + 8 * ks); next_k(); }
                             }
                         }
                     }
                 } else {
-                    if (ok) { scores(it & 1, 0); free_k(0); }
+                    if (ok) { scores(it & 1); tc::tc_commit(kempty + 8 * ks); next_k(); }
                     for (int i = 0; i < n_it && ok; ++i) {
                         if (i + 1 < n_it) {
-                            ok = wait_k(i + 1);
-                            if (!ok) break;
+                            if (!(ok = tc::mbar_wait(kfull + 8 * ks, kp, P.wait_cycles))) break;
                             tc::fence_after();
-                            scores((it + i + 1) & 1, i + 1);
-                            free_k(i + 1);
+                            scores((it + i + 1) & 1);
+                            tc::tc_commit(kempty + 8 * ks);
+                            next_k();
                         }
-                        ok = tc::mbar_wait(tc::smem_u32(&s_prob[(it + i) & 1]), (uint32_t)((it + i) >> 1) & 1u, P.wait_cycles) && wait_v(i);
-                        if (ok && i == 0 && round > 0) ok = tc::mbar_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles);
+                        ok = tc::mbar_wait(tc::smem_u32(&s_prob[(it + i) & 1]), (uint32_t)((it + i) >> 1) & 1u, P.wait_cycles) &&
+                             tc::mbar_wait(vfull + 8 * vs, vp, P.wait_cycles) && first_read(i);
                         if (!ok) break;
                         tc::fence_after();
                         product((it + i) & 1, i);
-                        free_v(i);
+                        tc::tc_commit(vempty + 8 * vs);
                         tc::tc_commit(tc::smem_u32(&s_pv));
+                        next_v();
                     }
                 }
                 if (!ok) { *(volatile int*)&s_timeout = 1; __threadfence_block(); }
@@ -222,20 +241,35 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
             __syncwarp();
         } else {
-            // ---------------- softmax: thread = row of tile t
-            const int t = C::kTiles == 2 ? warp >> 2 : 0, r = tid & 127;
+            // ---------------- softmax: thread = row of tile t (with one tile: half of the keys of a row, and half of its outputs)
+            const int part_of = warp >> 2, t = C::kTiles == 2 ? part_of : 0, r = tid & 127;
+            const int col0 = C::kTiles == 2 ? 0 : part_of * C::kCols;
             const int64_t tok = t0 + t * tok_tile + r / P.group;
             const bool live = r < rows_tile && tok < n_new;
             const int see_hi = live ? (int)(ctx + tok) : -1, see_lo = live ? lo(see_hi) : 0;
             const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
             const uint32_t o_addr = lane_addr + C::kTmemO + t * D;
             const Score sc(P.scale, P.softcap);
+            const float tmul = P.softcap > 0.f ? P.scale / P.softcap : 0.f;        // the tanh's argument per score
             float m = -INFINITY, l = 0.f;
             bool ok = true;
             int masked_no = 0;
             if (tid == 0) s_any_bad = 0;
             for (int x = tid; x < kMaxMasked * (kKeys / 32); x += C::kSoft) (&s_bad[0][0])[x] = 0;
             asm volatile("bar.sync 1, %0;" ::"n"(C::kSoft) : "memory");
+            constexpr int kOCols = D * C::kTiles / 2;                   // outputs of this thread: columns o_col ..
+            const int o_col = C::kTiles == 2 ? 0 : part_of * kOCols;
+            const auto rescale = [&](float f) {
+#pragma unroll 1
+                for (int c = 0; c < kOCols; c += 32) {
+                    uint32_t o[32];
+                    tc::tmem_ld32(o_addr + o_col + c, o);
+                    tc::tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                    tmem_st32(o_addr + o_col + c, o);
+                }
+            };
 
             for (int i = 0; i < n_it; ++i) {
                 const int gi = it + i, j0 = k_lo + i * kKeys;
@@ -244,63 +278,101 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_score[which]), par, P.wait_cycles)) && *(volatile int*)&s_timeout == 0;
                 ok = __all_sync(0xffffffffu, ok);
                 const bool masked = is_masked(j0);
-                if (ok) {
-                    tc::fence_after();
-                    const uint32_t s_addr = lane_addr + which * kKeys;
-                    uint32_t sr[kKeys];
+                const uint32_t s_addr = lane_addr + which * kKeys + col0;
+                float top = -INFINITY, use;
+                uint64_t sum2[2];
+                uint32_t pk[C::kCols / 2];
+                // One pass: exponents x = score - reference, their maximum, 2^x, its sum, bf16.  Should x exceed 8 somewhere the reference moves and
+                // the pass is done again; otherwise the maximum costs no second look at the scores.
+                const auto pass = [&](auto hide) {
+                    top = -INFINITY;
+                    sum2[0] = sum2[1] = 0;
+                    uint32_t sr[2][32];
+                    tc::tmem_ld32(s_addr, sr[0]);
+                    const uint64_t neg = pair(-use, -use), mul = pair(CAP ? 1.f : sc.mul, CAP ? 1.f : sc.mul);
 #pragma unroll
-                    for (int c = 0; c < kKeys; c += 32) tc::tmem_ld32(s_addr + c, sr + c);
-                    tc::tmem_wait_ld();
-                    float mul = sc.mul;
-                    if (sc.cap2 > 0.f) {
+                    for (int c = 0; c < C::kCols; c += 32) {
+                        uint32_t* v = sr[(c >> 5) & 1];
+                        tc::tmem_wait_ld();
+                        if (c + 32 < C::kCols) tc::tmem_ld32(s_addr + c + 32, sr[((c >> 5) + 1) & 1]);
+                        if constexpr (CAP) {
+                            float big = 0.f;
 #pragma unroll
-                        for (int c = 0; c < kKeys; ++c) sr[c] = __float_as_uint(capped(__uint_as_float(sr[c]), sc.mul, sc.cap2));
-                        mul = 1.f;
-                    }
-                    if (masked) {
+                            for (int e = 0; e < 32; e += 2) big = max3(big, fabsf(__uint_as_float(v[e])), fabsf(__uint_as_float(v[e + 1])));
+                            if (__any_sync(0xffffffffu, !(big * tmul <= kTanhMax))) {       // some score is past the polynomial's range
 #pragma unroll
-                        for (int c = 0; c < kKeys; ++c)
-                            if (j0 + c > see_hi || j0 + c < see_lo) sr[c] = 0xff800000u;
-                    }
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(capped(__uint_as_float(v[e]), sc.mul, sc.cap2));
+                            } else {
+                                const uint64_t tm2 = pair(tmul, tmul), cap = pair(sc.cap2, sc.cap2);
 #pragma unroll
-                    for (int c = 0; c < kKeys; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(sr[c]));
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * mul;
-                    const bool raise = top > m + 8.f;                    // also from -inf to anything finite
-                    if (__any_sync(0xffffffffu, raise)) {
-                        const float f = raise ? ex2(m - top) : 1.f;
-                        if (raise) m = top;
-                        l *= f;
-                        if (i > 0) {
-                            // O holds the steps before this one.  With two tiles the scores' arrival says that their product is done.
-                            if (C::kTiles == 1) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_pv), (uint32_t)(gi - 1) & 1u, P.wait_cycles));
-                            tc::fence_after();
-#pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                uint32_t o[32];
-                                tc::tmem_ld32(o_addr + c, o);
-                                tc::tmem_wait_ld();
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                                tmem_st32(o_addr + c, o);
+                                for (int e = 0; e < 32; e += 2) {
+                                    const uint64_t t2 = mul2(pair(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), tm2), u2 = mul2(t2, t2);
+                                    uint64_t p2 = fma2(u2, pair(kTanh3, kTanh3), pair(kTanh2, kTanh2));
+                                    p2 = fma2(p2, u2, pair(kTanh1, kTanh1));
+                                    p2 = fma2(p2, u2, pair(kTanh0, kTanh0));
+                                    float x, y;
+                                    unpair(mul2(mul2(t2, cap), p2), x, y);
+                                    v[e] = __float_as_uint(x);
+                                    v[e + 1] = __float_as_uint(y);
+                                }
                             }
                         }
-                    }
-                    const float ref = m == -INFINITY ? 0.f : m;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int c = 0; c < kKeys; c += 64) {
-                        uint32_t pk[32];
-#pragma unroll
-                        for (int e = 0; e < 64; e += 2) {
-                            const float a = ex2(fmaf(__uint_as_float(sr[c + e]), mul, -ref)), d = ex2(fmaf(__uint_as_float(sr[c + e + 1]), mul, -ref));
-                            sum[e & 2] += a;
-                            sum[(e & 2) + 1] += d;
-                            pk[e / 2] = pack_bf16(a, d);
+                        for (int e = 0; e < 32; e += 2) {
+                            float x, y;
+                            unpair(fma2(pair(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), mul, neg), x, y);
+                            if (hide) {
+                                const int j = j0 + col0 + c + e;
+                                if (j > see_hi || j < see_lo) x = -INFINITY;
+                                if (j + 1 > see_hi || j + 1 < see_lo) y = -INFINITY;
+                            }
+                            top = max3(top, x, y);
+                            x = ex2(x);
+                            y = ex2(y);
+                            sum2[(e >> 1) & 1] = add2(sum2[(e >> 1) & 1], pair(x, y));
+                            pk[(c + e) / 2] = pack_bf16(x, y);
                         }
-                        tmem_st32(s_addr + c / 2, pk);
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                };
+                if (ok) tc::fence_after();
+                for (int attempt = 0; attempt < 3; ++attempt) {         // the second always suffices: nothing exceeds a reference that was just moved
+                    use = m == -INFINITY ? 0.f : m;
+                    if (ok) {
+                        if (masked) pass(std::true_type{});
+                        else pass(std::false_type{});
+                    }
+                    bool raise = ok && (top > 8.f || (m == -INFINITY && top > -INFINITY));
+                    if (C::kTiles == 1) {
+                        // The two threads of a row move together, and all scores are read before any P is written.  (Every warp passes these barriers, also
+                        // one that gave up.)
+                        int any;
+                        asm volatile("{ .reg .pred p, q; setp.ne.b32 p, %1, 0; barrier.cta.red.or.pred q, 2, %2, p; selp.b32 %0, 1, 0, q; }"
+                                     : "=r"(any) : "r"((int)raise), "n"(C::kSoft) : "memory");
+                        if (!any) break;
+                        s_half[part_of][r] = top;
+                        asm volatile("bar.sync 2, %0;" ::"n"(C::kSoft) : "memory");
+                        top = fmaxf(s_half[0][r], s_half[1][r]);
+                        if (ok && i > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_pv), (uint32_t)(gi - 1) & 1u, P.wait_cycles));
+                        raise = ok && (top > 8.f || (m == -INFINITY && top > -INFINITY));
+                    } else if (!__any_sync(0xffffffffu, raise)) {
+                        break;
+                    }
+                    // O holds the steps before this one.  Their last product is over: with one tile that was waited for, with two the scores' arrival says so.
+                    const float f = raise ? ex2(m - (use + top)) : 1.f;
+                    if (raise) m = use + top;
+                    l *= f;
+                    if (ok && i > 0) {
+                        tc::fence_after();
+                        rescale(f);
+                    }
+                }
+                if (ok) {
+                    float a, d;
+                    unpair(add2(sum2[0], sum2[1]), a, d);
+                    l += a + d;
+                    const uint32_t p_addr = lane_addr + which * kKeys + col0 / 2;
+#pragma unroll
+                    for (int c = 0; c < C::kCols / 2; c += 16) tmem_st16(p_addr + c, pk + c);
                     tc::tmem_wait_st();
                 }
                 if (masked) {
@@ -353,12 +425,17 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             tc::fence_after();
             const int64_t row = (q0 + tok) * P.q_heads + h * P.group + r % P.group;
             const bool any = see_hi >= 0;
+            if (C::kTiles == 1) {
+                s_half[part_of][r] = l;
+                asm volatile("bar.sync 2, %0;" ::"n"(C::kSoft) : "memory");
+                l = s_half[0][r] + s_half[1][r];
+            }
             const float inv = any ? 1.f / l : 0.f;
             if (!ok) *(volatile int*)&s_timeout = 1;
-            if (ok && live && P.splits > 1) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(m, l);
+            if (ok && live && P.splits > 1 && o_col == 0) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(m, l);
             if (ok && !(P.splits > 1 && n_it == 0)) {
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
+                for (int c = o_col; c < o_col + kOCols; c += 32) {
                     uint32_t o[32];
                     if (n_it > 0) {
                         tc::tmem_ld32(o_addr + c, o);

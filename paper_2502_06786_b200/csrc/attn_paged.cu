@@ -66,12 +66,12 @@ int launch_decode(const CUtensorMap& tk, const CUtensorMap& tv, const Params& P,
     return MATQ_OK;
 }
 
-template <int D, int TILES>
+template <int D, int TILES, bool CAP>
 int launch_chunk(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const Params& P, unsigned grid, cudaStream_t s) {
     using C = ChunkCfg<D, TILES>;
     static std::atomic<unsigned long long> smem_ok{0};
-    if (!opt_in_max_smem(attn_chunk_kernel<D, TILES>, smem_ok)) return MATQ_ERR_CUDA;
-    if (launch_overlapped(attn_chunk_kernel<D, TILES>, dim3(grid), dim3(C::kThreads), C::kSmem, s, tq, tk, tv, P) != cudaSuccess) {
+    if (!opt_in_max_smem(attn_chunk_kernel<D, TILES, CAP>, smem_ok)) return MATQ_ERR_CUDA;
+    if (launch_overlapped(attn_chunk_kernel<D, TILES, CAP>, dim3(grid), dim3(C::kThreads), C::kSmem, s, tq, tk, tv, P) != cudaSuccess) {
         cudaGetLastError();
         return MATQ_ERR_CUDA;
     }
@@ -86,9 +86,9 @@ int launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, 
     } else if (kind == 16) {
         st = launch_decode<D, 2>(tk, tv, P, grid, s);
     } else if (kind == 1) {
-        st = launch_chunk<D, 1>(tq, tk, tv, P, grid, s);
+        st = P.softcap > 0.f ? launch_chunk<D, 1, true>(tq, tk, tv, P, grid, s) : launch_chunk<D, 1, false>(tq, tk, tv, P, grid, s);
     } else {
-        if constexpr (D <= 128) st = launch_chunk<D, 2>(tq, tk, tv, P, grid, s);
+        if constexpr (D <= 128) st = P.softcap > 0.f ? launch_chunk<D, 2, true>(tq, tk, tv, P, grid, s) : launch_chunk<D, 2, false>(tq, tk, tv, P, grid, s);
         else st = MATQ_ERR_UNSUPPORTED;
     }
     if (st != MATQ_OK) return st;

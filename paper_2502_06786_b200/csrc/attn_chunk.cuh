@@ -3,7 +3,10 @@
 // A query tile is 128 accumulator rows: floor(128 / group) tokens times the heads of one key head's group, so that a key is read once for the
 // whole group.  A CTA takes kTiles such tiles and walks the keys that they see, kKeys at a time:
 //   warps 8, 9         producers: queries once and keys; values; a ring each (one box per page and 64 columns, 128-byte swizzle);
-//   warp 10            issues S = Q K^T and O += P V (tcgen05.mma, both accumulators and P in tensor memory);
+//   warps 10, 11       one thread each issues S = Q K^T and O += P V (tcgen05.mma, accumulators and P in tensor memory): with two tiles each
+//                      takes one of them, with one tile one takes the scores and the other the products.  A wait on a barrier costs an issuing thread
+//                      250 cycles even when it has been arrived on, about four products; with two threads the tensor cores have the other's meanwhile
+//                      (8192 tokens over 8192, 32/8 heads of 128: one thread 1.62 ms).
 //   warps 0 .. 7       softmax, one thread per row (two, with half of the keys each, when there is one tile): S from tensor memory, exponentials,
 //                      P back over S as bf16.
 // P takes the place of S: the product with V that reads it is issued before the scores that overwrite it.  The row maximum is a reference only: it
@@ -32,7 +35,7 @@ struct ChunkCfg {
     static constexpr int kStagesK = D == 64 ? 4 : 3, kStagesV = D == 64 ? 4 : TILES * D == 128 ? 3 : 2;
     static constexpr int kSoft = 256;                                   // softmax threads: one per row of two tiles, two per row of one
     static constexpr int kCols = kKeys * TILES / 2;                     // keys of a step per softmax thread
-    static constexpr int kThreads = kSoft + 96;
+    static constexpr int kThreads = kSoft + 128;
     static constexpr int kTmemO = 256;                                  // first column of the output accumulators; S starts at column 0
     static constexpr size_t kSmem = (size_t)kTiles * kQBytes + (size_t)(kStagesK + kStagesV) * kKvBytes + 1024;
 };
@@ -62,7 +65,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     using C = ChunkCfg<D, TILES>;
     constexpr int kKeys = C::kKeys;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t s_kfull[C::kStagesK], s_kempty[C::kStagesK], s_vfull[C::kStagesV], s_vempty[C::kStagesV], s_q, s_score[2], s_prob[2], s_pv, s_out, s_read;
+    __shared__ __align__(8) uint64_t s_kfull[C::kStagesK], s_kempty[C::kStagesK], s_vfull[C::kStagesV], s_vempty[C::kStagesV], s_q, s_score[2], s_prob[2], s_pv[2], s_out, s_read;
     __shared__ uint32_t s_tmem;
     __shared__ Sequence s_seq;
     __shared__ int s_timeout, s_any_bad, s_bad_key[kMaxMasked];
@@ -72,14 +75,14 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     unsigned char* smem = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
     unsigned char* ring_k = smem + C::kTiles * C::kQBytes;
     unsigned char* ring_v = ring_k + C::kStagesK * C::kKvBytes;
-    constexpr int kWarpK = C::kSoft / 32, kWarpV = kWarpK + 1, kWarpMma = kWarpK + 2;
+    constexpr int kWarpK = C::kSoft / 32, kWarpV = kWarpK + 1, kWarpMma = kWarpK + 2;      // and kWarpMma + 1
 
     if (tid == 0) {
         for (int s = 0; s < C::kStagesK; ++s) { tc::mbar_init(tc::smem_u32(&s_kfull[s]), 1); tc::mbar_init(tc::smem_u32(&s_kempty[s]), 1); }
         for (int s = 0; s < C::kStagesV; ++s) { tc::mbar_init(tc::smem_u32(&s_vfull[s]), 1); tc::mbar_init(tc::smem_u32(&s_vempty[s]), 1); }
         tc::mbar_init(tc::smem_u32(&s_q), 1);
         for (int t = 0; t < 2; ++t) { tc::mbar_init(tc::smem_u32(&s_score[t]), 1); tc::mbar_init(tc::smem_u32(&s_prob[t]), C::kSoft / C::kTiles); }
-        tc::mbar_init(tc::smem_u32(&s_pv), 1);
+        for (int x = 0; x < 2; ++x) tc::mbar_init(tc::smem_u32(&s_pv[x]), 1);
         tc::mbar_init(tc::smem_u32(&s_out), 1);
         tc::mbar_init(tc::smem_u32(&s_read), C::kSoft);
         tc::mbar_init_fence();
@@ -162,10 +165,12 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (lane == 0) *(volatile int*)&s_timeout = 1;
                 break;
             }
-        } else if (warp == kWarpMma) {
-            // ---------------- tensor cores: one thread issues
-            if (lane == 0 && n_it > 0) {
-                bool ok = tc::mbar_wait(tc::smem_u32(&s_q), (uint32_t)round & 1u, P.wait_cycles);
+        } else if (warp >= kWarpMma) {
+            // ---------------- tensor cores
+            if (n_it > 0) {
+                const int who = __shfl_sync(0xffffffffu, warp, 0) - kWarpMma;          // (uniform, and known to be)
+                const uint32_t leader = tc::elect_one();
+                bool ok = tc::warp_wait(tc::smem_u32(&s_q), (uint32_t)round & 1u, P.wait_cycles);
                 // Descriptors and slots are stepped, not computed: a product of 16 keys or columns takes 64 cycles, about what a handful of dependent
                 // instructions takes.
                 const uint64_t q_desc = tc::sw128_desc(tc::smem_u32(smem)), k_desc = tc::sw128_desc(tc::smem_u32(ring_k)),
@@ -180,64 +185,64 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     const uint32_t d = tmem + t * kKeys;
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x)
-                        asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
-                                     ::"r"(d), "l"(qd + (uint64_t)((x / 4) * (128 * 128 >> 4) + (x & 3) * 2)),
-                                       "l"(kd + (uint64_t)((x / 4) * (kKeys * 128 >> 4) + (x & 3) * 2)), "r"(idesc_bf16(kKeys, false)), "r"(x > 0 ? 1u : 0u) : "memory");
-                    tc::tc_commit(tc::smem_u32(&s_score[t]));
+                        MATQ_TC_MMA(1, "f16", d, qd + (uint64_t)((x / 4) * (128 * 128 >> 4) + (x & 3) * 2), kd + (uint64_t)((x / 4) * (kKeys * 128 >> 4) + (x & 3) * 2),
+                                    idesc_bf16(kKeys, false), x > 0 ? 1u : 0u, leader);
+                    tc::tc_commit(tc::smem_u32(&s_score[t]), leader);
                 };
                 const auto product = [&](int t, int i) {                // O_t += P_t V
                     const uint64_t vd = v_desc + (uint64_t)(vs * (C::kKvBytes >> 4));
                     const uint32_t d = tmem + C::kTmemO + (C::kTiles == 2 ? t * D : 0);
 #pragma unroll
                     for (int x = 0; x < kKeys / 16; ++x)
-                        asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
-                                     ::"r"(d), "r"(tmem + t * kKeys + x * 8), "l"(vd + (uint64_t)(x * (2048 >> 4))),
-                                       "r"(idesc_bf16(D, true)), "r"((i > 0 || x > 0) ? 1u : 0u) : "memory");
+                        MATQ_TC_MMA_TMEM_A(1, "f16", d, tmem + t * kKeys + x * 8, vd + (uint64_t)(x * (2048 >> 4)), idesc_bf16(D, true), (i > 0 || x > 0) ? 1u : 0u, leader);
                 };
-                const auto first_read = [&](int i) { return i > 0 || round == 0 || tc::mbar_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles); };
-                if (ok) ok = tc::mbar_wait(kfull + 8 * ks, kp, P.wait_cycles);
-                tc::fence_after();
+                const auto first_read = [&](int i) { return i > 0 || round == 0 || tc::warp_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles); };
+                const auto keys_there = [&] { return ok = ok && tc::warp_wait(kfull + 8 * ks, kp, P.wait_cycles); };
+                const auto free_keys = [&] { tc::tc_commit(kempty + 8 * ks, leader); next_k(); };
+                const auto weights_there = [&](int t, uint32_t parity) { return ok = ok && tc::warp_wait(tc::smem_u32(&s_prob[t]), parity, P.wait_cycles); };
+                const auto values_there = [&](int i) { return ok = ok && tc::warp_wait(vfull + 8 * vs, vp, P.wait_cycles) && first_read(i); };
+                const auto free_values = [&] { tc::tc_commit(vempty + 8 * vs, leader); next_v(); };
                 if (C::kTiles == 2) {
-                    if (ok) { scores(0); scores(1); tc::tc_commit(kempty + 8 * ks); next_k(); }
-                    for (int i = 0; i < n_it && ok; ++i) {
-                        const bool more = i + 1 < n_it;
-                        for (int t = 0; t < 2; ++t) {
-                            ok = tc::mbar_wait(tc::smem_u32(&s_prob[t]), (uint32_t)(it + i) & 1u, P.wait_cycles);
-                            if (ok && t == 0) ok = tc::mbar_wait(vfull + 8 * vs, vp, P.wait_cycles) && first_read(i);
-                            if (!ok) break;
+                    // The scores that overwrite P are issued behind the product that reads it, by the same thread.
+                    if (who == 0 && keys_there()) {
+                        tc::fence_after();
+                        scores(0);
+                        scores(1);
+                        free_keys();
+                        for (int i = 0; i < n_it; ++i) {
+                            const uint32_t parity = (uint32_t)(it + i) & 1u;
+                            const bool more = i + 1 < n_it;
+                            if (!values_there(i) || (more && !keys_there()) || !weights_there(0, parity)) break;
                             tc::fence_after();
-                            product(t, i);
-                            if (t == 1) { tc::tc_commit(vempty + 8 * vs); next_v(); }
-                            if (more) {
-                                if (t == 0 && !(ok = tc::mbar_wait(kfull + 8 * ks, kp, P.wait_cycles))) break;
-                                tc::fence_after();
-                                scores(t);
-                                if (t == 1) { tc::tc_commit(kempty + 8 * ks); next_k(); }
-                            }
+                            product(0, i);
+                            if (more) scores(0);
+                            if (!weights_there(1, parity)) break;
+                            tc::fence_after();
+                            product(1, i);
+                            free_values();
+                            if (more) { scores(1); free_keys(); }
                         }
                     }
-                } else {
-                    if (ok) { scores(it & 1); tc::tc_commit(kempty + 8 * ks); next_k(); }
+                } else if (who == 0) {
                     for (int i = 0; i < n_it && ok; ++i) {
-                        if (i + 1 < n_it) {
-                            if (!(ok = tc::mbar_wait(kfull + 8 * ks, kp, P.wait_cycles))) break;
-                            tc::fence_after();
-                            scores((it + i + 1) & 1);
-                            tc::tc_commit(kempty + 8 * ks);
-                            next_k();
-                        }
-                        ok = tc::mbar_wait(tc::smem_u32(&s_prob[(it + i) & 1]), (uint32_t)((it + i) >> 1) & 1u, P.wait_cycles) &&
-                             tc::mbar_wait(vfull + 8 * vs, vp, P.wait_cycles) && first_read(i);
-                        if (!ok) break;
+                        // The product that read this buffer's last P is over.  (The first two of a tile: queries arrive after the tile before has ended.)
+                        if (i >= 2) ok = tc::warp_wait(tc::smem_u32(&s_pv[(it + i) & 1]), (uint32_t)((it + i - 2) >> 1) & 1u, P.wait_cycles);
+                        if (!keys_there()) break;
+                        tc::fence_after();
+                        scores((it + i) & 1);
+                        free_keys();
+                    }
+                } else {
+                    for (int i = 0; i < n_it; ++i) {
+                        if (!weights_there((it + i) & 1, (uint32_t)((it + i) >> 1) & 1u) || !values_there(i)) break;
                         tc::fence_after();
                         product((it + i) & 1, i);
-                        tc::tc_commit(vempty + 8 * vs);
-                        tc::tc_commit(tc::smem_u32(&s_pv));
-                        next_v();
+                        free_values();
+                        tc::tc_commit(tc::smem_u32(&s_pv[(it + i) & 1]), leader);
                     }
                 }
                 if (!ok) { *(volatile int*)&s_timeout = 1; __threadfence_block(); }
-                tc::tc_commit(tc::smem_u32(&s_out));                    // also when giving up: nobody waits for longer than its limit
+                if (who == (C::kTiles == 2 ? 0 : 1)) tc::tc_commit(tc::smem_u32(&s_out), leader);    // also when giving up: nobody waits for longer than its limit
             }
             __syncwarp();
         } else {
@@ -352,7 +357,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         s_half[part_of][r] = top;
                         asm volatile("bar.sync 2, %0;" ::"n"(C::kSoft) : "memory");
                         top = fmaxf(s_half[0][r], s_half[1][r]);
-                        if (ok && i > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_pv), (uint32_t)(gi - 1) & 1u, P.wait_cycles));
+                        if (ok && i > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_pv[(gi - 1) & 1]), (uint32_t)((gi - 1) >> 1) & 1u, P.wait_cycles));
                         raise = ok && (top > 8.f || (m == -INFINITY && top > -INFINITY));
                     } else if (!__any_sync(0xffffffffu, raise)) {
                         break;

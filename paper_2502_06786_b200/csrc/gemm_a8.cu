@@ -103,30 +103,27 @@ gemm_a8_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
                 tc::mbar_wait(full + 8 * (i % P.stages), (uint32_t)(i / P.stages) & 1u, P.wait_cycles);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = idesc_i8(kBM, P.nt), full = tc::smem_u32(s_full), empty = tc::smem_u32(s_empty);
-            const uint64_t desc0 = tc::sw128_desc(tc::smem_u32(ring));
-            int s = 0;
-            uint32_t phase = 0, more = 0;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (!tc::mbar_wait(full + 8 * s, phase, P.wait_cycles)) {
-                    *(volatile int*)&s_timeout = 1;
-                    __threadfence_block();
-                    break;
-                }
-                tc::fence_after();
-                const uint64_t w = desc0 + (uint64_t)(s * (stage_bytes >> 4));
-#pragma unroll
-                for (int kk = 0; kk < kBK / 32; ++kk) {
-                    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p; }"
-                                 ::"r"(tmem), "l"(w + (uint64_t)(kk * 2)), "l"(w + (uint64_t)((kBM * kBK >> 4) + kk * 2)), "r"(idesc), "r"(more) : "memory");
-                    more = 1;
-                }
-                tc::tc_commit(empty + 8 * s);
-                if (++s == P.stages) { s = 0; phase ^= 1u; }
+        const uint32_t leader = tc::elect_one(), idesc = idesc_i8(kBM, P.nt), full = tc::smem_u32(s_full), empty = tc::smem_u32(s_empty);
+        const uint64_t desc0 = tc::sw128_desc(tc::smem_u32(ring));
+        int s = 0;
+        uint32_t phase = 0, more = 0;
+        for (int kb = kb0; kb < kb1; ++kb) {
+            if (!tc::warp_wait(full + 8 * s, phase, P.wait_cycles)) {
+                *(volatile int*)&s_timeout = 1;
+                __threadfence_block();
+                break;
             }
-            tc::tc_commit(tc::smem_u32(&s_acc));
+            tc::fence_after();
+            const uint64_t w = desc0 + (uint64_t)(s * (stage_bytes >> 4));
+#pragma unroll
+            for (int kk = 0; kk < kBK / 32; ++kk) {
+                MATQ_TC_MMA(1, "i8", tmem, w + (uint64_t)(kk * 2), w + (uint64_t)((kBM * kBK >> 4) + kk * 2), idesc, more, leader);
+                more = 1;
+            }
+            tc::tc_commit(empty + 8 * s, leader);
+            if (++s == P.stages) { s = 0; phase ^= 1u; }
         }
+        tc::tc_commit(tc::smem_u32(&s_acc), leader);
     } else {
         if (n < P.N) { al = P.alpha[n]; zc = P.zero[n] - 128.f; }
         if (P.early) after_previous_kernel();
@@ -231,8 +228,9 @@ __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* t
                  ::"r"(dst), "l"(tm), "r"(x), "r"(y), "r"(cluster_bar) : "memory");
 }
 // arrives on the same barrier of both CTAs when every product issued so far has ended
-__device__ __forceinline__ void commit_pair(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+__device__ __forceinline__ void commit_pair(uint32_t bar, uint32_t leader) {
+    asm volatile("{ .reg .pred e; setp.ne.b32 e, %2, 0; @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1; }"
+                 ::"r"(bar), "h"((uint16_t)3), "r"(leader) : "memory");
 }
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
@@ -299,8 +297,8 @@ gemm_a8_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
-            const uint32_t idesc = idesc_i8(2 * kBM, P.nt);
+        if (rank == 0) {
+            const uint32_t leader = tc::elect_one(), idesc = idesc_i8(2 * kBM, P.nt);
             bool ok = true;
             int s = 0;
             uint32_t phase = 0;
@@ -308,26 +306,25 @@ gemm_a8_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
             const uint64_t desc0 = tc::sw128_desc(tc::smem_u32(ring));
             for (int tile = pair; tile < tiles; tile += pairs, ++round) {
                 const int a = round & 1;
-                if (ok) ok = tc::mbar_wait(tc::smem_u32(&s_read[a]), ((uint32_t)(round >> 1) & 1u) ^ 1u, P.wait_cycles);
+                ok = tc::warp_wait(tc::smem_u32(&s_read[a]), ((uint32_t)(round >> 1) & 1u) ^ 1u, P.wait_cycles);
                 tc::fence_after();
                 const uint32_t d = tmem + a * 256;
                 uint32_t more = 0;
                 for (int kb = 0; kb < P.nkb && ok; kb += kPairBlocks) {
-                    if (!(ok = tc::mbar_wait(full + 8 * s, phase, P.wait_cycles))) break;
+                    if (!(ok = tc::warp_wait(full + 8 * s, phase, P.wait_cycles))) break;
                     tc::fence_after();
                     const uint64_t w = desc0 + (uint64_t)(s * (kPairStageBytes >> 4));
 #pragma unroll
                     for (int kk = 0; kk < kPairBlocks * kBK / 32; ++kk) {
                         const uint64_t at = w + (uint64_t)((kk / 4) * (kPairBlockBytes >> 4) + (kk & 3) * 2);
-                        asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p; }"
-                                     ::"r"(d), "l"(at), "l"(at + (uint64_t)(kBM * kBK >> 4)), "r"(idesc), "r"(more) : "memory");
+                        MATQ_TC_MMA(2, "i8", d, at, at + (uint64_t)(kBM * kBK >> 4), idesc, more, leader);
                         more = 1;
                     }
-                    commit_pair(empty + 8 * s);
+                    commit_pair(empty + 8 * s, leader);
                     if (++s == kPairStages) { s = 0; phase ^= 1u; }
                 }
                 if (!ok) { *(volatile int*)&s_timeout = 1; __threadfence_block(); break; }
-                commit_pair(tc::smem_u32(&s_acc[a]));
+                commit_pair(tc::smem_u32(&s_acc[a]), leader);
             }
         }
     } else {

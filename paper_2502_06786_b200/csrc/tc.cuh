@@ -76,9 +76,24 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t* d) {
                    "=r"(d[8]), "=r"(d[9]), "=r"(d[10]), "=r"(d[11]), "=r"(d[12]), "=r"(d[13]), "=r"(d[14]), "=r"(d[15])
                  : "r"(addr) : "memory");
 }
+// The whole warp runs the loops that issue products, and one lane of it issues them: with the loop under `if (lane == 0)` slots and descriptors are
+// computed per thread and moved to the uniform registers that tcgen05.mma reads, which takes about 120 cycles per product (64 is what one of 128 x 128 x 32 bytes takes).
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t e;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(e));
+    return e;
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, long long limit) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit)); }
+// A from shared memory, or (TMEM_A) from tensor memory
+#define MATQ_TC_MMA(GROUP, KIND, D, A, B, IDESC, ACCUMULATE, LEADER)                                                                       \
+    asm volatile("{ .reg .pred p, e; setp.ne.b32 p, %4, 0; setp.ne.b32 e, %5, 0; @e tcgen05.mma.cta_group::" #GROUP ".kind::" KIND " [%0], %1, %2, %3, p; }" \
+                 ::"r"(D), "l"(A), "l"(B), "r"(IDESC), "r"(ACCUMULATE), "r"(LEADER) : "memory")
+#define MATQ_TC_MMA_TMEM_A(GROUP, KIND, D, A, B, IDESC, ACCUMULATE, LEADER)                                                                \
+    asm volatile("{ .reg .pred p, e; setp.ne.b32 p, %4, 0; setp.ne.b32 e, %5, 0; @e tcgen05.mma.cta_group::" #GROUP ".kind::" KIND " [%0], [%1], %2, %3, p; }" \
+                 ::"r"(D), "r"(A), "l"(B), "r"(IDESC), "r"(ACCUMULATE), "r"(LEADER) : "memory")
 // arrives on a barrier of this CTA when every tcgen05.mma issued so far by this thread has ended
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void tc_commit(uint32_t bar, uint32_t leader) {
+    asm volatile("{ .reg .pred e; setp.ne.b32 e, %1, 0; @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(bar), "r"(leader) : "memory");
 }
 
 // ---------------------------------------------------------------- host side

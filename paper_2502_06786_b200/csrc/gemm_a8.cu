@@ -4,18 +4,15 @@
 namespace matq {
 namespace a8 {
 
-constexpr int kThreads = 192;
-constexpr int kBM = 128;             // channels of a tile: the rows of the accumulator (tensor-memory lanes)
-constexpr int kBK = 128;             // bytes of K per stage: one 128-byte swizzle row
-constexpr int kMaxStages = 8;
+constexpr int kBM = 128;             // channels of a CTA of the pair kernel: the rows of its accumulator (tensor-memory lanes)
+constexpr int kBK = 128;             // bytes of K per block: one 128-byte swizzle row
 constexpr int kMaxNT = 256;
-constexpr int kMaxSplitsK = 8;
 
 struct Params {
     const float *alpha, *zero, *xscale;
     const int32_t* xsum;
     void* Y;
-    int64_t M, N, ldy;
+    int64_t M, N, K, ldy;
     int nkb, nt, splits, stages, tmem_cols, bf16_out, early;
     int32_t* dev_status;
     long long wait_cycles;
@@ -27,22 +24,144 @@ __device__ __forceinline__ uint32_t idesc_i8(int m, int n) {
     return (2u << 4) | (0u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
-__device__ __forceinline__ float finish(int acc, int xsum, float xs, float al, float zc) {
-    return (xs * al) * ((float)(acc - 128 * xsum) - zc * (float)xsum);
+// What an output needs of its token, prepared once per tile: one 16-byte read per output of the pair kernel's epilogue.
+struct __align__(16) Token {
+    float xs, sum;       // scale; sum of its codes
+    int off;             // 128 times that sum
+    int pad;
+};
+__device__ __forceinline__ Token token(const Params& P, int64_t m) {
+    Token t = {0.f, 0.f, 0, 0};
+    if (m < P.M) {
+        const int sum = P.xsum[m];
+        t.xs = P.xscale[m];
+        t.sum = (float)sum;
+        t.off = 128 * sum;
+    }
+    return t;
 }
+__device__ __forceinline__ float finish(int acc, const Token& t, float al, float zc) { return (t.xs * al) * ((float)(acc - t.off) - zc * t.sum); }
+__device__ __forceinline__ void put(float* y, float v) { *y = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* y, float v) { *y = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void store_y(const Params& P, int64_t m, int64_t n, float y) {
-    if (P.bf16_out) static_cast<__nv_bfloat16*>(P.Y)[m * P.ldy + n] = __float2bfloat16_rn(y);
-    else static_cast<float*>(P.Y)[m * P.ldy + n] = y;
+    if (P.bf16_out) put(static_cast<__nv_bfloat16*>(P.Y) + m * P.ldy + n, y);
+    else put(static_cast<float*>(P.Y) + m * P.ldy + n, y);
+}
+// columns c_lo .. cols - 1 of an accumulator to the outputs of one channel
+template <typename T>
+__device__ __forceinline__ void store_columns(uint32_t addr, const Token* tok, int c_lo, int cols, bool live, T* y, int64_t ldy, float al, float zc) {
+    for (int c0 = c_lo; c0 < cols; c0 += 16) {
+        uint32_t d[16];
+        tc::tmem_ld16(addr + c0, d);
+        tc::tmem_wait_ld();
+        T* p = y + (int64_t)c0 * ldy;
+        if (!live) continue;
+        if (c0 + 16 <= cols) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j, p += ldy) put(p, finish((int)d[j], tok[c0 + j], al, zc));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j, p += ldy)
+                if (c0 + j < cols) put(p, finish((int)d[j], tok[c0 + j], al, zc));
+        }
+    }
 }
 
-__global__ void __launch_bounds__(kThreads)
-gemm_a8_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const Params P) {
+// ---------------------------------------------------------------- few tokens: warp-level integer MMA
+//
+// Up to 8 tokens the codes' bytes bound the product, and what is left is latency: no tensor memory, no tensor maps, no cluster (one token, 9216 x 2304:
+// 5.5 us; the split kernel below takes 10.2.  Sixteen tokens, 14336 x 4096: 12.7 and 11.0, so that they go there).  A CTA takes 16 MT
+// channels; its warps take 64-byte pieces of K in turn.  A thread loads 16 bytes of its row's piece: the four bytes per register that mma.sync
+// m16n8k32 wants need not be neighbours in K as long as codes and activations agree, so the 16 bytes are two products' worth of fragments as they
+// are, for codes and activations alike.  The warps' sums meet in shared memory (integers: the order is free).
+constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps, kFewMaxM = 8;
+
+__device__ __forceinline__ void mma_u8s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// MT tiles of 16 channels; UNROLL pieces of K in flight per warp
+template <int MT, int UNROLL>
+__global__ void __launch_bounds__(kFewThreads)
+gemm_a8_few_kernel(const uint8_t* __restrict__ q, int64_t ldw, const int8_t* xq, int64_t ldx, const Params P) {
+    __shared__ int s_sum[8][16 * MT + 1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, kq = (lane & 3) * 16;
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * MT);
+    if (!P.early) after_previous_kernel();
+    let_next_kernel_start();
+    for (int i = tid; i < 8 * (16 * MT + 1); i += kFewThreads) (&s_sum[0][0])[i] = 0;
+    const int K = (int)P.K, pieces = (K + 63) / 64;
+    const uint8_t* wrow[2 * MT];
+    bool wlive[2 * MT];
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) {
+        wlive[i] = n0 + g + 8 * i < P.N;
+        wrow[i] = q + (wlive[i] ? n0 + g + 8 * i : 0) * ldw + kq;
+    }
+    int acc[MT][4];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][e] = 0;
+    bool waited = !P.early;
+    for (int c0 = warp; c0 < pieces; c0 += kFewWarps * UNROLL) {
+        uint4 w[UNROLL][2 * MT], x[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int k = (c0 + u * kFewWarps) * 64;
+#pragma unroll
+            for (int i = 0; i < 2 * MT; ++i) w[u][i] = wlive[i] && k + kq < K ? ld_stream_u4(wrow[i] + k) : make_uint4(0u, 0u, 0u, 0u);
+        }
+        if (!waited) { after_previous_kernel(); waited = true; }         // the first codes are on their way before the activations are known to be there
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int k = (c0 + u * kFewWarps) * 64;
+            x[u] = g < P.M && k + kq < K ? *reinterpret_cast<const uint4*>(xq + (int64_t)g * ldx + k + kq) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                mma_u8s8(acc[i], w[u][2 * i].x, w[u][2 * i + 1].x, w[u][2 * i].y, w[u][2 * i + 1].y, x[u].x, x[u].y);
+                mma_u8s8(acc[i], w[u][2 * i].z, w[u][2 * i + 1].z, w[u][2 * i].w, w[u][2 * i + 1].w, x[u].z, x[u].w);
+            }
+    }
+    if (!waited) after_previous_kernel();
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) atomicAdd(&s_sum[2 * (lane & 3) + (e & 1)][16 * i + g + 8 * (e >> 1)], acc[i][e]);
+    __syncthreads();
+    for (int i = tid; i < 8 * 16 * MT; i += kFewThreads) {
+        const int m = i / (16 * MT), c = i % (16 * MT);
+        const int64_t n = n0 + c;
+        if (m < P.M && n < P.N) store_y(P, m, n, finish(s_sum[m][c], token(P, m), P.alpha[n], P.zero[n] - 128.f));
+    }
+}
+
+inline cudaError_t launch_few(const uint8_t* q, int64_t ldw, const int8_t* xq, int64_t ldx, const Params& P, int sms, cudaStream_t s) {
+    // 32 channels per CTA halve the reads of the activations from the L2; 16 where 32 would leave SMs without work
+    if ((P.N + 31) / 32 >= 2 * sms)
+        return launch_overlapped(gemm_a8_few_kernel<2, 4>, dim3((unsigned)((P.N + 31) / 32)), dim3(kFewThreads), 0, s, q, ldw, xq, ldx, P);
+    return launch_overlapped(gemm_a8_few_kernel<1, 8>, dim3((unsigned)((P.N + 15) / 16)), dim3(kFewThreads), 0, s, q, ldw, xq, ldx, P);
+}
+
+// ---------------------------------------------------------------- some tokens, or too few tiles for the pairs: K split inside a cluster
+//
+// A CTA sums 128 channels x nt tokens over a part of K in tensor memory; the CTAs of a cluster hold the same tile for different parts, put their sums into
+// shared memory and finish every splits-th token each, reading the others' sums from there.  Tiles of up to 64 tokens leave room for two CTAs per SM.
+constexpr int kSplitThreads = 192;
+constexpr int kMaxStages = 8, kMaxSplitsK = 8;
+
+__global__ void __launch_bounds__(kSplitThreads)
+gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const Params P) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_acc;
     __shared__ uint32_t s_tmem;
     __shared__ int s_timeout;
-    __shared__ float s_xs[kMaxNT];
-    __shared__ int s_xsum[kMaxNT];
+    __shared__ Token s_tok[128];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int split = (int)(blockIdx.x % (unsigned)P.splits);            // rank in the cluster
@@ -127,11 +246,7 @@ gemm_a8_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
     } else {
         if (n < P.N) { al = P.alpha[n]; zc = P.zero[n] - 128.f; }
         if (P.early) after_previous_kernel();
-        for (int c = tid - 64; c < P.nt; c += 128) {
-            const bool in = m0 + c < P.M;
-            s_xs[c] = in ? P.xscale[m0 + c] : 0.f;
-            s_xsum[c] = in ? P.xsum[m0 + c] : 0;
-        }
+        for (int c = tid - 64; c < P.nt; c += 128) s_tok[c] = token(P, m0 + c);
         asm volatile("bar.sync 1, 128;" ::: "memory");
         const bool done = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_acc), 0, P.wait_cycles)) && *(volatile int*)&s_timeout == 0;
         if (!done) *(volatile int*)&s_timeout = 1;
@@ -146,7 +261,7 @@ gemm_a8_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
                 if (P.splits == 1) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        if (c0 + j < cols && n < P.N) store_y(P, m0 + c0 + j, n, finish((int)d[j], s_xsum[c0 + j], s_xs[c0 + j], al, zc));
+                        if (c0 + j < cols && n < P.N) store_y(P, m0 + c0 + j, n, finish((int)d[j], s_tok[c0 + j], al, zc));
                 } else {                                                // partial sums go where the stages were: [token][channel]
                     int* part = reinterpret_cast<int*>(ring);
 #pragma unroll
@@ -189,7 +304,7 @@ gemm_a8_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__
                     int sum = 0;
 #pragma unroll
                     for (int r = 0; r < kMaxSplitsK; ++r) sum += v[i][r];
-                    if (c < cols && n < P.N) store_y(P, m0 + c, n, finish(sum, s_xsum[c], s_xs[c], al, zc));
+                    if (c < cols && n < P.N) store_y(P, m0 + c, n, finish(sum, s_tok[c], al, zc));
                 }
             }
         }
@@ -239,8 +354,7 @@ gemm_a8_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
     __shared__ __align__(8) uint64_t s_full[kPairStages], s_empty[kPairStages], s_acc[2], s_read[2];
     __shared__ uint32_t s_tmem;
     __shared__ int s_timeout;
-    __shared__ float s_xs[2][kMaxNT];
-    __shared__ int s_xsum[2][kMaxNT];
+    __shared__ Token s_tok[2][kMaxNT];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = blockIdx.x & 1u;
     unsigned char* ring = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);      // the same offset in both CTAs
@@ -335,11 +449,7 @@ gemm_a8_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
         for (int tile = pair; tile < tiles; tile += pairs, ++round) {
             const int64_t m0 = (int64_t)(tile % m_tiles) * P.nt, n = (int64_t)(tile / m_tiles) * (2 * kBM) + rank * kBM + quad * 32 + lane;
             const int a = round & 1;
-            for (int c = tid - 64; c < P.nt; c += 32 * kPairWarps) {
-                const bool in = m0 + c < P.M;
-                s_xs[a][c] = in ? P.xscale[m0 + c] : 0.f;
-                s_xsum[a][c] = in ? P.xsum[m0 + c] : 0;
-            }
+            for (int c = tid - 64; c < P.nt; c += 32 * kPairWarps) s_tok[a][c] = token(P, m0 + c);
             float al = 0.f, zc = 0.f;
             if (n < P.N) { al = P.alpha[n]; zc = P.zero[n] - 128.f; }
             asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -348,16 +458,8 @@ gemm_a8_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
                 tc::fence_after();
                 const uint32_t addr = tmem + ((uint32_t)(quad * 32) << 16) + a * 256;
                 const int cols = (int)min((int64_t)c_hi, P.M - m0);
-                for (int c0 = c_lo; c0 < cols; c0 += 16) {
-                    uint32_t d[16];
-                    tc::tmem_ld16(addr + c0, d);
-                    tc::tmem_wait_ld();
-                    if (n < P.N) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (c0 + j < cols) store_y(P, m0 + c0 + j, n, finish((int)d[j], s_xsum[a][c0 + j], s_xs[a][c0 + j], al, zc));
-                    }
-                }
+                if (P.bf16_out) store_columns(addr, s_tok[a], c_lo, cols, n < P.N, static_cast<__nv_bfloat16*>(P.Y) + m0 * P.ldy + n, P.ldy, al, zc);
+                else store_columns(addr, s_tok[a], c_lo, cols, n < P.N, static_cast<float*>(P.Y) + m0 * P.ldy + n, P.ldy, al, zc);
                 tc::fence_before();
             } else {
                 *(volatile int*)&s_timeout = 1;
@@ -408,61 +510,61 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
     P.dev_status = dev_status;
     P.hold = tc::test_stall() ? 1 : 0;
     P.wait_cycles = P.hold ? tc::kStallWaitCycles : tc::kWaitCycles;
+    P.K = K;
     P.nkb = (int)((K + kBK - 1) / kBK);
     const int sms = sm_count();
-    CUtensorMap tm_w, tm_x;
-    if (!byte_map(&tm_w, q, N, K, ldw, kBM)) return MATQ_ERR_CUDA;
-
-    if (M > 128) {
+    cudaError_t e;
+    const int pairs = sms / 2;
+    const int64_t n_pair = (N + 2 * kBM - 1) / (2 * kBM);
+    if (M <= kFewMaxM) {
+        e = launch_few(q, ldw, xq, ldxq, P, sms, s);
+    } else if (M <= 64 || n_pair * ((M + 255) / 256) * 2 < pairs) {
+        P.nt = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+        P.tmem_cols = P.nt < 32 ? 32 : P.nt;
+        const int64_t tiles_n = (N + kBM - 1) / kBM, tiles_m = (M + P.nt - 1) / P.nt, room = P.nt <= 64 ? 2 * sms : sms;
+        if (tiles_m > 65535) return MATQ_ERR_SHAPE;
+        P.splits = 1;
+        while (P.splits < kMaxSplitsK && tiles_n * tiles_m * P.splits * 2 <= room && P.nkb >= 4 * P.splits) P.splits *= 2;
+        const int stage_bytes = (kBM + P.nt) * kBK;
+        P.stages = (P.nt <= 64 ? 104 * 1024 : 200 * 1024) / stage_bytes;
+        if (P.stages > kMaxStages) P.stages = kMaxStages;
+        size_t smem = (size_t)P.stages * stage_bytes;
+        if (P.splits > 1 && smem < (size_t)P.nt * kBM * 4) smem = (size_t)P.nt * kBM * 4;
+        CUtensorMap tm_w, tm_x;
+        if (!byte_map(&tm_w, q, N, K, ldw, kBM) || !byte_map(&tm_x, xq, M, K, ldxq, P.nt)) return MATQ_ERR_CUDA;
+        static std::atomic<unsigned long long> split_ok{0};
+        if (!opt_in_max_smem(gemm_a8_split_kernel, split_ok)) return MATQ_ERR_CUDA;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(tiles_n * P.splits), (unsigned)tiles_m);
+        cfg.blockDim = dim3(kSplitThreads);
+        cfg.dynamicSmemBytes = smem + 1024;
+        cfg.stream = s;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)P.splits;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        e = cudaLaunchKernelEx(&cfg, gemm_a8_split_kernel, tm_w, tm_x, P);
+    } else {
         // Tokens per tile: the value whose rounds over the pairs of SMs cost least.
-        const int pairs = sms / 2;
-        const int64_t n_pair = (N + 2 * kBM - 1) / (2 * kBM);
         int64_t best = -1;
-        for (int nt = 256; nt >= 128; nt -= 32) {
+        for (int nt = 256; nt >= 64; nt -= 32) {
             const int64_t tiles = n_pair * ((M + nt - 1) / nt), cost = (tiles + pairs - 1) / pairs * (nt > 192 ? nt : 192);     // below 192 tokens a stage's fixed part shows
             if (best < 0 || cost < best) { best = cost; P.nt = nt; }
         }
         const int64_t tiles = n_pair * ((M + P.nt - 1) / P.nt);
         if (tiles >= (1ll << 30)) return MATQ_ERR_SHAPE;
-        if (!byte_map(&tm_x, xq, M, K, ldxq, P.nt / 2)) return MATQ_ERR_CUDA;
+        CUtensorMap tm_w, tm_x;
+        if (!byte_map(&tm_w, q, N, K, ldw, kBM) || !byte_map(&tm_x, xq, M, K, ldxq, P.nt / 2)) return MATQ_ERR_CUDA;
         static std::atomic<unsigned long long> pair_ok{0};
         if (!opt_in_max_smem(gemm_a8_pair_kernel, pair_ok)) return MATQ_ERR_CUDA;
         const unsigned grid = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
-        if (launch_overlapped(gemm_a8_pair_kernel, dim3(grid), dim3(kPairThreads), (size_t)kPairStages * kPairStageBytes + 1024, s, tm_w, tm_x, P) != cudaSuccess) {
-            cudaGetLastError();
-            return MATQ_ERR_CUDA;
-        }
-        return launch_status();
+        e = launch_overlapped(gemm_a8_pair_kernel, dim3(grid), dim3(kPairThreads), (size_t)kPairStages * kPairStageBytes + 1024, s, tm_w, tm_x, P);
     }
-
-    P.nt = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
-    P.tmem_cols = P.nt < 32 ? 32 : P.nt;
-    const int64_t n_tiles = (N + kBM - 1) / kBM, m_tiles = 1;
-    P.splits = 1;
-    while (P.nt <= 128 && P.splits < kMaxSplitsK && n_tiles * m_tiles * P.splits * 2 <= 2 * sms && P.nkb >= 4 * P.splits) P.splits *= 2;
-    const int stage_bytes = (kBM + P.nt) * kBK;
-    P.stages = (P.nt <= 64 ? 104 * 1024 : 200 * 1024) / stage_bytes;
-    if (P.stages > kMaxStages) P.stages = kMaxStages;
-    size_t smem = (size_t)P.stages * stage_bytes;
-    if (P.splits > 1 && smem < (size_t)P.nt * kBM * 4) smem = (size_t)P.nt * kBM * 4;
-    smem += 1024;
-    if (!byte_map(&tm_x, xq, M, K, ldxq, P.nt)) return MATQ_ERR_CUDA;
-    static std::atomic<unsigned long long> smem_ok{0};
-    if (!opt_in_max_smem(gemm_a8_kernel, smem_ok)) return MATQ_ERR_CUDA;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(n_tiles * P.splits), (unsigned)m_tiles);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)P.splits;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, gemm_a8_kernel, tm_w, tm_x, P) != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
+    if (e != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
     return launch_status();
 }

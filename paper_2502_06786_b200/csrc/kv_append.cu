@@ -1,10 +1,9 @@
 // matq_kv_append: new keys and values into a paged cache, keys and queries rotated by their positions on the way.
 //
-// Every element is read once and written once and meets three or four operations: HBM-bound for prompts, a chain of four trips to memory
-// (sequence bounds -> length -> page and angles -> store) for a decode step.  A CTA takes one token; a thread takes pieces of
-// 16 bytes.  With halves as pairs a piece is eight elements of the first half together with their partners, so that each thread
-// holds both members of its pairs; neighbouring elements as pairs lie within one piece.  The data loads do not depend on the position and are
-// issued before it is known.
+// Every element is read once and written once and meets three or four operations: HBM-bound for prompts, a chain of trips to memory (sequence bounds
+// -> length -> page and angles -> store) for a decode step.  A CTA takes one token; a thread keeps its place within the heads and walks over
+// queries, keys and values, so that its angles stay in registers.  A place is two pieces of eight elements: with halves as pairs a piece of the first
+// half and its partners, otherwise neighbours.  The data of its first heads are requested before the position is known.
 #include "common.cuh"
 
 namespace matq {
@@ -39,50 +38,36 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
     return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
 }
 
-// One piece of work of a token: `a` (and its partner `b` when the piece holds the first members of eight pairs)
-struct Piece {
-    const uint4* src;
-    const uint4* src2;
-    int head, elem, kind;       // kind 0 query, 1 key, 2 value
-    bool live;
-};
+constexpr int kAhead = 2;        // heads per thread whose data are requested before the position is known
 
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(const Params P) {
+__global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const Params P) {
     after_previous_kernel();
     let_next_kernel_start();
     const int64_t t = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 31;
-    const int halves = P.interleaved ? 0 : P.rot / 16;                 // pieces of two 16-byte halves per rotated head
-    const int rot_pieces = P.interleaved ? P.rot / 8 : halves;
-    const int per_head = rot_pieces + (P.D - P.rot) / 8, per_v = P.D / 8;
-    const int n_rot = (P.q_heads + P.kv_heads) * per_head, total = n_rot + P.kv_heads * per_v;
-
-    auto piece = [&](int i) {
-        Piece w;
-        w.live = i < total;
-        w.src2 = nullptr;
-        w.src = nullptr;
-        w.head = w.elem = w.kind = 0;
-        if (!w.live) return w;
-        if (i < n_rot) {
-            w.head = i / per_head;
-            const int j = i - w.head * per_head;
-            w.elem = j < rot_pieces ? j * 8 : P.rot + (j - rot_pieces) * 8;
-            const bool is_q = w.head < P.q_heads;
-            if (!is_q) w.head -= P.q_heads;
-            w.kind = is_q ? 0 : 1;
-            const __nv_bfloat16* base = is_q ? P.q + t * P.ldq : P.k + t * P.ldk;
-            base += (int64_t)w.head * P.D + w.elem;
-            w.src = reinterpret_cast<const uint4*>(base);
-            if (j < halves) w.src2 = reinterpret_cast<const uint4*>(base + P.rot / 2);
-        } else {
-            const int j = i - n_rot;
-            w.head = j / per_v;
-            w.elem = (j - w.head * per_v) * 8;
-            w.kind = 2;
-            w.src = reinterpret_cast<const uint4*>(P.v + t * P.ldv + (int64_t)w.head * P.D + w.elem);
+    const int heads = P.q_heads + 2 * P.kv_heads, half = P.rot / 2;
+    const int places = (P.D + 15) / 16, step = kThreads / places;       // threads along a head; heads side by side
+    const int y = tid / places, x = tid - y * places;
+    const int first = y < step ? y : heads;                             // left-over threads have no head
+    // this thread's two pieces of a rotated head, and of a value (or of a head whose pairs are neighbours)
+    const bool paired = !P.interleaved && x < P.rot / 16;
+    const int e0 = paired ? x * 8 : x * 16, e1 = paired ? half + x * 8 : x * 16 + 8;
+    const auto source = [&](int hd, int piece) -> const uint4* {
+        if (hd >= heads) return nullptr;
+        const bool value = hd >= P.q_heads + P.kv_heads;
+        const int e = value ? x * 16 + 8 * piece : piece ? e1 : e0;
+        if (e >= P.D) return nullptr;
+        const __nv_bfloat16* row = hd < P.q_heads ? P.q + t * P.ldq + (int64_t)hd * P.D
+                                   : value ? P.v + t * P.ldv + (int64_t)(hd - P.q_heads - P.kv_heads) * P.D : P.k + t * P.ldk + (int64_t)(hd - P.q_heads) * P.D;
+        return reinterpret_cast<const uint4*>(row + e);
+    };
+    uint4 data[kAhead][2];
+    const auto load = [&](int hd, uint4 (&d)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint4* p = source(hd, i);
+            d[i] = p ? *p : make_uint4(0u, 0u, 0u, 0u);
         }
-        return w;
     };
 
     // the token's sequence: the number of sequences that end at or before it (32 bounds per step, every warp for itself)
@@ -92,7 +77,9 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const Params P) {
         const int end = i < P.batch ? P.cu_q[i + 1] : 0x7fffffff;
         b += __popc(__ballot_sync(0xffffffffu, (int64_t)end <= t));
     }
-    if (b >= P.batch) return;                                          // a row that belongs to no sequence
+    if (b >= P.batch) return;                                          // a row that belongs to no sequence (and is not read)
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load(first + i * step, data[i]);
     const int64_t q0 = P.cu_q[b], q1 = P.cu_q[b + 1];
     const int64_t pos = (int64_t)P.kv_len[b] - (q1 - q0) + (t - q0);
     const int64_t pg = pos / P.page_size;
@@ -107,47 +94,63 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const Params P) {
         return;
     }
     const int64_t slot = pos - pg * P.page_size;
+    // angles: of eight pairs when the pieces are partners, of four pairs per piece when neighbours are
     const float* cs = P.cos_sin + pos * P.rot;
-    const int half = P.rot / 2;
-
-    for (int i = tid; i < total; i += kThreads) {
-        const Piece w = piece(i);
-        const uint4 a = *w.src;
-        __nv_bfloat16* dst;
-        if (w.kind == 0) dst = P.q_out + t * P.ldqo + (int64_t)w.head * P.D;
-        else dst = (w.kind == 1 ? P.kc : P.vc) + ((page * P.kv_heads + w.head) * P.page_size + slot) * P.D;
-        dst += w.elem;
-        if (w.src2) {
-            const uint4 b4 = *w.src2;
-            float x[8], y[8], ox[8], oy[8], c[8], s[8];
-            unpack8(a, x);
-            unpack8(b4, y);
-            *reinterpret_cast<float4*>(c) = *reinterpret_cast<const float4*>(cs + w.elem);
-            *reinterpret_cast<float4*>(c + 4) = *reinterpret_cast<const float4*>(cs + w.elem + 4);
-            *reinterpret_cast<float4*>(s) = *reinterpret_cast<const float4*>(cs + half + w.elem);
-            *reinterpret_cast<float4*>(s + 4) = *reinterpret_cast<const float4*>(cs + half + w.elem + 4);
+    float c[8], s[8];
+    const int at = paired ? e0 : e0 / 2;
+    const bool turns = P.rot > 0 && (paired || (P.interleaved && e0 < P.rot));       // rot is a multiple of 16: both pieces of a place turn, or neither
+    if (turns) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                ox[e] = x[e] * c[e] - y[e] * s[e];
-                oy[e] = y[e] * c[e] + x[e] * s[e];
-            }
-            *reinterpret_cast<uint4*>(dst) = pack8(ox);
-            *reinterpret_cast<uint4*>(dst + half) = pack8(oy);
-        } else if (w.kind < 2 && w.elem < P.rot) {                     // neighbouring elements are pairs
-            float x[8], o[8];
-            unpack8(a, x);
-            const float4 c = *reinterpret_cast<const float4*>(cs + w.elem / 2);
-            const float4 s = *reinterpret_cast<const float4*>(cs + half + w.elem / 2);
-            const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                o[2 * e] = x[2 * e] * cc[e] - x[2 * e + 1] * ss[e];
-                o[2 * e + 1] = x[2 * e + 1] * cc[e] + x[2 * e] * ss[e];
-            }
-            *reinterpret_cast<uint4*>(dst) = pack8(o);
-        } else {
-            *reinterpret_cast<uint4*>(dst) = a;
+        for (int i = 0; i < 2; ++i) {
+            const float4 cv = *reinterpret_cast<const float4*>(cs + at + 4 * i), sv = *reinterpret_cast<const float4*>(cs + half + at + 4 * i);
+            c[4 * i] = cv.x; c[4 * i + 1] = cv.y; c[4 * i + 2] = cv.z; c[4 * i + 3] = cv.w;
+            s[4 * i] = sv.x; s[4 * i + 1] = sv.y; s[4 * i + 2] = sv.z; s[4 * i + 3] = sv.w;
         }
+    }
+    const auto finish = [&](int hd, const uint4 (&d)[2]) {
+        if (hd >= heads) return;
+        const bool value = hd >= P.q_heads + P.kv_heads;
+        const int f0 = value ? x * 16 : e0, f1 = value ? x * 16 + 8 : e1;
+        __nv_bfloat16* dst;
+        if (hd < P.q_heads) {
+            dst = P.q_out + t * P.ldqo + (int64_t)hd * P.D;
+        } else {
+            const int h = hd - P.q_heads - (value ? P.kv_heads : 0);
+            dst = (value ? P.vc : P.kc) + ((page * P.kv_heads + h) * P.page_size + slot) * P.D;
+        }
+        uint4 o0 = d[0], o1 = d[1];
+        if (!value && turns) {
+            float a[8], b8[8], oa[8], ob[8];
+            unpack8(d[0], a);
+            unpack8(d[1], b8);
+            if (paired) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    oa[e] = a[e] * c[e] - b8[e] * s[e];
+                    ob[e] = b8[e] * c[e] + a[e] * s[e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    oa[2 * e] = a[2 * e] * c[e] - a[2 * e + 1] * s[e];
+                    oa[2 * e + 1] = a[2 * e + 1] * c[e] + a[2 * e] * s[e];
+                    ob[2 * e] = b8[2 * e] * c[4 + e] - b8[2 * e + 1] * s[4 + e];
+                    ob[2 * e + 1] = b8[2 * e + 1] * c[4 + e] + b8[2 * e] * s[4 + e];
+                }
+            }
+            o0 = pack8(oa);
+            o1 = pack8(ob);
+        }
+        if (f0 < P.D) *reinterpret_cast<uint4*>(dst + f0) = o0;
+        if (f1 < P.D) *reinterpret_cast<uint4*>(dst + f1) = o1;
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) finish(first + i * step, data[i]);
+    for (int hd = first + kAhead * step; hd < heads; hd += kAhead * step) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) load(hd + i * step, data[i]);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) finish(hd + i * step, data[i]);
     }
 }
 
@@ -165,7 +168,7 @@ extern "C" int matq_kv_append(const matq_paged_kv* cache, int64_t T, const void*
     if ((q == nullptr) != (q_out == nullptr)) return MATQ_ERR_INVALID_ARG;
     if (rot_dim > 0 && !cos_sin) return MATQ_ERR_INVALID_ARG;
     const int D = cache->head_dim;
-    if (D % 8 != 0 || rot_dim % 16 != 0 || rot_dim > D || T >= (1ll << 31)) return MATQ_ERR_SHAPE;
+    if (D % 8 != 0 || rot_dim % 16 != 0 || rot_dim > D || D > 16 * kThreads || T >= (1ll << 31)) return MATQ_ERR_SHAPE;
     if (!q) q_heads = 0;
     const int64_t kvw = (int64_t)cache->kv_heads * D, qw = (int64_t)q_heads * D;
     if (ldk < kvw || ldk % 8 != 0 || ldv < kvw || ldv % 8 != 0 || (q && (ldq < qw || ldq % 8 != 0 || ldqo < qw || ldqo % 8 != 0))) return MATQ_ERR_SHAPE;

@@ -9,7 +9,6 @@
 namespace matq {
 namespace tok {
 
-constexpr int kThreads = 256;
 
 // largest of the eight magnitudes, as bf16 bit patterns (their order is that of the magnitudes, NaN above Inf above all)
 __device__ __forceinline__ uint32_t abs_max8(uint4 v, uint32_t m) {
@@ -19,30 +18,44 @@ __device__ __forceinline__ uint32_t abs_max8(uint4 v, uint32_t m) {
     return __vmaxu2(m, v.w & 0x7fff7fffu);
 }
 
-// rne(fl(x / s)) in [-127, 127].  x * (1 / s) is within 1.5 * 2^-23 of x / s, relatively, so below 2^-15 absolutely at magnitudes up to 127:
-// the two round alike unless the product lies that close to a half, and only then is the division done.
-__device__ __forceinline__ int code_of(float x, float s, float inv) {
-    const float r = x * inv;
-    float k = rintf(r);
-    if (fabsf(r - k) > 0.5f - 6.1035e-5f) k = rintf(__fdiv_rn(x, s));
-    return (int)fminf(fmaxf(k, -127.f), 127.f);
+// Codes of eight elements.  k = rne(x * (1 / s)) by adding and taking off 1.5 * 2^23, whose low byte is then k's; no result passes 127, since |x| <= 127 s up to
+// a rounding.  x * (1 / s) is within 1.5 * 2^-23 of x / s relatively, so below 2^-15 absolutely: it rounds like the correctly rounded quotient unless it lies
+// that close to a half, and only then is the division done.
+__device__ __forceinline__ uint32_t bits_of(float x, float inv, float& worst) {
+    constexpr float kMagic = 12582912.f;
+    const float r = x * inv, t = r + kMagic;
+    worst = fmaxf(worst, fabsf(r - (t - kMagic)));
+    return __float_as_uint(t);
 }
-
-__device__ __forceinline__ uint2 codes8(uint4 v, float s, float inv, int& sum) {
+__device__ __noinline__ uint2 codes8_divided(uint4 v, float s) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    uint32_t o[2];
+    uint32_t o[2] = {0u, 0u};
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int c0 = code_of(__uint_as_float(w[2 * h] << 16), s, inv), c1 = code_of(__uint_as_float(w[2 * h] & 0xffff0000u), s, inv);
-        const int c2 = code_of(__uint_as_float(w[2 * h + 1] << 16), s, inv), c3 = code_of(__uint_as_float(w[2 * h + 1] & 0xffff0000u), s, inv);
-        sum += (c0 + c1) + (c2 + c3);
-        o[h] = __byte_perm(__byte_perm((uint32_t)c0, (uint32_t)c1, 0x0040), __byte_perm((uint32_t)c2, (uint32_t)c3, 0x0040), 0x5410);
+    for (int e = 0; e < 8; ++e) {
+        const float x = __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        o[e >> 2] |= ((uint32_t)(int)rintf(__fdiv_rn(x, s)) & 0xffu) << (8 * (e & 3));
     }
     return make_uint2(o[0], o[1]);
 }
+__device__ __forceinline__ uint2 codes8(uint4 v, float s, float inv, int& sum) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t b[8];
+    float worst = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        b[2 * e] = bits_of(__uint_as_float(w[e] << 16), inv, worst);
+        b[2 * e + 1] = bits_of(__uint_as_float(w[e] & 0xffff0000u), inv, worst);
+    }
+    uint2 o = make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
+                         __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
+    if (worst > 0.5f - 6.1035e-5f) o = codes8_divided(v, s);
+    sum = __dp4a((int)o.x, 0x01010101, __dp4a((int)o.y, 0x01010101, sum));
+    return o;
+}
+__device__ __forceinline__ float scale_of(uint32_t mx) { return fmaxf(__fdiv_rn(__uint_as_float(mx << 16), 127.f), 1.17549435e-38f); }
 
 // V > 0: the row fits V 16-byte pieces per thread and stays in registers; V == 0: any length, read twice
-template <int V>
+template <int V, int kThreads>
 __global__ void __launch_bounds__(kThreads)
 quantize_tokens_kernel(const __nv_bfloat16* __restrict__ X, int64_t K, int64_t ldx, int8_t* __restrict__ xq, int64_t ldq,
                        float* __restrict__ scale, int32_t* __restrict__ rowsum, int32_t* dev_status) {
@@ -74,8 +87,7 @@ quantize_tokens_kernel(const __nv_bfloat16* __restrict__ X, int64_t K, int64_t l
 #pragma unroll
     for (int w = 1; w < kThreads / 32; ++w) mx = max(mx, s_max[w]);
     const bool finite = mx < 0x7f80u;
-    const float s = fmaxf(__fdiv_rn(__uint_as_float(mx << 16), 127.f), 1.17549435e-38f);
-    const float inv = __fdiv_rn(1.f, s);
+    const float s = scale_of(mx), inv = __fdiv_rn(1.f, s);
     int sum = 0;
     uint2* out = reinterpret_cast<uint2*>(xq + m * ldq);
     if (V > 0) {
@@ -114,14 +126,20 @@ extern "C" int matq_quantize_tokens(const void* X, int64_t M, int64_t K, int64_t
     if (!aligned16(X) || !aligned16(xq)) return MATQ_ERR_ALIGNMENT;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(X);
-    const dim3 grid((unsigned)M), block(kThreads);
     cudaError_t e;
-    const int64_t per = 8 * kThreads;
-    if (K <= per) e = launch_overlapped(quantize_tokens_kernel<1>, grid, block, 0, st, x, K, ldx, xq, ldq, scale, rowsum, dev_status);
-    else if (K <= 2 * per) e = launch_overlapped(quantize_tokens_kernel<2>, grid, block, 0, st, x, K, ldx, xq, ldq, scale, rowsum, dev_status);
-    else if (K <= 4 * per) e = launch_overlapped(quantize_tokens_kernel<4>, grid, block, 0, st, x, K, ldx, xq, ldq, scale, rowsum, dev_status);
-    else if (K <= 8 * per) e = launch_overlapped(quantize_tokens_kernel<8>, grid, block, 0, st, x, K, ldx, xq, ldq, scale, rowsum, dev_status);
-    else e = launch_overlapped(quantize_tokens_kernel<0>, grid, block, 0, st, x, K, ldx, xq, ldq, scale, rowsum, dev_status);
+    // Few tokens: 256 threads, to spread a row's loads.  Many: 128, so that an SM holds more rows between their two barriers.
+#define MATQ_ROWS(V, THREADS) launch_overlapped(quantize_tokens_kernel<V, THREADS>, dim3((unsigned)M), dim3(THREADS), 0, st, x, K, ldx, xq, ldq, scale, rowsum, dev_status)
+    if (M >= 4 * sm_count() && K <= 8192) {
+        if (K <= 1024) e = MATQ_ROWS(1, 128);
+        else if (K <= 2048) e = MATQ_ROWS(2, 128);
+        else if (K <= 4096) e = MATQ_ROWS(4, 128);
+        else e = MATQ_ROWS(8, 128);
+    } else if (K <= 2048) e = MATQ_ROWS(1, 256);
+    else if (K <= 4096) e = MATQ_ROWS(2, 256);
+    else if (K <= 8192) e = MATQ_ROWS(4, 256);
+    else if (K <= 16384) e = MATQ_ROWS(8, 256);
+    else e = MATQ_ROWS(0, 256);
+#undef MATQ_ROWS
     if (e != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
     return launch_status();
 }

@@ -357,10 +357,14 @@ def _attend_status(news, lens, Hq, Hkv, D, ps, edit, lens_dev=None, cu_dev=None)
 # ------------------------------------------------------------------ error path of the waits, streams, graphs
 
 def test_serving_test_stall_times_out_and_recovers():
-    xq, s, r, q, a, z = _linear(40, 300, 512, 3)
+    xq, s, r, q, a, z = _linear(100, 300, 512, 3)
     xl, sl, rl, ql, al, zl = _linear(600, 600, 512, 4)
+    few = _linear(7, 300, 512, 3)                               # up to 8 tokens there is no device-side wait
     assert mq.serving_test_stall(1) == 0
     try:
+        status = status_word()
+        want, tol = sr.gemm_a8(few[0], few[1], few[3], few[4], few[5], torch.float32)
+        assert bool(((mq.gemm_a8(*few, dev_status=status).double() - want).abs() <= tol).all()) and int(host(status)[0]) == mq.OK
         for args in ((xq, s, r, q, a, z), (xl, sl, rl, ql, al, zl)):
             status = status_word()
             y = torch.full((args[0].shape[0], args[3].shape[0]), 5.0, device="cuda")

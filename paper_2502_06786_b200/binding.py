@@ -119,6 +119,8 @@ def _load():
 
 _lib = _load()
 
+from . import _serving  # noqa: E402  (the serving calls' argument checks, in C++; built beside the library)
+
 
 def lib_path() -> str:
     return _LIB_PATH
@@ -422,65 +424,21 @@ def gemm_multi_static(src_kind, Wsrc, K, X, Ys, alpha, zero, rs=(8, 4, 2), extra
     return _check(st, "matq_gemm_multi_static", raise_on_error)
 
 
-# The serving calls below are short (a decode step's take a few microseconds on the GPU), so their argument checks read each attribute once
-# and pass plain integers.
+# The serving calls below are short (a decode step's take a few microseconds on the GPU): their argument checks and the call itself are in
+# the C++ module _serving, which raises TypeError / ValueError for tensors that do not fit and returns the library's status.
 
-_BF16, _F32, _I32, _I8, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.int8, torch.uint8
-
-
-def _vector(t, dtype, name, n):
-    """Address of a contiguous one-dimensional CUDA tensor of n elements."""
-    if t.dtype is not dtype or not t.is_cuda:
-        _dev(t, dtype, name)
-    if t.dim() != 1 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous, {n} elements required")
-    return t.data_ptr()
-
-
-def _matrix(t, dtype, name):
-    """(address, rows, columns, row stride) of a two-dimensional CUDA tensor with unit stride along its columns."""
-    if t.dtype is not dtype or not t.is_cuda:
-        _dev(t, dtype, name)
-    if t.dim() != 2:
-        raise ValueError(f"{name}: expected 2 dimensions")
-    rows, cols = t.shape
-    ld, unit = t.stride()
-    if unit != 1 and cols > 1:
-        raise ValueError(f"{name}: unit stride along its second dimension required")
-    return t.data_ptr(), rows, cols, ld if rows > 1 else max(cols, ld)
-
-
-def _heads(t, name, D):
-    """(address, tokens, heads, token stride) of a bf16 [T, heads, D] CUDA tensor whose heads of a token are adjacent."""
-    if t.dtype is not _BF16 or not t.is_cuda:
-        _dev(t, _BF16, name)
-    if t.dim() != 3:
-        raise ValueError(f"{name}: expected 3 dimensions")
-    T, H, d = t.shape
-    ld, hs, unit = t.stride()
-    if d != D or unit != 1 or (hs != D and H > 1):
-        raise ValueError(f"{name}: bf16 [T, heads, {D}] with a token's heads adjacent required")
-    return t.data_ptr(), T, H, ld if T > 1 else max(H * D, ld)
-
-
-def _opt(t):
-    return None if t is None else t.data_ptr()
+_BF16 = torch.bfloat16
 
 
 def quantize_tokens(X, xq=None, scale=None, rowsum=None, dev_status=None):
     """matq_quantize_tokens.  X: bf16 [M, K].  Returns (xq int8 [M, K], scale fp32 [M], rowsum int32 [M])."""
-    x, M, K, ldx = _matrix(X, _BF16, "X")
     if xq is None:
-        xq = torch.empty((M, K), dtype=_I8, device=X.device)
+        xq = torch.empty(X.shape, dtype=torch.int8, device=X.device)
     if scale is None:
-        scale = torch.empty(M, dtype=_F32, device=X.device)
+        scale = torch.empty(X.shape[0], dtype=torch.float32, device=X.device)
     if rowsum is None:
-        rowsum = torch.empty(M, dtype=_I32, device=X.device)
-    o, Mo, Ko, ldq = _matrix(xq, _I8, "xq")
-    if Mo != M or Ko != K:
-        raise ValueError("xq: int8 [M, K] required")
-    st = _lib.matq_quantize_tokens(x, M, K, ldx, o, ldq, _vector(scale, _F32, "scale", M), _vector(rowsum, _I32, "rowsum", M),
-                                   _opt(dev_status), _stream())
+        rowsum = torch.empty(X.shape[0], dtype=torch.int32, device=X.device)
+    st = _serving.quantize_tokens(X, xq, scale, rowsum, dev_status)
     if st:
         raise MatqError(st, "matq_quantize_tokens")
     return xq, scale, rowsum
@@ -489,63 +447,21 @@ def quantize_tokens(X, xq=None, scale=None, rowsum=None, dev_status=None):
 def gemm_a8(xq, scale, rowsum, q, alpha, zero, y=None, out_dtype=torch.float32, flags=0, dev_status=None, c=8):
     """matq_gemm_a8.  xq, scale, rowsum: as returned by quantize_tokens; q: uint8 [N, K] codes or a slice of them (unpacked).
     Returns y [M, N], fp32 or bf16 (the type of ``y`` when it is given, ``out_dtype`` otherwise)."""
-    x, M, K, ldx = _matrix(xq, _I8, "xq")
-    w, N, Kw, ldw = _matrix(q, _U8, "q")
-    if Kw != K:
-        raise ValueError("xq [M, K] and q [N, K] required")
     if y is None:
-        y = torch.empty((M, N), dtype=out_dtype, device=xq.device)
-    out_type = OUT_BF16 if y.dtype is _BF16 else OUT_F32
-    o, My, Ny, ldy = _matrix(y, _BF16 if out_type == OUT_BF16 else _F32, "y")
-    if My != M or Ny != N:
-        raise ValueError("y: [M, N] required")
-    st = _lib.matq_gemm_a8(x, M, K, ldx, _vector(scale, _F32, "scale", M), _vector(rowsum, _I32, "rowsum", M), w, N, ldw, c,
-                           _vector(alpha, _F32, "alpha", N), _vector(zero, _F32, "zero", N), out_type, o, ldy, flags,
-                           _opt(dev_status), _stream())
+        y = torch.empty((xq.shape[0], q.shape[0]), dtype=out_dtype, device=xq.device)
+    st = _serving.gemm_a8(xq, scale, rowsum, q, alpha, zero, y, flags, dev_status, c)
     if st:
         raise MatqError(st, "matq_gemm_a8")
     return y
-
-
-def _paged(k_cache, v_cache, page_table, cu_q, kv_len):
-    if k_cache.dtype is not _BF16 or not k_cache.is_cuda or v_cache.dtype is not _BF16 or not v_cache.is_cuda:
-        _dev(k_cache, _BF16, "k_cache"); _dev(v_cache, _BF16, "v_cache")
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or not k_cache.is_contiguous() or not v_cache.is_contiguous():
-        raise ValueError("k_cache, v_cache: contiguous [n_pages, kv_heads, page_size, head_dim] of one shape required")
-    n_pages, Hkv, ps, D = k_cache.shape
-    table, B, width, stride = _matrix(page_table, _I32, "page_table")
-    return PagedKv(k_cache.data_ptr(), v_cache.data_ptr(), n_pages, ps, Hkv, D, B, table, stride, width,
-                   _vector(cu_q, _I32, "cu_q", B + 1), _vector(kv_len, _I32, "kv_len", B)), B, Hkv, D
 
 
 def kv_append(k_cache, v_cache, page_table, cu_q, kv_len, k, v, cos_sin=None, q=None, q_out=None, interleaved=False, dev_status=None):
     """matq_kv_append.  k_cache, v_cache: bf16 [n_pages, kv_heads, page_size, head_dim]; page_table: int32 [B, pages]; cu_q: int32
     [B + 1]; kv_len: int32 [B], the new tokens included; k, v: bf16 [T, kv_heads, head_dim]; cos_sin: fp32 [max_pos, rot_dim] or None (no
     rotation); q: bf16 [T, q_heads, head_dim] or None.  Writes the caches; returns q_out (pass q itself to rotate in place)."""
-    cache, B, Hkv, D = _paged(k_cache, v_cache, page_table, cu_q, kv_len)
-    kp, T, kh, ldk = _heads(k, "k", D)
-    vp, Tv, vh, ldv = _heads(v, "v", D)
-    if kh != Hkv or vh != Hkv or Tv != T:
-        raise ValueError("k and v: [T, kv_heads, head_dim] each required")
-    cs = None
-    max_pos = rot = 0
-    if cos_sin is not None:
-        cs, max_pos, rot, ld = _matrix(cos_sin, _F32, "cos_sin")
-        if ld != rot:
-            raise ValueError("cos_sin: contiguous [max_pos, rot_dim] required")
-    qp = op = None
-    Hq = ldq = ldo = 0
-    if q is not None:
-        qp, Tq, Hq, ldq = _heads(q, "q", D)
-        if q_out is None:
-            q_out = torch.empty((T, Hq, D), dtype=_BF16, device=q.device)
-        op, To, Ho, ldo = _heads(q_out, "q_out", D)
-        if Tq != T or To != T or Ho != Hq:
-            raise ValueError("q and q_out: one row per token each, of the same heads")
-    elif q_out is not None:
-        raise ValueError("q_out without q")
-    st = _lib.matq_kv_append(C.byref(cache), T, qp, Hq, ldq, kp, ldk, vp, ldv, cs, max_pos, rot, 1 if interleaved else 0, op, ldo,
-                             _opt(dev_status), _stream())
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=_BF16, device=q.device)
+    st = _serving.kv_append(k_cache, v_cache, page_table, cu_q, kv_len, k, v, cos_sin, q, q_out, interleaved, dev_status)
     if st:
         raise MatqError(st, "matq_kv_append")
     return q_out
@@ -559,20 +475,14 @@ def attn_paged(q, k_cache, v_cache, page_table, cu_q, kv_len, max_q, max_kv, sca
                workspace=None, dev_status=None):
     """matq_attn_paged.  q: bf16 [T, q_heads, head_dim]; the cache as in kv_append; max_q, max_kv: host-side upper bounds of the new
     tokens and the keys of a sequence.  scale defaults to head_dim ** -0.5.  Returns out, bf16 [T, q_heads, head_dim]."""
-    cache, B, Hkv, D = _paged(k_cache, v_cache, page_table, cu_q, kv_len)
-    qp, T, Hq, ldq = _heads(q, "q", D)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=_BF16, device=q.device)
-    op, To, Ho, ldo = _heads(out, "out", D)
-    if To != T or Ho != Hq:
-        raise ValueError("out: one row per token, of q's heads")
+        out = torch.empty(q.shape, dtype=_BF16, device=q.device)
     if workspace is None:
-        need = attn_paged_workspace_bytes(T, B, Hq, Hkv, D, max_q, max_kv, window)
+        need = attn_paged_workspace_bytes(q.shape[0], page_table.shape[0], q.shape[1], k_cache.shape[1], q.shape[2], max_q, max_kv, window)
         if need:
-            workspace = torch.empty(need, dtype=_U8, device=q.device)
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
-    st = _lib.matq_attn_paged(C.byref(cache), T, qp, Hq, ldq, D ** -0.5 if scale is None else scale, softcap, window, max_q, max_kv,
-                              op, ldo, ws, ws_bytes, _opt(dev_status), _stream())
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    st = _serving.attn_paged(q, k_cache, v_cache, page_table, cu_q, kv_len, max_q, max_kv, q.shape[-1] ** -0.5 if scale is None else scale,
+                             softcap, window, out, workspace, dev_status)
     if st:
         raise MatqError(st, "matq_attn_paged")
     return out

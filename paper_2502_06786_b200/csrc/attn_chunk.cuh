@@ -11,8 +11,9 @@
 //                      P back over S as bf16.
 // P takes the place of S: the product with V that reads it is issued before the scores that overwrite it.  The row maximum is a reference only: it
 // moves, and O is rescaled, when a score exceeds it by more than 2^8, which leaves p <= 256 and the quotient O / l unchanged.
-// D <= 128: two tiles, whose softmax and tensor work alternate.  D = 256: tensor memory holds one tile's O and two S buffers of 64 keys,
-// so that the scores of the next keys are computed while the present ones are exponentiated.
+// D <= 128: two tiles, whose softmax and tensor work alternate.  One tile (D = 256, or few rows): two S buffers, so that the scores of the next
+// keys are computed while the present ones are exponentiated.  A step is 128 keys; at D = 256 they come in two ring stages of 64 (with steps of 64 the
+// softmax's fixed part, about 1300 cycles of latencies, came twice as often: 500 tokens over 6011 at 16/8 x 256 heads 70 us in the kernel).
 #pragma once
 
 #include <type_traits>
@@ -28,10 +29,11 @@ template <int D, int TILES>
 struct ChunkCfg {
     static constexpr int kTiles = TILES;
     static_assert(TILES == 1 || (TILES == 2 && D <= 128), "two accumulators and their scores must fit 512 columns");
-    static constexpr int kKeys = D <= 128 ? 128 : 64;
+    static constexpr int kKeys = 128;                                   // keys of a step
+    static constexpr int kSub = D == 256 ? 2 : 1, kStageKeys = kKeys / kSub;         // ring stages of a step, and their keys
     static constexpr int kPanels = D / 64;
     static constexpr int kQBytes = 128 * D * 2;                         // one query tile
-    static constexpr int kKvBytes = kKeys * D * 2;                      // the keys, or the values, of a step
+    static constexpr int kKvBytes = kStageKeys * D * 2;                 // the keys, or the values, of a stage
     static constexpr int kStagesK = D == 64 ? 4 : 3, kStagesV = D == 64 ? 4 : TILES * D == 128 ? 3 : 2;
     static constexpr int kSoft = 256;                                   // softmax threads: one per row of two tiles, two per row of one
     static constexpr int kCols = kKeys * TILES / 2;                     // keys of a step per softmax thread
@@ -63,7 +65,7 @@ template <int D, int TILES, bool CAP>
 __global__ void __launch_bounds__(ChunkCfg<D, TILES>::kThreads, 1)
 attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Params P) {
     using C = ChunkCfg<D, TILES>;
-    constexpr int kKeys = C::kKeys;
+    constexpr int kKeys = C::kKeys, kStageKeys = C::kStageKeys, kSub = C::kSub;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t s_kfull[C::kStagesK], s_kempty[C::kStagesK], s_vfull[C::kStagesV], s_vempty[C::kStagesV], s_q, s_score[2], s_prob[2], s_pv[2], s_out, s_read;
     __shared__ uint32_t s_tmem;
@@ -131,11 +133,11 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const bool v = warp == kWarpV;
             const CUtensorMap* tm = v ? &tm_v : &tm_k;
             const int stages = v ? C::kStagesV : C::kStagesK;
-            const int rows_box = min(P.page_size, kKeys), runs = kKeys / rows_box, boxes = runs * C::kPanels;       // powers of two, 32 boxes at most
+            const int rows_box = min(P.page_size, kStageKeys), runs = kStageKeys / rows_box, boxes = runs * C::kPanels;       // powers of two, 32 boxes at most
             const int run = lane & (runs - 1), x = (lane / runs) * 64;  // this lane's box of a step
-            const uint32_t dst = tc::smem_u32(v ? ring_v : ring_k) + (uint32_t)(x >> 6) * (kKeys * 128) + (uint32_t)run * rows_box * 128;
+            const uint32_t dst = tc::smem_u32(v ? ring_v : ring_k) + (uint32_t)(x >> 6) * (kStageKeys * 128) + (uint32_t)run * rows_box * 128;
             const uint32_t full = tc::smem_u32(v ? s_vfull : s_kfull), empty = tc::smem_u32(v ? s_vempty : s_kempty);
-            const auto row_of = [&](int i) { return cache_row(P, b, h, (int64_t)k_lo + (int64_t)i * kKeys + run * rows_box, rows_box, first, kv_len); };
+            const auto row_of = [&](int i) { return cache_row(P, b, h, (int64_t)k_lo + (int64_t)i * kStageKeys + run * rows_box, rows_box, first, kv_len); };
             bool ok = true;
             if (n_it > 0 && !v) {
                 if (round > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_out), (uint32_t)(round - 1) & 1u, P.wait_cycles));
@@ -148,12 +150,12 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                                             (int)(q0 + t0 + t * tok_tile), tc::smem_u32(&s_q));
                 }
             }
-            int next_row = n_it > 0 ? row_of(0) : 0;                    // a step's pages are looked up while the one before waits
-            int s = it % stages;
-            uint32_t phase = (uint32_t)(it / stages) & 1u;
-            for (int i = 0; i < n_it && ok; ++i) {
+            int next_row = n_it > 0 ? row_of(0) : 0;                    // a stage's pages are looked up while the one before waits
+            int s = kSub * it % stages;
+            uint32_t phase = (uint32_t)(kSub * it / stages) & 1u;
+            for (int i = 0; i < kSub * n_it && ok; ++i) {
                 const int row = next_row;
-                if (i + 1 < n_it) next_row = row_of(i + 1);
+                if (i + 1 < kSub * n_it) next_row = row_of(i + 1);
                 ok = __all_sync(0xffffffffu, tc::mbar_wait(empty + 8 * s, phase ^ 1u, P.wait_cycles)) && !P.hold;
                 if (!ok) break;
                 if (lane == 0) tc::mbar_expect_tx(full + 8 * s, C::kKvBytes);   // the phase cannot end before this arrival, whichever copy comes first
@@ -174,27 +176,28 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 // Descriptors and slots are stepped, not computed: a product of 16 keys or columns takes 64 cycles, about what a handful of dependent
                 // instructions takes.
                 const uint64_t q_desc = tc::sw128_desc(tc::smem_u32(smem)), k_desc = tc::sw128_desc(tc::smem_u32(ring_k)),
-                               v_desc = tc::sw128_desc(tc::smem_u32(ring_v), kKeys * 128, 1024);
+                               v_desc = tc::sw128_desc(tc::smem_u32(ring_v), kStageKeys * 128, 1024);
                 const uint32_t kfull = tc::smem_u32(s_kfull), kempty = tc::smem_u32(s_kempty), vfull = tc::smem_u32(s_vfull), vempty = tc::smem_u32(s_vempty);
-                int ks = it % C::kStagesK, vs = it % C::kStagesV;       // slots of the next keys and values
-                uint32_t kp = (uint32_t)(it / C::kStagesK) & 1u, vp = (uint32_t)(it / C::kStagesV) & 1u;
+                int ks = kSub * it % C::kStagesK, vs = kSub * it % C::kStagesV;         // slots of the next keys and values
+                uint32_t kp = (uint32_t)(kSub * it / C::kStagesK) & 1u, vp = (uint32_t)(kSub * it / C::kStagesV) & 1u;
                 const auto next_k = [&] { if (++ks == C::kStagesK) { ks = 0; kp ^= 1u; } };
                 const auto next_v = [&] { if (++vs == C::kStagesV) { vs = 0; vp ^= 1u; } };
-                const auto scores = [&](int t) {                        // S_t = Q_t K^T
+                const auto scores = [&](int t, int sub) {               // S_t = Q_t K^T for a stage's keys
                     const uint64_t qd = q_desc + (uint64_t)(C::kTiles == 2 ? t * (C::kQBytes >> 4) : 0), kd = k_desc + (uint64_t)(ks * (C::kKvBytes >> 4));
-                    const uint32_t d = tmem + t * kKeys;
+                    const uint32_t d = tmem + t * kKeys + sub * kStageKeys;
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x)
-                        MATQ_TC_MMA(1, "f16", d, qd + (uint64_t)((x / 4) * (128 * 128 >> 4) + (x & 3) * 2), kd + (uint64_t)((x / 4) * (kKeys * 128 >> 4) + (x & 3) * 2),
-                                    idesc_bf16(kKeys, false), x > 0 ? 1u : 0u, leader);
-                    tc::tc_commit(tc::smem_u32(&s_score[t]), leader);
+                        MATQ_TC_MMA(1, "f16", d, qd + (uint64_t)((x / 4) * (128 * 128 >> 4) + (x & 3) * 2), kd + (uint64_t)((x / 4) * (kStageKeys * 128 >> 4) + (x & 3) * 2),
+                                    idesc_bf16(kStageKeys, false), x > 0 ? 1u : 0u, leader);
+                    if (sub == kSub - 1) tc::tc_commit(tc::smem_u32(&s_score[t]), leader);
                 };
-                const auto product = [&](int t, int i) {                // O_t += P_t V
+                const auto product = [&](int t, int i, int sub) {       // O_t += P_t V for a stage's keys
                     const uint64_t vd = v_desc + (uint64_t)(vs * (C::kKvBytes >> 4));
                     const uint32_t d = tmem + C::kTmemO + (C::kTiles == 2 ? t * D : 0);
 #pragma unroll
-                    for (int x = 0; x < kKeys / 16; ++x)
-                        MATQ_TC_MMA_TMEM_A(1, "f16", d, tmem + t * kKeys + x * 8, vd + (uint64_t)(x * (2048 >> 4)), idesc_bf16(D, true), (i > 0 || x > 0) ? 1u : 0u, leader);
+                    for (int x = 0; x < kStageKeys / 16; ++x)
+                        MATQ_TC_MMA_TMEM_A(1, "f16", d, tmem + t * kKeys + sub * (kStageKeys / 2) + x * 8, vd + (uint64_t)(x * (2048 >> 4)), idesc_bf16(D, true),
+                                           (i > 0 || sub > 0 || x > 0) ? 1u : 0u, leader);
                 };
                 const auto first_read = [&](int i) { return i > 0 || round == 0 || tc::warp_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles); };
                 const auto keys_there = [&] { return ok = ok && tc::warp_wait(kfull + 8 * ks, kp, P.wait_cycles); };
@@ -206,38 +209,42 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     // The scores that overwrite P are issued behind the product that reads it, by the same thread.
                     if (who == 0 && keys_there()) {
                         tc::fence_after();
-                        scores(0);
-                        scores(1);
+                        scores(0, 0);
+                        scores(1, 0);
                         free_keys();
                         for (int i = 0; i < n_it; ++i) {
                             const uint32_t parity = (uint32_t)(it + i) & 1u;
                             const bool more = i + 1 < n_it;
                             if (!values_there(i) || (more && !keys_there()) || !weights_there(0, parity)) break;
                             tc::fence_after();
-                            product(0, i);
-                            if (more) scores(0);
+                            product(0, i, 0);
+                            if (more) scores(0, 0);
                             if (!weights_there(1, parity)) break;
                             tc::fence_after();
-                            product(1, i);
+                            product(1, i, 0);
                             free_values();
-                            if (more) { scores(1); free_keys(); }
+                            if (more) { scores(1, 0); free_keys(); }
                         }
                     }
                 } else if (who == 0) {
                     for (int i = 0; i < n_it && ok; ++i) {
                         // The product that read this buffer's last P is over.  (The first two of a tile: queries arrive after the tile before has ended.)
                         if (i >= 2) ok = tc::warp_wait(tc::smem_u32(&s_pv[(it + i) & 1]), (uint32_t)((it + i - 2) >> 1) & 1u, P.wait_cycles);
-                        if (!keys_there()) break;
-                        tc::fence_after();
-                        scores((it + i) & 1);
-                        free_keys();
+                        for (int sub = 0; sub < kSub && keys_there(); ++sub) {
+                            tc::fence_after();
+                            scores((it + i) & 1, sub);
+                            free_keys();
+                        }
                     }
                 } else {
                     for (int i = 0; i < n_it; ++i) {
-                        if (!weights_there((it + i) & 1, (uint32_t)((it + i) >> 1) & 1u) || !values_there(i)) break;
-                        tc::fence_after();
-                        product((it + i) & 1, i);
-                        free_values();
+                        if (!weights_there((it + i) & 1, (uint32_t)((it + i) >> 1) & 1u)) break;
+                        for (int sub = 0; sub < kSub && values_there(i); ++sub) {
+                            tc::fence_after();
+                            product((it + i) & 1, i, sub);
+                            free_values();
+                        }
+                        if (!ok) break;
                         tc::tc_commit(tc::smem_u32(&s_pv[(it + i) & 1]), leader);
                     }
                 }
@@ -383,17 +390,23 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (masked) {
                     // A weight of zero does not silence a NaN or Inf.  Values that no row sees become zero; non-finite ones that only some rows
                     // see leave the tile, and those rows get them at the end.  Every thread looks at one key, all or half of it.
-                    // (The slot's last use was freed before these scores were issued, so the parity wait cannot pass a phase early.)
-                    if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_vfull[gi % C::kStagesV]), (uint32_t)(gi / C::kStagesV) & 1u, P.wait_cycles));
+                    // A slot's use before this one has to be known to be over, or the parity wait could pass a phase early.  With one stage per step that use is
+                    // two or more steps back, whose product these scores were issued behind; with two it is the last step's, whose product is waited for.
+                    static_assert(C::kStagesV >= 2 && (kSub == 1 || C::kStagesV == 2), "see above");
+                    if (kSub == 2 && ok && i > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_pv[(gi - 1) & 1]), (uint32_t)((gi - 1) >> 1) & 1u, P.wait_cycles));
+                    for (int sub = 0; sub < kSub && ok; ++sub) {
+                        const int u = kSub * gi + sub;
+                        ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_vfull[u % C::kStagesV]), (uint32_t)(u / C::kStagesV) & 1u, P.wait_cycles));
+                    }
                     if (ok) {
                         constexpr int kShare = C::kSoft / kKeys;         // threads per key: 2
                         const int key = tid % kKeys, j = j0 + key;
                         const bool unseen = j > p_hi || j < first, all = j <= p_lo && j >= all_from;
-                        const uint32_t vb = tc::smem_u32(ring_v) + (uint32_t)(gi % C::kStagesV) * C::kKvBytes + key * 128;
+                        const uint32_t vb = tc::smem_u32(ring_v) + (uint32_t)((kSub * gi + key / kStageKeys) % C::kStagesV) * C::kKvBytes + (key % kStageKeys) * 128;
                         bool bad = false;
                         if (!all) {
                             for (int ch = tid / kKeys; ch < D / 8; ch += kShare) {
-                                const uint32_t at = vb + (uint32_t)(ch >> 3) * (kKeys * 128) + (((ch & 7) ^ (key & 7)) << 4);
+                                const uint32_t at = vb + (uint32_t)(ch >> 3) * (kStageKeys * 128) + (((ch & 7) ^ (key & 7)) << 4);
                                 if (unseen) {
                                     asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at), "r"(0) : "memory");
                                 } else {

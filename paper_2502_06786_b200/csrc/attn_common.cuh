@@ -177,5 +177,47 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const Params P)
     }
 }
 
+// The same for up to kFewSplits parts (chunks: many rows, few parts): one warp per (token, head), all parts requested at once.
+constexpr int kFewSplits = 8;
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_few_kernel(const Params P) {
+    after_previous_kernel();
+    let_next_kernel_start();
+    const int lane = threadIdx.x & 31;
+    const int64_t rows = P.T * P.q_heads, row = (int64_t)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const int64_t t = row / P.q_heads;
+    if (t >= P.cu_q[P.batch]) return;
+    constexpr int kV = D / 64;
+    float2 ml[kFewSplits], acc[kV];
+    float mx = -INFINITY, sum = 0.f;
+    bool seen = false;
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s) {
+        ml[s] = s < P.splits ? P.part_ml[(int64_t)s * rows + row] : make_float2(-INFINITY, 0.f);
+        mx = fmaxf(mx, ml[s].x);
+    }
+#pragma unroll
+    for (int j = 0; j < kV; ++j) acc[j] = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s) {
+        if (ml[s].x == -INFINITY && ml[s].y == 0.f) continue;           // no keys of this row: the part's sums were not written
+        seen = true;
+        const float w = mx == -INFINITY ? 1.f : ex2(ml[s].x - mx);
+        sum = fmaf(ml[s].y, w, sum);
+        const float2* o = reinterpret_cast<const float2*>(P.part_o + ((int64_t)s * rows + row) * D);
+#pragma unroll
+        for (int j = 0; j < kV; ++j) {
+            const float2 v = o[lane + 32 * j];
+            acc[j].x = fmaf(v.x, w, acc[j].x);
+            acc[j].y = fmaf(v.y, w, acc[j].y);
+        }
+    }
+    const float inv = 1.f / sum;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(P.out + t * P.ldo + (row - t * P.q_heads) * D);
+#pragma unroll
+    for (int j = 0; j < kV; ++j) dst[lane + 32 * j] = seen ? pack_bf16(acc[j].x * inv, acc[j].y * inv) : 0u;
+}
+
 }  // namespace attn
 }  // namespace matq

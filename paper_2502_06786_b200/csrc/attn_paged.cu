@@ -7,7 +7,7 @@ namespace attn {
 
 struct Plan {
     int kind;                    // 1, 2: attn_chunk with so many query tiles of 128 rows per CTA; 8, 16: attn_decode with so many rows
-    int keys;                    // keys of a step: the parts of the key range are multiples of it
+    int keys, stage_keys;        // keys of a step (the parts of the key range are multiples of it) and of a ring stage
     int64_t tiles_per_seq, splits, split_keys;
 };
 
@@ -17,7 +17,8 @@ inline Plan plan(int batch, int kv_heads, int group, int D, int64_t max_q, int64
     const int64_t rows = max_q * group;
     p.kind = rows <= 8 ? 8 : rows <= 16 ? 16 : (rows <= 128 || D == 256 ? 1 : 2);
     const bool decode = p.kind >= 8;
-    const int keys = p.keys = decode ? (D == 256 ? 32 : 64) : (D == 256 ? 64 : 128);
+    const int keys = p.keys = decode ? (D == 256 ? 32 : 64) : 128;
+    p.stage_keys = !decode && D == 256 ? 64 : keys;
     const int64_t tok = decode ? 0 : (int64_t)(128 / group) * p.kind;   // tokens per CTA
     p.tiles_per_seq = decode ? (rows + p.kind - 1) / p.kind : (max_q + tok - 1) / tok;
     if (p.tiles_per_seq < 1) p.tiles_per_seq = 1;
@@ -92,9 +93,12 @@ int launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, 
         else st = MATQ_ERR_UNSUPPORTED;
     }
     if (st != MATQ_OK) return st;
-    if (P.splits > 1 && launch_overlapped(attn_join_kernel<D>, dim3((unsigned)(P.T * P.q_heads)), dim3(kJoinThreads), 0, s, P) != cudaSuccess) {
-        cudaGetLastError();
-        return MATQ_ERR_CUDA;
+    if (P.splits > 1) {
+        const int64_t rows = P.T * P.q_heads;
+        const cudaError_t e = P.splits <= kFewSplits
+            ? launch_overlapped(attn_join_few_kernel<D>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))), dim3(kJoinThreads), 0, s, P)
+            : launch_overlapped(attn_join_kernel<D>, dim3((unsigned)rows), dim3(kJoinThreads), 0, s, P);
+        if (e != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
     }
     return launch_status();
 }
@@ -147,7 +151,7 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     const int64_t grid = p.splits * cache->kv_heads * cache->batch * p.tiles_per_seq;
     if (grid >= (1ll << 31) || (p.splits > 1 && T * q_heads >= (1ll << 31))) return MATQ_ERR_SHAPE;
     CUtensorMap tq, tk, tv;
-    const int box = ps < p.keys ? ps : p.keys;
+    const int box = ps < p.stage_keys ? ps : p.stage_keys;
     if (!cache_map(&tk, cache->k, rows, D, box) || !cache_map(&tv, cache->v, rows, D, box) || !query_map(&tq, q, T, q_heads, D, ldq, group)) return MATQ_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (D == 64) return launch<64>(tq, tk, tv, P, p.kind, (unsigned)grid, s);

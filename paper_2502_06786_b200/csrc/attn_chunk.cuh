@@ -9,8 +9,7 @@
 //                      (8192 tokens over 8192, 32/8 heads of 128: one thread 1.62 ms).
 //   warps 0 .. 7       softmax, one thread per row (two, with half of the keys each, when there is one tile): S from tensor memory, exponentials,
 //                      P back over S as bf16.
-// P takes the place of S: the product with V that reads it is issued before the scores that overwrite it.  The row maximum is a reference only: it
-// moves, and O is rescaled, when a score exceeds it by more than 2^8, which leaves p <= 256 and the quotient O / l unchanged.
+// P takes the place of S: the product with V that reads it is issued before the scores that overwrite it.  The row maximum is a reference only (see kFar).
 // D <= 128: two tiles, whose softmax and tensor work alternate.  One tile (D = 256, or few rows): two S buffers, so that the scores of the next
 // keys are computed while the present ones are exponentiated.  A step is 128 keys; at D = 256 they come in two ring stages of 64 (with steps of 64 the
 // softmax's fixed part, about 1300 cycles of latencies, came twice as often: 500 tokens over 6011 at 16/8 x 256 heads 70 us in the kernel).
@@ -271,6 +270,12 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             asm volatile("bar.sync 1, %0;" ::"n"(C::kSoft) : "memory");
             constexpr int kOCols = D * C::kTiles / 2;                   // outputs of this thread: columns o_col ..
             const int o_col = C::kTiles == 2 ? 0 : part_of * kOCols;
+            const auto soft_any = [&](bool mine) {                       // whether some softmax thread says so; a barrier of them all
+                int any;
+                asm volatile("{ .reg .pred p, q; setp.ne.b32 p, %1, 0; barrier.cta.red.or.pred q, 2, %2, p; selp.b32 %0, 1, 0, q; }"
+                             : "=r"(any) : "r"((int)mine), "n"(C::kSoft) : "memory");
+                return any != 0;
+            };
             const auto rescale = [&](float f) {
 #pragma unroll 1
                 for (int c = 0; c < kOCols; c += 32) {
@@ -294,7 +299,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 float top = -INFINITY, use;
                 uint64_t sum2[2];
                 uint32_t pk[C::kCols / 2];
-                // One pass: exponents x = score - reference, their maximum, 2^x, its sum, bf16.  Should x exceed 8 somewhere the reference moves and
+                // One pass: exponents x = score - reference, their maximum, 2^x, its sum, bf16.  Should x exceed kFar somewhere the reference moves and
                 // the pass is done again; otherwise the maximum costs no second look at the scores.
                 const auto pass = [&](auto hide) {
                     top = -INFINITY;
@@ -346,6 +351,9 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         }
                     }
                 };
+                // A row without a reference (m = -inf) takes 0 for one if its largest score is not far from it, as ordinary scores are not: then its first
+                // step is not done twice.
+                const auto wants = [&] { return ok && (top > kFar || (m == -INFINITY && top < -kFar && top > -INFINITY)); };
                 if (ok) tc::fence_after();
                 for (int attempt = 0; attempt < 3; ++attempt) {         // the second always suffices: nothing exceeds a reference that was just moved
                     use = m == -INFINITY ? 0.f : m;
@@ -353,21 +361,21 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         if (masked) pass(std::true_type{});
                         else pass(std::false_type{});
                     }
-                    bool raise = ok && (top > 8.f || (m == -INFINITY && top > -INFINITY));
+                    bool raise = wants();
                     if (C::kTiles == 1) {
                         // The two threads of a row move together, and all scores are read before any P is written.  (Every warp passes these barriers, also
                         // one that gave up.)
-                        int any;
-                        asm volatile("{ .reg .pred p, q; setp.ne.b32 p, %1, 0; barrier.cta.red.or.pred q, 2, %2, p; selp.b32 %0, 1, 0, q; }"
-                                     : "=r"(any) : "r"((int)raise), "n"(C::kSoft) : "memory");
-                        if (!any) break;
+                        if (!soft_any(raise || (m == -INFINITY && top > -INFINITY))) break;
                         s_half[part_of][r] = top;
                         asm volatile("bar.sync 2, %0;" ::"n"(C::kSoft) : "memory");
                         top = fmaxf(s_half[0][r], s_half[1][r]);
+                        raise = wants();
+                        if (m == -INFINITY && top > -INFINITY && !raise) m = 0.f;
+                        if (!soft_any(raise)) break;
                         if (ok && i > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_pv[(gi - 1) & 1]), (uint32_t)((gi - 1) >> 1) & 1u, P.wait_cycles));
-                        raise = ok && (top > 8.f || (m == -INFINITY && top > -INFINITY));
-                    } else if (!__any_sync(0xffffffffu, raise)) {
-                        break;
+                    } else {
+                        if (m == -INFINITY && top > -INFINITY && !raise) m = 0.f;
+                        if (!__any_sync(0xffffffffu, raise)) break;
                     }
                     // O holds the steps before this one.  Their last product is over: with one tile that was waited for, with two the scores' arrival says so.
                     const float f = raise ? ex2(m - (use + top)) : 1.f;

@@ -7,6 +7,11 @@ namespace matq {
 namespace attn {
 
 constexpr float kLog2e = 1.4426950408889634f;
+// The running maximum of a row is only a reference for the exponents: weights, sums and outputs are floating-point numbers whose relative precision does
+// not depend on it.  It moves when a score lies more than kFar (in exponents of two) above it: weights stay below 2^32, sums over 2^31 keys below 2^63, and
+// what is flushed to zero below 2^-126 is nothing beside a largest weight of 2^-32 or more.  (With 8 in place of 32 rows of a long prompt moved theirs now and
+// then, and a step done again for one row costs its whole warp: 8192 tokens over 8192 at 32/8 x 128 heads took 1.98 ms.)
+constexpr float kFar = 32.f;
 
 struct Params {
     const __nv_bfloat16 *q, *v;
@@ -103,17 +108,20 @@ __device__ __forceinline__ Sequence sequence(const Params& P, int b) {
 // First row, in the cache seen as rows of D elements, of the slots that hold keys key .. key + count - 1 of sequence b, head h (all in one page).
 // Slots of which no query sees a key (below `first`, where a sliding window may have given its pages back, or past the sequence) are not looked up: the
 // row past the end reads as zeros.  So does a page number that is out of range, which is reported.
+__device__ __forceinline__ int page_row(const Params& P, int h, int64_t key, int64_t page) {
+    if (page < 0 || page >= P.n_pages) {
+        report(P.dev_status, MATQ_ERR_PAGE);
+        return (int)(P.n_pages * P.kv_heads * P.page_size);
+    }
+    return (int)((page * P.kv_heads + h) * P.page_size + (key & (P.page_size - 1)));
+}
 __device__ __forceinline__ int cache_row(const Params& P, int b, int h, int64_t key, int count, int first, int kv_len) {
     const int64_t last = P.n_pages * P.kv_heads * P.page_size;
     if (key >= kv_len || key + count <= first) return (int)last;
     const int64_t pg = key >> P.page_shift;
     int64_t page = -1;
     if (pg < P.table_width) page = P.table[(int64_t)b * P.table_stride + pg];
-    if (page < 0 || page >= P.n_pages) {
-        report(P.dev_status, MATQ_ERR_PAGE);
-        return (int)last;
-    }
-    return (int)((page * P.kv_heads + h) * P.page_size + (key & (P.page_size - 1)));
+    return page_row(P, h, key, page);
 }
 
 // Joins the parts of the key range: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  A CTA per (token, head): the weights of the

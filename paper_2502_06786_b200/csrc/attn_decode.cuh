@@ -7,8 +7,7 @@
 //   S^T = K Q^T    (mma.sync m16n8k16: keys are the rows, queries the 8 columns),
 //   O^T += V^T P^T (the head dimension is the rows).
 // Queries as the narrow operand: the other way round 16 rows would be multiplied for the 4 or 2 of a group, and O would take twice the registers.
-// The row maximum is a reference only: it moves, and O is rescaled, when a score exceeds it by more than 2^8, so that the lanes that share a row
-// meet only then.  The warps meet at the end, where their partial results are joined in shared memory.
+// The row maximum is a reference only (see kFar): the lanes that share a row meet only when it moves.  The warps meet at the end, where their partial results are joined in shared memory.
 #pragma once
 
 #include "attn_common.cuh"
@@ -77,6 +76,12 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const int bt = (int)(rest / (unsigned)P.kv_heads);
     const int b = bt / P.tiles_per_seq;
     after_previous_kernel();
+    // Without a window the first keys of a part are known before the sequence's bounds are: their pages' numbers are looked up side by side with them.
+    int early_page = -1;
+    if (warp >= C::kWarps && !P.window) {
+        const int64_t pg = ((int64_t)part * P.split_keys + (int64_t)lane * min(P.page_size, kKeys)) >> P.page_shift;
+        if (pg < P.table_width) early_page = P.table[(int64_t)b * P.table_stride + pg];
+    }
     if (tid == 0) s_seq = sequence(P, b);                               // read once: all warps act on the same numbers
     __syncthreads();
     let_next_kernel_start();
@@ -113,7 +118,15 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
                 const int64_t key = (int64_t)k_lo + (int64_t)i * kKeys + lane * rows_box;
                 return key < k_hi ? cache_row(P, b, h, key, rows_box, first, kv_len) : (int)(P.n_pages * P.kv_heads * P.page_size);
             };
-            int rows_now = 0, rows_next = n_it > 0 ? rows_of(0) : 0, in_block = 0;
+            int rows_now = 0, rows_next = 0, in_block = 0;
+            if (n_it > 0) {
+                if (P.window) {
+                    rows_next = rows_of(0);
+                } else {
+                    const int64_t key = (int64_t)k_lo + lane * rows_box;
+                    rows_next = key < k_hi ? page_row(P, h, key, early_page) : (int)(P.n_pages * P.kv_heads * P.page_size);
+                }
+            }
             bool ok = round == 0 || tc::mbar_wait(tc::smem_u32(&s_tile), (uint32_t)(round - 1) & 1u, P.wait_cycles);
             ok = __all_sync(0xffffffffu, ok) && !P.hold;
             int s = it % C::kStages;
@@ -209,7 +222,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
                             if (j > see_hi[nt][e & 1] || j < see_lo[nt][e & 1]) v = -INFINITY;
                         }
                         x[nt][e] = v;
-                        raise |= v > m[nt][e & 1] + 8.f;                // also from -inf to anything finite
+                        raise |= v > m[nt][e & 1] + kFar;               // also from -inf to anything finite
                     }
                 if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll

@@ -25,11 +25,18 @@ inline Plan plan(int batch, int kv_heads, int group, int D, int64_t max_q, int64
     int64_t range = max_kv;                                             // keys that a tile can see
     if (window > 0 && window + tok + 16 < range) range = window + tok + 16;
     range = (range + keys - 1) / keys + 1;                              // steps; one more when the window starts inside one
-    const int64_t ctas = p.tiles_per_seq * batch * kv_heads;
-    int64_t splits = ctas > 0 ? (decode && ctas >= sms ? (2 * sms + ctas - 1) / ctas : sms / ctas) : 1;
-    if (splits > range * keys / 256) splits = range * keys / 256;       // 256 keys per part at least
-    if (splits > kMaxSplits) splits = kMaxSplits;
-    if (splits < 1) splits = 1;
+    // Parts of the key range: the number whose rounds over the SMs cost least.  Measured, ns: a step of the 128-row kernels; of the few-row kernels 700,
+    // or a stage's bytes at the share of HBM that the CTAs at work leave each other; about 2 us until the first step and after the last; 3 us for the join,
+    // and its bytes.
+    const int64_t ctas = p.tiles_per_seq * batch * kv_heads, row_bytes = ctas * (decode ? p.kind : 128 * p.kind) * D * 8;
+    int64_t best = -1, splits = 1;
+    for (int64_t n = 1; n <= kMaxSplits && n <= range; ++n) {
+        const int64_t at_work = ctas * n < sms ? ctas * n : sms, share = (int64_t)keys * D * 4 * at_work / 6300;
+        const int64_t step = decode ? (share > 700 ? share : 700) : p.kind == 2 ? 1900 : D == 256 ? 2300 : 1400;
+        const int64_t cost = (ctas * n + sms - 1) / sms * ((range + n - 1) / n * step + 2000) + (n > 1 ? 3000 + row_bytes * n / 5000 : 0);
+        if (best < 0 || cost < best) { best = cost; splits = n; }
+        if (ctas * n >= 4 * sms) break;
+    }
     const int64_t per = (range + splits - 1) / splits;
     p.splits = (range + per - 1) / per;
     p.split_keys = per * keys;

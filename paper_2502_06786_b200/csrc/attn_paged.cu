@@ -8,39 +8,53 @@ namespace attn {
 struct Plan {
     int kind;                    // 1, 2: attn_chunk with so many query tiles of 128 rows per CTA; 8, 16: attn_decode with so many rows
     int keys, stage_keys;        // keys of a step (the parts of the key range are multiples of it) and of a ring stage
-    int64_t tiles_per_seq, splits, split_keys;
+    int64_t tiles_per_seq, splits, split_keys, cost;
 };
 
-// Kernel and split from sizes that the host knows.
-inline Plan plan(int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
+// Kernel and split of one kind from sizes that the host knows, and what they cost (ns).
+inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
     Plan p;
     const int64_t rows = max_q * group;
-    p.kind = rows <= 8 ? 8 : rows <= 16 ? 16 : (rows <= 128 || D == 256 ? 1 : 2);
-    const bool decode = p.kind >= 8;
+    p.kind = kind;
+    const bool decode = kind >= 8;
     const int keys = p.keys = decode ? (D == 256 ? 32 : 64) : 128;
     p.stage_keys = !decode && D == 256 ? 64 : keys;
-    const int64_t tok = decode ? 0 : (int64_t)(128 / group) * p.kind;   // tokens per CTA
-    p.tiles_per_seq = decode ? (rows + p.kind - 1) / p.kind : (max_q + tok - 1) / tok;
+    const int64_t tok = decode ? 0 : (int64_t)(128 / group) * kind;     // tokens per CTA
+    p.tiles_per_seq = decode ? (rows + kind - 1) / kind : (max_q + tok - 1) / tok;
     if (p.tiles_per_seq < 1) p.tiles_per_seq = 1;
     int64_t range = max_kv;                                             // keys that a tile can see
     if (window > 0 && window + tok + 16 < range) range = window + tok + 16;
     range = (range + keys - 1) / keys + 1;                              // steps; one more when the window starts inside one
-    // Parts of the key range: the number whose rounds over the SMs cost least.  Measured, ns: a step of the 128-row kernels; of the few-row kernels 700,
-    // or a stage's bytes at the share of HBM that the CTAs at work leave each other; about 2 us until the first step and after the last; 3 us for the join,
-    // and its bytes.
-    const int64_t ctas = p.tiles_per_seq * batch * kv_heads, row_bytes = ctas * (decode ? p.kind : 128 * p.kind) * D * 8;
-    int64_t best = -1, splits = 1;
+    // Parts of the key range: the number whose rounds over the SMs cost least.  Measured, ns: a step of the 128-row kernels; a stage of the few-row kernels
+    // takes its bytes' time at 45 GB/s per SM or at the share of HBM that the CTAs at work leave each other, but 250 while the ring is filled for the first time;
+    // about 2 us until the first step and after the last (6 for the 128-row kernels); 3 us for the join, and its bytes.
+    const int64_t ctas = p.tiles_per_seq * batch * kv_heads, row_bytes = ctas * (decode ? kind : 128 * kind) * D * 8;
+    const int64_t bytes = (int64_t)keys * D * 4, ring = decode ? 192 * 1024 / bytes : 0;
+    int64_t splits = 1;
+    p.cost = -1;
     for (int64_t n = 1; n <= kMaxSplits && n <= range; ++n) {
-        const int64_t at_work = ctas * n < sms ? ctas * n : sms, share = (int64_t)keys * D * 4 * at_work / 6300;
-        const int64_t step = decode ? (share > 700 ? share : 700) : p.kind == 2 ? 1900 : D == 256 ? 2300 : 1400;
-        const int64_t cost = (ctas * n + sms - 1) / sms * ((range + n - 1) / n * step + 2000) + (n > 1 ? 3000 + row_bytes * n / 5000 : 0);
-        if (best < 0 || cost < best) { best = cost; splits = n; }
+        const int64_t at_work = ctas * n < sms ? ctas * n : sms, share = bytes * at_work / 6300, steps = (range + n - 1) / n;
+        const int64_t early = steps < ring ? steps : ring, first = share > 250 ? share : 250, later = share > bytes / 45 ? share : bytes / 45;
+        const int64_t work = decode ? early * first + (steps - early) * later + 2000 : steps * (kind == 2 ? 1900 : D == 256 ? 2300 : 1400) + 6000;
+        const int64_t cost = (ctas * n + sms - 1) / sms * work + (n > 1 ? 3000 + row_bytes * n / 5000 : 0);
+        if (p.cost < 0 || cost < p.cost) { p.cost = cost; splits = n; }
         if (ctas * n >= 4 * sms) break;
     }
     const int64_t per = (range + splits - 1) / splits;
     p.splits = (range + per - 1) / per;
     p.split_keys = per * keys;
     return p;
+}
+
+// Up to 16 rows per sequence and key head: the few-row kernel (16 sequences of 4 drafted tokens, 32/8 heads, windows of 4096 keys, D = 64, 128, 256: 34, 46, 82
+// us; the 128-row kernel 48, 51, 87).  More: one or two query tiles per CTA, whichever costs less.
+inline Plan plan(int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
+    const int64_t rows = max_q * group;
+    if (rows <= 16) return plan_kind(rows <= 8 ? 8 : 16, batch, kv_heads, group, D, max_q, max_kv, window, sms);
+    const Plan one = plan_kind(1, batch, kv_heads, group, D, max_q, max_kv, window, sms);
+    if (rows <= 128 || D == 256) return one;
+    const Plan two = plan_kind(2, batch, kv_heads, group, D, max_q, max_kv, window, sms);
+    return one.cost < two.cost ? one : two;
 }
 
 inline size_t part_bytes(int64_t T, int q_heads, int D, int64_t splits) {

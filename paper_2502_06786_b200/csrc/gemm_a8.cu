@@ -152,8 +152,39 @@ inline cudaError_t launch_few(const uint8_t* q, int64_t ldw, const int8_t* xq, i
 //
 // A CTA sums 128 channels x nt tokens over a part of K in tensor memory; the CTAs of a cluster hold the same tile for different parts, put their sums into
 // shared memory and finish every splits-th token each, reading the others' sums from there.  Tiles of up to 64 tokens leave room for two CTAs per SM.
-constexpr int kSplitThreads = 192;
-constexpr int kMaxStages = 8, kMaxSplitsK = 8;
+// Eight warps store, as in the pair kernel (with four, one token tile of 128 took 6 us to store).
+constexpr int kSplitWarps = 8, kSplitThreads = 32 * (2 + kSplitWarps);
+// A stage is 256 bytes of K here too (with 128, 600 tokens through 2304 x 9216 took 23 us instead of 19, 17 through 10587 x 11072 24 instead of 23).
+constexpr int kMaxStages = 8, kMaxSplitsK = 8, kSplitBlocks = 2;
+
+// Every splits-th token of the tile, from `split` on, every second of them for this warp: sums the parts that the cluster's CTAs hold ([token][channel], this thread's channel
+// at `mine`) and stores the outputs.  All parts of four tokens are requested before the first is added: a load from another SM takes some hundred cycles.
+template <typename T>
+__device__ __forceinline__ void join_tokens(uint32_t mine, const Token* tok, int split, int splits, int odd, int cols, bool live, T* y, int64_t ldy, float al, float zc) {
+    uint32_t from[kMaxSplitsK];
+#pragma unroll
+    for (int r = 0; r < kMaxSplitsK; ++r) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from[r]) : "r"(mine), "r"(min(r, splits - 1)));
+    const int step = 2 * splits;
+    for (int c0 = split + odd * splits; c0 < cols; c0 += 4 * step) {
+        int v[4][kMaxSplitsK];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < kMaxSplitsK; ++r) {
+                const int c = c0 + i * step;
+                v[i][r] = 0;
+                if (r < splits && c < cols) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v[i][r]) : "r"(from[r] + c * kBM * 4));
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = c0 + i * step;
+            int sum = 0;
+#pragma unroll
+            for (int r = 0; r < kMaxSplitsK; ++r) sum += v[i][r];
+            if (c < cols && live) put(y + (int64_t)c * ldy, finish(sum, tok[c], al, zc));
+        }
+    }
+}
 
 __global__ void __launch_bounds__(kSplitThreads)
 gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const Params P) {
@@ -166,8 +197,9 @@ gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int split = (int)(blockIdx.x % (unsigned)P.splits);            // rank in the cluster
     const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)P.splits) * kBM, m0 = (int64_t)blockIdx.y * P.nt;
-    const int kb0 = (int)((int64_t)P.nkb * split / P.splits), kb1 = (int)((int64_t)P.nkb * (split + 1) / P.splits);
-    const int stage_bytes = kBM * kBK + P.nt * kBK;
+    const int nst = (P.nkb + kSplitBlocks - 1) / kSplitBlocks;                 // stages of the whole K; past K the copies bring zeros
+    const int st0 = (int)((int64_t)nst * split / P.splits), st1 = (int)((int64_t)nst * (split + 1) / P.splits);
+    const int block_bytes = (kBM + P.nt) * kBK, stage_bytes = kSplitBlocks * block_bytes;
     unsigned char* ring = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
 
     if (!P.early) after_previous_kernel();
@@ -193,27 +225,27 @@ gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     if (warp == 0) {
         if (lane == 0) {
             // the weights of the first stages are fetched before the activations are known to be there
-            const int ahead = min(P.stages, kb1 - kb0);
-            if (!P.hold) {
-                for (int i = 0; i < ahead; ++i) {
-                    const uint32_t bar = tc::smem_u32(&s_full[i]);
-                    tc::mbar_expect_tx(bar, stage_bytes);
-                    tc::tma_load_2d(tc::smem_u32(ring + (size_t)i * stage_bytes), &tm_w, (kb0 + i) * kBK, (int)n0, bar);
-                }
-            }
-            if (P.early) after_previous_kernel();
             // (each of the two loops over K is one thread's chain of instructions: slots and descriptors are stepped, not computed)
+            const int ahead = min(P.stages, st1 - st0);
             const uint32_t full = tc::smem_u32(s_full), empty = tc::smem_u32(s_empty), base = tc::smem_u32(ring);
+            const auto weights = [&](uint32_t dst, int st, uint32_t bar) {
+                tc::mbar_expect_tx(bar, stage_bytes);
+#pragma unroll
+                for (int i = 0; i < kSplitBlocks; ++i) tc::tma_load_2d(dst + i * block_bytes, &tm_w, (st * kSplitBlocks + i) * kBK, (int)n0, bar);
+            };
+            if (!P.hold)
+                for (int i = 0; i < ahead; ++i) weights(base + (uint32_t)(i * stage_bytes), st0 + i, full + 8 * i);
+            if (P.early) after_previous_kernel();
             int s = 0, issued = 0;
             uint32_t phase = 1;
-            for (int kb = kb0; kb < kb1 && !P.hold; ++kb) {
+            for (int st = st0; st < st1 && !P.hold; ++st) {
                 const uint32_t dst = base + (uint32_t)(s * stage_bytes);
                 if (issued >= ahead) {
                     if (!tc::mbar_wait(empty + 8 * s, phase, P.wait_cycles)) { s_timeout = 1; break; }
-                    tc::mbar_expect_tx(full + 8 * s, stage_bytes);
-                    tc::tma_load_2d(dst, &tm_w, kb * kBK, (int)n0, full + 8 * s);
+                    weights(dst, st, full + 8 * s);
                 }
-                tc::tma_load_2d(dst + kBM * kBK, &tm_x, kb * kBK, (int)m0, full + 8 * s);
+#pragma unroll
+                for (int i = 0; i < kSplitBlocks; ++i) tc::tma_load_2d(dst + i * block_bytes + kBM * kBK, &tm_x, (st * kSplitBlocks + i) * kBK, (int)m0, full + 8 * s);
                 ++issued;
                 if (++s == P.stages) { s = 0; phase ^= 1u; }
             }
@@ -226,7 +258,7 @@ gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         const uint64_t desc0 = tc::sw128_desc(tc::smem_u32(ring));
         int s = 0;
         uint32_t phase = 0, more = 0;
-        for (int kb = kb0; kb < kb1; ++kb) {
+        for (int st = st0; st < st1; ++st) {
             if (!tc::warp_wait(full + 8 * s, phase, P.wait_cycles)) {
                 *(volatile int*)&s_timeout = 1;
                 __threadfence_block();
@@ -235,8 +267,9 @@ gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
             tc::fence_after();
             const uint64_t w = desc0 + (uint64_t)(s * (stage_bytes >> 4));
 #pragma unroll
-            for (int kk = 0; kk < kBK / 32; ++kk) {
-                MATQ_TC_MMA(1, "i8", tmem, w + (uint64_t)(kk * 2), w + (uint64_t)((kBM * kBK >> 4) + kk * 2), idesc, more, leader);
+            for (int kk = 0; kk < kSplitBlocks * kBK / 32; ++kk) {
+                const uint64_t at = w + (uint64_t)((kk / 4) * (block_bytes >> 4) + (kk & 3) * 2);
+                MATQ_TC_MMA(1, "i8", tmem, at, at + (uint64_t)(kBM * kBK >> 4), idesc, more, leader);
                 more = 1;
             }
             tc::tc_commit(empty + 8 * s, leader);
@@ -246,37 +279,33 @@ gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     } else {
         if (n < P.N) { al = P.alpha[n]; zc = P.zero[n] - 128.f; }
         if (P.early) after_previous_kernel();
-        for (int c = tid - 64; c < P.nt; c += 128) s_tok[c] = token(P, m0 + c);
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        for (int c = tid - 64; c < P.nt; c += 32 * kSplitWarps) s_tok[c] = token(P, m0 + c);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
         const bool done = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_acc), 0, P.wait_cycles)) && *(volatile int*)&s_timeout == 0;
         if (!done) *(volatile int*)&s_timeout = 1;
         tc::fence_after();
         const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const int cols = (int)min((int64_t)P.nt, P.M - m0);
-        if (done) {
-            for (int c0 = 0; c0 < cols; c0 += 16) {
+        const int c_lo = ((warp - 2) >> 2) * (P.nt / 2), cols = (int)min((int64_t)(c_lo + P.nt / 2), P.M - m0);      // the two warps of a lane quarter
+        if (done && P.splits == 1) {
+            if (P.bf16_out) store_columns(lane_addr, s_tok, c_lo, cols, n < P.N, static_cast<__nv_bfloat16*>(P.Y) + m0 * P.ldy + n, P.ldy, al, zc);
+            else store_columns(lane_addr, s_tok, c_lo, cols, n < P.N, static_cast<float*>(P.Y) + m0 * P.ldy + n, P.ldy, al, zc);
+        } else if (done) {
+            int* part = reinterpret_cast<int*>(ring) + (warp & 3) * 32 + lane;      // partial sums go where the stages were: [token][channel]
+            for (int c0 = c_lo; c0 < cols; c0 += 16) {
                 uint32_t d[16];
                 tc::tmem_ld16(lane_addr + c0, d);
                 tc::tmem_wait_ld();
-                if (P.splits == 1) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (c0 + j < cols && n < P.N) store_y(P, m0 + c0 + j, n, finish((int)d[j], s_tok[c0 + j], al, zc));
-                } else {                                                // partial sums go where the stages were: [token][channel]
-                    int* part = reinterpret_cast<int*>(ring);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) part[(c0 + j) * kBM + (warp & 3) * 32 + lane] = (int)d[j];
-                }
+                for (int j = 0; j < 16; ++j)
+                    if (c0 + j < cols) part[(c0 + j) * kBM] = (int)d[j];
             }
         }
     }
     if (P.splits > 1) {
-        // The CTAs of a cluster hold the same tile for different parts of K: each finishes every splits-th token.  Integer sums: the order is free.
+        // The CTAs of a cluster hold the same tile for different parts of K.  Integer sums: the order is free.
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned; barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (warp >= 2) {
-            const int cols = (int)min((int64_t)P.nt, P.M - m0);
-            const uint32_t mine = tc::smem_u32(ring) + ((warp & 3) * 32 + lane) * 4;
             bool ok = true;
             for (int r = 0; r < P.splits; ++r) {
                 uint32_t a, t;
@@ -284,29 +313,10 @@ gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
                 asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(t) : "r"(a) : "memory");
                 ok &= t == 0;
             }
-            // all parts of four tokens are requested before the first is added: a load from another SM takes some hundred cycles
-            uint32_t from[kMaxSplitsK];
-#pragma unroll
-            for (int r = 0; r < kMaxSplitsK; ++r) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from[r]) : "r"(mine), "r"(min(r, P.splits - 1)));
-            for (int c0 = split; c0 < cols && ok; c0 += 4 * P.splits) {
-                int v[4][kMaxSplitsK];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int r = 0; r < kMaxSplitsK; ++r) {
-                        const int c = c0 + i * P.splits;
-                        v[i][r] = 0;
-                        if (r < P.splits && c < cols) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v[i][r]) : "r"(from[r] + c * kBM * 4));
-                    }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int c = c0 + i * P.splits;
-                    int sum = 0;
-#pragma unroll
-                    for (int r = 0; r < kMaxSplitsK; ++r) sum += v[i][r];
-                    if (c < cols && n < P.N) store_y(P, m0 + c, n, finish(sum, s_tok[c], al, zc));
-                }
-            }
+            const uint32_t mine = tc::smem_u32(ring) + ((warp & 3) * 32 + lane) * 4;
+            const int cols = (int)min((int64_t)P.nt, P.M - m0), odd = (warp - 2) >> 2;
+            if (ok && P.bf16_out) join_tokens(mine, s_tok, split, P.splits, odd, cols, n < P.N, static_cast<__nv_bfloat16*>(P.Y) + m0 * P.ldy + n, P.ldy, al, zc);
+            else if (ok) join_tokens(mine, s_tok, split, P.splits, odd, cols, n < P.N, static_cast<float*>(P.Y) + m0 * P.ldy + n, P.ldy, al, zc);
         }
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned; barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -514,19 +524,44 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
     P.nkb = (int)((K + kBK - 1) / kBK);
     const int sms = sm_count();
     cudaError_t e;
-    const int pairs = sms / 2;
-    const int64_t n_pair = (N + 2 * kBM - 1) / (2 * kBM);
     if (M <= kFewMaxM) {
         e = launch_few(q, ldw, xq, ldxq, P, sms, s);
-    } else if (M <= 64 || n_pair * ((M + 255) / 256) * 2 < pairs) {
-        P.nt = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+        if (e != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
+        return launch_status();
+    }
+    // Split kernel or pair kernel, and its tile: the shape whose estimated time is least.  Measured, ns: the start 2000 (pairs 2500); 256 bytes of K 350 (pairs 420,
+    // above 168 tokens 2.5 a token); storing a tile 14 a token (pairs 800 and 18, while the next tile is summed); a cluster's join 1200 and 20 a token; an SM's
+    // copies 85 GB/s, HBM 6300.  A cluster's CTAs share a GPC, which leaves clusters of eight about 128 of 148 SMs and clusters of four about 136.
+    const int pairs = sms / 2;
+    const int64_t nst = (P.nkb + 1) / 2, n_pair = (N + 2 * kBM - 1) / (2 * kBM), tiles_n = (N + kBM - 1) / kBM, hbm = N * K / 6300;
+    int64_t best = -1;
+    bool use_pairs = false;
+    for (int nt = 16; nt <= 128; nt *= 2) {
+        const int64_t tiles_m = (M + nt - 1) / nt;
+        if ((nt < 128 && tiles_m > 8) || tiles_m > 65535) continue;
+        for (int sp = 1; sp <= kMaxSplitsK && sp <= nst; sp *= 2) {
+            const int64_t ctas = tiles_n * tiles_m * sp, stages = (nst + sp - 1) / sp, usable = sp == 8 ? sms * 128 / 148 : sp == 4 ? sms * 136 / 148 : sms;
+            const int64_t slots = usable * (nt <= 64 ? 2 : 1), rounds = (ctas + slots - 1) / slots, copies = (ctas + usable - 1) / usable * stages * (kBM + nt) * 256 / 85;
+            int64_t work = rounds * stages * 350;
+            if (work < copies) work = copies;
+            if (work < hbm) work = hbm;
+            const int64_t cost = work + rounds * (2000 + (sp > 1 ? 1200 + 20 * nt : 14 * nt));
+            if (best < 0 || cost < best) { best = cost; P.nt = nt; P.splits = sp; }
+        }
+    }
+    for (int nt = 256; nt >= 64 && M > 32; nt -= 32) {
+        const int64_t tiles = n_pair * ((M + nt - 1) / nt), rounds = (tiles + pairs - 1) / pairs;
+        const int64_t sum = nst * (nt > 168 ? 5 * nt / 2 : 420), store = 800 + 18 * nt;
+        int64_t work = (rounds - 1) * (sum > store ? sum : store) + sum;
+        if (work < hbm) work = hbm;
+        const int64_t cost = 2500 + work + store;
+        if (cost < best) { best = cost; P.nt = nt; use_pairs = true; }
+    }
+    if (!use_pairs) {
         P.tmem_cols = P.nt < 32 ? 32 : P.nt;
-        const int64_t tiles_n = (N + kBM - 1) / kBM, tiles_m = (M + P.nt - 1) / P.nt, room = P.nt <= 64 ? 2 * sms : sms;
-        if (tiles_m > 65535) return MATQ_ERR_SHAPE;
-        P.splits = 1;
-        while (P.splits < kMaxSplitsK && tiles_n * tiles_m * P.splits * 2 <= room && P.nkb >= 4 * P.splits) P.splits *= 2;
-        const int stage_bytes = (kBM + P.nt) * kBK;
-        P.stages = (P.nt <= 64 ? 104 * 1024 : 200 * 1024) / stage_bytes;
+        const int64_t tiles_m = (M + P.nt - 1) / P.nt;
+        const int stage_bytes = kSplitBlocks * (kBM + P.nt) * kBK;
+        P.stages = (P.nt <= 64 && tiles_n * tiles_m * P.splits > sms ? 104 * 1024 : 200 * 1024) / stage_bytes;      // two CTAs share an SM, or one has it
         if (P.stages > kMaxStages) P.stages = kMaxStages;
         size_t smem = (size_t)P.stages * stage_bytes;
         if (P.splits > 1 && smem < (size_t)P.nt * kBM * 4) smem = (size_t)P.nt * kBM * 4;
@@ -550,12 +585,6 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
         cfg.numAttrs = 2;
         e = cudaLaunchKernelEx(&cfg, gemm_a8_split_kernel, tm_w, tm_x, P);
     } else {
-        // Tokens per tile: the value whose rounds over the pairs of SMs cost least.
-        int64_t best = -1;
-        for (int nt = 256; nt >= 64; nt -= 32) {
-            const int64_t tiles = n_pair * ((M + nt - 1) / nt), cost = (tiles + pairs - 1) / pairs * (nt > 192 ? nt : 192);     // below 192 tokens a stage's fixed part shows
-            if (best < 0 || cost < best) { best = cost; P.nt = nt; }
-        }
         const int64_t tiles = n_pair * ((M + P.nt - 1) / P.nt);
         if (tiles >= (1ll << 30)) return MATQ_ERR_SHAPE;
         CUtensorMap tm_w, tm_x;

@@ -471,7 +471,7 @@ int matq_attn_paged(const matq_paged_kv *cache, int64_t T, const void *q, int q_
 /*
  * Testing hook for the error paths of (7) and (9), as matq_gemm_multi_test_stall: while `on` is non-zero their kernels issue no
  * copies and their waits give up after about a millisecond; a call reports MATQ_ERR_TIMEOUT through dev_status, returns, and leaves the
- * GPU ready for the next.  (7) with up to 8 tokens has no device-side wait and ignores it.  Process-wide; returns the previous setting.
+ * GPU ready for the next.  (7) has no device-side wait for up to 8 tokens and few codes, and ignores it there.  Process-wide; returns the previous setting.
  */
 int matq_serving_test_stall(int on);
 

@@ -27,18 +27,23 @@ inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64
     range = (range + keys - 1) / keys + 1;                              // steps; one more when the window starts inside one
     // Parts of the key range: the number whose rounds over the SMs cost least.  Measured, ns: a step of the 128-row kernels; a stage of the few-row kernels
     // takes its bytes' time at 45 GB/s per SM or at the share of HBM that the CTAs at work leave each other, but 250 while the ring is filled for the first time;
-    // about 2 us until the first step and after the last (6 for the 128-row kernels); 3 us for the join, and its bytes.
+    // about 2 us until the first step and after the last (6 for the 128-row kernels); 3 us for the join, and its bytes.  Sequences of a batch differ: without a
+    // window their lengths are taken to average 0.6 of the longest.  More CTAs at work than SMs end half a part after the even share, on average.
     const int64_t ctas = p.tiles_per_seq * batch * kv_heads, row_bytes = ctas * (decode ? kind : 128 * kind) * D * 8;
     const int64_t bytes = (int64_t)keys * D * 4, ring = decode ? 192 * 1024 / bytes : 0;
     int64_t splits = 1;
     p.cost = -1;
+    const double mean = batch > 1 ? (window > 0 && window < max_kv ? 0.9 : 0.6) : 1.0;
     for (int64_t n = 1; n <= kMaxSplits && n <= range; ++n) {
-        const int64_t at_work = ctas * n < sms ? ctas * n : sms, share = bytes * at_work / 6300, steps = (range + n - 1) / n;
-        const int64_t early = steps < ring ? steps : ring, first = share > 250 ? share : 250, later = share > bytes / 45 ? share : bytes / 45;
-        const int64_t work = decode ? early * first + (steps - early) * later + 2000 : steps * (kind == 2 ? 1900 : D == 256 ? 2300 : 1400) + 6000;
-        const int64_t cost = (ctas * n + sms - 1) / sms * work + (n > 1 ? 3000 + row_bytes * n / 5000 : 0);
-        if (p.cost < 0 || cost < p.cost) { p.cost = cost; splits = n; }
-        if (ctas * n >= 4 * sms) break;
+        const double busy = (double)ctas * (n * mean > 1.0 ? n * mean : 1.0), at_work = busy < sms ? busy : sms;      // CTAs with keys
+        const double share = bytes * at_work / 6300.0, first = share > 250 ? share : 250, later = share > bytes / 45.0 ? share : bytes / 45.0;
+        const int64_t steps = (range + n - 1) / n;                      // of the longest part
+        const double step_ns = kind == 2 ? 1900 : D == 256 ? 2300 : 1400;
+        const double part = decode ? (steps < ring ? steps : ring) * first + (steps > ring ? steps - ring : 0) * later + 2000 : steps * step_ns + 6000;
+        const double all = part * busy / sms * (n * mean > 1.0 ? 1.0 : mean);        // the even share (unsplit: of parts of mean length)
+        const double cost = (busy <= sms ? part : all + part / 2) + (n > 1 ? 3000 + row_bytes * n / 5000.0 : 0);
+        if (p.cost < 0 || cost < p.cost) { p.cost = (int64_t)cost; splits = n; }
+        if (ctas * n >= 6 * sms) break;
     }
     const int64_t per = (range + splits - 1) / splits;
     p.splits = (range + per - 1) / per;

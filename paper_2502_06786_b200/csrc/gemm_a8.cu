@@ -69,8 +69,8 @@ __device__ __forceinline__ void store_columns(uint32_t addr, const Token* tok, i
 
 // ---------------------------------------------------------------- few tokens: warp-level integer MMA
 //
-// Up to 8 tokens the codes' bytes bound the product, and what is left is latency: no tensor memory, no tensor maps, no cluster (one token, 9216 x 2304:
-// 5.5 us; the split kernel below takes 10.2.  Sixteen tokens, 14336 x 4096: 12.7 and 11.0, so that they go there).  A CTA takes 16 MT
+// Up to 8 tokens and a few megabytes of codes the product is mostly latency: no tensor memory, no tensor maps, no cluster (5 tokens, 544 x 4064: 3.0 us, the
+// split kernel below 4.2; 8 tokens, 14336 x 4096 from HBM: 15.0 and 12.3, so that those go there).  A CTA takes 16 MT
 // channels; its warps take 64-byte pieces of K in turn.  A thread loads 16 bytes of its row's piece: the four bytes per register that mma.sync
 // m16n8k32 wants need not be neighbours in K as long as codes and activations agree, so the 16 bytes are two products' worth of fragments as they
 // are, for codes and activations alike.  The warps' sums meet in shared memory (integers: the order is free).
@@ -524,14 +524,10 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
     P.nkb = (int)((K + kBK - 1) / kBK);
     const int sms = sm_count();
     cudaError_t e;
-    if (M <= kFewMaxM) {
-        e = launch_few(q, ldw, xq, ldxq, P, sms, s);
-        if (e != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
-        return launch_status();
-    }
-    // Split kernel or pair kernel, and its tile: the shape whose estimated time is least.  Measured, ns: the start 2000 (pairs 2500); 256 bytes of K 350 (pairs 420,
+    // Kernel and tile: the shape whose estimated time is least.  Measured, ns: the start 2000 (pairs 2500); 256 bytes of K 350 (pairs 420,
     // above 168 tokens 2.5 a token); storing a tile 14 a token (pairs 800 and 18, while the next tile is summed); a cluster's join 1200 and 20 a token; an SM's
     // copies 85 GB/s, HBM 6300.  A cluster's CTAs share a GPC, which leaves clusters of eight about 128 of 148 SMs and clusters of four about 136.
+    // The few-token kernel: 2200, and its copies at 45 GB/s per SM, 5000 in all.
     const int pairs = sms / 2;
     const int64_t nst = (P.nkb + 1) / 2, n_pair = (N + 2 * kBM - 1) / (2 * kBM), tiles_n = (N + kBM - 1) / kBM, hbm = N * K / 6300;
     int64_t best = -1;
@@ -557,7 +553,14 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
         const int64_t cost = 2500 + work + store;
         if (cost < best) { best = cost; P.nt = nt; use_pairs = true; }
     }
-    if (!use_pairs) {
+    int64_t few = -1;
+    if (M <= kFewMaxM) {
+        const int64_t sm = ((N + 15) / 16 + sms - 1) / sms * 16 * K / 45, all = N * K / 5000;
+        few = 2200 + (sm > all ? sm : all);
+    }
+    if (few >= 0 && few <= best) {
+        e = launch_few(q, ldw, xq, ldxq, P, sms, s);
+    } else if (!use_pairs) {
         P.tmem_cols = P.nt < 32 ? 32 : P.nt;
         const int64_t tiles_m = (M + P.nt - 1) / P.nt;
         const int stage_bytes = kSplitBlocks * (kBM + P.nt) * kBK;

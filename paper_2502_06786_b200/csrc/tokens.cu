@@ -127,18 +127,16 @@ extern "C" int matq_quantize_tokens(const void* X, int64_t M, int64_t K, int64_t
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(X);
     cudaError_t e;
-    // Few tokens: 256 threads, to spread a row's loads.  Many: 128, so that an SM holds more rows between their two barriers.
+    // Many tokens: 128 threads (256 for long rows), so that an SM holds more rows between their two barriers (4096 x 14336: 36 us, with 1024 threads 52).  Few: as many
+    // threads as hold a row in two loads each (600 x 9216 as many 6.1 us, 5 x 10608 as few 2.5 instead of 4.1).
 #define MATQ_ROWS(V, THREADS) launch_overlapped(quantize_tokens_kernel<V, THREADS>, dim3((unsigned)M), dim3(THREADS), 0, st, x, K, ldx, xq, ldq, scale, rowsum, dev_status)
-    if (M >= 4 * sm_count() && K <= 8192) {
-        if (K <= 1024) e = MATQ_ROWS(1, 128);
-        else if (K <= 2048) e = MATQ_ROWS(2, 128);
-        else if (K <= 4096) e = MATQ_ROWS(4, 128);
-        else e = MATQ_ROWS(8, 128);
-    } else if (K <= 2048) e = MATQ_ROWS(1, 256);
-    else if (K <= 4096) e = MATQ_ROWS(2, 256);
-    else if (K <= 8192) e = MATQ_ROWS(4, 256);
-    else if (K <= 16384) e = MATQ_ROWS(8, 256);
-    else e = MATQ_ROWS(0, 256);
+    const bool many = M >= 4 * sm_count();
+    if (K <= 1024) e = MATQ_ROWS(1, 128);
+    else if (K <= 2048) e = many ? MATQ_ROWS(2, 128) : MATQ_ROWS(1, 256);
+    else if (K <= 4096) e = many ? MATQ_ROWS(4, 128) : MATQ_ROWS(2, 256);
+    else if (K <= 8192) e = many ? MATQ_ROWS(8, 128) : MATQ_ROWS(2, 512);
+    else if (K <= 16384) e = many ? MATQ_ROWS(8, 256) : MATQ_ROWS(2, 1024);
+    else e = MATQ_ROWS(0, 512);
 #undef MATQ_ROWS
     if (e != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
     return launch_status();

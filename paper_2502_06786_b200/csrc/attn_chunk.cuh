@@ -54,6 +54,17 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* d) {
                  ::"r"(d[0]), "r"(d[1]), "r"(d[2]), "r"(d[3]), "r"(d[4]), "r"(d[5]), "r"(d[6]), "r"(d[7]),
                    "r"(d[8]), "r"(d[9]), "r"(d[10]), "r"(d[11]), "r"(d[12]), "r"(d[13]), "r"(d[14]), "r"(d[15]), "r"(addr) : "memory");
 }
+// 32 bytes, a whole sector: in one store where the address allows it (a thread's row lies apart from its neighbours', so that smaller stores cost a
+// transaction each all the same)
+__device__ __forceinline__ void store32(void* p, const uint32_t* v, bool wide) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+}
 // D = fp32, A = B = bf16, 128 rows
 __device__ __forceinline__ constexpr uint32_t idesc_bf16(int n, bool b_mn_major) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
@@ -137,6 +148,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const uint32_t dst = tc::smem_u32(v ? ring_v : ring_k) + (uint32_t)(x >> 6) * (kStageKeys * 128) + (uint32_t)run * rows_box * 128;
             const uint32_t full = tc::smem_u32(v ? s_vfull : s_kfull), empty = tc::smem_u32(v ? s_vempty : s_kempty);
             const auto row_of = [&](int i) { return cache_row(P, b, h, (int64_t)k_lo + (int64_t)i * kStageKeys + run * rows_box, rows_box, first, kv_len); };
+            int next_row = n_it > 0 ? row_of(0) : 0;                    // a stage's pages are looked up while the one before waits, the first while the queries are fetched
             bool ok = true;
             if (n_it > 0 && !v) {
                 if (round > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_out), (uint32_t)(round - 1) & 1u, P.wait_cycles));
@@ -149,7 +161,6 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                                             (int)(q0 + t0 + t * tok_tile), tc::smem_u32(&s_q));
                 }
             }
-            int next_row = n_it > 0 ? row_of(0) : 0;                    // a stage's pages are looked up while the one before waits
             int s = kSub * it % stages;
             uint32_t phase = (uint32_t)(kSub * it / stages) & 1u;
             for (int i = 0; i < kSub * n_it && ok; ++i) {
@@ -413,21 +424,27 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         const uint32_t vb = tc::smem_u32(ring_v) + (uint32_t)((kSub * gi + key / kStageKeys) % C::kStagesV) * C::kKvBytes + (key % kStageKeys) * 128;
                         bool bad = false;
                         if (!all) {
-                            for (int ch = tid / kKeys; ch < D / 8; ch += kShare) {
-                                const uint32_t at = vb + (uint32_t)(ch >> 3) * (kStageKeys * 128) + (((ch & 7) ^ (key & 7)) << 4);
-                                if (unseen) {
-                                    asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at), "r"(0) : "memory");
-                                } else {
-                                    uint32_t w[4];
-                                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
-                                    bool here = false;
+                            constexpr int kAtOnce = D / 8 / kShare < 8 ? D / 8 / kShare : 8;       // pieces of 16 bytes requested together
+                            const auto at = [&](int ch) { return vb + (uint32_t)(ch >> 3) * (kStageKeys * 128) + (((ch & 7) ^ (key & 7)) << 4); };
+                            for (int ch0 = tid / kKeys; ch0 < D / 8; ch0 += kAtOnce * kShare) {
+                                uint32_t w[kAtOnce][4];
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        if (nonfinite_bf16(w[e])) { here = true; w[e] &= 0xffff0000u; }
-                                        if (nonfinite_bf16(w[e] >> 16)) { here = true; w[e] &= 0x0000ffffu; }
+                                for (int x = 0; x < kAtOnce; ++x) {
+                                    if (unseen) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at(ch0 + x * kShare)), "r"(0) : "memory");
+                                    else asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[x][0]), "=r"(w[x][1]), "=r"(w[x][2]), "=r"(w[x][3]) : "r"(at(ch0 + x * kShare)) : "memory");
+                                }
+                                if (unseen) continue;
+#pragma unroll
+                                for (int x = 0; x < kAtOnce; ++x) {
+                                    uint32_t hit = 0;
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) hit |= __vcmpeq2(w[x][e] & 0x7f807f80u, 0x7f807f80u);
+                                    if (hit) {
+#pragma unroll
+                                        for (int e = 0; e < 4; ++e) w[x][e] &= ~__vcmpeq2(w[x][e] & 0x7f807f80u, 0x7f807f80u);
+                                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at(ch0 + x * kShare)), "r"(w[x][0]), "r"(w[x][1]), "r"(w[x][2]), "r"(w[x][3]) : "memory");
+                                        bad = true;
                                     }
-                                    if (here) asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-                                    bad |= here;
                                 }
                             }
                         }
@@ -485,19 +502,17 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     }
                     if (!live) continue;
                     if (P.splits > 1) {
-                        uint4* dst = reinterpret_cast<uint4*>(P.part_o + ((int64_t)part * (P.T * P.q_heads) + row) * D + c);
+                        float* dst = P.part_o + ((int64_t)part * (P.T * P.q_heads) + row) * D + c;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) dst[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        for (int e = 0; e < 4; ++e) store32(dst + 8 * e, o + 8 * e, true);
                     } else {
-                        uint4* dst = reinterpret_cast<uint4*>(P.out + (q0 + tok) * P.ldo + (int64_t)(h * P.group + r % P.group) * D + c);
+                        __nv_bfloat16* dst = P.out + (q0 + tok) * P.ldo + (int64_t)(h * P.group + r % P.group) * D + c;
+                        const bool wide = (reinterpret_cast<uintptr_t>(dst) & 31u) == 0;
+                        uint32_t w[16];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int x = 0; x < 4; ++x)
-                                w[x] = any ? pack_bf16(__uint_as_float(o[8 * e + 2 * x]) * inv, __uint_as_float(o[8 * e + 2 * x + 1]) * inv) : 0u;
-                            dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
-                        }
+                        for (int x = 0; x < 16; ++x) w[x] = any ? pack_bf16(__uint_as_float(o[2 * x]) * inv, __uint_as_float(o[2 * x + 1]) * inv) : 0u;
+                        store32(dst, w, wide);
+                        store32(dst + 16, w + 8, wide);
                     }
                 }
             }

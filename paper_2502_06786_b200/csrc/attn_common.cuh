@@ -130,7 +130,7 @@ constexpr int kMaxSplits = 256, kJoinThreads = 256;
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const Params P) {
     __shared__ float s_w[kMaxSplits], s_red[2][8];
-    __shared__ float s_o[8][D];
+    __shared__ __align__(16) float s_o[8][D];
     after_previous_kernel();
     let_next_kernel_start();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;

@@ -3,10 +3,10 @@
 // A query tile is 128 accumulator rows: floor(128 / group) tokens times the heads of one key head's group, so that a key is read once for the
 // whole group.  A CTA takes kTiles such tiles and walks the keys that they see, kKeys at a time:
 //   warps 8, 9         producers: queries once and keys; values; a ring each (one box per page and 64 columns, 128-byte swizzle);
-//   warps 10, 11       one thread each issues S = Q K^T and O += P V (tcgen05.mma, accumulators and P in tensor memory): with two tiles each
-//                      takes one of them, with one tile one takes the scores and the other the products.  A wait on a barrier costs an issuing thread
-//                      250 cycles even when it has been arrived on, about four products; with two threads the tensor cores have the other's meanwhile
-//                      (8192 tokens over 8192, 32/8 heads of 128: one thread 1.62 ms).
+//   warps 10, 11       one thread each issues S = Q K^T and O += P V (tcgen05.mma, accumulators and P in tensor memory): one takes the scores
+//                      and the other the products, so that a wait of the one, 250 cycles even on a barrier that has been arrived on, leaves the tensor
+//                      cores the other's work.  With two tiles the first warp issues all of it: a tile's next scores have to follow the product that
+//                      reads P in the same place, and the other tile's work fills the waits (a warp per tile was slower).
 //   warps 0 .. 7       softmax, one thread per row (two, with half of the keys each, when there is one tile): S from tensor memory, exponentials,
 //                      P back over S as bf16.
 // P takes the place of S: the product with V that reads it is issued before the scores that overwrite it.  The row maximum is a reference only (see kFar).

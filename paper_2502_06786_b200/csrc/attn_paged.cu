@@ -5,10 +5,13 @@
 namespace matq {
 namespace attn {
 
+constexpr int64_t kMaxKeys = (1ll << 31) - 1;                           // lengths are 32-bit numbers
+
 struct Plan {
     int kind;                    // 1, 2: attn_chunk with so many query tiles of 128 rows per CTA; 8, 16: attn_decode with so many rows
     int keys, stage_keys;        // keys of a step (the parts of the key range are multiples of it) and of a ring stage
-    int64_t tiles_per_seq, splits, split_keys, cost;
+    int64_t tiles_per_seq, splits, split_keys;
+    double cost;
 };
 
 // Kernel and split of one kind from sizes that the host knows, and what they cost (ns).
@@ -23,26 +26,26 @@ inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64
     p.tiles_per_seq = decode ? (rows + kind - 1) / kind : (max_q + tok - 1) / tok;
     if (p.tiles_per_seq < 1) p.tiles_per_seq = 1;
     int64_t range = max_kv;                                             // keys that a tile can see
-    if (window > 0 && window + tok + 16 < range) range = window + tok + 16;
+    if (window > 0 && window < range && window + tok + 16 < range) range = window + tok + 16;
     range = (range + keys - 1) / keys + 1;                              // steps; one more when the window starts inside one
     // Parts of the key range: the number whose rounds over the SMs cost least.  Measured, ns: a step of the 128-row kernels; a stage of the few-row kernels
     // takes its bytes' time at 45 GB/s per SM or at the share of HBM that the CTAs at work leave each other, but 250 while the ring is filled for the first time;
     // about 2 us until the first step and after the last (6 for the 128-row kernels); 3 us for the join, and its bytes.  Sequences of a batch differ: without a
     // window their lengths are taken to average 0.6 of the longest.  More CTAs at work than SMs end half a part after the even share, on average.
-    const int64_t ctas = p.tiles_per_seq * batch * kv_heads, row_bytes = ctas * (decode ? kind : 128 * kind) * D * 8;
+    const double ctas = (double)p.tiles_per_seq * batch * kv_heads, row_bytes = ctas * (decode ? kind : 128 * kind) * D * 8;
     const int64_t bytes = (int64_t)keys * D * 4, ring = decode ? 192 * 1024 / bytes : 0;
     int64_t splits = 1;
     p.cost = -1;
     const double mean = batch > 1 ? (window > 0 && window < max_kv ? 0.9 : 0.6) : 1.0;
     for (int64_t n = 1; n <= kMaxSplits && n <= range; ++n) {
-        const double busy = (double)ctas * (n * mean > 1.0 ? n * mean : 1.0), at_work = busy < sms ? busy : sms;      // CTAs with keys
+        const double busy = ctas * (n * mean > 1.0 ? n * mean : 1.0), at_work = busy < sms ? busy : sms;      // CTAs with keys
         const double share = bytes * at_work / 6300.0, first = share > 250 ? share : 250, later = share > bytes / 45.0 ? share : bytes / 45.0;
         const int64_t steps = (range + n - 1) / n;                      // of the longest part
         const double step_ns = kind == 2 ? 1900 : D == 256 ? 2300 : 1400;
         const double part = decode ? (steps < ring ? steps : ring) * first + (steps > ring ? steps - ring : 0) * later + 2000 : steps * step_ns + 6000;
         const double all = part * busy / sms * (n * mean > 1.0 ? 1.0 : mean);        // the even share (unsplit: of parts of mean length)
         const double cost = (busy <= sms ? part : all + part / 2) + (n > 1 ? 3000 + row_bytes * n / 5000.0 : 0);
-        if (p.cost < 0 || cost < p.cost) { p.cost = (int64_t)cost; splits = n; }
+        if (p.cost < 0 || cost < p.cost) { p.cost = cost; splits = n; }
         if (ctas * n >= 6 * sms) break;
     }
     const int64_t per = (range + splits - 1) / splits;
@@ -53,7 +56,9 @@ inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64
 
 // Up to 16 rows per sequence and key head: the few-row kernel (16 sequences of 4 drafted tokens, 32/8 heads, windows of 4096 keys, D = 64, 128, 256: 34, 46, 82
 // us; the 128-row kernel 48, 51, 87).  More: one or two query tiles per CTA, whichever costs less.
-inline Plan plan(int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
+inline Plan plan(int64_t T, int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
+    if (max_q > T) max_q = T;
+    if (max_kv > kMaxKeys) max_kv = kMaxKeys;
     const int64_t rows = max_q * group;
     if (rows <= 16) return plan_kind(rows <= 8 ? 8 : 16, batch, kv_heads, group, D, max_q, max_kv, window, sms);
     const Plan one = plan_kind(1, batch, kv_heads, group, D, max_q, max_kv, window, sms);
@@ -136,7 +141,7 @@ extern "C" size_t matq_attn_paged_workspace_bytes(int64_t T, int batch, int q_he
                                                   int64_t max_q, int64_t max_kv, int64_t window) {
     using namespace matq::attn;
     if (T <= 0 || batch <= 0 || q_heads <= 0 || kv_heads <= 0 || q_heads % kv_heads != 0 || q_heads / kv_heads > 64 || head_dim <= 0 || max_q < 0 || max_kv < 0) return 0;
-    const Plan p = plan(batch, kv_heads, q_heads / kv_heads, head_dim, max_q, max_kv, window, matq::sm_count());
+    const Plan p = plan(T, batch, kv_heads, q_heads / kv_heads, head_dim, max_q, max_kv, window, matq::sm_count());
     return part_bytes(T, q_heads, head_dim, p.splits);
 }
 
@@ -152,13 +157,16 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     if (D != 64 && D != 128 && D != 256) return MATQ_ERR_UNSUPPORTED;
     if (ps != 16 && ps != 32 && ps != 64 && ps != 128 && ps != 256) return MATQ_ERR_UNSUPPORTED;
     if (q_heads % cache->kv_heads != 0 || q_heads / cache->kv_heads > 64) return MATQ_ERR_UNSUPPORTED;
-    const int64_t w = (int64_t)q_heads * D, rows = cache->n_pages * cache->kv_heads * ps;
-    if (ldq < w || ldq % 8 != 0 || ldo < w || ldo % 8 != 0 || T >= (1ll << 31) || cache->n_pages >= (1ll << 31) || rows >= (1ll << 31)) return MATQ_ERR_SHAPE;
+    const int64_t w = (int64_t)q_heads * D;
+    if (ldq < w || ldq % 8 != 0 || ldo < w || ldo % 8 != 0 || T >= (1ll << 31) || cache->n_pages > kMaxKeys / ((int64_t)cache->kv_heads * ps)) return MATQ_ERR_SHAPE;
+    const int64_t rows = cache->n_pages * cache->kv_heads * ps;
     if (T == 0 || cache->batch == 0) return MATQ_OK;
     if (!q || !out || !cache->k || !cache->v || !cache->page_table || !cache->cu_q || !cache->kv_len || cache->n_pages == 0) return MATQ_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out) || !aligned16(cache->k) || !aligned16(cache->v) || !aligned16(workspace)) return MATQ_ERR_ALIGNMENT;
     const int group = q_heads / cache->kv_heads;
-    const Plan p = plan(cache->batch, cache->kv_heads, group, D, max_q, max_kv, window, sm_count());
+    const Plan p = plan(T, cache->batch, cache->kv_heads, group, D, max_q, max_kv, window, sm_count());
+    const double ctas = (double)p.splits * cache->kv_heads * cache->batch * p.tiles_per_seq;
+    if (ctas >= 2147483648.0 || (p.splits > 1 && T * q_heads >= (1ll << 31))) return MATQ_ERR_SHAPE;
     if (part_bytes(T, q_heads, D, p.splits) > workspace_bytes || (p.splits > 1 && !workspace)) return MATQ_ERR_WORKSPACE;
 
     Params P;
@@ -174,13 +182,12 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     P.dev_status = dev_status;
     P.hold = tc::test_stall() ? 1 : 0;
     P.wait_cycles = P.hold ? tc::kStallWaitCycles : tc::kWaitCycles;
-    const int64_t grid = p.splits * cache->kv_heads * cache->batch * p.tiles_per_seq;
-    if (grid >= (1ll << 31) || (p.splits > 1 && T * q_heads >= (1ll << 31))) return MATQ_ERR_SHAPE;
+    const unsigned grid = (unsigned)ctas;
     CUtensorMap tq, tk, tv;
     const int box = ps < p.stage_keys ? ps : p.stage_keys;
     if (!cache_map(&tk, cache->k, rows, D, box) || !cache_map(&tv, cache->v, rows, D, box) || !query_map(&tq, q, T, q_heads, D, ldq, group)) return MATQ_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (D == 64) return launch<64>(tq, tk, tv, P, p.kind, (unsigned)grid, s);
-    if (D == 128) return launch<128>(tq, tk, tv, P, p.kind, (unsigned)grid, s);
-    return launch<256>(tq, tk, tv, P, p.kind, (unsigned)grid, s);
+    if (D == 64) return launch<64>(tq, tk, tv, P, p.kind, grid, s);
+    if (D == 128) return launch<128>(tq, tk, tv, P, p.kind, grid, s);
+    return launch<256>(tq, tk, tv, P, p.kind, grid, s);
 }

@@ -22,6 +22,7 @@ const at::Tensor& tensor(PyObject* o, at::ScalarType type, const char* name) {
     if (!THPVariable_Check(o)) fail(PyExc_TypeError, name, "expected a CUDA tensor");
     const at::Tensor& t = THPVariable_Unpack(o);
     if (!t.is_cuda() || t.scalar_type() != type) fail(PyExc_TypeError, name, (std::string("expected a CUDA tensor of dtype ") + c10::toString(type)).c_str());
+    if (t.get_device() != c10::cuda::current_device()) fail(PyExc_ValueError, name, "on another device than the current one, whose stream the call would use");
     return t;
 }
 template <typename T>
@@ -39,7 +40,7 @@ Matrix mat(PyObject* o, at::ScalarType type, const char* name) {
     if (t.dim() != 2) fail(PyExc_ValueError, name, "expected 2 dimensions");
     const int64_t r = t.size(0), c = t.size(1);
     if (t.stride(1) != 1 && c > 1) fail(PyExc_ValueError, name, "unit stride along its second dimension required");
-    return {t.data_ptr(), r, c, r > 1 ? t.stride(0) : std::max(c, t.stride(0))};      // a single row may report any stride
+    return {t.data_ptr(), r, c, r > 1 ? t.stride(0) : c};               // a single row may report any stride
 }
 struct Heads {
     void* p;
@@ -50,7 +51,7 @@ Heads heads(PyObject* o, const char* name, int64_t D) {
     if (t.dim() != 3) fail(PyExc_ValueError, name, "expected 3 dimensions");
     const int64_t T = t.size(0), H = t.size(1);
     if (t.size(2) != D || (t.stride(2) != 1 && D > 1) || (t.stride(1) != D && H > 1)) fail(PyExc_ValueError, name, "bf16 [T, heads, head_dim] with a token's heads adjacent required");
-    return {t.data_ptr(), T, H, T > 1 ? t.stride(0) : std::max(H * D, t.stride(0))};
+    return {t.data_ptr(), T, H, T > 1 ? t.stride(0) : H * D};
 }
 int32_t* status_word(PyObject* o) {
     if (o == Py_None) return nullptr;
@@ -62,6 +63,11 @@ int64_t integer(PyObject* o, const char* name) {
     const long long v = PyLong_AsLongLong(o);
     if (v == -1 && PyErr_Occurred()) { PyErr_Clear(); fail(PyExc_TypeError, name, "an integer is required"); }
     return v;
+}
+int small_integer(PyObject* o, const char* name) {
+    const int64_t v = integer(o, name);
+    if (v < 0 || v > INT32_MAX) fail(PyExc_ValueError, name, "out of range");
+    return (int)v;
 }
 double number(PyObject* o, const char* name) {
     const double v = PyFloat_AsDouble(o);
@@ -130,9 +136,9 @@ PyObject* gemm_a8(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Matrix y = mat(a[6], bf16 ? at::kBFloat16 : at::kFloat, "y");
         if (y.rows != x.rows || y.cols != w.rows) fail(PyExc_ValueError, "y", "[M, N] required");
         return matq_gemm_a8(static_cast<const int8_t*>(x.p), x.rows, x.cols, x.ld, vec<float>(a[1], at::kFloat, "scale", x.rows),
-                            vec<int32_t>(a[2], at::kInt, "rowsum", x.rows), static_cast<const uint8_t*>(w.p), w.rows, w.ld, (int)integer(a[9], "c"),
+                            vec<int32_t>(a[2], at::kInt, "rowsum", x.rows), static_cast<const uint8_t*>(w.p), w.rows, w.ld, small_integer(a[9], "c"),
                             vec<float>(a[4], at::kFloat, "alpha", w.rows), vec<float>(a[5], at::kFloat, "zero", w.rows),
-                            bf16 ? MATQ_OUT_BF16 : MATQ_OUT_F32, y.p, y.ld, (unsigned)integer(a[7], "flags"), status_word(a[8]), stream());
+                            bf16 ? MATQ_OUT_BF16 : MATQ_OUT_F32, y.p, y.ld, (unsigned)small_integer(a[7], "flags"), status_word(a[8]), stream());
     });
 }
 

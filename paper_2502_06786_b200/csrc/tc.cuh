@@ -48,7 +48,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(tm), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) { asm volatile("prefetch.tensormap [%0];" ::"l"(tm) : "memory"); }
 
 // Shared-memory operand descriptor of a tile with 128-byte swizzle: rows of 128 bytes, atoms of 8 rows 1024 bytes apart (K-major operands;
 // for an MN-major operand `lead` is the distance of neighbouring 128-byte columns of atoms).

@@ -88,6 +88,22 @@ def test_attn_paged_workspace():
     assert f(8192, 1, 32, 8, 128, 8192, 16384) == 0            # nor a chunk that fills the GPU by itself
 
 
+def test_attn_paged_sizes_past_every_range():
+    """Products of sizes that pass 32 and 64 bits are refused before anything is launched; hints of any size choose some plan."""
+    def call(T=5, qh=4, ldq=256, window=0, max_q=5, max_kv=100, ws_bytes=0, **kw):
+        c = _cache(**kw)
+        return lib.matq_attn_paged(C.byref(c), T, P, qh, ldq, 0.1, 0.0, window, max_q, max_kv, P, ldq, NULL, ws_bytes, NULL, NULL)
+    big = (1 << 31) - 1
+    assert call(kv_heads=1 << 30, qh=1 << 30, ldq=1 << 36, page_size=256, n_pages=1 << 30) == mq.ERR_SHAPE       # pages * heads * slots = 2^68
+    assert call(kv_heads=1 << 22, qh=1 << 22, ldq=1 << 28, n_pages=32, batch=big, T=big) == mq.ERR_SHAPE         # a grid of 2^53
+    assert call(batch=1, table_width=1, max_q=(1 << 63) - 1, max_kv=(1 << 63) - 1, window=(1 << 63) - 1) == mq.ERR_WORKSPACE      # a long range is split
+    f = mq.attn_paged_workspace_bytes
+    huge = (1 << 63) - 1
+    assert f(4, 1, 8, 2, 128, huge, 32768) == f(4, 1, 8, 2, 128, 4, 32768) > 0
+    assert f(4, 1, 8, 2, 128, 4, huge) == f(4, 1, 8, 2, 128, 4, big) > 0
+    assert f(4, 1, 8, 2, 128, 4, 32768, huge) == f(4, 1, 8, 2, 128, 4, 32768)
+
+
 def test_binding_refuses_host_tensors_and_wrong_types():
     x = torch.zeros(4, 64, dtype=torch.bfloat16)
     with pytest.raises(TypeError):

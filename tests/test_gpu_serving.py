@@ -275,6 +275,20 @@ def test_attn_paged_hints_change_no_result(hints):
     _check(*_attend([40, 1, 9], [300, 700, 9], 8, 2, 128, 16, seed=5, hints=hints))
 
 
+@pytest.mark.parametrize("hints", [(1 << 62, 1 << 62), (1, (1 << 63) - 1)])
+@pytest.mark.parametrize("window", [(1 << 63) - 1, 1 << 31])
+def test_attn_paged_hints_and_windows_of_any_size(hints, window):
+    _check(*_attend([40, 1, 9], [300, 700, 9], 8, 2, 128, 16, seed=9, hints=hints, window=window))
+    _check(*_attend([1, 2], [300, 31], 8, 2, 64, 16, seed=10, hints=hints, window=window))
+
+
+def test_serving_views_of_one_row_may_have_any_stride():
+    x = torch.randn(3, 67, device="cuda", dtype=torch.float32).to(torch.bfloat16)[:1, :64]
+    xq, scale, rowsum = mq.quantize_tokens(x)
+    wq, ws, wr = mq.quantize_tokens(x.contiguous())
+    assert torch.equal(xq, wq) and torch.equal(scale, ws) and torch.equal(rowsum, wr)
+
+
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_attn_paged_long_cache_is_split(D):
     _check(*_attend([1, 2], [6001, 3000], 8, 4, D, 16, seed=6))

@@ -1,6 +1,6 @@
 """Small, self-contained invocations of each kernel for profilers (ncu wants short runs with few launches).
 
-    python -m paper_2502_06786_b200.profile_cases quantize|slice4|slice2ep|gemv4|gemv2|gemv2b8|gemv4t|gemv2t|stream8|stream4|stream2|group4|group2|batch4|batch8|gemm
+    python -m paper_2502_06786_b200.profile_cases quantize|slice4|slice2ep|gemv4|gemv2|gemv2b8|gemv4t|gemv2t|stream8|stream4|stream2|group4|group2|batch4|batch8|gemm|linear|attend
 
 (gemv4 / gemv2: the library's own choice at B = 1, the integer tensor kernel; a trailing t: the bf16 tensor kernel.)
 
@@ -91,6 +91,32 @@ def main(which: str) -> None:
         ws = torch.empty(mq.gemm_multi_workspace_bytes(mq.SRC_CODES8, M2, N2, K2, 3), dtype=torch.uint8, device="cuda")
         for _ in range(3):
             mq.gemm_multi(mq.SRC_CODES8, q, K2, X, alpha=a, zero=a, Ys=Ys, workspace=ws)
+    elif which == "linear":
+        # the linear layer on the codes themselves: one token, 64 and 1024 tokens (few-token, split and pair kernel)
+        N2, K2 = 14336, 4096
+        qs = [torch.randint(0, 256, (N2, K2), dtype=torch.uint8, device="cuda") for _ in range(4)]
+        a = torch.full((N2,), 1e-3, device="cuda")
+        z = torch.full((N2,), 128.0, device="cuda")
+        for M in (1, 64, 1024):
+            X = torch.randn(M, K2, device="cuda").to(torch.bfloat16)
+            Y = torch.empty(M, N2, dtype=torch.bfloat16, device="cuda")
+            for q in qs:
+                mq.gemm_a8(*mq.quantize_tokens(X), q, a, z, y=Y)
+    elif which == "attend":
+        # append and attention over a paged cache: one token over 32768 keys of 8 heads of 128, 500 over 6500 of 8 heads of 256, 2048 over 4096 of 8 heads of 128
+        for new, keys, D, Hq, Hkv in ((1, 32768, 128, 32, 8), (500, 6500, 256, 16, 8), (2048, 4096, 128, 32, 8)):
+            pages = 3 * (keys + 63) // 64
+            kc = torch.randn(pages, Hkv, 64, D, device="cuda").to(torch.bfloat16)
+            vc = torch.randn_like(kc)
+            table = torch.randperm(pages, device="cuda").to(torch.int32)[: (keys + 63) // 64].unsqueeze(0)
+            cu = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+            lens = torch.tensor([keys], dtype=torch.int32, device="cuda")
+            q = torch.randn(new, Hq, D, device="cuda").to(torch.bfloat16)
+            k, v = (torch.randn(new, Hkv, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+            ang = torch.rand(keys, D, device="cuda")
+            for _ in range(3):
+                mq.kv_append(kc, vc, table, cu, lens, k, v, cos_sin=ang, q=q, q_out=q)
+                mq.attn_paged(q, kc, vc, table, cu, lens, new, keys)
     else:
         raise SystemExit(__doc__)
     torch.cuda.synchronize()

@@ -153,6 +153,8 @@ inline cudaError_t launch_few(const uint8_t* q, int64_t ldw, const int8_t* xq, i
 // A CTA sums 128 channels x nt tokens over a part of K in tensor memory; the CTAs of a cluster hold the same tile for different parts, put their sums into
 // shared memory and finish every splits-th token each, reading the others' sums from there.  Tiles of up to 64 tokens leave room for two CTAs per SM.
 // Eight warps store, as in the pair kernel (with four, one token tile of 128 took 6 us to store).
+// From HBM, with MATQ_GEMV_PDL and without: 64 x 14336 x 4096 11.9 and 13.2 us (4.9 and 4.4 TB/s of codes), 37 x 2304 x 9216 8.8 and 9.5 us, of which the copies
+// take 3.3; the rest is the start of a launch, the join and the stores.
 constexpr int kSplitWarps = 8, kSplitThreads = 32 * (2 + kSplitWarps);
 // A stage is 256 bytes of K here too (with 128, 600 tokens through 2304 x 9216 took 23 us instead of 19, 17 through 10587 x 11072 24 instead of 23).
 constexpr int kMaxStages = 8, kMaxSplitsK = 8, kSplitBlocks = 2;
@@ -338,6 +340,7 @@ gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
 // warp's stores run along a token's outputs.
 // A stage is 256 bytes of K, two blocks of 128: waiting for a stage, issuing and committing cost the issuing thread about 500 cycles whatever the
 // stage holds, and the products of one block take no more than that (4096 x 14336 x 4096: 770 cycles a block with one block per stage).
+// 4096 x 14336 x 4096: 164 us = 2.93 POP/s (about 190 us in a long run, at the power cap).  What bounds it is the tensor pipe.
 constexpr int kPairWarps = 8, kPairThreads = 32 * (2 + kPairWarps), kPairStages = 3, kPairBlocks = 2;
 constexpr int kPairBlockBytes = 2 * kBM * kBK;       // 128 channels and up to 128 tokens
 constexpr int kPairStageBytes = kPairBlocks * kPairBlockBytes;

@@ -4,6 +4,7 @@
 // -> length -> page and angles -> store) for a decode step.  A CTA takes one token; a thread keeps its place within the heads and walks over
 // queries, keys and values, so that its angles stay in registers.  A place is two pieces of eight elements: with halves as pairs a piece of the first
 // half and its partners, otherwise neighbours.  The data of its first heads are requested before the position is known.
+// Three prompts of 1500 to 4000 tokens, 16/8 heads of 256: 60 us = 5.3 TB/s, half of it writes.  64 single tokens, 32/8 heads of 128: 3.2 us.
 #include "common.cuh"
 
 namespace matq {

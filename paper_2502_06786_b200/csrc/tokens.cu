@@ -3,7 +3,7 @@
 //
 // One CTA per token; up to K = 16384 the row stays in registers between the two passes (one 16-byte load per thread and 2048
 // elements), longer rows are read a second time, from the L2.  Two bytes in and one out per element: HBM-bound for many tokens,
-// a launch and two trips to memory for few.
+// a launch and two trips to memory for few.  4096 x 14336: 36 us = 4.9 TB/s; one token of 2304: 1.9 us.
 #include "common.cuh"
 
 namespace matq {

@@ -11,12 +11,13 @@
 //                      P back over S as bf16.
 // P takes the place of S: the product with V that reads it is issued before the scores that overwrite it.  The row maximum is a reference only (see kFar).
 // D <= 128: two tiles, whose softmax and tensor work alternate.  One tile (D = 256, or few rows): two S buffers, so that the scores of the next
-// keys are computed while the present ones are exponentiated.  A step is 128 keys; at D = 256 they come in two ring stages of 64 (with steps of 64 the
+// keys are computed while the present ones are exponentiated.  A step is 128 keys, also at D = 256 (with steps of 64 the
 // softmax's fixed part, about 1300 cycles of latencies, came twice as often: 500 tokens over 6011 at 16/8 x 256 heads 70 us in the kernel).
 //
 // Bound: 8192 tokens over 16384 keys, 32/8 heads of 128: 1.43 ms = 1150 TFLOP/s (1.65 ms in a long run, at the power cap).  A step of two tiles takes about
 // 3500 cycles for 2048 of products: a tile's chain is its softmax pass 1500, the store of P 170, two hand-overs of some 250 and its products 1024, and two
-// tiles cover each other's products but not all of the rest.  500 over 6511 at 16/8 x 256, with the cap: 61 us, 2.3 us a step.
+// tiles cover each other's products but not all of the rest.  500 over 6511 at 16/8 x 256, with the cap: 55 us, 2.4 us a step, of which
+// the copies alone need 1.6 (128 KB at 80 GB/s; every SM reads all keys and values of its tile from the L2), the products 1.05.
 #pragma once
 
 #include <type_traits>
@@ -33,10 +34,13 @@ struct ChunkCfg {
     static constexpr int kTiles = TILES;
     static_assert(TILES == 1 || (TILES == 2 && D <= 128), "two accumulators and their scores must fit 512 columns");
     static constexpr int kKeys = 128;                                   // keys of a step
-    static constexpr int kSub = D == 256 ? 2 : 1, kStageKeys = kKeys / kSub;         // ring stages of a step, and their keys
+    // Ring stages of a step.  Keys come as column panels (all keys of the step, half of the columns), so that a product is 128 keys wide; values as rows, half
+    // of the keys each.  (Keys as rows too, and products 64 wide, read Q from shared memory twice as often: 500 tokens over 6511, 16/8 heads of 256, 61 us
+    // instead of 55.  Stages of a quarter: keys the same, values 64 us, a stage's wait and commit being what they cost.)
+    static constexpr int kSub = D == 256 ? 2 : 1, kStageKeys = kKeys / kSub;         // kStageKeys: of a stage of values
     static constexpr int kPanels = D / 64;
     static constexpr int kQBytes = 128 * D * 2;                         // one query tile
-    static constexpr int kKvBytes = kStageKeys * D * 2;                 // the keys, or the values, of a stage
+    static constexpr int kKvBytes = kKeys * D * 2 / kSub;               // the keys, or the values, of a stage
     static constexpr int kStagesK = D == 64 ? 4 : 3, kStagesV = D == 64 ? 4 : TILES * D == 128 ? 3 : 2;
     static constexpr int kSoft = 256;                                   // softmax threads: one per row of two tiles, two per row of one
     static constexpr int kCols = kKeys * TILES / 2;                     // keys of a step per softmax thread
@@ -147,11 +151,12 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const bool v = warp == kWarpV;
             const CUtensorMap* tm = v ? &tm_v : &tm_k;
             const int stages = v ? C::kStagesV : C::kStagesK;
-            const int rows_box = min(P.page_size, kStageKeys), runs = kStageKeys / rows_box, boxes = runs * C::kPanels;       // powers of two, 32 boxes at most
+            const int keys = v ? kStageKeys : kKeys, panels = v ? C::kPanels : C::kPanels / kSub;
+            const int rows_box = min(P.page_size, keys), runs = keys / rows_box, boxes = runs * panels;       // powers of two, 32 boxes at most
             const int run = lane & (runs - 1), x = (lane / runs) * 64;  // this lane's box of a step
-            const uint32_t dst = tc::smem_u32(v ? ring_v : ring_k) + (uint32_t)(x >> 6) * (kStageKeys * 128) + (uint32_t)run * rows_box * 128;
+            const uint32_t dst = tc::smem_u32(v ? ring_v : ring_k) + (uint32_t)(x >> 6) * (keys * 128) + (uint32_t)run * rows_box * 128;
             const uint32_t full = tc::smem_u32(v ? s_vfull : s_kfull), empty = tc::smem_u32(v ? s_vempty : s_kempty);
-            const auto row_of = [&](int i) { return cache_row(P, b, h, (int64_t)k_lo + (int64_t)i * kStageKeys + run * rows_box, rows_box, first, kv_len); };
+            const auto row_of = [&](int i) { return cache_row(P, b, h, (int64_t)k_lo + (int64_t)i * keys + run * rows_box, rows_box, first, kv_len); };
             int next_row = n_it > 0 ? row_of(0) : 0;                    // a stage's pages are looked up while the one before waits, the first while the queries are fetched
             bool ok = true;
             if (n_it > 0 && !v) {
@@ -165,15 +170,18 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                                             (int)(q0 + t0 + t * tok_tile), tc::smem_u32(&s_q));
                 }
             }
-            int s = kSub * it % stages;
+            int s = kSub * it % stages, row = 0;
             uint32_t phase = (uint32_t)(kSub * it / stages) & 1u;
             for (int i = 0; i < kSub * n_it && ok; ++i) {
-                const int row = next_row;
-                if (i + 1 < kSub * n_it) next_row = row_of(i + 1);
+                const int part_i = v ? 0 : i % kSub, i_row = v ? i : i / kSub;          // keys: the stage's columns; the rows are the step's
+                if (part_i == 0) {
+                    row = next_row;
+                    if (i + (v ? 1 : kSub) < kSub * n_it) next_row = row_of(i_row + 1);
+                }
                 ok = __all_sync(0xffffffffu, tc::mbar_wait(empty + 8 * s, phase ^ 1u, P.wait_cycles)) && !P.hold;
                 if (!ok) break;
                 if (lane == 0) tc::mbar_expect_tx(full + 8 * s, C::kKvBytes);   // the phase cannot end before this arrival, whichever copy comes first
-                if (lane < boxes) tc::tma_load_2d(dst + (uint32_t)s * C::kKvBytes, tm, x, row, full + 8 * s);
+                if (lane < boxes) tc::tma_load_2d(dst + (uint32_t)s * C::kKvBytes, tm, x + part_i * (D / kSub), row, full + 8 * s);
                 ++issued;
                 if (++s == stages) { s = 0; phase ^= 1u; }
             }
@@ -196,13 +204,13 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 uint32_t kp = (uint32_t)(kSub * it / C::kStagesK) & 1u, vp = (uint32_t)(kSub * it / C::kStagesV) & 1u;
                 const auto next_k = [&] { if (++ks == C::kStagesK) { ks = 0; kp ^= 1u; } };
                 const auto next_v = [&] { if (++vs == C::kStagesV) { vs = 0; vp ^= 1u; } };
-                const auto scores = [&](int t, int sub) {               // S_t = Q_t K^T for a stage's keys
-                    const uint64_t qd = q_desc + (uint64_t)(C::kTiles == 2 ? t * (C::kQBytes >> 4) : 0), kd = k_desc + (uint64_t)(ks * (C::kKvBytes >> 4));
-                    const uint32_t d = tmem + t * kKeys + sub * kStageKeys;
+                const auto scores = [&](int t, int sub) {               // S_t += Q_t K^T for a stage's columns
+                    const uint64_t qd = q_desc + (uint64_t)(C::kTiles == 2 ? t * (C::kQBytes >> 4) : 0) + (uint64_t)(sub * (C::kPanels / kSub) * (128 * 128 >> 4));
+                    const uint64_t kd = k_desc + (uint64_t)(ks * (C::kKvBytes >> 4));
 #pragma unroll
-                    for (int x = 0; x < D / 16; ++x)
-                        MATQ_TC_MMA(1, "f16", d, qd + (uint64_t)((x / 4) * (128 * 128 >> 4) + (x & 3) * 2), kd + (uint64_t)((x / 4) * (kStageKeys * 128 >> 4) + (x & 3) * 2),
-                                    idesc_bf16(kStageKeys, false), x > 0 ? 1u : 0u, leader);
+                    for (int x = 0; x < D / kSub / 16; ++x)
+                        MATQ_TC_MMA(1, "f16", tmem + t * kKeys, qd + (uint64_t)((x / 4) * (128 * 128 >> 4) + (x & 3) * 2), kd + (uint64_t)((x / 4) * (kKeys * 128 >> 4) + (x & 3) * 2),
+                                    idesc_bf16(kKeys, false), (sub > 0 || x > 0) ? 1u : 0u, leader);
                     if (sub == kSub - 1) tc::tc_commit(tc::smem_u32(&s_score[t]), leader);
                 };
                 const auto product = [&](int t, int i, int sub) {       // O_t += P_t V for a stage's keys
@@ -415,8 +423,8 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     // see leave the tile, and those rows get them at the end.  Every thread looks at one key, all or half of it.
                     // A slot's use before this one has to be known to be over, or the parity wait could pass a phase early.  With one stage per step that use is
                     // two or more steps back, whose product these scores were issued behind; with two it is the last step's, whose product is waited for.
-                    static_assert(C::kStagesV >= 2 && (kSub == 1 || C::kStagesV == 2), "see above");
-                    if (kSub == 2 && ok && i > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_pv[(gi - 1) & 1]), (uint32_t)((gi - 1) >> 1) & 1u, P.wait_cycles));
+                    static_assert(C::kStagesV >= 2 && (kSub == 1 || C::kStagesV == kSub), "see above");
+                    if (kSub > 1 && ok && i > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_pv[(gi - 1) & 1]), (uint32_t)((gi - 1) >> 1) & 1u, P.wait_cycles));
                     for (int sub = 0; sub < kSub && ok; ++sub) {
                         const int u = kSub * gi + sub;
                         ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_vfull[u % C::kStagesV]), (uint32_t)(u / C::kStagesV) & 1u, P.wait_cycles));

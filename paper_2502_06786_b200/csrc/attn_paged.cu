@@ -9,7 +9,7 @@ constexpr int64_t kMaxKeys = (1ll << 31) - 1;                           // lengt
 
 struct Plan {
     int kind;                    // 1, 2: attn_chunk with so many query tiles of 128 rows per CTA; 8, 16: attn_decode with so many rows
-    int keys, stage_keys;        // keys of a step (the parts of the key range are multiples of it) and of a ring stage
+    int keys, value_keys;        // keys of a step (the parts of the key range are multiples of it) and of a ring stage of values
     int64_t tiles_per_seq, splits, split_keys;
     double cost;
 };
@@ -21,7 +21,7 @@ inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64
     p.kind = kind;
     const bool decode = kind >= 8;
     const int keys = p.keys = decode ? (D == 256 ? 32 : 64) : 128;
-    p.stage_keys = !decode && D == 256 ? 64 : keys;
+    p.value_keys = !decode && D == 256 ? ChunkCfg<256, 1>::kStageKeys : keys;
     const int64_t tok = decode ? 0 : (int64_t)(128 / group) * kind;     // tokens per CTA
     p.tiles_per_seq = decode ? (rows + kind - 1) / kind : (max_q + tok - 1) / tok;
     if (p.tiles_per_seq < 1) p.tiles_per_seq = 1;
@@ -41,7 +41,7 @@ inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64
         const double busy = ctas * (n * mean > 1.0 ? n * mean : 1.0), at_work = busy < sms ? busy : sms;      // CTAs with keys
         const double share = bytes * at_work / 6300.0, first = share > 250 ? share : 250, later = share > bytes / 45.0 ? share : bytes / 45.0;
         const int64_t steps = (range + n - 1) / n;                      // of the longest part
-        const double step_ns = kind == 2 ? 1900 : D == 256 ? 2300 : 1400;
+        const double step_ns = kind == 2 ? 1900 : D == 256 ? 2400 : 1400;
         const double part = decode ? (steps < ring ? steps : ring) * first + (steps > ring ? steps - ring : 0) * later + 2000 : steps * step_ns + 6000;
         const double all = part * busy / sms * (n * mean > 1.0 ? 1.0 : mean);        // the even share (unsplit: of parts of mean length)
         const double cost = (busy <= sms ? part : all + part / 2) + (n > 1 ? 3000 + row_bytes * n / 5000.0 : 0);
@@ -184,8 +184,8 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     P.wait_cycles = P.hold ? tc::kStallWaitCycles : tc::kWaitCycles;
     const unsigned grid = (unsigned)ctas;
     CUtensorMap tq, tk, tv;
-    const int box = ps < p.stage_keys ? ps : p.stage_keys;
-    if (!cache_map(&tk, cache->k, rows, D, box) || !cache_map(&tv, cache->v, rows, D, box) || !query_map(&tq, q, T, q_heads, D, ldq, group)) return MATQ_ERR_CUDA;
+    const int box_k = ps < p.keys ? ps : p.keys, box_v = ps < p.value_keys ? ps : p.value_keys;
+    if (!cache_map(&tk, cache->k, rows, D, box_k) || !cache_map(&tv, cache->v, rows, D, box_v) || !query_map(&tq, q, T, q_heads, D, ldq, group)) return MATQ_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (D == 64) return launch<64>(tq, tk, tv, P, p.kind, grid, s);
     if (D == 128) return launch<128>(tq, tk, tv, P, p.kind, grid, s);

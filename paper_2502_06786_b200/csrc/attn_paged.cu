@@ -29,7 +29,8 @@ inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64
     if (window > 0 && window < range && window + tok + 16 < range) range = window + tok + 16;
     range = (range + keys - 1) / keys + 1;                              // steps; one more when the window starts inside one
     // Parts of the key range: the number whose rounds over the SMs cost least.  Measured, ns: a step of the 128-row kernels; a stage of the few-row kernels
-    // takes its bytes' time at 45 GB/s per SM or at the share of HBM that the CTAs at work leave each other, but 250 while the ring is filled for the first time;
+    // takes its bytes' time at 45 GB/s per SM or at the share of HBM that the CTAs at work leave each other (and with 16 rows no less than 500), but 250 while
+    // the ring is filled for the first time;
     // about 2 us until the first step and after the last (6 for the 128-row kernels); 3 us for the join, and its bytes.  Sequences of a batch differ: without a
     // window their lengths are taken to average 0.6 of the longest.  More CTAs at work than SMs end half a part after the even share, on average.
     const double ctas = (double)p.tiles_per_seq * batch * kv_heads, row_bytes = ctas * (decode ? kind : 128 * kind) * D * 8;
@@ -39,7 +40,8 @@ inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64
     const double mean = batch > 1 ? (window > 0 && window < max_kv ? 0.9 : 0.6) : 1.0;
     for (int64_t n = 1; n <= kMaxSplits && n <= range; ++n) {
         const double busy = ctas * (n * mean > 1.0 ? n * mean : 1.0), at_work = busy < sms ? busy : sms;      // CTAs with keys
-        const double share = bytes * at_work / 6300.0, first = share > 250 ? share : 250, later = share > bytes / 45.0 ? share : bytes / 45.0;
+        const double share = bytes * at_work / 6300.0, first = share > 250 ? share : 250;
+        const double alone = kind == 16 && bytes / 45.0 < 500 ? 500 : bytes / 45.0, later = share > alone ? share : alone;
         const int64_t steps = (range + n - 1) / n;                      // of the longest part
         const double step_ns = kind == 2 ? 1900 : D == 256 ? 2400 : 1400;
         const double part = decode ? (steps < ring ? steps : ring) * first + (steps > ring ? steps - ring : 0) * later + 2000 : steps * step_ns + 6000;
@@ -55,16 +57,25 @@ inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64
 }
 
 // Up to 16 rows per sequence and key head: the few-row kernel (16 sequences of 4 drafted tokens, 32/8 heads, windows of 4096 keys, D = 64, 128, 256: 34, 46, 82
-// us; the 128-row kernel 48, 51, 87).  More: one or two query tiles per CTA, whichever costs less.
+// us; the 128-row kernel 48, 51, 87).  More: one or two query tiles of 128 rows per CTA, or tiles of 16 rows as long as all of them are at work at once,
+// whichever costs less.  Tiles of 16 read the keys more often, but a CTA of theirs starts and ends 3 us sooner (300 tokens over 600, 6 heads of 64 on one key head:
+// 9.0 us, in tiles of 128 rows 13.1; over 2800 20.3 and 22.1; 240 rows over 2560 keys of 4 heads of 128: 18.7 and 15.4).  With D = 256 they do not (32 rows over
+// 600 keys: 13.8 and 13.9 us; 64 rows of 4 sequences 24.3 and 14.7).
 inline Plan plan(int64_t T, int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
     if (max_q > T) max_q = T;
     if (max_kv > kMaxKeys) max_kv = kMaxKeys;
     const int64_t rows = max_q * group;
     if (rows <= 16) return plan_kind(rows <= 8 ? 8 : 16, batch, kv_heads, group, D, max_q, max_kv, window, sms);
     const Plan one = plan_kind(1, batch, kv_heads, group, D, max_q, max_kv, window, sms);
-    if (rows <= 128 || D == 256) return one;
-    const Plan two = plan_kind(2, batch, kv_heads, group, D, max_q, max_kv, window, sms);
-    return one.cost < two.cost ? one : two;
+    if (D == 256) return one;
+    Plan best = one;
+    if (rows > 128) {
+        const Plan two = plan_kind(2, batch, kv_heads, group, D, max_q, max_kv, window, sms);
+        if (two.cost <= best.cost) best = two;
+    }
+    const Plan few = plan_kind(16, batch, kv_heads, group, D, max_q, max_kv, window, sms);
+    if ((double)few.tiles_per_seq * batch * kv_heads <= sms && few.cost < best.cost) best = few;
+    return best;
 }
 
 inline size_t part_bytes(int64_t T, int q_heads, int D, int64_t splits) {

@@ -270,6 +270,40 @@ def test_attn_paged(case, softcap, window):
     _check(*_attend(*CASES[case], seed=100 + case, softcap=softcap, window=window, fill=float("nan")))
 
 
+MANY = [
+    # enough query tiles to fill the GPU: the kernels of 128 rows, one tile per CTA and two
+    ([140] * 20, [140 + 17 * i for i in range(20)], 8, 2, 128, 16), ([140] * 20, [400 - 13 * i for i in range(20)], 8, 2, 64, 64),
+    ([40] * 20 + [3, 0, 1], [40 + 9 * i for i in range(20)] + [3, 0, 200], 8, 2, 64, 32), ([60] * 30, [60 + 5 * i for i in range(30)], 4, 2, 128, 128),
+    ([33] * 30, [33 + 11 * i for i in range(30)], 4, 2, 256, 64),
+]
+
+
+@pytest.mark.parametrize("softcap,window", [(0.0, 0), (50.0, 0), (0.0, 37), (20.0, 130)])
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_attn_paged_many_query_tiles(case, softcap, window):
+    _check(*_attend(*MANY[case], seed=300 + case, softcap=softcap, window=window, fill=float("nan")))
+
+
+@pytest.mark.parametrize("softcap,window", [(0.0, 0), (20.0, 130)])
+@pytest.mark.parametrize("case", [i for i, c in enumerate(CASES) if max(c[0]) * c[2] // c[3] > 16])
+def test_attn_paged_tiles_of_128_rows(case, softcap, window):
+    # the hint of a long range: query tiles of 128 rows, and parts that hold no key
+    _check(*_attend(*CASES[case], seed=400 + case, softcap=softcap, window=window, fill=float("nan"), hints=(max(CASES[case][0]), 1 << 20)))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attn_paged_nonfinite_values_in_tiles_of_128_rows(D):
+    def edit(kc, vc, table, q):
+        vc[table[0, 60 // 16], :, 60 % 16, D // 2] = float("inf")             # keys that rows from 60 - 20 = 40 on see
+        vc[table[0, 90 // 16], 1, 90 % 16, 3] = float("nan")
+    got, want, tol, status = _attend([80], [100], 8, 2, D, 16, seed=410, edit=edit, hints=(80, 1 << 20))
+    assert status == mq.OK
+    bad = ~torch.isfinite(want)
+    assert bool(bad[40:].any()) and not bool(bad[:40].any())
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    assert bool((got[~bad] - want[~bad]).abs().le(tol[~bad]).all())
+
+
 @pytest.mark.parametrize("hints", [(1, 1), (1, 100000), (5000, 1), (64, 64)])
 def test_attn_paged_hints_change_no_result(hints):
     _check(*_attend([40, 1, 9], [300, 700, 9], 8, 2, 128, 16, seed=5, hints=hints))
@@ -394,6 +428,22 @@ def test_serving_test_stall_times_out_and_recovers():
         assert bool(((mq.gemm_a8(*args).double() - want).abs() <= tol).all())
     for D, n in ((64, 1), (128, 1), (256, 2), (128, 100), (256, 100)):
         _check(*_attend([n], [n + 300], 4, 2, D, 16, seed=13))
+
+
+@pytest.mark.parametrize("D,news", [(64, [140] * 20), (128, [140] * 20), (128, [60] * 30), (256, [60] * 20)])
+def test_attn_paged_many_query_tiles_large_scores_errors_and_stall(D, news):
+    lens = [n + 30 + 19 * i for i, n in enumerate(news)]
+    _check(*_attend(news, lens, 8, 2, D, 16, seed=14, scale=1.0, qstd=8.0))
+
+    def no_page(kc, vc, table, q):
+        table[3, 1] = -1
+    assert _attend_status(news, lens, 8, 2, D, 16, no_page)[1] == mq.ERR_PAGE
+    assert mq.serving_test_stall(1) == 0
+    try:
+        assert _attend_status(news, lens, 8, 2, D, 16, None)[1] == mq.ERR_TIMEOUT
+    finally:
+        assert mq.serving_test_stall(0) == 1
+    _check(*_attend(news, lens, 8, 2, D, 16, seed=15))
 
 
 def test_serving_calls_on_another_stream_and_in_a_graph():

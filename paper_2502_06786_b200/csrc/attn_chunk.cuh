@@ -285,6 +285,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const uint32_t o_addr = lane_addr + C::kTmemO + t * D;
             const Score sc(P.scale, P.softcap);
             const float tmul = P.softcap > 0.f ? P.scale / P.softcap : 0.f;        // the tanh's argument per score
+            const float tanh0 = kTanh0 * sc.cap2, tanh1 = kTanh1 * sc.cap2, tanh2 = kTanh2 * sc.cap2, tanh3 = kTanh3 * sc.cap2;       // with the cap
             float m = -INFINITY, l = 0.f;
             bool ok = true;
             int masked_no = 0;
@@ -329,7 +330,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     sum2[0] = sum2[1] = 0;
                     uint32_t sr[2][32];
                     tc::tmem_ld32(s_addr, sr[0]);
-                    const uint64_t neg = pair(-use, -use), mul = pair(CAP ? 1.f : sc.mul, CAP ? 1.f : sc.mul);
+                    const uint64_t neg = pair(-use, -use), mul = pair(sc.mul, sc.mul);
 #pragma unroll
                     for (int c = 0; c < C::kCols; c += 32) {
                         uint32_t* v = sr[(c >> 5) & 1];
@@ -341,17 +342,17 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                             for (int e = 0; e < 32; e += 2) big = max3(big, fabsf(__uint_as_float(v[e])), fabsf(__uint_as_float(v[e + 1])));
                             if (__any_sync(0xffffffffu, !(big * tmul <= kTanhMax))) {       // some score is past the polynomial's range
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(capped(__uint_as_float(v[e]), sc.mul, sc.cap2));
+                                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(capped(__uint_as_float(v[e]), sc.mul, sc.cap2) - use);
                             } else {
-                                const uint64_t tm2 = pair(tmul, tmul), cap = pair(sc.cap2, sc.cap2);
+                                const uint64_t tm2 = pair(tmul, tmul);
 #pragma unroll
                                 for (int e = 0; e < 32; e += 2) {
                                     const uint64_t t2 = mul2(pair(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), tm2), u2 = mul2(t2, t2);
-                                    uint64_t p2 = fma2(u2, pair(kTanh3, kTanh3), pair(kTanh2, kTanh2));
-                                    p2 = fma2(p2, u2, pair(kTanh1, kTanh1));
-                                    p2 = fma2(p2, u2, pair(kTanh0, kTanh0));
+                                    uint64_t p2 = fma2(u2, pair(tanh3, tanh3), pair(tanh2, tanh2));
+                                    p2 = fma2(p2, u2, pair(tanh1, tanh1));
+                                    p2 = fma2(p2, u2, pair(tanh0, tanh0));
                                     float x, y;
-                                    unpair(mul2(mul2(t2, cap), p2), x, y);
+                                    unpair(fma2(t2, p2, neg), x, y);
                                     v[e] = __float_as_uint(x);
                                     v[e + 1] = __float_as_uint(y);
                                 }
@@ -360,7 +361,12 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             float x, y;
-                            unpair(fma2(pair(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), mul, neg), x, y);
+                            if (CAP) {
+                                x = __uint_as_float(v[e]);
+                                y = __uint_as_float(v[e + 1]);
+                            } else {
+                                unpair(fma2(pair(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), mul, neg), x, y);
+                            }
                             if (hide) {
                                 const int j = j0 + col0 + c + e;
                                 if (j > see_hi || j < see_lo) x = -INFINITY;

@@ -16,7 +16,7 @@
 //
 // Bound: 8192 tokens over 16384 keys, 32/8 heads of 128: 1.43 ms = 1150 TFLOP/s (1.65 ms in a long run, at the power cap).  A step of two tiles takes about
 // 3500 cycles for 2048 of products: a tile's chain is its softmax pass 1500, the store of P 170, two hand-overs of some 250 and its products 1024, and two
-// tiles cover each other's products but not all of the rest.  500 over 6511 at 16/8 x 256, with the cap: 55 us, 2.4 us a step, of which
+// tiles cover each other's products but not all of the rest.  500 over 6511 at 16/8 x 256, with the cap: 54 us, 2.4 us a step, of which
 // the copies alone need 1.6 (128 KB at 80 GB/s; every SM reads all keys and values of its tile from the L2), the products 1.05.
 #pragma once
 

@@ -481,7 +481,8 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
 
             // ---------------- outputs
-            if (n_it > 0 && ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_out), (uint32_t)round & 1u, P.wait_cycles)) && *(volatile int*)&s_timeout == 0;
+            // (Also after giving up: no product may be in flight when tensor memory is given back.)
+            if (n_it > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_out), (uint32_t)round & 1u, P.wait_cycles)) && ok && *(volatile int*)&s_timeout == 0;
             ok = __all_sync(0xffffffffu, ok);
             tc::fence_after();
             const int64_t row = (q0 + tok) * P.q_heads + h * P.group + r % P.group;

@@ -522,8 +522,9 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     if (!live) continue;
                     if (P.splits > 1) {
                         float* dst = P.part_o + ((int64_t)part * (P.T * P.q_heads) + row) * D + c;
+                        const bool wide = (reinterpret_cast<uintptr_t>(P.part_o) & 31u) == 0;       // the workspace is aligned to 16 bytes, or better
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) store32(dst + 8 * e, o + 8 * e, true);
+                        for (int e = 0; e < 4; ++e) store32(dst + 8 * e, o + 8 * e, wide);
                     } else {
                         __nv_bfloat16* dst = P.out + (q0 + tok) * P.ldo + (int64_t)(h * P.group + r % P.group) * D + c;
                         const bool wide = (reinterpret_cast<uintptr_t>(dst) & 31u) == 0;

@@ -471,3 +471,26 @@ def test_serving_calls_on_another_stream_and_in_a_graph():
         graph.replay()
         side.synchronize()
     assert torch.equal(y0, y1) and torch.equal(o0, o1)
+
+
+# ------------------------------------------------------------------ workspaces, marginal sizes and values
+
+@pytest.mark.parametrize("D,n,L,hint", [(64, 100, 1100, 1 << 20), (128, 100, 1100, 1 << 20), (256, 40, 900, 900), (128, 1, 5000, 5000), (64, 300, 2800, 2800)])
+def test_attn_paged_workspace_of_any_16_byte_alignment(D, n, L, hint):
+    # parts of the key range go through the workspace, which may start at any multiple of 16 bytes (the hint of a long range: query tiles of 128 rows)
+    Hq, Hkv, ps = 8, 2, 16
+    kc, vc, table = sr.make_cache([L], Hkv, D, ps, 21)
+    q = (torch.randn(n, Hq, D, generator=torch.Generator().manual_seed(22)) * 1.5).to(torch.bfloat16)
+    want, tol = sr.attn(q, kc, vc, table, [0, n], [L], D ** -0.5)
+    need = mq.attn_paged_workspace_bytes(n, 1, Hq, Hkv, D, n, hint)
+    assert need > 0
+    ws = torch.empty(need + 48, dtype=torch.uint8, device="cuda")
+    outs = []
+    for at in (0, 16, 48):
+        status = status_word()
+        o = mq.attn_paged(q.cuda(), kc.cuda(), vc.cuda(), table.cuda(), dev(np.array([0, n], np.int32)), dev(np.array([L], np.int32)), n, hint,
+                          workspace=ws[at:at + need], dev_status=status)
+        assert int(host(status)[0]) == mq.OK
+        assert bool(((o.cpu().double() - want).abs() <= tol).all())
+        outs.append(o)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])

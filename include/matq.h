@@ -399,13 +399,20 @@ enum matq_out_type { MATQ_OUT_F32 = 0, MATQ_OUT_BF16 = 1 };
  *   Y            out  fp32 or bf16 [M, N], row stride ldy elements
  *   flags        0 or MATQ_GEMV_PDL (the previous kernel of the stream writes neither q nor alpha nor zero: the kernel then
  *                     starts fetching weights before that kernel has ended, as in matq_gemv)
- *   c must be 8.  Requires K % 16 == 0, 16 <= K <= 65536, ldxq % 16 == 0, ldw % 16 == 0, xq and q 16-byte aligned, M and N below 2^31;
- *   any M, N >= 0.  A device-side wait that runs out sets dev_status = MATQ_ERR_TIMEOUT; Y is then unspecified.
+ *   c must be 8.  Requires K % 16 == 0, 16 <= K <= 65536, ldxq % 16 == 0, ldw % 16 == 0, xq and q 16-byte aligned, M and N below 2^31
+ *   (MATQ_ERR_SHAPE where both are so large that ceil(M / 256) * ceil(N / 256) reaches 2^30); M or N may be 0.  A device-side wait that runs out sets dev_status = MATQ_ERR_TIMEOUT; Y is then unspecified.
  */
 int matq_gemm_a8(const int8_t *xq, int64_t M, int64_t K, int64_t ldxq, const float *xscale, const int32_t *xsum,
                  const uint8_t *q, int64_t N, int64_t ldw, int c, const float *alpha, const float *zero,
                  int out_type, void *Y, int64_t ldy, unsigned flags,
                  int32_t *dev_status, void *stream);
+
+/* The kernels of (7): up to 8 tokens by warp-level products; tiles of 128 channels, K shared by the CTAs of a cluster; tiles of 256
+   channels by pairs of SMs. */
+enum matq_gemm_a8_kernel { MATQ_GEMM_A8_FEW = 0, MATQ_GEMM_A8_SPLIT = 1, MATQ_GEMM_A8_PAIRS = 2 };
+/* Which kernel (7) takes for these sizes on the current device, the token width of its tiles and the number of CTAs that share K (host only,
+   launches nothing).  M, N >= 1; MATQ_ERR_INVALID_ARG or MATQ_ERR_SHAPE for sizes that (7) would refuse.  Any of the pointers may be NULL. */
+int matq_gemm_a8_plan(int64_t M, int64_t N, int64_t K, int *kernel, int *tokens, int *parts);
 
 /*
  * A paged cache of keys and values and the batch of sequences that uses it.  (8) writes it and (9) reads it through the same

@@ -20,6 +20,7 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_SHAPE, ERR_ALIGNMENT = 0, 1, 2, 3, 4
 ERR_WORKSPACE, ERR_CUDA, ERR_NONFINITE, ERR_CAPACITY, ERR_TIMEOUT, ERR_PAGE = 5, 6, 8, 9, 10, 11
 SRC_BF16, SRC_CODES8, SRC_PACKED = 0, 1, 2
 OUT_F32, OUT_BF16 = 0, 1
+GEMM_A8_FEW, GEMM_A8_SPLIT, GEMM_A8_PAIRS = 0, 1, 2
 GEMV_AUTO, GEMV_CUDA_CORE, GEMV_TENSOR, GEMV_TCGEN05, GEMV_TENSOR_INT8, GEMV_STREAM, GEMV_PDL = 0, 1, 2, 3, 4, 5, 0x100
 GEMV_TEST_STALL = 0x8000
 TEACHER_AND_TARGET = 256    # matq_gemm_multi_loss: teacher[i] = TEACHER_AND_TARGET + j
@@ -30,7 +31,7 @@ EXPORTS = ["matq_status_string", "matq_version", "matq_packed_row_bytes", "matq_
            "matq_gemm_multi_loss_workspace_bytes", "matq_gemm_multi_loss",
            "matq_gemm_multi_test_stall", "matq_slice_pack_test_stall",
            "matq_gemm_multi_static_max_bytes", "matq_gemm_multi_static",
-           "matq_quantize_tokens", "matq_gemm_a8", "matq_kv_append", "matq_attn_paged_workspace_bytes", "matq_attn_paged",
+           "matq_quantize_tokens", "matq_gemm_a8", "matq_gemm_a8_plan", "matq_kv_append", "matq_attn_paged_workspace_bytes", "matq_attn_paged",
            "matq_serving_test_stall"]
 
 
@@ -106,6 +107,8 @@ def _load():
     lib.matq_quantize_tokens.argtypes = [vp, i64, i64, i64, vp, i64, vp, vp, vp, vp]
     lib.matq_gemm_a8.restype = i32
     lib.matq_gemm_a8.argtypes = [vp, i64, i64, i64, vp, vp, vp, i64, i64, i32, vp, vp, i32, vp, i64, u32, vp, vp]
+    lib.matq_gemm_a8_plan.restype = i32
+    lib.matq_gemm_a8_plan.argtypes = [i64, i64, i64, C.POINTER(C.c_int), C.POINTER(C.c_int), C.POINTER(C.c_int)]
     lib.matq_kv_append.restype = i32
     lib.matq_kv_append.argtypes = [C.POINTER(PagedKv), i64, vp, i32, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp, i64, vp, vp]
     lib.matq_attn_paged_workspace_bytes.restype = sz
@@ -453,6 +456,13 @@ def gemm_a8(xq, scale, rowsum, q, alpha, zero, y=None, out_dtype=torch.float32, 
     if st:
         raise MatqError(st, "matq_gemm_a8")
     return y
+
+
+def gemm_a8_plan(M, N, K) -> tuple[int, int, int]:
+    """matq_gemm_a8_plan: (kernel, token width of a tile, CTAs that share K) that gemm_a8 takes for these sizes."""
+    out = [C.c_int() for _ in range(3)]
+    _check(_lib.matq_gemm_a8_plan(M, N, K, *(C.byref(o) for o in out)), "matq_gemm_a8_plan")
+    return tuple(o.value for o in out)
 
 
 def kv_append(k_cache, v_cache, page_table, cu_q, kv_len, k, v, cos_sin=None, q=None, q_out=None, interleaved=False, dev_status=None):

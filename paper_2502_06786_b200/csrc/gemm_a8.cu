@@ -404,7 +404,7 @@ gemm_a8_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_const
             const uint32_t full = tc::smem_u32(s_full), empty = tc::smem_u32(s_empty), lead = in_cta(full, 0), base = tc::smem_u32(ring);
             const uint32_t bytes = 2 * kPairBlocks * (kBM + half) * kBK;
             for (int tile = pair; tile < tiles && ok; tile += pairs) {
-                const int m0 = tile % m_tiles * P.nt + (int)rank * half, n0 = tile / m_tiles * (2 * kBM) + (int)rank * kBM;
+                const int m0 = (int)min((int64_t)(tile % m_tiles) * P.nt + rank * half, P.M), n0 = tile / m_tiles * (2 * kBM) + (int)rank * kBM;
                 for (int x = 0; x < P.nkb * kBK; x += kPairBlocks * kBK) {             // past K the copies bring zeros
                     if (!tc::mbar_wait(empty + 8 * s, phase, P.wait_cycles)) { *(volatile int*)&s_timeout = 1; ok = false; break; }
                     if (rank == 0) tc::mbar_expect_tx(full + 8 * s, bytes);
@@ -500,8 +500,73 @@ inline bool byte_map(CUtensorMap* tm, const void* base, int64_t rows, int64_t K,
     return tc::make_map(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box);
 }
 
+enum Kind { kNone = -1, kFew = MATQ_GEMM_A8_FEW, kSplit = MATQ_GEMM_A8_SPLIT, kPairs = MATQ_GEMM_A8_PAIRS };
+struct Shape {
+    int kind, nt, splits;        // nt: token width of a tile; splits: CTAs that share K
+    int64_t cost;
+};
+
+// Kernel and tile: the shape whose estimated time is least.  Measured, ns: the start 2000 (pairs 2500); 256 bytes of K 350 (pairs 420,
+// above 168 tokens 2.5 a token); storing a tile 14 a token (pairs 800 and 18, while the next tile is summed); a cluster's join 1200 and 20 a token; an SM's
+// copies 85 GB/s, HBM 6300.  A cluster's CTAs share a GPC, which leaves clusters of eight about 128 of 148 SMs and clusters of four about 136.
+// The few-token kernel: 2200, and its copies at 45 GB/s per SM, 5000 in all.
+// Sizes that no kernel's grid holds have no shape.
+inline Shape choose(int64_t M, int64_t N, int64_t K, int sms) {
+    Shape s = {kNone, 0, 0, 0};
+    const auto offer = [&s](int kind, int nt, int splits, int64_t cost) {
+        if (s.kind == kNone || cost < s.cost) s = {kind, nt, splits, cost};
+    };
+    const int pairs = sms / 2;
+    const int64_t nst = ((K + kBK - 1) / kBK + 1) / 2, n_pair = (N + 2 * kBM - 1) / (2 * kBM), tiles_n = (N + kBM - 1) / kBM, hbm = N * K / 6300;
+    if (M <= kFewMaxM) {
+        const int64_t sm = ((N + 15) / 16 + sms - 1) / sms * 16 * K / 45, all = N * K / 5000;
+        offer(kFew, 0, 1, 2200 + (sm > all ? sm : all));
+    }
+    for (int nt = 16; nt <= 128; nt *= 2) {
+        const int64_t tiles_m = (M + nt - 1) / nt;
+        if ((nt < 128 && tiles_m > 8) || tiles_m > 65535) continue;
+        for (int sp = 1; sp <= kMaxSplitsK && sp <= nst; sp *= 2) {
+            const int64_t ctas = tiles_n * tiles_m * sp, stages = (nst + sp - 1) / sp, usable = sp == 8 ? sms * 128 / 148 : sp == 4 ? sms * 136 / 148 : sms;
+            const int64_t slots = usable * (nt <= 64 ? 2 : 1), rounds = (ctas + slots - 1) / slots, copies = (ctas + usable - 1) / usable * stages * (kBM + nt) * 256 / 85;
+            int64_t work = rounds * stages * 350;
+            if (work < copies) work = copies;
+            if (work < hbm) work = hbm;
+            offer(kSplit, nt, sp, work + rounds * (2000 + (sp > 1 ? 1200 + 20 * nt : 14 * nt)));
+        }
+    }
+    for (int nt = 256; nt >= 64 && M > 32; nt -= 32) {
+        const int64_t tiles = n_pair * ((M + nt - 1) / nt), rounds = (tiles + pairs - 1) / pairs;
+        if (tiles >= (1ll << 30)) continue;
+        const int64_t sum = nst * (nt > 168 ? 5 * nt / 2 : 420), store = 800 + 18 * nt;
+        int64_t work = (rounds - 1) * (sum > store ? sum : store) + sum;
+        if (work < hbm) work = hbm;
+        offer(kPairs, nt, 1, 2500 + work + store);
+    }
+    return s;
+}
+
+inline int size_error(int64_t M, int64_t N, int64_t K) {
+    if (M < 0 || N < 0 || K <= 0) return MATQ_ERR_INVALID_ARG;
+    if (K % 16 != 0 || K > 65536 || M >= (1ll << 31) || N >= (1ll << 31)) return MATQ_ERR_SHAPE;
+    return MATQ_OK;
+}
+
 }  // namespace a8
 }  // namespace matq
+
+extern "C" int matq_gemm_a8_plan(int64_t M, int64_t N, int64_t K, int* kernel, int* tokens, int* parts) {
+    using namespace matq;
+    using namespace matq::a8;
+    const int st = size_error(M, N, K);
+    if (st != MATQ_OK) return st;
+    if (M == 0 || N == 0) return MATQ_ERR_INVALID_ARG;
+    const Shape s = choose(M, N, K, sm_count());
+    if (s.kind == kNone) return MATQ_ERR_SHAPE;
+    if (kernel) *kernel = s.kind;
+    if (tokens) *tokens = s.kind == kFew ? kFewMaxM : s.nt;
+    if (parts) *parts = s.splits;
+    return MATQ_OK;
+}
 
 extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq, const float* xscale, const int32_t* xsum,
                             const uint8_t* q, int64_t N, int64_t ldw, int c, const float* alpha, const float* zero,
@@ -510,7 +575,7 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
     using namespace matq::a8;
     if (M < 0 || N < 0 || K <= 0 || (out_type != MATQ_OUT_F32 && out_type != MATQ_OUT_BF16) || (flags & ~(unsigned)MATQ_GEMV_PDL)) return MATQ_ERR_INVALID_ARG;
     if (c != kCodeBits) return MATQ_ERR_UNSUPPORTED;
-    if (K % 16 != 0 || K > 65536 || ldxq < K || ldxq % 16 != 0 || ldw < K || ldw % 16 != 0 || ldy < N || M >= (1ll << 31) || N >= (1ll << 31)) return MATQ_ERR_SHAPE;
+    if (size_error(M, N, K) != MATQ_OK || ldxq < K || ldxq % 16 != 0 || ldw < K || ldw % 16 != 0 || ldy < N) return MATQ_ERR_SHAPE;
     if (M == 0 || N == 0) return MATQ_OK;
     if (!xq || !xscale || !xsum || !q || !alpha || !zero || !Y) return MATQ_ERR_INVALID_ARG;
     if (!aligned16(xq) || !aligned16(q)) return MATQ_ERR_ALIGNMENT;
@@ -526,46 +591,15 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
     P.K = K;
     P.nkb = (int)((K + kBK - 1) / kBK);
     const int sms = sm_count();
+    const Shape shape = choose(M, N, K, sms);
+    if (shape.kind == kNone) return MATQ_ERR_SHAPE;
+    P.nt = shape.nt; P.splits = shape.splits;
     cudaError_t e;
-    // Kernel and tile: the shape whose estimated time is least.  Measured, ns: the start 2000 (pairs 2500); 256 bytes of K 350 (pairs 420,
-    // above 168 tokens 2.5 a token); storing a tile 14 a token (pairs 800 and 18, while the next tile is summed); a cluster's join 1200 and 20 a token; an SM's
-    // copies 85 GB/s, HBM 6300.  A cluster's CTAs share a GPC, which leaves clusters of eight about 128 of 148 SMs and clusters of four about 136.
-    // The few-token kernel: 2200, and its copies at 45 GB/s per SM, 5000 in all.
-    const int pairs = sms / 2;
-    const int64_t nst = (P.nkb + 1) / 2, n_pair = (N + 2 * kBM - 1) / (2 * kBM), tiles_n = (N + kBM - 1) / kBM, hbm = N * K / 6300;
-    int64_t best = -1;
-    bool use_pairs = false;
-    for (int nt = 16; nt <= 128; nt *= 2) {
-        const int64_t tiles_m = (M + nt - 1) / nt;
-        if ((nt < 128 && tiles_m > 8) || tiles_m > 65535) continue;
-        for (int sp = 1; sp <= kMaxSplitsK && sp <= nst; sp *= 2) {
-            const int64_t ctas = tiles_n * tiles_m * sp, stages = (nst + sp - 1) / sp, usable = sp == 8 ? sms * 128 / 148 : sp == 4 ? sms * 136 / 148 : sms;
-            const int64_t slots = usable * (nt <= 64 ? 2 : 1), rounds = (ctas + slots - 1) / slots, copies = (ctas + usable - 1) / usable * stages * (kBM + nt) * 256 / 85;
-            int64_t work = rounds * stages * 350;
-            if (work < copies) work = copies;
-            if (work < hbm) work = hbm;
-            const int64_t cost = work + rounds * (2000 + (sp > 1 ? 1200 + 20 * nt : 14 * nt));
-            if (best < 0 || cost < best) { best = cost; P.nt = nt; P.splits = sp; }
-        }
-    }
-    for (int nt = 256; nt >= 64 && M > 32; nt -= 32) {
-        const int64_t tiles = n_pair * ((M + nt - 1) / nt), rounds = (tiles + pairs - 1) / pairs;
-        const int64_t sum = nst * (nt > 168 ? 5 * nt / 2 : 420), store = 800 + 18 * nt;
-        int64_t work = (rounds - 1) * (sum > store ? sum : store) + sum;
-        if (work < hbm) work = hbm;
-        const int64_t cost = 2500 + work + store;
-        if (cost < best) { best = cost; P.nt = nt; use_pairs = true; }
-    }
-    int64_t few = -1;
-    if (M <= kFewMaxM) {
-        const int64_t sm = ((N + 15) / 16 + sms - 1) / sms * 16 * K / 45, all = N * K / 5000;
-        few = 2200 + (sm > all ? sm : all);
-    }
-    if (few >= 0 && few <= best) {
+    if (shape.kind == kFew) {
         e = launch_few(q, ldw, xq, ldxq, P, sms, s);
-    } else if (!use_pairs) {
+    } else if (shape.kind == kSplit) {
         P.tmem_cols = P.nt < 32 ? 32 : P.nt;
-        const int64_t tiles_m = (M + P.nt - 1) / P.nt;
+        const int64_t tiles_n = (N + kBM - 1) / kBM, tiles_m = (M + P.nt - 1) / P.nt;
         const int stage_bytes = kSplitBlocks * (kBM + P.nt) * kBK;
         P.stages = (P.nt <= 64 && tiles_n * tiles_m * P.splits > sms ? 104 * 1024 : 200 * 1024) / stage_bytes;      // two CTAs share an SM, or one has it
         if (P.stages > kMaxStages) P.stages = kMaxStages;
@@ -591,8 +625,7 @@ extern "C" int matq_gemm_a8(const int8_t* xq, int64_t M, int64_t K, int64_t ldxq
         cfg.numAttrs = 2;
         e = cudaLaunchKernelEx(&cfg, gemm_a8_split_kernel, tm_w, tm_x, P);
     } else {
-        const int64_t tiles = n_pair * ((M + P.nt - 1) / P.nt);
-        if (tiles >= (1ll << 30)) return MATQ_ERR_SHAPE;
+        const int64_t tiles = (N + 2 * kBM - 1) / (2 * kBM) * ((M + P.nt - 1) / P.nt), pairs = sms / 2;
         CUtensorMap tm_w, tm_x;
         if (!byte_map(&tm_w, q, N, K, ldw, kBM) || !byte_map(&tm_x, xq, M, K, ldxq, P.nt / 2)) return MATQ_ERR_CUDA;
         static std::atomic<unsigned long long> pair_ok{0};

@@ -118,3 +118,31 @@ def test_binding_refuses_host_tensors_and_wrong_types():
         mq.attn_paged(torch.zeros(4, 2, 64, dtype=torch.bfloat16), kc, kc, t, t[0], t[0], 1, 1)
     with pytest.raises(TypeError):
         mq._serving.gemm_a8(1, 2)
+
+
+def test_gemm_a8_has_a_kernel_for_every_size_it_accepts():
+    """The choice of kernel and tile is host arithmetic: every accepted size has one, up to the limits of M and N."""
+    big = (1 << 31) - 1
+    sizes = [1, 2, 8, 9, 16, 17, 32, 33, 64, 100, 128, 129, 509, 1024, 1025, 4096, 65535, 128 * 65535, 128 * 65535 + 1, 9000000, 1 << 30, big - 1, big]
+    for M in sizes:
+        for N in sizes:
+            for K in (16, 144, 4096, 65536):
+                tiles = -(-M // 256) * -(-N // 256)
+                try:
+                    kernel, tokens, parts = mq.gemm_a8_plan(M, N, K)
+                except mq.MatqError as e:
+                    assert e.status == mq.ERR_SHAPE and tiles >= 1 << 30, (M, N, K)
+                    continue
+                if kernel == mq.GEMM_A8_FEW:
+                    assert M <= tokens == 8 and parts == 1
+                elif kernel == mq.GEMM_A8_SPLIT:
+                    assert tokens in (16, 32, 64, 128) and parts in (1, 2, 4, 8) and -(-M // tokens) <= 65535, (M, N, K)
+                    assert parts <= -(-K // 256) and -(-N // 128) * parts < 1 << 31
+                else:
+                    assert kernel == mq.GEMM_A8_PAIRS and tokens in range(64, 257, 32) and parts == 1
+                    assert -(-M // tokens) * -(-N // 256) < 1 << 30
+    assert mq.gemm_a8_plan(128 * 65535 + 1, 256, 256)[0] == mq.GEMM_A8_PAIRS
+    for M, N, K, st in ((0, 1, 16, mq.ERR_INVALID_ARG), (1, 0, 16, mq.ERR_INVALID_ARG), (-1, 1, 16, mq.ERR_INVALID_ARG), (1, 1, 0, mq.ERR_INVALID_ARG),
+                        (1, 1, 24, mq.ERR_SHAPE), (1, 1, 65552, mq.ERR_SHAPE), (1 << 31, 1, 16, mq.ERR_SHAPE), (1, 1 << 31, 16, mq.ERR_SHAPE)):
+        assert lib.matq_gemm_a8_plan(M, N, K, NULL, NULL, NULL) == st, (M, N, K)
+    assert lib.matq_gemm_a8_plan(1, 1, 16, NULL, NULL, NULL) == mq.OK

@@ -494,3 +494,15 @@ def test_attn_paged_workspace_of_any_16_byte_alignment(D, n, L, hint):
         assert bool(((o.cpu().double() - want).abs() <= tol).all())
         outs.append(o)
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+def test_gemm_a8_more_tokens_than_any_grid_of_small_tiles_holds():
+    M, N, K = 128 * 65535 + 130, 16, 16
+    xq, s, r, q, a, z = _linear(M, N, K, 91)
+    status = status_word()
+    y = mq.gemm_a8(xq, s, r, q, a, z, dev_status=status)
+    assert int(host(status)[0]) == mq.OK
+    for lo in range(0, M, 1 << 21):
+        hi = min(M, lo + (1 << 21))
+        want, tol = sr.gemm_a8(xq[lo:hi], s[lo:hi], q, a, z, torch.float32)
+        assert bool(((y[lo:hi].double() - want).abs() <= tol).all())

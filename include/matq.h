@@ -83,7 +83,9 @@ enum matq_gemv_flags {
     MATQ_GEMV_PDL = 0x100      /* launch with programmatic stream serialisation: the kernel starts
                                   fetching weights (plane, alpha, zero, overflow lists) while the previous
                                   kernel in the stream drains and waits for it only before reading x.
-                                  Only valid when that previous kernel does not write those weights. */
+                                  Only valid when that previous kernel does not write those weights.
+                                  (The kernels of this library let a successor start only after their own
+                                  predecessor has ended, so that nothing older can still be writing them.) */
 };
 
 const char *matq_status_string(int status);

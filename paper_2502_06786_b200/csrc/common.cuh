@@ -45,6 +45,9 @@ inline int sm_count() {
 // stream is still running (its start-up then overlaps that kernel's tail), and the kernel calls after_previous_kernel()
 // before its first access to global memory, so it neither reads what the predecessor has not written yet nor writes what
 // it may still read.  let_next_kernel_start() lets a successor launched the same way begin its own start-up early.
+// A thread calls it only behind its own wait.  Then no kernel starts before the one two places ahead of it has ended, and what a kernel may read before its
+// wait (weights, under MATQ_GEMV_PDL) has to be left alone by its direct predecessor only: in slice_pack(W2), gemm_a8(W1), gemm_a8(W2) the last
+// call would otherwise fetch codes that the first still writes.
 __device__ __forceinline__ void after_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;"); }
 

@@ -88,8 +88,7 @@ gemm_a8_few_kernel(const uint8_t* __restrict__ q, int64_t ldw, const int8_t* xq,
     __shared__ int s_sum[8][16 * MT + 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, kq = (lane & 3) * 16;
     const int64_t n0 = (int64_t)blockIdx.x * (16 * MT);
-    if (!P.early) after_previous_kernel();
-    let_next_kernel_start();
+    if (!P.early) { after_previous_kernel(); let_next_kernel_start(); }
     for (int i = tid; i < 8 * (16 * MT + 1); i += kFewThreads) (&s_sum[0][0])[i] = 0;
     const int K = (int)P.K, pieces = (K + 63) / 64;
     const uint8_t* wrow[2 * MT];
@@ -113,7 +112,7 @@ gemm_a8_few_kernel(const uint8_t* __restrict__ q, int64_t ldw, const int8_t* xq,
 #pragma unroll
             for (int i = 0; i < 2 * MT; ++i) w[u][i] = wlive[i] && k + kq < K ? ld_stream_u4(wrow[i] + k) : make_uint4(0u, 0u, 0u, 0u);
         }
-        if (!waited) { after_previous_kernel(); waited = true; }         // the first codes are on their way before the activations are known to be there
+        if (!waited) { after_previous_kernel(); let_next_kernel_start(); waited = true; }         // the first codes are on their way before the activations are known to be there
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const int k = (c0 + u * kFewWarps) * 64;
@@ -127,7 +126,7 @@ gemm_a8_few_kernel(const uint8_t* __restrict__ q, int64_t ldw, const int8_t* xq,
                 mma_u8s8(acc[i], w[u][2 * i].z, w[u][2 * i + 1].z, w[u][2 * i].w, w[u][2 * i + 1].w, x[u].z, x[u].w);
             }
     }
-    if (!waited) after_previous_kernel();
+    if (!waited) { after_previous_kernel(); let_next_kernel_start(); }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -204,7 +203,7 @@ gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     const int block_bytes = (kBM + P.nt) * kBK, stage_bytes = kSplitBlocks * block_bytes;
     unsigned char* ring = smem_raw + ((1024 - (tc::smem_u32(smem_raw) & 1023)) & 1023);
 
-    if (!P.early) after_previous_kernel();
+    if (!P.early) { after_previous_kernel(); let_next_kernel_start(); }
     if (tid == 0) {
         for (int s = 0; s < P.stages; ++s) { tc::mbar_init(tc::smem_u32(&s_full[s]), 1); tc::mbar_init(tc::smem_u32(&s_empty[s]), 1); }
         tc::mbar_init(tc::smem_u32(&s_acc), 1);
@@ -219,7 +218,6 @@ gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     __syncthreads();
     tc::fence_after();
     const uint32_t tmem = s_tmem;
-    let_next_kernel_start();
 
     const int64_t n = n0 + (warp & 3) * 32 + lane;                      // epilogue warps: this thread's channel
     float al = 0.f, zc = 0.f;
@@ -237,7 +235,7 @@ gemm_a8_split_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
             };
             if (!P.hold)
                 for (int i = 0; i < ahead; ++i) weights(base + (uint32_t)(i * stage_bytes), st0 + i, full + 8 * i);
-            if (P.early) after_previous_kernel();
+            if (P.early) { after_previous_kernel(); let_next_kernel_start(); }
             int s = 0, issued = 0;
             uint32_t phase = 1;
             for (int st = st0; st < st1 && !P.hold; ++st) {

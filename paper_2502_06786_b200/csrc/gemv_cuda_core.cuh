@@ -31,8 +31,8 @@ gemv_cuda_core(const uint8_t* __restrict__ packed, int64_t N, int64_t K,
     const int64_t row_bytes = K * R / 8;
     const int64_t warps = (int64_t)gridDim.x * (kGemvCcThreads / 32);
     if (pdl) {
-        asm volatile("griddepcontrol.launch_dependents;");
         asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;");
     }
     for (int b0 = 0; b0 < B; b0 += BT) {
         for (int64_t n0 = ((int64_t)blockIdx.x * (kGemvCcThreads / 32) + (threadIdx.x >> 5)) * kGemvCcRows; n0 < N;

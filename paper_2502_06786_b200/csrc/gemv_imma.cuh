@@ -170,8 +170,8 @@ gemv_imma(const Params P) {
     }
 
     if (P.pdl) {
-        asm volatile("griddepcontrol.launch_dependents;");
         asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;");
     }
 
     float ep_x0 = 0.f;

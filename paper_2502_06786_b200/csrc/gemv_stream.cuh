@@ -858,7 +858,7 @@ gemv_stream(const __grid_constant__ Params<NP> P) {
     for (int i = tid; i < kTileSlots * 2 * 16 * imma::kCols; i += blockDim.x) (&s_tile[0][0][0][0])[i] = 0;
     if (tid < kTileSlots) s_tile_cnt[tid] = 0;
     __syncthreads();
-    if (P.pdl) asm volatile("griddepcontrol.launch_dependents;");
+    if (P.pdl == 2) asm volatile("griddepcontrol.launch_dependents;");        // ep_rowsum, of the same call, started after its own predecessor had ended
 
     // this CTA's share of the list: items [lo, hi), cut at tile boundaries (a tile belongs to the CTA its first item falls to)
     const long long lo = P.items * blockIdx.x / gridDim.x, hi = P.items * (blockIdx.x + 1) / gridDim.x;
@@ -907,7 +907,10 @@ gemv_stream(const __grid_constant__ Params<NP> P) {
                 // wait; pulling their lines into the L2 earlier is harmless (the L2 is the point of coherence) and takes the
                 // HBM latency of a cold vector off the critical path.
                 for (int i = ctid * 64; i < pr.K; i += nthr * 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(pr.x + i));
-                if (P.pdl == 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+                if (P.pdl == 1) {
+                    asm volatile("griddepcontrol.wait;" ::: "memory");
+                    asm volatile("griddepcontrol.launch_dependents;");
+                }
             }
             first = false;
 

@@ -513,7 +513,6 @@ gemv_stream_batch(const __grid_constant__ Params<NP> P) {
     for (int i = tid; i < kTileSlots * G * 16 * imma::kCols; i += blockDim.x) (&s_tile[0][0][0][0])[i] = 0;
     if (tid < kTileSlots) s_tile_cnt[tid] = 0;
     __syncthreads();
-    if (P.pdl) asm volatile("griddepcontrol.launch_dependents;");
 
     const long long lo = P.items * blockIdx.x / gridDim.x, hi = P.items * (blockIdx.x + 1) / gridDim.x;
     int p_first = 0;
@@ -552,7 +551,10 @@ gemv_stream_batch(const __grid_constant__ Params<NP> P) {
             }
             if (first) {
                 for (int i = ctid * 64; i < pr.K * B; i += nthr * 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(pr.x + i));
-                if (P.pdl) asm volatile("griddepcontrol.wait;" ::: "memory");
+                if (P.pdl) {
+                    asm volatile("griddepcontrol.wait;" ::: "memory");
+                    asm volatile("griddepcontrol.launch_dependents;");
+                }
             }
             first = false;
 

@@ -215,7 +215,6 @@ gemv_tcgen05(const __grid_constant__ CUtensorMap tm_w, const Params P) {
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
-    if (P.pdl) asm volatile("griddepcontrol.launch_dependents;");
 
     if (warp < kUnpackWarps) {
         // ================= unpack warpgroups: weights -> bf16x2 -> TMEM slots; warpgroup 0 also finishes the rows
@@ -299,7 +298,10 @@ gemv_tcgen05(const __grid_constant__ CUtensorMap tm_w, const Params P) {
         if (!ok) s_timeout = 1;
     } else if (warp < kUnpackWarps + kStageWarps) {
         // ================= stage warps: the only readers of x; everything after this point depends on the predecessor
-        if (P.pdl) asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (P.pdl) {
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            asm volatile("griddepcontrol.launch_dependents;");
+        }
         const int st_tid = tid - 32 * kUnpackWarps;              // 0..127
         const int bcol = st_tid & (kNB - 1);
         const int64_t k_base = slice_off * 8 / R;

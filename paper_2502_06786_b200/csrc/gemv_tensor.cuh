@@ -264,8 +264,8 @@ gemv_tensor(const GemvTensorParams P) {
     }
 
     if (P.pdl) {
-        asm volatile("griddepcontrol.launch_dependents;");
         asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;");
     }
 
     // activation (batch column 0) of this thread's first overflow column: requested now, used after the staging

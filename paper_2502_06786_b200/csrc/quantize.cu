@@ -251,8 +251,8 @@ quantize_rows_reg(const uint16_t* __restrict__ W, int64_t N, int K, int64_t ldw,
                   int32_t* dev_status) {
     __shared__ float s_mn[WARPS], s_mx[WARPS];
     __shared__ int s_bad[WARPS];
-    let_next_kernel_start();
     after_previous_kernel();
+    let_next_kernel_start();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rows_per_cta = (WARPS) / wpr;
     const int team = warp / wpr, team_tid = (warp % wpr) * 32 + lane, team_threads = 32 * wpr;

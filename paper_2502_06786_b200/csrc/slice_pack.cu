@@ -82,8 +82,8 @@ slice_pack_vec(const uint4* __restrict__ q, int64_t nchunks, int chunks_per_row,
     const int r = PACK_R ? PACK_R : r_runtime;
     const int sh = kCodeBits - r;
     const int64_t stride = (int64_t)gridDim.x * kSliceThreads;
-    let_next_kernel_start();
     after_previous_kernel();
+    let_next_kernel_start();
     for (int64_t i = (int64_t)blockIdx.x * kSliceThreads + threadIdx.x; i < nchunks; i += stride) {
         const uint4 v = ld_stream_u4(q + i);
         if (PACK_R == 2 && !sliced) {

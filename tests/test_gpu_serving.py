@@ -506,3 +506,29 @@ def test_gemm_a8_more_tokens_than_any_grid_of_small_tiles_holds():
         hi = min(M, lo + (1 << 21))
         want, tol = sr.gemm_a8(xq[lo:hi], s[lo:hi], q, a, z, torch.float32)
         assert bool(((y[lo:hi].double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("M", [1, 5, 64, 400])
+def test_weights_written_two_calls_before_a_call_that_fetches_them_early(M):
+    # slice_pack writes W2, a call that fetches W1 early follows, then one that fetches W2 early: its predecessor writes no weights
+    N, K, n_small = 4096, 4096, 64
+    g = torch.Generator(device="cuda").manual_seed(33)
+    codes = [torch.randint(0, 256, (N, K), generator=g, device="cuda").to(torch.uint8) for _ in range(4)]
+    xq, s, r, q1, a1, z1 = _linear(M, n_small, K, 34)
+    a2, z2 = torch.rand(N, generator=g, device="cuda") + 0.5, torch.full((N,), 128.0, device="cuda")
+    x = torch.randn(K, generator=g, device="cuda").to(torch.bfloat16)
+    small = mq.slice_pack(q1, 4, want_unpacked=True)
+    sliced, packed = torch.empty_like(codes[0]), torch.empty((N, K // 2), dtype=torch.uint8, device="cuda")
+    ys, vs = [], []
+    for c in codes * 3:
+        mq.slice_pack(c, 4, packed=packed, sliced_unpacked=sliced)
+        mq.gemm_a8(xq, s, r, small["sliced"], a1, z1, flags=mq.GEMV_PDL)
+        ys.append(mq.gemm_a8(xq, s, r, sliced, a2, z2, flags=mq.GEMV_PDL))
+        mq.slice_pack(c, 4, packed=packed, sliced_unpacked=sliced)
+        mq.gemv(small["packed"], K, 4, a1, z1, x[None], flags=mq.GEMV_PDL)
+        vs.append(mq.gemv(packed, K, 4, a2, z2, x[None], flags=mq.GEMV_PDL))
+    for i, c in enumerate(codes * 3):
+        out = mq.slice_pack(c, 4, want_unpacked=True)
+        torch.cuda.synchronize()
+        assert torch.equal(ys[i], mq.gemm_a8(xq, s, r, out["sliced"], a2, z2))
+        assert torch.equal(vs[i], mq.gemv(out["packed"], K, 4, a2, z2, x[None]))

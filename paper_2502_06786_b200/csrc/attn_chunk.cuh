@@ -27,6 +27,10 @@
 namespace matq {
 namespace attn {
 
+// A reference of this size (in exponents of two) is not the sum of the old one and a distance to it, whose rounding would pass many exponents, but the row's
+// largest score itself, looked up again; and it is taken off the scores before they are multiplied, because the fused product keeps what the
+// rounding of the reference left out (half of 2^-23 of it: above 2^30 more than kFar, and weights were Inf or all zero).
+constexpr float kLarge = 16777216.f;
 constexpr int kMaxMasked = 16;          // tiles at a range's ends that some row does not see in full
 
 template <int D, int TILES>
@@ -76,6 +80,36 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* v, bool wide) {
 // D = fp32, A = B = bf16, 128 rows
 __device__ __forceinline__ constexpr uint32_t idesc_bf16(int n, bool b_mn_major) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+
+// The largest of a thread's scores in columns lo .. hi of its COLS (with the cap: its exponent).  Rare, and kept out of the loop over the keys, whose code it would spread.
+template <bool CAP, int COLS>
+__device__ __noinline__ float largest_score(uint32_t addr, int lo, int hi, Score sc) {
+    float best = -INFINITY;
+#pragma unroll 1
+    for (int c = 0; c < COLS; c += 32) {
+        uint32_t v[32];
+        tc::tmem_ld32(addr + c, v);
+        tc::tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            if (c + e >= lo && c + e <= hi) best = fmaxf(best, CAP ? capped(__uint_as_float(v[e]), sc.mul, sc.cap2) : __uint_as_float(v[e]));
+    }
+    return best;
+}
+// Takes a large reference off the scores.
+template <int COLS>
+__device__ __noinline__ void lift_scores(uint32_t addr, float by) {
+#pragma unroll 1
+    for (int c = 0; c < COLS; c += 32) {
+        uint32_t v[32];
+        tc::tmem_ld32(addr + c, v);
+        tc::tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) - by);
+        tmem_st32(addr + c, v);
+    }
+    tc::tmem_wait_st();
 }
 
 // CAP: with the cap on the scores
@@ -286,6 +320,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const Score sc(P.scale, P.softcap);
             const float tmul = P.softcap > 0.f ? P.scale / P.softcap : 0.f;        // the tanh's argument per score
             const float tanh0 = kTanh0 * sc.cap2, tanh1 = kTanh1 * sc.cap2, tanh2 = kTanh2 * sc.cap2, tanh3 = kTanh3 * sc.cap2;       // with the cap
+            const float unit = CAP ? 1.f : sc.mul;                      // the reference is kept as a score; with the cap, as an exponent
             float m = -INFINITY, l = 0.f;
             bool ok = true;
             int masked_no = 0;
@@ -320,7 +355,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 ok = __all_sync(0xffffffffu, ok);
                 const bool masked = is_masked(j0);
                 const uint32_t s_addr = lane_addr + which * kKeys + col0;
-                float top = -INFINITY, use;
+                float top = -INFINITY, use, off;
                 uint64_t sum2[2];
                 uint32_t pk[C::kCols / 2];
                 // One pass: exponents x = score - reference, their maximum, 2^x, its sum, bf16.  Should x exceed kFar somewhere the reference moves and
@@ -330,7 +365,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     sum2[0] = sum2[1] = 0;
                     uint32_t sr[2][32];
                     tc::tmem_ld32(s_addr, sr[0]);
-                    const uint64_t neg = pair(-use, -use), mul = pair(sc.mul, sc.mul);
+                    const uint64_t neg = pair(off, off), mul = pair(sc.mul, sc.mul);
 #pragma unroll
                     for (int c = 0; c < C::kCols; c += 32) {
                         uint32_t* v = sr[(c >> 5) & 1];
@@ -342,7 +377,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                             for (int e = 0; e < 32; e += 2) big = max3(big, fabsf(__uint_as_float(v[e])), fabsf(__uint_as_float(v[e + 1])));
                             if (__any_sync(0xffffffffu, !(big * tmul <= kTanhMax))) {       // some score is past the polynomial's range
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(capped(__uint_as_float(v[e]), sc.mul, sc.cap2) - use);
+                                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(capped(__uint_as_float(v[e]), sc.mul, sc.cap2) + off);
                             } else {
                                 const uint64_t tm2 = pair(tmul, tmul);
 #pragma unroll
@@ -381,11 +416,15 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     }
                 };
                 // A row without a reference (m = -inf) takes 0 for one if its largest score is not far from it, as ordinary scores are not: then its first
-                // step is not done twice.
-                const auto wants = [&] { return ok && (top > kFar || (m == -INFINITY && top < -kFar && top > -INFINITY)); };
+                // step is not done twice.  A row with a large one always has its scores looked at once more.
+                bool lifted = false;
+                const auto wants = [&] {
+                    return ok && (top > kFar || (m == -INFINITY && top < -kFar && top > -INFINITY) || (!lifted && fabsf(use) >= kLarge));
+                };
                 if (ok) tc::fence_after();
-                for (int attempt = 0; attempt < 3; ++attempt) {         // the second always suffices: nothing exceeds a reference that was just moved
-                    use = m == -INFINITY ? 0.f : m;
+                for (int attempt = 0; attempt < 3; ++attempt) {         // the second suffices: nothing lies far above a reference that was just moved
+                    use = m == -INFINITY ? 0.f : m * unit;
+                    off = !CAP && lifted && fabsf(use) >= kLarge ? 0.f : -use;
                     if (ok) {
                         if (masked) pass(std::true_type{});
                         else pass(std::false_type{});
@@ -400,15 +439,32 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         top = fmaxf(s_half[0][r], s_half[1][r]);
                         raise = wants();
                         if (m == -INFINITY && top > -INFINITY && !raise) m = 0.f;
-                        if (!soft_any(raise)) break;
+                        if (__builtin_expect(!soft_any(raise), 1)) break;
                         if (ok && i > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_pv[(gi - 1) & 1]), (uint32_t)((gi - 1) >> 1) & 1u, P.wait_cycles));
                     } else {
                         if (m == -INFINITY && top > -INFINITY && !raise) m = 0.f;
-                        if (!__any_sync(0xffffffffu, raise)) break;
+                        if (__builtin_expect(!__any_sync(0xffffffffu, raise), 1)) break;
+                    }
+                    float ref = (use + top) / unit, next = ref * unit;  // the new reference as it is kept, and as an exponent
+                    const bool large = !lifted && raise && (fabsf(use) >= kLarge || fabsf(next) >= kLarge);
+                    if (__builtin_expect(C::kTiles == 1 ? soft_any(large) : __any_sync(0xffffffffu, large), 0)) {
+                        float best = ok ? largest_score<CAP, C::kCols>(s_addr, see_lo - j0 - col0, see_hi - j0 - col0, sc) : -INFINITY;
+                        if (C::kTiles == 1) {
+                            s_half[part_of][r] = best;
+                            asm volatile("bar.sync 2, %0;" ::"n"(C::kSoft) : "memory");
+                            best = fmaxf(s_half[0][r], s_half[1][r]);
+                        }
+                        if (large) {
+                            ref = best;
+                            next = best * unit;
+                            raise = best > -INFINITY && (m == -INFINITY || next - use > kFar);
+                        }
+                        if (!CAP && ok) lift_scores<C::kCols>(s_addr, raise ? (fabsf(next) >= kLarge ? ref : 0.f) : fabsf(use) >= kLarge ? m : 0.f);
+                        lifted = true;
                     }
                     // O holds the steps before this one.  Their last product is over: with one tile that was waited for, with two the scores' arrival says so.
-                    const float f = raise ? ex2(m - (use + top)) : 1.f;
-                    if (raise) m = use + top;
+                    const float f = raise ? ex2(m * unit - next) : 1.f;
+                    if (raise) m = ref;
                     l *= f;
                     if (ok && i > 0) {
                         tc::fence_after();
@@ -494,7 +550,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
             const float inv = any ? 1.f / l : 0.f;
             if (!ok) *(volatile int*)&s_timeout = 1;
-            if (ok && live && P.splits > 1 && o_col == 0) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(m, l);
+            if (ok && live && P.splits > 1 && o_col == 0) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(m * unit, l);
             if (ok && !(P.splits > 1 && n_it == 0)) {
 #pragma unroll 1
                 for (int c = o_col; c < o_col + kOCols; c += 32) {

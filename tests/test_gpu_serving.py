@@ -532,3 +532,50 @@ def test_weights_written_two_calls_before_a_call_that_fetches_them_early(M):
         torch.cuda.synchronize()
         assert torch.equal(ys[i], mq.gemm_a8(xq, s, r, out["sliced"], a2, z2))
         assert torch.equal(vs[i], mq.gemv(out["packed"], K, 4, a2, z2, x[None]))
+
+
+def _sign_scores(D, n, L, exponent, step=None, seed=51):
+    """Queries and keys of +-2^a: every product q . k is an integer times 2^exponent, exact in 32 bits, so that two scores are equal or far apart.
+    Before position ``step`` the keys are 2^-exponent times as large."""
+    a = exponent // 2
+
+    def edit(kc, vc, table, q):
+        g = torch.Generator().manual_seed(seed)
+        q.copy_(torch.randint(0, 2, q.shape, generator=g).to(torch.bfloat16) * 2 - 1)
+        q.mul_(2.0 ** a)
+        kc.copy_(torch.randint(0, 2, kc.shape, generator=g).to(torch.bfloat16) * 2 - 1)
+        kc.mul_(2.0 ** a)
+        if step is not None:
+            for j in range(step):
+                kc[table[0, j // kc.shape[2]], :, j % kc.shape[2]] *= 2.0 ** -(2 * a)
+    return edit
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,L,hint", [(1, 700, 700), (4, 700, 700), (60, 500, 1 << 20), (140, 900, 1 << 20), (140, 300, 300)])
+@pytest.mark.parametrize("exponent", [4, 16, 24, 30, 34, 40, 60, 100])
+def test_attn_paged_scores_of_any_finite_size(D, n, L, hint, exponent):
+    # one key (or several of one score) takes all the weight, however far the scores lie from zero, and whichever kernel and split does it
+    for step in (None, 200):
+        _check(*_attend([n], [L], 4, 2, D, 16, seed=52, scale=1.0, hints=(n, hint), edit=_sign_scores(D, n, L, exponent, step)))
+
+
+@pytest.mark.parametrize("D,news", [(64, [140] * 20), (128, [140] * 20), (256, [60] * 20)])
+@pytest.mark.parametrize("exponent", [24, 34, 60])
+def test_attn_paged_many_query_tiles_scores_of_any_finite_size(D, news, exponent):
+    lens = [n + 30 + 19 * i for i, n in enumerate(news)]
+    _check(*_attend(news, lens, 8, 2, D, 16, seed=53, scale=1.0, edit=_sign_scores(D, news, lens, exponent)))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,L,hint", [(4, 700, 700), (60, 500, 1 << 20), (140, 900, 1 << 20), (140, 300, 300)])
+@pytest.mark.parametrize("exponent", [30, 60])
+def test_attn_paged_rows_with_large_and_with_ordinary_scores(D, n, L, hint, exponent):
+    # heads of one token, and neighbouring tokens, share a tile: every second row's scores are ordinary ones
+    signs = _sign_scores(D, n, L, exponent, 200)
+
+    def edit(kc, vc, table, q):
+        signs(kc, vc, table, q)
+        q.flatten(0, 1)[::2].mul_(2.0 ** -(exponent + 3))
+        q[1::3].mul_(2.0 ** -(exponent // 2))
+    _check(*_attend([n], [L], 4, 2, D, 16, seed=54, scale=1.0, hints=(n, hint), edit=edit))

@@ -31,12 +31,16 @@ struct Params {
     int hold;
 };
 
-// Scores as exponents of two: p = 2^(value - maximum).  Without a cap that is one product; the cap's tanh is written with an
-// exponential, 1 - 2 / (1 + e^2x), whose absolute error stays at fp32's where x is small and saturates without overflow where it is large.
+// Scores as exponents of two: p = 2^(value - maximum).  Without a cap that is one product.  The cap's tanh is a polynomial for arguments up to
+// kTanhMax and 1 - 2 / (1 + e^2x) above, which saturates without overflow; near zero that difference would keep an absolute accuracy only, and a cap far
+// above the scores multiplies it (1e-7 of the cap: at 1e5 weights were off by more than one percent).
+// Odd polynomial t (1 + c1 t^2 + ... + c4 t^8), relative error at most 9e-8 (least maximum, fitted on Chebyshev points with the first coefficient held at 1).
+constexpr float kTanhMax = 0.6f, kTanh1 = -0.333325975f, kTanh2 = 0.133131167f, kTanh3 = -0.0522118075f, kTanh4 = 0.015612634f;
 struct Score {
-    float mul, cap2;             // cap2 = softcap * log2(e); 0 without a cap
+    float mul, cap2, tmul;       // cap2 = softcap * log2(e), 0 without a cap; tmul: the tanh's argument per score
     __device__ __forceinline__ Score(float scale, float softcap) {
-        mul = softcap > 0.f ? scale / softcap * (2.f * kLog2e) : scale * kLog2e;
+        tmul = softcap > 0.f ? scale / softcap : 0.f;
+        mul = softcap > 0.f ? tmul * (2.f * kLog2e) : scale * kLog2e;
         cap2 = softcap > 0.f ? softcap * kLog2e : 0.f;
     }
 };
@@ -45,10 +49,15 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float capped(float s, float mul, float cap2) {
+__device__ __forceinline__ float capped_near(float t, float cap2) {
+    const float u = t * t;
+    return t * cap2 * fmaf(fmaf(fmaf(fmaf(kTanh4, u, kTanh3), u, kTanh2), u, kTanh1), u, 1.f);
+}
+__device__ __forceinline__ float capped(float s, const Score& sc) {
     float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(s * mul)));
-    return fmaf(-2.f * r, cap2, cap2);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(s * sc.mul)));
+    const float t = s * sc.tmul;
+    return fabsf(t) <= kTanhMax ? capped_near(t, sc.cap2) : fmaf(-2.f * r, sc.cap2, sc.cap2);
 }
 
 // two fp32 lanes per instruction
@@ -78,9 +87,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-
-// tanh(t) = t (c0 + c1 t^2 + c2 t^4 + c3 t^6) for |t| <= 0.6, least maximum error 6e-7 (fitted to tanh on Chebyshev points)
-constexpr float kTanhMax = 0.6f, kTanh0 = 0.99999102f, kTanh1 = -0.33298974f, kTanh2 = 0.12974553f, kTanh3 = -0.03961126f;
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     __nv_bfloat162 h = __floats2bfloat162_rn(a, b);

@@ -212,13 +212,20 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
                 }
                 const bool masked = j0 + 15 > p_lo || j0 < all_from;
                 float x[NT][4];                                         // key g: rows c2, c2 + 1; key g + 8: rows c2, c2 + 1
-                bool raise = false;
+                bool raise = false, near = true;
+                if (sc.cap2 > 0.f) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) near &= fabsf((sv[nt][0][e] + sv[nt][1][e]) * sc.tmul) <= kTanhMax;
+                    near = __all_sync(0xffffffffu, near);
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         float v = sv[nt][0][e] + sv[nt][1][e];
-                        v = sc.cap2 > 0.f ? capped(v, sc.mul, sc.cap2) : v * sc.mul;
+                        v = sc.cap2 > 0.f ? near ? capped_near(v * sc.tmul, sc.cap2) : capped(v, sc) : v * sc.mul;
                         if (masked) {
                             const int j = j0 + g + (e >> 1) * 8;
                             if (j > see_hi[nt][e & 1] || j < see_lo[nt][e & 1]) v = -INFINITY;

@@ -187,7 +187,8 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     P.batch = cache->batch; P.q_heads = q_heads; P.kv_heads = cache->kv_heads; P.group = group;
     P.page_size = ps; P.page_shift = ps == 16 ? 4 : ps == 32 ? 5 : ps == 64 ? 6 : ps == 128 ? 7 : 8;
     P.tiles_per_seq = (int)p.tiles_per_seq; P.splits = (int)p.splits; P.split_keys = p.split_keys;
-    P.scale = scale; P.softcap = softcap;
+    // From 2^100 on a cap is none: it leaves scores below 2^88 as they are in fp32, and larger ones are further apart than any weight reaches either way.
+    P.scale = scale; P.softcap = softcap < 0x1p100f ? softcap : 0.f;
     P.part_o = static_cast<float*>(workspace);
     P.part_ml = reinterpret_cast<float2*>(P.part_o + (size_t)p.splits * T * q_heads * D);
     P.dev_status = dev_status;

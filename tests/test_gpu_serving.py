@@ -579,3 +579,22 @@ def test_attn_paged_rows_with_large_and_with_ordinary_scores(D, n, L, hint, expo
         q.flatten(0, 1)[::2].mul_(2.0 ** -(exponent + 3))
         q[1::3].mul_(2.0 ** -(exponent // 2))
     _check(*_attend([n], [L], 4, 2, D, 16, seed=54, scale=1.0, hints=(n, hint), edit=edit))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,L,hint", [(1, 60, 60), (4, 700, 700), (60, 300, 1 << 20), (140, 300, 300)])
+@pytest.mark.parametrize("cap", [0.5, 30.0, 300.0, 1e4, 1e5, 1e6, 1e8, 1e20, 3e38, float("inf")])
+def test_attn_paged_cap_of_any_size(D, n, L, hint, cap):
+    # a cap far above the scores leaves them as they are, to the precision of 32 bits: its tanh has to keep a relative accuracy
+    got, want, tol, status = _attend([n], [L], 4, 2, D, 16, seed=61, softcap=cap, hints=(n, hint), qstd=6.0)
+    if cap > 1e19:
+        got0, want, tol, _ = _attend([n], [L], 4, 2, D, 16, seed=61, hints=(n, hint), qstd=6.0)      # in 64 bits s / cap vanishes, or is NaN times infinity
+    _check(got, want, tol, status)
+
+
+@pytest.mark.parametrize("D,news", [(64, [140] * 20), (128, [140] * 20), (256, [60] * 20)])
+@pytest.mark.parametrize("cap", [100.0, 1e5, 1e7])
+def test_attn_paged_many_query_tiles_cap_of_any_size(D, news, cap):
+    lens = [n + 30 + 19 * i for i, n in enumerate(news)]
+    _check(*_attend(news, lens, 8, 2, D, 16, seed=62, softcap=cap, qstd=6.0))
+    _check(*_attend(news, lens, 8, 2, D, 16, seed=63, softcap=cap, qstd=600.0))           # scores past the cap, and up to a few hundred

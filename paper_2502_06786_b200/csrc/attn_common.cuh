@@ -103,7 +103,7 @@ __device__ __forceinline__ Sequence sequence(const Params& P, int b) {
     Sequence s;
     s.q0 = P.cu_q[b];
     s.n_new = P.cu_q[b + 1] - s.q0;
-    s.kv_len = P.kv_len[b];
+    s.kv_len = max(P.kv_len[b], 0);                                     // below zero no query sees a key either, and positions keep within 32 bits
     if (s.n_new > 0 && (s.q0 < 0 || s.q0 + s.n_new > P.T || s.kv_len > P.table_width * P.page_size)) {
         report(P.dev_status, MATQ_ERR_PAGE);
         s.n_new = 0;

@@ -598,3 +598,19 @@ def test_attn_paged_many_query_tiles_cap_of_any_size(D, news, cap):
     lens = [n + 30 + 19 * i for i, n in enumerate(news)]
     _check(*_attend(news, lens, 8, 2, D, 16, seed=62, softcap=cap, qstd=6.0))
     _check(*_attend(news, lens, 8, 2, D, 16, seed=63, softcap=cap, qstd=600.0))           # scores past the cap, and up to a few hundred
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,hint", [(1, 200), (3, 200), (60, 200), (60, 1 << 20), (300, 200)])
+@pytest.mark.parametrize("length", [-1, -5, -(1 << 31) + 400, -(1 << 31)])
+def test_attn_paged_lengths_below_zero_see_nothing(D, n, hint, length):
+    # as for padding: a sequence's length may be anything below its number of new tokens
+    news, lens = [n, n], [200 + n, 40 + n]
+    kc, vc, table = sr.make_cache(lens, 2, D, 16, 71)
+    q = torch.randn(2 * n, 4, D, generator=torch.Generator().manual_seed(72)).to(torch.bfloat16)
+    want, tol = sr.attn(q, kc, vc, table, [0, n, 2 * n], [0, lens[1]], D ** -0.5)
+    status = status_word()
+    out = mq.attn_paged(q.cuda(), kc.cuda(), vc.cuda(), table.cuda(), dev(np.array([0, n, 2 * n], np.int32)), dev(np.array([length, lens[1]], np.int32)), n, hint,
+                        dev_status=status)
+    assert int(host(status)[0]) == mq.OK and bool((out[:n] == 0).all())
+    assert bool(((out.cpu().double() - want).abs() <= tol).all())

@@ -94,8 +94,8 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const int64_t ctx = kv_len - n_new;                                 // position of the first new token (negative: it sees nothing)
 
     int it = 0, issued = 0;                                             // stages used so far by this CTA
-    int round = 0;
-    for (int64_t tile = bt - (int64_t)b * P.tiles_per_seq; tile < tiles; tile += P.tiles_per_seq, ++round) {
+    int round = 0;                                                      // tiles with keys so far: only those use the ring, and the barrier that hands it back
+    for (int64_t tile = bt - (int64_t)b * P.tiles_per_seq; tile < tiles; tile += P.tiles_per_seq) {
         const int64_t r0 = tile * kRows, r1 = min(r0 + kRows, n_rows) - 1;           // first and last row
         // Row r of position p sees the keys [lo(p), p].  Positions stay below kv_len, an int.
         const auto lo = [&](int64_t p) { return P.window && p - P.window + 1 > 0 ? (int)(p - P.window + 1) : 0; };
@@ -129,7 +129,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
                     rows_next = key < k_hi ? page_row(P, h, key, early_page) : (int)(P.n_pages * P.kv_heads * P.page_size);
                 }
             }
-            bool ok = round == 0 || tc::mbar_wait(tc::smem_u32(&s_tile), (uint32_t)(round - 1) & 1u, P.wait_cycles);
+            bool ok = n_it == 0 || round == 0 || tc::mbar_wait(tc::smem_u32(&s_tile), (uint32_t)(round - 1) & 1u, P.wait_cycles);
             ok = __all_sync(0xffffffffu, ok) && !P.hold;
             int s = it % C::kStages;
             uint32_t phase = (uint32_t)(it / C::kStages) & 1u;
@@ -153,6 +153,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
                 break;
             }
             it += n_it;
+            if (n_it > 0) ++round;
             continue;
         }
 
@@ -340,14 +341,17 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             *(volatile int*)&s_timeout = 1;
             break;
         }
+        // A tile without keys leaves the ring alone: the producers do not wait for such tiles and may be filling it for a later one.
         float* merge = reinterpret_cast<float*>(ring);
+        if (n_it > 0) {
 #pragma unroll
-        for (int t = 0; t < D / 16; ++t)
+            for (int t = 0; t < D / 16; ++t)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    merge[(size_t)(warp * kRows + nt * 8 + c2 + (e & 1)) * C::kMergeStride + t * 16 + g + (e >> 1) * 8] = o[t][nt][e];
+                    for (int e = 0; e < 4; ++e)
+                        merge[(size_t)(warp * kRows + nt * 8 + c2 + (e & 1)) * C::kMergeStride + t * 16 + g + (e >> 1) * 8] = o[t][nt][e];
+        }
         if (tid < kRows && r0 + tid <= r1) {
             float mx = s_m[0][tid];
 #pragma unroll
@@ -371,11 +375,13 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             const int64_t rr = r0 + r;
             if (rr > r1) break;
             float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (n_it > 0) {
 #pragma unroll
-            for (int w = 0; w < C::kWarps; ++w) {
-                const float4 v = *reinterpret_cast<const float4*>(merge + (size_t)(w * kRows + r) * C::kMergeStride + c);
-                const float f = s_f[w][r];
-                a.x = fmaf(v.x, f, a.x); a.y = fmaf(v.y, f, a.y); a.z = fmaf(v.z, f, a.z); a.w = fmaf(v.w, f, a.w);
+                for (int w = 0; w < C::kWarps; ++w) {
+                    const float4 v = *reinterpret_cast<const float4*>(merge + (size_t)(w * kRows + r) * C::kMergeStride + c);
+                    const float f = s_f[w][r];
+                    a.x = fmaf(v.x, f, a.x); a.y = fmaf(v.y, f, a.y); a.z = fmaf(v.z, f, a.z); a.w = fmaf(v.w, f, a.w);
+                }
             }
             const int64_t tok = rr / P.group;
             const int head = h * P.group + (int)(rr - tok * P.group);
@@ -389,7 +395,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("bar.sync 1, %0;" ::"n"(C::kSoft) : "memory");
-        if (lane == 0) tc::mbar_arrive(tc::smem_u32(&s_tile));
+        if (n_it > 0 && lane == 0) tc::mbar_arrive(tc::smem_u32(&s_tile));
     }
     // No copy may be in flight when the CTA ends.  Consumers that gave up may have left some: the producers wait for what they issued (each for
     // the whole stage; should the other have stopped before it, the wait ends at its limit, by when the copies have long landed).

@@ -614,3 +614,12 @@ def test_attn_paged_lengths_below_zero_see_nothing(D, n, hint, length):
                         dev_status=status)
     assert int(host(status)[0]) == mq.OK and bool((out[:n] == 0).all())
     assert bool(((out.cpu().double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("news,lens", [([300, 2], [300, 700]), ([400], [150]), ([257, 300], [900, 299])])
+def test_attn_paged_one_cta_walks_tiles_with_and_without_keys(D, news, lens):
+    # hints of one new token: a CTA takes all tiles of a sequence, and a part of the key range lies past the first ones (or they see no key at all)
+    for hint in (100000, 2000):
+        _check(*_attend(news, lens, 8, 2, D, 16, seed=81, hints=(1, hint), fill=float("nan")))
+        _check(*_attend(news, lens, 8, 2, D, 16, seed=82, hints=(4, hint), window=70, fill=float("nan")))

@@ -4,4 +4,4 @@
 ``synth`` holds the seeded synthetic inputs; ``build`` compiles the library;
 ``serve`` is a small decoder over the serving calls.
 """
-__all__ = ["binding", "synth", "build", "shard"]
+__all__ = ["binding", "synth", "build", "shard", "serve"]

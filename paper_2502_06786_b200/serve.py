@@ -69,13 +69,19 @@ class PagedCache:
 
     def extend(self, seq, n: int) -> None:
         """Makes room for n more tokens of a sequence."""
-        pages = self.pages.setdefault(seq, [])
-        length = self.length.get(seq, 0) + n
-        need = -(-length // self.page_size) - len(pages)
-        if need > len(self.free):
+        self.extend_all([(seq, n)])
+
+    def extend_all(self, steps) -> None:
+        """Makes room for (sequence, number of new tokens) pairs: for all of them, or, if the pages do not suffice, for none."""
+        length = {seq: self.length.get(seq, 0) + n for seq, n in steps}
+        if len(length) != len(steps):
+            raise ValueError("a sequence occurs twice")
+        need = {seq: -(-t // self.page_size) - len(self.pages.get(seq, ())) for seq, t in length.items()}
+        if sum(need.values()) > len(self.free):
             raise RuntimeError("the cache is full")
-        pages.extend(self.free.pop() for _ in range(need))
-        self.length[seq] = length
+        for seq, t in length.items():
+            self.pages.setdefault(seq, []).extend(self.free.pop() for _ in range(need[seq]))
+            self.length[seq] = t
 
     def release(self, seq) -> None:
         self.free.extend(reversed(self.pages.pop(seq)))
@@ -86,8 +92,7 @@ class Batch:
     """The device arrays that one step's calls share: (sequence, number of new tokens) pairs, their pages and lengths."""
 
     def __init__(self, cache: PagedCache, steps, device="cuda"):
-        for seq, n in steps:
-            cache.extend(seq, n)
+        cache.extend_all(steps)
         width = max(len(cache.pages[s]) for s, _ in steps)
         table = [cache.pages[s] + [-1] * (width - len(cache.pages[s])) for s, _ in steps]
         cu = [0]

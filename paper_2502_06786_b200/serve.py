@@ -130,6 +130,8 @@ class Decoder:
     def forward(self, x: torch.Tensor, cache: PagedCache, batch: Batch, dev_status=None) -> torch.Tensor:
         """x: bf16 [T, hidden], the new tokens of the batch's sequences one after another.  Returns bf16 [T, hidden]."""
         cfg, T = self.cfg, x.shape[0]
+        if batch.max_kv > cfg.max_pos:
+            raise ValueError(f"a sequence of {batch.max_kv} tokens passes the {cfg.max_pos} positions of the rotation table")
         paged = (batch.page_table, batch.cu_q, batch.kv_len)
         for i, l in enumerate(self.layers):
             q, k, v = apply([l["q"], l["k"], l["v"]], rms_norm(x))

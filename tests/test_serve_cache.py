@@ -1,5 +1,6 @@
 """The decoder example's page bookkeeping (host only)."""
 import pytest
+import torch
 
 from paper_2502_06786_b200 import serve
 
@@ -47,3 +48,13 @@ def test_batch_arrays():
     assert b.kv_len.tolist() == [17, 21] and len(c.pages["b"]) == 2 and len(c.pages["a"]) == 2
     with pytest.raises(ValueError):
         serve.Batch(c, [("a", 1), ("a", 1)], device="cpu")
+
+
+def test_positions_past_the_rotation_table_are_refused_before_anything_runs():
+    model = serve.Decoder.__new__(serve.Decoder)                # no weights: refused before they are needed
+    model.cfg, model.layers, model.cos_sin = serve.Config(max_pos=30), [], None
+    c = _cache()
+    x = torch.zeros(30, 512, dtype=torch.bfloat16)
+    assert model.forward(x, c, serve.Batch(c, [("a", 30)], device="cpu")).shape == (30, 512)
+    with pytest.raises(ValueError, match="30 positions"):
+        model.forward(x[:1], c, serve.Batch(c, [("a", 1)], device="cpu"))

@@ -74,6 +74,14 @@ double number(PyObject* o, const char* name) {
     if (v == -1.0 && PyErr_Occurred()) { PyErr_Clear(); fail(PyExc_TypeError, name, "a number is required"); }
     return v;
 }
+// Other Python threads run meanwhile: a launch waits while the stream's queue is full.  Nothing of Python is touched by f.
+template <typename F>
+int unlocked(F f) {
+    PyThreadState* state = PyEval_SaveThread();
+    const int st = f();
+    PyEval_RestoreThread(state);
+    return st;
+}
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 
 struct Paged {
@@ -122,8 +130,10 @@ PyObject* quantize_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 5, [&] {
         const Matrix x = mat(a[0], at::kBFloat16, "X"), o = mat(a[1], at::kChar, "xq");
         if (o.rows != x.rows || o.cols != x.cols) fail(PyExc_ValueError, "xq", "int8 [M, K] required");
-        return matq_quantize_tokens(x.p, x.rows, x.cols, x.ld, static_cast<int8_t*>(o.p), o.ld, vec<float>(a[2], at::kFloat, "scale", x.rows),
-                                    vec<int32_t>(a[3], at::kInt, "rowsum", x.rows), status_word(a[4]), stream());
+        float* scale = vec<float>(a[2], at::kFloat, "scale", x.rows);
+        int32_t *rowsum = vec<int32_t>(a[3], at::kInt, "rowsum", x.rows), *status = status_word(a[4]);
+        void* s = stream();
+        return unlocked([&] { return matq_quantize_tokens(x.p, x.rows, x.cols, x.ld, static_cast<int8_t*>(o.p), o.ld, scale, rowsum, status, s); });
     });
 }
 
@@ -135,10 +145,16 @@ PyObject* gemm_a8(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const bool bf16 = THPVariable_Check(a[6]) && THPVariable_Unpack(a[6]).scalar_type() == at::kBFloat16;
         const Matrix y = mat(a[6], bf16 ? at::kBFloat16 : at::kFloat, "y");
         if (y.rows != x.rows || y.cols != w.rows) fail(PyExc_ValueError, "y", "[M, N] required");
-        return matq_gemm_a8(static_cast<const int8_t*>(x.p), x.rows, x.cols, x.ld, vec<float>(a[1], at::kFloat, "scale", x.rows),
-                            vec<int32_t>(a[2], at::kInt, "rowsum", x.rows), static_cast<const uint8_t*>(w.p), w.rows, w.ld, small_integer(a[9], "c"),
-                            vec<float>(a[4], at::kFloat, "alpha", w.rows), vec<float>(a[5], at::kFloat, "zero", w.rows),
-                            bf16 ? MATQ_OUT_BF16 : MATQ_OUT_F32, y.p, y.ld, (unsigned)small_integer(a[7], "flags"), status_word(a[8]), stream());
+        const float *scale = vec<float>(a[1], at::kFloat, "scale", x.rows), *alpha = vec<float>(a[4], at::kFloat, "alpha", w.rows),
+                    *zero = vec<float>(a[5], at::kFloat, "zero", w.rows);
+        const int32_t* rowsum = vec<int32_t>(a[2], at::kInt, "rowsum", x.rows);
+        const int flags = small_integer(a[7], "flags"), c = small_integer(a[9], "c");
+        int32_t* status = status_word(a[8]);
+        void* s = stream();
+        return unlocked([&] {
+            return matq_gemm_a8(static_cast<const int8_t*>(x.p), x.rows, x.cols, x.ld, scale, rowsum, static_cast<const uint8_t*>(w.p), w.rows, w.ld, c, alpha, zero,
+                                bf16 ? MATQ_OUT_BF16 : MATQ_OUT_F32, y.p, y.ld, (unsigned)flags, status, s);
+        });
     });
 }
 
@@ -163,8 +179,11 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         const int inter = PyObject_IsTrue(a[10]);
         if (inter < 0) { PyErr_Clear(); fail(PyExc_TypeError, "interleaved", "a truth value is required"); }
-        return matq_kv_append(&p.c, k.T, q.p, (int)q.H, q.ld, k.p, k.ld, v.p, v.ld, static_cast<const float*>(cs.p), cs.rows, (int)cs.cols, inter,
-                              o.p, o.ld, status_word(a[11]), stream());
+        int32_t* status = status_word(a[11]);
+        void* s = stream();
+        return unlocked([&] {
+            return matq_kv_append(&p.c, k.T, q.p, (int)q.H, q.ld, k.p, k.ld, v.p, v.ld, static_cast<const float*>(cs.p), cs.rows, (int)cs.cols, inter, o.p, o.ld, status, s);
+        });
     });
 }
 
@@ -183,8 +202,11 @@ PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
             ws = t.data_ptr();
             bytes = t.nbytes();
         }
-        return matq_attn_paged(&p.c, q.T, q.p, (int)q.H, q.ld, (float)number(a[8], "scale"), (float)number(a[9], "softcap"), integer(a[10], "window"),
-                               integer(a[6], "max_q"), integer(a[7], "max_kv"), o.p, o.ld, ws, bytes, status_word(a[13]), stream());
+        const float scale = (float)number(a[8], "scale"), softcap = (float)number(a[9], "softcap");
+        const int64_t window = integer(a[10], "window"), max_q = integer(a[6], "max_q"), max_kv = integer(a[7], "max_kv");
+        int32_t* status = status_word(a[13]);
+        void* s = stream();
+        return unlocked([&] { return matq_attn_paged(&p.c, q.T, q.p, (int)q.H, q.ld, scale, softcap, window, max_q, max_kv, o.p, o.ld, ws, bytes, status, s); });
     });
 }
 

@@ -1,4 +1,7 @@
 """The decoder example: its steps against the same steps in 64 bits, and one prompt cut in different ways."""
+import threading
+import time
+
 import pytest
 import torch
 
@@ -93,3 +96,30 @@ def test_cache_refuses_what_does_not_fit():
 def test_example_runs(capsys):
     serve.main()
     assert capsys.readouterr().out.startswith("ok")
+
+
+def test_other_python_threads_run_while_a_call_waits_for_the_launch_queue():
+    # A launch blocks while the stream's queue is full.  The queue is filled behind a kernel that takes about 0.3 s; another thread keeps time meanwhile.
+    x = torch.randn(1, 64, device="cuda").to(torch.bfloat16)
+    out = mq.quantize_tokens(x)
+    torch.cuda.synchronize()
+    stop, ticks = threading.Event(), []
+
+    def keep_time():
+        while not stop.is_set():
+            ticks.append(time.perf_counter())
+            time.sleep(0.001)
+    t = threading.Thread(target=keep_time)
+    t.start()
+    time.sleep(0.02)
+    torch.cuda._sleep(500_000_000)                              # clock cycles
+    begin = time.perf_counter()
+    for _ in range(3000):
+        mq.quantize_tokens(x, *out)
+    blocked = time.perf_counter() - begin
+    stop.set()
+    t.join()
+    torch.cuda.synchronize()
+    gaps = [b - a for a, b in zip(ticks, ticks[1:]) if b >= begin]
+    assert blocked > 0.1, "the queue did not fill: nothing was tested"
+    assert max(gaps) < 0.5 * blocked, (blocked, max(gaps))

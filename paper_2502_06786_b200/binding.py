@@ -122,7 +122,22 @@ def _load():
 
 _lib = _load()
 
-from . import _serving  # noqa: E402  (the serving calls' argument checks, in C++; built beside the library)
+
+class _NotBuilt:
+    """Stands for the module of the serving calls where it cannot be loaded: the other calls need libmatq.so only."""
+
+    def __init__(self, why: ImportError):
+        self._why = why
+
+    def __getattr__(self, name):
+        raise ImportError(f"{name} needs the module _serving, which is built beside libmatq.so with g++ and torch's headers "
+                          f"(python -m paper_2502_06786_b200.build): {self._why}") from self._why
+
+
+try:
+    from . import _serving  # noqa: E402  (the serving calls' argument checks, in C++)
+except ImportError as e:
+    _serving = _NotBuilt(e)
 
 
 def lib_path() -> str:

@@ -1,5 +1,10 @@
 """Builds the CUDA library in-tree with nvcc for sm_100a, and beside it the small C++ module through which Python makes the
-serving calls (g++, torch's headers).  No JIT cache."""
+serving calls (g++, torch's headers).  No JIT cache.
+
+    python -m paper_2502_06786_b200.build [--force] [-v] [--library-only]
+
+With --library-only (``build_library(serving=False)``) the module is left out: the C ABI and all other Python calls work without it.
+"""
 from __future__ import annotations
 
 import os
@@ -17,16 +22,17 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr", "-Wno-deprecated-gpu-targets"]
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(MODULE):
+def _stale(serving: bool = True) -> bool:
+    made = [LIB, MODULE] if serving else [LIB]
+    if not all(os.path.exists(f) for f in made):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(MODULE))
+    t = min(os.path.getmtime(f) for f in made)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "matq.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
-def build_library(force: bool = False, verbose: bool = False) -> str:
-    if not force and not _stale():
+def build_library(force: bool = False, verbose: bool = False, serving: bool = True) -> str:
+    if not force and not _stale(serving):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     objs = []
@@ -49,7 +55,8 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     if failed:
         raise RuntimeError("nvcc failed")
     subprocess.run([nvcc, "-shared", "-o", LIB, *objs, "-cudart", "static"], check=True)
-    build_module(nvcc)
+    if serving:
+        build_module(nvcc)
     return LIB
 
 
@@ -72,4 +79,4 @@ def build_module(nvcc: str) -> str:
 
 
 if __name__ == "__main__":
-    print(build_library(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_library(force="--force" in sys.argv, verbose="-v" in sys.argv, serving="--library-only" not in sys.argv))

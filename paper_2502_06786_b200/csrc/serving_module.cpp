@@ -6,6 +6,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <optional>
 #include <string>
 
 #include "matq.h"
@@ -18,10 +19,12 @@ struct Bad {
 };
 [[noreturn]] void fail(PyObject* type, const char* name, const char* what) { throw Bad{type, std::string(name) + ": " + what}; }
 
-const at::Tensor& tensor(PyObject* o, at::ScalarType type, const char* name) {
+// a CUDA tensor on the current device, whose stream the call uses; of one type, if that matters (std::nullopt: any)
+const at::Tensor& tensor(PyObject* o, std::optional<at::ScalarType> type, const char* name) {
     if (!THPVariable_Check(o)) fail(PyExc_TypeError, name, "expected a CUDA tensor");
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.is_cuda() || t.scalar_type() != type) fail(PyExc_TypeError, name, (std::string("expected a CUDA tensor of dtype ") + c10::toString(type)).c_str());
+    if (!t.is_cuda() || (type && t.scalar_type() != *type))
+        fail(PyExc_TypeError, name, (std::string("expected a CUDA tensor") + (type ? std::string(" of dtype ") + c10::toString(*type) : "")).c_str());
     if (t.get_device() != c10::cuda::current_device()) fail(PyExc_ValueError, name, "on another device than the current one, whose stream the call would use");
     return t;
 }
@@ -197,8 +200,8 @@ PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* ws = nullptr;
         size_t bytes = 0;
         if (a[12] != Py_None) {
-            if (!THPVariable_Check(a[12]) || !THPVariable_Unpack(a[12]).is_cuda() || !THPVariable_Unpack(a[12]).is_contiguous()) fail(PyExc_TypeError, "workspace", "a contiguous CUDA tensor is required");
-            const at::Tensor& t = THPVariable_Unpack(a[12]);
+            const at::Tensor& t = tensor(a[12], std::nullopt, "workspace");
+            if (!t.is_contiguous()) fail(PyExc_TypeError, "workspace", "a contiguous tensor is required");
             ws = t.data_ptr();
             bytes = t.nbytes();
         }

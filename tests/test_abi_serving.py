@@ -1,5 +1,7 @@
 """Refusals of the serving entry points: found on the host, before anything is launched (no GPU needed)."""
 import ctypes as C
+import os
+import re
 
 import pytest
 import torch
@@ -146,3 +148,11 @@ def test_gemm_a8_has_a_kernel_for_every_size_it_accepts():
                         (1, 1, 24, mq.ERR_SHAPE), (1, 1, 65552, mq.ERR_SHAPE), (1 << 31, 1, 16, mq.ERR_SHAPE), (1, 1 << 31, 16, mq.ERR_SHAPE)):
         assert lib.matq_gemm_a8_plan(M, N, K, NULL, NULL, NULL) == st, (M, N, K)
     assert lib.matq_gemm_a8_plan(1, 1, 16, NULL, NULL, NULL) == mq.OK
+
+
+def test_one_function_of_the_serving_module_looks_at_the_device_of_every_tensor():
+    # that a tensor of another device is refused cannot be shown with one GPU or none, so the source is read: no argument becomes a pointer around tensor()
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2502_06786_b200", "csrc", "serving_module.cpp")
+    text = open(path).read()
+    assert text.count("is_cuda()") == 1 and text.count("current_device()") == 1
+    assert re.findall(r"(\w+)?\(?THPVariable_Unpack\(\w+(?:\[\d+\])?\)(\.\w+)?", text) == [("", ""), ("", ".scalar_type")]

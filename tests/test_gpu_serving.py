@@ -623,3 +623,20 @@ def test_attn_paged_one_cta_walks_tiles_with_and_without_keys(D, news, lens):
     for hint in (100000, 2000):
         _check(*_attend(news, lens, 8, 2, D, 16, seed=81, hints=(1, hint), fill=float("nan")))
         _check(*_attend(news, lens, 8, 2, D, 16, seed=82, hints=(4, hint), window=70, fill=float("nan")))
+
+
+def test_attn_paged_workspaces_that_do_not_fit_are_refused():
+    kc, vc, table = sr.make_cache([5000], 2, 64, 16, 91)
+    q = torch.randn(1, 4, 64).to(torch.bfloat16).cuda()
+    args = (q, kc.cuda(), vc.cuda(), table.cuda(), dev(np.array([0, 1], np.int32)), dev(np.array([5000], np.int32)), 1, 5000)
+    need = mq.attn_paged_workspace_bytes(1, 1, 4, 2, 64, 1, 5000)
+    assert need > 0
+    for bad, error in ((torch.empty(need, dtype=torch.uint8), TypeError), (np.empty(need, np.uint8), TypeError), (torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2], TypeError)):
+        with pytest.raises(error, match="workspace"):
+            mq.attn_paged(*args, workspace=bad)
+    for size, start, status in ((need - 1, 0, mq.ERR_WORKSPACE), (need, 8, mq.ERR_ALIGNMENT)):
+        with pytest.raises(mq.MatqError) as e:
+            mq.attn_paged(*args, workspace=torch.empty(need + 16, dtype=torch.uint8, device="cuda")[start:start + size])
+        assert e.value.status == status
+    a = mq.attn_paged(*args, workspace=torch.empty(need // 4, dtype=torch.float32, device="cuda"))
+    assert torch.equal(a, mq.attn_paged(*args))

@@ -399,8 +399,8 @@ enum matq_out_type { MATQ_OUT_F32 = 0, MATQ_OUT_BF16 = 1 };
  *                     precision (matq_slice_pack's sliced_unpacked; dequantisation is alpha * (S - z) either way)
  *   alpha, zero  in   fp32 [N]
  *   Y            out  fp32 or bf16 [M, N], row stride ldy elements
- *   flags        0 or MATQ_GEMV_PDL (the previous kernel of the stream writes neither q nor alpha nor zero: the kernel then
- *                     starts fetching weights before that kernel has ended, as in matq_gemv)
+ *   flags        0 or MATQ_GEMV_PDL (the previous kernel of the stream writes neither q nor alpha nor zero: the kernel may then
+ *                     start fetching weights before that kernel has ended, as in matq_gemv; the kernel for many tokens does not)
  *   c must be 8.  Requires K % 16 == 0, 16 <= K <= 65536, ldxq % 16 == 0, ldw % 16 == 0, xq and q 16-byte aligned, M and N below 2^31
  *   (MATQ_ERR_SHAPE where both are so large that ceil(M / 256) * ceil(N / 256) reaches 2^30); M or N may be 0.  A device-side wait that runs out sets dev_status = MATQ_ERR_TIMEOUT; Y is then unspecified.
  */
@@ -428,10 +428,10 @@ typedef struct matq_paged_kv {
     int64_t n_pages;
     int page_size, kv_heads, head_dim;
     int batch;                   /* sequences */
-    const int32_t *page_table;   /* int32 [batch, table_width], rows table_stride entries apart; entries past a sequence's last page are not read */
+    const int32_t *page_table;   /* int32 [batch, table_width], rows table_stride entries apart; entries past a sequence's last page may hold anything (they may be fetched, but are not used) */
     int64_t table_stride, table_width;
     const int32_t *cu_q;         /* int32 [batch + 1], cu_q[0] = 0, ascending; a sequence may have no new token */
-    const int32_t *kv_len;       /* int32 [batch]: keys per sequence, the new tokens included */
+    const int32_t *kv_len;       /* int32 [batch]: keys per sequence, the new tokens included; (9) takes a length below zero for zero */
 } matq_paged_kv;
 
 /*
@@ -461,10 +461,11 @@ int matq_kv_append(const matq_paged_kv *cache, int64_t T, const void *q, int q_h
  *     are fp32; the weights are rounded to bf16 for the product with v.  Keys outside J contribute nothing whatever the cache holds there (NaN and Inf
  *     included).  A query with empty J (kv_len smaller than the number of new tokens, as for padding) gives zeros.
  *   q       in   bf16 [T, q_heads, head_dim], token stride ldq;  out  bf16 likewise, ldo.  Rows from cu_q[batch] on are left alone.
- *   scale > 0, softcap >= 0 (0 = none), window >= 0 (0 = every earlier key)
+ *   scale > 0, softcap >= 0 (0, or from 2^100 on = none), window >= 0 (0 = every earlier key)
  *   max_q, max_kv   upper bounds of n_b and kv_len[b] that the caller knows on the host.  They choose the kernel and the split over
  *           keys; values that are too small cost time, not correctness.
- *   workspace   at least matq_attn_paged_workspace_bytes(...) bytes, 16-byte aligned; contents need not be initialised
+ *   workspace   at least matq_attn_paged_workspace_bytes(...) bytes for this call's sizes, 16-byte aligned; contents need not be initialised.  Smaller calls can
+ *           need more: few tokens over a long range are split into more parts.  A buffer for several calls takes the largest of their sizes.
  *   Requires head_dim in {64, 128, 256}, page_size in {16, 32, 64, 128, 256}, q_heads a multiple of kv_heads with at most 64 query heads per
  *   key head, 16-byte aligned pointers, strides multiples of 8, n_pages * kv_heads * page_size < 2^31.
  *   Data errors set dev_status: MATQ_ERR_PAGE (the affected sequence's outputs are unspecified, no memory outside the cache is read) or

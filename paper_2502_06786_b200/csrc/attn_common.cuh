@@ -13,6 +13,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 // then, and a step done again for one row costs its whole warp: 8192 tokens over 8192 at 32/8 x 128 heads took 1.98 ms.)
 constexpr float kFar = 32.f;
 
+// The weights 2^x are rounded to bf16 for the product with v, as v and the outputs are: that is what the tensor cores take beside bf16 values, and half the
+// registers and tensor memory of fp32.  Each is off by 2^-8 of itself at most, so an output by 2^-8 of sum_j p_j |v_j|; their sum is taken before the rounding.
+// Against 64 bits the outputs of 64 ragged tokens (500 over 6511) are off by 2.1e-3 (2.3e-3) of their norm, of which rounding the outputs is 1.7e-3.
+
 struct Params {
     const __nv_bfloat16 *q, *v;
     __nv_bfloat16* out;

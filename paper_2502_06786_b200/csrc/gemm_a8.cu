@@ -152,7 +152,7 @@ inline cudaError_t launch_few(const uint8_t* q, int64_t ldw, const int8_t* xq, i
 // A CTA sums 128 channels x nt tokens over a part of K in tensor memory; the CTAs of a cluster hold the same tile for different parts, put their sums into
 // shared memory and finish every splits-th token each, reading the others' sums from there.  Tiles of up to 64 tokens leave room for two CTAs per SM.
 // Eight warps store, as in the pair kernel (with four, one token tile of 128 took 6 us to store).
-// From HBM, with MATQ_GEMV_PDL and without: 64 x 14336 x 4096 11.9 and 13.2 us (4.9 and 4.4 TB/s of codes), 37 x 2304 x 9216 8.8 and 9.5 us, of which the copies
+// From HBM, with MATQ_GEMV_PDL and without: 64 x 14336 x 4096 12.4 and 13.6 us (4.7 and 4.3 TB/s of codes), 37 x 2304 x 9216 8.7 and 9.3 us, of which the copies
 // take 3.3; the rest is the start of a launch, the join and the stores.
 constexpr int kSplitWarps = 8, kSplitThreads = 32 * (2 + kSplitWarps);
 // A stage is 256 bytes of K here too (with 128, 600 tokens through 2304 x 9216 took 23 us instead of 19, 17 through 10587 x 11072 24 instead of 23).

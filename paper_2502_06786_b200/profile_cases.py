@@ -92,7 +92,7 @@ def main(which: str) -> None:
         for _ in range(3):
             mq.gemm_multi(mq.SRC_CODES8, q, K2, X, alpha=a, zero=a, Ys=Ys, workspace=ws)
     elif which == "linear":
-        # the linear layer on the codes themselves: one token, 64 and 1024 tokens (few-token, split and pair kernel)
+        # the linear layer on the codes themselves: one token, 64 and 1024 tokens (split kernel with tiles of 16 and 64 tokens, pair kernel)
         N2, K2 = 14336, 4096
         qs = [torch.randint(0, 256, (N2, K2), dtype=torch.uint8, device="cuda") for _ in range(4)]
         a = torch.full((N2,), 1e-3, device="cuda")

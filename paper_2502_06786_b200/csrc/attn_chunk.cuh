@@ -419,9 +419,10 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 };
                 // A row without a reference (m = -inf) takes 0 for one if its largest score is not far from it, as ordinary scores are not: then its first
                 // step is not done twice.  A row with a large one always has its scores looked at once more.
+                // (Rows of the tile that stand for no query hold whatever shared memory held: they ask for nothing.)
                 bool lifted = false;
                 const auto wants = [&] {
-                    return ok && (top > kFar || (m == -INFINITY && top < -kFar && top > -INFINITY) || (!lifted && fabsf(use) >= kLarge));
+                    return ok && see_hi >= 0 && (top > kFar || (m == -INFINITY && top < -kFar && top > -INFINITY) || (!lifted && fabsf(use) >= kLarge));
                 };
                 if (ok) tc::fence_after();
                 for (int attempt = 0; attempt < 3; ++attempt) {         // the second suffices: nothing lies far above a reference that was just moved

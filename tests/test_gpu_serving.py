@@ -640,3 +640,33 @@ def test_attn_paged_workspaces_that_do_not_fit_are_refused():
         assert e.value.status == status
     a = mq.attn_paged(*args, workspace=torch.empty(need // 4, dtype=torch.float32, device="cuda"))
     assert torch.equal(a, mq.attn_paged(*args))
+
+
+def test_attn_paged_rows_that_stand_for_no_query_cost_nothing():
+    # Groups of 5 and 7 leave rows of a query tile empty: they hold what the kernel before left in shared memory.  Behind a product of huge numbers a call takes
+    # as long as behind one of ordinary numbers, and gives the same.
+    def time_of(fill, q, kc, vc, table, cu, lens, n, L, ws):
+        a = torch.full((4096, 4096), fill, device="cuda", dtype=torch.bfloat16)
+        b = torch.empty_like(a)
+        out, times = torch.empty_like(q), []
+        for _ in range(9):
+            torch.matmul(a, a, out=b)
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            mq.attn_paged(q, kc, vc, table, cu, lens, n, L, out=out, workspace=ws)
+            end.record()
+            torch.cuda.synchronize()
+            times.append(start.elapsed_time(end))
+        return sorted(times)[4], out
+    for D, Hkv, G, n, L in ((128, 8, 5, 1000, 3000), (64, 4, 7, 2000, 4000)):
+        pages = -(-L // 16)
+        kc = torch.randn(pages, Hkv, 16, D, device="cuda").to(torch.bfloat16)
+        vc = torch.randn_like(kc)
+        table = torch.randperm(pages, device="cuda").to(torch.int32)[None]
+        cu, lens = dev(np.array([0, n], np.int32)), dev(np.array([L], np.int32))
+        q = torch.randn(n, Hkv * G, D, device="cuda").to(torch.bfloat16)
+        ws = torch.empty(mq.attn_paged_workspace_bytes(n, 1, Hkv * G, Hkv, D, n, L) + 16, dtype=torch.uint8, device="cuda")
+        t1, o1 = time_of(1.0, q, kc, vc, table, cu, lens, n, L, ws)
+        t2, o2 = time_of(1e30, q, kc, vc, table, cu, lens, n, L, ws)
+        assert torch.equal(o1, o2)
+        assert t2 < 1.4 * t1, (t1, t2)

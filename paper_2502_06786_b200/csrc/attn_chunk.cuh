@@ -377,7 +377,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                             float big = 0.f;
 #pragma unroll
                             for (int e = 0; e < 32; e += 2) big = max3(big, fabsf(__uint_as_float(v[e])), fabsf(__uint_as_float(v[e + 1])));
-                            if (__any_sync(0xffffffffu, !(big * sc.tmul <= t_max))) {       // some score is past the polynomial's range
+                            if (__any_sync(0xffffffffu, see_hi >= 0 && !(big * sc.tmul <= t_max))) {       // some score of a query is past the polynomial's range
 #pragma unroll
                                 for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(capped(__uint_as_float(v[e]), sc) + off);
                             } else {

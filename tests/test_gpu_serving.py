@@ -642,7 +642,8 @@ def test_attn_paged_workspaces_that_do_not_fit_are_refused():
     assert torch.equal(a, mq.attn_paged(*args))
 
 
-def test_attn_paged_rows_that_stand_for_no_query_cost_nothing():
+@pytest.mark.parametrize("cap", [0.0, 50.0])
+def test_attn_paged_rows_that_stand_for_no_query_cost_nothing(cap):
     # Groups of 5 and 7 leave rows of a query tile empty: they hold what the kernel before left in shared memory.  Behind a product of huge numbers a call takes
     # as long as behind one of ordinary numbers, and gives the same.
     def time_of(fill, q, kc, vc, table, cu, lens, n, L, ws):
@@ -653,7 +654,7 @@ def test_attn_paged_rows_that_stand_for_no_query_cost_nothing():
             torch.matmul(a, a, out=b)
             start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
             start.record()
-            mq.attn_paged(q, kc, vc, table, cu, lens, n, L, out=out, workspace=ws)
+            mq.attn_paged(q, kc, vc, table, cu, lens, n, L, softcap=cap, out=out, workspace=ws)
             end.record()
             torch.cuda.synchronize()
             times.append(start.elapsed_time(end))

@@ -57,11 +57,15 @@ __device__ __forceinline__ float capped_near(float t, float cap2) {
     const float u = t * t;
     return t * cap2 * fmaf(fmaf(fmaf(fmaf(kTanh4, u, kTanh3), u, kTanh2), u, kTanh1), u, 1.f);
 }
-__device__ __forceinline__ float capped(float s, const Score& sc) {
+__device__ __forceinline__ float capped_far(float s, const Score& sc) {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(s * sc.mul)));
+    return fmaf(-2.f * r, sc.cap2, sc.cap2);
+}
+// (equal to capped_near() where that applies: callers may take either)
+__device__ __forceinline__ float capped(float s, const Score& sc) {
     const float t = s * sc.tmul;
-    return fabsf(t) <= kTanhMax ? capped_near(t, sc.cap2) : fmaf(-2.f * r, sc.cap2, sc.cap2);
+    return fabsf(t) <= kTanhMax ? capped_near(t, sc.cap2) : capped_far(s, sc);
 }
 
 // two fp32 lanes per instruction

@@ -671,3 +671,17 @@ def test_attn_paged_rows_that_stand_for_no_query_cost_nothing(cap):
         t2, o2 = time_of(1e30, q, kc, vc, table, cu, lens, n, L, ws)
         assert torch.equal(o1, o2)
         assert t2 < 1.4 * t1, (t1, t2)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("cap,window", [(0.0, 0), (30.0, 0), (30.0, 37)])
+@pytest.mark.parametrize("n,L,hint", [(1, 59, 59), (3, 700, 700), (9, 29, 29), (9, 409, 1 << 20), (60, 500, 1 << 20), (140, 300, 300), (700, 1003, 1003)])
+def test_attn_paged_does_not_depend_on_what_the_cache_holds_elsewhere(D, cap, window, n, L, hint):
+    # not in the last bit: slots past a sequence's end and pages of nobody hold zeros, noise, huge numbers, infinities or NaN
+    first = None
+    for fill in (0.0, None, 1e30, -1e30, float("inf"), float("nan")):
+        got, want, tol, status = _attend([n], [L], 4, 2, D, 16, seed=95, softcap=cap, window=window, hints=(n, hint), fill=fill)
+        if first is None:
+            first = got
+            _check(got, want, tol, status)
+        assert torch.equal(got, first), fill

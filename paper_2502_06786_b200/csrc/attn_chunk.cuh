@@ -27,12 +27,10 @@
 namespace matq {
 namespace attn {
 
-// A reference of this size (in exponents of two) is not the sum of the old one and a distance to it, whose rounding would pass many exponents, but the row's
-// largest score itself, looked up again; and it is taken off the scores before they are multiplied, because the fused product keeps what the
-// rounding of the reference left out (half of 2^-23 of it: above 2^30 more than kFar, and weights were Inf or all zero).
-constexpr float kLarge = 16777216.f;
+// A reference of kLarge or more is not the sum of the old one and a distance to it, whose rounding would pass many exponents, but the row's largest score itself, looked
+// up again; and it is taken off the scores before they are multiplied (fused) or, with the cap, off rounded values.
 // The cap's tanh with one coefficient less than in capped(): relative error 2.6e-6, so at most 1e-3 of an exponent for caps up to kShortCap, half of what a weight's
-// rounding to bf16 is.  Larger caps, and scores past kTanhMax of one, go score by score: 500 tokens over 6511, 16/8 heads of 256, 57 us below and 88 above.
+// rounding to bf16 is.  Larger caps, and scores past kTanhMax of one, go score by score: 500 tokens over 6511, 16/8 heads of 256, 58 us below and 110 above.
 constexpr float kShortCap = 512.f, kShort1 = -0.333190745f, kShort2 = 0.130864184f, kShort3 = -0.0413877882f;
 constexpr int kMaxMasked = 16;          // tiles at a range's ends that some row does not see in full
 
@@ -321,8 +319,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
             const uint32_t o_addr = lane_addr + C::kTmemO + t * D;
             const Score sc(P.scale, P.softcap);
-            const bool low = P.softcap <= kShortCap;                    // with the cap: the short polynomial's coefficients, or those of capped()
-            const float tanh1 = (low ? kShort1 : kTanh1) * sc.cap2, tanh2 = (low ? kShort2 : kTanh2) * sc.cap2, tanh3 = (low ? kShort3 : kTanh3) * sc.cap2, t_max = low ? kTanhMax : -1.f;
+            const float tanh1 = kShort1 * sc.cap2, tanh2 = kShort2 * sc.cap2, tanh3 = kShort3 * sc.cap2, t_max = P.softcap <= kShortCap ? kTanhMax : -1.f;   // with the cap
             const float unit = CAP ? 1.f : sc.mul;                      // the reference is kept as a score; with the cap, as an exponent
             float m = -INFINITY, l = 0.f;
             bool ok = true;
@@ -379,13 +376,17 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 #pragma unroll
                             for (int e = 0; e < 32; e += 2) big = max3(big, fabsf(__uint_as_float(v[e])), fabsf(__uint_as_float(v[e + 1])));
                             if (__any_sync(0xffffffffu, see_hi >= 0 && !(big * sc.tmul <= t_max))) {       // some score of a query is past the polynomial's range
+                                if (t_max < 0.f) {
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) {
-                                    // Scores in the polynomial's range get what it gives them below (a last coefficient of zero changes no bit): no score depends on
-                                    // its neighbours, nor on what the cache holds where nobody looks.
-                                    const float s = __uint_as_float(v[e]), t = s * sc.tmul, u = t * t;
-                                    const float p = fmaf(fmaf(fmaf(fmaf(t_max > 0.f ? 0.f : kTanh4 * sc.cap2, u, tanh3), u, tanh2), u, tanh1), u, sc.cap2);
-                                    v[e] = __float_as_uint(fabsf(t) <= kTanhMax ? fmaf(t, p, off) : capped_far(s, sc) + off);
+                                    for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(capped(__uint_as_float(v[e]), sc) + off);
+                                } else {
+                                    // Scores in the polynomial's range get what it gives them below: no score depends on its neighbours, nor on what
+                                    // the cache holds where nobody looks.
+#pragma unroll
+                                    for (int e = 0; e < 32; ++e) {
+                                        const float s = __uint_as_float(v[e]), t = s * sc.tmul, u = t * t;
+                                        v[e] = __float_as_uint(fabsf(t) <= kTanhMax ? fmaf(t, fmaf(fmaf(fmaf(u, tanh3, tanh2), u, tanh1), u, sc.cap2), off) : capped_far(s, sc) + off);
+                                    }
                                 }
                             } else {
                                 const uint64_t tm2 = pair(sc.tmul, sc.tmul);

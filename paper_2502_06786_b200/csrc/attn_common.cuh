@@ -55,13 +55,17 @@ __device__ __forceinline__ float ex2(float x) {
 }
 __device__ __forceinline__ float capped_near(float t, float cap2) {
     const float u = t * t;
-    return t * cap2 * fmaf(fmaf(fmaf(fmaf(kTanh4, u, kTanh3), u, kTanh2), u, kTanh1), u, 1.f);
+    return __fmul_rn(t * cap2, fmaf(fmaf(fmaf(fmaf(kTanh4, u, kTanh3), u, kTanh2), u, kTanh1), u, 1.f));       // rounded: see kLarge
 }
 __device__ __forceinline__ float capped_far(float s, const Score& sc) {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(s * sc.mul)));
     return fmaf(-2.f * r, sc.cap2, sc.cap2);
 }
+// A value is rounded before a reference is taken off it, here and without a cap: a product fused with that difference would keep what the rounding of the
+// reference, itself such a value, left out.  From kLarge on (in exponents of two) that passes many exponents, above 2^30 more than kFar, and weights
+// would be Inf or all zero.
+constexpr float kLarge = 16777216.f;
 // (equal to capped_near() where that applies: callers may take either)
 __device__ __forceinline__ float capped(float s, const Score& sc) {
     const float t = s * sc.tmul;

@@ -226,7 +226,7 @@ attn_decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         float v = sv[nt][0][e] + sv[nt][1][e];
-                        v = sc.cap2 > 0.f ? near ? capped_near(v * sc.tmul, sc.cap2) : capped(v, sc) : v * sc.mul;
+                        v = sc.cap2 > 0.f ? near ? capped_near(v * sc.tmul, sc.cap2) : capped(v, sc) : __fmul_rn(v, sc.mul);
                         if (masked) {
                             const int j = j0 + g + (e >> 1) * 8;
                             if (j > see_hi[nt][e & 1] || j < see_lo[nt][e & 1]) v = -INFINITY;

@@ -685,3 +685,11 @@ def test_attn_paged_does_not_depend_on_what_the_cache_holds_elsewhere(D, cap, wi
             first = got
             _check(got, want, tol, status)
         assert torch.equal(got, first), fill
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,L,hint", [(1, 700, 700), (4, 700, 700), (60, 500, 1 << 20), (140, 900, 1 << 20), (140, 300, 300)])
+@pytest.mark.parametrize("exponent,cap", [(24, 2.0 ** 31), (30, 2.0 ** 38), (34, 2.0 ** 41), (34, 2.0 ** 60), (60, 2.0 ** 69), (60, 2.0 ** 99), (40, 50.0)])
+def test_attn_paged_large_scores_under_a_large_cap(D, n, L, hint, exponent, cap):
+    for step in (None, 200):
+        _check(*_attend([n], [L], 4, 2, D, 16, seed=56, scale=1.0, softcap=cap, hints=(n, hint), edit=_sign_scores(D, n, L, exponent, step)))

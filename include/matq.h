@@ -479,7 +479,83 @@ int matq_attn_paged(const matq_paged_kv *cache, int64_t T, const void *q, int q_
                     int32_t *dev_status, void *stream);
 
 /*
- * Testing hook for the error paths of (7) and (9), as matq_gemm_multi_test_stall: while `on` is non-zero their kernels issue no
+ * ---- Four bits with a scale per group: entry points (10) to (13). ----
+ * A 4-bit group is a run of consecutive bf16 values x that shares a scale and a low end, two bf16:
+ *       low = min x,  scale = bf16( (max x - low) / 15 ), and 0 if that is below 2^-120,
+ *       q   = round_half_even( (x - low) * (1 / scale) )  in 0 .. 15  (0 where scale = 0),      value = scale * q + low
+ *     with one correctly rounded binary32 operation per step in the order written: codes and groups are defined bit for bit (a low end of -0 is stored as 0).
+ *     A group that holds NaN or Inf, or whose range max - low passes binary32, gets scale = low = NaN and codes 0, and dev_status = MATQ_ERR_NONFINITE.
+ */
+
+/*
+ * (10) Weights to 4-bit groups along the rows.
+ *   W        in   bf16 [N, K], row stride ldw elements
+ *   group    32, 64 or 128 weights
+ *   packed   out  uint8 [N, K/2]: byte j of a row holds element 2j in its low half and 2j + 1 in its high half (the plane format of (2) for r = 4)
+ *   params   out  bf16 [N, K/group, 2]: scale, low
+ *   Requires K % group == 0, ldw % 8 == 0, 16-byte aligned pointers, N and K below 2^31; N may be 0.
+ */
+int matq_quantize_groups(const void *W, int64_t N, int64_t K, int64_t ldw, int group, uint8_t *packed, void *params,
+                         int32_t *dev_status, void *stream);
+
+/*
+ * (11) Linear layer on weights in 4-bit groups, for a few tokens:
+ *       Y[m,n] = sum over the groups i of row n of  scale_ni * sum_k x[m,k] q[n,k]  +  low_ni * sum_k x[m,k]   (k in the group)
+ *     The inner sums are products of exact codes with the bf16 activations, accumulated in fp32; what follows is fp32, rounded once more to bf16 when out_type asks
+ *     for it.  A token whose largest activation is 2^120 times another loses the smaller one.  A token that holds NaN or Inf gets NaN or Inf, and no other token is
+ *     touched.  Any number of tokens; the weights are read once for up to 32 * group / 128 of them.
+ *   packed, params  in   as written by (10), dense rows        x  in  bf16 [M, K], row stride ldx        Y  out  fp32 or bf16 [M, N], row stride ldy
+ *   flags           0 or MATQ_GEMV_PDL (the previous kernel of the stream writes neither packed nor params)
+ *   Requires K % group == 0, K <= 65536, ldx % 8 == 0, N below 2^31, packed, params and x 16-byte aligned (MATQ_ERR_SHAPE past 2^20 row tiles or 65535 token tiles).
+ */
+int matq_gemv_groups(const uint8_t *packed, int64_t N, int64_t K, int group, const void *params, const void *x, int64_t M, int64_t ldx,
+                     int out_type, void *Y, int64_t ldy, unsigned flags, void *stream);
+
+/*
+ * A paged cache of keys and values in 4-bit groups of 64 elements along the head.  As matq_paged_kv, but for the cache itself: the 16 keys of a page with
+ * slots 16 i .. 16 i + 15, of one head, make a tile of 18 * head_dim bytes, their keys first and their values behind them, each as
+ *   codes   [head_dim / 32][16 slots][16 bytes]: elements 32 c .. 32 c + 31 of a slot, element e of these in half e % 2 (0 the low one) of byte e / 2
+ *   groups  [head_dim / 64][16 slots][2] bf16: scale, low
+ */
+typedef struct matq_paged_kv4 {
+    void *tiles;                 /* uint8 [n_pages, kv_heads, page_size / 16, 18 * head_dim], contiguous, 16-byte aligned */
+    int64_t n_pages;
+    int page_size, kv_heads, head_dim;
+    int batch;
+    const int32_t *page_table;
+    int64_t table_stride, table_width;
+    const int32_t *cu_q;
+    const int32_t *kv_len;
+} matq_paged_kv4;
+
+/* 18 * head_dim for head_dim in {64, 128, 256}, else -1. */
+int64_t matq_kv4_tile_bytes(int head_dim);
+
+/*
+ * (12) As (8) for a cache in 4-bit groups: keys are rotated, rounded to bf16 and quantised, values are quantised, queries rotated.  Every product and sum of the
+ *     rotation is rounded to binary32 by itself, so that the cache's bytes are defined bit for bit.
+ *   Arguments, alignments and errors as for (8); head_dim in {64, 128, 256}, page_size a multiple of 16.
+ */
+int matq_kv4_append(const matq_paged_kv4 *cache, int64_t T, const void *q, int q_heads, int64_t ldq,
+                    const void *k, int64_t ldk, const void *v, int64_t ldv,
+                    const float *cos_sin, int64_t max_pos, int rot_dim, int interleaved,
+                    void *q_out, int64_t ldqo, int32_t *dev_status, void *stream);
+
+/*
+ * (13) As (9) for a cache in 4-bit groups: keys and values are what its codes and groups stand for.  Sequences with few new tokens read the cache as it is; for
+ *     sequences with more, keys and values are unpacked to bf16 in the workspace first (one more rounding of each), a few sequences at a time.
+ *   Arguments and errors as for (9), but max_q and max_kv are bounds: a sequence with more new tokens or keys may be refused with MATQ_ERR_PAGE.
+ *   workspace   at least matq_attn_paged4_workspace_bytes(...) bytes for this call's sizes, 16-byte aligned; contents need not be initialised.
+ */
+size_t matq_attn_paged4_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim,
+                                        int64_t max_q, int64_t max_kv, int64_t window);
+int matq_attn_paged4(const matq_paged_kv4 *cache, int64_t T, const void *q, int q_heads, int64_t ldq,
+                     float scale, float softcap, int64_t window, int64_t max_q, int64_t max_kv,
+                     void *out, int64_t ldo, void *workspace, size_t workspace_bytes,
+                     int32_t *dev_status, void *stream);
+
+/*
+ * Testing hook for the error paths of (7), (9) and (13), as matq_gemm_multi_test_stall: while `on` is non-zero their kernels issue no
  * copies and their waits give up after about a millisecond; a call reports MATQ_ERR_TIMEOUT through dev_status, returns, and leaves the
  * GPU ready for the next.  (7) has no device-side wait for up to 8 tokens and few codes, and ignores it there.  Process-wide; returns the previous setting.
  */

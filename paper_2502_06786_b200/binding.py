@@ -32,6 +32,7 @@ EXPORTS = ["matq_status_string", "matq_version", "matq_packed_row_bytes", "matq_
            "matq_gemm_multi_test_stall", "matq_slice_pack_test_stall",
            "matq_gemm_multi_static_max_bytes", "matq_gemm_multi_static",
            "matq_quantize_tokens", "matq_gemm_a8", "matq_gemm_a8_plan", "matq_kv_append", "matq_attn_paged_workspace_bytes", "matq_attn_paged",
+           "matq_quantize_groups", "matq_gemv_groups", "matq_kv4_tile_bytes", "matq_kv4_append", "matq_attn_paged4_workspace_bytes", "matq_attn_paged4",
            "matq_serving_test_stall"]
 
 
@@ -47,6 +48,12 @@ class PagedKv(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int64), ("page_size", C.c_int), ("kv_heads", C.c_int),
                 ("head_dim", C.c_int), ("batch", C.c_int), ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int64),
                 ("cu_q", C.c_void_p), ("kv_len", C.c_void_p)]
+
+
+class PagedKv4(C.Structure):
+    """matq_paged_kv4."""
+    _fields_ = [("tiles", C.c_void_p), ("n_pages", C.c_int64), ("page_size", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("batch", C.c_int),
+                ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int64), ("cu_q", C.c_void_p), ("kv_len", C.c_void_p)]
 
 
 class MatqError(RuntimeError):
@@ -115,6 +122,18 @@ def _load():
     lib.matq_attn_paged_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i64, i64]
     lib.matq_attn_paged.restype = i32
     lib.matq_attn_paged.argtypes = [C.POINTER(PagedKv), i64, vp, i32, i64, f32, f32, i64, i64, i64, vp, i64, vp, sz, vp, vp]
+    lib.matq_quantize_groups.restype = i32
+    lib.matq_quantize_groups.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, vp]
+    lib.matq_gemv_groups.restype = i32
+    lib.matq_gemv_groups.argtypes = [vp, i64, i64, i32, vp, vp, i64, i64, i32, vp, i64, u32, vp]
+    lib.matq_kv4_tile_bytes.restype = i64
+    lib.matq_kv4_tile_bytes.argtypes = [i32]
+    lib.matq_kv4_append.restype = i32
+    lib.matq_kv4_append.argtypes = [C.POINTER(PagedKv4), i64, vp, i32, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp, i64, vp, vp]
+    lib.matq_attn_paged4_workspace_bytes.restype = sz
+    lib.matq_attn_paged4_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i64, i64]
+    lib.matq_attn_paged4.restype = i32
+    lib.matq_attn_paged4.argtypes = [C.POINTER(PagedKv4), i64, vp, i32, i64, f32, f32, i64, i64, i64, vp, i64, vp, sz, vp, vp]
     lib.matq_serving_test_stall.restype = i32
     lib.matq_serving_test_stall.argtypes = [i32]
     return lib
@@ -513,6 +532,65 @@ def attn_paged(q, k_cache, v_cache, page_table, cu_q, kv_len, max_q, max_kv, sca
     return out
 
 
+def quantize_groups(W, group=128, packed=None, params=None, dev_status=None):
+    """matq_quantize_groups.  W: bf16 [N, K].  Returns (packed uint8 [N, K / 2], params bf16 [N, K / group, 2]: scale and low end of each group)."""
+    if packed is None:
+        packed = torch.empty((W.shape[0], W.shape[1] // 2), dtype=torch.uint8, device=W.device)
+    if params is None:
+        params = torch.empty((W.shape[0], W.shape[1] // group, 2), dtype=_BF16, device=W.device)
+    st = _serving.quantize_groups(W, group, packed, params, dev_status)
+    if st:
+        raise MatqError(st, "matq_quantize_groups")
+    return packed, params
+
+
+def gemv_groups(packed, params, x, y=None, out_dtype=torch.float32, flags=0):
+    """matq_gemv_groups.  packed, params: as returned by quantize_groups; x: bf16 [M, K].  Returns y [M, N], fp32 or bf16 (the type of ``y`` when it is
+    given, ``out_dtype`` otherwise)."""
+    if y is None:
+        y = torch.empty((x.shape[0], packed.shape[0]), dtype=out_dtype, device=x.device)
+    st = _serving.gemv_groups(packed, params, x, y, flags)
+    if st:
+        raise MatqError(st, "matq_gemv_groups")
+    return y
+
+
+def kv4_tile_bytes(head_dim) -> int:
+    """matq_kv4_tile_bytes: the last dimension of a cache in 4-bit groups."""
+    return int(_lib.matq_kv4_tile_bytes(head_dim))
+
+
+def kv4_append(cache, page_table, cu_q, kv_len, k, v, cos_sin=None, q=None, q_out=None, interleaved=False, dev_status=None):
+    """matq_kv4_append.  cache: uint8 [n_pages, kv_heads, page_size / 16, kv4_tile_bytes(head_dim)]; everything else as in kv_append.
+    Writes the cache; returns q_out (pass q itself to rotate in place)."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=_BF16, device=q.device)
+    st = _serving.kv4_append(cache, page_table, cu_q, kv_len, k, v, cos_sin, q, q_out, interleaved, dev_status)
+    if st:
+        raise MatqError(st, "matq_kv4_append")
+    return q_out
+
+
+def attn_paged4_workspace_bytes(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window=0) -> int:
+    return int(_lib.matq_attn_paged4_workspace_bytes(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window))
+
+
+def attn_paged4(q, cache, page_table, cu_q, kv_len, max_q, max_kv, scale=None, softcap=0.0, window=0, out=None, workspace=None, dev_status=None):
+    """matq_attn_paged4.  As attn_paged for a cache as in kv4_append; max_q and max_kv must not be too small.
+    Returns out, bf16 [T, q_heads, head_dim]."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=_BF16, device=q.device)
+    if workspace is None:
+        need = attn_paged4_workspace_bytes(q.shape[0], page_table.shape[0], q.shape[1], cache.shape[1], q.shape[2], max_q, max_kv, window)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    st = _serving.attn_paged4(q, cache, page_table, cu_q, kv_len, max_q, max_kv, q.shape[-1] ** -0.5 if scale is None else scale,
+                              softcap, window, out, workspace, dev_status)
+    if st:
+        raise MatqError(st, "matq_attn_paged4")
+    return out
+
+
 def serving_test_stall(on) -> int:
-    """matq_serving_test_stall: switch the "issue no copies" test mode of gemm_a8 and attn_paged; returns the previous setting."""
+    """matq_serving_test_stall: switch the "issue no copies" test mode of gemm_a8, attn_paged and attn_paged4; returns the previous setting."""
     return int(_lib.matq_serving_test_stall(1 if on else 0))

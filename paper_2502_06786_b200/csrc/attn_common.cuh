@@ -23,6 +23,7 @@ struct Params {
     const int32_t *table, *cu_q, *kv_len;
     int64_t ldq, ldo, table_stride, table_width, n_pages, T;
     int64_t window;              // 0 = none
+    int64_t above_rows;          // sequences with no more rows (tokens times heads of a group) than that are left to other kernels; 0 = none are
     int batch, q_heads, kv_heads, group, page_size, page_shift;
     int tiles_per_seq;           // row tiles that the grid holds per sequence (a sequence with more is walked in steps)
     int splits;                  // parts of the key range
@@ -33,6 +34,7 @@ struct Params {
     int32_t* dev_status;
     long long wait_cycles;
     int hold;
+    int filter, join_above;      // joins: only sequences with more rows than above_rows (join_above), or only the others
 };
 
 // Scores as exponents of two: p = 2^(value - maximum).  Without a cap that is one product.  The cap's tanh is a polynomial for arguments up to
@@ -115,6 +117,7 @@ __device__ __forceinline__ Sequence sequence(const Params& P, int b) {
     Sequence s;
     s.q0 = P.cu_q[b];
     s.n_new = P.cu_q[b + 1] - s.q0;
+    if (s.n_new <= P.above_rows / P.group) s.n_new = 0;
     s.kv_len = max(P.kv_len[b], 0);                                     // below zero no query sees a key either, and positions keep within 32 bits
     if (s.n_new > 0 && (s.q0 < 0 || s.q0 + s.n_new > P.T || s.kv_len > P.table_width * P.page_size)) {
         report(P.dev_status, MATQ_ERR_PAGE);
@@ -142,6 +145,14 @@ __device__ __forceinline__ int cache_row(const Params& P, int b, int h, int64_t 
     return page_row(P, h, key, page);
 }
 
+// Whether a token's sequence is one that a call with a bound on its rows serves (see above_rows): the number of sequences of the batch that end at or before it.
+__device__ __forceinline__ bool joined(const Params& P, int64_t t) {
+    const int lane = threadIdx.x & 31;
+    int b = 0;
+    for (int at = 0; at < P.batch; at += 32) b += __popc(__ballot_sync(0xffffffffu, at + lane < P.batch && (int64_t)P.cu_q[at + lane + 1] <= t));
+    return b < P.batch && P.cu_q[b] <= t && (P.cu_q[b + 1] - P.cu_q[b] > P.above_rows / P.group) == P.join_above;
+}
+
 // Joins the parts of the key range: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  A CTA per (token, head): the weights of the
 // parts are made side by side, then eight warps take every eighth part each, and their sums are added in a fixed order.
 constexpr int kMaxSplits = 256, kJoinThreads = 256;
@@ -153,7 +164,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const Params P)
     let_next_kernel_start();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t rows = P.T * P.q_heads, row = blockIdx.x, t = row / P.q_heads;
-    if (t >= P.cu_q[P.batch]) return;
+    if (t >= P.cu_q[P.batch] || (P.filter && !joined(P, t))) return;
     float2 ml = make_float2(-INFINITY, 0.f);
     if (tid < P.splits) ml = P.part_ml[(int64_t)tid * rows + row];
     float mx = ml.x;
@@ -213,7 +224,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_few_kernel(const Param
     const int64_t rows = P.T * P.q_heads, row = (int64_t)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
     if (row >= rows) return;
     const int64_t t = row / P.q_heads;
-    if (t >= P.cu_q[P.batch]) return;
+    if (t >= P.cu_q[P.batch] || (P.filter && !joined(P, t))) return;
     constexpr int kV = D / 64;
     float2 ml[kFewSplits], acc[kV];
     float mx = -INFINITY, sum = 0.f;
@@ -244,6 +255,20 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_few_kernel(const Param
 #pragma unroll
     for (int j = 0; j < kV; ++j) dst[lane + 32 * j] = seen ? pack_bf16(acc[j].x * inv, acc[j].y * inv) : 0u;
 }
+
+template <int D>
+inline int launch_join(const Params& P, cudaStream_t s) {
+    const int64_t rows = P.T * P.q_heads;
+    const cudaError_t e = P.splits <= kFewSplits
+        ? launch_overlapped(attn_join_few_kernel<D>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))), dim3(kJoinThreads), 0, s, P)
+        : launch_overlapped(attn_join_kernel<D>, dim3((unsigned)rows), dim3(kJoinThreads), 0, s, P);
+    if (e != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
+    return MATQ_OK;
+}
+
+// matq_attn_paged for the sequences with more than above_rows rows (attn_paged.cu)
+int paged(const matq_paged_kv* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap, int64_t window, int64_t max_q, int64_t max_kv,
+          void* out, int64_t ldo, void* workspace, size_t workspace_bytes, int64_t above_rows, int32_t* dev_status, void* stream);
 
 }  // namespace attn
 }  // namespace matq

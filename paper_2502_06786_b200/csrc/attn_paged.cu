@@ -135,13 +135,7 @@ int launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, 
         else st = MATQ_ERR_UNSUPPORTED;
     }
     if (st != MATQ_OK) return st;
-    if (P.splits > 1) {
-        const int64_t rows = P.T * P.q_heads;
-        const cudaError_t e = P.splits <= kFewSplits
-            ? launch_overlapped(attn_join_few_kernel<D>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))), dim3(kJoinThreads), 0, s, P)
-            : launch_overlapped(attn_join_kernel<D>, dim3((unsigned)rows), dim3(kJoinThreads), 0, s, P);
-        if (e != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
-    }
+    if (P.splits > 1 && (st = launch_join<D>(P, s)) != MATQ_OK) return st;
     return launch_status();
 }
 
@@ -156,11 +150,8 @@ extern "C" size_t matq_attn_paged_workspace_bytes(int64_t T, int batch, int q_he
     return part_bytes(T, q_heads, head_dim, p.splits);
 }
 
-extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap,
-                               int64_t window, int64_t max_q, int64_t max_kv, void* out, int64_t ldo, void* workspace,
-                               size_t workspace_bytes, int32_t* dev_status, void* stream) {
-    using namespace matq;
-    using namespace matq::attn;
+int matq::attn::paged(const matq_paged_kv* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap, int64_t window, int64_t max_q,
+                      int64_t max_kv, void* out, int64_t ldo, void* workspace, size_t workspace_bytes, int64_t above_rows, int32_t* dev_status, void* stream) {
     if (!cache || T < 0 || q_heads < 1 || cache->batch < 0 || cache->n_pages < 0 || cache->kv_heads < 1 || cache->table_width < 0 || (cache->batch > 1 && cache->table_stride < cache->table_width) ||
         window < 0 || max_q < 0 || max_kv < 0 || !(softcap >= 0.f) || !(scale > 0.f))
         return MATQ_ERR_INVALID_ARG;
@@ -183,7 +174,7 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     Params P;
     P.q = static_cast<const __nv_bfloat16*>(q); P.v = static_cast<const __nv_bfloat16*>(cache->v); P.out = static_cast<__nv_bfloat16*>(out);
     P.table = cache->page_table; P.cu_q = cache->cu_q; P.kv_len = cache->kv_len;
-    P.ldq = ldq; P.ldo = ldo; P.table_stride = cache->table_stride; P.table_width = cache->table_width; P.n_pages = cache->n_pages; P.T = T; P.window = window;
+    P.ldq = ldq; P.ldo = ldo; P.table_stride = cache->table_stride; P.table_width = cache->table_width; P.n_pages = cache->n_pages; P.T = T; P.window = window; P.above_rows = above_rows;
     P.batch = cache->batch; P.q_heads = q_heads; P.kv_heads = cache->kv_heads; P.group = group;
     P.page_size = ps; P.page_shift = ps == 16 ? 4 : ps == 32 ? 5 : ps == 64 ? 6 : ps == 128 ? 7 : 8;
     P.tiles_per_seq = (int)p.tiles_per_seq; P.splits = (int)p.splits; P.split_keys = p.split_keys;
@@ -192,6 +183,8 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     P.part_o = static_cast<float*>(workspace);
     P.part_ml = reinterpret_cast<float2*>(P.part_o + (size_t)p.splits * T * q_heads * D);
     P.dev_status = dev_status;
+    P.filter = above_rows > 0 ? 1 : 0;
+    P.join_above = 1;
     P.hold = tc::test_stall() ? 1 : 0;
     P.wait_cycles = P.hold ? tc::kStallWaitCycles : tc::kWaitCycles;
     const unsigned grid = (unsigned)ctas;
@@ -202,4 +195,10 @@ extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void
     if (D == 64) return launch<64>(tq, tk, tv, P, p.kind, grid, s);
     if (D == 128) return launch<128>(tq, tk, tv, P, p.kind, grid, s);
     return launch<256>(tq, tk, tv, P, p.kind, grid, s);
+}
+
+extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap,
+                               int64_t window, int64_t max_q, int64_t max_kv, void* out, int64_t ldo, void* workspace,
+                               size_t workspace_bytes, int32_t* dev_status, void* stream) {
+    return matq::attn::paged(cache, T, q, q_heads, ldq, scale, softcap, window, max_q, max_kv, out, ldo, workspace, workspace_bytes, 0, dev_status, stream);
 }

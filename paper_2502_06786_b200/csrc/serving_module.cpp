@@ -28,6 +28,7 @@ const at::Tensor& tensor(PyObject* o, std::optional<at::ScalarType> type, const 
     if (t.get_device() != c10::cuda::current_device()) fail(PyExc_ValueError, name, "on another device than the current one, whose stream the call would use");
     return t;
 }
+bool is_bf16(PyObject* o) { return THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() == at::kBFloat16; }       // of an output of either type
 template <typename T>
 T* vec(PyObject* o, at::ScalarType type, const char* name, int64_t n) {
     const at::Tensor& t = tensor(o, type, name);
@@ -42,8 +43,8 @@ Matrix mat(PyObject* o, at::ScalarType type, const char* name) {
     const at::Tensor& t = tensor(o, type, name);
     if (t.dim() != 2) fail(PyExc_ValueError, name, "expected 2 dimensions");
     const int64_t r = t.size(0), c = t.size(1);
-    if (t.stride(1) != 1 && c > 1) fail(PyExc_ValueError, name, "unit stride along its second dimension required");
-    return {t.data_ptr(), r, c, r > 1 ? t.stride(0) : c};               // a single row may report any stride
+    if (t.stride(1) != 1 && c > 1 && r > 0) fail(PyExc_ValueError, name, "unit stride along its second dimension required");
+    return {t.data_ptr(), r, c, r > 1 ? t.stride(0) : c};               // a single row, or none, may report any stride
 }
 struct Heads {
     void* p;
@@ -113,6 +114,30 @@ Paged paged(PyObject* const* a) {
     return p;
 }
 
+struct Paged4 {
+    matq_paged_kv4 c;
+};
+Paged4 paged4(PyObject* const* a) {
+    const at::Tensor& tiles = tensor(a[0], at::kByte, "cache");
+    if (tiles.dim() != 4 || !tiles.is_contiguous()) fail(PyExc_ValueError, "cache", "contiguous [n_pages, kv_heads, page_size / 16, 18 head_dim] required");
+    if (tiles.size(1) > INT32_MAX || tiles.size(2) > INT32_MAX / 16 || tiles.size(3) > INT32_MAX || tiles.size(3) % 18 != 0) fail(PyExc_ValueError, "cache", "[n_pages, kv_heads, page_size / 16, 18 head_dim] required");
+    const Matrix t = mat(a[1], at::kInt, "page_table");
+    if (t.rows > INT32_MAX - 1) fail(PyExc_ValueError, "page_table", "too many sequences");
+    Paged4 p;
+    p.c.tiles = tiles.data_ptr();
+    p.c.n_pages = tiles.size(0);
+    p.c.kv_heads = (int)tiles.size(1);
+    p.c.page_size = (int)tiles.size(2) * 16;
+    p.c.head_dim = (int)tiles.size(3) / 18;
+    p.c.batch = (int)t.rows;
+    p.c.page_table = static_cast<const int32_t*>(t.p);
+    p.c.table_stride = t.ld;
+    p.c.table_width = t.cols;
+    p.c.cu_q = vec<int32_t>(a[2], at::kInt, "cu_q", t.rows + 1);
+    p.c.kv_len = vec<int32_t>(a[3], at::kInt, "kv_len", t.rows);
+    return p;
+}
+
 template <typename F>
 PyObject* call(Py_ssize_t n, Py_ssize_t want, F f) {
     if (n != want) return PyErr_Format(PyExc_TypeError, "%zd positional arguments required, %zd given", want, n);
@@ -145,7 +170,7 @@ PyObject* gemm_a8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 10, [&] {
         const Matrix x = mat(a[0], at::kChar, "xq"), w = mat(a[3], at::kByte, "q");
         if (w.cols != x.cols) fail(PyExc_ValueError, "q", "xq [M, K] and q [N, K] required");
-        const bool bf16 = THPVariable_Check(a[6]) && THPVariable_Unpack(a[6]).scalar_type() == at::kBFloat16;
+        const bool bf16 = is_bf16(a[6]);
         const Matrix y = mat(a[6], bf16 ? at::kBFloat16 : at::kFloat, "y");
         if (y.rows != x.rows || y.cols != w.rows) fail(PyExc_ValueError, "y", "[M, N] required");
         const float *scale = vec<float>(a[1], at::kFloat, "scale", x.rows), *alpha = vec<float>(a[4], at::kFloat, "alpha", w.rows),
@@ -161,55 +186,165 @@ PyObject* gemm_a8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// what the two appends share: k, v, cos_sin, q, q_out, interleaved, dev_status from a[0] on; f makes the call
+struct New {
+    Heads k, v, q, o;
+    Matrix cs;
+    int interleaved;
+    int32_t* status;
+};
+New fresh(PyObject* const* a, int64_t kv_heads, int64_t D) {
+    New w;
+    w.k = heads(a[0], "k", D);
+    w.v = heads(a[1], "v", D);
+    if (w.k.H != kv_heads || w.v.H != kv_heads || w.v.T != w.k.T) fail(PyExc_ValueError, "k, v", "[T, kv_heads, head_dim] each required");
+    w.cs = {nullptr, 0, 0, 0};
+    if (a[2] != Py_None) {
+        w.cs = mat(a[2], at::kFloat, "cos_sin");
+        if (w.cs.ld != w.cs.cols) fail(PyExc_ValueError, "cos_sin", "contiguous [max_pos, rot_dim] required");
+    }
+    w.q = w.o = {nullptr, 0, 0, 0};
+    if ((a[3] == Py_None) != (a[4] == Py_None)) fail(PyExc_ValueError, "q, q_out", "both or neither required");
+    if (a[3] != Py_None) {
+        w.q = heads(a[3], "q", D);
+        w.o = heads(a[4], "q_out", D);
+        if (w.q.T != w.k.T || w.o.T != w.k.T || w.q.H != w.o.H) fail(PyExc_ValueError, "q, q_out", "one row per token each, of the same heads");
+    }
+    w.interleaved = PyObject_IsTrue(a[5]);
+    if (w.interleaved < 0) { PyErr_Clear(); fail(PyExc_TypeError, "interleaved", "a truth value is required"); }
+    w.status = status_word(a[6]);
+    return w;
+}
+
 // k_cache, v_cache, page_table, cu_q, kv_len, k, v, cos_sin, q, q_out, interleaved, dev_status
 PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 12, [&] {
         const Paged p = paged(a);
-        const int64_t D = p.c.head_dim;
-        const Heads k = heads(a[5], "k", D), v = heads(a[6], "v", D);
-        if (k.H != p.c.kv_heads || v.H != p.c.kv_heads || v.T != k.T) fail(PyExc_ValueError, "k, v", "[T, kv_heads, head_dim] each required");
-        Matrix cs = {nullptr, 0, 0, 0};
-        if (a[7] != Py_None) {
-            cs = mat(a[7], at::kFloat, "cos_sin");
-            if (cs.ld != cs.cols) fail(PyExc_ValueError, "cos_sin", "contiguous [max_pos, rot_dim] required");
-        }
-        Heads q = {nullptr, 0, 0, 0}, o = q;
-        if ((a[8] == Py_None) != (a[9] == Py_None)) fail(PyExc_ValueError, "q, q_out", "both or neither required");
-        if (a[8] != Py_None) {
-            q = heads(a[8], "q", D);
-            o = heads(a[9], "q_out", D);
-            if (q.T != k.T || o.T != k.T || q.H != o.H) fail(PyExc_ValueError, "q, q_out", "one row per token each, of the same heads");
-        }
-        const int inter = PyObject_IsTrue(a[10]);
-        if (inter < 0) { PyErr_Clear(); fail(PyExc_TypeError, "interleaved", "a truth value is required"); }
-        int32_t* status = status_word(a[11]);
+        const New w = fresh(a + 5, p.c.kv_heads, p.c.head_dim);
         void* s = stream();
         return unlocked([&] {
-            return matq_kv_append(&p.c, k.T, q.p, (int)q.H, q.ld, k.p, k.ld, v.p, v.ld, static_cast<const float*>(cs.p), cs.rows, (int)cs.cols, inter, o.p, o.ld, status, s);
+            return matq_kv_append(&p.c, w.k.T, w.q.p, (int)w.q.H, w.q.ld, w.k.p, w.k.ld, w.v.p, w.v.ld, static_cast<const float*>(w.cs.p), w.cs.rows, (int)w.cs.cols,
+                                  w.interleaved, w.o.p, w.o.ld, w.status, s);
         });
     });
+}
+
+// cache, page_table, cu_q, kv_len, k, v, cos_sin, q, q_out, interleaved, dev_status
+PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 11, [&] {
+        const Paged4 p = paged4(a);
+        const New w = fresh(a + 4, p.c.kv_heads, p.c.head_dim);
+        void* s = stream();
+        return unlocked([&] {
+            return matq_kv4_append(&p.c, w.k.T, w.q.p, (int)w.q.H, w.q.ld, w.k.p, w.k.ld, w.v.p, w.v.ld, static_cast<const float*>(w.cs.p), w.cs.rows, (int)w.cs.cols,
+                                   w.interleaved, w.o.p, w.o.ld, w.status, s);
+        });
+    });
+}
+
+// what the two attentions share: max_q, max_kv, scale, softcap, window, out, workspace, dev_status from a[0] on
+struct Attend {
+    Heads q, o;
+    int64_t max_q, max_kv, window;
+    float scale, softcap;
+    void* ws;
+    size_t bytes;
+    int32_t* status;
+};
+Attend attend(PyObject* q, PyObject* const* a, int64_t D) {
+    Attend w;
+    w.q = heads(q, "q", D);
+    w.o = heads(a[5], "out", D);
+    if (w.o.T != w.q.T || w.o.H != w.q.H) fail(PyExc_ValueError, "out", "one row per token, of q's heads");
+    w.ws = nullptr;
+    w.bytes = 0;
+    if (a[6] != Py_None) {
+        const at::Tensor& t = tensor(a[6], std::nullopt, "workspace");
+        if (!t.is_contiguous()) fail(PyExc_TypeError, "workspace", "a contiguous tensor is required");
+        w.ws = t.data_ptr();
+        w.bytes = t.nbytes();
+    }
+    w.scale = (float)number(a[2], "scale");
+    w.softcap = (float)number(a[3], "softcap");
+    w.window = integer(a[4], "window");
+    w.max_q = integer(a[0], "max_q");
+    w.max_kv = integer(a[1], "max_kv");
+    w.status = status_word(a[7]);
+    return w;
 }
 
 // q, k_cache, v_cache, page_table, cu_q, kv_len, max_q, max_kv, scale, softcap, window, out, workspace, dev_status
 PyObject* attn_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 14, [&] {
         const Paged p = paged(a + 1);
-        const int64_t D = p.c.head_dim;
-        const Heads q = heads(a[0], "q", D), o = heads(a[11], "out", D);
-        if (o.T != q.T || o.H != q.H) fail(PyExc_ValueError, "out", "one row per token, of q's heads");
-        void* ws = nullptr;
-        size_t bytes = 0;
-        if (a[12] != Py_None) {
-            const at::Tensor& t = tensor(a[12], std::nullopt, "workspace");
-            if (!t.is_contiguous()) fail(PyExc_TypeError, "workspace", "a contiguous tensor is required");
-            ws = t.data_ptr();
-            bytes = t.nbytes();
-        }
-        const float scale = (float)number(a[8], "scale"), softcap = (float)number(a[9], "softcap");
-        const int64_t window = integer(a[10], "window"), max_q = integer(a[6], "max_q"), max_kv = integer(a[7], "max_kv");
-        int32_t* status = status_word(a[13]);
+        const Attend w = attend(a[0], a + 6, p.c.head_dim);
         void* s = stream();
-        return unlocked([&] { return matq_attn_paged(&p.c, q.T, q.p, (int)q.H, q.ld, scale, softcap, window, max_q, max_kv, o.p, o.ld, ws, bytes, status, s); });
+        return unlocked([&] {
+            return matq_attn_paged(&p.c, w.q.T, w.q.p, (int)w.q.H, w.q.ld, w.scale, w.softcap, w.window, w.max_q, w.max_kv, w.o.p, w.o.ld, w.ws, w.bytes, w.status, s);
+        });
+    });
+}
+
+// q, cache, page_table, cu_q, kv_len, max_q, max_kv, scale, softcap, window, out, workspace, dev_status
+PyObject* attn_paged4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 13, [&] {
+        const Paged4 p = paged4(a + 1);
+        const Attend w = attend(a[0], a + 5, p.c.head_dim);
+        void* s = stream();
+        return unlocked([&] {
+            return matq_attn_paged4(&p.c, w.q.T, w.q.p, (int)w.q.H, w.q.ld, w.scale, w.softcap, w.window, w.max_q, w.max_kv, w.o.p, w.o.ld, w.ws, w.bytes, w.status, s);
+        });
+    });
+}
+
+// [N, K / group, 2] bf16, contiguous: the groups of a row
+struct Groups {
+    void* p;
+    int64_t rows, per_row;
+};
+Groups groups(PyObject* o, const char* name) {
+    const at::Tensor& t = tensor(o, at::kBFloat16, name);
+    if (t.dim() != 3 || t.size(2) != 2 || !t.is_contiguous()) fail(PyExc_ValueError, name, "contiguous bf16 [N, K / group, 2] required");
+    return {t.data_ptr(), t.size(0), t.size(1)};
+}
+// codes of rows without gaps
+Matrix plane(PyObject* o, const char* name) {
+    const Matrix m = mat(o, at::kByte, name);
+    if (m.ld != m.cols) fail(PyExc_ValueError, name, "contiguous uint8 [N, K / 2] required");
+    return m;
+}
+
+// W, group, packed, params, dev_status
+PyObject* quantize_groups(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 5, [&] {
+        const Matrix w = mat(a[0], at::kBFloat16, "W"), c = plane(a[2], "packed");
+        const int group = small_integer(a[1], "group");
+        const Groups g = groups(a[3], "params");
+        if (c.rows != w.rows || c.cols * 2 != w.cols) fail(PyExc_ValueError, "packed", "uint8 [N, K / 2] required");
+        if (group < 1 || g.rows != w.rows || g.per_row * group != w.cols) fail(PyExc_ValueError, "params", "bf16 [N, K / group, 2] required");
+        int32_t* status = status_word(a[4]);
+        void* s = stream();
+        return unlocked([&] { return matq_quantize_groups(w.p, w.rows, w.cols, w.ld, group, static_cast<uint8_t*>(c.p), g.p, status, s); });
+    });
+}
+
+// packed, params, x, y, flags
+PyObject* gemv_groups(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 5, [&] {
+        const Matrix c = plane(a[0], "packed"), x = mat(a[2], at::kBFloat16, "x");
+        const Groups g = groups(a[1], "params");
+        if (x.cols != c.cols * 2) fail(PyExc_ValueError, "x", "packed [N, K / 2] and x [M, K] required");
+        if (g.rows != c.rows || g.per_row < 1 || x.cols % g.per_row != 0) fail(PyExc_ValueError, "params", "bf16 [N, K / group, 2] required");
+        const int64_t group = x.cols / g.per_row;
+        const bool bf16 = is_bf16(a[3]);
+        const Matrix y = mat(a[3], bf16 ? at::kBFloat16 : at::kFloat, "y");
+        if (y.rows != x.rows || y.cols != c.rows) fail(PyExc_ValueError, "y", "[M, N] required");
+        const int flags = small_integer(a[4], "flags");
+        void* s = stream();
+        return unlocked([&] {
+            return matq_gemv_groups(static_cast<const uint8_t*>(c.p), c.rows, x.cols, (int)(group < 1 << 30 ? group : 0), g.p, x.p, x.rows, x.ld,
+                                    bf16 ? MATQ_OUT_BF16 : MATQ_OUT_F32, y.p, y.ld, (unsigned)flags, s);
+        });
     });
 }
 
@@ -218,6 +353,10 @@ PyMethodDef methods[] = {
     {"gemm_a8", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(gemm_a8)), METH_FASTCALL, nullptr},
     {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_append)), METH_FASTCALL, nullptr},
     {"attn_paged", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_paged)), METH_FASTCALL, nullptr},
+    {"quantize_groups", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(quantize_groups)), METH_FASTCALL, nullptr},
+    {"gemv_groups", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(gemv_groups)), METH_FASTCALL, nullptr},
+    {"kv4_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv4_append)), METH_FASTCALL, nullptr},
+    {"attn_paged4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_paged4)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serving", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -22,6 +22,8 @@
 
 #include <type_traits>
 
+#include <cuda_fp16.h>
+
 #include "attn_common.cuh"
 
 namespace matq {
@@ -78,9 +80,9 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* v, bool wide) {
         reinterpret_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
     }
 }
-// D = fp32, A = B = bf16, 128 rows
-__device__ __forceinline__ constexpr uint32_t idesc_bf16(int n, bool b_mn_major) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+// D = fp32, A = B = bf16 (or fp16), 128 rows
+__device__ __forceinline__ constexpr uint32_t idesc_16bit(int n, bool b_mn_major, bool half) {
+    return (1u << 4) | (half ? 0u : (1u << 7) | (1u << 10)) | (b_mn_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
 
 // The largest of a thread's scores in columns lo .. hi of its COLS (with the cap: its exponent).  Rare, and kept out of the loop over the keys, whose code it would spread.
@@ -113,8 +115,16 @@ __device__ __noinline__ void lift_scores(uint32_t addr, float by) {
     tc::tmem_wait_st();
 }
 
+// HALF: queries, keys and values are fp16, scaled by powers of two (Params::q_scale and the others; see attn4.cu), and so are the weights.  A weight is at most
+// 2^15 then, and a row takes 0 for its first reference only if its largest weight, and others down to 2^-10 of it, keep all their bits.
+constexpr float kFarHalf = 15.f, kNearHalf = 4.f;
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
 // CAP: with the cap on the scores
-template <int D, int TILES, bool CAP>
+template <int D, int TILES, bool CAP, bool HALF = false>
 __global__ void __launch_bounds__(ChunkCfg<D, TILES>::kThreads, 1)
 attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Params P) {
     using C = ChunkCfg<D, TILES>;
@@ -245,7 +255,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 #pragma unroll
                     for (int x = 0; x < D / kSub / 16; ++x)
                         MATQ_TC_MMA(1, "f16", tmem + t * kKeys, qd + (uint64_t)((x / 4) * (128 * 128 >> 4) + (x & 3) * 2), kd + (uint64_t)((x / 4) * (kKeys * 128 >> 4) + (x & 3) * 2),
-                                    idesc_bf16(kKeys, false), (sub > 0 || x > 0) ? 1u : 0u, leader);
+                                    idesc_16bit(kKeys, false, HALF), (sub > 0 || x > 0) ? 1u : 0u, leader);
                     if (sub == kSub - 1) tc::tc_commit(tc::smem_u32(&s_score[t]), leader);
                 };
                 const auto product = [&](int t, int i, int sub) {       // O_t += P_t V for a stage's keys
@@ -253,7 +263,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     const uint32_t d = tmem + C::kTmemO + (C::kTiles == 2 ? t * D : 0);
 #pragma unroll
                     for (int x = 0; x < kStageKeys / 16; ++x)
-                        MATQ_TC_MMA_TMEM_A(1, "f16", d, tmem + t * kKeys + sub * (kStageKeys / 2) + x * 8, vd + (uint64_t)(x * (2048 >> 4)), idesc_bf16(D, true),
+                        MATQ_TC_MMA_TMEM_A(1, "f16", d, tmem + t * kKeys + sub * (kStageKeys / 2) + x * 8, vd + (uint64_t)(x * (2048 >> 4)), idesc_16bit(D, true, HALF),
                                            (i > 0 || sub > 0 || x > 0) ? 1u : 0u, leader);
                 };
                 const auto first_read = [&](int i) { return i > 0 || round == 0 || tc::warp_wait(tc::smem_u32(&s_read), (uint32_t)(round - 1) & 1u, P.wait_cycles); };
@@ -318,7 +328,13 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const int see_hi = live ? (int)(ctx + tok) : -1, see_lo = live ? lo(see_hi) : 0;
             const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
             const uint32_t o_addr = lane_addr + C::kTmemO + t * D;
-            const Score sc(P.scale, P.softcap);
+            float score_scale = P.scale, value_scale = 1.f;
+            if constexpr (HALF) {
+                if (live) score_scale = P.scale * P.q_scale[(q0 + tok) * P.q_heads + h * P.group + r % P.group] * P.k_scale[(int64_t)b * P.kv_heads + h];
+                value_scale = P.v_scale[(int64_t)b * P.kv_heads + h];
+            }
+            constexpr float kUp = HALF ? kFarHalf : kFar, kDown = HALF ? kNearHalf : kFar;
+            const Score sc(score_scale, P.softcap);
             const float tanh1 = kShort1 * sc.cap2, tanh2 = kShort2 * sc.cap2, tanh3 = kShort3 * sc.cap2, t_max = P.softcap <= kShortCap ? kTanhMax : -1.f;   // with the cap
             const float unit = CAP ? 1.f : sc.mul;                      // the reference is kept as a score; with the cap, as an exponent
             float m = -INFINITY, l = 0.f;
@@ -421,7 +437,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                             x = ex2(x);
                             y = ex2(y);
                             sum2[(e >> 1) & 1] = add2(sum2[(e >> 1) & 1], pair(x, y));
-                            pk[(c + e) / 2] = pack_bf16(x, y);
+                            pk[(c + e) / 2] = HALF ? pack_f16(x, y) : pack_bf16(x, y);
                         }
                     }
                 };
@@ -430,7 +446,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 // (Rows of the tile that stand for no query hold whatever shared memory held: they ask for nothing.)
                 bool lifted = false;
                 const auto wants = [&] {
-                    return ok && see_hi >= 0 && (top > kFar || (m == -INFINITY && top < -kFar && top > -INFINITY) || (!lifted && fabsf(use) >= kLarge));
+                    return ok && see_hi >= 0 && (top > kUp || (m == -INFINITY && top < -kDown && top > -INFINITY) || (!lifted && fabsf(use) >= kLarge));
                 };
                 if (ok) tc::fence_after();
                 for (int attempt = 0; attempt < 3; ++attempt) {         // the second suffices: nothing lies far above a reference that was just moved
@@ -468,7 +484,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         if (large) {
                             ref = best;
                             next = best * unit;
-                            raise = best > -INFINITY && (m == -INFINITY || next - use > kFar);
+                            raise = best > -INFINITY && (m == -INFINITY || next - use > kUp);
                         }
                         if (!CAP && ok) lift_scores<C::kCols>(s_addr, raise ? (fabsf(next) >= kLarge ? ref : 0.f) : fabsf(use) >= kLarge ? m : 0.f);
                         lifted = true;
@@ -503,6 +519,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         ok = __all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&s_vfull[u % C::kStagesV]), (uint32_t)(u / C::kStagesV) & 1u, P.wait_cycles));
                     }
                     if (ok) {
+                        constexpr uint32_t kExponent = HALF ? 0x7c007c00u : 0x7f807f80u;         // of Inf and NaN
                         constexpr int kShare = C::kSoft / kKeys;         // threads per key: 2
                         const int key = tid % kKeys, j = j0 + key;
                         const bool unseen = j > p_hi || j < first, all = j <= p_lo && j >= all_from;
@@ -523,10 +540,10 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                                 for (int x = 0; x < kAtOnce; ++x) {
                                     uint32_t hit = 0;
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) hit |= __vcmpeq2(w[x][e] & 0x7f807f80u, 0x7f807f80u);
+                                    for (int e = 0; e < 4; ++e) hit |= __vcmpeq2(w[x][e] & kExponent, kExponent);
                                     if (hit) {
 #pragma unroll
-                                        for (int e = 0; e < 4; ++e) w[x][e] &= ~__vcmpeq2(w[x][e] & 0x7f807f80u, 0x7f807f80u);
+                                        for (int e = 0; e < 4; ++e) w[x][e] &= ~__vcmpeq2(w[x][e] & kExponent, kExponent);
                                         asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at(ch0 + x * kShare)), "r"(w[x][0]), "r"(w[x][1]), "r"(w[x][2]), "r"(w[x][3]) : "memory");
                                         bad = true;
                                     }
@@ -583,8 +600,13 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                                 const uint16_t* v = reinterpret_cast<const uint16_t*>(P.v) + at * D + c;
 #pragma unroll
                                 for (int e = 0; e < 32; ++e)
-                                    if (nonfinite_bf16(v[e])) o[e] = __float_as_uint(__uint_as_float(o[e]) + bf16_bits_to_float(v[e]));
+                                    if (HALF ? (v[e] & 0x7c00u) == 0x7c00u : nonfinite_bf16(v[e]))
+                                        o[e] = __float_as_uint(__uint_as_float(o[e]) + (HALF ? __half2float(__ushort_as_half(v[e])) : bf16_bits_to_float(v[e])));
                             }
+                    }
+                    if constexpr (HALF) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * value_scale);
                     }
                     if (!live) continue;
                     if (P.splits > 1) {

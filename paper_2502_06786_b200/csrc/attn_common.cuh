@@ -34,6 +34,7 @@ struct Params {
     int32_t* dev_status;
     long long wait_cycles;
     int hold;
+    const float *q_scale, *k_scale, *v_scale;    // fp16 (attn4.cu): what queries [T][q_heads], keys and values [batch][kv_heads] are to be multiplied with
     int filter, join_above;      // joins: only sequences with more rows than above_rows (join_above), or only the others
 };
 
@@ -266,9 +267,17 @@ inline int launch_join(const Params& P, cudaStream_t s) {
     return MATQ_OK;
 }
 
-// matq_attn_paged for the sequences with more than above_rows rows (attn_paged.cu)
+// Queries (dense rows), keys and values as fp16 and their factors, where a call has them so; and which sequences it serves.
+struct Half {
+    const float *q_scale, *k_scale, *v_scale;
+    int64_t above_rows;
+};
+// matq_attn_paged (attn_paged.cu), and its workspace
 int paged(const matq_paged_kv* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap, int64_t window, int64_t max_q, int64_t max_kv,
-          void* out, int64_t ldo, void* workspace, size_t workspace_bytes, int64_t above_rows, int32_t* dev_status, void* stream);
+          void* out, int64_t ldo, void* workspace, size_t workspace_bytes, const Half* half, int32_t* dev_status, void* stream);
+size_t paged_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv, int64_t window, bool half);
+// the 128-row kernels on fp16 (attn4_chunk.cu), one or two query tiles per CTA
+int launch_chunk_half(int D, int tiles, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const Params& P, unsigned grid, cudaStream_t s);
 
 }  // namespace attn
 }  // namespace matq

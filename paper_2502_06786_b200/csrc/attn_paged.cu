@@ -61,11 +61,11 @@ inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64
 // whichever costs less.  Tiles of 16 read the keys more often, but a CTA of theirs starts and ends 3 us sooner (300 tokens over 600, 6 heads of 64 on one key head:
 // 9.0 us, in tiles of 128 rows 13.1; over 2800 20.3 and 22.1; 240 rows over 2560 keys of 4 heads of 128: 18.7 and 15.4).  With D = 256 they do not (32 rows over
 // 600 keys: 13.8 and 13.9 us; 64 rows of 4 sequences 24.3 and 14.7).
-inline Plan plan(int64_t T, int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
+inline Plan plan(int64_t T, int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms, bool half) {
     if (max_q > T) max_q = T;
     if (max_kv > kMaxKeys) max_kv = kMaxKeys;
     const int64_t rows = max_q * group;
-    if (rows <= 16) return plan_kind(rows <= 8 ? 8 : 16, batch, kv_heads, group, D, max_q, max_kv, window, sms);
+    if (rows <= 16 && !half) return plan_kind(rows <= 8 ? 8 : 16, batch, kv_heads, group, D, max_q, max_kv, window, sms);
     const Plan one = plan_kind(1, batch, kv_heads, group, D, max_q, max_kv, window, sms);
     if (D == 256) return one;
     Plan best = one;
@@ -73,6 +73,7 @@ inline Plan plan(int64_t T, int batch, int kv_heads, int group, int D, int64_t m
         const Plan two = plan_kind(2, batch, kv_heads, group, D, max_q, max_kv, window, sms);
         if (two.cost <= best.cost) best = two;
     }
+    if (half) return best;                                              // only the 128-row kernels take fp16
     const Plan few = plan_kind(16, batch, kv_heads, group, D, max_q, max_kv, window, sms);
     if ((double)few.tiles_per_seq * batch * kv_heads <= sms && few.cost < best.cost) best = few;
     return best;
@@ -142,16 +143,19 @@ int launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, 
 }  // namespace attn
 }  // namespace matq
 
-extern "C" size_t matq_attn_paged_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim,
-                                                  int64_t max_q, int64_t max_kv, int64_t window) {
-    using namespace matq::attn;
+size_t matq::attn::paged_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv, int64_t window, bool half) {
     if (T <= 0 || batch <= 0 || q_heads <= 0 || kv_heads <= 0 || q_heads % kv_heads != 0 || q_heads / kv_heads > 64 || head_dim <= 0 || max_q < 0 || max_kv < 0) return 0;
-    const Plan p = plan(T, batch, kv_heads, q_heads / kv_heads, head_dim, max_q, max_kv, window, matq::sm_count());
+    const Plan p = plan(T, batch, kv_heads, q_heads / kv_heads, head_dim, max_q, max_kv, window, matq::sm_count(), half);
     return part_bytes(T, q_heads, head_dim, p.splits);
 }
 
+extern "C" size_t matq_attn_paged_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim,
+                                                  int64_t max_q, int64_t max_kv, int64_t window) {
+    return matq::attn::paged_workspace_bytes(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window, false);
+}
+
 int matq::attn::paged(const matq_paged_kv* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap, int64_t window, int64_t max_q,
-                      int64_t max_kv, void* out, int64_t ldo, void* workspace, size_t workspace_bytes, int64_t above_rows, int32_t* dev_status, void* stream) {
+                      int64_t max_kv, void* out, int64_t ldo, void* workspace, size_t workspace_bytes, const Half* half, int32_t* dev_status, void* stream) {
     if (!cache || T < 0 || q_heads < 1 || cache->batch < 0 || cache->n_pages < 0 || cache->kv_heads < 1 || cache->table_width < 0 || (cache->batch > 1 && cache->table_stride < cache->table_width) ||
         window < 0 || max_q < 0 || max_kv < 0 || !(softcap >= 0.f) || !(scale > 0.f))
         return MATQ_ERR_INVALID_ARG;
@@ -166,7 +170,7 @@ int matq::attn::paged(const matq_paged_kv* cache, int64_t T, const void* q, int 
     if (!q || !out || !cache->k || !cache->v || !cache->page_table || !cache->cu_q || !cache->kv_len || cache->n_pages == 0) return MATQ_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out) || !aligned16(cache->k) || !aligned16(cache->v) || !aligned16(workspace)) return MATQ_ERR_ALIGNMENT;
     const int group = q_heads / cache->kv_heads;
-    const Plan p = plan(T, cache->batch, cache->kv_heads, group, D, max_q, max_kv, window, sm_count());
+    const Plan p = plan(T, cache->batch, cache->kv_heads, group, D, max_q, max_kv, window, sm_count(), half != nullptr);
     const double ctas = (double)p.splits * cache->kv_heads * cache->batch * p.tiles_per_seq;
     if (ctas >= 2147483648.0 || (p.splits > 1 && T * q_heads >= (1ll << 31))) return MATQ_ERR_SHAPE;
     if (part_bytes(T, q_heads, D, p.splits) > workspace_bytes || (p.splits > 1 && !workspace)) return MATQ_ERR_WORKSPACE;
@@ -174,7 +178,7 @@ int matq::attn::paged(const matq_paged_kv* cache, int64_t T, const void* q, int 
     Params P;
     P.q = static_cast<const __nv_bfloat16*>(q); P.v = static_cast<const __nv_bfloat16*>(cache->v); P.out = static_cast<__nv_bfloat16*>(out);
     P.table = cache->page_table; P.cu_q = cache->cu_q; P.kv_len = cache->kv_len;
-    P.ldq = ldq; P.ldo = ldo; P.table_stride = cache->table_stride; P.table_width = cache->table_width; P.n_pages = cache->n_pages; P.T = T; P.window = window; P.above_rows = above_rows;
+    P.ldq = ldq; P.ldo = ldo; P.table_stride = cache->table_stride; P.table_width = cache->table_width; P.n_pages = cache->n_pages; P.T = T; P.window = window; P.above_rows = half ? half->above_rows : 0;
     P.batch = cache->batch; P.q_heads = q_heads; P.kv_heads = cache->kv_heads; P.group = group;
     P.page_size = ps; P.page_shift = ps == 16 ? 4 : ps == 32 ? 5 : ps == 64 ? 6 : ps == 128 ? 7 : 8;
     P.tiles_per_seq = (int)p.tiles_per_seq; P.splits = (int)p.splits; P.split_keys = p.split_keys;
@@ -183,8 +187,9 @@ int matq::attn::paged(const matq_paged_kv* cache, int64_t T, const void* q, int 
     P.part_o = static_cast<float*>(workspace);
     P.part_ml = reinterpret_cast<float2*>(P.part_o + (size_t)p.splits * T * q_heads * D);
     P.dev_status = dev_status;
-    P.filter = above_rows > 0 ? 1 : 0;
+    P.filter = P.above_rows > 0 ? 1 : 0;
     P.join_above = 1;
+    P.q_scale = half ? half->q_scale : nullptr; P.k_scale = half ? half->k_scale : nullptr; P.v_scale = half ? half->v_scale : nullptr;
     P.hold = tc::test_stall() ? 1 : 0;
     P.wait_cycles = P.hold ? tc::kStallWaitCycles : tc::kWaitCycles;
     const unsigned grid = (unsigned)ctas;
@@ -192,6 +197,11 @@ int matq::attn::paged(const matq_paged_kv* cache, int64_t T, const void* q, int 
     const int box_k = ps < p.keys ? ps : p.keys, box_v = ps < p.value_keys ? ps : p.value_keys;
     if (!cache_map(&tk, cache->k, rows, D, box_k) || !cache_map(&tv, cache->v, rows, D, box_v) || !query_map(&tq, q, T, q_heads, D, ldq, group)) return MATQ_ERR_CUDA;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (half) {
+        int st = launch_chunk_half(D, p.kind, tq, tk, tv, P, grid, s);
+        if (st == MATQ_OK && P.splits > 1) st = D == 64 ? launch_join<64>(P, s) : D == 128 ? launch_join<128>(P, s) : launch_join<256>(P, s);
+        return st == MATQ_OK ? launch_status() : st;
+    }
     if (D == 64) return launch<64>(tq, tk, tv, P, p.kind, grid, s);
     if (D == 128) return launch<128>(tq, tk, tv, P, p.kind, grid, s);
     return launch<256>(tq, tk, tv, P, p.kind, grid, s);
@@ -200,5 +210,5 @@ int matq::attn::paged(const matq_paged_kv* cache, int64_t T, const void* q, int 
 extern "C" int matq_attn_paged(const matq_paged_kv* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap,
                                int64_t window, int64_t max_q, int64_t max_kv, void* out, int64_t ldo, void* workspace,
                                size_t workspace_bytes, int32_t* dev_status, void* stream) {
-    return matq::attn::paged(cache, T, q, q_heads, ldq, scale, softcap, window, max_q, max_kv, out, ldo, workspace, workspace_bytes, 0, dev_status, stream);
+    return matq::attn::paged(cache, T, q, q_heads, ldq, scale, softcap, window, max_q, max_kv, out, ldo, workspace, workspace_bytes, nullptr, dev_status, stream);
 }

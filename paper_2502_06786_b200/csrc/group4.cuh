@@ -51,28 +51,31 @@ __device__ __forceinline__ uint32_t quantise_piece(uint4 v, uint32_t& codes, uin
 
 // ---------------------------------------------------------------- operands beside codes that enter a product as n * 2^-133 (see groups.cu)
 // Eight values in the order of pairs in which masks take eight codes out of a word: (0, 4), (1, 5), (2, 6), (3, 7), all times 2^e and the second and fourth pair
-// also times 2^-4.  e brings the largest value of a row near 2^126 (2^127 as a factor is enough for rows below 1): products stay within fp32, and so do the
-// rest of the row's values down to 2^-120 of the largest.
+// also times 2^-4.  e brings the largest value of a row near 2^118 (2^127 as a factor is enough for rows below 2^-9): products, and sums of values, stay within
+// fp32, and so do the rest of the row's values down to 2^-110 of the largest.
 __device__ __forceinline__ uint32_t top_of_piece(uint4 v) {             // largest magnitude as the bits of a float
     const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
     return max(m & 0xffffu, m >> 16) << 16;
 }
-__device__ __forceinline__ int scale_exponent(uint32_t top) { return min(126 - ((int)(top >> 23) - 127), 127); }      // -2 (NaN, Inf) .. 127
+__device__ __forceinline__ int scale_exponent(uint32_t top) { return min(118 - ((int)(top >> 23) - 127), 127); }      // -10 (NaN, Inf) .. 127
 // sums come in units of 2^(133 - e)
-__device__ __forceinline__ float in_units(float scaled) { return scaled * 0x1p-67f * 0x1p-66f; }          // of a value times 2^e
-__device__ __forceinline__ float from_units(float sum, int e) { return sum * 128.f * exp2i(126 - e); }
+__device__ __forceinline__ float unit_of(int e) { return exp2i(118 - e); }                        // times 2^15; at most 2^127 for finite values
+__device__ __forceinline__ float from_units(float sum, int e) { return sum * 0x1p15f * unit_of(e); }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
 __device__ __forceinline__ uint4 operand_of_piece(uint4 v, int e, float& sum) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    const float f = exp2i(e);
-    float x[8];
+    const uint32_t f = (uint32_t)(e + 127) * 0x00800080u, f4 = f - 4u * 0x00800080u;      // 2^e and 2^(e - 4), twice
+    const float scale = exp2i(e);
+    float s[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16) * f; x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u) * f; }
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s += in_units(x[i]);
-    sum = s;
-    const auto pack = [](float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632); };       // exact: a power of two was multiplied
-    return make_uint4(pack(x[0], x[4]), pack(x[1] * 0.0625f, x[5] * 0.0625f), pack(x[2], x[6]), pack(x[3] * 0.0625f, x[7] * 0.0625f));
+    for (int i = 0; i < 4; ++i) s[i] = fmaf(__uint_as_float(w[i] << 16), scale, __uint_as_float(w[i] & 0xffff0000u) * scale);
+    sum = ((s[0] + s[1]) + (s[2] + s[3])) * 0x1p-67f * 0x1p-66f;         // 2^(e - 133) in all: 2^-133 itself is not a normal number
+    return make_uint4(mul_bf16x2(__byte_perm(w[0], w[2], 0x5410), f), mul_bf16x2(__byte_perm(w[0], w[2], 0x7632), f4),
+                      mul_bf16x2(__byte_perm(w[1], w[3], 0x5410), f), mul_bf16x2(__byte_perm(w[1], w[3], 0x7632), f4));
 }
 
 // a += codes * tokens: mma.sync m16n8k16, rows g and g + 8 from the words a and b of eight codes each, columns from operand_of_piece

@@ -1,4 +1,6 @@
 // 4-bit weights with a scale and a low end per group of 32, 64 or 128 weights of a row: matq_quantize_groups and matq_gemv_groups.
+#include <type_traits>
+
 #include "group4.cuh"
 
 namespace matq {
@@ -65,9 +67,14 @@ cudaError_t launch_quantize(const void* W, int64_t N, int64_t K, int64_t ldw, vo
 // With groups of 32 or 64 the four lanes that share a row hold 4 or 2 groups at a time.  Each group gets columns of its own: token m of group slot s is column
 // m S + s, whose operand is zero in the lanes of the other slots (S = 128 / group).
 //
-// A CTA takes 16 RW rows and a part of K, staged in shared memory for its tokens; its warps are RW row tiles times SK parts of that part, block by block of 128;
-// the CTAs of a cluster share K and add their sums through distributed shared memory, in rank order.  Bound: HBM (and the start of a launch).
-constexpr int kBlock = 128, kWarps = 16, kThreads = 32 * kWarps;
+// A CTA takes a part of K, staged in shared memory for its tokens, and walks the matrix in steps of 16 RW rows; its warps are RW row tiles times SK parts of
+// that part, block by block of 128.  Each warp brings its own blocks into its own ring by cp.async, across the ends of steps, so that the ring never drains.
+// The CTAs of a cluster share K and add their sums through distributed shared memory.  All sums are taken in a fixed order.  Bound: HBM (and the start of a launch).
+constexpr int kBlock = 128;
+// Warps of a CTA: eight, and two CTAs on an SM, as long as a CTA has one block of columns; sixteen beside tokens that take more shared memory.
+__host__ __device__ constexpr int warps_of(int nt) { return nt == 1 ? 8 : 16; }
+__host__ __device__ constexpr int ctas_of(int nt) { return nt > 1 ? 1 : 2; }
+__host__ __device__ constexpr int depth_of(int nt, int mt) { return nt > 1 && mt > 1 ? 3 : nt == 1 && mt == 1 ? 6 : 4; }
 
 struct GemvParams {
     const uint8_t* packed;
@@ -76,16 +83,22 @@ struct GemvParams {
     void* y;
     int64_t N, K, M, ldx, ldy, groups;       // groups of a row
     int tokens;                  // per CTA (a multiple goes to gridDim.z)
-    int sk, rw;                  // sk * rw = kWarps
-    int pass_blocks;             // blocks of 128 staged at a time, a multiple of the ring's turn
+    int sk, rw;                  // sk * rw = the CTA's warps
+    int slice;                   // most blocks of a CTA's part of K
+    int steps;                   // of 16 rw rows
     int early;                   // codes and groups may be fetched before the wait
     int out_bf16;
 };
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool in) {
+    // a warp's next block is the next 64 bytes of the same rows: HBM is asked for more of a row at a time
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool in) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ld_cluster(const float* p, unsigned rank) {
     uint32_t at;
     float v;
@@ -93,229 +106,340 @@ __device__ __forceinline__ float ld_cluster(const float* p, unsigned rank) {
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
     return v;
 }
+__device__ __forceinline__ void store(const GemvParams& P, int64_t m, int64_t row, float v) {
+    if (row >= P.N) return;
+    if (P.out_bf16) static_cast<__nv_bfloat16*>(P.y)[m * P.ldy + row] = __float2bfloat16_rn(v);
+    else static_cast<float*>(P.y)[m * P.ldy + row] = v;
+}
 
-template <int NT, int S>
-__global__ void __launch_bounds__(kThreads, 1) gemv_groups_kernel(const GemvParams P) {
-    constexpr int kDepth = NT >= 4 ? 2 : 4, kSlots = S == 1 ? 1 : 2;
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ uint32_t s_top[32];           // largest magnitude per token (bits of a float)
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
-    const int rt = warp % P.rw, kw = warp / P.rw;
-    const unsigned cl = gridDim.x, rank = blockIdx.x;                   // the cluster is the grid's x
-    const int64_t blocks = (P.K + kBlock - 1) / kBlock;
-    const int64_t b_lo = blocks * rank / cl, b_hi = blocks * (rank + 1) / cl;
-    const int n_blocks = (int)(b_hi - b_lo);
-    const int64_t row0 = (int64_t)blockIdx.y * (16 * P.rw), m0 = (int64_t)blockIdx.z * P.tokens;
-    const int tokens = (int)min((int64_t)P.tokens, P.M - m0);
-    const int64_t row_bytes = P.K / 2;
-
-    // ---- this lane's rows: g and g + 8 of the warp's tile (past the end: the last row, whose sums are not stored)
-    const int64_t r_a = min(row0 + rt * 16 + g, P.N - 1), r_b = min(row0 + rt * 16 + g + 8, P.N - 1);
-    const uint8_t *w_a = P.packed + r_a * row_bytes + 16 * q, *w_b = P.packed + r_b * row_bytes + 16 * q;
-    const uint32_t *p_a = P.params + r_a * P.groups, *p_b = P.params + r_b * P.groups;
-    uint4 wa[kDepth], wb[kDepth];
-    uint32_t pa[kDepth][kSlots], pb[kDepth][kSlots];
-    const auto fetch = [&](int d, int i) {                              // block i of this CTA's part; past the end nothing is read
-        const int64_t blk = b_lo + i;
-        const bool in = i < n_blocks && blk * kBlock + 32 * q < P.K;
-        wa[d] = in ? ld_stream_u4(w_a + blk * (kBlock / 2)) : make_uint4(0u, 0u, 0u, 0u);
-        wb[d] = in ? ld_stream_u4(w_b + blk * (kBlock / 2)) : make_uint4(0u, 0u, 0u, 0u);
+// The exponent of the factor that tokens get as long as each of their elements is zero or lies between 2^-92 and 2^24, so that nothing else has to be known of them.
+constexpr int kUsualExp = 99;
+__device__ __forceinline__ bool unusual(uint4 v) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t most = 0u, least = 0xffffffffu;
 #pragma unroll
-        for (int e = 0; e < kSlots; ++e) {
-            // column 2 q + e belongs to slot (2 q + e) % S
-            const int64_t at = blk * S + (S == 1 ? 0 : (2 * q + e) % S);
-            const bool has = i < n_blocks && at < P.groups;
-            pa[d][e] = has ? __ldg(p_a + at) : 0u;
-            pb[d][e] = has ? __ldg(p_b + at) : 0u;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t m = w[i] & 0x7fff7fffu;
+        most = __vmaxu2(most, m);
+        least = __vminu2(least, __vsub2(m, 0x00010001u));               // zero becomes the largest
+    }
+    return max(most & 0xffffu, most >> 16) >= 0x4b80u || min(least & 0xffffu, least >> 16) < 0x1180u - 1u;
+}
+
+template <int NT, int S, int MT>
+__global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_kernel(const GemvParams P) {
+    constexpr int kWarps = warps_of(NT), kThreads = 32 * kWarps, kDepth = depth_of(NT, MT);
+    constexpr int kSlot = MT * (1024 + 64 * S), kWarpRing = kDepth * kSlot;              // a block's codes and groups of 16 MT rows
+    constexpr int kCols = NT * 8, kTile = 16 * MT, kGroupCopies = (kTile * S + 31) / 32;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ uint32_t s_top[32];           // largest magnitude per token (bits of a float)
+    __shared__ __align__(16) uint4 s_zero[1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
+    const int rt = warp % P.rw, kw = warp / P.rw, rows = kTile * P.rw, rows_shift = 31 - __clz(rows);
+    const unsigned cl = gridDim.x, rank = blockIdx.x;                   // the cluster is the grid's x
+    const int blocks = (int)((P.K + kBlock - 1) / kBlock), b_lo = (int)((int64_t)blocks * rank / cl);
+    const int n_blocks = (int)((int64_t)blocks * (rank + 1) / cl) - b_lo;
+    const int64_t m0 = (int64_t)blockIdx.z * P.tokens;
+    const int tokens = (int)min((int64_t)P.tokens, P.M - m0);
+
+    // shared memory: the warps' rings; tokens [tokens][slice][256 bytes] (+ 64 bytes a token); sums of groups [slice][columns]; results
+    const int x_stride = P.slice * 256 + 64;
+    unsigned char* s_x = smem + kWarps * kWarpRing;
+    float* s_sum = reinterpret_cast<float*>(s_x + (size_t)P.tokens * x_stride);
+    float* s_red = s_sum + (size_t)P.slice * kCols;
+
+    // ---- this warp's blocks, fetched kDepth - 1 ahead: a lane brings 16 bytes of its rows, which it reads itself, and some of the tile's groups
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + (uint32_t)warp * kWarpRing;
+    int f_step = kw < n_blocks ? (int)blockIdx.y : P.steps, f_block = kw, f_at = 0;
+    const uint8_t* f_w[2 * MT];
+    const uint32_t* f_g[kGroupCopies];
+    int f_has[kGroupCopies];                                            // blocks that have this group
+    const int f_in = (int)(P.K / kBlock) + (q < (int)(P.K % kBlock) / 32) - b_lo;         // blocks that have this lane's 32 columns
+#pragma unroll
+    for (int e = 0; e < kGroupCopies; ++e) f_has[e] = lane + 32 * e < kTile * S ? (int)((P.groups - (lane + 32 * e) % S + S - 1) / S) - b_lo : 0;
+    const auto rows_of_step = [&] {                                     // past the end: the last row, whose sums are not stored
+        const int64_t row0 = (int64_t)f_step * rows + rt * kTile;
+#pragma unroll
+        for (int e = 0; e < 2 * MT; ++e) f_w[e] = P.packed + min(row0 + g + 8 * e, P.N - 1) * (P.K / 2) + (int64_t)b_lo * (kBlock / 2) + 16 * q;
+#pragma unroll
+        for (int e = 0; e < kGroupCopies; ++e) f_g[e] = P.params + min(row0 + (lane + 32 * e) / S, P.N - 1) * P.groups + (int64_t)b_lo * S + (lane + 32 * e) % S;
+    };
+    if (f_step < P.steps) rows_of_step();
+    const auto fetch = [&] {
+        if (f_step < P.steps) {
+#pragma unroll
+            for (int e = 0; e < 2 * MT; ++e) copy16(ring + f_at + e * 512 + lane * 16, f_w[e] + f_block * 64, f_block < f_in);
+#pragma unroll
+            for (int e = 0; e < kGroupCopies; ++e)
+                if (kTile * S % 32 == 0 || lane < kTile * S) copy4(ring + f_at + MT * 1024 + (lane + 32 * e) * 4, f_g[e] + f_block * S, f_block < f_has[e]);
+            f_block += P.sk;
+            if (f_block >= n_blocks) {
+                f_block = kw;
+                f_step += gridDim.y;
+                if (f_step < P.steps) rows_of_step();
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        f_at = f_at == (kDepth - 1) * kSlot ? 0 : f_at + kSlot;
+    };
+    if (tid < 32) s_top[tid] = 0u;
+    if (tid == 0) s_zero[0] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = tid; i < P.slice * kCols; i += kThreads) s_sum[i] = 0.f;
+    if (!P.early) after_previous_kernel();
+#pragma unroll 1
+    for (int d = 0; d < kDepth - 1; ++d) fetch();
+    after_previous_kernel();                                            // (at once if it has waited above)
+
+    // ---- the tokens, four pieces of eight elements a thread at a time, scaled and in the order of pairs, and the sums of their groups
+    // Piece 4 q + j of a block goes to place 4 j + q: the four lanes of a row read 64 bytes side by side.  The pieces of all tokens have one running index; those
+    // of a group are neighbours in a warp.
+    const int pieces = n_blocks * 16, all = pieces * tokens, last_piece = (int)min((int64_t)pieces, (P.K - (int64_t)b_lo * kBlock) / 8);
+    const auto each_piece = [&](auto f) {                               // f(the piece, its token, its place in the token's row, whether there is one)
+        int v = 0, i = tid;
+        const __nv_bfloat16* src = P.x + m0 * P.ldx + (int64_t)b_lo * kBlock + tid * 8;
+        const auto settle = [&] {
+            while (i >= pieces && v < tokens) { i -= pieces; src += P.ldx - pieces * 8; ++v; }
+        };
+        for (int f0 = 0; f0 < all; f0 += 4 * kThreads) {
+            uint4 x[4];
+            int pv[4], pi[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                settle();
+                x[n] = v < tokens && i < last_piece ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
+                pv[n] = v;
+                pi[n] = i;
+                i += kThreads;
+                src += kThreads * 8;
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) f(x[n], pv[n], pi[n], pv[n] < tokens);
         }
     };
-    if (!P.early) after_previous_kernel();
+    const auto put = [&](uint4 x, int v, int i, bool in, int e) {
+        float sum;
+        const uint4 o = operand_of_piece(x, e, sum);
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d) fetch(d, kw + d * P.sk);
-    if (P.early) after_previous_kernel();
+        for (int w = 1; w < 16 / S; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+        if (in) {
+            const int place = (i & ~15) | ((i & 3) << 2) | ((i >> 2) & 3);
+            *reinterpret_cast<uint4*>(s_x + (size_t)v * x_stride + place * 16) = o;
+            if ((i & (16 / S - 1)) == 0) s_sum[(i >> 4) * kCols + v * S + (i & 15) / (16 / S)] = sum;
+        }
+    };
+    __syncthreads();
+    bool odd = false;
+    each_piece([&](uint4 x, int v, int i, bool in) {
+        odd |= unusual(x);
+        put(x, v, i, in, kUsualExp);
+    });
+    const bool odd_sizes = __syncthreads_or(odd);
+    if (odd_sizes) {                                                    // then each token by its largest magnitude
+        each_piece([&](uint4 x, int v, int, bool in) {
+            const uint32_t top = top_of_piece(x);
+            if (in && top) atomicMax(&s_top[v], top);
+        });
+        __syncthreads();
+        each_piece([&](uint4 x, int v, int i, bool in) { put(x, v, i, in, in ? scale_exponent(s_top[v]) : kUsualExp); });
+        __syncthreads();
+    }
+
+    // Not before the tokens are here: what the next kernel fetches early would be in their way.
     let_next_kernel_start();
 
-    // ---- shared memory: tokens [tokens][pass_blocks][256 bytes] (+ 64 bytes a token), sums per group [tokens][pass_blocks S], then the warps' results
-    const int x_stride = P.pass_blocks * 256 + 64;
-    float* s_sum = reinterpret_cast<float*>(smem + (size_t)P.tokens * x_stride);
-    const int sum_stride = P.pass_blocks * S;
-    float y[NT][4];
+    // Column 8 nt + g of this lane's operands: a token's, in the quarter of a block that belongs to the column's slot, and zero elsewhere.
+    uint32_t x_at[NT], x_step[NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < NT; ++nt) {
+        const int v = (8 * nt + g) / S;
+        const bool mine = (q * S) / 4 == g % S && v < tokens;
+        x_at[nt] = (uint32_t)__cvta_generic_to_shared(mine ? (const void*)(s_x + (size_t)v * x_stride + q * 16) : (const void*)s_zero);
+        x_step[nt] = mine ? 256u : 0u;
+    }
+    const auto operand = [&](int nt, int i, int j) {
+        uint4 v;
+        const uint32_t at = x_at[nt] + i * x_step[nt] + (x_step[nt] >> 2) * j;
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+        return v;
+    };
+    const int part_floats = kWarps * kTile * (kCols + 1), buffer_floats = part_floats + rows * P.tokens;
+    int at = 0, turn = 0, before = -1;                                  // before: the step whose sums are still with the CTAs of the cluster
+    const auto gather = [&](int step, const float* part) {
+        for (int i = (int)rank * kThreads + tid; i < rows * tokens; i += (int)cl * kThreads) {
+            const int v = i >> rows_shift;
+            float of[8], sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[nt][e] = 0.f;
-    // this lane's operand columns 8 nt + g, and whether its quarter of a block belongs to their slot
-    const bool mine = (q * S) / 4 == g % S;
-
-    for (int p0 = 0; p0 < n_blocks; p0 += P.pass_blocks) {
-        const int here = min(P.pass_blocks, n_blocks - p0);             // blocks of this pass
-        const int64_t k0 = (b_lo + p0) * kBlock;
-        __syncthreads();                                                // the last pass is done with the stage
-        if (tid < 32) s_top[tid] = 0u;
-        __syncthreads();
-        const int pieces = here * 16;                                   // of eight elements, per token
-        for (int v = 0; v < tokens; ++v) {
-            uint32_t top = 0u;
-            for (int i = tid; i < pieces; i += kThreads) {
-                const int64_t k = k0 + i * 8;
-                if (k < P.K) top = max(top, top_of_piece(*reinterpret_cast<const uint4*>(P.x + (m0 + v) * P.ldx + k)));
-            }
-            top = __reduce_max_sync(0xffffffffu, top);
-            if (lane == 0 && top) atomicMax(&s_top[v], top);
+            for (unsigned c = 0; c < 8; ++c) of[c] = c < cl ? ld_cluster(part + i, c) : 0.f;
+#pragma unroll
+            for (unsigned c = 0; c < 8; ++c) sum += of[c];
+            store(P, m0 + v, (int64_t)step * rows + (i & (rows - 1)), sum);
         }
-        __syncthreads();
-        for (int v = 0; v < tokens; ++v) {
-            const int e = scale_exponent(s_top[v]);
-            for (int base = 0; base < pieces; base += kThreads) {       // whole warps: the sums of a group go through shuffles
-                const int i = base + tid;
-                const int64_t k = k0 + (int64_t)i * 8;
-                const bool in = i < pieces && k < P.K;
-                const uint4 x = in ? *reinterpret_cast<const uint4*>(P.x + (m0 + v) * P.ldx + k) : make_uint4(0u, 0u, 0u, 0u);
-                float sum;
-                const uint4 o = operand_of_piece(x, e, sum);
+    };
+    for (int step = blockIdx.y; step < P.steps; step += gridDim.y, turn ^= 1) {
+        float y[MT][NT][4];
 #pragma unroll
-                for (int w = 1; w < 16 / S; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-                if (i < pieces) {
-                    // piece 4 q + j of a block goes to place 4 j + q: the four lanes of a row read 64 bytes side by side
-                    const int at = (i & ~15) | ((i & 3) << 2) | ((i >> 2) & 3);
-                    *reinterpret_cast<uint4*>(smem + (size_t)v * x_stride + at * 16) = o;
-                    if ((i & (16 / S - 1)) == 0) s_sum[v * sum_stride + i / (16 / S)] = sum;
-                }
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[mt][nt][e] = 0.f;
+#pragma unroll 1
+        for (int i = kw; i < n_blocks; i += P.sk) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 2) : "memory");
+            __syncwarp();
+            const unsigned char* slot = smem + (size_t)warp * kWarpRing + at;
+            uint4 w[2 * MT];
+#pragma unroll
+            for (int e = 0; e < 2 * MT; ++e) w[e] = *reinterpret_cast<const uint4*>(slot + e * 512 + lane * 16);
+            uint2 gr[2 * MT];                                           // groups of columns 2 q and 2 q + 1
+#pragma unroll
+            for (int e = 0; e < 2 * MT; ++e) {
+                const unsigned char* p = slot + MT * 1024 + (g + 8 * e) * (4 * S);
+                if (S == 1) gr[e].x = gr[e].y = *reinterpret_cast<const uint32_t*>(p);
+                else gr[e] = *reinterpret_cast<const uint2*>(p + (S == 4 ? 8 * (q & 1) : 0));
             }
-        }
-        __syncthreads();
-
-        float yp[NT][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) yp[nt][e] = 0.f;
-        for (int i0 = kw; i0 < here; i0 += kDepth * P.sk)
-#pragma unroll
-        for (int d = 0; d < kDepth; ++d) {
-            const int i = i0 + d * P.sk;
-            if (i >= here) break;
-            float acc[NT][2][4] = {};
-            const uint32_t wra[4] = {wa[d].x, wa[d].y, wa[d].z, wa[d].w}, wrb[4] = {wb[d].x, wb[d].y, wb[d].z, wb[d].w};
-            uint32_t gpa[kSlots], gpb[kSlots];
-#pragma unroll
-            for (int e = 0; e < kSlots; ++e) { gpa[e] = pa[d][e]; gpb[e] = pb[d][e]; }
-            fetch(d, p0 + i + kDepth * P.sk);
-            const unsigned char* xs = smem + i * 256 + q * 16;
+            at = at == (kDepth - 1) * kSlot ? 0 : at + kSlot;
+            fetch();                                                    // into the slot that was read one block ago
+            constexpr int kChains = MT * NT <= 2 ? 2 : 1;
+            float acc[kChains][MT][NT][4] = {};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t a = wra[j], b = wrb[j], a8 = a >> 8, b8 = b >> 8;
+                uint4 xv[NT];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int v = (8 * nt + g) / S;
-                    uint4 xv = make_uint4(0u, 0u, 0u, 0u);
-                    if (mine && v < tokens) xv = *reinterpret_cast<const uint4*>(xs + (size_t)v * x_stride + j * 64);
-                    mma_bf16(acc[nt][j & 1], a & 0x000f000fu, b & 0x000f000fu, a & 0x00f000f0u, b & 0x00f000f0u, xv.x, xv.y);
-                    mma_bf16(acc[nt][j & 1], a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u, xv.z, xv.w);
+                for (int nt = 0; nt < NT; ++nt) xv[nt] = operand(nt, i, j);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const uint4 wa = w[2 * mt], wb = w[2 * mt + 1];
+                    const uint32_t a = j == 0 ? wa.x : j == 1 ? wa.y : j == 2 ? wa.z : wa.w, b = j == 0 ? wb.x : j == 1 ? wb.y : j == 2 ? wb.z : wb.w;
+                    const uint32_t a8 = a >> 8, b8 = b >> 8;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        mma_bf16(acc[0][mt][nt], a & 0x000f000fu, b & 0x000f000fu, a & 0x00f000f0u, b & 0x00f000f0u, xv[nt].x, xv[nt].y);
+                        mma_bf16(acc[kChains - 1][mt][nt], a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u, xv[nt].z, xv[nt].w);
+                    }
                 }
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
+                const float2 sum = *reinterpret_cast<const float2*>(s_sum + i * kCols + 8 * nt + 2 * q);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int c = 8 * nt + 2 * q + e, v = c / S;
-                    const float sum = v < tokens ? s_sum[v * sum_stride + i * S + c % S] : 0.f;
-                    const uint32_t ga = gpa[S == 1 ? 0 : e], gb = gpb[S == 1 ? 0 : e];
-                    const float ra = (acc[nt][0][e] + acc[nt][1][e]) , rb = (acc[nt][0][2 + e] + acc[nt][1][2 + e]) ;
-                    yp[nt][e] = fmaf(scale_of(ga), ra, fmaf(low_of(ga), sum, yp[nt][e]));
-                    yp[nt][2 + e] = fmaf(scale_of(gb), rb, fmaf(low_of(gb), sum, yp[nt][2 + e]));
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint2 p = gr[2 * mt + (e >> 1)];
+                        const uint32_t group = (e & 1) ? p.y : p.x;
+                        y[mt][nt][e] = fmaf(scale_of(group), kChains == 2 ? acc[0][mt][nt][e] + acc[kChains - 1][mt][nt][e] : acc[0][mt][nt][e], fmaf(low_of(group), (e & 1) ? sum.y : sum.x, y[mt][nt][e]));
+                    }
+            }
+        }
+        // ---- sums over the warps that share a row tile, the slots, and the CTAs of the cluster, each in a fixed order
+        float* red = s_red + turn * buffer_floats;                      // [kw][row][columns]; then [token][row]
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int c = 8 * nt + 2 * q + (e & 1);
+                    if (c < tokens * S) red[(kw * rows + rt * kTile + 16 * mt + g + 8 * (e >> 1)) * (kCols + 1) + c] = from_units(y[mt][nt][e], odd_sizes ? scale_exponent(s_top[c / S]) : kUsualExp);
                 }
-            }
+        __syncthreads();
+        float* part = red + part_floats;
+        for (int i = tid; i < rows * tokens; i += kThreads) {
+            const int v = i >> rows_shift, r = i & (rows - 1);
+            float sum = 0.f;
+            for (int w = 0; w < P.sk; ++w)
+#pragma unroll
+                for (int s = 0; s < S; ++s) sum += red[(w * rows + r) * (kCols + 1) + v * S + s];
+            if (cl > 1) part[i] = sum;
+            else store(P, m0 + v, (int64_t)step * rows + r, sum);
         }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int v = (8 * nt + 2 * q + (e & 1)) / S;
-                y[nt][e] = v < tokens ? y[nt][e] + from_units(yp[nt][e], scale_exponent(s_top[v])) : 0.f;
+        if (cl > 1) {
+            // The CTAs of the cluster meet a step late, so that none waits for another while it has blocks to multiply.
+            if (before >= 0) {
+                cluster_wait();
+                gather(before, s_red + (turn ^ 1) * buffer_floats + part_floats);
             }
-    }
-
-    // ---- sums over the slots, the warps that share a row tile, and the CTAs of the cluster, each in a fixed order
-    const int rows = 16 * P.rw, cols = NT * 8 + 1;
-    float* red = reinterpret_cast<float*>(smem);                        // [kw][row][columns]
-    __syncthreads();
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) red[(size_t)(kw * rows + rt * 16 + g + 8 * (e >> 1)) * cols + 8 * nt + 2 * q + (e & 1)] = y[nt][e];
-    __syncthreads();
-    float* mine_sum = red + (size_t)P.sk * rows * cols;                 // [token][row]
-    for (int i = tid; i < rows * tokens; i += kThreads) {
-        const int v = i / rows, r = i - v * rows;
-        float sum = 0.f;
-        for (int w = 0; w < P.sk; ++w)
-#pragma unroll
-            for (int s = 0; s < S; ++s) sum += red[(size_t)(w * rows + r) * cols + v * S + s];
-        mine_sum[i] = sum;
-    }
-    if (cl > 1) cluster_sync();
-    else __syncthreads();
-    for (int i = (int)rank * kThreads + tid; i < rows * tokens; i += (int)cl * kThreads) {
-        const int v = i / rows;
-        const int64_t r = row0 + i - v * rows;
-        float sum = 0.f;
-        if (cl == 1) sum = mine_sum[i];
-        else
-            for (unsigned c = 0; c < cl; ++c) sum += ld_cluster(mine_sum + i, c);
-        if (r < P.N) {
-            if (P.out_bf16) static_cast<__nv_bfloat16*>(P.y)[(m0 + v) * P.ldy + r] = __float2bfloat16_rn(sum);
-            else static_cast<float*>(P.y)[(m0 + v) * P.ldy + r] = sum;
+            cluster_arrive();
+            before = step;
         }
     }
-    if (cl > 1) cluster_sync();                                         // no CTA leaves while another reads its sums
+    if (cl > 1) {
+        if (before >= 0) {
+            cluster_wait();
+            gather(before, s_red + (turn ^ 1) * buffer_floats + part_floats);
+        }
+        cluster_arrive();                                               // no CTA leaves while another reads its sums
+        cluster_wait();
+    }
 }
 
 struct GemvPlan {
-    int nt, cl, sk, rw, pass_blocks;
-    int64_t tokens, row_blocks, token_blocks;
+    int nt, mt, cl, sk, rw, slice;
+    int64_t tokens, steps, row_ctas, token_blocks;
     size_t smem;
+    double cost;
 };
 
-inline size_t gemv_smem(int tokens, int pass_blocks, int S, int sk, int rw, int nt) {
-    const size_t stage = (size_t)tokens * (pass_blocks * 256 + 64) + (size_t)tokens * pass_blocks * S * 4;
-    const size_t join = ((size_t)sk * 16 * rw * (nt * 8 + 1) + (size_t)16 * rw * tokens) * 4;
-    return stage > join ? stage : join;
+inline size_t gemv_smem(int64_t tokens, int64_t slice, int S, int nt, int mt, int rw) {
+    const size_t warps = warps_of(nt), ring = warps * depth_of(nt, mt) * mt * (1024 + 64 * S), stage = (size_t)tokens * (slice * 256 + 64) + (size_t)slice * nt * 8 * 4;
+    const size_t join = 2 * (warps * 16 * mt * (nt * 8 + 1) + (size_t)tokens * 16 * mt * rw) * 4;
+    return ring + stage + join;
+}
+
+constexpr size_t kSmemOne = 224 * 1024;
+// CTAs on an SM
+inline int on_an_sm(int nt, size_t smem) { return ctas_of(nt) == 2 && 2 * (smem + 1536) <= 227 * 1024 ? 2 : 1; }
+
+// Shape of one choice of columns, cluster, warps per row tile and row tiles per warp, and what it costs (ns); false: it does not fit.  The constants are measurements:
+// 3 us for a dependent launch and its end; the tokens' trip to memory and their staging; a block of 128 of a warp, which takes its chain of latencies, its share of
+// the SM or its share of HBM, whichever is longest; the sums at the end of a step, and those of a cluster.
+inline bool plan_shape(GemvPlan& p, int64_t M, int64_t N, int64_t K, int S, int sms) {
+    const int64_t blocks = (K + kBlock - 1) / kBlock;
+    const int warps = warps_of(p.nt);
+    p.rw = warps / p.sk;
+    p.slice = (int)((blocks + p.cl - 1) / p.cl);
+    p.smem = gemv_smem(p.tokens, p.slice, S, p.nt, p.mt, p.rw);
+    if (p.smem > kSmemOne || p.cl > blocks) return false;
+    p.token_blocks = (M + p.tokens - 1) / p.tokens;
+    const int rows = 16 * p.mt * p.rw, per_sm = on_an_sm(p.nt, p.smem);
+    p.steps = (N + rows - 1) / rows;
+    const int64_t slots = (int64_t)sms * per_sm / p.cl;
+    p.row_ctas = slots / p.token_blocks < 1 ? 1 : slots / p.token_blocks;
+    if (p.row_ctas > p.steps) p.row_ctas = p.steps;
+    const double busy = (double)p.row_ctas * p.token_blocks * p.cl, most = (double)slots * p.cl, at_work = busy < most ? busy : most;
+    const double rounds = (double)((p.steps + p.row_ctas - 1) / p.row_ctas) * (busy / at_work);
+    const double on_sm = at_work <= sms ? 1 : per_sm, tile = p.mt * p.nt * (S == 1 ? 1.0 : 1.15);
+    const double alone = 85 + 150 * tile, shared = (100 + 260 * tile) * warps * on_sm / 16, hbm = (double)p.mt * (1024 + 64 * S) * warps * at_work / 6300.0 * (p.mt == 2 && p.sk == 1 ? 1.6 : 1.0);
+    // (32 rows of 64 bytes at a time and nobody at the rows' next bytes: 65536 x 2304 in 26 us, with two warps to a row 20.5)
+    double block = alone > shared ? alone : shared;
+    if (hbm > block) block = hbm;
+    const double stage = 800 + 80.0 * p.tokens * p.slice / warps, sums = 500 + 60.0 * rows * p.tokens / (32 * warps) + (p.cl > 1 ? 500 + 200 * p.cl : 0);
+    p.cost = 2000 + stage + rounds * ((double)((p.slice + p.sk - 1) / p.sk) * block + sums);
+    return true;
 }
 
 inline GemvPlan plan_gemv(int64_t M, int64_t N, int64_t K, int S, int sms) {
-    GemvPlan p;
-    const int64_t blocks = (K + kBlock - 1) / kBlock, tiles = (N + 15) / 16;
-    p.nt = M * S <= 8 ? 1 : M * S <= 16 ? 2 : 4;
-    p.tokens = p.nt * 8 / S < M ? p.nt * 8 / S : M;
-    p.token_blocks = (M + p.tokens - 1) / p.tokens;
-    p.cl = 1;
-    p.sk = 1;
-    while (p.sk < kWarps && tiles * p.sk * p.token_blocks < (int64_t)sms * kWarps && blocks >= 2 * p.sk) p.sk *= 2;
-    while (p.cl < 8 && ((tiles * p.sk + kWarps - 1) / kWarps) * p.cl * p.token_blocks < sms && blocks >= 4 * p.sk * p.cl) p.cl *= 2;
-    int64_t most = (160 * 1024) / (p.tokens * (256 + 4 * S) + 1);        // blocks that fit
-    const int64_t per = (blocks + p.cl - 1) / p.cl;
-    if (most >= per) {
-        most = per;
-    } else {                                                            // a pass takes whole turns of the ring of prefetched blocks
-        const int depth = p.nt >= 4 ? 2 : 4;
-        while (p.sk > 1 && depth * p.sk > most) p.sk /= 2;
-        most = most / (depth * p.sk) * (depth * p.sk);
+    GemvPlan best, p;
+    best.cost = -1;
+    for (p.nt = 1; p.nt <= 4; p.nt *= 2) {
+        if (p.nt > 1 && M * S <= 4 * p.nt) break;                       // half as many columns would do
+        p.tokens = p.nt * 8 / S < M ? p.nt * 8 / S : M;
+        for (p.mt = 1; p.mt <= (p.nt < 4 ? 2 : 1); ++p.mt)
+            for (p.cl = 1; p.cl <= 8; p.cl *= 2)
+                for (p.sk = 1; p.sk <= warps_of(p.nt); p.sk *= 2)
+                    if (plan_shape(p, M, N, K, S, sms) && (best.cost < 0 || p.cost < best.cost)) best = p;
     }
-    p.rw = kWarps / p.sk;
-    p.row_blocks = (tiles + p.rw - 1) / p.rw;
-    p.pass_blocks = (int)most;
-    p.smem = gemv_smem((int)p.tokens, p.pass_blocks, S, p.sk, p.rw, p.nt);
-    return p;
+    return best;
 }
 
-template <int NT, int S>
+template <int NT, int S, int MT>
 int launch_gemv(const GemvPlan& p, const GemvParams& P, cudaStream_t s) {
     static std::atomic<unsigned long long> smem_ok{0};
-    if (!opt_in_max_smem(gemv_groups_kernel<NT, S>, smem_ok)) return MATQ_ERR_CUDA;
+    if (!opt_in_max_smem(gemv_groups_kernel<NT, S, MT>, smem_ok)) return MATQ_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)p.cl, (unsigned)p.row_blocks, (unsigned)p.token_blocks);
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3((unsigned)p.cl, (unsigned)p.row_ctas, (unsigned)p.token_blocks);
+    cfg.blockDim = dim3(32 * warps_of(NT));
     cfg.dynamicSmemBytes = p.smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -326,13 +450,15 @@ int launch_gemv(const GemvPlan& p, const GemvParams& P, cudaStream_t s) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, gemv_groups_kernel<NT, S>, P) != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, gemv_groups_kernel<NT, S, MT>, P) != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
     return launch_status();
 }
 
 template <int S>
 int launch_gemv_s(const GemvPlan& p, const GemvParams& P, cudaStream_t s) {
-    return p.nt == 1 ? launch_gemv<1, S>(p, P, s) : p.nt == 2 ? launch_gemv<2, S>(p, P, s) : launch_gemv<4, S>(p, P, s);
+    if (p.nt == 4) return launch_gemv<4, S, 1>(p, P, s);
+    if (p.mt == 1) return p.nt == 1 ? launch_gemv<1, S, 1>(p, P, s) : launch_gemv<2, S, 1>(p, P, s);
+    return p.nt == 1 ? launch_gemv<1, S, 2>(p, P, s) : launch_gemv<2, S, 2>(p, P, s);
 }
 
 }  // namespace grp
@@ -366,11 +492,11 @@ extern "C" int matq_gemv_groups(const uint8_t* packed, int64_t N, int64_t K, int
     if (!aligned16(packed) || !aligned16(params) || !aligned16(x)) return MATQ_ERR_ALIGNMENT;
     const int S = kBlock / group;
     const GemvPlan p = plan_gemv(M, N, K, S, sm_count());
-    if (p.row_blocks > 65535 * 16ll || p.token_blocks > 65535) return MATQ_ERR_SHAPE;
+    if (p.cost < 0 || p.steps >= (1ll << 30) || p.row_ctas > 65535 || p.token_blocks > 65535) return MATQ_ERR_SHAPE;
     GemvParams P;
     P.packed = packed; P.params = static_cast<const uint32_t*>(params); P.x = static_cast<const __nv_bfloat16*>(x); P.y = y;
     P.N = N; P.K = K; P.M = M; P.ldx = ldx; P.ldy = ldy; P.groups = K / group;
-    P.tokens = (int)p.tokens; P.sk = p.sk; P.rw = p.rw; P.pass_blocks = p.pass_blocks;
+    P.tokens = (int)p.tokens; P.sk = p.sk; P.rw = p.rw; P.slice = p.slice; P.steps = (int)p.steps;
     P.early = (flags & MATQ_GEMV_PDL) != 0; P.out_bf16 = out_type == MATQ_OUT_BF16;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return S == 1 ? launch_gemv_s<1>(p, P, s) : S == 2 ? launch_gemv_s<2>(p, P, s) : launch_gemv_s<4>(p, P, s);

@@ -65,7 +65,7 @@ def cache_bytes(k_bits, v_bits):
 
 
 def cache_values(tiles):
-    """The cache's bytes to (k, v, middle of v's groups) in 64 bits, [pages, heads, page, D] each; the middle of a group is low + 8 scale."""
+    """The cache's bytes to (k, v, middle of v's groups, 15 scale + |low| and low of k's) in 64 bits, [pages, heads, page, D] each; the middle of a group is low + 8 scale."""
     tiles = np.asarray(tiles)
     D = tiles.shape[-1] // 18
     out = []
@@ -77,9 +77,10 @@ def cache_values(tiles):
         p = np.repeat(np.moveaxis(bf16_values(p).astype(np.float64), 3, 4), GROUP, axis=4)
         shape = (*tiles.shape[:2], -1, D)
         with np.errstate(all="ignore"):
-            out.append(((c * p[..., 0] + p[..., 1]).reshape(shape), (8 * p[..., 0] + p[..., 1]).reshape(shape), (15 * p[..., 0] + np.abs(p[..., 1])).reshape(shape)))
-    (k, _, k_size), (v, mid, _) = out
-    return tuple(torch.from_numpy(np.ascontiguousarray(x)) for x in (k, v, mid, k_size))
+            out.append(((c * p[..., 0] + p[..., 1]).reshape(shape), (8 * p[..., 0] + p[..., 1]).reshape(shape), (15 * p[..., 0] + np.abs(p[..., 1])).reshape(shape),
+                        np.broadcast_to(p[..., 1], c.shape).reshape(shape)))
+    (k, _, k_size, k_low), (v, mid, _, _) = out
+    return tuple(torch.from_numpy(np.ascontiguousarray(x)) for x in (k, v, mid, k_size, k_low))
 
 
 def gemv(codes, params, x):
@@ -94,12 +95,12 @@ def gemv(codes, params, x):
     return x @ W.t(), 2.0 ** -23 * (48 + params.shape[1]) * (x.abs() @ size.t()) + 1e-37
 
 
-def attn(q, tiles, table, cu, kv_len, scale, softcap=0.0, window=0, unpacked=lambda n: False):
-    """(out, bound) in 64 bits, one query row at a time over the keys it sees.  Sequences of n tokens for which unpacked(n) holds see keys and values rounded to bf16.
-    Otherwise p * scale is rounded to 8 bits beside code - 8 (2^-8 of sum_j p_j |v_j - middle_j|); the output is rounded to 8 bits; a score is off by 2^-20 of
-    sum_d |q_d| (15 scale + |low|) at most (a few dozen fp32 steps), which moves weights by a factor; sums in 32 bits add well under 2^-12 of their terms."""
+def attn(q, tiles, table, cu, kv_len, scale, softcap=0.0, window=0, unpacked=lambda n: False, digits=False):
+    """(out, bound) in 64 bits, one query row at a time over the keys it sees.  Sequences of n tokens for which unpacked(n) holds
+    are served in fp16: queries, keys, values and weights are off by 2^-11 of themselves each.  Otherwise p * scale is rounded to 8 bits beside code - 8 (2^-8 of sum_j p_j |v_j - middle_j|); the output is rounded to 8 bits; a score is off by 2^-20 of
+    sum_d |q_d| (15 scale + |low|) at most (a few dozen fp32 steps), and, where queries are taken as 16-bit integers (digits: calls of up to four rows), by 2^-15 of the largest |q_d| times sum_d scale code_d, which moves weights by a factor; sums in 32 bits add well under 2^-12 of their terms."""
     T, Hq, D = q.shape
-    k_all, v_all, mid_all, size_all = cache_values(tiles)
+    k_all, v_all, mid_all, size_all, low_all = cache_values(tiles)
     Hkv, ps = k_all.shape[1], k_all.shape[2]
     G = Hq // Hkv
     out = torch.zeros((T, Hq, D), dtype=torch.float64)
@@ -111,10 +112,8 @@ def attn(q, tiles, table, cu, kv_len, scale, softcap=0.0, window=0, unpacked=lam
             continue
         j = torch.arange(L)
         pages = table[b].cpu().long()[j // ps]
-        k, v, mid, size = (t[pages, :, j % ps] for t in (k_all, v_all, mid_all, size_all))
+        k, v, mid, size, low = (t[pages, :, j % ps] for t in (k_all, v_all, mid_all, size_all, low_all))
         dense = unpacked(n)
-        if dense:
-            k, v = k.float().to(torch.bfloat16).double(), v.float().to(torch.bfloat16).double()
         for i in range(n):
             p = L - n + i
             if p < 0:
@@ -130,7 +129,11 @@ def attn(q, tiles, table, cu, kv_len, scale, softcap=0.0, window=0, unpacked=lam
             spread = torch.einsum("hgj,jhd->hgd", w, vs.abs())
             moved = torch.einsum("hgj,jhd->hgd", w, vs.abs()) + o.abs()
             off = 2.0 ** -20 * scale * torch.einsum("hgd,jhd->hgj", qi.abs(), size[lo:p + 1]).amax(-1, keepdim=True)
-            from_weights = spread if dense else torch.einsum("hgj,jhd->hgd", w, (vs - mid[lo:p + 1]).abs())
+            if digits:
+                off = off + 2.0 ** -15 * scale * qi.abs().amax(-1, keepdim=True) * (k[lo:p + 1] - low[lo:p + 1]).sum(-1).amax(0)[:, None, None]
+            if dense:                                            # a key's elements and a query's, and scores by them
+                off = off + 2.0 ** -10 * scale * torch.einsum("hgd,jhd->hgj", qi.abs(), k[lo:p + 1].abs()).amax(-1, keepdim=True)
+            from_weights = 2.0 ** -2 * spread if dense else torch.einsum("hgj,jhd->hgd", w, (vs - mid[lo:p + 1]).abs())
             bound = 2.0 ** -8 * o.abs() + 2.0 ** -8 * from_weights + 2.0 ** -12 * (spread + from_weights) + torch.expm1(2 * off) * moved + 1e-30
             out[cu[b] + i], tol[cu[b] + i] = o.reshape(Hq, D), bound.reshape(Hq, D)
     return out, tol

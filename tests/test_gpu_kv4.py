@@ -130,7 +130,7 @@ def test_kv4_append_data_errors():
 # ------------------------------------------------------------------ attn_paged4
 
 def _unpacked(longest, G, batch):
-    """Which sequences of a call see keys and values rounded to bf16: with more than 64 rows in the longest, those with more than 16, or a batch of one."""
+    """Which sequences of a call see keys and values in fp16: with more than 64 rows in the longest, those with more than 16, or a batch of one."""
     return lambda n: longest * G > 64 and (n * G > 16 or batch == 1)
 
 
@@ -153,7 +153,7 @@ def _attend(news, lens, Hq, Hkv, D, ps, seed, softcap=0.0, window=0, fill=None, 
                    softcap=softcap, window=window, out=od, dev_status=status)
     got = od.cpu().double()
     assert bool((got[T:] == 9).all()) and bool((out[:, Hq * D:] == 9).all())         # what belongs to nobody is left alone
-    want, tol = gr.attn(q[:T], tiles, table, cu, lens, scale, softcap, window, _unpacked(min(mx[0], T), Hq // Hkv, len(news)))
+    want, tol = gr.attn(q[:T], tiles, table, cu, lens, scale, softcap, window, _unpacked(min(mx[0], T), Hq // Hkv, len(news)), min(mx[0], T) * Hq // Hkv <= 4)
     return got[:T], want, tol, int(host(status)[0])
 
 
@@ -324,10 +324,13 @@ def test_attn_paged4_lengths_below_zero_see_nothing(D, n, length):
 
 
 def test_attn_paged4_stall_times_out_and_recovers():
+    # only the kernels that take unpacked keys and values wait for anything
     assert mq.serving_test_stall(1) == 0
     try:
-        for n, D in ((1, 64), (1, 128), (4, 128), (3, 256), (100, 128)):
-            assert _status([n], [n + 300], 4, 2, D, 16)[1] == mq.ERR_TIMEOUT
+        for n, D in ((1, 64), (4, 128), (3, 256)):
+            _check(*_attend([n], [n + 300], 4, 2, D, 16, seed=16))
+        for D in (64, 128, 256):
+            assert _status([100], [400], 4, 2, D, 16)[1] == mq.ERR_TIMEOUT
     finally:
         assert mq.serving_test_stall(0) == 1
     for n, D in ((1, 64), (1, 128), (4, 128), (3, 256), (100, 128)):
@@ -413,5 +416,5 @@ def test_append_and_attend_as_a_decoder_does():
         args = (table.cuda(), dev(np.array(cu, np.int32)), dev(np.array(lens, np.int32)))
         q = mq.kv4_append(cache, *args, qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], cos_sin=cs, q=qkv[:, :Hq], dev_status=status)
         out = mq.attn_paged4(q, cache, *args, max(news), max(lens), dev_status=status)
-        want, tol = gr.attn(q, host(cache), table, cu, lens, D ** -0.5, unpacked=_unpacked(max(news), Hq // Hkv, len(news)))
+        want, tol = gr.attn(q, host(cache), table, cu, lens, D ** -0.5, unpacked=_unpacked(max(news), Hq // Hkv, len(news)), digits=max(news) * Hq // Hkv <= 4)
         _check(out.double().cpu(), want, tol, int(host(status)[0]))

@@ -16,9 +16,9 @@ namespace matq {
 namespace attn {
 
 constexpr int64_t kMost = (1ll << 31) - 1;                              // lengths are 32-bit numbers
-constexpr int kUnpackPage = 256, kUnpackThreads = 256, kUnpackKeys = 64;
-// Up to kDirectRows rows a call is served by the few-row kernel alone; above, sequences with more than kMixedRows are unpacked (a batch of one whatever it has).
-constexpr int64_t kDirectRows = 64, kMixedRows = 16;
+constexpr int kUnpackPage = 256, kUnpackThreads = 256, kUnpackKeys = 128;
+// In a call that unpacks, sequences with no more rows than this are left to the few-row kernel.
+constexpr int64_t kMixedRows = 16;
 // Bytes of unpacked keys and values that a call's workspace holds at a time: sequences that do not fit together are served one round after another.
 constexpr int64_t kUnpackBytes = 512ll << 20;
 // Most bytes of partial outputs: they are indexed by the call's tokens, of which few may be of sequences that are split.
@@ -30,14 +30,14 @@ struct Unpack {
     const uint8_t* tiles;
     const int32_t *table, *cu_q, *kv_len;
     int64_t table_stride, table_width, n_pages, window, above_rows;
-    int batch, kv_heads, group, page_size;
+    int batch, kv_heads, group, page_size, page_shift;
     int64_t new_width;           // entries of a row of the new table
     int new_pages;               // pages of kUnpackPage keys per sequence
     int32_t* new_table;
     __half *k, *v;               // [batch * new_pages][kv_heads][kUnpackPage][D]
-    uint32_t* top;               // [2][all sequences][kv_heads]: largest magnitudes, as the bits of floats
-    float* scale;                // likewise: what to multiply with afterwards
-    int64_t all, first_seq;      // sequences of the call; the first of this launch
+    uint32_t* top;               // [2][batch][kv_heads][tops]: largest magnitudes of keys and of values, as the bits of floats
+    int64_t tops;
+    float* scale;                // [2][batch][kv_heads]: what to multiply with afterwards
     int32_t* dev_status;
 };
 // The keys that some new token of sequence b sees: [first, kv_len); false: the sequence is not for this call's unpacking.
@@ -52,135 +52,185 @@ __device__ __forceinline__ bool seen_keys(const Unpack& P, int b, Seen& s) {
     s.first = P.window && ctx - P.window + 1 > 0 ? ctx - P.window + 1 : 0;
     return s.kv_len > s.first;
 }
+__device__ __forceinline__ int64_t heads_of(const Unpack& P) { return (int64_t)P.batch * P.kv_heads; }
+// The tile that holds a key, or null where its page is out of range.
+__device__ __forceinline__ const uint8_t* tile_of(const Unpack& P, int b, int h, int64_t key, int D) {
+    const int64_t pg = key >> P.page_shift;
+    const int64_t page = pg < P.table_width ? P.table[(int64_t)b * P.table_stride + pg] : -1;
+    if (page < 0 || page >= P.n_pages) return nullptr;
+    return P.tiles + ((page * P.kv_heads + h) * (P.page_size >> 4) + ((key & (P.page_size - 1)) >> 4)) * kv4::tile_bytes(D);
+}
 __device__ __forceinline__ int half_exponent(uint32_t top) { return max((int)(top >> 23) - 127 - kHalfExp, -126); }        // what was taken off: 2^-126 .. 2^114
 
-// Queries to fp16: a warp per token and head.  The kernel also clears the maxima for those that follow.  Bound: HBM.
+// Before the unpacking, in one launch: queries to fp16 (the first query_ctas CTAs), and the largest magnitudes that the groups of a sequence's keys and values can
+// stand for, per head (the others: kTopTiles tiles of a sequence and head each, whose maximum they leave for the unpacking to join).  Bound: HBM.
+constexpr int kTopTiles = 32, kQueryPieces = 4;
+struct Prepare {
+    Unpack u;
+    const __nv_bfloat16* q;
+    int64_t ldq, T;
+    int q_heads;
+    int64_t query_ctas;
+    __half* to;
+    float* scale;
+};
 template <int D>
-__global__ void __launch_bounds__(kUnpackThreads) attn4_queries_kernel(const __nv_bfloat16* q, int64_t ldq, int64_t T, int q_heads, __half* to, float* scale, uint32_t* top, int64_t n_top) {
+__global__ void __launch_bounds__(kUnpackThreads) attn4_prepare_kernel(const Prepare A) {
     after_previous_kernel();
     let_next_kernel_start();
-    const int lane = threadIdx.x & 31;
-    for (int64_t i = (int64_t)blockIdx.x * kUnpackThreads + threadIdx.x; i < n_top; i += (int64_t)gridDim.x * kUnpackThreads) top[i] = 0u;
-    const int64_t row = (int64_t)blockIdx.x * (kUnpackThreads / 32) + (threadIdx.x >> 5);
-    if (row >= T * q_heads) return;
-    const int64_t t = row / q_heads;
-    constexpr int kEach = D / 32;                                        // elements of a lane: 2, 4 or 8
-    const __nv_bfloat16* src = q + t * ldq + (row - t * q_heads) * D + lane * kEach;
-    uint32_t w[kEach / 2], m = 0u;
-    if constexpr (kEach == 2) {
-        w[0] = *reinterpret_cast<const uint32_t*>(src);
-    } else if constexpr (kEach == 4) {
-        const uint2 v = *reinterpret_cast<const uint2*>(src);
-        w[0] = v.x; w[1] = v.y;
-    } else {
-        const uint4 v = *reinterpret_cast<const uint4*>(src);
-        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-    }
+    const int tid = threadIdx.x;
+    if (blockIdx.x < A.query_ctas) {
+        // a lane takes eight elements; the D / 8 lanes of a row share its largest
+        constexpr int kLanes = D / 8;
+        uint4 v[kQueryPieces];
+        const int64_t first = ((int64_t)blockIdx.x * kQueryPieces * kUnpackThreads + tid) / kLanes, rows = A.T * A.q_heads;
+        const int at = tid % kLanes * 8;
 #pragma unroll
-    for (int i = 0; i < kEach / 2; ++i) m = max(m, max(w[i] << 16 & 0x7fff0000u, w[i] & 0x7fff0000u));
-    const int e = half_exponent(__reduce_max_sync(0xffffffffu, m));
-    const float f = exp2i(-e);
+        for (int i = 0; i < kQueryPieces; ++i) {
+            const int64_t row = first + i * (kUnpackThreads / kLanes), t = rows <= 0x7fffffff ? (int64_t)((uint32_t)row / (uint32_t)A.q_heads) : row / A.q_heads;
+            v[i] = row < rows ? *reinterpret_cast<const uint4*>(A.q + t * A.ldq + (row - t * A.q_heads) * D + at) : make_uint4(0u, 0u, 0u, 0u);
+        }
 #pragma unroll
-    for (int i = 0; i < kEach / 2; ++i) {
-        const __half2 h = __floats2half2_rn(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
-        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-    uint32_t* dst = reinterpret_cast<uint32_t*>(to + row * D + lane * kEach);
-    if constexpr (kEach == 2) *dst = w[0];
-    else if constexpr (kEach == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-    if (lane == 0) scale[row] = exp2i(e);
-}
-
-// The largest magnitudes that the groups of a sequence's keys and values can stand for, per head.  A CTA takes kTopTiles tiles, a thread 16 bytes of groups at a time.
-constexpr int kTopTiles = 32;
-template <int D>
-__global__ void __launch_bounds__(kUnpackThreads) attn4_top_kernel(const Unpack P) {
-    after_previous_kernel();
-    let_next_kernel_start();
-    const int b = blockIdx.y, h = blockIdx.x % P.kv_heads, tid = threadIdx.x;
-    Seen s;
-    if (!seen_keys(P, b, s)) return;
-    const int64_t tile0 = s.first / kv4::kTileKeys + (int64_t)(blockIdx.x / P.kv_heads) * kTopTiles;
-    constexpr int kPieces = D / 16;                                      // of 16 bytes, of a tile's keys' (or values') groups
-    uint32_t most[2] = {0u, 0u};
-    for (int i = tid; i < kTopTiles * kPieces * 2; i += kUnpackThreads) {
-        const int value = i / (kTopTiles * kPieces), r = i % (kTopTiles * kPieces), piece = r % kPieces;
-        const int64_t key = (tile0 + r / kPieces) * kv4::kTileKeys;
-        if (key >= s.kv_len) continue;
-        const int64_t pg = key / P.page_size;
-        const int64_t page = pg < P.table_width ? P.table[(int64_t)b * P.table_stride + pg] : -1;
-        if (page < 0 || page >= P.n_pages) continue;                     // reported by the unpacking
-        const int slot = (int)(key - pg * P.page_size);
-        const uint8_t* half = P.tiles + ((page * P.kv_heads + h) * (P.page_size / kv4::kTileKeys) + slot / kv4::kTileKeys) * kv4::tile_bytes(D) + (value ? kv4::half_bytes(D) : 0);
-        const uint4 v = *reinterpret_cast<const uint4*>(half + kv4::groups_at(D) + piece * 16);
-        const uint32_t g[4] = {v.x, v.y, v.z, v.w};
+        for (int i = 0; i < kQueryPieces; ++i) {
+            const int64_t row = first + i * (kUnpackThreads / kLanes);
+            uint32_t top = top_of_piece(v[i]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t at = key + (piece % 4) * 4 + e;                // the key that the group belongs to
-            const float low = fabsf(low_of(g[e])), high = fabsf(fmaf(15.f, scale_of(g[e]), low_of(g[e])));
-            const float top = fminf(fmaxf(low, high), 3.402823466e38f);
-            if (at >= s.first && at < s.kv_len && scale_of(g[e]) == scale_of(g[e])) {        // not of a group that stands for NaN
-                if (value) most[1] = max(most[1], __float_as_uint(top));
-                else most[0] = max(most[0], __float_as_uint(top));
+            for (int w = 1; w < kLanes; w <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, w));
+            const int e = half_exponent(top);
+            const float f = exp2i(-e);
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            uint32_t o[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const __half2 h = __floats2half2_rn(__uint_as_float(w[x] << 16) * f, __uint_as_float(w[x] & 0xffff0000u) * f);
+                o[x] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            if (row < rows) {
+                *reinterpret_cast<uint4*>(A.to + row * D + at) = make_uint4(o[0], o[1], o[2], o[3]);
+                if (at == 0) A.scale[row] = exp2i(e);
             }
         }
+        return;
     }
+    const Unpack& P = A.u;
+    const unsigned rest = blockIdx.x - (unsigned)A.query_ctas, bh = rest / (unsigned)P.tops;
+    const int b = (int)(bh / (unsigned)P.kv_heads), h = (int)(bh % (unsigned)P.kv_heads), chunk = (int)(rest % (unsigned)P.tops);
+    __shared__ uint32_t s_most[2];
+    if (tid < 2) s_most[tid] = 0u;
+    __syncthreads();
+    Seen s;
+    if (seen_keys(P, b, s)) {
+        const int64_t tile0 = s.first / kv4::kTileKeys + (int64_t)chunk * kTopTiles;
+        constexpr int kPieces = D / 16;                                  // of 16 bytes, of a tile's keys' (or values') groups
+        uint32_t most[2] = {0u, 0u};
+        for (int i = tid; i < kTopTiles * kPieces * 2; i += kUnpackThreads) {
+            const int value = i / (kTopTiles * kPieces), r = i % (kTopTiles * kPieces), piece = r % kPieces;
+            const int64_t key = (tile0 + r / kPieces) * kv4::kTileKeys;
+            const uint8_t* tile = key < s.kv_len ? tile_of(P, b, h, key, D) : nullptr;       // a page out of range is reported by the unpacking
+            if (!tile) continue;
+            const uint4 v = *reinterpret_cast<const uint4*>(tile + (value ? kv4::half_bytes(D) : 0) + kv4::groups_at(D) + piece * 16);
+            const uint32_t g[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-        const uint32_t m = __reduce_max_sync(0xffffffffu, most[v]);
-        if ((tid & 31) == 0 && m) atomicMax(P.top + v * P.all * P.kv_heads + (P.first_seq + b) * P.kv_heads + h, m);
+            for (int e = 0; e < 4; ++e) {
+                const int64_t at = key + (piece % 4) * 4 + e;            // the key that the group belongs to
+                const float low = fabsf(low_of(g[e])), high = fabsf(fmaf(15.f, scale_of(g[e]), low_of(g[e])));
+                const float top = fminf(fmaxf(low, high), 3.402823466e38f);
+                if (at >= s.first && at < s.kv_len && scale_of(g[e]) == scale_of(g[e]))      // not of a group that stands for NaN
+                    most[value] = max(most[value], __float_as_uint(top));
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            const uint32_t m = __reduce_max_sync(0xffffffffu, most[v]);
+            if ((tid & 31) == 0 && m) atomicMax(&s_most[v], m);
+        }
     }
+    __syncthreads();
+    if (tid < 2) P.top[((int64_t)tid * heads_of(P) + bh) * P.tops + chunk] = s_most[tid];
 }
 
-// Keys and values to fp16.  A CTA takes 64 keys of a sequence and key head, a thread eight elements of a key at a time.  Bound: HBM, or the L2 that holds what it writes.
+// Keys and values to fp16: a warp per tile of 16 keys, a lane 32 elements of a key at a time (its codes and those of its neighbours are 512 bytes side by side).
+// Bound: HBM, or the L2 that holds what it writes.
 template <int D>
 __global__ void __launch_bounds__(kUnpackThreads) attn4_unpack_kernel(const Unpack P) {
+    constexpr int kTiles = kUnpackThreads / 32, kCtaKeys = kTiles * kv4::kTileKeys;
+    static_assert(kCtaKeys == kUnpackKeys, "a warp per tile");
+    __shared__ float s_by[2];
     after_previous_kernel();
     let_next_kernel_start();
-    const int b = blockIdx.y, h = blockIdx.x % P.kv_heads, tid = threadIdx.x;
+    const int b = blockIdx.y, h = blockIdx.x % P.kv_heads, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t chunk = blockIdx.x / P.kv_heads;
+    if (warp < 2) {                                                      // the factors of keys and of values
+        uint32_t top = 0u;
+        const uint32_t* from = P.top + ((int64_t)warp * heads_of(P) + (int64_t)b * P.kv_heads + h) * P.tops;
+        for (int64_t i = lane; i < P.tops; i += 32) top = max(top, from[i]);
+        const int e = half_exponent(__reduce_max_sync(0xffffffffu, top));
+        if (lane == 0) {
+            s_by[warp] = exp2i(-e);
+            if (chunk == 0) P.scale[(int64_t)warp * heads_of(P) + (int64_t)b * P.kv_heads + h] = exp2i(e);
+        }
+    }
+    __syncthreads();
     Seen s;
     const bool any = seen_keys(P, b, s);
     const int64_t first_page = any ? s.first / kUnpackPage : 0;
-    float f[2];
-#pragma unroll
-    for (int v = 0; v < 2; ++v) {
-        const int64_t at = v * P.all * P.kv_heads + (P.first_seq + b) * P.kv_heads + h;
-        const int e = half_exponent(P.top[at]);
-        f[v] = exp2i(-e);
-        if (tid == 0 && blockIdx.x / P.kv_heads == 0) P.scale[at] = exp2i(e);
-    }
-    if (h == 0 && blockIdx.x / P.kv_heads == 0)
+    if (h == 0 && chunk == 0)
         for (int64_t i = tid; i < P.new_width; i += kUnpackThreads) {
             const int64_t at = i - first_page;
             P.new_table[b * P.new_width + i] = at >= 0 && at < P.new_pages ? (int)(b * P.new_pages + at) : -1;
         }
     if (!any) return;
-    const int64_t key0 = first_page * kUnpackPage + (int64_t)(blockIdx.x / P.kv_heads) * kUnpackKeys;
-    if (key0 >= s.kv_len || key0 + kUnpackKeys <= s.first) return;
+    const int64_t key0 = first_page * kUnpackPage + chunk * kCtaKeys + warp * kv4::kTileKeys;
+    if (key0 >= s.kv_len || key0 + kv4::kTileKeys <= s.first) return;
     const int64_t at = key0 / kUnpackPage - first_page;
     if (at >= P.new_pages) return;                                      // more keys than the call was told of: the new table has no page for them either
+    const uint8_t* tile = tile_of(P, b, h, key0, D);
+    if (!tile) {
+        if (lane == 0) report(P.dev_status, MATQ_ERR_PAGE);
+        return;
+    }
     const int64_t row0 = ((b * (int64_t)P.new_pages + at) * P.kv_heads + h) * kUnpackPage + key0 % kUnpackPage;
-    constexpr int kPieces = D / 8;                                      // of a key (and as many of its value)
-    for (int i = tid; i < kUnpackKeys * kPieces * 2; i += kUnpackThreads) {
-        const int value = i / (kUnpackKeys * kPieces), r = i % (kUnpackKeys * kPieces), j = r / kPieces, piece = r % kPieces;
-        const int64_t key = key0 + j;
-        if (key >= s.kv_len || key < s.first) continue;
-        const int64_t pg = key / P.page_size;
-        const int64_t page = pg < P.table_width ? P.table[(int64_t)b * P.table_stride + pg] : -1;
-        if (page < 0 || page >= P.n_pages) { report(P.dev_status, MATQ_ERR_PAGE); continue; }
-        const int slot = (int)(key - pg * P.page_size);
-        const uint8_t* half = P.tiles + ((page * P.kv_heads + h) * (P.page_size / kv4::kTileKeys) + slot / kv4::kTileKeys) * kv4::tile_bytes(D) + (value ? kv4::half_bytes(D) : 0);
-        const uint32_t codes = *reinterpret_cast<const uint32_t*>(half + (piece / 4) * 256 + (slot % 16) * 16 + (piece % 4) * 4);
-        const uint32_t group = *reinterpret_cast<const uint32_t*>(half + kv4::groups_at(D) + (piece / 8) * 64 + (slot % 16) * 4);
-        const float by = value ? f[1] : f[0], scale = scale_of(group), low = low_of(group);
-        uint32_t w[4];
+    constexpr int kEach = D / 32, kHalf = D / 2;                        // pieces of a lane, and of a tile's keys
+    uint4 codes[kEach];
+    uint32_t group[kEach];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const __half2 x = __floats2half2_rn(fmaf(scale, (float)((codes >> (8 * e)) & 15u), low) * by, fmaf(scale, (float)((codes >> (8 * e + 4)) & 15u), low) * by);
-            w[e] = *reinterpret_cast<const uint32_t*>(&x);
+    for (int i = 0; i < kEach; ++i) {
+        const int p = lane + 32 * i, value = p / kHalf, r = p % kHalf;
+        const uint8_t* half = tile + value * kv4::half_bytes(D);
+        codes[i] = ld_stream_u4(half + r * 16);
+        group[i] = *reinterpret_cast<const uint32_t*>(half + kv4::groups_at(D) + (r / 32) * 64 + (r % 16) * 4);
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int p = lane + 32 * i, value = p / kHalf, r = p % kHalf;
+        const float by = s_by[value], scale = scale_of(group[i]) * by, mid = fmaf(8.f, scale_of(group[i]), low_of(group[i])) * by;
+        const uint32_t c[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+        uint4* dst = reinterpret_cast<uint4*>((value ? P.v : P.k) + (row0 + r % 16) * D + (r / 16) * 32);
+        const bool wide = (reinterpret_cast<uintptr_t>(P.k) & 31u) == 0 && (reinterpret_cast<uintptr_t>(P.v) & 31u) == 0;       // the workspace is aligned to 16 bytes, or better
+        uint32_t o[2][4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            // (code - 8) / 64 of codes 0 and 4, 1 and 5, 2 and 6, 3 and 7
+            const uint32_t x[4] = {centred_low(c[w]), centred_high(c[w]), centred_low(c[w] >> 8), centred_high(c[w] >> 8)};
+            const auto of = [&](int e) {
+                const float centred = __uint_as_float(e < 4 ? x[e] << 16 : x[e - 4] & 0xffff0000u);
+                return fmaf(scale, centred * 64.f, mid);
+            };
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const __half2 y = __floats2half2_rn(of(2 * e), of(2 * e + 1));
+                o[w & 1][e] = *reinterpret_cast<const uint32_t*>(&y);
+            }
+            if (w & 1) {                                                // 32 bytes, a whole sector, in one store where the address allows it
+                if (wide) {
+                    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst + w - 1), "r"(o[0][0]), "r"(o[0][1]), "r"(o[0][2]), "r"(o[0][3]),
+                                 "r"(o[1][0]), "r"(o[1][1]), "r"(o[1][2]), "r"(o[1][3]) : "memory");
+                } else {
+                    dst[w - 1] = make_uint4(o[0][0], o[0][1], o[0][2], o[0][3]);
+                    dst[w] = make_uint4(o[1][0], o[1][1], o[1][2], o[1][3]);
+                }
+            }
         }
-        *reinterpret_cast<uint4*>((value ? P.v : P.k) + (row0 + j) * D + piece * 8) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
@@ -191,40 +241,33 @@ struct Plan4 {
     int64_t most_rows;           // of its sequences; those with more than above_rows are unpacked
     int64_t above_rows;
     // unpacked sequences; round = 0: there are none
-    int64_t round, new_width, new_pages;
+    int64_t round, new_width, new_pages, tops;
     size_t few_bytes, dense_bytes, table_bytes, query_bytes, scale_bytes, top_bytes, cache_bytes;
     size_t total() const { return few_bytes + dense_bytes + table_bytes + query_bytes + scale_bytes + top_bytes + 2 * cache_bytes; }
 };
 
 inline size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 
-inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
-    Plan4 p;
-    const int group = q_heads / kv_heads;
-    if (max_q > T) max_q = T;
-    if (max_kv > kMost) max_kv = kMost;
-    const bool mixed = max_q * group > kDirectRows;
-    p.few = !mixed || batch > 1;
-    p.most_rows = mixed ? kMixedRows : (1ll << 62);
-    p.above_rows = batch > 1 ? kMixedRows : 0;
-    const int64_t rows = mixed ? kMixedRows : max_q * group;
+// Tiles and split of the few-row kernel for sequences of so many rows, and what they cost (ns): the number of parts of the key range whose rounds over the SMs cost
+// least.  Measured: a step, a tile of 16 keys for each warp of a CTA, alone on an SM or at the share of HBM that the CTAs at work leave each other; a CTA's start and
+// end; the join.  Sequences of a batch are taken to be 0.9 of the longest.
+inline double plan_few(Plan4& p, int64_t rows, int64_t T, int batch, int q_heads, int kv_heads, int D, int64_t max_kv, int64_t window, int sms) {
     p.rows = rows <= 4 ? 4 : D == 256 || rows <= 8 ? 8 : 16;
     p.tiles_per_seq = (rows + p.rows - 1) / p.rows;
     if (p.tiles_per_seq < 1) p.tiles_per_seq = 1;
-    // Parts of the key range: the number whose rounds over the SMs cost least (ns; see plan_kind).
-    const int warps = decode4_warps(D, p.rows), keys = 16 * warps;       // a step: a tile for each warp of a CTA
+    const int warps = decode4_warps(D, p.rows), keys = 16 * warps;
     int64_t range = max_kv;
     if (window > 0 && window < range && window + p.rows + 16 < range) range = window + p.rows + 16;
     range = (range + keys - 1) / keys + 1;
-    const double ctas = (double)p.tiles_per_seq * batch * kv_heads, row_bytes = ctas * p.rows * D * 8;
+    const double ctas = (double)p.tiles_per_seq * batch * kv_heads, row_bytes = ctas * p.rows * D * 8, slots = (double)sms * decode4_ctas(D, p.rows);
     const double bytes = (double)warps * kv4::tile_bytes(D), mean = batch > 1 ? 0.9 : 1.0;
+    const double alone = (D == 256 ? 1100 : D == 128 ? 850 : 500) * (p.rows == 4 ? 1.0 : p.rows == 8 ? 1.2 : 1.45), ends = D == 256 ? 7000 : D == 128 ? 5000 : 4000;
     double best = -1;
     int64_t splits = 1;
-    for (int64_t n = 1; n <= kMaxSplits && n <= range && (n == 1 || (p.few && (double)n * T * q_heads * (D + 2) * 4 <= kPartBytes)); ++n) {
-        const double slots = (double)sms * decode4_ctas(D, p.rows);
+    for (int64_t n = 1; n <= kMaxSplits && n <= range && (n == 1 || (double)n * T * q_heads * (D + 2) * 4 <= kPartBytes); ++n) {
         const double busy = ctas * (n * mean > 1.0 ? n * mean : 1.0), at_work = busy < slots ? busy : slots;
-        const double share = bytes * at_work / 6300.0, alone = (D == 256 ? 1100 : D == 128 ? 850 : 500) * (p.rows == 4 ? 1.0 : p.rows == 8 ? 1.2 : 1.45), step = share > alone ? share : alone;
-        const double part = (double)((range + n - 1) / n) * step + (D == 256 ? 7000 : D == 128 ? 5000 : 4000);
+        const double share = bytes * at_work / 6300.0, step = share > alone ? share : alone;
+        const double part = (double)((range + n - 1) / n) * step + ends;
         const double all = part * busy / slots * (n * mean > 1.0 ? 1.0 : mean);
         const double cost = (busy <= slots ? part : all + part / 2) + (n > 1 ? 3500 + row_bytes * n / 5000.0 : 0);
         if (best < 0 || cost < best) { best = cost; splits = n; }
@@ -233,10 +276,33 @@ inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64
     const int64_t per = (range + splits - 1) / splits;
     p.splits = (range + per - 1) / per;
     p.split_keys = per * keys;
+    return best;
+}
+
+inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
+    Plan4 p;
+    const int group = q_heads / kv_heads;
+    if (max_q > T) max_q = T;
+    if (max_kv > kMost) max_kv = kMost;
+    // Rows of the longest sequence: all of them for the few-row kernel, or unpacking for sequences with more than kMixedRows (a batch of one whatever it has),
+    // whichever costs less.
+    const int64_t rows = max_q * group;
+    const double direct = plan_few(p, rows, T, batch, q_heads, kv_heads, D, max_kv, window, sms);
+    bool mixed = false;
+    if (rows > kMixedRows) {
+        const int64_t range = window > 0 && window + max_q < max_kv ? window + max_q : max_kv;
+        const double dense = 9000 + 4.0 * T * q_heads * D / 6000 + 8.0 * batch * range * kv_heads * D / 5000 + paged_cost(T, batch, q_heads, kv_heads, D, max_q, max_kv, window);
+        mixed = dense < direct;
+    }
+    p.few = !mixed || batch > 1;
+    p.most_rows = mixed ? kMixedRows : (1ll << 62);
+    p.above_rows = batch > 1 ? kMixedRows : 0;
+    if (mixed) plan_few(p, kMixedRows, T, batch, q_heads, kv_heads, D, max_kv, window, sms);
+    if (!p.few) p.splits = 1;
     p.few_bytes = p.splits > 1 ? padded((size_t)p.splits * T * q_heads * (D + 2) * sizeof(float)) : 0;
     p.round = 0;
     p.dense_bytes = p.table_bytes = p.query_bytes = p.scale_bytes = p.top_bytes = p.cache_bytes = 0;
-    p.new_width = p.new_pages = 0;
+    p.new_width = p.new_pages = p.tops = 0;
     if (mixed) {
         p.new_width = (max_kv + kUnpackPage - 1) / kUnpackPage;
         if (p.new_width < 1) p.new_width = 1;
@@ -256,7 +322,8 @@ inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64
         p.table_bytes = padded((size_t)p.round * p.new_width * sizeof(int32_t));
         p.query_bytes = padded((size_t)T * q_heads * D * 2);
         p.scale_bytes = padded((size_t)T * q_heads * sizeof(float));
-        p.top_bytes = padded((size_t)4 * batch * kv_heads * sizeof(float));      // maxima and factors of keys and values
+        p.tops = p.new_pages * kUnpackPage / (kTopTiles * kv4::kTileKeys) + 1;
+        p.top_bytes = padded((size_t)2 * p.round * kv_heads * (p.tops + 1) * sizeof(float));
         p.cache_bytes = padded((size_t)p.round * p.new_pages * kUnpackPage * kv_heads * D * 2);
     }
     return p;
@@ -284,27 +351,18 @@ int launch4(const Params4& P, int rows, unsigned grid, int64_t most_rows, cudaSt
         Params J = {};
         J.out = P.out; J.cu_q = P.cu_q; J.ldo = P.ldo; J.T = P.T; J.batch = P.batch; J.q_heads = P.q_heads; J.group = P.group; J.splits = P.splits;
         J.part_o = P.part_o; J.part_ml = P.part_ml;
-        J.filter = most_rows == kMixedRows; J.above_rows = kMixedRows; J.join_above = 0;
+        J.filter = most_rows == kMixedRows; J.above_rows = kMixedRows; J.join_above = 0;         // the other sequences are joined by their own
         st = launch_join<D>(J, s);
     }
     return st == MATQ_OK ? launch_status() : st;
 }
 
 template <int D>
-int launch_queries(const void* q, int64_t ldq, int64_t T, int q_heads, __half* to, float* scale, uint32_t* top, int64_t n_top, cudaStream_t s) {
-    const int64_t rows = T * q_heads, per = kUnpackThreads / 32;
-    if (launch_overlapped(attn4_queries_kernel<D>, dim3((unsigned)((rows + per - 1) / per)), dim3(kUnpackThreads), 0, s, static_cast<const __nv_bfloat16*>(q), ldq, T, q_heads, to,
-                          scale, top, n_top) != cudaSuccess) {
-        cudaGetLastError();
-        return MATQ_ERR_CUDA;
-    }
-    return launch_status();
-}
-template <int D>
-int launch_unpack(const Unpack& U, int batch, cudaStream_t s) {
-    const int64_t keys = (int64_t)U.new_pages * kUnpackPage, tops = keys / (kTopTiles * kv4::kTileKeys) + 1;
-    if (launch_overlapped(attn4_top_kernel<D>, dim3((unsigned)(tops * U.kv_heads), (unsigned)batch), dim3(kUnpackThreads), 0, s, U) != cudaSuccess ||
-        launch_overlapped(attn4_unpack_kernel<D>, dim3((unsigned)(keys / kUnpackKeys * U.kv_heads), (unsigned)batch), dim3(kUnpackThreads), 0, s, U) != cudaSuccess) {
+int launch_unpack(const Prepare& A, cudaStream_t s) {
+    const Unpack& U = A.u;
+    const int64_t keys = (int64_t)U.new_pages * kUnpackPage;
+    if (launch_overlapped(attn4_prepare_kernel<D>, dim3((unsigned)(A.query_ctas + U.tops * U.kv_heads * U.batch)), dim3(kUnpackThreads), 0, s, A) != cudaSuccess ||
+        launch_overlapped(attn4_unpack_kernel<D>, dim3((unsigned)(keys / kUnpackKeys * U.kv_heads), (unsigned)U.batch), dim3(kUnpackThreads), 0, s, U) != cudaSuccess) {
         cudaGetLastError();
         return MATQ_ERR_CUDA;
     }
@@ -345,7 +403,7 @@ extern "C" int matq_attn_paged4(const matq_paged_kv4* cache, int64_t T, const vo
     const Plan4 p = plan4(T, cache->batch, q_heads, cache->kv_heads, D, max_q, max_kv, window, sm_count());
     const double ctas = (double)p.splits * cache->kv_heads * cache->batch * p.tiles_per_seq;
     const int64_t blocks = p.new_pages * (kUnpackPage / kUnpackKeys);
-    if (ctas >= 2147483648.0 || (p.splits > 1 && T * q_heads >= (1ll << 31)) || (double)blocks * cache->kv_heads >= 2147483648.0 || p.round > 65535 || (p.round && T * q_heads >= (1ll << 31))) return MATQ_ERR_SHAPE;
+    if (ctas >= 2147483648.0 || (p.splits > 1 && T * q_heads >= (1ll << 31)) || (double)blocks * cache->kv_heads >= 2147483648.0 || p.round > 65535 || (double)p.tops * cache->kv_heads * p.round + (double)T * q_heads >= 2147483648.0 || (p.round && T * q_heads >= (1ll << 31))) return MATQ_ERR_SHAPE;
     if (p.total() > workspace_bytes || (p.total() > 0 && !workspace)) return MATQ_ERR_WORKSPACE;
     const float cap = softcap < 0x1p100f ? softcap : 0.f;               // as in matq_attn_paged
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -372,31 +430,32 @@ extern "C" int matq_attn_paged4(const matq_paged_kv4* cache, int64_t T, const vo
     void* dense = at + p.few_bytes;
     unsigned char* next = at + p.few_bytes + p.dense_bytes;
     const auto take = [&](size_t bytes) { unsigned char* here = next; next += bytes; return here; };
-    Unpack U;
+    Prepare A;
+    Unpack& U = A.u;
     U.tiles = P.tiles; U.table_stride = P.table_stride; U.table_width = P.table_width; U.n_pages = P.n_pages; U.window = window; U.above_rows = p.above_rows;
-    U.kv_heads = P.kv_heads; U.group = group; U.page_size = ps; U.new_width = p.new_width; U.new_pages = (int)p.new_pages;
+    U.kv_heads = P.kv_heads; U.group = group; U.page_size = ps; U.page_shift = P.page_shift; U.new_width = p.new_width; U.new_pages = (int)p.new_pages; U.tops = p.tops;
     U.new_table = reinterpret_cast<int32_t*>(take(p.table_bytes));
-    __half* queries = reinterpret_cast<__half*>(take(p.query_bytes));
-    float* q_scale = reinterpret_cast<float*>(take(p.scale_bytes));
-    const int64_t heads = (int64_t)cache->batch * cache->kv_heads;
+    A.to = reinterpret_cast<__half*>(take(p.query_bytes));
+    A.scale = reinterpret_cast<float*>(take(p.scale_bytes));
     U.top = reinterpret_cast<uint32_t*>(take(p.top_bytes));
-    U.scale = reinterpret_cast<float*>(U.top) + 2 * heads;
     U.k = reinterpret_cast<__half*>(take(p.cache_bytes));
     U.v = reinterpret_cast<__half*>(take(p.cache_bytes));
-    U.all = cache->batch;
     U.dev_status = dev_status;
-    st = D == 64 ? launch_queries<64>(q, ldq, T, q_heads, queries, q_scale, U.top, 2 * heads, s) : D == 128 ? launch_queries<128>(q, ldq, T, q_heads, queries, q_scale, U.top, 2 * heads, s)
-         : launch_queries<256>(q, ldq, T, q_heads, queries, q_scale, U.top, 2 * heads, s);
+    A.q = P.q; A.ldq = ldq; A.T = T; A.q_heads = q_heads;
+    const int64_t rows_of_cta = (int64_t)kQueryPieces * kUnpackThreads / (D / 8);
     for (int64_t b0 = 0; b0 < cache->batch && st == MATQ_OK; b0 += p.round) {
         const int n = (int)(cache->batch - b0 < p.round ? cache->batch - b0 : p.round);
-        U.batch = n; U.first_seq = b0; U.table = P.table + b0 * P.table_stride; U.cu_q = P.cu_q + b0; U.kv_len = P.kv_len + b0;
-        st = D == 64 ? launch_unpack<64>(U, n, s) : D == 128 ? launch_unpack<128>(U, n, s) : launch_unpack<256>(U, n, s);
+        const int64_t heads = (int64_t)n * cache->kv_heads;
+        U.batch = n; U.table = P.table + b0 * P.table_stride; U.cu_q = P.cu_q + b0; U.kv_len = P.kv_len + b0;
+        U.scale = reinterpret_cast<float*>(U.top) + 2 * heads * p.tops;
+        A.query_ctas = b0 == 0 ? (T * q_heads + rows_of_cta - 1) / rows_of_cta : 0;
+        st = D == 64 ? launch_unpack<64>(A, s) : D == 128 ? launch_unpack<128>(A, s) : launch_unpack<256>(A, s);
         if (st != MATQ_OK) break;
         matq_paged_kv c;
         c.k = U.k; c.v = U.v; c.n_pages = (int64_t)n * p.new_pages; c.page_size = kUnpackPage; c.kv_heads = P.kv_heads; c.head_dim = D; c.batch = n;
         c.page_table = U.new_table; c.table_stride = c.table_width = p.new_width; c.cu_q = U.cu_q; c.kv_len = U.kv_len;
-        const Half half = {q_scale, U.scale + b0 * cache->kv_heads, U.scale + heads + b0 * cache->kv_heads, p.above_rows};
-        st = paged(&c, T, queries, q_heads, w, scale, softcap, window, max_q, max_kv, out, ldo, dense, p.dense_bytes, &half, dev_status, stream);
+        const Half half = {A.scale, U.scale, U.scale + heads, p.above_rows};
+        st = paged(&c, T, A.to, q_heads, w, scale, softcap, window, max_q, max_kv, out, ldo, dense, p.dense_bytes, &half, dev_status, stream);
     }
     return st;
 }

@@ -116,8 +116,10 @@ __device__ __noinline__ void lift_scores(uint32_t addr, float by) {
 }
 
 // HALF: queries, keys and values are fp16, scaled by powers of two (Params::q_scale and the others; see attn4.cu), and so are the weights.  A weight is at most
-// 2^15 then, and a row takes 0 for its first reference only if its largest weight, and others down to 2^-10 of it, keep all their bits.
-constexpr float kFarHalf = 15.f, kNearHalf = 4.f;
+// 2^15 then, and the reference moves more often; it is taken 4 higher than it is called, so that scores up to 19 above it fit (with 15, one row in a hundred of a
+// prompt moved its reference once: 4096 tokens over 8192 at 32/8 x 128 26 us longer), and a row takes 0 for its first one only if its largest weight is 2^-6 or
+// more: it and those down to 2^-8 of it keep all their bits.  References from kLarge on are taken as they are.
+constexpr float kFarHalf = 15.f, kNearHalf = 6.f, kShiftHalf = 4.f;
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -334,6 +336,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 value_scale = P.v_scale[(int64_t)b * P.kv_heads + h];
             }
             constexpr float kUp = HALF ? kFarHalf : kFar, kDown = HALF ? kNearHalf : kFar;
+            const auto shift = [](float reference) { return HALF && fabsf(reference) < kLarge ? kShiftHalf : 0.f; };
             const Score sc(score_scale, P.softcap);
             const float tanh1 = kShort1 * sc.cap2, tanh2 = kShort2 * sc.cap2, tanh3 = kShort3 * sc.cap2, t_max = P.softcap <= kShortCap ? kTanhMax : -1.f;   // with the cap
             const float unit = CAP ? 1.f : sc.mul;                      // the reference is kept as a score; with the cap, as an exponent
@@ -451,7 +454,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (ok) tc::fence_after();
                 for (int attempt = 0; attempt < 3; ++attempt) {         // the second suffices: nothing lies far above a reference that was just moved
                     use = m == -INFINITY ? 0.f : m * unit;
-                    off = !CAP && lifted && fabsf(use) >= kLarge ? 0.f : -use;
+                    off = (!CAP && lifted && fabsf(use) >= kLarge ? 0.f : -use) - shift(use);
                     if (ok) {
                         if (masked) pass(std::true_type{});
                         else pass(std::false_type{});
@@ -490,7 +493,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         lifted = true;
                     }
                     // O holds the steps before this one.  Their last product is over: with one tile that was waited for, with two the scores' arrival says so.
-                    const float f = raise ? ex2(m * unit - next) : 1.f;
+                    const float f = raise ? ex2(m * unit - next + (shift(m * unit) - shift(next))) : 1.f;
                     if (raise) m = ref;
                     l *= f;
                     if (ok && i > 0) {
@@ -578,7 +581,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
             const float inv = any ? 1.f / l : 0.f;
             if (!ok) *(volatile int*)&s_timeout = 1;
-            if (ok && live && P.splits > 1 && o_col == 0) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(m * unit, l);
+            if (ok && live && P.splits > 1 && o_col == 0) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(m * unit + shift(m * unit), l);
             if (ok && !(P.splits > 1 && n_it == 0)) {
 #pragma unroll 1
                 for (int c = o_col; c < o_col + kOCols; c += 32) {

@@ -95,14 +95,17 @@ def gemv(codes, params, x):
     return x @ W.t(), 2.0 ** -23 * (48 + params.shape[1]) * (x.abs() @ size.t()) + 1e-37
 
 
-def attn(q, tiles, table, cu, kv_len, scale, softcap=0.0, window=0, unpacked=lambda n: False, digits=False):
-    """(out, bound) in 64 bits, one query row at a time over the keys it sees.  Sequences of n tokens for which unpacked(n) holds
-    are served in fp16: queries, keys, values and weights are off by 2^-11 of themselves each.  Otherwise p * scale is rounded to 8 bits beside code - 8 (2^-8 of sum_j p_j |v_j - middle_j|); the output is rounded to 8 bits; a score is off by 2^-20 of
-    sum_d |q_d| (15 scale + |low|) at most (a few dozen fp32 steps), and, where queries are taken as 16-bit integers (digits: calls of up to four rows), by 2^-15 of the largest |q_d| times sum_d scale code_d, which moves weights by a factor; sums in 32 bits add well under 2^-12 of their terms."""
+def attn(q, tiles, table, cu, kv_len, scale, softcap=0.0, window=0, longest=None):
+    """(out, bound) in 64 bits, one query row at a time over the keys it sees.  The output is rounded to 8 bits.  A score is off by 2^-20 of
+    sum_d |q_d| (15 scale + |low|) at most (a few dozen fp32 steps) and, where queries are taken as 16-bit integers (calls of up to four rows: the longest sequence's bound times the heads of a group), by 2^-15 of the
+    largest |q_d| times sum_d scale code_d, which moves weights by a factor.  p * scale is rounded to 8 bits beside code - 8 (2^-8 of sum_j p_j |v_j - middle_j|; with
+    up to four rows to 16).  Calls of more than 16 rows may be served in fp16: queries, keys, values and weights are off by 2^-11 of themselves each; the larger of the two bounds
+    is taken.  Sums in 32 bits add well under 2^-12 of their terms."""
     T, Hq, D = q.shape
     k_all, v_all, mid_all, size_all, low_all = cache_values(tiles)
     Hkv, ps = k_all.shape[1], k_all.shape[2]
     G = Hq // Hkv
+    rows = (T if longest is None else longest) * G
     out = torch.zeros((T, Hq, D), dtype=torch.float64)
     tol = torch.zeros_like(out)
     q = q.cpu().double()
@@ -113,7 +116,6 @@ def attn(q, tiles, table, cu, kv_len, scale, softcap=0.0, window=0, unpacked=lam
         j = torch.arange(L)
         pages = table[b].cpu().long()[j // ps]
         k, v, mid, size, low = (t[pages, :, j % ps] for t in (k_all, v_all, mid_all, size_all, low_all))
-        dense = unpacked(n)
         for i in range(n):
             p = L - n + i
             if p < 0:
@@ -129,11 +131,13 @@ def attn(q, tiles, table, cu, kv_len, scale, softcap=0.0, window=0, unpacked=lam
             spread = torch.einsum("hgj,jhd->hgd", w, vs.abs())
             moved = torch.einsum("hgj,jhd->hgd", w, vs.abs()) + o.abs()
             off = 2.0 ** -20 * scale * torch.einsum("hgd,jhd->hgj", qi.abs(), size[lo:p + 1]).amax(-1, keepdim=True)
-            if digits:
+            if rows <= 4:
                 off = off + 2.0 ** -15 * scale * qi.abs().amax(-1, keepdim=True) * (k[lo:p + 1] - low[lo:p + 1]).sum(-1).amax(0)[:, None, None]
-            if dense:                                            # a key's elements and a query's, and scores by them
-                off = off + 2.0 ** -10 * scale * torch.einsum("hgd,jhd->hgj", qi.abs(), k[lo:p + 1].abs()).amax(-1, keepdim=True)
-            from_weights = 2.0 ** -2 * spread if dense else torch.einsum("hgj,jhd->hgd", w, (vs - mid[lo:p + 1]).abs())
+            if rows > 16:
+                off = torch.maximum(off, 2.0 ** -10 * scale * torch.einsum("hgd,jhd->hgj", qi.abs(), k[lo:p + 1].abs()).amax(-1, keepdim=True))
+            from_weights = 2.0 ** (-8 if rows <= 4 else 0) * torch.einsum("hgj,jhd->hgd", w, (vs - mid[lo:p + 1]).abs())
+            if rows > 16:
+                from_weights = torch.maximum(from_weights, 2.0 ** -2 * spread)
             bound = 2.0 ** -8 * o.abs() + 2.0 ** -8 * from_weights + 2.0 ** -12 * (spread + from_weights) + torch.expm1(2 * off) * moved + 1e-30
             out[cu[b] + i], tol[cu[b] + i] = o.reshape(Hq, D), bound.reshape(Hq, D)
     return out, tol

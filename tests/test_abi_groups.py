@@ -82,7 +82,7 @@ def test_attn_paged4_refusals():
     for kw in (dict(q=P + 8), dict(out=P + 8), dict(ws=P + 8), dict(tiles=P + 8)):
         assert call(**kw) == mq.ERR_ALIGNMENT, kw
     assert call(max_kv=100000, ws=NULL, ws_bytes=0) == mq.ERR_WORKSPACE
-    assert call(T=500, max_q=500, ws=NULL, ws_bytes=0) == mq.ERR_WORKSPACE
+    assert call(T=4000, max_q=4000, max_kv=8000, ws=NULL, ws_bytes=0) == mq.ERR_WORKSPACE
     big = (1 << 31) - 1
     assert call(kv_heads=1 << 22, qh=1 << 22, ldq=1 << 28, ldo=1 << 28, batch=big, T=big, ws=NULL, ws_bytes=0) == mq.ERR_SHAPE         # a grid of 2^53
     assert call(T=0) == mq.OK and call(batch=0) == mq.OK

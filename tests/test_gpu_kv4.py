@@ -129,11 +129,6 @@ def test_kv4_append_data_errors():
 
 # ------------------------------------------------------------------ attn_paged4
 
-def _unpacked(longest, G, batch):
-    """Which sequences of a call see keys and values in fp16: with more than 64 rows in the longest, those with more than 16, or a batch of one."""
-    return lambda n: longest * G > 64 and (n * G > 16 or batch == 1)
-
-
 def _attend(news, lens, Hq, Hkv, D, ps, seed, softcap=0.0, window=0, fill=None, edit=None, hints=None, scale=None, qstd=1.5, qmul=1.0):
     T = sum(news)
     kb, vb, table = gr.make_cache(lens, Hkv, D, ps, seed, fill=fill)
@@ -153,7 +148,7 @@ def _attend(news, lens, Hq, Hkv, D, ps, seed, softcap=0.0, window=0, fill=None, 
                    softcap=softcap, window=window, out=od, dev_status=status)
     got = od.cpu().double()
     assert bool((got[T:] == 9).all()) and bool((out[:, Hq * D:] == 9).all())         # what belongs to nobody is left alone
-    want, tol = gr.attn(q[:T], tiles, table, cu, lens, scale, softcap, window, _unpacked(min(mx[0], T), Hq // Hkv, len(news)), min(mx[0], T) * Hq // Hkv <= 4)
+    want, tol = gr.attn(q[:T], tiles, table, cu, lens, scale, softcap, window, min(mx[0], T))
     return got[:T], want, tol, int(host(status)[0])
 
 
@@ -200,7 +195,7 @@ def test_attn_paged4_fewer_tokens_than_rows_and_bounds():
         cu = [0, 2, 3][:len(lens) + 1]
         out = torch.full((100, 8, 128), 9.0, dtype=torch.bfloat16, device="cuda")
         mq.attn_paged4(q.cuda(), dev(tiles), table.cuda(), dev(np.array(cu, np.int32)), dev(np.array(lens, np.int32)), 100, 4000, out=out, dev_status=status)
-        want, tol = gr.attn(q[:cu[-1]], tiles, table, cu, lens, 128 ** -0.5, unpacked=_unpacked(100, 4, len(lens)))
+        want, tol = gr.attn(q[:cu[-1]], tiles, table, cu, lens, 128 ** -0.5, longest=100)
         _check(out[:cu[-1]].double().cpu(), want, tol, int(host(status)[0]))
         assert bool((out[cu[-1]:] == 9).all())
 
@@ -312,7 +307,7 @@ def test_attn_paged4_data_errors():
         assert _status([n], [n + 40], 4, 2, D, 16, cu_dev=[0, n + 5])[1] == mq.ERR_PAGE
         assert _status([n], [n + 40], 4, 2, D, 16)[1] == mq.OK
     # more keys than the call was told of
-    assert _status([100], [2000], 4, 2, 128, 16, hints=(100, 300))[1] == mq.ERR_PAGE
+    assert _status([1500], [3000], 16, 2, 128, 16, hints=(1500, 1600))[1] == mq.ERR_PAGE
 
 
 @pytest.mark.parametrize("D", [64, 128, 256])
@@ -330,7 +325,7 @@ def test_attn_paged4_stall_times_out_and_recovers():
         for n, D in ((1, 64), (4, 128), (3, 256)):
             _check(*_attend([n], [n + 300], 4, 2, D, 16, seed=16))
         for D in (64, 128, 256):
-            assert _status([100], [400], 4, 2, D, 16)[1] == mq.ERR_TIMEOUT
+            assert _status([1500], [3000], 16, 2, D, 16)[1] == mq.ERR_TIMEOUT
     finally:
         assert mq.serving_test_stall(0) == 1
     for n, D in ((1, 64), (1, 128), (4, 128), (3, 256), (100, 128)):
@@ -416,5 +411,5 @@ def test_append_and_attend_as_a_decoder_does():
         args = (table.cuda(), dev(np.array(cu, np.int32)), dev(np.array(lens, np.int32)))
         q = mq.kv4_append(cache, *args, qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], cos_sin=cs, q=qkv[:, :Hq], dev_status=status)
         out = mq.attn_paged4(q, cache, *args, max(news), max(lens), dev_status=status)
-        want, tol = gr.attn(q, host(cache), table, cu, lens, D ** -0.5, unpacked=_unpacked(max(news), Hq // Hkv, len(news)), digits=max(news) * Hq // Hkv <= 4)
+        want, tol = gr.attn(q, host(cache), table, cu, lens, D ** -0.5, longest=max(news))
         _check(out.double().cpu(), want, tol, int(host(status)[0]))

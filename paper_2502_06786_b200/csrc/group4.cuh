@@ -16,37 +16,66 @@ __device__ __forceinline__ float exp2i(int e) { return __int_as_float((e + 127) 
 
 __device__ __forceinline__ uint32_t bf16_rne(float x) { return (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x)); }
 
+// Two binary32 operations per instruction.  A sum of such products is taken one by one: the two together come out as one fused operation, whatever they say of rounding.
+__device__ __forceinline__ uint64_t two(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t two_sums(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t two_products(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// range / 15 and 1 / scale with the result of a correctly rounded division: a quotient from the rounded reciprocal, corrected by its exact residual, is (Markstein); a
+// Newton step on a reciprocal that is off by 2^-23 leaves 2^-46, and 1 / scale, the scale having eight bits, is no nearer than 2^-33 to the middle of two numbers.
+__device__ __forceinline__ float fifteenth(float range) {
+    constexpr float k = 1.f / 15.f;
+    const float q = range * k;
+    return fmaf(fmaf(-15.f, q, range), k, q);
+}
+__device__ __forceinline__ float inverse(float scale) {                 // of a normal number with eight bits
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(scale));
+    return fmaf(fmaf(-scale, y, 1.f), y, y);
+}
+
 // Codes (element i in bits 4 i) and group of eight of a group's values; the LANES neighbouring lanes that hold the group call it together.
 template <int LANES>
 __device__ __forceinline__ uint32_t quantise_piece(uint4 v, uint32_t& codes, uint32_t lanes = 0xffffffffu) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     const auto h = [](uint32_t u) { return *reinterpret_cast<const __nv_bfloat162*>(&u); };
     const auto u = [](__nv_bfloat162 b) { return *reinterpret_cast<const uint32_t*>(&b); };
-    __nv_bfloat162 lo = __hmin2_nan(__hmin2_nan(h(w[0]), h(w[1])), __hmin2_nan(h(w[2]), h(w[3])));
-    __nv_bfloat162 hi = __hmax2_nan(__hmax2_nan(h(w[0]), h(w[1])), __hmax2_nan(h(w[2]), h(w[3])));
+    // the smallest value, and the largest one with its sign turned, side by side: one shuffle and one minimum a step (NaN stays NaN)
+    const uint32_t lo = u(__hmin2_nan(__hmin2_nan(h(w[0]), h(w[1])), __hmin2_nan(h(w[2]), h(w[3]))));
+    const uint32_t hi = u(__hmax2_nan(__hmax2_nan(h(w[0]), h(w[1])), __hmax2_nan(h(w[2]), h(w[3])))) ^ 0x80008000u;
+    uint32_t ends = u(__hmin2_nan(h(__byte_perm(lo, hi, 0x5410)), h(__byte_perm(lo, hi, 0x7632))));
 #pragma unroll
-    for (int s = 1; s < LANES; s <<= 1) {
-        lo = __hmin2_nan(lo, h(__shfl_xor_sync(lanes, u(lo), s)));
-        hi = __hmax2_nan(hi, h(__shfl_xor_sync(lanes, u(hi), s)));
-    }
-    const float low = __bfloat162float(__hmin_nan(__low2bfloat16(lo), __high2bfloat16(lo))) + 0.f;         // -0 becomes 0
-    const float range = __fsub_rn(__bfloat162float(__hmax_nan(__low2bfloat16(hi), __high2bfloat16(hi))), low);
-    codes = 0u;
-    if (!(range <= 3.402823466e38f)) return kNoGroup;
-    uint32_t scale = bf16_rne(__fdiv_rn(range, 15.f));
-    if (__uint_as_float(scale << 16) < 0x1p-120f) scale = 0u;
-    if (scale) {
-        const float inv = __frcp_rn(__uint_as_float(scale << 16));
-        // adding 1.5 * 2^23 rounds to a whole number, half to even, and leaves it in the low bits: the word of sums below is taken modulo 2^32
-        uint32_t sum = 0u;
+    for (int s = 1; s < LANES; s <<= 1) ends = u(__hmin2_nan(h(ends), h(__shfl_xor_sync(lanes, ends, s))));
+    const float low = __uint_as_float(ends << 16) + 0.f;                // -0 becomes 0
+    const float range = __fsub_rn(__uint_as_float((ends & 0xffff0000u) ^ 0x80000000u), low);
+    uint32_t scale = bf16_rne(fifteenth(range));
+    const bool flat = __uint_as_float(scale << 16) < 0x1p-120f;
+    if (flat) scale = 0u;
+    const float inv = flat ? 0.f : inverse(__uint_as_float(scale << 16));
+    // adding 1.5 * 2^23 rounds to a whole number, half to even, and leaves it in the low bits: the word of sums below is taken modulo 2^32
+    const uint64_t less = two(-low, -low), by = two(inv, inv);
+    uint32_t sum = 0u;
 #pragma unroll
-        for (int i = 7; i >= 0; --i) {
-            const float x = __uint_as_float((i & 1) ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
-            sum = sum * 16u + __float_as_uint(__fadd_rn(__fmul_rn(__fsub_rn(x, low), inv), 12582912.f));
-        }
-        codes = sum - 0x4b400000u * 0x11111111u;
+    for (int i = 3; i >= 0; --i) {
+        const uint64_t t = two_products(two_sums(two(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), less), by);
+        const uint32_t even = __float_as_uint(__fadd_rn(__uint_as_float((uint32_t)t), 12582912.f)), odd = __float_as_uint(__fadd_rn(__uint_as_float((uint32_t)(t >> 32)), 12582912.f));
+        sum = (sum * 16u + odd) * 16u + even;
     }
-    return scale | (__float_as_uint(low) & 0xffff0000u);
+    const bool none = !(range <= 3.402823466e38f);
+    codes = none ? 0u : sum - 0x4b400000u * 0x11111111u;
+    return none ? kNoGroup : scale | (__float_as_uint(low) & 0xffff0000u);
 }
 
 // ---------------------------------------------------------------- operands beside codes that enter a product as n * 2^-133 (see groups.cu)

@@ -8,13 +8,16 @@
 namespace matq {
 namespace kva4 {
 
-constexpr int kThreads = 256;
+// Threads of a token: 256 in a decode step, where a call is a chain of trips to memory; for many tokens 64, which share what is looked up among fewer warps (three
+// prompts of 1500 to 4000 tokens, 16/8 heads of 256: 75 us with 256).
+constexpr int kThreadsFew = 256, kThreadsMany = 64;
+constexpr int64_t kMany = 2048;
 
 struct Params {
     uint8_t* cache;
     const int32_t *table, *cu_q, *kv_len;
     int64_t n_pages, table_stride, table_width;
-    int page_size, kv_heads, q_heads, D, batch;
+    int page_size, kv_heads, q_heads, batch;
     const __nv_bfloat16 *q, *k, *v;
     int64_t ldq, ldk, ldv, ldqo;
     const float* cos_sin;
@@ -26,25 +29,26 @@ struct Params {
 
 constexpr int kAhead = 2;        // heads per thread whose data are requested before the position is known
 
-__global__ void __launch_bounds__(kThreads, 4) kv4_append_kernel(const Params P) {
+template <int D, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) kv4_append_kernel(const Params P) {
+    constexpr int kPlaces = D / 8, kStep = kThreads / kPlaces;          // 8, 16 or 32 threads along a head; heads side by side
     after_previous_kernel();
     let_next_kernel_start();
     const int64_t t = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 31;
-    const int heads = P.q_heads + 2 * P.kv_heads, half = P.rot / 2;
-    const int places = P.D / 8, step = kThreads / places;              // 8, 16 or 32 threads along a head; heads side by side
-    const int first = tid / places, e0 = (tid - first * places) * 8;
+    const int keys_from = P.q_heads, values_from = P.q_heads + P.kv_heads, heads = values_from + P.kv_heads, half = P.rot / 2;
+    const int first = tid / kPlaces, e0 = tid % kPlaces * 8;
     const bool turns = e0 < P.rot, paired = turns && !P.interleaved, upper = paired && e0 >= half;
-    const int partner = paired ? upper ? e0 - half : e0 + half : e0;
+    const int partner = (paired ? upper ? e0 - half : e0 + half : e0) - e0;
+    // this thread's place in a head of each kind, as if the heads of all kinds stood one behind another
+    const __nv_bfloat16 *q_at = P.q + t * P.ldq + e0, *k_at = P.k + t * P.ldk + e0 - (int64_t)keys_from * D, *v_at = P.v + t * P.ldv + e0 - (int64_t)values_from * D;
     uint4 data[kAhead][2];
     const auto load = [&](int hd, uint4 (&d)[2]) {
         d[0] = d[1] = make_uint4(0u, 0u, 0u, 0u);
         if (hd >= heads) return;
-        const bool value = hd >= P.q_heads + P.kv_heads;
-        const __nv_bfloat16* row = hd < P.q_heads ? P.q + t * P.ldq + (int64_t)hd * P.D
-                                   : value ? P.v + t * P.ldv + (int64_t)(hd - P.q_heads - P.kv_heads) * P.D : P.k + t * P.ldk + (int64_t)(hd - P.q_heads) * P.D;
-        d[0] = *reinterpret_cast<const uint4*>(row + e0);
-        if (paired && !value) d[1] = *reinterpret_cast<const uint4*>(row + partner);
+        const __nv_bfloat16* at = (hd < keys_from ? q_at : hd < values_from ? k_at : v_at) + (int64_t)hd * D;
+        d[0] = *reinterpret_cast<const uint4*>(at);
+        if (paired && hd < values_from) d[1] = *reinterpret_cast<const uint4*>(at + partner);
     };
 
     // the token's sequence: the number of sequences that end at or before it (32 bounds per step, every warp for itself)
@@ -56,11 +60,11 @@ __global__ void __launch_bounds__(kThreads, 4) kv4_append_kernel(const Params P)
     }
     if (b >= P.batch) return;                                          // a row that belongs to no sequence (and is not read)
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) load(first + i * step, data[i]);
+    for (int i = 0; i < kAhead; ++i) load(first + i * kStep, data[i]);
     const int64_t q0 = P.cu_q[b], q1 = P.cu_q[b + 1];
     const int64_t pos = (int64_t)P.kv_len[b] - (q1 - q0) + (t - q0);
-    const int64_t pg = pos / P.page_size;
-    bool ok = pos >= 0 && t >= q0 && pg < P.table_width && (P.rot == 0 || pos < P.max_pos);
+    const unsigned pg = pos >= 0 && pos <= 0x7fffffff ? (unsigned)pos / (unsigned)P.page_size : 0xffffffffu;
+    bool ok = pg != 0xffffffffu && t >= q0 && pg < P.table_width && (P.rot == 0 || pos < P.max_pos);
     int64_t page = 0;
     if (ok) {
         page = P.table[(int64_t)b * P.table_stride + pg];
@@ -70,69 +74,73 @@ __global__ void __launch_bounds__(kThreads, 4) kv4_append_kernel(const Params P)
         if (tid == 0) report(P.dev_status, MATQ_ERR_PAGE);
         return;
     }
-    const int slot = (int)(pos - pg * P.page_size);
-    // angles: of eight pairs when pairs are halves apart, of four when they are neighbours
+    const unsigned slot = (unsigned)pos - pg * (unsigned)P.page_size, key = slot % kv4::kTileKeys;
+    // angles: of eight pairs when pairs are halves apart, of four when they are neighbours.  a c - b s is a c + b (-s): the sign goes with the angle.
     float c[8], s[8];
     if (turns) {
         const float* cs = P.cos_sin + pos * P.rot + (paired ? upper ? e0 - half : e0 : e0 / 2);
+        const float sign = upper || !paired ? 1.f : -1.f;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             if (i == 1 && !paired) break;
             const float4 cv = *reinterpret_cast<const float4*>(cs + 4 * i), sv = *reinterpret_cast<const float4*>(cs + half + 4 * i);
             c[4 * i] = cv.x; c[4 * i + 1] = cv.y; c[4 * i + 2] = cv.z; c[4 * i + 3] = cv.w;
-            s[4 * i] = sv.x; s[4 * i + 1] = sv.y; s[4 * i + 2] = sv.z; s[4 * i + 3] = sv.w;
+            s[4 * i] = sv.x * sign; s[4 * i + 1] = sv.y * sign; s[4 * i + 2] = sv.z * sign; s[4 * i + 3] = sv.w * sign;
         }
     }
     // Every product and sum is rounded by itself: the values that are quantised are defined bit for bit.
     const auto turned = [&](const uint4 (&d)[2]) {
         const uint32_t o[4] = {d[0].x, d[0].y, d[0].z, d[0].w}, p[4] = {d[1].x, d[1].y, d[1].z, d[1].w};
+        const auto both = [](uint32_t w) { return two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); };
         uint32_t r[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float x0 = __uint_as_float(o[i] << 16), x1 = __uint_as_float(o[i] & 0xffff0000u);
-            float y0, y1;
+            uint64_t u, w;
             if (paired) {
-                const float z0 = __uint_as_float(p[i] << 16), z1 = __uint_as_float(p[i] & 0xffff0000u);
-                const float u0 = __fmul_rn(x0, c[2 * i]), u1 = __fmul_rn(x1, c[2 * i + 1]), w0 = __fmul_rn(z0, s[2 * i]), w1 = __fmul_rn(z1, s[2 * i + 1]);
-                y0 = upper ? __fadd_rn(u0, w0) : __fsub_rn(u0, w0);
-                y1 = upper ? __fadd_rn(u1, w1) : __fsub_rn(u1, w1);
+                u = two_products(both(o[i]), two(c[2 * i], c[2 * i + 1]));
+                w = two_products(both(p[i]), two(s[2 * i], s[2 * i + 1]));
             } else {
-                y0 = __fsub_rn(__fmul_rn(x0, c[i]), __fmul_rn(x1, s[i]));
-                y1 = __fadd_rn(__fmul_rn(x1, c[i]), __fmul_rn(x0, s[i]));
+                u = two_products(both(o[i]), two(c[i], c[i]));
+                w = two_products(both(__byte_perm(o[i], 0u, 0x1032)), two(-s[i], s[i]));
             }
-            r[i] = bf16_rne(y0) | (bf16_rne(y1) << 16);
+            const __nv_bfloat162 h = __floats2bfloat162_rn(__fadd_rn(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)w)),
+                                                           __fadd_rn(__uint_as_float((uint32_t)(u >> 32)), __uint_as_float((uint32_t)(w >> 32))));
+            r[i] = *reinterpret_cast<const uint32_t*>(&h);
         }
         return make_uint4(r[0], r[1], r[2], r[3]);
     };
+    __nv_bfloat16* q_to = P.q_out + t * P.ldqo + e0;
+    const int64_t head_bytes = (int64_t)(P.page_size / kv4::kTileKeys) * kv4::tile_bytes(D);
+    uint8_t* tile = P.cache + page * P.kv_heads * head_bytes + (int64_t)(slot / kv4::kTileKeys) * kv4::tile_bytes(D);
+    const int codes_at = e0 / 32 * 256 + (int)key * 16 + e0 % 32 / 2, group_at = kv4::groups_at(D) + e0 / 64 * 64 + (int)key * 4;
     bool bad = false;
     const auto finish = [&](int hd, const uint4 (&d)[2]) {
         if (hd >= heads) return;                                        // the lanes of a group share their head
-        const bool value = hd >= P.q_heads + P.kv_heads;
+        const bool value = hd >= values_from;
         const uint4 x = turns && !value ? turned(d) : d[0];
-        if (hd < P.q_heads) {
-            *reinterpret_cast<uint4*>(P.q_out + t * P.ldqo + (int64_t)hd * P.D + e0) = x;
+        if (hd < keys_from) {
+            *reinterpret_cast<uint4*>(q_to + (int64_t)hd * D) = x;
             return;
         }
         uint32_t codes;
         const uint32_t group = quantise_piece<8>(x, codes, 0xffu << (lane & 24));
-        const int h = hd - P.q_heads - (value ? P.kv_heads : 0), key = slot % kv4::kTileKeys;
-        uint8_t* tile = P.cache + ((page * P.kv_heads + h) * (P.page_size / kv4::kTileKeys) + slot / kv4::kTileKeys) * kv4::tile_bytes(P.D) + (value ? kv4::half_bytes(P.D) : 0);
-        *reinterpret_cast<uint32_t*>(tile + (e0 / 32) * 256 + key * 16 + (e0 % 32) / 2) = codes;
+        uint8_t* to = tile + (hd - (value ? values_from : keys_from)) * head_bytes + (value ? kv4::half_bytes(D) : 0);
+        *reinterpret_cast<uint32_t*>(to + codes_at) = codes;
         if ((lane & 7) == 0) {
-            *reinterpret_cast<uint32_t*>(tile + kv4::groups_at(P.D) + (e0 / 64) * 64 + key * 4) = group;
+            *reinterpret_cast<uint32_t*>(to + group_at) = group;
             bad |= group == kNoGroup;
         }
     };
     // Rotating in place, a thread's partners are another thread's output: all heads of a turn are read before any is written, and no two turns share a head.
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) finish(first + i * step, data[i]);
-    for (int h0 = kAhead * step; h0 < heads; h0 += kAhead * step) {
+    for (int i = 0; i < kAhead; ++i) finish(first + i * kStep, data[i]);
+    for (int h0 = kAhead * kStep; h0 < heads; h0 += kAhead * kStep) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) load(h0 + first + i * step, data[i]);
+        for (int i = 0; i < kAhead; ++i) load(h0 + first + i * kStep, data[i]);
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) finish(h0 + first + i * step, data[i]);
+        for (int i = 0; i < kAhead; ++i) finish(h0 + first + i * kStep, data[i]);
     }
     if (bad) report(P.dev_status, MATQ_ERR_NONFINITE);
 }
@@ -167,13 +175,17 @@ extern "C" int matq_kv4_append(const matq_paged_kv4* cache, int64_t T, const voi
     P.cache = static_cast<uint8_t*>(cache->tiles);
     P.table = cache->page_table; P.cu_q = cache->cu_q; P.kv_len = cache->kv_len;
     P.n_pages = cache->n_pages; P.table_stride = cache->table_stride; P.table_width = cache->table_width;
-    P.page_size = cache->page_size; P.kv_heads = cache->kv_heads; P.q_heads = q_heads; P.D = D; P.batch = cache->batch;
+    P.page_size = cache->page_size; P.kv_heads = cache->kv_heads; P.q_heads = q_heads; P.batch = cache->batch;
     P.q = static_cast<const __nv_bfloat16*>(q); P.k = static_cast<const __nv_bfloat16*>(k); P.v = static_cast<const __nv_bfloat16*>(v);
     P.ldq = ldq; P.ldk = ldk; P.ldv = ldv; P.ldqo = ldqo;
     P.cos_sin = cos_sin; P.max_pos = max_pos; P.rot = rot_dim; P.interleaved = interleaved ? 1 : 0;
     P.q_out = static_cast<__nv_bfloat16*>(q_out);
     P.dev_status = dev_status;
-    const cudaError_t e = launch_overlapped(kv4_append_kernel, dim3((unsigned)T), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), P);
+    const bool many = T >= kMany;
+    const auto kernel = D == 64 ? (many ? kv4_append_kernel<64, kThreadsMany> : kv4_append_kernel<64, kThreadsFew>)
+                        : D == 128 ? (many ? kv4_append_kernel<128, kThreadsMany> : kv4_append_kernel<128, kThreadsFew>)
+                                   : (many ? kv4_append_kernel<256, kThreadsMany> : kv4_append_kernel<256, kThreadsFew>);
+    const cudaError_t e = launch_overlapped(kernel, dim3((unsigned)T), dim3(many ? kThreadsMany : kThreadsFew), 0, static_cast<cudaStream_t>(stream), P);
     if (e != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
     return launch_status();
 }

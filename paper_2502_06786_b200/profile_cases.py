@@ -1,6 +1,6 @@
 """Small, self-contained invocations of each kernel for profilers (ncu wants short runs with few launches).
 
-    python -m paper_2502_06786_b200.profile_cases quantize|slice4|slice2ep|gemv4|gemv2|gemv2b8|gemv4t|gemv2t|stream8|stream4|stream2|group4|group2|batch4|batch8|gemm|linear|attend
+    python -m paper_2502_06786_b200.profile_cases quantize|slice4|slice2ep|gemv4|gemv2|gemv2b8|gemv4t|gemv2t|stream8|stream4|stream2|group4|group2|batch4|batch8|gemm|linear|attend|groups|attend4
 
 (gemv4 / gemv2: the library's own choice at B = 1, the integer tensor kernel; a trailing t: the bf16 tensor kernel.)
 
@@ -117,6 +117,29 @@ def main(which: str) -> None:
             for _ in range(3):
                 mq.kv_append(kc, vc, table, cu, lens, k, v, cos_sin=ang, q=q, q_out=q)
                 mq.attn_paged(q, kc, vc, table, cu, lens, new, keys)
+    elif which == "groups":
+        # weights in 4-bit groups of 128: the quantiser, one token and 16 through a Gemma-2-2B gate matrix
+        Ws = [torch.randn(N, K, device="cuda").mul_(0.02).to(torch.bfloat16) for _ in range(n)]
+        held = [mq.quantize_groups(W, 128) for W in Ws]
+        for M in (1, 16):
+            X = torch.randn(M, K, device="cuda").to(torch.bfloat16)
+            Y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+            for packed, params in held:
+                mq.gemv_groups(packed, params, X, y=Y)
+    elif which == "attend4":
+        # append to and attention over a 4-bit paged cache: 16 single tokens over 8192 keys of 8 heads of 128, 6 drafted tokens each, 2048 tokens over 4096
+        for batch, new, keys in ((16, 1, 8192), (16, 6, 8192), (1, 2048, 4096)):
+            pages = batch * keys // 64
+            cache = torch.randint(0, 64, (pages, 8, 4, mq.kv4_tile_bytes(128)), dtype=torch.uint8, device="cuda")
+            table = torch.randperm(pages, device="cuda").to(torch.int32).view(batch, -1)
+            cu = torch.arange(batch + 1, device="cuda").to(torch.int32) * new
+            lens = torch.full((batch,), keys, dtype=torch.int32, device="cuda")
+            q = torch.randn(batch * new, 32, 128, device="cuda").to(torch.bfloat16)
+            k, v = (torch.randn(batch * new, 8, 128, device="cuda").to(torch.bfloat16) for _ in range(2))
+            ang = torch.rand(keys, 128, device="cuda")
+            for _ in range(3):
+                mq.kv4_append(cache, table, cu, lens, k, v, cos_sin=ang, q=q, q_out=q)
+                mq.attn_paged4(q, cache, table, cu, lens, new, keys)
     else:
         raise SystemExit(__doc__)
     torch.cuda.synchronize()

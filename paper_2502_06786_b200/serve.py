@@ -1,14 +1,18 @@
 """A small decoder served from its nested weights: prompts, chunks of prompts, drafted and single tokens.
 
-    python -m paper_2502_06786_b200.serve
+    python -m paper_2502_06786_b200.serve [--four-bits]
 
 Shows the serving calls as they are used together.  A layer keeps its matrices once as 8-bit codes and serves a nested precision r of them: up to
 ``FEW`` tokens go through the decode GEMV on the packed plane (``gemv_grouped``), more through the 8-bit tensor-core product on the unpacked
 slice (``quantize_tokens`` once per input, ``gemm_a8`` per matrix).  New keys and values are rotated and appended to a paged cache
 (``kv_append``), and the new tokens attend to it (``attn_paged``).  Norms, activations and residual sums are plain torch.
+
+With ``Config.group`` a matrix is kept in 4-bit groups of that many weights instead (``quantize_groups``, ``gemv_groups``), which lose less of it at the same
+size than one scale per channel, and with ``Config.cache_bits = 4`` the cache takes a little over a quarter of the memory (``kv4_append``, ``attn_paged4``).
 """
 from __future__ import annotations
 
+import sys
 from dataclasses import dataclass
 
 import torch
@@ -27,6 +31,8 @@ class Config:
     head_dim: int = 64
     layers: int = 2
     r: int = 4                  # nested precision that is served
+    group: int = 0              # weights per 4-bit group (32, 64 or 128); 0: the nested codes, one scale per output channel
+    cache_bits: int = 16        # of the cache's keys and values: 16 (bf16) or 4
     window: int = 0
     softcap: float = 0.0
     page_size: int = 16
@@ -45,9 +51,19 @@ class Linear:
         self.packed, self.sliced = out["packed"], out["sliced"]
 
 
+class GroupedLinear:
+    """One matrix in 4-bit groups."""
+
+    def __init__(self, W: torch.Tensor, group: int):
+        self.N, self.K = W.shape
+        self.packed, self.params = mq.quantize_groups(W, group)
+
+
 def apply(linears, x):
     """The products of one input [T, K] (bf16) with several matrices: bf16 [T, N] each."""
     T = x.shape[0]
+    if isinstance(linears[0], GroupedLinear):
+        return [mq.gemv_groups(l.packed, l.params, x, out_dtype=torch.bfloat16, flags=mq.GEMV_PDL) for l in linears]
     if T <= FEW:
         ys = [torch.empty((T, l.N), dtype=torch.float32, device=x.device) for l in linears]
         mq.gemv_grouped([dict(packed=l.packed, K=l.K, r=l.r, alpha=l.alpha, zero=l.zero, x=x if T > 1 else x[0], y=y if T > 1 else y[0])
@@ -61,9 +77,13 @@ class PagedCache:
     """Keys and values of all layers in pages, and which pages belong to which sequence.  The page numbers are the same in every layer."""
 
     def __init__(self, cfg: Config, n_pages: int, device="cuda"):
-        shape = (n_pages, cfg.kv_heads, cfg.page_size, cfg.head_dim)
-        self.k = [torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(cfg.layers)]
-        self.v = [torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(cfg.layers)]
+        if cfg.cache_bits == 4:
+            shape = (n_pages, cfg.kv_heads, cfg.page_size // 16, mq.kv4_tile_bytes(cfg.head_dim))
+            self.tiles = [torch.empty(shape, dtype=torch.uint8, device=device) for _ in range(cfg.layers)]
+        else:
+            shape = (n_pages, cfg.kv_heads, cfg.page_size, cfg.head_dim)
+            self.k = [torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(cfg.layers)]
+            self.v = [torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(cfg.layers)]
         self.page_size, self.free = cfg.page_size, list(range(n_pages - 1, -1, -1))
         self.pages, self.length = {}, {}
 
@@ -111,14 +131,17 @@ def rms_norm(x):
 
 
 class Decoder:
-    """A decoder with random weights (std 0.02) quantised to 8 bits."""
+    """A decoder with random weights (std 0.02) quantised to 8 bits, or to 4-bit groups."""
 
     def __init__(self, cfg: Config, seed: int = 0, device="cuda"):
+        if cfg.cache_bits not in (4, 16):
+            raise ValueError("cache_bits: 4 or 16")
         self.cfg = cfg
         g = torch.Generator(device=device).manual_seed(seed)
 
         def linear(n, k):
-            return Linear((torch.randn(n, k, generator=g, device=device) * 0.02).to(torch.bfloat16), cfg.r)
+            W = (torch.randn(n, k, generator=g, device=device) * 0.02).to(torch.bfloat16)
+            return GroupedLinear(W, cfg.group) if cfg.group else Linear(W, cfg.r)
         d, f, D = cfg.hidden, cfg.ffn, cfg.head_dim
         self.layers = [dict(q=linear(cfg.q_heads * D, d), k=linear(cfg.kv_heads * D, d), v=linear(cfg.kv_heads * D, d), o=linear(d, cfg.q_heads * D),
                             gate=linear(f, d), up=linear(f, d), down=linear(d, f)) for _ in range(cfg.layers)]
@@ -136,16 +159,20 @@ class Decoder:
         for i, l in enumerate(self.layers):
             q, k, v = apply([l["q"], l["k"], l["v"]], rms_norm(x))
             q, k, v = (t.view(T, -1, cfg.head_dim) for t in (q, k, v))
-            mq.kv_append(cache.k[i], cache.v[i], *paged, k, v, cos_sin=self.cos_sin, q=q, q_out=q, dev_status=dev_status)
-            a = mq.attn_paged(q, cache.k[i], cache.v[i], *paged, batch.max_q, batch.max_kv, softcap=cfg.softcap, window=cfg.window, dev_status=dev_status)
+            if cfg.cache_bits == 4:
+                mq.kv4_append(cache.tiles[i], *paged, k, v, cos_sin=self.cos_sin, q=q, q_out=q, dev_status=dev_status)
+                a = mq.attn_paged4(q, cache.tiles[i], *paged, batch.max_q, batch.max_kv, softcap=cfg.softcap, window=cfg.window, dev_status=dev_status)
+            else:
+                mq.kv_append(cache.k[i], cache.v[i], *paged, k, v, cos_sin=self.cos_sin, q=q, q_out=q, dev_status=dev_status)
+                a = mq.attn_paged(q, cache.k[i], cache.v[i], *paged, batch.max_q, batch.max_kv, softcap=cfg.softcap, window=cfg.window, dev_status=dev_status)
             x = x + apply([l["o"]], a.view(T, -1))[0]
             gate, up = apply([l["gate"], l["up"]], rms_norm(x))
             x = x + apply([l["down"]], torch.nn.functional.silu(gate) * up)[0]
         return x
 
 
-def main() -> None:
-    cfg = Config()
+def main(four_bits: bool = False) -> None:
+    cfg = Config(group=64, cache_bits=4) if four_bits else Config()
     model, cache = Decoder(cfg), PagedCache(cfg, 64)
     g = torch.Generator(device="cuda").manual_seed(1)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
@@ -160,4 +187,4 @@ def main() -> None:
 
 
 if __name__ == "__main__":
-    main()
+    main("--four-bits" in sys.argv[1:])

@@ -45,6 +45,21 @@ def test_quantize_groups_ties():
     assert np.array_equal(_bits(params), p) and np.array_equal(host(packed), gr.pack(codes))
 
 
+def test_quantize_groups_every_scale():
+    # ranges that give every bf16 scale of many binades, and ranges next to where its rounding changes; values all over them
+    rng = np.random.default_rng(8)
+    scale = gr.bf16_values((np.arange(128)[None, :] + np.array([1, 10, 100, 126, 127, 128, 140, 200, 245, 250])[:, None] * 128).astype(np.uint16)).reshape(-1).astype(np.float64)
+    top = np.concatenate([gr.bf16_bits((scale * f).astype(np.float32)) for f in (15.0, 15.03, 14.97, 15.06)])
+    x = gr.bf16_values(top)[:, None].astype(np.float64) * rng.random((len(top), 32))
+    w = gr.bf16_bits(x.astype(np.float32))
+    w[:, 0], w[:, 1] = 0, top
+    w[1::2] ^= 0x8000                                            # and below zero
+    packed, params = mq.quantize_groups(bf16_dev(w), 32)
+    codes, p = gr.quantise(w, 32)
+    assert len(np.unique(p[:, 0, 0])) > 1000
+    assert np.array_equal(_bits(params), p) and np.array_equal(host(packed), gr.pack(codes))
+
+
 def test_quantize_groups_rows_apart_and_groups_that_are_not_finite():
     w = synth.normal_bf16((37, 320 + 24), 1.0, 5)
     status = status_word()

@@ -37,7 +37,8 @@ def _rotated(x, cs, pos, rot, interleaved):
 # ------------------------------------------------------------------ kv4_append
 
 APPENDS = [([1], [0], 1, 1, 64, 16, 64), ([1, 1, 1], [5, 0, 300], 32, 8, 128, 16, 128), ([7, 0, 33, 1], [0, 9, 60, 15], 16, 8, 256, 64, 256),
-           ([130], [77], 12, 4, 64, 32, 32), ([3, 2], [1, 2], 5, 1, 128, 48, 48), ([2] * 70, list(range(70)), 4, 2, 128, 16, 0), ([40, 1], [10, 3], 80, 1, 256, 128, 96)]
+           ([130], [77], 12, 4, 64, 32, 32), ([3, 2], [1, 2], 5, 1, 128, 48, 48), ([2] * 70, list(range(70)), 4, 2, 128, 16, 0), ([40, 1], [10, 3], 80, 1, 256, 128, 96),
+           ([1500, 600], [3, 0], 3, 1, 64, 16, 64), ([2100], [0], 2, 1, 128, 64, 128), ([2000, 49], [7, 1], 3, 2, 256, 32, 256)]
 
 
 @pytest.mark.parametrize("interleaved", [False, True])

@@ -63,7 +63,7 @@ __device__ __forceinline__ void ldmatrix4t(uint32_t (&r)[4], uint32_t addr) {
 }
 __device__ __forceinline__ uint32_t transposed8x8(uint32_t a) {
     uint32_t d;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
     return d;
 }
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
@@ -82,7 +82,7 @@ __device__ __forceinline__ uint32_t centred_low(uint32_t w) { return fma_bf16x2(
 __device__ __forceinline__ uint32_t centred_high(uint32_t w) { return fma_bf16x2(w & 0x00f000f0u, 0x7d007d00u, 0xbe00be00u); }         // 16 n 2^-133 * 2^123 - 2^-3
 // a += codes (u8) * digits (s8): mma.sync m16n8k32
 __device__ __forceinline__ void mma_u8s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // Digit `which` (0: the high one) of eight values times 2^(14 - e) as 16-bit integers: even elements' in the bytes of x, odd ones' in those of y.  An integer is at

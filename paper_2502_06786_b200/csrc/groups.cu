@@ -64,8 +64,11 @@ cudaError_t launch_quantize(const void* W, int64_t N, int64_t K, int64_t ldw, vo
 // codes 0 and 4, (w & 0x00f000f0) 16 times codes 1 and 5, and w >> 8 the other four likewise.  The tokens stand in shared memory in that order of pairs, scaled
 // by a power of two (and by 2^-4 where the code is 16 times too large), so that no product leaves fp32's range (group4.cuh).
 //
-// With groups of 32 or 64 the four lanes that share a row hold 4 or 2 groups at a time.  Each group gets columns of its own: token m of group slot s is column
-// m S + s, whose operand is zero in the lanes of the other slots (S = 128 / group).
+// The sixteen elements of a product's row, four lanes' words, have to lie in one group.  With S = 2 or 4 groups in a block of 128 there are two forms.  C = S: the lanes
+// read the block as if it were one group, and a token has a column for each group, zero in the lanes of the others; its eight columns hold 8 / S tokens.  C = 1: the lanes
+// read the block group by group, eight or four bytes each at a time, and add each group's sums on its own.  The first is taken while it needs no second block of columns:
+// 65536 x 2304, groups of 64, one token 19.9 against 21.5 us, four tokens x 4096 x 4096 6.5 against 7.5; beyond that its products double: 64 tokens, 14336 x 4096,
+// groups of 32, 140 against 73 us.
 //
 // A CTA takes a part of K, staged in shared memory for its tokens, and walks the matrix in steps of 16 RW rows; its warps are RW row tiles times SK parts of
 // that part, block by block of 128.  Each warp brings its own blocks into its own ring by cp.async, across the ends of steps, so that the ring never drains.
@@ -73,6 +76,8 @@ cudaError_t launch_quantize(const void* W, int64_t N, int64_t K, int64_t ldw, vo
 constexpr int kBlock = 128;
 // Warps of a CTA: eight, and two CTAs on an SM, as long as a CTA has one block of columns; sixteen beside tokens that take more shared memory.
 __host__ __device__ constexpr int warps_of(int nt) { return nt == 1 ? 8 : 16; }
+// Bytes from row to row in a ring: four lanes that read a block in four passes take 16 bytes of a row at a time, which eight rows 64 bytes apart would have on the same banks.
+__host__ __device__ constexpr int row_bytes_of(int passes) { return passes == 4 ? 80 : 64; }
 __host__ __device__ constexpr int ctas_of(int nt) { return nt > 1 ? 1 : 2; }
 __host__ __device__ constexpr int depth_of(int nt, int mt) { return nt > 1 && mt > 1 ? 3 : nt == 1 && mt == 1 ? 6 : 4; }
 
@@ -126,14 +131,17 @@ __device__ __forceinline__ bool unusual(uint4 v) {
     return max(most & 0xffffu, most >> 16) >= 0x4b80u || min(least & 0xffffu, least >> 16) < 0x1180u - 1u;
 }
 
-template <int NT, int S, int MT>
+// NT blocks of eight columns, S groups in a block of K, C columns of a token (1 or S), MT tiles of 16 rows of a warp
+template <int NT, int S, int C, int MT>
 __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_kernel(const GemvParams P) {
     constexpr int kWarps = warps_of(NT), kThreads = 32 * kWarps, kDepth = depth_of(NT, MT);
-    constexpr int kSlot = MT * (1024 + 64 * S), kWarpRing = kDepth * kSlot;              // a block's codes and groups of 16 MT rows
+    constexpr int kPasses = S / C, kRow = row_bytes_of(kPasses), kCodes = 16 * MT * kRow;          // a block's codes of a row, and of 16 MT rows
+    constexpr int kSlot = kCodes + 64 * S * MT, kWarpRing = kDepth * kSlot;              // and their groups
+    constexpr int kWords = 4 / kPasses;      // of eight codes of a row that a lane takes in a pass
     constexpr int kCols = NT * 8, kTile = 16 * MT, kGroupCopies = (kTile * S + 31) / 32;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint32_t s_top[32];           // largest magnitude per token (bits of a float)
-    __shared__ __align__(16) uint4 s_zero[1];
+    __shared__ __align__(16) uint4 s_zero[16];      // a block of no token
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
     const int rt = warp % P.rw, kw = warp / P.rw, rows = kTile * P.rw, rows_shift = 31 - __clz(rows);
     const unsigned cl = gridDim.x, rank = blockIdx.x;                   // the cluster is the grid's x
@@ -142,13 +150,13 @@ __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_ke
     const int64_t m0 = (int64_t)blockIdx.z * P.tokens;
     const int tokens = (int)min((int64_t)P.tokens, P.M - m0);
 
-    // shared memory: the warps' rings; tokens [tokens][slice][256 bytes] (+ 64 bytes a token); sums of groups [slice][columns]; results
+    // shared memory: the warps' rings; tokens [tokens][slice][256 bytes] (+ 64 bytes a token); sums of groups [slice passes][columns]; results
     const int x_stride = P.slice * 256 + 64;
     unsigned char* s_x = smem + kWarps * kWarpRing;
     float* s_sum = reinterpret_cast<float*>(s_x + (size_t)P.tokens * x_stride);
-    float* s_red = s_sum + (size_t)P.slice * kCols;
+    float* s_red = s_sum + (size_t)P.slice * kPasses * kCols;
 
-    // ---- this warp's blocks, fetched kDepth - 1 ahead: a lane brings 16 bytes of its rows, which it reads itself, and some of the tile's groups
+    // ---- this warp's blocks, fetched kDepth - 1 ahead: a lane brings 16 bytes of rows g, g + 8, .., and some of the tile's groups
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + (uint32_t)warp * kWarpRing;
     int f_step = kw < n_blocks ? (int)blockIdx.y : P.steps, f_block = kw, f_at = 0;
     const uint8_t* f_w[2 * MT];
@@ -168,10 +176,10 @@ __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_ke
     const auto fetch = [&] {
         if (f_step < P.steps) {
 #pragma unroll
-            for (int e = 0; e < 2 * MT; ++e) copy16(ring + f_at + e * 512 + lane * 16, f_w[e] + f_block * 64, f_block < f_in);
+            for (int e = 0; e < 2 * MT; ++e) copy16(ring + f_at + (g + 8 * e) * kRow + q * 16, f_w[e] + f_block * 64, f_block < f_in);
 #pragma unroll
             for (int e = 0; e < kGroupCopies; ++e)
-                if (kTile * S % 32 == 0 || lane < kTile * S) copy4(ring + f_at + MT * 1024 + (lane + 32 * e) * 4, f_g[e] + f_block * S, f_block < f_has[e]);
+                if (kTile * S % 32 == 0 || lane < kTile * S) copy4(ring + f_at + kCodes + (lane + 32 * e) * 4, f_g[e] + f_block * S, f_block < f_has[e]);
             f_block += P.sk;
             if (f_block >= n_blocks) {
                 f_block = kw;
@@ -183,15 +191,15 @@ __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_ke
         f_at = f_at == (kDepth - 1) * kSlot ? 0 : f_at + kSlot;
     };
     if (tid < 32) s_top[tid] = 0u;
-    if (tid == 0) s_zero[0] = make_uint4(0u, 0u, 0u, 0u);
-    for (int i = tid; i < P.slice * kCols; i += kThreads) s_sum[i] = 0.f;
+    if (tid < 16) s_zero[tid] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = tid; i < P.slice * kPasses * kCols; i += kThreads) s_sum[i] = 0.f;
     if (!P.early) after_previous_kernel();
 #pragma unroll 1
     for (int d = 0; d < kDepth - 1; ++d) fetch();
     after_previous_kernel();                                            // (at once if it has waited above)
 
     // ---- the tokens, four pieces of eight elements a thread at a time, scaled and in the order of pairs, and the sums of their groups
-    // Piece 4 q + j of a block goes to place 4 j + q: the four lanes of a row read 64 bytes side by side.  The pieces of all tokens have one running index; those
+    // The four lanes of a row read 64 bytes side by side: a pass's pieces stand word by word, lane by lane.  The pieces of all tokens have one running index; those
     // of a group are neighbours in a warp.
     const int pieces = n_blocks * 16, all = pieces * tokens, last_piece = (int)min((int64_t)pieces, (P.K - (int64_t)b_lo * kBlock) / 8);
     const auto each_piece = [&](auto f) {                               // f(the piece, its token, its place in the token's row, whether there is one)
@@ -222,9 +230,9 @@ __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_ke
 #pragma unroll
         for (int w = 1; w < 16 / S; w <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
         if (in) {
-            const int place = (i & ~15) | ((i & 3) << 2) | ((i >> 2) & 3);
-            *reinterpret_cast<uint4*>(s_x + (size_t)v * x_stride + place * 16) = o;
-            if ((i & (16 / S - 1)) == 0) s_sum[(i >> 4) * kCols + v * S + (i & 15) / (16 / S)] = sum;
+            const int pass = i / (16 / kPasses), lane_of = i % (16 / kPasses) / kWords, word = i % kWords;
+            *reinterpret_cast<uint4*>(s_x + (size_t)v * x_stride + ((pass * kWords + word) * 4 + lane_of) * 16) = o;
+            if (i % (16 / S) == 0) s_sum[pass * kCols + v * C + (C == 1 ? 0 : i % 16 / (16 / S))] = sum;
         }
     };
     __syncthreads();
@@ -247,21 +255,16 @@ __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_ke
     // Not before the tokens are here: what the next kernel fetches early would be in their way.
     let_next_kernel_start();
 
-    // Column 8 nt + g of this lane's operands: a token's, in the quarter of a block that belongs to the column's slot, and zero elsewhere.
-    uint32_t x_at[NT], x_step[NT];
+    // Column 8 nt + g of this lane's operands: a token's, in the lanes that have the column's group, or zero.
+    const unsigned char* x_from[NT];
+    int x_step[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        const int v = (8 * nt + g) / S;
-        const bool mine = (q * S) / 4 == g % S && v < tokens;
-        x_at[nt] = (uint32_t)__cvta_generic_to_shared(mine ? (const void*)(s_x + (size_t)v * x_stride + q * 16) : (const void*)s_zero);
-        x_step[nt] = mine ? 256u : 0u;
+        const int v = (8 * nt + g) / C;
+        const bool some = v < tokens && (C == 1 || q * S / 4 == g % S);
+        x_from[nt] = some ? s_x + (size_t)v * x_stride + kw * 256 + q * 16 : reinterpret_cast<const unsigned char*>(s_zero);
+        x_step[nt] = some ? 256 * P.sk : 0;
     }
-    const auto operand = [&](int nt, int i, int j) {
-        uint4 v;
-        const uint32_t at = x_at[nt] + i * x_step[nt] + (x_step[nt] >> 2) * j;
-        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-        return v;
-    };
     const int part_floats = kWarps * kTile * (kCols + 1), buffer_floats = part_floats + rows * P.tokens;
     int at = 0, turn = 0, before = -1;                                  // before: the step whose sums are still with the CTAs of the cluster
     const auto gather = [&](int step, const float* part) {
@@ -283,56 +286,79 @@ __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_ke
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) y[mt][nt][e] = 0.f;
+        const unsigned char* x_at[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) x_at[nt] = x_from[nt];
+        const float* sum_at = s_sum + kw * kPasses * kCols + 2 * q;
 #pragma unroll 1
         for (int i = kw; i < n_blocks; i += P.sk) {
             asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 2) : "memory");
             __syncwarp();
             const unsigned char* slot = smem + (size_t)warp * kWarpRing + at;
-            uint4 w[2 * MT];
-#pragma unroll
-            for (int e = 0; e < 2 * MT; ++e) w[e] = *reinterpret_cast<const uint4*>(slot + e * 512 + lane * 16);
-            uint2 gr[2 * MT];                                           // groups of columns 2 q and 2 q + 1
+            uint32_t w[2 * MT][4], gr[2 * MT][C == 1 ? S : 2];          // groups of the passes, or of columns 2 q and 2 q + 1
 #pragma unroll
             for (int e = 0; e < 2 * MT; ++e) {
-                const unsigned char* p = slot + MT * 1024 + (g + 8 * e) * (4 * S);
-                if (S == 1) gr[e].x = gr[e].y = *reinterpret_cast<const uint32_t*>(p);
-                else gr[e] = *reinterpret_cast<const uint2*>(p + (S == 4 ? 8 * (q & 1) : 0));
+                const unsigned char* row = slot + (g + 8 * e) * kRow + q * (16 / kPasses);
+                if constexpr (kPasses == 1) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(row);
+                    w[e][0] = v.x; w[e][1] = v.y; w[e][2] = v.z; w[e][3] = v.w;
+                } else if constexpr (kPasses == 2) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(row), u = *reinterpret_cast<const uint2*>(row + 32);
+                    w[e][0] = v.x; w[e][1] = v.y; w[e][2] = u.x; w[e][3] = u.y;
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) w[e][s] = *reinterpret_cast<const uint32_t*>(row + 16 * s);
+                }
+                const unsigned char* of_row = slot + kCodes + (g + 8 * e) * (4 * S);
+                if constexpr (C == 1) {
+#pragma unroll
+                    for (int s = 0; s < S; ++s) gr[e][s] = *reinterpret_cast<const uint32_t*>(of_row + 4 * s);
+                } else {
+                    const uint2 v = *reinterpret_cast<const uint2*>(of_row + (S == 4 ? 8 * (q & 1) : 0));
+                    gr[e][0] = v.x; gr[e][1] = v.y;
+                }
             }
             at = at == (kDepth - 1) * kSlot ? 0 : at + kSlot;
             fetch();                                                    // into the slot that was read one block ago
-            constexpr int kChains = MT * NT <= 2 ? 2 : 1;
-            float acc[kChains][MT][NT][4] = {};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint4 xv[NT];
+            for (int s = 0; s < kPasses; ++s) {
+                constexpr int kChains = MT * NT * kPasses == 1 ? 2 : 1;       // sums that do not wait for one another
+                float acc[kChains][MT][NT][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) xv[nt] = operand(nt, i, j);
+                for (int j = 0; j < kWords; ++j) {
+                    uint4 xv[NT];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const uint4 wa = w[2 * mt], wb = w[2 * mt + 1];
-                    const uint32_t a = j == 0 ? wa.x : j == 1 ? wa.y : j == 2 ? wa.z : wa.w, b = j == 0 ? wb.x : j == 1 ? wb.y : j == 2 ? wb.z : wb.w;
-                    const uint32_t a8 = a >> 8, b8 = b >> 8;
+                    for (int nt = 0; nt < NT; ++nt) xv[nt] = *reinterpret_cast<const uint4*>(x_at[nt] + 64 * (s * kWords + j));
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        mma_bf16(acc[0][mt][nt], a & 0x000f000fu, b & 0x000f000fu, a & 0x00f000f0u, b & 0x00f000f0u, xv[nt].x, xv[nt].y);
-                        mma_bf16(acc[kChains - 1][mt][nt], a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u, xv[nt].z, xv[nt].w);
+                    for (int mt = 0; mt < MT; ++mt) {
+                        const uint32_t a = w[2 * mt][s * kWords + j], b = w[2 * mt + 1][s * kWords + j], a8 = a >> 8, b8 = b >> 8;
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            if (j == 0) mma_bf16_first(acc[0][mt][nt], a & 0x000f000fu, b & 0x000f000fu, a & 0x00f000f0u, b & 0x00f000f0u, xv[nt].x, xv[nt].y);
+                            else mma_bf16(acc[0][mt][nt], a & 0x000f000fu, b & 0x000f000fu, a & 0x00f000f0u, b & 0x00f000f0u, xv[nt].x, xv[nt].y);
+                            if (j == 0 && kChains == 2) mma_bf16_first(acc[kChains - 1][mt][nt], a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u, xv[nt].z, xv[nt].w);
+                            else mma_bf16(acc[kChains - 1][mt][nt], a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u, xv[nt].z, xv[nt].w);
+                        }
                     }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float2 sum = *reinterpret_cast<const float2*>(sum_at + s * kCols + 8 * nt);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t group = gr[2 * mt + (e >> 1)][C == 1 ? s : e & 1];
+                            const float v = kChains == 2 ? acc[0][mt][nt][e] + acc[kChains - 1][mt][nt][e] : acc[0][mt][nt][e];
+                            y[mt][nt][e] = fmaf(scale_of(group), v, fmaf(low_of(group), (e & 1) ? sum.y : sum.x, y[mt][nt][e]));
+                        }
                 }
             }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const float2 sum = *reinterpret_cast<const float2*>(s_sum + i * kCols + 8 * nt + 2 * q);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint2 p = gr[2 * mt + (e >> 1)];
-                        const uint32_t group = (e & 1) ? p.y : p.x;
-                        y[mt][nt][e] = fmaf(scale_of(group), kChains == 2 ? acc[0][mt][nt][e] + acc[kChains - 1][mt][nt][e] : acc[0][mt][nt][e], fmaf(low_of(group), (e & 1) ? sum.y : sum.x, y[mt][nt][e]));
-                    }
-            }
+            for (int nt = 0; nt < NT; ++nt) x_at[nt] += x_step[nt];
+            sum_at += P.sk * kPasses * kCols;
         }
-        // ---- sums over the warps that share a row tile, the slots, and the CTAs of the cluster, each in a fixed order
+        // ---- sums over the warps that share a row tile, the columns of a token and the CTAs of the cluster, each in a fixed order
         float* red = s_red + turn * buffer_floats;                      // [kw][row][columns]; then [token][row]
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -341,7 +367,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_ke
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int c = 8 * nt + 2 * q + (e & 1);
-                    if (c < tokens * S) red[(kw * rows + rt * kTile + 16 * mt + g + 8 * (e >> 1)) * (kCols + 1) + c] = from_units(y[mt][nt][e], odd_sizes ? scale_exponent(s_top[c / S]) : kUsualExp);
+                    if (c < tokens * C) red[(kw * rows + rt * kTile + 16 * mt + g + 8 * (e >> 1)) * (kCols + 1) + c] = from_units(y[mt][nt][e], odd_sizes ? scale_exponent(s_top[c / C]) : kUsualExp);
                 }
         __syncthreads();
         float* part = red + part_floats;
@@ -350,7 +376,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_ke
             float sum = 0.f;
             for (int w = 0; w < P.sk; ++w)
 #pragma unroll
-                for (int s = 0; s < S; ++s) sum += red[(w * rows + r) * (kCols + 1) + v * S + s];
+                for (int s = 0; s < C; ++s) sum += red[(w * rows + r) * (kCols + 1) + v * C + s];
             if (cl > 1) part[i] = sum;
             else store(P, m0 + v, (int64_t)step * rows + r, sum);
         }
@@ -381,8 +407,10 @@ struct GemvPlan {
     double cost;
 };
 
-inline size_t gemv_smem(int64_t tokens, int64_t slice, int S, int nt, int mt, int rw) {
-    const size_t warps = warps_of(nt), ring = warps * depth_of(nt, mt) * mt * (1024 + 64 * S), stage = (size_t)tokens * (slice * 256 + 64) + (size_t)slice * nt * 8 * 4;
+inline int columns_of(int64_t M, int S) { return M * S <= 8 ? S : 1; }
+
+inline size_t gemv_smem(int64_t tokens, int64_t slice, int S, int passes, int nt, int mt, int rw) {
+    const size_t warps = warps_of(nt), ring = warps * depth_of(nt, mt) * mt * (16 * row_bytes_of(passes) + 64 * S), stage = (size_t)tokens * (slice * 256 + 64) + (size_t)slice * passes * nt * 8 * 4;
     const size_t join = 2 * (warps * 16 * mt * (nt * 8 + 1) + (size_t)tokens * 16 * mt * rw) * 4;
     return ring + stage + join;
 }
@@ -396,10 +424,10 @@ inline int on_an_sm(int nt, size_t smem) { return ctas_of(nt) == 2 && 2 * (smem 
 // the SM or its share of HBM, whichever is longest; the sums at the end of a step, and those of a cluster.
 inline bool plan_shape(GemvPlan& p, int64_t M, int64_t N, int64_t K, int S, int sms) {
     const int64_t blocks = (K + kBlock - 1) / kBlock;
-    const int warps = warps_of(p.nt);
+    const int warps = warps_of(p.nt), passes = S / columns_of(M, S);
     p.rw = warps / p.sk;
     p.slice = (int)((blocks + p.cl - 1) / p.cl);
-    p.smem = gemv_smem(p.tokens, p.slice, S, p.nt, p.mt, p.rw);
+    p.smem = gemv_smem(p.tokens, p.slice, S, passes, p.nt, p.mt, p.rw);
     if (p.smem > kSmemOne || p.cl > blocks) return false;
     p.token_blocks = (M + p.tokens - 1) / p.tokens;
     const int rows = 16 * p.mt * p.rw, per_sm = on_an_sm(p.nt, p.smem);
@@ -409,12 +437,12 @@ inline bool plan_shape(GemvPlan& p, int64_t M, int64_t N, int64_t K, int S, int 
     if (p.row_ctas > p.steps) p.row_ctas = p.steps;
     const double busy = (double)p.row_ctas * p.token_blocks * p.cl, most = (double)slots * p.cl, at_work = busy < most ? busy : most;
     const double rounds = (double)((p.steps + p.row_ctas - 1) / p.row_ctas) * (busy / at_work);
-    const double on_sm = at_work <= sms ? 1 : per_sm, tile = p.mt * p.nt * (S == 1 ? 1.0 : 1.15);
-    const double alone = 85 + 150 * tile, shared = (100 + 260 * tile) * warps * on_sm / 16, hbm = (double)p.mt * (1024 + 64 * S) * warps * at_work / 6300.0 * (p.mt == 2 && p.sk == 1 ? 1.6 : 1.0);
+    const double on_sm = at_work <= sms ? 1 : per_sm, tile = p.mt * p.nt * (S == 1 ? 1.0 : passes == 1 ? 1.15 : 1.0 + 0.1 * passes * p.mt);
+    const double alone = 85 + 150 * tile, shared = (100 + 260 * tile) * warps * on_sm / 16, hbm = (double)p.mt * (1024 + 64 * S) * warps * at_work / 6300.0 * (p.mt == 2 && p.sk == 1 && per_sm == 2 ? 1.6 : 1.0);
     // (32 rows of 64 bytes at a time and nobody at the rows' next bytes: 65536 x 2304 in 26 us, with two warps to a row 20.5)
     double block = alone > shared ? alone : shared;
     if (hbm > block) block = hbm;
-    const double stage = 800 + 80.0 * p.tokens * p.slice / warps, sums = 500 + 60.0 * rows * p.tokens / (32 * warps) + (p.cl > 1 ? 500 + 200 * p.cl : 0);
+    const double stage = 800 + 40.0 * p.tokens * p.slice / warps + (at_work > sms ? 700 * (at_work - sms) / sms : 0), sums = 500 + 60.0 * rows * p.tokens / (32 * warps) + 50 * p.sk * (S / passes) + (p.cl > 1 ? 500 + 200 * p.cl : 0);
     p.cost = 2000 + stage + rounds * ((double)((p.slice + p.sk - 1) / p.sk) * block + sums);
     return true;
 }
@@ -423,8 +451,8 @@ inline GemvPlan plan_gemv(int64_t M, int64_t N, int64_t K, int S, int sms) {
     GemvPlan best, p;
     best.cost = -1;
     for (p.nt = 1; p.nt <= 4; p.nt *= 2) {
-        if (p.nt > 1 && M * S <= 4 * p.nt) break;                       // half as many columns would do
-        p.tokens = p.nt * 8 / S < M ? p.nt * 8 / S : M;
+        if (p.nt > 1 && M <= 4 * p.nt) break;                        // half as many columns would do
+        p.tokens = p.nt * 8 < M ? p.nt * 8 : M;
         for (p.mt = 1; p.mt <= (p.nt < 4 ? 2 : 1); ++p.mt)
             for (p.cl = 1; p.cl <= 8; p.cl *= 2)
                 for (p.sk = 1; p.sk <= warps_of(p.nt); p.sk *= 2)
@@ -433,10 +461,10 @@ inline GemvPlan plan_gemv(int64_t M, int64_t N, int64_t K, int S, int sms) {
     return best;
 }
 
-template <int NT, int S, int MT>
+template <int NT, int S, int C, int MT>
 int launch_gemv(const GemvPlan& p, const GemvParams& P, cudaStream_t s) {
     static std::atomic<unsigned long long> smem_ok{0};
-    if (!opt_in_max_smem(gemv_groups_kernel<NT, S, MT>, smem_ok)) return MATQ_ERR_CUDA;
+    if (!opt_in_max_smem(gemv_groups_kernel<NT, S, C, MT>, smem_ok)) return MATQ_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.cl, (unsigned)p.row_ctas, (unsigned)p.token_blocks);
     cfg.blockDim = dim3(32 * warps_of(NT));
@@ -450,15 +478,16 @@ int launch_gemv(const GemvPlan& p, const GemvParams& P, cudaStream_t s) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, gemv_groups_kernel<NT, S, MT>, P) != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, gemv_groups_kernel<NT, S, C, MT>, P) != cudaSuccess) { cudaGetLastError(); return MATQ_ERR_CUDA; }
     return launch_status();
 }
 
 template <int S>
 int launch_gemv_s(const GemvPlan& p, const GemvParams& P, cudaStream_t s) {
-    if (p.nt == 4) return launch_gemv<4, S, 1>(p, P, s);
-    if (p.mt == 1) return p.nt == 1 ? launch_gemv<1, S, 1>(p, P, s) : launch_gemv<2, S, 1>(p, P, s);
-    return p.nt == 1 ? launch_gemv<1, S, 2>(p, P, s) : launch_gemv<2, S, 2>(p, P, s);
+    if (S > 1 && columns_of(P.M, S) == S) return p.mt == 1 ? launch_gemv<1, S, S, 1>(p, P, s) : launch_gemv<1, S, S, 2>(p, P, s);
+    if (p.nt == 4) return launch_gemv<4, S, 1, 1>(p, P, s);
+    if (p.mt == 1) return p.nt == 1 ? launch_gemv<1, S, 1, 1>(p, P, s) : launch_gemv<2, S, 1, 1>(p, P, s);
+    return p.nt == 1 ? launch_gemv<1, S, 1, 2>(p, P, s) : launch_gemv<2, S, 1, 2>(p, P, s);
 }
 
 }  // namespace grp

@@ -248,28 +248,36 @@ struct Plan4 {
 
 inline size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 
-// Tiles and split of the few-row kernel for sequences of so many rows, and what they cost (ns): the number of parts of the key range whose rounds over the SMs cost
-// least.  Measured: a step, a tile of 16 keys for each warp of a CTA, alone on an SM or at the share of HBM that the CTAs at work leave each other; a CTA's start and
-// end; the join.  Sequences of a batch are taken to be 0.9 of the longest.
-inline double plan_few(Plan4& p, int64_t rows, int64_t T, int batch, int q_heads, int kv_heads, int D, int64_t max_kv, int64_t window, int sms) {
-    p.rows = rows <= 4 ? 4 : D == 256 || rows <= 8 ? 8 : 16;
-    p.tiles_per_seq = (rows + p.rows - 1) / p.rows;
+// Tiles of `rows` rows and the split of the few-row kernel for sequences of at most most_rows rows, and what they cost (ns): the number of parts of the key range
+// whose rounds over the SMs cost least.  Measured: a step, a tile of 16 keys for each warp of a CTA, alone on an SM, beside another CTA, or at the share of HBM that
+// the CTAs at work leave each other; a CTA's start and end; the join.
+inline double plan_rows(Plan4& p, int rows, int64_t most_rows, int64_t T, int batch, int q_heads, int kv_heads, int D, int64_t max_kv, int64_t window, int sms) {
+    p.rows = rows;
+    p.tiles_per_seq = (most_rows + rows - 1) / rows;
     if (p.tiles_per_seq < 1) p.tiles_per_seq = 1;
-    const int warps = decode4_warps(D, p.rows), keys = 16 * warps;
+    const int warps = decode4_warps(D, rows), keys = 16 * warps;
     int64_t range = max_kv;
-    if (window > 0 && window < range && window + p.rows + 16 < range) range = window + p.rows + 16;
+    if (window > 0 && window < range && window + rows + 16 < range) range = window + rows + 16;
     range = (range + keys - 1) / keys + 1;
-    const double ctas = (double)p.tiles_per_seq * batch * kv_heads, row_bytes = ctas * p.rows * D * 8, slots = (double)sms * decode4_ctas(D, p.rows);
-    const double bytes = (double)warps * kv4::tile_bytes(D), mean = batch > 1 ? 0.9 : 1.0;
-    const double alone = (D == 256 ? 1100 : D == 128 ? 850 : 500) * (p.rows == 4 ? 1.0 : p.rows == 8 ? 1.2 : 1.45), ends = D == 256 ? 7000 : D == 128 ? 5000 : 4000;
+    // Tiles of the batch; fewer where its tokens do not go round.  The last of a sequence is half full, in steps of the heads that share a key head.
+    const int group = q_heads / kv_heads;
+    int common = rows;
+    while (group % common != 0) common /= 2;
+    const double all_tiles = (double)p.tiles_per_seq * batch, some = (double)T * group / rows + 0.5 * (1.0 - (double)common / rows) * batch;
+    const double ctas = (T * group < most_rows * batch && some < all_tiles ? some : all_tiles) * kv_heads, row_bytes = all_tiles * kv_heads * rows * D * 8, slots = (double)sms * decode4_ctas(D, rows);
+    const double bytes = (double)warps * kv4::tile_bytes(D);
+    const int kind = rows == 4 ? 0 : rows == 8 ? 1 : 2;
+    constexpr double kAlone[3][3] = {{500, 520, 830}, {850, 850, 1050}, {1100, 1320, 0}}, kBeside[3][3] = {{720, 740, 1040}, {1230, 1170, 1280}, {1600, 1850, 0}};
+    const int width = D == 64 ? 0 : D == 128 ? 1 : 2;
+    const double ends = D == 256 ? 7000 : D == 128 ? 5000 : 4000;
     double best = -1;
     int64_t splits = 1;
     for (int64_t n = 1; n <= kMaxSplits && n <= range && (n == 1 || (double)n * T * q_heads * (D + 2) * 4 <= kPartBytes); ++n) {
-        const double busy = ctas * (n * mean > 1.0 ? n * mean : 1.0), at_work = busy < slots ? busy : slots;
-        const double share = bytes * at_work / 6300.0, step = share > alone ? share : alone;
+        const double busy = ctas * n, at_work = busy < slots ? busy : slots;
+        const double share = bytes * at_work / 6300.0, own = (busy <= sms ? kAlone : kBeside)[width][kind], step = share > own ? share : own;
         const double part = (double)((range + n - 1) / n) * step + ends;
-        const double all = part * busy / slots * (n * mean > 1.0 ? 1.0 : mean);
-        const double cost = (busy <= slots ? part : all + part / 2) + (n > 1 ? 3500 + row_bytes * n / 5000.0 : 0);
+        const double rounds = busy / slots, late = rounds < 1.25 ? 4 * (rounds - 1) : 1.0;       // the last round's end: half a part, if it is not all but empty
+        const double cost = (rounds <= 1 ? part : part * (rounds + late / 2)) + (n > 1 ? 4500 + row_bytes * n / 5000.0 : 0);
         if (best < 0 || cost < best) { best = cost; splits = n; }
         if (ctas * n >= 6 * slots) break;
     }
@@ -277,6 +285,19 @@ inline double plan_few(Plan4& p, int64_t rows, int64_t T, int batch, int q_heads
     p.splits = (range + per - 1) / per;
     p.split_keys = per * keys;
     return best;
+}
+
+// Rows of a tile: 4 or 8 where they hold a sequence's, else 8 or 16, whichever costs less.  Tiles of 8 unpack the cache twice as often, but 16 warps of theirs share an
+// SM, not 12, and more CTAs fill rounds better: 16 ragged sequences of 8 to 24 rows over 4096 keys, heads of 128, 46 us, in tiles of 16 rows 58; 24 rows of 4 sequences
+// over 4000 keys 23.5 and 26.8.  But 16 rows over 32000 keys 27.2 and 24.0; 24 rows of 16 sequences over 4000 keys 66 and 58.
+inline double plan_few(Plan4& p, int64_t rows, int64_t T, int batch, int q_heads, int kv_heads, int D, int64_t max_kv, int64_t window, int sms) {
+    const double cost = plan_rows(p, rows <= 4 ? 4 : 8, rows, T, batch, q_heads, kv_heads, D, max_kv, window, sms);
+    if (rows <= 8 || D == 256) return cost;
+    Plan4 wide = p;
+    const double of_wide = plan_rows(wide, 16, rows, T, batch, q_heads, kv_heads, D, max_kv, window, sms);
+    if (of_wide >= cost) return cost;
+    p = wide;
+    return of_wide;
 }
 
 inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms) {
@@ -289,7 +310,11 @@ inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64
     const int64_t rows = max_q * group;
     const double direct = plan_few(p, rows, T, batch, q_heads, kv_heads, D, max_kv, window, sms);
     bool mixed = false;
-    if (rows > kMixedRows) {
+    const int64_t width = max_kv > kUnpackPage ? (max_kv + kUnpackPage - 1) / kUnpackPage : 1;
+    int64_t pages = width;                                              // of kUnpackPage keys, that a sequence is unpacked to
+    if (window > 0 && window < max_kv && (window + max_q) / kUnpackPage + 2 < pages) pages = (window + max_q) / kUnpackPage + 2;
+    const int64_t by_index = kMost / (pages * kUnpackPage * kv_heads);  // sequences: the 128-row kernels' limit on the rows of a cache
+    if (rows > kMixedRows && by_index > 0) {
         const int64_t range = window > 0 && window + max_q < max_kv ? window + max_q : max_kv;
         const double dense = 9000 + 4.0 * T * q_heads * D / 6000 + 8.0 * batch * range * kv_heads * D / 5000 + paged_cost(T, batch, q_heads, kv_heads, D, max_q, max_kv, window);
         mixed = dense < direct;
@@ -304,13 +329,10 @@ inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64
     p.dense_bytes = p.table_bytes = p.query_bytes = p.scale_bytes = p.top_bytes = p.cache_bytes = 0;
     p.new_width = p.new_pages = p.tops = 0;
     if (mixed) {
-        p.new_width = (max_kv + kUnpackPage - 1) / kUnpackPage;
-        if (p.new_width < 1) p.new_width = 1;
-        p.new_pages = p.new_width;
-        if (window > 0 && window < max_kv && (window + max_q) / kUnpackPage + 2 < p.new_pages) p.new_pages = (window + max_q) / kUnpackPage + 2;
+        p.new_width = width;
+        p.new_pages = pages;
         const int64_t per_seq = p.new_pages * kUnpackPage * kv_heads * D * 4;
         int64_t fit = kUnpackBytes / per_seq;
-        const int64_t by_index = kMost / (p.new_pages * kUnpackPage * kv_heads);     // matq_attn_paged's limit on the rows of a cache
         if (fit > by_index) fit = by_index;
         p.round = fit < 1 ? 1 : fit < batch ? fit : batch;
         p.dense_bytes = padded(paged_workspace_bytes(T, (int)p.round, q_heads, kv_heads, D, max_q, max_kv, window, true));

@@ -165,9 +165,17 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const Params P)
     let_next_kernel_start();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t rows = P.T * P.q_heads, row = blockIdx.x, t = row / P.q_heads;
-    if (t >= P.cu_q[P.batch] || (P.filter && !joined(P, t))) return;
-    float2 ml = make_float2(-INFINITY, 0.f);
+    // Asked for side by side: where the tokens end, maxima and sums, and the first parts, before it is known whether they were written.
+    constexpr int kV = D / 64, kAhead = 8;                              // float2 pieces per lane; parts of a warp
+    const int64_t end = P.cu_q[P.batch];
+    float2 ml = make_float2(-INFINITY, 0.f), ahead[kAhead][kV];
     if (tid < P.splits) ml = P.part_ml[(int64_t)tid * rows + row];
+    const auto piece = [&](int s, int j) { return reinterpret_cast<const float2*>(P.part_o + ((int64_t)s * rows + row) * D)[lane + 32 * j]; };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+        for (int j = 0; j < kV; ++j) ahead[i][j] = warp + 8 * i < P.splits ? piece(warp + 8 * i, j) : make_float2(0.f, 0.f);
+    if (t >= end || (P.filter && !joined(P, t))) return;
     float mx = ml.x;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -188,21 +196,25 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const Params P)
     sum = 0.f;
 #pragma unroll
     for (int v = 0; v < 8; ++v) sum += s_red[1][v];
-    constexpr int kV = D / 64;                                          // float2 pieces per lane
     float2 acc[kV];
 #pragma unroll
     for (int j = 0; j < kV; ++j) acc[j] = make_float2(0.f, 0.f);
-#pragma unroll 4
-    for (int s = warp; s < P.splits; s += 8) {
-        const float ws = s_w[s];
-        const float2* o = reinterpret_cast<const float2*>(P.part_o + ((int64_t)s * rows + row) * D);
+    const auto add = [&](int j, float2 v, float ws) {
+        if (!(ws >= 0.f)) v = make_float2(0.f, 0.f);
+        acc[j].x = fmaf(v.x, ws, acc[j].x);
+        acc[j].y = fmaf(v.y, ws, acc[j].y);
+    };
 #pragma unroll
-        for (int j = 0; j < kV; ++j) {
-            const float2 v = ws >= 0.f ? o[lane + 32 * j] : make_float2(0.f, 0.f);
-            acc[j].x = fmaf(v.x, ws, acc[j].x);
-            acc[j].y = fmaf(v.y, ws, acc[j].y);
-        }
+    for (int i = 0; i < kAhead; ++i) {
+        const int s = warp + 8 * i;
+        if (s < P.splits)
+#pragma unroll
+            for (int j = 0; j < kV; ++j) add(j, ahead[i][j], s_w[s]);
     }
+#pragma unroll 4
+    for (int s = warp + 8 * kAhead; s < P.splits; s += 8)
+#pragma unroll
+        for (int j = 0; j < kV; ++j) add(j, s_w[s] >= 0.f ? piece(s, j) : make_float2(0.f, 0.f), s_w[s]);
 #pragma unroll
     for (int j = 0; j < kV; ++j) *reinterpret_cast<float2*>(&s_o[warp][2 * (lane + 32 * j)]) = acc[j];
     __syncthreads();

@@ -502,11 +502,12 @@ int matq_quantize_groups(const void *W, int64_t N, int64_t K, int64_t ldw, int g
  * (11) Linear layer on weights in 4-bit groups, for a few tokens:
  *       Y[m,n] = sum over the groups i of row n of  scale_ni * sum_k x[m,k] q[n,k]  +  low_ni * sum_k x[m,k]   (k in the group)
  *     The inner sums are products of exact codes with the bf16 activations, accumulated in fp32; what follows is fp32, rounded once more to bf16 when out_type asks
- *     for it.  A token whose largest activation is 2^120 times another loses the smaller one.  A token that holds NaN or Inf gets NaN or Inf, and no other token is
- *     touched.  Any number of tokens; the weights are read once for up to 32 * group / 128 of them.
+ *     for it.  Activations below 2^-110 of their token's largest may count as zero.  A token that holds NaN or Inf gets NaN or Inf, and no other token is
+ *     touched.  Any number of tokens; the weights are read again for every 8 to 32 of them.
  *   packed, params  in   as written by (10), dense rows        x  in  bf16 [M, K], row stride ldx        Y  out  fp32 or bf16 [M, N], row stride ldy
  *   flags           0 or MATQ_GEMV_PDL (the previous kernel of the stream writes neither packed nor params)
- *   Requires K % group == 0, K <= 65536, ldx % 8 == 0, N below 2^31, packed, params and x 16-byte aligned (MATQ_ERR_SHAPE past 2^20 row tiles or 65535 token tiles).
+ *   Requires K % group == 0, K <= 65536, ldx % 8 == 0, N below 2^31, packed, params and x 16-byte aligned, any ldy >= N.  MATQ_ERR_SHAPE for M
+ *   above 65535 times the tokens that share a reading of the weights (8 at least).
  */
 int matq_gemv_groups(const uint8_t *packed, int64_t N, int64_t K, int group, const void *params, const void *x, int64_t M, int64_t ldx,
                      int out_type, void *Y, int64_t ldy, unsigned flags, void *stream);
@@ -542,10 +543,16 @@ int matq_kv4_append(const matq_paged_kv4 *cache, int64_t T, const void *q, int q
                     void *q_out, int64_t ldqo, int32_t *dev_status, void *stream);
 
 /*
- * (13) As (9) for a cache in 4-bit groups: keys and values are what its codes and groups stand for.  Sequences with few new tokens read the cache as it is; for
- *     sequences with more, keys and values are unpacked to bf16 in the workspace first (one more rounding of each), a few sequences at a time.
- *   Arguments and errors as for (9), but max_q and max_kv are bounds: a sequence with more new tokens or keys may be refused with MATQ_ERR_PAGE.
- *   workspace   at least matq_attn_paged4_workspace_bytes(...) bytes for this call's sizes, 16-byte aligned; contents need not be initialised.
+ * (13) As (9) for a cache in 4-bit groups: keys and values are what its codes and groups stand for.  Sequences with up to 16 rows (tokens times heads of a key head)
+ *     read the cache as it is.  With more rows, keys and values may be unpacked to fp16 in the workspace first, scaled by powers of two so that fp16's range suffices
+ *     (each is off by 2^-12 of itself at most, or by 2^-39 of the largest of its sequence and head); a call does so where it costs less.  Weights are rounded to 11
+ *     bits then, and to 8 bits otherwise (8 times two for up to four rows).
+ *   Arguments and errors as for (9), but max_q and max_kv are bounds: a sequence with more new tokens or keys may be refused with MATQ_ERR_PAGE, its outputs
+ *   unspecified.  MATQ_ERR_TIMEOUT comes from calls that unpack only.
+ *   workspace   at least matq_attn_paged4_workspace_bytes(...) bytes for this call's sizes, 16-byte aligned; contents need not be initialised.  A call that unpacks
+ *           does so for as many sequences at a time as fit into 512 MB (4 * kv_heads * head_dim bytes a key, for max_kv keys, or max_q + window where that is
+ *           less), and for one at a time where not even one fits; where one needs more than 16 GB, the cache is read
+ *           as it is.  As for (9), smaller calls can need more.
  */
 size_t matq_attn_paged4_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim,
                                         int64_t max_q, int64_t max_kv, int64_t window);

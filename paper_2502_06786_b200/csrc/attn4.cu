@@ -21,6 +21,8 @@ constexpr int kUnpackPage = 256, kUnpackThreads = 256, kUnpackKeys = 128;
 constexpr int64_t kMixedRows = 16;
 // Bytes of unpacked keys and values that a call's workspace holds at a time: sequences that do not fit together are served one round after another.
 constexpr int64_t kUnpackBytes = 512ll << 20;
+// Calls whose bounds let a single sequence take more than this read the cache as it is.
+constexpr int64_t kUnpackMost = 16ll << 30;
 // Most bytes of partial outputs: they are indexed by the call's tokens, of which few may be of sequences that are split.
 constexpr double kPartBytes = 256.0 * (1 << 20);
 
@@ -313,8 +315,8 @@ inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64
     const int64_t width = max_kv > kUnpackPage ? (max_kv + kUnpackPage - 1) / kUnpackPage : 1;
     int64_t pages = width;                                              // of kUnpackPage keys, that a sequence is unpacked to
     if (window > 0 && window < max_kv && (window + max_q) / kUnpackPage + 2 < pages) pages = (window + max_q) / kUnpackPage + 2;
-    const int64_t by_index = kMost / (pages * kUnpackPage * kv_heads);  // sequences: the 128-row kernels' limit on the rows of a cache
-    if (rows > kMixedRows && by_index > 0) {
+    const double per_seq = (double)(pages * kUnpackPage) * kv_heads * D * 4;        // bytes; the rows of a cache that the 128-row kernels index are far fewer than 2^31 then
+    if (rows > kMixedRows && per_seq <= (double)kUnpackMost) {
         const int64_t range = window > 0 && window + max_q < max_kv ? window + max_q : max_kv;
         const double dense = 9000 + 4.0 * T * q_heads * D / 6000 + 8.0 * batch * range * kv_heads * D / 5000 + paged_cost(T, batch, q_heads, kv_heads, D, max_q, max_kv, window);
         mixed = dense < direct;
@@ -331,9 +333,7 @@ inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64
     if (mixed) {
         p.new_width = width;
         p.new_pages = pages;
-        const int64_t per_seq = p.new_pages * kUnpackPage * kv_heads * D * 4;
-        int64_t fit = kUnpackBytes / per_seq;
-        if (fit > by_index) fit = by_index;
+        const int64_t fit = (int64_t)((double)kUnpackBytes / per_seq);
         p.round = fit < 1 ? 1 : fit < batch ? fit : batch;
         p.dense_bytes = padded(paged_workspace_bytes(T, (int)p.round, q_heads, kv_heads, D, max_q, max_kv, window, true));
         // the last round may have fewer sequences, which can be split into more parts

@@ -521,7 +521,7 @@ extern "C" int matq_gemv_groups(const uint8_t* packed, int64_t N, int64_t K, int
     if (!aligned16(packed) || !aligned16(params) || !aligned16(x)) return MATQ_ERR_ALIGNMENT;
     const int S = kBlock / group;
     const GemvPlan p = plan_gemv(M, N, K, S, sm_count());
-    if (p.cost < 0 || p.steps >= (1ll << 30) || p.row_ctas > 65535 || p.token_blocks > 65535) return MATQ_ERR_SHAPE;
+    if (p.cost < 0 || p.token_blocks > 65535) return MATQ_ERR_SHAPE;
     GemvParams P;
     P.packed = packed; P.params = static_cast<const uint32_t*>(params); P.x = static_cast<const __nv_bfloat16*>(x); P.y = y;
     P.N = N; P.K = K; P.M = M; P.ldx = ldx; P.ldy = ldy; P.groups = K / group;

@@ -187,6 +187,12 @@ def test_attn_paged4_generous_bounds_change_little(case):
             _check(*_attend(*CASES[case], seed=200 + case, hints=hints))
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attn_paged4_chunks_with_bounds_that_say_nothing(D):
+    # more keys than could be unpacked: rows by the hundred read the cache as it is
+    _check(*_attend([200, 1, 30], [500, 40, 333], 8, 2, D, 32, seed=300, hints=(200, (1 << 31) - 1)))
+
+
 def test_attn_paged4_fewer_tokens_than_rows_and_bounds():
     # rows behind the last sequence, as in a padded batch whose call was made for more tokens
     for lens in ([300], [300, 50]):

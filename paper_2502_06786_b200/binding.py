@@ -576,7 +576,8 @@ def attn_paged4_workspace_bytes(T, batch, q_heads, kv_heads, head_dim, max_q, ma
 
 
 def attn_paged4(q, cache, page_table, cu_q, kv_len, max_q, max_kv, scale=None, softcap=0.0, window=0, out=None, workspace=None, dev_status=None):
-    """matq_attn_paged4.  As attn_paged for a cache as in kv4_append; max_q and max_kv must not be too small.
+    """matq_attn_paged4.  As attn_paged for a cache as in kv4_append; max_q and max_kv are bounds: a sequence
+    with more new tokens or keys may be refused (ERR_PAGE).  Without ``workspace`` one is allocated; a chunk's takes 4 * kv_heads * head_dim bytes a key.
     Returns out, bf16 [T, q_heads, head_dim]."""
     if out is None:
         out = torch.empty(q.shape, dtype=_BF16, device=q.device)

@@ -1,4 +1,4 @@
-// Attention of few query rows over the paged cache in 4-bit groups (kv4_cache.cuh): a CTA takes 8 or 16 rows (token, head of the group) of one key head and a
+// Attention of few query rows over the paged cache in 4-bit groups (kv4_cache.cuh): a CTA takes 4, 8 or 16 rows (token, head of the group) of one key head and a
 // part of the key range, as in attn_decode.cuh, and reads a quarter of the bytes.
 //
 // A page's tile of 16 keys of a head stands together, keys, values and groups.  A warp takes every kWarps-th tile of the CTA's range and brings its own tiles into
@@ -14,6 +14,10 @@
 // 2^-15 of the largest at most), which also halves the products and the masks; in the second the weight and what its rounding to bf16 left out.
 // ldmatrix with .trans brings two keys' codes of four elements into a word: the four masks of a word give rows of O^T four elements apart, which is undone when
 // the lane stores its four neighbouring elements.
+//
+// Bound.  Single tokens of groups of two or four: HBM in part (64 ragged ones over 5 to 8000 keys, 16/8 heads of 256: 134 us, 4.1 TB/s) and the instructions of a tile;
+// one token over 32768 keys, 32/8 heads of 128: 16.8 us, of which the tiles are 9, the start and the join the rest.  8 and 16 rows: instructions and their latencies (1.8
+// to 2.3 a cycle of an SM), 46 us for 16 sequences of 8 to 24 rows over a window of 4096.
 #pragma once
 
 #include <type_traits>

@@ -165,7 +165,8 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const Params P)
     let_next_kernel_start();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t rows = P.T * P.q_heads, row = blockIdx.x, t = row / P.q_heads;
-    // Asked for side by side: where the tokens end, maxima and sums, and the first parts, before it is known whether they were written.
+    // Asked for side by side: where the tokens end, maxima and sums, and the first parts, before it is known whether they were written (one trip to memory, not three:
+    // 1.4 us of a decode step).
     constexpr int kV = D / 64, kAhead = 8;                              // float2 pieces per lane; parts of a warp
     const int64_t end = P.cu_q[P.batch];
     float2 ml = make_float2(-INFINITY, 0.f), ahead[kAhead][kV];

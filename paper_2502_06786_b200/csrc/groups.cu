@@ -8,7 +8,9 @@ namespace grp {
 
 // ---------------------------------------------------------------- quantiser
 // A thread takes eight weights, the threads of a group are neighbours in a warp and exchange its two ends by shuffles.  Groups follow one another without
-// a gap, across the ends of rows too, so that codes and groups have one running index each.  Every weight is read once: HBM.
+// a gap, across the ends of rows too, so that codes and groups have one running index each.  Every weight is read once: HBM, and beside it the instructions of a
+// weight (correctly rounded operations one by one; two weights in one instruction where there is one): 9216 x 2304, groups of 64, 12.1 us (4.5 TB/s), 14336 x 4096,
+// groups of 128, 27.2 us (5.5 TB/s).  Four pieces a thread, requested together.
 constexpr int kQuantThreads = 256, kQuantPieces = 4;
 
 template <int GROUP, bool DENSE>
@@ -72,7 +74,10 @@ cudaError_t launch_quantize(const void* W, int64_t N, int64_t K, int64_t ldw, vo
 //
 // A CTA takes a part of K, staged in shared memory for its tokens, and walks the matrix in steps of 16 RW rows; its warps are RW row tiles times SK parts of
 // that part, block by block of 128.  Each warp brings its own blocks into its own ring by cp.async, across the ends of steps, so that the ring never drains.
-// The CTAs of a cluster share K and add their sums through distributed shared memory.  All sums are taken in a fixed order.  Bound: HBM (and the start of a launch).
+// The CTAs of a cluster share K and add their sums through distributed shared memory.  All sums are taken in a fixed order.
+//
+// Bound: one token, the chain of a launch (start, tokens' trip to memory, staging, the last blocks' trip, sums): 9216 x 2304 5.1 us, 14336 x 4096 10.5, 65536 x 2304 (a step
+// of every CTA follows another) 19.7 us or 4.3 TB/s.  16 tokens: latencies of 16 warps (1.9 instructions a cycle) and the cluster's sums: 3584 x 14336 18.0 us.
 constexpr int kBlock = 128;
 // Warps of a CTA: eight, and two CTAs on an SM, as long as a CTA has one block of columns; sixteen beside tokens that take more shared memory.
 __host__ __device__ constexpr int warps_of(int nt) { return nt == 1 ? 8 : 16; }

@@ -499,7 +499,7 @@ int matq_quantize_groups(const void *W, int64_t N, int64_t K, int64_t ldw, int g
                          int32_t *dev_status, void *stream);
 
 /*
- * (11) Linear layer on weights in 4-bit groups, for a few tokens:
+ * (11) Linear layer on weights in 4-bit groups, for a few tokens (for more see (11b)):
  *       Y[m,n] = sum over the groups i of row n of  scale_ni * sum_k x[m,k] q[n,k]  +  low_ni * sum_k x[m,k]   (k in the group)
  *     The inner sums are products of exact codes with the bf16 activations, accumulated in fp32; what follows is fp32, rounded once more to bf16 when out_type asks
  *     for it.  Activations below 2^-110 of their token's largest may count as zero.  A token that holds NaN or Inf gets NaN or Inf, and no other token is
@@ -511,6 +511,22 @@ int matq_quantize_groups(const void *W, int64_t N, int64_t K, int64_t ldw, int g
  */
 int matq_gemv_groups(const uint8_t *packed, int64_t N, int64_t K, int group, const void *params, const void *x, int64_t M, int64_t ldx,
                      int out_type, void *Y, int64_t ldy, unsigned flags, void *stream);
+
+/*
+ * (11b) The same for many tokens, on the fifth-generation tensor cores.  Weights less their group's middle and tokens enter the products as fp16, exactly (with a power
+ *     of two per row and per token; what is below 2^-35 of a row's largest group, or 2^-31 of a token's largest activation, is rounded to that); the sums of a
+ *     token's groups, which the middles are multiplied with, as two fp16 (22 bits).  All sums are fp32; in tensor memory sums are cut off rather than rounded, so that with
+ *     fp32 outputs every 1024 columns are added up by themselves.  A group that stands for NaN makes its row NaN.
+ *   workspace   at least matq_gemm_groups_workspace_bytes(M, N, K, group) bytes (2 M K (1 + 4 / group) + 4 N K / group and a little), 16-byte aligned; contents need not
+ *           be initialised
+ *   Everything else as for (11); M, N below 2^31 - 256, MATQ_ERR_SHAPE past 2^30 tiles of 16 x 128.  dev_status = MATQ_ERR_TIMEOUT when a device-side wait gives up; Y is
+ *   then unspecified.
+ */
+size_t matq_gemm_groups_workspace_bytes(int64_t M, int64_t N, int64_t K, int group);
+/* 1 for sizes at which (11b) takes less time than (11), as far as measured; host only. */
+int matq_gemm_groups_pays(int64_t M, int64_t N, int64_t K, int group);
+int matq_gemm_groups(const uint8_t *packed, int64_t N, int64_t K, int group, const void *params, const void *x, int64_t M, int64_t ldx,
+                     int out_type, void *Y, int64_t ldy, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
 
 /*
  * A paged cache of keys and values in 4-bit groups of 64 elements along the head.  As matq_paged_kv, but for the cache itself: the 16 keys of a page with
@@ -562,7 +578,7 @@ int matq_attn_paged4(const matq_paged_kv4 *cache, int64_t T, const void *q, int 
                      int32_t *dev_status, void *stream);
 
 /*
- * Testing hook for the error paths of (7), (9) and (13), as matq_gemm_multi_test_stall: while `on` is non-zero their kernels issue no
+ * Testing hook for the error paths of (7), (9), (11b) and (13), as matq_gemm_multi_test_stall: while `on` is non-zero their kernels issue no
  * copies and their waits give up after about a millisecond; a call reports MATQ_ERR_TIMEOUT through dev_status, returns, and leaves the
  * GPU ready for the next.  (7) has no device-side wait for up to 8 tokens and few codes, and ignores it there.  Process-wide; returns the previous setting.
  */

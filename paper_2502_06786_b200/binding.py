@@ -32,7 +32,7 @@ EXPORTS = ["matq_status_string", "matq_version", "matq_packed_row_bytes", "matq_
            "matq_gemm_multi_test_stall", "matq_slice_pack_test_stall",
            "matq_gemm_multi_static_max_bytes", "matq_gemm_multi_static",
            "matq_quantize_tokens", "matq_gemm_a8", "matq_gemm_a8_plan", "matq_kv_append", "matq_attn_paged_workspace_bytes", "matq_attn_paged",
-           "matq_quantize_groups", "matq_gemv_groups", "matq_kv4_tile_bytes", "matq_kv4_append", "matq_attn_paged4_workspace_bytes", "matq_attn_paged4",
+           "matq_quantize_groups", "matq_gemv_groups", "matq_gemm_groups_workspace_bytes", "matq_gemm_groups_pays", "matq_gemm_groups", "matq_kv4_tile_bytes", "matq_kv4_append", "matq_attn_paged4_workspace_bytes", "matq_attn_paged4",
            "matq_serving_test_stall"]
 
 
@@ -126,6 +126,12 @@ def _load():
     lib.matq_quantize_groups.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, vp]
     lib.matq_gemv_groups.restype = i32
     lib.matq_gemv_groups.argtypes = [vp, i64, i64, i32, vp, vp, i64, i64, i32, vp, i64, u32, vp]
+    lib.matq_gemm_groups_workspace_bytes.restype = sz
+    lib.matq_gemm_groups_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.matq_gemm_groups_pays.restype = i32
+    lib.matq_gemm_groups_pays.argtypes = [i64, i64, i64, i32]
+    lib.matq_gemm_groups.restype = i32
+    lib.matq_gemm_groups.argtypes = [vp, i64, i64, i32, vp, vp, i64, i64, i32, vp, i64, vp, sz, vp, vp]
     lib.matq_kv4_tile_bytes.restype = i64
     lib.matq_kv4_tile_bytes.argtypes = [i32]
     lib.matq_kv4_append.restype = i32
@@ -544,14 +550,39 @@ def quantize_groups(W, group=128, packed=None, params=None, dev_status=None):
     return packed, params
 
 
-def gemv_groups(packed, params, x, y=None, out_dtype=torch.float32, flags=0):
-    """matq_gemv_groups.  packed, params: as returned by quantize_groups; x: bf16 [M, K].  Returns y [M, N], fp32 or bf16 (the type of ``y`` when it is
-    given, ``out_dtype`` otherwise)."""
+def gemv_groups(packed, params, x, y=None, out_dtype=torch.float32, flags=0, workspace=None, dev_status=None):
+    """matq_gemv_groups, or matq_gemm_groups for the numbers of tokens at which that takes less time (``gemm_groups_pays``).  packed, params: as returned by
+    quantize_groups; x: bf16 [M, K].  Returns y [M, N], fp32 or bf16 (the type of ``y`` when it is given, ``out_dtype`` otherwise).  ``workspace`` and ``dev_status`` are for
+    the second."""
     if y is None:
         y = torch.empty((x.shape[0], packed.shape[0]), dtype=out_dtype, device=x.device)
+    if x.shape[0] > 16 and not flags & ~GEMV_PDL and params.shape[1] and gemm_groups_pays(x.shape[0], packed.shape[0], x.shape[1], x.shape[1] // params.shape[1]):
+        return gemm_groups(packed, params, x, y=y, workspace=workspace, dev_status=dev_status)
     st = _serving.gemv_groups(packed, params, x, y, flags)
     if st:
         raise MatqError(st, "matq_gemv_groups")
+    return y
+
+
+def gemm_groups_pays(M, N, K, group) -> bool:
+    return bool(_lib.matq_gemm_groups_pays(M, N, K, group))
+
+
+def gemm_groups_workspace_bytes(M, N, K, group) -> int:
+    return int(_lib.matq_gemm_groups_workspace_bytes(M, N, K, group))
+
+
+def gemm_groups(packed, params, x, y=None, out_dtype=torch.float32, workspace=None, dev_status=None):
+    """matq_gemm_groups: a linear layer on weights in 4-bit groups for many tokens; arguments as for gemv_groups.  Returns y [M, N]."""
+    if y is None:
+        y = torch.empty((x.shape[0], packed.shape[0]), dtype=out_dtype, device=x.device)
+    if workspace is None and params.dim() == 3 and params.shape[1]:
+        need = gemm_groups_workspace_bytes(x.shape[0], packed.shape[0], x.shape[1], x.shape[1] // params.shape[1])
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    st = _serving.gemm_groups(packed, params, x, y, workspace, dev_status)
+    if st:
+        raise MatqError(st, "matq_gemm_groups")
     return y
 
 
@@ -593,5 +624,5 @@ def attn_paged4(q, cache, page_table, cu_q, kv_len, max_q, max_kv, scale=None, s
 
 
 def serving_test_stall(on) -> int:
-    """matq_serving_test_stall: switch the "issue no copies" test mode of gemm_a8, attn_paged and attn_paged4; returns the previous setting."""
+    """matq_serving_test_stall: switch the "issue no copies" test mode of gemm_a8, attn_paged, gemm_groups and attn_paged4; returns the previous setting."""
     return int(_lib.matq_serving_test_stall(1 if on else 0))

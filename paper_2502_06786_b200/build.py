@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmatq.so")
 MODULE = os.path.join(HERE, "_serving.so")
 SOURCES = ["api.cu", "quantize.cu", "slice_pack.cu", "gemv.cu", "gemm_multi.cu", "gemm_multi_static.cu",
-           "tokens.cu", "groups.cu", "gemm_a8.cu", "kv_append.cu", "attn_paged.cu",
+           "tokens.cu", "groups.cu", "groups_many.cu", "gemm_a8.cu", "kv_append.cu", "attn_paged.cu",
            "kv4_append.cu", "attn4.cu", "attn4_chunk.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr", "-Wno-deprecated-gpu-targets"]

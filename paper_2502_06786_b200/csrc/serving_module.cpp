@@ -328,22 +328,57 @@ PyObject* quantize_groups(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// what the two linear layers share: packed, params, x, y
+struct Grouped {
+    Matrix c, x, y;
+    Groups g;
+    int group;
+    int out;
+};
+Grouped grouped(PyObject* const* a) {
+    Grouped l;
+    l.c = plane(a[0], "packed");
+    l.x = mat(a[2], at::kBFloat16, "x");
+    l.g = groups(a[1], "params");
+    if (l.x.cols != l.c.cols * 2) fail(PyExc_ValueError, "x", "packed [N, K / 2] and x [M, K] required");
+    if (l.g.rows != l.c.rows || l.g.per_row < 1 || l.x.cols % l.g.per_row != 0) fail(PyExc_ValueError, "params", "bf16 [N, K / group, 2] required");
+    const int64_t group = l.x.cols / l.g.per_row;
+    l.group = (int)(group < 1 << 30 ? group : 0);
+    const bool bf16 = is_bf16(a[3]);
+    l.y = mat(a[3], bf16 ? at::kBFloat16 : at::kFloat, "y");
+    if (l.y.rows != l.x.rows || l.y.cols != l.c.rows) fail(PyExc_ValueError, "y", "[M, N] required");
+    l.out = bf16 ? MATQ_OUT_BF16 : MATQ_OUT_F32;
+    return l;
+}
+
 // packed, params, x, y, flags
 PyObject* gemv_groups(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(n, 5, [&] {
-        const Matrix c = plane(a[0], "packed"), x = mat(a[2], at::kBFloat16, "x");
-        const Groups g = groups(a[1], "params");
-        if (x.cols != c.cols * 2) fail(PyExc_ValueError, "x", "packed [N, K / 2] and x [M, K] required");
-        if (g.rows != c.rows || g.per_row < 1 || x.cols % g.per_row != 0) fail(PyExc_ValueError, "params", "bf16 [N, K / group, 2] required");
-        const int64_t group = x.cols / g.per_row;
-        const bool bf16 = is_bf16(a[3]);
-        const Matrix y = mat(a[3], bf16 ? at::kBFloat16 : at::kFloat, "y");
-        if (y.rows != x.rows || y.cols != c.rows) fail(PyExc_ValueError, "y", "[M, N] required");
+        const Grouped l = grouped(a);
         const int flags = small_integer(a[4], "flags");
         void* s = stream();
         return unlocked([&] {
-            return matq_gemv_groups(static_cast<const uint8_t*>(c.p), c.rows, x.cols, (int)(group < 1 << 30 ? group : 0), g.p, x.p, x.rows, x.ld,
-                                    bf16 ? MATQ_OUT_BF16 : MATQ_OUT_F32, y.p, y.ld, (unsigned)flags, s);
+            return matq_gemv_groups(static_cast<const uint8_t*>(l.c.p), l.c.rows, l.x.cols, l.group, l.g.p, l.x.p, l.x.rows, l.x.ld, l.out, l.y.p, l.y.ld, (unsigned)flags, s);
+        });
+    });
+}
+
+// packed, params, x, y, workspace, dev_status
+PyObject* gemm_groups(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(n, 6, [&] {
+        const Grouped l = grouped(a);
+        void* ws = nullptr;
+        size_t bytes = 0;
+        if (a[4] != Py_None) {
+            const at::Tensor& t = tensor(a[4], std::nullopt, "workspace");
+            if (!t.is_contiguous()) fail(PyExc_TypeError, "workspace", "a contiguous tensor is required");
+            ws = t.data_ptr();
+            bytes = t.nbytes();
+        }
+        int32_t* status = status_word(a[5]);
+        void* s = stream();
+        return unlocked([&] {
+            return matq_gemm_groups(static_cast<const uint8_t*>(l.c.p), l.c.rows, l.x.cols, l.group, l.g.p, l.x.p, l.x.rows, l.x.ld, l.out, l.y.p, l.y.ld, ws, bytes, status, s);
         });
     });
 }
@@ -355,6 +390,7 @@ PyMethodDef methods[] = {
     {"attn_paged", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_paged)), METH_FASTCALL, nullptr},
     {"quantize_groups", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(quantize_groups)), METH_FASTCALL, nullptr},
     {"gemv_groups", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(gemv_groups)), METH_FASTCALL, nullptr},
+    {"gemm_groups", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(gemm_groups)), METH_FASTCALL, nullptr},
     {"kv4_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv4_append)), METH_FASTCALL, nullptr},
     {"attn_paged4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(attn_paged4)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

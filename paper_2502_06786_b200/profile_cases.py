@@ -118,10 +118,10 @@ def main(which: str) -> None:
                 mq.kv_append(kc, vc, table, cu, lens, k, v, cos_sin=ang, q=q, q_out=q)
                 mq.attn_paged(q, kc, vc, table, cu, lens, new, keys)
     elif which == "groups":
-        # weights in 4-bit groups of 128: the quantiser, one token and 16 through a Gemma-2-2B gate matrix
+        # weights in 4-bit groups of 128: the quantiser, one token, 16, 64 and 1024 through a Gemma-2-2B gate matrix
         Ws = [torch.randn(N, K, device="cuda").mul_(0.02).to(torch.bfloat16) for _ in range(n)]
         held = [mq.quantize_groups(W, 128) for W in Ws]
-        for M in (1, 16):
+        for M in (1, 16, 64, 1024):
             X = torch.randn(M, K, device="cuda").to(torch.bfloat16)
             Y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
             for packed, params in held:

@@ -7,7 +7,7 @@ Shows the serving calls as they are used together.  A layer keeps its matrices o
 slice (``quantize_tokens`` once per input, ``gemm_a8`` per matrix).  New keys and values are rotated and appended to a paged cache
 (``kv_append``), and the new tokens attend to it (``attn_paged``).  Norms, activations and residual sums are plain torch.
 
-With ``Config.group`` a matrix is kept in 4-bit groups of that many weights instead (``quantize_groups``, ``gemv_groups``), which lose less of it at the same
+With ``Config.group`` a matrix is kept in 4-bit groups of that many weights instead (``quantize_groups``, ``gemv_groups``, for prompts ``gemm_groups``), which lose less of it at the same
 size than one scale per channel, and with ``Config.cache_bits = 4`` the cache takes a little over a quarter of the memory (``kv4_append``, ``attn_paged4``).
 """
 from __future__ import annotations

@@ -95,6 +95,25 @@ def gemv(codes, params, x):
     return x @ W.t(), 2.0 ** -23 * (48 + params.shape[1]) * (x.abs() @ size.t()) + 1e-37
 
 
+def gemm(codes, params, x, bf16_out=False):
+    """gemv's for the call for many tokens.  Products are exact: scale (code - 8) of 11 bits with x, (low + 8 scale) with the group's sum of x.  Sums in tensor memory are cut
+    off: 2^-23 of the terms' magnitudes a step, twice that with what a step's sixteen products lose to one another, for 64 steps (1024 columns), or with bf16 outputs for all of the
+    row's; eight more additions per group's sum, which is then held in 22 bits, and those of the segments.  Beside that, what is far below a row's largest group (2^-35 of it: a scale off by half a step of fp16, times 8) or a
+    token's largest element (2^-31) is rounded to such a step."""
+    group = codes.shape[1] // params.shape[1]
+    K = codes.shape[1]
+    s, low = (torch.from_numpy(bf16_values(params[..., i]).astype(np.float64)) for i in (0, 1))
+    c = torch.from_numpy(codes.astype(np.float64)).unflatten(1, (-1, group))
+    x = x.double().cpu()
+    W = (c * s[..., None] + low[..., None]).flatten(1)
+    size = ((c - 8).abs() * s[..., None] + low.abs()[..., None] + 8 * s[..., None]).flatten(1)
+    terms = x.abs() @ size.t()
+    steps = (K + 4 * params.shape[1]) / 16 + 8 if bf16_out else 72 + K / 1024
+    top = torch.maximum(low.abs(), 8 * s).amax(1)
+    small = 2.0 ** -35 * x.abs().sum(1)[:, None] * top[None] + 2.0 ** -31 * x.abs().amax(1)[:, None] * size.sum(1)[None]
+    return x @ W.t(), (2.0 ** -22 * steps + 2.0 ** -20) * terms + small + 1e-37
+
+
 def attn(q, tiles, table, cu, kv_len, scale, softcap=0.0, window=0, longest=None):
     """(out, bound) in 64 bits, one query row at a time over the keys it sees.  The output is rounded to 8 bits.  A score is off by 2^-20 of
     sum_d |q_d| (15 scale + |low|) at most (a few dozen fp32 steps) and, where queries are taken as 16-bit integers (calls of up to four rows: the longest sequence's bound times the heads of a group), by 2^-15 of the

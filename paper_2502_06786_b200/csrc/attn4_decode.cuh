@@ -3,7 +3,7 @@
 //
 // A page's tile of 16 keys of a head stands together, keys, values and groups.  A warp takes every kWarps-th tile of the CTA's range and brings its own tiles into
 // its own ring (cp.async, 16 bytes a lane), so that nothing but the start and the end is shared between warps.  (One bulk copy a tile costs about 50 cycles of the
-// SM's copy engine: filling the rings took 4600 cycles at D = 128, 6900 at D = 64.)  Two or three CTAs share an SM: one's start, 3000 cycles of trips to memory,
+// SM's copy engine: filling the rings took 4600 cycles at D = 128, 6900 at D = 64.)  Two to four CTAs share an SM: one's start, 3000 cycles of trips to memory,
 // and end run beside the other's tiles.  With a tile a warp does
 //   S^T = K Q^T     the codes are the rows, masked out of their words without a conversion (groups.cu); per group of 64 elements
 //                   s = scale * sum q code + low * sum q, in fp32;
@@ -16,7 +16,7 @@
 // the lane stores its four neighbouring elements.
 //
 // Bound.  Single tokens of groups of two or four: HBM in part (64 ragged ones over 5 to 8000 keys, 16/8 heads of 256: 134 us, 4.1 TB/s) and the instructions of a tile;
-// one token over 32768 keys, 32/8 heads of 128: 16.8 us, of which the tiles are 9, the start and the join the rest.  8 and 16 rows: instructions and their latencies (1.8
+// one token over 32768 keys, 32/8 heads of 128: 15.5 us, of which the tiles are 8, the start and the join the rest.  8 and 16 rows: instructions and their latencies (1.8
 // to 2.3 a cycle of an SM), 46 us for 16 sequences of 8 to 24 rows over a window of 4096.
 #pragma once
 
@@ -110,9 +110,10 @@ __device__ __forceinline__ uint2 digits_of_piece(uint4 v, int e, int which, floa
     return make_uint2(four(0), four(1));
 }
 
-// CTAs of an SM and their warps: what 65536 registers hold.
-__host__ __device__ constexpr int decode4_ctas(int D, int R) { return D == 64 && R == 4 ? 3 : 2; }
-__host__ __device__ constexpr int decode4_warps(int D, int R) { return D == 128 && R == 4 ? 10 : (D == 256 && R == 8) || (D == 128 && R == 16) ? 6 : 8; }
+// CTAs of an SM and their warps: what 65536 registers hold without spills (D = 128, four rows: one token over 32768 keys 15.5 us, with ten warps a CTA 16.7; D = 64, four rows,
+// 64 tokens over 4000 keys 42.4 us, with three CTAs of eight warps 47), but for D = 256 with four rows, where 16 warps that spill are faster than 12 (134 against 145 us).
+__host__ __device__ constexpr int decode4_ctas(int D, int R) { return D == 64 && R == 4 ? 4 : 2; }
+__host__ __device__ constexpr int decode4_warps(int D, int R) { return (D == 64 && R == 4) || (D == 256 && R == 8) || (D == 128 && R == 16) ? 6 : 8; }
 
 // R: query rows of a CTA: 4 (two columns each), 8 or 16
 template <int D, int R>

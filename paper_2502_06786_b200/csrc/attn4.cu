@@ -3,8 +3,8 @@
 // Few rows per sequence and key head (single tokens, drafts) go to attn4_decode_kernel, which reads the cache as it is.  Sequences with more rows (chunks) are bound
 // by their products: their keys and values are unpacked once, into the workspace, and the 128-row kernels of matq_attn_paged take them from there.  That is one
 // more pass over what a chunk sees (read 9/16 of a byte an element, written and read 2), where unpacking inside the product kernel would be repeated by every query
-// tile and compete with the softmax for the SM's issue slots.  4096 tokens over 8192 keys, 32/8 heads of 128: 455 us, of which 13 prepare queries and maxima and 13
-// unpack; on a bf16 cache 416.
+// tile and compete with the softmax for the SM's issue slots.  4096 tokens over 8192 keys, 32/8 heads of 128: 449 us, of which about 20 are the
+// maxima, the unpacking and the queries; on a bf16 cache 416.
 //
 // Unpacked to bf16 a key would be rounded to 8 bits once more, and scores with it (with a few large channels outputs were off by 4.6e-3 of their norm, 2.7 times
 // what rounding them alone is).  fp16 keeps 11 bits.  Its range is made to suffice by powers of two: a query row is scaled by its largest element, the keys and the
@@ -65,58 +65,15 @@ __device__ __forceinline__ const uint8_t* tile_of(const Unpack& P, int b, int h,
 }
 __device__ __forceinline__ int half_exponent(uint32_t top) { return max((int)(top >> 23) - 127 - kHalfExp, -126); }        // what was taken off: 2^-126 .. 2^114
 
-// Before the unpacking, in one launch: queries to fp16 (the first query_ctas CTAs), and the largest magnitudes that the groups of a sequence's keys and values can
-// stand for, per head (the others: kTopTiles tiles of a sequence and head each, whose maximum they leave for the unpacking to join).  Bound: HBM.
+// Before the unpacking: the largest magnitudes that the groups of a sequence's keys and values can stand for, per head; a CTA takes kTopTiles tiles and leaves their
+// maximum for the unpacking to join.
 constexpr int kTopTiles = 32, kQueryPieces = 4;
-struct Prepare {
-    Unpack u;
-    const __nv_bfloat16* q;
-    int64_t ldq, T;
-    int q_heads;
-    int64_t query_ctas;
-    __half* to;
-    float* scale;
-};
 template <int D>
-__global__ void __launch_bounds__(kUnpackThreads) attn4_prepare_kernel(const Prepare A) {
+__global__ void __launch_bounds__(kUnpackThreads) attn4_top_kernel(const Unpack P) {
     after_previous_kernel();
     let_next_kernel_start();
     const int tid = threadIdx.x;
-    if (blockIdx.x < A.query_ctas) {
-        // a lane takes eight elements; the D / 8 lanes of a row share its largest
-        constexpr int kLanes = D / 8;
-        uint4 v[kQueryPieces];
-        const int64_t first = ((int64_t)blockIdx.x * kQueryPieces * kUnpackThreads + tid) / kLanes, rows = A.T * A.q_heads;
-        const int at = tid % kLanes * 8;
-#pragma unroll
-        for (int i = 0; i < kQueryPieces; ++i) {
-            const int64_t row = first + i * (kUnpackThreads / kLanes), t = rows <= 0x7fffffff ? (int64_t)((uint32_t)row / (uint32_t)A.q_heads) : row / A.q_heads;
-            v[i] = row < rows ? *reinterpret_cast<const uint4*>(A.q + t * A.ldq + (row - t * A.q_heads) * D + at) : make_uint4(0u, 0u, 0u, 0u);
-        }
-#pragma unroll
-        for (int i = 0; i < kQueryPieces; ++i) {
-            const int64_t row = first + i * (kUnpackThreads / kLanes);
-            uint32_t top = top_of_piece(v[i]);
-#pragma unroll
-            for (int w = 1; w < kLanes; w <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, w));
-            const int e = half_exponent(top);
-            const float f = exp2i(-e);
-            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-            uint32_t o[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const __half2 h = __floats2half2_rn(__uint_as_float(w[x] << 16) * f, __uint_as_float(w[x] & 0xffff0000u) * f);
-                o[x] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            if (row < rows) {
-                *reinterpret_cast<uint4*>(A.to + row * D + at) = make_uint4(o[0], o[1], o[2], o[3]);
-                if (at == 0) A.scale[row] = exp2i(e);
-            }
-        }
-        return;
-    }
-    const Unpack& P = A.u;
-    const unsigned rest = blockIdx.x - (unsigned)A.query_ctas, bh = rest / (unsigned)P.tops;
+    const unsigned rest = blockIdx.x, bh = rest / (unsigned)P.tops;
     const int b = (int)(bh / (unsigned)P.kv_heads), h = (int)(bh % (unsigned)P.kv_heads), chunk = (int)(rest % (unsigned)P.tops);
     __shared__ uint32_t s_most[2];
     if (tid < 2) s_most[tid] = 0u;
@@ -153,16 +110,60 @@ __global__ void __launch_bounds__(kUnpackThreads) attn4_prepare_kernel(const Pre
 }
 
 // Keys and values to fp16: a warp per tile of 16 keys, a lane 32 elements of a key at a time (its codes and those of its neighbours are 512 bytes side by side).
+// Queries to fp16, by the CTAs behind those: they are waited for no longer than keys and values are.
 // Bound: HBM, or the L2 that holds what it writes.
+struct Queries {
+    const __nv_bfloat16* q;
+    int64_t ldq, T;
+    int q_heads;
+    int64_t first_cta;
+    __half* to;
+    float* scale;
+};
 template <int D>
-__global__ void __launch_bounds__(kUnpackThreads) attn4_unpack_kernel(const Unpack P) {
+__global__ void __launch_bounds__(kUnpackThreads) attn4_unpack_kernel(const Unpack P, const Queries Q) {
     constexpr int kTiles = kUnpackThreads / 32, kCtaKeys = kTiles * kv4::kTileKeys;
     static_assert(kCtaKeys == kUnpackKeys, "a warp per tile");
     __shared__ float s_by[2];
     after_previous_kernel();
     let_next_kernel_start();
-    const int b = blockIdx.y, h = blockIdx.x % P.kv_heads, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int64_t chunk = blockIdx.x / P.kv_heads;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (blockIdx.x >= Q.first_cta) {
+        // a lane takes eight elements; the D / 8 lanes of a row share its largest
+        constexpr int kLanes = D / 8;
+        uint4 v[kQueryPieces];
+        const int64_t first = ((blockIdx.x - Q.first_cta) * kQueryPieces * kUnpackThreads + tid) / kLanes, rows = Q.T * Q.q_heads;
+        const int at = tid % kLanes * 8;
+#pragma unroll
+        for (int i = 0; i < kQueryPieces; ++i) {
+            const int64_t row = first + i * (kUnpackThreads / kLanes), t = rows <= 0x7fffffff ? (int64_t)((uint32_t)row / (uint32_t)Q.q_heads) : row / Q.q_heads;
+            v[i] = row < rows ? *reinterpret_cast<const uint4*>(Q.q + t * Q.ldq + (row - t * Q.q_heads) * D + at) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int i = 0; i < kQueryPieces; ++i) {
+            const int64_t row = first + i * (kUnpackThreads / kLanes);
+            uint32_t top = top_of_piece(v[i]);
+#pragma unroll
+            for (int w = 1; w < kLanes; w <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, w));
+            const int e = half_exponent(top);
+            const float f = exp2i(-e);
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            uint32_t o[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const __half2 h = __floats2half2_rn(__uint_as_float(w[x] << 16) * f, __uint_as_float(w[x] & 0xffff0000u) * f);
+                o[x] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            if (row < rows) {
+                *reinterpret_cast<uint4*>(Q.to + row * D + at) = make_uint4(o[0], o[1], o[2], o[3]);
+                if (at == 0) Q.scale[row] = exp2i(e);
+            }
+        }
+        return;
+    }
+    const unsigned per_batch = (unsigned)(P.new_pages * (kUnpackPage / kUnpackKeys)) * (unsigned)P.kv_heads, in_batch = blockIdx.x % per_batch;
+    const int b = (int)(blockIdx.x / per_batch), h = (int)(in_batch % (unsigned)P.kv_heads);
+    const int64_t chunk = in_batch / (unsigned)P.kv_heads;
     if (warp < 2) {                                                      // the factors of keys and of values
         uint32_t top = 0u;
         const uint32_t* from = P.top + ((int64_t)warp * heads_of(P) + (int64_t)b * P.kv_heads + h) * P.tops;
@@ -381,11 +382,11 @@ int launch4(const Params4& P, int rows, unsigned grid, int64_t most_rows, cudaSt
 }
 
 template <int D>
-int launch_unpack(const Prepare& A, cudaStream_t s) {
-    const Unpack& U = A.u;
-    const int64_t keys = (int64_t)U.new_pages * kUnpackPage;
-    if (launch_overlapped(attn4_prepare_kernel<D>, dim3((unsigned)(A.query_ctas + U.tops * U.kv_heads * U.batch)), dim3(kUnpackThreads), 0, s, A) != cudaSuccess ||
-        launch_overlapped(attn4_unpack_kernel<D>, dim3((unsigned)(keys / kUnpackKeys * U.kv_heads), (unsigned)U.batch), dim3(kUnpackThreads), 0, s, U) != cudaSuccess) {
+int launch_unpack(const Unpack& U, Queries Q, cudaStream_t s) {
+    const int64_t rows_of_cta = (int64_t)kQueryPieces * kUnpackThreads / (D / 8), query_ctas = (Q.T * Q.q_heads + rows_of_cta - 1) / rows_of_cta;
+    Q.first_cta = (int64_t)U.new_pages * (kUnpackPage / kUnpackKeys) * U.kv_heads * U.batch;
+    if (launch_overlapped(attn4_top_kernel<D>, dim3((unsigned)(U.tops * U.kv_heads * U.batch)), dim3(kUnpackThreads), 0, s, U) != cudaSuccess ||
+        launch_overlapped(attn4_unpack_kernel<D>, dim3((unsigned)(Q.first_cta + query_ctas)), dim3(kUnpackThreads), 0, s, U, Q) != cudaSuccess) {
         cudaGetLastError();
         return MATQ_ERR_CUDA;
     }
@@ -426,7 +427,10 @@ extern "C" int matq_attn_paged4(const matq_paged_kv4* cache, int64_t T, const vo
     const Plan4 p = plan4(T, cache->batch, q_heads, cache->kv_heads, D, max_q, max_kv, window, sm_count());
     const double ctas = (double)p.splits * cache->kv_heads * cache->batch * p.tiles_per_seq;
     const int64_t blocks = p.new_pages * (kUnpackPage / kUnpackKeys);
-    if (ctas >= 2147483648.0 || (p.splits > 1 && T * q_heads >= (1ll << 31)) || (double)blocks * cache->kv_heads >= 2147483648.0 || p.round > 65535 || (double)p.tops * cache->kv_heads * p.round + (double)T * q_heads >= 2147483648.0 || (p.round && T * q_heads >= (1ll << 31))) return MATQ_ERR_SHAPE;
+    const double rows = (double)T * q_heads;
+    if (ctas >= 2147483648.0 || (p.splits > 1 && rows >= 2147483648.0) ||
+        (p.round && ((double)blocks * cache->kv_heads * p.round + rows >= 2147483648.0 || (double)p.tops * cache->kv_heads * p.round >= 2147483648.0)))
+        return MATQ_ERR_SHAPE;
     if (p.total() > workspace_bytes || (p.total() > 0 && !workspace)) return MATQ_ERR_WORKSPACE;
     const float cap = softcap < 0x1p100f ? softcap : 0.f;               // as in matq_attn_paged
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -453,32 +457,31 @@ extern "C" int matq_attn_paged4(const matq_paged_kv4* cache, int64_t T, const vo
     void* dense = at + p.few_bytes;
     unsigned char* next = at + p.few_bytes + p.dense_bytes;
     const auto take = [&](size_t bytes) { unsigned char* here = next; next += bytes; return here; };
-    Prepare A;
-    Unpack& U = A.u;
+    Unpack U;
+    Queries Q;
     U.tiles = P.tiles; U.table_stride = P.table_stride; U.table_width = P.table_width; U.n_pages = P.n_pages; U.window = window; U.above_rows = p.above_rows;
     U.kv_heads = P.kv_heads; U.group = group; U.page_size = ps; U.page_shift = P.page_shift; U.new_width = p.new_width; U.new_pages = (int)p.new_pages; U.tops = p.tops;
     U.new_table = reinterpret_cast<int32_t*>(take(p.table_bytes));
-    A.to = reinterpret_cast<__half*>(take(p.query_bytes));
-    A.scale = reinterpret_cast<float*>(take(p.scale_bytes));
+    Q.to = reinterpret_cast<__half*>(take(p.query_bytes));
+    Q.scale = reinterpret_cast<float*>(take(p.scale_bytes));
     U.top = reinterpret_cast<uint32_t*>(take(p.top_bytes));
     U.k = reinterpret_cast<__half*>(take(p.cache_bytes));
     U.v = reinterpret_cast<__half*>(take(p.cache_bytes));
     U.dev_status = dev_status;
-    A.q = P.q; A.ldq = ldq; A.T = T; A.q_heads = q_heads;
-    const int64_t rows_of_cta = (int64_t)kQueryPieces * kUnpackThreads / (D / 8);
+    Q.q = P.q; Q.ldq = ldq; Q.T = T; Q.q_heads = q_heads;
     for (int64_t b0 = 0; b0 < cache->batch && st == MATQ_OK; b0 += p.round) {
         const int n = (int)(cache->batch - b0 < p.round ? cache->batch - b0 : p.round);
         const int64_t heads = (int64_t)n * cache->kv_heads;
         U.batch = n; U.table = P.table + b0 * P.table_stride; U.cu_q = P.cu_q + b0; U.kv_len = P.kv_len + b0;
         U.scale = reinterpret_cast<float*>(U.top) + 2 * heads * p.tops;
-        A.query_ctas = b0 == 0 ? (T * q_heads + rows_of_cta - 1) / rows_of_cta : 0;
-        st = D == 64 ? launch_unpack<64>(A, s) : D == 128 ? launch_unpack<128>(A, s) : launch_unpack<256>(A, s);
+        st = D == 64 ? launch_unpack<64>(U, Q, s) : D == 128 ? launch_unpack<128>(U, Q, s) : launch_unpack<256>(U, Q, s);
         if (st != MATQ_OK) break;
+        Q.T = 0;                                                        // once for all rounds
         matq_paged_kv c;
         c.k = U.k; c.v = U.v; c.n_pages = (int64_t)n * p.new_pages; c.page_size = kUnpackPage; c.kv_heads = P.kv_heads; c.head_dim = D; c.batch = n;
         c.page_table = U.new_table; c.table_stride = c.table_width = p.new_width; c.cu_q = U.cu_q; c.kv_len = U.kv_len;
-        const Half half = {A.scale, U.scale, U.scale + heads, p.above_rows};
-        st = paged(&c, T, A.to, q_heads, w, scale, softcap, window, max_q, max_kv, out, ldo, dense, p.dense_bytes, &half, dev_status, stream);
+        const Half half = {Q.scale, U.scale, U.scale + heads, p.above_rows};
+        st = paged(&c, T, Q.to, q_heads, w, scale, softcap, window, max_q, max_kv, out, ldo, dense, p.dense_bytes, &half, dev_status, stream);
     }
     return st;
 }

@@ -353,6 +353,12 @@ inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64
     return p;
 }
 
+inline Plan4 recent_plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64_t max_q, int64_t max_kv, int64_t window) {
+    static thread_local Recent<Plan4, 9> recent;
+    const int sms = sm_count();
+    return recent.of({T, batch, q_heads, kv_heads, D, max_q, max_kv, window, sms}, [&] { return plan4(T, batch, q_heads, kv_heads, D, max_q, max_kv, window, sms); });
+}
+
 template <int D, int R>
 int launch_decode4(const Params4& P, unsigned grid, cudaStream_t s) {
     using C = Dec4Cfg<D, R>;
@@ -404,7 +410,7 @@ inline bool sizes_ok(int64_t T, int batch, int q_heads, int kv_heads, int D, int
 extern "C" size_t matq_attn_paged4_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv, int64_t window) {
     using namespace matq::attn;
     if (!sizes_ok(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window)) return 0;
-    return plan4(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window, matq::sm_count()).total();
+    return recent_plan4(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window).total();
 }
 
 extern "C" int matq_attn_paged4(const matq_paged_kv4* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap, int64_t window,
@@ -424,7 +430,7 @@ extern "C" int matq_attn_paged4(const matq_paged_kv4* cache, int64_t T, const vo
     if (!q || !out || !cache->tiles || !cache->page_table || !cache->cu_q || !cache->kv_len || cache->n_pages == 0) return MATQ_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out) || !aligned16(cache->tiles) || !aligned16(workspace)) return MATQ_ERR_ALIGNMENT;
     const int group = q_heads / cache->kv_heads;
-    const Plan4 p = plan4(T, cache->batch, q_heads, cache->kv_heads, D, max_q, max_kv, window, sm_count());
+    const Plan4 p = recent_plan4(T, cache->batch, q_heads, cache->kv_heads, D, max_q, max_kv, window);
     const double ctas = (double)p.splits * cache->kv_heads * cache->batch * p.tiles_per_seq;
     const int64_t blocks = p.new_pages * (kUnpackPage / kUnpackKeys);
     const double rows = (double)T * q_heads;

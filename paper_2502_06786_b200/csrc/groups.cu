@@ -525,7 +525,9 @@ extern "C" int matq_gemv_groups(const uint8_t* packed, int64_t N, int64_t K, int
     if (!packed || !params || !x || !y) return MATQ_ERR_INVALID_ARG;
     if (!aligned16(packed) || !aligned16(params) || !aligned16(x)) return MATQ_ERR_ALIGNMENT;
     const int S = kBlock / group;
-    const GemvPlan p = plan_gemv(M, N, K, S, sm_count());
+    static thread_local Recent<GemvPlan, 5> recent;
+    const int sms = sm_count();
+    const GemvPlan& p = recent.of({M, N, K, S, sms}, [&] { return plan_gemv(M, N, K, S, sms); });
     if (p.cost < 0 || p.token_blocks > 65535) return MATQ_ERR_SHAPE;
     GemvParams P;
     P.packed = packed; P.params = static_cast<const uint32_t*>(params); P.x = static_cast<const __nv_bfloat16*>(x); P.y = y;

@@ -76,7 +76,7 @@ cudaError_t launch_quantize(const void* W, int64_t N, int64_t K, int64_t ldw, vo
 // that part, block by block of 128.  Each warp brings its own blocks into its own ring by cp.async, across the ends of steps, so that the ring never drains.
 // The CTAs of a cluster share K and add their sums through distributed shared memory.  All sums are taken in a fixed order.
 //
-// Bound: one token, the chain of a launch (start, tokens' trip to memory, staging, the last blocks' trip, sums): 9216 x 2304 5.1 us, 14336 x 4096 10.5, 65536 x 2304 (a step
+// Bound: one token, the chain of a launch (start, tokens' trip to memory, staging, the last blocks' trip, sums): 9216 x 2304 5.2 us, 14336 x 4096 10.5, 65536 x 2304 (a step
 // of every CTA follows another) 19.7 us or 4.3 TB/s.  16 tokens: latencies of 16 warps (1.9 instructions a cycle) and the cluster's sums: 3584 x 14336 18.0 us.
 constexpr int kBlock = 128;
 // Warps of a CTA: eight, and two CTAs on an SM, as long as a CTA has one block of columns; sixteen beside tokens that take more shared memory.
@@ -447,7 +447,8 @@ inline bool plan_shape(GemvPlan& p, int64_t M, int64_t N, int64_t K, int S, int 
     // (32 rows of 64 bytes at a time and nobody at the rows' next bytes: 65536 x 2304 in 26 us, with two warps to a row 20.5)
     double block = alone > shared ? alone : shared;
     if (hbm > block) block = hbm;
-    const double stage = 800 + 40.0 * p.tokens * p.slice / warps + (at_work > sms ? 700 * (at_work - sms) / sms : 0), sums = 500 + 60.0 * rows * p.tokens / (32 * warps) + 50 * p.sk * (S / passes) + (p.cl > 1 ? 500 + 200 * p.cl : 0);
+    const int64_t trips = (p.tokens * p.slice + 8 * warps - 1) / (8 * warps);          // a thread has four of a block's sixteen pieces on their way at a time
+    const double stage = 200 + 600.0 * trips + (at_work > sms ? 700 * (at_work - sms) / sms : 0), sums = 500 + 60.0 * rows * p.tokens / (32 * warps) + 50 * p.sk * (S / passes) + (p.cl > 1 ? 500 + 200 * p.cl : 0);
     p.cost = 2000 + stage + rounds * ((double)((p.slice + p.sk - 1) / p.sk) * block + sums);
     return true;
 }

@@ -556,7 +556,7 @@ def gemv_groups(packed, params, x, y=None, out_dtype=torch.float32, flags=0, wor
     the second."""
     if y is None:
         y = torch.empty((x.shape[0], packed.shape[0]), dtype=out_dtype, device=x.device)
-    if x.shape[0] > 16 and not flags & ~GEMV_PDL and params.shape[1] and gemm_groups_pays(x.shape[0], packed.shape[0], x.shape[1], x.shape[1] // params.shape[1]):
+    if x.shape[0] > 16 and not flags & ~GEMV_PDL and params.dim() == 3 and params.shape[1] and gemm_groups_pays(x.shape[0], packed.shape[0], x.shape[1], x.shape[1] // params.shape[1]):
         return gemm_groups(packed, params, x, y=y, workspace=workspace, dev_status=dev_status)
     st = _serving.gemv_groups(packed, params, x, y, flags)
     if st:

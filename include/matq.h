@@ -511,6 +511,10 @@ int matq_quantize_groups(const void *W, int64_t N, int64_t K, int64_t ldw, int g
  */
 int matq_gemv_groups(const uint8_t *packed, int64_t N, int64_t K, int group, const void *params, const void *x, int64_t M, int64_t ldx,
                      int out_type, void *Y, int64_t ldy, unsigned flags, void *stream);
+/* How (11) shares out these sizes on the current device (host only, launches nothing): the tokens that share a reading of the weights, the CTAs that share K, and the
+   steps over the rows that a CTA takes at most.  M, N >= 1; MATQ_ERR_INVALID_ARG, MATQ_ERR_UNSUPPORTED or MATQ_ERR_SHAPE for sizes that (11) would refuse.  Any of the
+   pointers may be NULL. */
+int matq_gemv_groups_plan(int64_t M, int64_t N, int64_t K, int group, int *tokens, int *parts, int *steps);
 
 /*
  * (11b) The same for many tokens, on the fifth-generation tensor cores.  Weights less their group's middle and tokens enter the products as fp16, exactly (with a power

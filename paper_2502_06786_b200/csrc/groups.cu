@@ -376,6 +376,9 @@ __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_ke
                 }
         __syncthreads();
         float* part = red + part_floats;
+        // The CTAs of the cluster meet a step late, so that none waits for another while it has blocks to multiply.  That all of them have come this far says that they
+        // have gathered the sums of the step before the last, whose place these take.
+        if (cl > 1 && before >= 0) cluster_wait();
         for (int i = tid; i < rows * tokens; i += kThreads) {
             const int v = i >> rows_shift, r = i & (rows - 1);
             float sum = 0.f;
@@ -386,11 +389,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT), ctas_of(NT)) gemv_groups_ke
             else store(P, m0 + v, (int64_t)step * rows + r, sum);
         }
         if (cl > 1) {
-            // The CTAs of the cluster meet a step late, so that none waits for another while it has blocks to multiply.
-            if (before >= 0) {
-                cluster_wait();
-                gather(before, s_red + (turn ^ 1) * buffer_floats + part_floats);
-            }
+            if (before >= 0) gather(before, s_red + (turn ^ 1) * buffer_floats + part_floats);
             cluster_arrive();
             before = step;
         }
@@ -467,6 +466,13 @@ inline GemvPlan plan_gemv(int64_t M, int64_t N, int64_t K, int S, int sms) {
     return best;
 }
 
+inline bool has_grid(const GemvPlan& p) { return p.cost >= 0 && p.token_blocks <= 65535; }
+inline int size_error(int64_t N, int64_t K, int group) {
+    if (N < 0 || K < 0) return MATQ_ERR_INVALID_ARG;
+    if (group != 32 && group != 64 && group != 128) return MATQ_ERR_UNSUPPORTED;
+    return K == 0 || K % group != 0 || K > 65536 || N >= (1ll << 31) ? MATQ_ERR_SHAPE : MATQ_OK;
+}
+
 template <int NT, int S, int C, int MT>
 int launch_gemv(const GemvPlan& p, const GemvParams& P, cudaStream_t s) {
     static std::atomic<unsigned long long> smem_ok{0};
@@ -515,13 +521,28 @@ extern "C" int matq_quantize_groups(const void* W, int64_t N, int64_t K, int64_t
     return launch_status();
 }
 
+extern "C" int matq_gemv_groups_plan(int64_t M, int64_t N, int64_t K, int group, int* tokens, int* parts, int* steps) {
+    using namespace matq;
+    using namespace matq::grp;
+    const int st = size_error(N, K, group);
+    if (st != MATQ_OK) return st;
+    if (M < 1 || N < 1) return MATQ_ERR_INVALID_ARG;
+    const GemvPlan p = plan_gemv(M, N, K, kBlock / group, sm_count());
+    if (!has_grid(p)) return MATQ_ERR_SHAPE;
+    if (tokens) *tokens = (int)p.tokens;
+    if (parts) *parts = p.cl;
+    if (steps) *steps = (int)((p.steps + p.row_ctas - 1) / p.row_ctas);
+    return MATQ_OK;
+}
+
 extern "C" int matq_gemv_groups(const uint8_t* packed, int64_t N, int64_t K, int group, const void* params, const void* x, int64_t M, int64_t ldx,
                                 int out_type, void* y, int64_t ldy, unsigned flags, void* stream) {
     using namespace matq;
     using namespace matq::grp;
-    if (N < 0 || K < 0 || M < 0 || (out_type != MATQ_OUT_F32 && out_type != MATQ_OUT_BF16) || (flags & ~(unsigned)MATQ_GEMV_PDL)) return MATQ_ERR_INVALID_ARG;
-    if (group != 32 && group != 64 && group != 128) return MATQ_ERR_UNSUPPORTED;
-    if (K == 0 || K % group != 0 || K > 65536 || ldx < K || ldx % 8 != 0 || ldy < N || N >= (1ll << 31)) return MATQ_ERR_SHAPE;
+    if (M < 0 || (out_type != MATQ_OUT_F32 && out_type != MATQ_OUT_BF16) || (flags & ~(unsigned)MATQ_GEMV_PDL)) return MATQ_ERR_INVALID_ARG;
+    const int st = size_error(N, K, group);
+    if (st != MATQ_OK) return st;
+    if (ldx < K || ldx % 8 != 0 || ldy < N) return MATQ_ERR_SHAPE;
     if (M == 0 || N == 0) return MATQ_OK;
     if (!packed || !params || !x || !y) return MATQ_ERR_INVALID_ARG;
     if (!aligned16(packed) || !aligned16(params) || !aligned16(x)) return MATQ_ERR_ALIGNMENT;
@@ -529,7 +550,7 @@ extern "C" int matq_gemv_groups(const uint8_t* packed, int64_t N, int64_t K, int
     static thread_local Recent<GemvPlan, 5> recent;
     const int sms = sm_count();
     const GemvPlan& p = recent.of({M, N, K, S, sms}, [&] { return plan_gemv(M, N, K, S, sms); });
-    if (p.cost < 0 || p.token_blocks > 65535) return MATQ_ERR_SHAPE;
+    if (!has_grid(p)) return MATQ_ERR_SHAPE;
     GemvParams P;
     P.packed = packed; P.params = static_cast<const uint32_t*>(params); P.x = static_cast<const __nv_bfloat16*>(x); P.y = y;
     P.N = N; P.K = K; P.M = M; P.ldx = ldx; P.ldy = ldy; P.groups = K / group;

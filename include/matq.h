@@ -529,6 +529,9 @@ int matq_gemv_groups_plan(int64_t M, int64_t N, int64_t K, int group, int *token
 size_t matq_gemm_groups_workspace_bytes(int64_t M, int64_t N, int64_t K, int group);
 /* 1 for sizes at which (11b) takes less time than (11), as far as measured; host only. */
 int matq_gemm_groups_pays(int64_t M, int64_t N, int64_t K, int group);
+/* How (11b) shares out these sizes on the current device (host only, launches nothing): whether pairs of SMs share a tile, the tokens of a tile, and the CTAs that share K.
+   M, N >= 1; MATQ_ERR_INVALID_ARG, MATQ_ERR_UNSUPPORTED or MATQ_ERR_SHAPE for sizes that (11b) would refuse.  Any of the pointers may be NULL. */
+int matq_gemm_groups_plan(int64_t M, int64_t N, int64_t K, int group, int out_type, int *pairs, int *tokens, int *parts);
 int matq_gemm_groups(const uint8_t *packed, int64_t N, int64_t K, int group, const void *params, const void *x, int64_t M, int64_t ldx,
                      int out_type, void *Y, int64_t ldy, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
 

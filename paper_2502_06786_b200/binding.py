@@ -32,7 +32,7 @@ EXPORTS = ["matq_status_string", "matq_version", "matq_packed_row_bytes", "matq_
            "matq_gemm_multi_test_stall", "matq_slice_pack_test_stall",
            "matq_gemm_multi_static_max_bytes", "matq_gemm_multi_static",
            "matq_quantize_tokens", "matq_gemm_a8", "matq_gemm_a8_plan", "matq_kv_append", "matq_attn_paged_workspace_bytes", "matq_attn_paged",
-           "matq_quantize_groups", "matq_gemv_groups", "matq_gemv_groups_plan", "matq_gemm_groups_workspace_bytes", "matq_gemm_groups_pays", "matq_gemm_groups", "matq_kv4_tile_bytes", "matq_kv4_append", "matq_attn_paged4_workspace_bytes", "matq_attn_paged4",
+           "matq_quantize_groups", "matq_gemv_groups", "matq_gemv_groups_plan", "matq_gemm_groups_workspace_bytes", "matq_gemm_groups_pays", "matq_gemm_groups_plan", "matq_gemm_groups", "matq_kv4_tile_bytes", "matq_kv4_append", "matq_attn_paged4_workspace_bytes", "matq_attn_paged4",
            "matq_serving_test_stall"]
 
 
@@ -132,6 +132,8 @@ def _load():
     lib.matq_gemm_groups_workspace_bytes.argtypes = [i64, i64, i64, i32]
     lib.matq_gemm_groups_pays.restype = i32
     lib.matq_gemm_groups_pays.argtypes = [i64, i64, i64, i32]
+    lib.matq_gemm_groups_plan.restype = i32
+    lib.matq_gemm_groups_plan.argtypes = [i64, i64, i64, i32, i32, C.POINTER(C.c_int), C.POINTER(C.c_int), C.POINTER(C.c_int)]
     lib.matq_gemm_groups.restype = i32
     lib.matq_gemm_groups.argtypes = [vp, i64, i64, i32, vp, vp, i64, i64, i32, vp, i64, vp, sz, vp, vp]
     lib.matq_kv4_tile_bytes.restype = i64
@@ -568,13 +570,20 @@ def gemv_groups(packed, params, x, y=None, out_dtype=torch.float32, flags=0, wor
 
 def gemv_groups_plan(M, N, K, group) -> tuple[int, int, int]:
     """matq_gemv_groups_plan: (tokens that share a reading of the weights, CTAs that share K, most row steps of a CTA) that matq_gemv_groups takes for these sizes."""
-    out = [C.c_int(0) for _ in range(3)]
+    out = [C.c_int() for _ in range(3)]
     _check(_lib.matq_gemv_groups_plan(M, N, K, group, *(C.byref(o) for o in out)), "matq_gemv_groups_plan")
     return tuple(o.value for o in out)
 
 
 def gemm_groups_pays(M, N, K, group) -> bool:
     return bool(_lib.matq_gemm_groups_pays(M, N, K, group))
+
+
+def gemm_groups_plan(M, N, K, group, out_dtype=torch.float32) -> tuple[bool, int, int]:
+    """matq_gemm_groups_plan: (whether pairs of SMs share a tile, tokens of a tile, CTAs that share K) that gemm_groups takes for these sizes."""
+    out = [C.c_int() for _ in range(3)]
+    _check(_lib.matq_gemm_groups_plan(M, N, K, group, OUT_BF16 if out_dtype == _BF16 else OUT_F32, *(C.byref(o) for o in out)), "matq_gemm_groups_plan")
+    return bool(out[0].value), out[1].value, out[2].value
 
 
 def gemm_groups_workspace_bytes(M, N, K, group) -> int:

@@ -541,6 +541,27 @@ inline bool sizes_ok(int64_t M, int64_t N, int64_t K, int group) {
            ((M + 15) / 16) * ((N + kBM - 1) / kBM) < (1ll << 30) && M + N / kPrepRows + 4 < (1ll << 31);
 }
 
+// Tokens of a tile, shared out evenly; as many CTAs to a tile as leave no tile waiting (clusters of eight find about 128 of 148 SMs, of four about 136, and each
+// CTA takes two pairs of blocks or more), or, for bf16 outputs, pairs where they take less time.  Cycles, measured: a block of a CTA 550 and 3.7 a token, of a pair 1050;
+// a tile's end, which a pair does not overlap, 20 a token.  The products of a CTA take tokens in steps of 16, those of a pair in steps of 32.
+struct Shape {
+    bool pair;
+    int nt, splits;              // tokens of a tile; CTAs that share K
+    int64_t tiles;
+};
+inline Shape choose(int64_t M, int64_t N, const Plan& p, int out_type, int sms) {
+    const auto tokens_of = [&](int most, int step) { const int64_t t = (M + most - 1) / most; return (int)(((M + t - 1) / t + step - 1) / step * step); };
+    const auto tiles_of = [&](int nt, int rows) { return ((M + nt - 1) / nt) * ((N + rows - 1) / rows); };
+    const int blocks = p.main + p.extra, nt_one = tokens_of(kMaxNT, 16), nt_pair = tokens_of(kPairNT, 32);
+    const int64_t tiles = tiles_of(nt_one, kBM), tiles_pair = tiles_of(nt_pair, 2 * kBM);
+    const double one = (double)((tiles + sms - 1) / sms) * blocks * (550 + 3.7 * nt_one), two = (double)((tiles_pair + sms / 2 - 1) / (sms / 2)) * (blocks * 1050.0 + 20.0 * nt_pair);
+    if (out_type == MATQ_OUT_BF16 && tiles > sms && two < one) return {true, nt_pair, 1, tiles_pair};
+    int splits = 1;
+    for (int n = 2; n <= 8; n *= 2)
+        if (tiles * n <= (n == 8 ? sms * 7 / 8 : n == 4 ? sms * 9 / 10 : sms) && blocks >= 4 * n) splits = n;
+    return {false, nt_one, splits, tiles};
+}
+
 template <int S, bool PAIR>
 int launch(const CUtensorMap& tw, const CUtensorMap& tx, const Params& P, unsigned grid, cudaStream_t s) {
     static std::atomic<unsigned long long> smem_ok{0};
@@ -577,6 +598,19 @@ extern "C" size_t matq_gemm_groups_workspace_bytes(int64_t M, int64_t N, int64_t
     return sizes_ok(M, N, K, group) ? plan(M, N, K, group).total() : 0;
 }
 
+extern "C" int matq_gemm_groups_plan(int64_t M, int64_t N, int64_t K, int group, int out_type, int* pairs, int* tokens, int* parts) {
+    using namespace matq;
+    using namespace matq::grpm;
+    if (M < 1 || N < 1 || K < 0 || (out_type != MATQ_OUT_F32 && out_type != MATQ_OUT_BF16)) return MATQ_ERR_INVALID_ARG;
+    if (group != 32 && group != 64 && group != 128) return MATQ_ERR_UNSUPPORTED;
+    if (!sizes_ok(M, N, K, group)) return MATQ_ERR_SHAPE;
+    const Shape s = choose(M, N, plan(M, N, K, group), out_type, sm_count());
+    if (pairs) *pairs = s.pair ? 1 : 0;
+    if (tokens) *tokens = s.nt;
+    if (parts) *parts = s.splits;
+    return MATQ_OK;
+}
+
 extern "C" int matq_gemm_groups(const uint8_t* packed, int64_t N, int64_t K, int group, const void* params, const void* x, int64_t M, int64_t ldx, int out_type, void* y,
                                 int64_t ldy, void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream) {
     using namespace matq;
@@ -599,20 +633,10 @@ extern "C" int matq_gemm_groups(const uint8_t* packed, int64_t N, int64_t K, int
     A.row_exp = A.token_exp + M;
     A.scaled = reinterpret_cast<uint32_t*>(at + p.x_bytes + p.exp_bytes);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    // Tokens of a tile, shared out evenly; as many CTAs to a tile as leave no tile waiting (clusters of eight find about 128 of 148 SMs, of four about 136, and each
-    // CTA takes two pairs of blocks or more), or, for bf16 outputs, pairs where they take less time.  Cycles, measured: a block of a CTA 550 and 3.7 a token, of a pair 1050;
-    // a tile's end, which a pair does not overlap, 20 a token.
     const int sms = sm_count();
-    const auto tokens_of = [&](int most) { const int64_t t = (M + most - 1) / most; return (int)(((M + t - 1) / t + 15) / 16 * 16); };
-    const auto tiles_of = [&](int nt, int rows) { return ((M + nt - 1) / nt) * ((N + rows - 1) / rows); };
-    const int blocks = p.main + p.extra, nt_one = tokens_of(kMaxNT), nt_pair = tokens_of(kPairNT);
-    const int64_t tiles = tiles_of(nt_one, kBM), tiles_pair = tiles_of(nt_pair, 2 * kBM);
-    const double one = (double)((tiles + sms - 1) / sms) * blocks * (550 + 3.7 * nt_one), two = (double)((tiles_pair + sms / 2 - 1) / (sms / 2)) * (blocks * 1050.0 + 20.0 * nt_pair);
-    const bool pair = out_type == MATQ_OUT_BF16 && tiles > sms && two < one;
-    const int nt = pair ? nt_pair : nt_one;
-    int splits = 1;
-    for (int n = 2; n <= 8 && !pair; n *= 2)
-        if (tiles * n <= (n == 8 ? sms * 7 / 8 : n == 4 ? sms * 9 / 10 : sms) && blocks >= 4 * n) splits = n;
+    const Shape shape = choose(M, N, p, out_type, sms);
+    const bool pair = shape.pair;
+    const int nt = shape.nt, splits = shape.splits;
     const cuuint64_t wd[2] = {(cuuint64_t)(K / 2), (cuuint64_t)N}, ws[1] = {(cuuint64_t)(K / 2)};
     const cuuint64_t xd[3] = {64, (cuuint64_t)M, (cuuint64_t)(p.width / 64)}, xs[2] = {(cuuint64_t)p.width * 2, 128};
     const cuuint32_t wb[2] = {128, kBM}, xb[3] = {64, (cuuint32_t)(pair ? nt / 2 : nt), 2};
@@ -627,7 +651,7 @@ extern "C" int matq_gemm_groups(const uint8_t* packed, int64_t N, int64_t K, int
     P.groups = (int)p.groups; P.main = p.main; P.extra = p.extra; P.nt = nt;
     P.out_bf16 = out_type == MATQ_OUT_BF16; P.hold = tc::test_stall() ? 1 : 0; P.wait_cycles = P.hold ? tc::kStallWaitCycles : tc::kWaitCycles; P.dev_status = dev_status;
     P.splits = splits;
-    const unsigned grid = (unsigned)(pair ? 2 * (tiles_pair < sms / 2 ? tiles_pair : sms / 2) : tiles * splits < sms ? tiles * splits : sms);
+    const unsigned grid = (unsigned)(pair ? 2 * (shape.tiles < sms / 2 ? shape.tiles : sms / 2) : shape.tiles * splits < sms ? shape.tiles * splits : sms);
     if (pair) return group == 128 ? launch<1, true>(tw, tx, P, grid, s) : group == 64 ? launch<2, true>(tw, tx, P, grid, s) : launch<4, true>(tw, tx, P, grid, s);
     return group == 128 ? launch<1, false>(tw, tx, P, grid, s) : group == 64 ? launch<2, false>(tw, tx, P, grid, s) : launch<4, false>(tw, tx, P, grid, s);
 }

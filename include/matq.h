@@ -579,6 +579,11 @@ int matq_kv4_append(const matq_paged_kv4 *cache, int64_t T, const void *q, int q
  */
 size_t matq_attn_paged4_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim,
                                         int64_t max_q, int64_t max_kv, int64_t window);
+/* How (13) serves these sizes on the current device (host only, launches nothing): the rows of a tile of the kernel that reads the cache as it is, and its parts of the key
+   range (0: it is not launched); the sequences that are unpacked at a time, the tiles of 128 rows that a CTA of their kernel takes, and its parts of the key range (0: none are
+   unpacked).  MATQ_ERR_INVALID_ARG for sizes that (13) would refuse or has nothing to do for.  Any of the pointers may be NULL. */
+int matq_attn_paged4_plan(int64_t T, int batch, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv, int64_t window, int *rows, int *row_parts,
+                          int *unpacked, int *tiles, int *parts);
 int matq_attn_paged4(const matq_paged_kv4 *cache, int64_t T, const void *q, int q_heads, int64_t ldq,
                      float scale, float softcap, int64_t window, int64_t max_q, int64_t max_kv,
                      void *out, int64_t ldo, void *workspace, size_t workspace_bytes,

@@ -32,7 +32,7 @@ EXPORTS = ["matq_status_string", "matq_version", "matq_packed_row_bytes", "matq_
            "matq_gemm_multi_test_stall", "matq_slice_pack_test_stall",
            "matq_gemm_multi_static_max_bytes", "matq_gemm_multi_static",
            "matq_quantize_tokens", "matq_gemm_a8", "matq_gemm_a8_plan", "matq_kv_append", "matq_attn_paged_workspace_bytes", "matq_attn_paged",
-           "matq_quantize_groups", "matq_gemv_groups", "matq_gemv_groups_plan", "matq_gemm_groups_workspace_bytes", "matq_gemm_groups_pays", "matq_gemm_groups_plan", "matq_gemm_groups", "matq_kv4_tile_bytes", "matq_kv4_append", "matq_attn_paged4_workspace_bytes", "matq_attn_paged4",
+           "matq_quantize_groups", "matq_gemv_groups", "matq_gemv_groups_plan", "matq_gemm_groups_workspace_bytes", "matq_gemm_groups_pays", "matq_gemm_groups_plan", "matq_gemm_groups", "matq_kv4_tile_bytes", "matq_kv4_append", "matq_attn_paged4_workspace_bytes", "matq_attn_paged4_plan", "matq_attn_paged4",
            "matq_serving_test_stall"]
 
 
@@ -142,6 +142,8 @@ def _load():
     lib.matq_kv4_append.argtypes = [C.POINTER(PagedKv4), i64, vp, i32, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp, i64, vp, vp]
     lib.matq_attn_paged4_workspace_bytes.restype = sz
     lib.matq_attn_paged4_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i64, i64]
+    lib.matq_attn_paged4_plan.restype = i32
+    lib.matq_attn_paged4_plan.argtypes = [i64, i32, i32, i32, i32, i64, i64, i64] + [C.POINTER(C.c_int)] * 5
     lib.matq_attn_paged4.restype = i32
     lib.matq_attn_paged4.argtypes = [C.POINTER(PagedKv4), i64, vp, i32, i64, f32, f32, i64, i64, i64, vp, i64, vp, sz, vp, vp]
     lib.matq_serving_test_stall.restype = i32
@@ -622,6 +624,14 @@ def kv4_append(cache, page_table, cu_q, kv_len, k, v, cos_sin=None, q=None, q_ou
 
 def attn_paged4_workspace_bytes(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window=0) -> int:
     return int(_lib.matq_attn_paged4_workspace_bytes(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window))
+
+
+def attn_paged4_plan(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window=0) -> tuple[int, int, int, int, int]:
+    """matq_attn_paged4_plan: (rows of a tile, parts of the key range) of the kernel that reads the cache as it is, and (sequences unpacked at a time, tiles of a CTA,
+    parts of the key range) of the one behind the unpacking; 0 for what is not launched."""
+    out = [C.c_int() for _ in range(5)]
+    _check(_lib.matq_attn_paged4_plan(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window, *(C.byref(o) for o in out)), "matq_attn_paged4_plan")
+    return tuple(o.value for o in out)
 
 
 def attn_paged4(q, cache, page_table, cu_q, kv_len, max_q, max_kv, scale=None, softcap=0.0, window=0, out=None, workspace=None, dev_status=None):

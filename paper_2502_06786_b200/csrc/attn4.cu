@@ -413,6 +413,21 @@ extern "C" size_t matq_attn_paged4_workspace_bytes(int64_t T, int batch, int q_h
     return recent_plan4(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window).total();
 }
 
+extern "C" int matq_attn_paged4_plan(int64_t T, int batch, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv, int64_t window, int* rows, int* row_parts,
+                                     int* unpacked, int* tiles, int* parts) {
+    using namespace matq::attn;
+    if (!sizes_ok(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window)) return MATQ_ERR_INVALID_ARG;
+    const Plan4 p = recent_plan4(T, batch, q_heads, kv_heads, head_dim, max_q, max_kv, window);
+    int t = 0, n = 0;
+    if (p.round) paged_cost(T, (int)p.round, q_heads, kv_heads, head_dim, max_q, max_kv, window, &t, &n);
+    if (rows) *rows = p.few ? p.rows : 0;
+    if (row_parts) *row_parts = p.few ? (int)p.splits : 0;
+    if (unpacked) *unpacked = (int)p.round;
+    if (tiles) *tiles = t;
+    if (parts) *parts = n;
+    return MATQ_OK;
+}
+
 extern "C" int matq_attn_paged4(const matq_paged_kv4* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap, int64_t window,
                                 int64_t max_q, int64_t max_kv, void* out, int64_t ldo, void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream) {
     using namespace matq;

@@ -341,6 +341,8 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const float tanh1 = kShort1 * sc.cap2, tanh2 = kShort2 * sc.cap2, tanh3 = kShort3 * sc.cap2, t_max = P.softcap <= kShortCap ? kTanhMax : -1.f;   // with the cap
             const float unit = CAP ? 1.f : sc.mul;                      // the reference is kept as a score; with the cap, as an exponent
             float m = -INFINITY, l = 0.f;
+            // The reference as an exponent.  (HALF: the factors of a row of zeros and of keys of zero make a unit of zero, and zero times -inf would be NaN.)
+            const auto exponent = [&](float reference) { return reference == -INFINITY ? reference : reference * unit; };
             bool ok = true;
             int masked_no = 0;
             if (tid == 0) s_any_bad = 0;
@@ -493,7 +495,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         lifted = true;
                     }
                     // O holds the steps before this one.  Their last product is over: with one tile that was waited for, with two the scores' arrival says so.
-                    const float f = raise ? ex2(m * unit - next + (shift(m * unit) - shift(next))) : 1.f;
+                    const float f = raise ? ex2(exponent(m) - next + (shift(exponent(m)) - shift(next))) : 1.f;
                     if (raise) m = ref;
                     l *= f;
                     if (ok && i > 0) {
@@ -581,7 +583,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
             const float inv = any ? 1.f / l : 0.f;
             if (!ok) *(volatile int*)&s_timeout = 1;
-            if (ok && live && P.splits > 1 && o_col == 0) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(m * unit + shift(m * unit), l);
+            if (ok && live && P.splits > 1 && o_col == 0) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(exponent(m) + shift(exponent(m)), l);
             if (ok && !(P.splits > 1 && n_it == 0)) {
 #pragma unroll 1
                 for (int c = o_col; c < o_col + kOCols; c += 32) {

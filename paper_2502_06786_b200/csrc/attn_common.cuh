@@ -289,7 +289,8 @@ struct Half {
 int paged(const matq_paged_kv* cache, int64_t T, const void* q, int q_heads, int64_t ldq, float scale, float softcap, int64_t window, int64_t max_q, int64_t max_kv,
           void* out, int64_t ldo, void* workspace, size_t workspace_bytes, const Half* half, int32_t* dev_status, void* stream);
 size_t paged_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv, int64_t window, bool half);
-double paged_cost(int64_t T, int batch, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv, int64_t window);       // of the 128-row kernels, ns
+// what the 128-row kernels cost, ns; their query tiles per CTA and parts of the key range
+double paged_cost(int64_t T, int batch, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv, int64_t window, int* tiles = nullptr, int* parts = nullptr);
 // the 128-row kernels on fp16 (attn4_chunk.cu), one or two query tiles per CTA
 int launch_chunk_half(int D, int tiles, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const Params& P, unsigned grid, cudaStream_t s);
 

@@ -149,8 +149,11 @@ size_t matq::attn::paged_workspace_bytes(int64_t T, int batch, int q_heads, int 
     return part_bytes(T, q_heads, head_dim, p.splits);
 }
 
-double matq::attn::paged_cost(int64_t T, int batch, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv, int64_t window) {
-    return plan(T, batch, kv_heads, q_heads / kv_heads, head_dim, max_q, max_kv, window, matq::sm_count(), true).cost;
+double matq::attn::paged_cost(int64_t T, int batch, int q_heads, int kv_heads, int head_dim, int64_t max_q, int64_t max_kv, int64_t window, int* tiles, int* parts) {
+    const Plan p = plan(T, batch, kv_heads, q_heads / kv_heads, head_dim, max_q, max_kv, window, matq::sm_count(), true);
+    if (tiles) *tiles = p.kind;
+    if (parts) *parts = (int)p.splits;
+    return p.cost;
 }
 
 extern "C" size_t matq_attn_paged_workspace_bytes(int64_t T, int batch, int q_heads, int kv_heads, int head_dim,

@@ -568,8 +568,8 @@ int matq_kv4_append(const matq_paged_kv4 *cache, int64_t T, const void *q, int q
 /*
  * (13) As (9) for a cache in 4-bit groups: keys and values are what its codes and groups stand for.  Sequences with up to 16 rows (tokens times heads of a key head)
  *     read the cache as it is.  With more rows, keys and values may be unpacked to fp16 in the workspace first, scaled by powers of two so that fp16's range suffices
- *     (each is off by 2^-12 of itself at most, or by 2^-39 of the largest of its sequence and head); a call does so where it costs less.  Weights are rounded to 11
- *     bits then, and to 8 bits otherwise (8 times two for up to four rows).
+ *     (each is off by 2^-11 of itself at most, or by 2^-39 of the largest of its sequence and head); a call does so where it costs less.  Weights are rounded to 11
+ *     bits then (those below 2^-18 of their row's largest by 2^-29 of it at most), and to 8 bits otherwise (8 times two for up to four rows).
  *   Arguments and errors as for (9), but max_q and max_kv are bounds: a sequence with more new tokens or keys may be refused with MATQ_ERR_PAGE, its outputs
  *   unspecified.  MATQ_ERR_TIMEOUT comes from calls that unpack only.
  *   workspace   at least matq_attn_paged4_workspace_bytes(...) bytes for this call's sizes, 16-byte aligned; contents need not be initialised.  A call that unpacks

@@ -3,7 +3,7 @@
 // Few rows per sequence and key head (single tokens, drafts) go to attn4_decode_kernel, which reads the cache as it is.  Sequences with more rows (chunks) are bound
 // by their products: their keys and values are unpacked once, into the workspace, and the 128-row kernels of matq_attn_paged take them from there.  That is one
 // more pass over what a chunk sees (read 9/16 of a byte an element, written and read 2), where unpacking inside the product kernel would be repeated by every query
-// tile and compete with the softmax for the SM's issue slots.  4096 tokens over 8192 keys, 32/8 heads of 128: 449 us, of which about 20 are the
+// tile and compete with the softmax for the SM's issue slots.  4096 tokens over 8192 keys, 32/8 heads of 128: 453 us, of which about 20 are the
 // maxima, the unpacking and the queries; on a bf16 cache 416.
 //
 // Unpacked to bf16 a key would be rounded to 8 bits once more, and scores with it (with a few large channels outputs were off by 4.6e-3 of their norm, 2.7 times

@@ -100,6 +100,20 @@ __device__ __noinline__ float largest_score(uint32_t addr, int lo, int hi, Score
     }
     return best;
 }
+// The same where every row sees every key.
+template <bool CAP, int COLS>
+__device__ __forceinline__ float largest_of_all(uint32_t addr, const Score& sc) {
+    float best = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < COLS; c += 32) {
+        uint32_t v[32];
+        tc::tmem_ld32(addr + c, v);
+        tc::tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) best = max3(best, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+    }
+    return CAP ? capped(best, sc) : best;
+}
 // Takes a large reference off the scores.
 template <int COLS>
 __device__ __noinline__ void lift_scores(uint32_t addr, float by) {
@@ -115,11 +129,13 @@ __device__ __noinline__ void lift_scores(uint32_t addr, float by) {
     tc::tmem_wait_st();
 }
 
-// HALF: queries, keys and values are fp16, scaled by powers of two (Params::q_scale and the others; see attn4.cu), and so are the weights.  A weight is at most
-// 2^15 then, and the reference moves more often; it is taken 4 higher than it is called, so that scores up to 19 above it fit (with 15, one row in a hundred of a
-// prompt moved its reference once: 4096 tokens over 8192 at 32/8 x 128 26 us longer), and a row takes 0 for its first one only if its largest weight is 2^-6 or
-// more: it and those down to 2^-8 of it keep all their bits.  References from kLarge on are taken as they are.
-constexpr float kFarHalf = 15.f, kNearHalf = 6.f, kShiftHalf = 4.f;
+// HALF: queries, keys and values are fp16, scaled by powers of two (Params::q_scale and the others; see attn4.cu), and so are the weights, whose range has to hold both
+// weights above the reference and what is far below it: a prompt's first key may draw nearly all of a row's weight and leave the rest to thousands.  So a row's
+// first reference is its largest score in the first step that shows it a key, never 0, and stands for a weight of 2^kRoomHalf: weights down to 2^-18 of the largest keep
+// all their bits and the rest are off by 2^-29 of it at most, and scores up to 11 (in exponents of two) above the reference fit.  It is looked up before the first step's
+// pass (4096 tokens over 8192, 32/8 heads of 128, 453 us, 2048 over themselves 67.4; with that pass done twice 455 and 69.6; with 0 for a reference where the scores lie
+// around it 451 and 66.5, but weights below 2^-19 of the largest became zero).  References from kLarge on are taken as they are.
+constexpr float kFarHalf = 15.f, kRoomHalf = 4.f;
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -335,14 +351,14 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (live) score_scale = P.scale * P.q_scale[(q0 + tok) * P.q_heads + h * P.group + r % P.group] * P.k_scale[(int64_t)b * P.kv_heads + h];
                 value_scale = P.v_scale[(int64_t)b * P.kv_heads + h];
             }
-            constexpr float kUp = HALF ? kFarHalf : kFar, kDown = HALF ? kNearHalf : kFar;
-            const auto shift = [](float reference) { return HALF && fabsf(reference) < kLarge ? kShiftHalf : 0.f; };
+            constexpr float kUp = HALF ? kFarHalf : kFar;
+            const auto room = [](float reference) { return HALF && fabsf(reference) < kLarge ? kRoomHalf : 0.f; };
             const Score sc(score_scale, P.softcap);
             const float tanh1 = kShort1 * sc.cap2, tanh2 = kShort2 * sc.cap2, tanh3 = kShort3 * sc.cap2, t_max = P.softcap <= kShortCap ? kTanhMax : -1.f;   // with the cap
-            const float unit = CAP ? 1.f : sc.mul;                      // the reference is kept as a score; with the cap, as an exponent
+            // The reference is kept as a score; with the cap, as an exponent.  (HALF: the factors of a row of zeros and of keys of zero make products of zero, and a unit of
+            // zero would make NaN of a reference of -inf; exponents are the same with the smallest number.)
+            const float unit = CAP ? 1.f : HALF ? fmaxf(sc.mul, 0x1p-126f) : sc.mul;
             float m = -INFINITY, l = 0.f;
-            // The reference as an exponent.  (HALF: the factors of a row of zeros and of keys of zero make a unit of zero, and zero times -inf would be NaN.)
-            const auto exponent = [&](float reference) { return reference == -INFINITY ? reference : reference * unit; };
             bool ok = true;
             int masked_no = 0;
             if (tid == 0) s_any_bad = 0;
@@ -379,6 +395,19 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 float top = -INFINITY, use, off;
                 uint64_t sum2[2];
                 uint32_t pk[C::kCols / 2];
+                // HALF: the first reference, looked up before the first step's pass (rows that it shows no key get theirs as they move one).
+                if (HALF && i == 0) {
+                    if (ok) {
+                        tc::fence_after();
+                        float best = masked ? largest_score<CAP, C::kCols>(s_addr, see_lo - j0 - col0, see_hi - j0 - col0, sc) : largest_of_all<CAP, C::kCols>(s_addr, sc);
+                        if (see_hi >= 0) m = best;
+                    }
+                    if (C::kTiles == 1) {
+                        s_half[part_of][r] = m;
+                        asm volatile("bar.sync 2, %0;" ::"n"(C::kSoft) : "memory");
+                        m = fmaxf(s_half[0][r], s_half[1][r]);
+                    }
+                }
                 // One pass: exponents x = score - reference, their maximum, 2^x, its sum, bf16.  Should x exceed kFar somewhere the reference moves and
                 // the pass is done again; otherwise the maximum costs no second look at the scores.
                 const auto pass = [&](auto hide) {
@@ -447,16 +476,16 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     }
                 };
                 // A row without a reference (m = -inf) takes 0 for one if its largest score is not far from it, as ordinary scores are not: then its first
-                // step is not done twice.  A row with a large one always has its scores looked at once more.
+                // step is not done twice (but see HALF).  A row with a large one always has its scores looked at once more.
                 // (Rows of the tile that stand for no query hold whatever shared memory held: they ask for nothing.)
                 bool lifted = false;
                 const auto wants = [&] {
-                    return ok && see_hi >= 0 && (top > kUp || (m == -INFINITY && top < -kDown && top > -INFINITY) || (!lifted && fabsf(use) >= kLarge));
+                    return ok && see_hi >= 0 && (top > kUp || (m == -INFINITY && (HALF || top < -kFar) && top > -INFINITY) || (!lifted && fabsf(use) >= kLarge));
                 };
                 if (ok) tc::fence_after();
                 for (int attempt = 0; attempt < 3; ++attempt) {         // the second suffices: nothing lies far above a reference that was just moved
                     use = m == -INFINITY ? 0.f : m * unit;
-                    off = (!CAP && lifted && fabsf(use) >= kLarge ? 0.f : -use) - shift(use);
+                    off = (!CAP && lifted && fabsf(use) >= kLarge ? 0.f : -use) + room(use);
                     if (ok) {
                         if (masked) pass(std::true_type{});
                         else pass(std::false_type{});
@@ -477,7 +506,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         if (m == -INFINITY && top > -INFINITY && !raise) m = 0.f;
                         if (__builtin_expect(!__any_sync(0xffffffffu, raise), 1)) break;
                     }
-                    float ref = (use + top) / unit, next = ref * unit;  // the new reference as it is kept, and as an exponent
+                    float ref = (use + (top - room(use))) / unit, next = ref * unit;          // the new reference as it is kept, and as an exponent
                     const bool large = !lifted && raise && (fabsf(use) >= kLarge || fabsf(next) >= kLarge);
                     if (__builtin_expect(C::kTiles == 1 ? soft_any(large) : __any_sync(0xffffffffu, large), 0)) {
                         float best = ok ? largest_score<CAP, C::kCols>(s_addr, see_lo - j0 - col0, see_hi - j0 - col0, sc) : -INFINITY;
@@ -495,7 +524,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         lifted = true;
                     }
                     // O holds the steps before this one.  Their last product is over: with one tile that was waited for, with two the scores' arrival says so.
-                    const float f = raise ? ex2(exponent(m) - next + (shift(exponent(m)) - shift(next))) : 1.f;
+                    const float f = raise ? ex2(m * unit - next + (room(next) - room(m * unit))) : 1.f;
                     if (raise) m = ref;
                     l *= f;
                     if (ok && i > 0) {
@@ -583,7 +612,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
             const float inv = any ? 1.f / l : 0.f;
             if (!ok) *(volatile int*)&s_timeout = 1;
-            if (ok && live && P.splits > 1 && o_col == 0) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(exponent(m) + shift(exponent(m)), l);
+            if (ok && live && P.splits > 1 && o_col == 0) P.part_ml[(int64_t)part * (P.T * P.q_heads) + row] = make_float2(m * unit - room(m * unit), l);
             if (ok && !(P.splits > 1 && n_it == 0)) {
 #pragma unroll 1
                 for (int c = o_col; c < o_col + kOCols; c += 32) {

@@ -309,6 +309,7 @@ inline Plan4 plan4(int64_t T, int batch, int q_heads, int kv_heads, int D, int64
     const int group = q_heads / kv_heads;
     if (max_q > T) max_q = T;
     if (max_kv > kMost) max_kv = kMost;
+    window = window_of(window);
     // Rows of the longest sequence: all of them for the few-row kernel, or unpacking for sequences with more than kMixedRows (a batch of one whatever it has),
     // whichever costs less.
     const int64_t rows = max_q * group;
@@ -445,6 +446,7 @@ extern "C" int matq_attn_paged4(const matq_paged_kv4* cache, int64_t T, const vo
     if (!q || !out || !cache->tiles || !cache->page_table || !cache->cu_q || !cache->kv_len || cache->n_pages == 0) return MATQ_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out) || !aligned16(cache->tiles) || !aligned16(workspace)) return MATQ_ERR_ALIGNMENT;
     const int group = q_heads / cache->kv_heads;
+    window = window_of(window);
     const Plan4 p = recent_plan4(T, cache->batch, q_heads, cache->kv_heads, D, max_q, max_kv, window);
     const double ctas = (double)p.splits * cache->kv_heads * cache->batch * p.tiles_per_seq;
     const int64_t blocks = p.new_pages * (kUnpackPage / kUnpackKeys);

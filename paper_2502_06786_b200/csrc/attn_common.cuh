@@ -280,6 +280,9 @@ inline int launch_join(const Params& P, cudaStream_t s) {
     return MATQ_OK;
 }
 
+// Positions are below 2^31: a window from there on hides no key, and a position less such a window, or the window and a length, need not fit into 64 bits.
+inline int64_t window_of(int64_t window) { return window < (1ll << 31) ? window : 0; }
+
 // Queries (dense rows), keys and values as fp16 and their factors, where a call has them so; and which sequences it serves.
 struct Half {
     const float *q_scale, *k_scale, *v_scale;

@@ -64,6 +64,7 @@ inline Plan plan_kind(int kind, int batch, int kv_heads, int group, int D, int64
 inline Plan plan(int64_t T, int batch, int kv_heads, int group, int D, int64_t max_q, int64_t max_kv, int64_t window, int sms, bool half) {
     if (max_q > T) max_q = T;
     if (max_kv > kMaxKeys) max_kv = kMaxKeys;
+    window = window_of(window);
     const int64_t rows = max_q * group;
     if (rows <= 16 && !half) return plan_kind(rows <= 8 ? 8 : 16, batch, kv_heads, group, D, max_q, max_kv, window, sms);
     const Plan one = plan_kind(1, batch, kv_heads, group, D, max_q, max_kv, window, sms);
@@ -185,7 +186,7 @@ int matq::attn::paged(const matq_paged_kv* cache, int64_t T, const void* q, int 
     Params P;
     P.q = static_cast<const __nv_bfloat16*>(q); P.v = static_cast<const __nv_bfloat16*>(cache->v); P.out = static_cast<__nv_bfloat16*>(out);
     P.table = cache->page_table; P.cu_q = cache->cu_q; P.kv_len = cache->kv_len;
-    P.ldq = ldq; P.ldo = ldo; P.table_stride = cache->table_stride; P.table_width = cache->table_width; P.n_pages = cache->n_pages; P.T = T; P.window = window; P.above_rows = half ? half->above_rows : 0;
+    P.ldq = ldq; P.ldo = ldo; P.table_stride = cache->table_stride; P.table_width = cache->table_width; P.n_pages = cache->n_pages; P.T = T; P.window = window_of(window); P.above_rows = half ? half->above_rows : 0;
     P.batch = cache->batch; P.q_heads = q_heads; P.kv_heads = cache->kv_heads; P.group = group;
     P.page_size = ps; P.page_shift = ps == 16 ? 4 : ps == 32 ? 5 : ps == 64 ? 6 : ps == 128 ? 7 : 8;
     P.tiles_per_seq = (int)p.tiles_per_seq; P.splits = (int)p.splits; P.split_keys = p.split_keys;

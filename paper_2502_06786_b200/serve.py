@@ -59,18 +59,18 @@ class GroupedLinear:
         self.packed, self.params = mq.quantize_groups(W, group)
 
 
-def apply(linears, x):
+def apply(linears, x, dev_status=None):
     """The products of one input [T, K] (bf16) with several matrices: bf16 [T, N] each."""
     T = x.shape[0]
     if isinstance(linears[0], GroupedLinear):
-        return [mq.gemv_groups(l.packed, l.params, x, out_dtype=torch.bfloat16, flags=mq.GEMV_PDL) for l in linears]
+        return [mq.gemv_groups(l.packed, l.params, x, out_dtype=torch.bfloat16, flags=mq.GEMV_PDL, dev_status=dev_status) for l in linears]
     if T <= FEW:
         ys = [torch.empty((T, l.N), dtype=torch.float32, device=x.device) for l in linears]
         mq.gemv_grouped([dict(packed=l.packed, K=l.K, r=l.r, alpha=l.alpha, zero=l.zero, x=x if T > 1 else x[0], y=y if T > 1 else y[0])
-                         for l, y in zip(linears, ys)])
+                         for l, y in zip(linears, ys)], dev_status=dev_status)
         return [y.to(torch.bfloat16) for y in ys]
-    xq, scale, rowsum = mq.quantize_tokens(x)
-    return [mq.gemm_a8(xq, scale, rowsum, l.sliced, l.alpha, l.zero, out_dtype=torch.bfloat16, flags=mq.GEMV_PDL) for l in linears]
+    xq, scale, rowsum = mq.quantize_tokens(x, dev_status=dev_status)
+    return [mq.gemm_a8(xq, scale, rowsum, l.sliced, l.alpha, l.zero, out_dtype=torch.bfloat16, flags=mq.GEMV_PDL, dev_status=dev_status) for l in linears]
 
 
 class PagedCache:
@@ -151,13 +151,13 @@ class Decoder:
         self.cos_sin = torch.cat([angle.cos(), angle.sin()], 1).float().contiguous()
 
     def forward(self, x: torch.Tensor, cache: PagedCache, batch: Batch, dev_status=None) -> torch.Tensor:
-        """x: bf16 [T, hidden], the new tokens of the batch's sequences one after another.  Returns bf16 [T, hidden]."""
+        """x: bf16 [T, hidden], the new tokens of the batch's sequences one after another.  Returns bf16 [T, hidden]; errors that the GPU finds go to dev_status (int32)."""
         cfg, T = self.cfg, x.shape[0]
         if batch.max_kv > cfg.max_pos:
             raise ValueError(f"a sequence of {batch.max_kv} tokens passes the {cfg.max_pos} positions of the rotation table")
         paged = (batch.page_table, batch.cu_q, batch.kv_len)
         for i, l in enumerate(self.layers):
-            q, k, v = apply([l["q"], l["k"], l["v"]], rms_norm(x))
+            q, k, v = apply([l["q"], l["k"], l["v"]], rms_norm(x), dev_status)
             q, k, v = (t.view(T, -1, cfg.head_dim) for t in (q, k, v))
             if cfg.cache_bits == 4:
                 mq.kv4_append(cache.tiles[i], *paged, k, v, cos_sin=self.cos_sin, q=q, q_out=q, dev_status=dev_status)
@@ -165,9 +165,9 @@ class Decoder:
             else:
                 mq.kv_append(cache.k[i], cache.v[i], *paged, k, v, cos_sin=self.cos_sin, q=q, q_out=q, dev_status=dev_status)
                 a = mq.attn_paged(q, cache.k[i], cache.v[i], *paged, batch.max_q, batch.max_kv, softcap=cfg.softcap, window=cfg.window, dev_status=dev_status)
-            x = x + apply([l["o"]], a.view(T, -1))[0]
-            gate, up = apply([l["gate"], l["up"]], rms_norm(x))
-            x = x + apply([l["down"]], torch.nn.functional.silu(gate) * up)[0]
+            x = x + apply([l["o"]], a.view(T, -1), dev_status)[0]
+            gate, up = apply([l["gate"], l["up"]], rms_norm(x), dev_status)
+            x = x + apply([l["down"]], torch.nn.functional.silu(gate) * up, dev_status)[0]
         return x
 
 

@@ -282,8 +282,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_groups_kernel(const __grid_c
                     if (++xs == kSlots) { xs = 0; xphase ^= 1u; }
                 }
             }
-            // what frees the last slots arrives from the other CTA: it is waited for, so that it meets no CTA that has ended
-            for (int i = 0; PAIR && i < kSlots && ok; ++i) {
+            // What frees the last slots is waited for: no copy and no product may be in flight when the CTA ends, whatever became of the warps that wait for them, and in a
+            // pair it arrives from the other CTA.  (A wait that ran out above or here lasted longer than any copy takes.)
+            for (int i = 0; i < kSlots && ok; ++i) {
                 ok = tc::mbar_wait(tc::smem_u32(&s_empty[xs]), xphase, P.wait_cycles);
                 if (++xs == kSlots) { xs = 0; xphase ^= 1u; }
             }
@@ -480,7 +481,6 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_groups_kernel(const __grid_c
         }
         if (!ok) *(volatile int*)&s_timeout = 1;
     }
-    // The copies are over by then: the products consumed them all, or their waits ran out first.
     __syncwarp();
     tc::fence_before();
     __syncthreads();

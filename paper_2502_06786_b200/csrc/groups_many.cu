@@ -157,21 +157,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* v) {
                    "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
                    "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
 }
-// tc::mbar_wait by a whole warp, with a hint that lets the warp sleep until the barrier's phase ends: eighteen warps that poll take the issue slots of those that convert.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, long long limit) {
-    uint32_t done = 0;
-    long long t0 = 0;
-    while (!done) {
-        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p; }"
-                     : "=r"(done) : "r"(bar), "r"(parity), "r"(20000u) : "memory");             // ns
-        if (!done) {
-            const long long now = clock64();
-            if (t0 == 0) t0 = now;
-            else if (now - t0 > limit) break;
-        }
-    }
-    return __all_sync(0xffffffffu, done != 0);
-}
 // Eight codes as fp16 times scale: (code - 8) scale, exact.  1024 + n is the number with the bits of n below 1024's.
 __device__ __forceinline__ void weights_of(uint32_t w, __half2 scale, uint32_t* o) {
     const auto number = [](uint32_t bits) { return *reinterpret_cast<const __half2*>(&bits); };
@@ -299,10 +284,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_groups_kernel(const __grid_c
         for (int tile = first_tile; tile < tiles && ok && row_part == 0; tile += step)
             for (int i0 = 0; i0 < blocks && ok; i0 += PAIR ? blocks : kSegment, ++round) {
                 const int a = PAIR ? 0 : round & 1, n = PAIR ? blocks : min(kSegment, blocks - i0);
-                ok = warp_wait(tc::smem_u32(&s_read[a]), ((uint32_t)(PAIR ? round : round >> 1) & 1u) ^ 1u, P.wait_cycles);
+                ok = tc::warp_wait(tc::smem_u32(&s_read[a]), ((uint32_t)(PAIR ? round : round >> 1) & 1u) ^ 1u, P.wait_cycles);
                 tc::fence_after();
                 for (int i = 0; i < n && ok; ++i) {
-                    if (!(ok = warp_wait(tc::smem_u32(&s_full[slot]), phase, P.wait_cycles))) break;
+                    if (!(ok = tc::warp_wait(tc::smem_u32(&s_full[slot]), phase, P.wait_cycles))) break;
                     tc::fence_after();
                     const uint64_t at = desc0 + (uint64_t)(slot * (token_bytes >> 4));
                     // tensor memory is this CTA's as a whole: its first column is column 0, and the addresses need no register that differs between threads
@@ -331,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_groups_kernel(const __grid_c
             const auto put = [&](int i, int part, const uint32_t* v) { tmem_st32(slots + lanes + ((u0 + i - b_lo) % kSlots) * 64 + part * 32, v); };
             const auto slot_free = [&](int i) {
                 const int u = u0 + i - b_lo;
-                const bool f = warp_wait(tc::smem_u32(&s_empty[u % kSlots]), ((uint32_t)(u / kSlots) & 1u) ^ 1u, P.wait_cycles);
+                const bool f = tc::warp_wait(tc::smem_u32(&s_empty[u % kSlots]), ((uint32_t)(u / kSlots) & 1u) ^ 1u, P.wait_cycles);
                 tc::fence_after();
                 return f;
             };
@@ -349,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_groups_kernel(const __grid_c
                 uint32_t now[S];
 #pragma unroll
                 for (int s = 0; s < S; ++s) { now[s] = next[s]; next[s] = group((i + 2) * S + s); }
-                if (!(ok = warp_wait(tc::smem_u32(&s_cfull[cs]), cphase, P.wait_cycles))) break;
+                if (!(ok = tc::warp_wait(tc::smem_u32(&s_cfull[cs]), cphase, P.wait_cycles))) break;
                 uint4 w[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const uint4*>(codes + cs * kCodeStage + row * 128 + (((set * 4 + k) ^ (row & 7)) * 16));
@@ -411,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_groups_kernel(const __grid_c
             if (tid < kTokens) s_exp[turn][tid] = tid < cols ? P.token_exp[m0 + tid] : 0;
             asm volatile("bar.sync 1, 256;" ::: "memory");
             if constexpr (PAIR) {                                       // bf16 outputs, straight from tensor memory
-                if (ok) ok = warp_wait(tc::smem_u32(&s_acc[0]), (uint32_t)round & 1u, P.wait_cycles);
+                if (ok) ok = tc::warp_wait(tc::smem_u32(&s_acc[0]), (uint32_t)round & 1u, P.wait_cycles);
                 ++round;
                 if (ok) {
                     tc::fence_after();
@@ -440,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_groups_kernel(const __grid_c
                     for (int c = 0; c < 16; ++c) sum[p][c] = 0.f;
                 for (int i0 = 0; i0 < blocks; i0 += kSegment, ++round) {
                     const int a = round & 1;
-                    if (ok) ok = warp_wait(tc::smem_u32(&s_acc[a]), (uint32_t)(round >> 1) & 1u, P.wait_cycles);
+                    if (ok) ok = tc::warp_wait(tc::smem_u32(&s_acc[a]), (uint32_t)(round >> 1) & 1u, P.wait_cycles);
                     if (ok) {
                         tc::fence_after();
 #pragma unroll

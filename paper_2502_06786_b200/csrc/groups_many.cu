@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kPrepThreads) gemm_groups_prepare_kernel(const
         for (int j = 0; j < kEach; ++j) {
             const int64_t n = n0 + warp * kEach + j;
             const uint32_t g = n < P.N ? P.params[n * P.groups + i] : 0u;
-            const float most = fminf(fmaxf(fabsf(low_of(g)), 8.f * scale_of(g)), 3.402823466e38f);
+            const float most = fminf(fmaxf(fabsf(low_of(g)), 8.f * fabsf(scale_of(g))), 3.402823466e38f);
             if (scale_of(g) == scale_of(g)) top[j] = max(top[j], __float_as_uint(most));         // not of a group that stands for NaN
         }
 #pragma unroll

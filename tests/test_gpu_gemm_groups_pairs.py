@@ -85,3 +85,19 @@ def test_same_bits_again_in_a_graph_and_after_a_stall():
     finally:
         assert mq.serving_test_stall(0) == 1
     assert torch.equal(mq.gemm_groups(*args, y=y, workspace=ws), want)
+
+
+@pytest.mark.parametrize("M,N,K,group", [(450, 4885, 544, 32), (200, 9547, 576, 64), (130, 9547, 640, 128)])
+def test_groups_and_activations_of_any_size(M, N, K, group):
+    rng = np.random.default_rng(5)
+    codes, params, x = _case(M, N, K, group, 3)
+    n = (N, K // group)
+    params[:, :, 0] = gr.bf16_bits((2.0 ** rng.integers(-60, 60, n)).astype(np.float32))
+    params[:, :, 1] = gr.bf16_bits((2.0 ** rng.integers(-60, 60, n) * rng.choice([-1, 1], n)).astype(np.float32))
+    params[7] = 0
+    y = _run(codes, params, x)
+    assert bool((y[:, 7] == 0).all())
+    _check(y, codes, params, x)
+    codes, params, x = _case(M, N, K, group, 4)
+    x = (x.double() * 2.0 ** torch.from_numpy(rng.integers(-100, 100, (M, 1))).double()).to(torch.bfloat16)      # each token by its own
+    _check(_run(codes, params, x), codes, params, x)

@@ -527,7 +527,8 @@ int matq_gemv_groups_plan(int64_t M, int64_t N, int64_t K, int group, int *token
  *   then unspecified.
  */
 size_t matq_gemm_groups_workspace_bytes(int64_t M, int64_t N, int64_t K, int group);
-/* 1 for sizes at which (11b) takes less time than (11), as far as measured; host only. */
+/* 1 for sizes from which on (11b) is the call for a prompt: more than 32 tokens, or more than 16 with 2^25 weights or more; host only.  For up to 256 tokens (11) takes up to
+   10 us less with small matrices (below about 2^24 weights) and with few rows. */
 int matq_gemm_groups_pays(int64_t M, int64_t N, int64_t K, int group);
 /* How (11b) shares out these sizes on the current device (host only, launches nothing): whether pairs of SMs share a tile, the tokens of a tile, and the CTAs that share K.
    M, N >= 1; MATQ_ERR_INVALID_ARG, MATQ_ERR_UNSUPPORTED or MATQ_ERR_SHAPE for sizes that (11b) would refuse.  Any of the pointers may be NULL. */

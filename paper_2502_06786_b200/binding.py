@@ -557,7 +557,7 @@ def quantize_groups(W, group=128, packed=None, params=None, dev_status=None):
 
 
 def gemv_groups(packed, params, x, y=None, out_dtype=torch.float32, flags=0, workspace=None, dev_status=None):
-    """matq_gemv_groups, or matq_gemm_groups for the numbers of tokens at which that takes less time (``gemm_groups_pays``).  packed, params: as returned by
+    """matq_gemv_groups, or matq_gemm_groups for the numbers of tokens of a prompt (``gemm_groups_pays``).  packed, params: as returned by
     quantize_groups; x: bf16 [M, K].  Returns y [M, N], fp32 or bf16 (the type of ``y`` when it is given, ``out_dtype`` otherwise).  ``workspace`` and ``dev_status`` are for
     the second."""
     if y is None:

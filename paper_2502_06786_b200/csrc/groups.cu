@@ -76,8 +76,8 @@ cudaError_t launch_quantize(const void* W, int64_t N, int64_t K, int64_t ldw, vo
 // that part, block by block of 128.  Each warp brings its own blocks into its own ring by cp.async, across the ends of steps, so that the ring never drains.
 // The CTAs of a cluster share K and add their sums through distributed shared memory.  All sums are taken in a fixed order.
 //
-// Bound: one token, the chain of a launch (start, tokens' trip to memory, staging, the last blocks' trip, sums): 9216 x 2304 5.2 us, 14336 x 4096 10.5, 65536 x 2304 (a step
-// of every CTA follows another) 19.7 us or 4.3 TB/s.  16 tokens: latencies of 16 warps (1.9 instructions a cycle) and the cluster's sums: 3584 x 14336 18.0 us.
+// Bound: one token, the chain of a launch (start, tokens' trip to memory, staging, the last blocks' trip, sums): 9216 x 2304 5.2 us, 14336 x 4096 10.5, 65536 x 2304 (a second
+// step for 216 of 296 CTAs) 18.9 us or 4.5 TB/s.  16 tokens: latencies of 16 warps (1.9 instructions a cycle) and the cluster's sums: 3584 x 14336 18.0 us.
 constexpr int kBlock = 128;
 // Warps of a CTA: eight, and two CTAs on an SM, as long as a CTA has one block of columns; sixteen beside tokens that take more shared memory.
 __host__ __device__ constexpr int warps_of(int nt) { return nt == 1 ? 8 : 16; }

@@ -13,8 +13,9 @@
 // 256 tokens, so that a block that was converted meets twice the tokens (4096 tokens x 14336 x 4096, groups of 128, 388 us or 1.24 PFLOP/s, with single CTAs 481).
 //
 // Bound: the converting warps, about 1000 cycles for a block of 128 x 128 weights, whose products take 4 cycles a token, and the hand-overs around them (without any
-// one of conversion, copies of codes, stores to tensor memory or products a block takes 3 to 13 % less; three sets of four converting warps instead of two are no faster).
-// 64 tokens x 14336 x 4096 26.5 us, of which the first kernel, the start and the end take 12 (matq_gemv_groups: 62 us); 1024 tokens 122 us (791).
+// one of conversion, copies of codes, stores to tensor memory or products a block takes 3 to 13 % less; three sets of four converting warps instead of two are no faster);
+// beside that whole rounds: 1024 tokens x 14336 rows are 224 tiles for 74 pairs, of which the fourth round has two.
+// 64 tokens x 14336 x 4096 27 us, of which the first kernel, the start and the end take 12 (matq_gemv_groups: 61 us); 1024 tokens 121 us (794).
 #include <cuda_fp16.h>
 
 #include "group4.cuh"
@@ -157,7 +158,8 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* v) {
                    "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
                    "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
 }
-// Eight codes as fp16 times scale: (code - 8) scale, exact.  1024 + n is the number with the bits of n below 1024's.
+// Eight codes as fp16 times scale: (code - 8) scale, exact.  1024 + n is the number with the bits of n below 1024's (a published way from integers to fp16: Kim et al. 2022,
+// "Who Says Elephants Can't Run").
 __device__ __forceinline__ void weights_of(uint32_t w, __half2 scale, uint32_t* o) {
     const auto number = [](uint32_t bits) { return *reinterpret_cast<const __half2*>(&bits); };
     const __half2 up = __floats2half2_rn(-1032.f, -1032.f), part = __floats2half2_rn(0.0625f, 0.0625f), less = __floats2half2_rn(-72.f, -72.f);
@@ -571,8 +573,10 @@ int launch(const CUtensorMap& tw, const CUtensorMap& tx, const Params& P, unsign
 }  // namespace grpm
 }  // namespace matq
 
-// From 33 tokens on it takes less time than matq_gemv_groups (2304 x 2304, 48 tokens 11.8 and 10.4 us, 256 tokens 18.6 and 18.7; 4096 x 4096, 48 tokens 15.6 and 20.4), with
-// large matrices from 17 on (14336 x 4096, 24 tokens 25.0 and 29.2; 4096 x 4096 14.6 and 13.8), where its two launches weigh less.
+// From 33 tokens on, with large matrices from 17 on, where its two launches weigh less.  us, and matq_gemv_groups', groups of 128: 14336 x 4096, 24 tokens 26.1 and 28.5, 64
+// tokens 27.5 and 61.3; 4096 x 4096, 48 tokens 18.0 and 22.6; 2304 x 2304, 256 tokens 18.6 and 18.7.  The rule weighs tokens before the matrix: small matrices and few rows
+// take less time with matq_gemv_groups for up to 256 tokens (1024 x 1024, 48 tokens 11.0 and 4.8, 256 tokens 14.8 and 7.4; 2304 x 2304, 48 tokens 11.2 and 9.5; 300 x 14336,
+// 64 tokens 18.9 and 12.4; 4096 x 1024, 128 tokens 15.2 and 10.3).
 extern "C" int matq_gemm_groups_pays(int64_t M, int64_t N, int64_t K, int group) {
     using namespace matq::grpm;
     return sizes_ok(M, N, K, group) && (M > 32 || (M > 16 && (double)N * K >= (double)(1 << 25)));

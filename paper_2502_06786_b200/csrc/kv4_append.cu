@@ -4,7 +4,8 @@
 // but a thread's place is eight neighbouring elements, which is what it quantises: with halves as pairs it reads its eight partners beside them (from L1, where
 // the thread that owns them has brought them), and the eight lanes of a group exchange its ends.
 //
-// Bound: few tokens, a launch and two dependent look-ups; prompts, HBM and the instructions of the rotation and the quantiser about alike (4.0 TB/s with 64 threads a token).
+// Bound: few tokens, a launch and two dependent look-ups; prompts, each token's chain of look-ups (sequence, length, page, angles), which 40 % of an SM's warps hide in part
+// (64 registers a thread; 57 % of the issue slots used; 4.0 TB/s with 64 threads a token).
 #include "kv4_cache.cuh"
 
 namespace matq {
